@@ -20,6 +20,9 @@
  *   lethe_segment_prune      Algorithm 1 itself: segmented breakpoint search, retention
  *                            set and eviction-threshold update (Sec. 4.2)
  *   lethe_collapsed_prune    retention by the head- and batch-collapsed score of Eq. 2
+ *   lethe_chunk_attend       a step of several new tokens per sequence (chunks of prompts, drafted tokens, mixed
+ *                            batches), also with modified scores
+ *   lethe_rotate             rotary positions with several axes for the queries and keys of such a step
  *
  * General conventions
  *   - Unless marked HOST, every pointer is a DEVICE pointer to memory owned by the
@@ -314,6 +317,91 @@ lethe_status lethe_collapsed_prune(lethe_ctx *ctx, const lethe_cache *cache, con
  */
 lethe_status lethe_prefill_seed(lethe_ctx *ctx, const lethe_cache *cache, const void *q_prompt, int32_t prompt_len,
                                 const float *scale, float gamma, void *stream);
+
+/*
+ * Score modification of a chunk's attention (models whose attention is not the plain softmax).  All tests are on
+ * ORIGINAL positions — token_pos of a query, pos[] of a key — because in a pruned cache a slot number says nothing
+ * about distance.  With x = scale * q_ih . K_j of a new token i (query head h of the model) and a slot j:
+ *   softcap > 0 : x <- softcap * tanh(x / softcap)
+ *   slopes      : x <- x - slopes[h] * |token_pos[i] - pos[j]|
+ *   prefix_len  : slots with pos[j] < prefix_len[b] are visible to every token of sequence b, also to earlier ones
+ *                 (the tokens of an image or of a prompt that is read both ways); all others causally
+ *   window > 0  : of these only slots with token_pos[i] - pos[j] < window
+ *   doc_start   : of these only slots with pos[j] >= doc_start[i] (packed documents: where token i's document begins)
+ * A token that no slot is visible to gets out = 0, lse = -inf and adds nothing to the relevance.
+ */
+typedef struct {
+    float softcap;             /* 0 = off; finite, >= 0                        */
+    int32_t window;            /* 0 = off; >= 0                                */
+    const float *slopes;       /* DEVICE [Hq] or NULL                          */
+    const int32_t *doc_start;  /* DEVICE [n_tokens] or NULL                    */
+    const int32_t *prefix_len; /* DEVICE [B] or NULL                           */
+} lethe_score_mod;
+
+/*
+ * Rotary positions with several axes (a token of an image or a video has a time, a height and a width).  The first
+ * rot_dim elements of a row form rot_dim / 2 pairs; pair p turns by the angle axis_pos[pair_axis[p]][token] *
+ * pair_freq[p]:  (a, b) -> (a cos - b sin, a sin + b cos); the elements from rot_dim on are copied.  An angle is
+ * the position times the frequency in turns (a 64-bit fraction), taken modulo one turn before it is rounded to fp32: far
+ * positions lose nothing, an angle is off by at most 2^-23 radians at any position.
+ */
+enum { LETHE_ROT_HALVES = 0, LETHE_ROT_PAIRS = 1 };
+typedef struct {
+    int32_t rot_dim;          /* even, 2 .. head_dim                                                          */
+    int32_t style;            /* LETHE_ROT_HALVES: pair p = elements (p, p + rot_dim / 2); LETHE_ROT_PAIRS: (2p, 2p + 1) */
+    int32_t n_axes;           /* 1 .. 4                                                                       */
+    const int32_t *pair_axis; /* HOST [rot_dim / 2], 0 .. n_axes - 1                                          */
+    const double *pair_freq;  /* HOST [rot_dim / 2], radians per position, at most 2 pi either way                    */
+    const int32_t *axis_pos;  /* DEVICE [n_axes][n_tokens], any int32                                         */
+} lethe_rotary;
+
+/*
+ * Rotate the queries and keys of n_tokens tokens (what a model does between its projections and the calls that
+ * append to the cache: the cache holds rotated keys, and pruning never turns them again).
+ *   dtype LETHE_F32 or LETHE_BF16; head_dim 64 or 128
+ *   q     [nl][n_tokens][Hq][D]  -> q_out      k  [nl][n_tokens][Hkv][D] -> k_out
+ * k and k_out may both be NULL (n_kv_heads is then ignored).  An output may be its own input (in place) but must
+ * not overlap anything else.  inverse != 0 turns backwards: the inverse, and the gradient of the forward call.
+ * Arithmetic in fp32, one rounding to the output type.  n_tokens = 0 does nothing.
+ */
+lethe_status lethe_rotate(lethe_ctx *ctx, const lethe_rotary *rotary, int32_t dtype, int32_t head_dim, int n_layers,
+                          int n_tokens, int n_q_heads, int n_kv_heads, const void *q, const void *k, int32_t inverse,
+                          void *q_out, void *k_out, void *stream);
+
+/*
+ * One step of SEVERAL new tokens per sequence for layers [layer_begin, layer_end): a chunk of a prompt, drafted
+ * tokens to verify, or a batch that mixes prompts and single tokens.  The tokens of all sequences are packed:
+ *   chunk_start [B+1] int32 (DEVICE)  tokens chunk_start[b] .. chunk_start[b+1]-1 are sequence b's, in order; T_b
+ *                                     of them, T_b = 0 leaves the sequence as it is
+ *   n_tokens                          rows of the packed arrays (rows before chunk_start[0] and from chunk_start[B]
+ *                                     on are never touched); 0: the call does nothing
+ *   max_chunk                         an upper bound of all T_b, at least 1 (sizes the launch; the tighter the better)
+ *   q      [nl][n_tokens][Hq][D]      k_new, v_new [nl][n_tokens][Hkv][D] (both NULL: attend without appending)
+ *   token_pos [n_tokens] int32        original positions (may be NULL when nothing is appended and `mod` has neither
+ *                                     slopes nor a window)
+ *   scale HOST float[L], gamma        as in lethe_decode_attend; gamma is a double here because its powers run to T:
+ *                                     fp32's 0.99 is off by 1e-8, which a hundred steps turn into 1e-6
+ *   mod                               NULL: plain attention
+ *   rotary                            NULL: q and k_new come rotated; else they are rotated on the way in, exactly as
+ *                                     by lethe_rotate
+ *   out    [nl][n_tokens][Hq][D]      lse [nl][n_tokens][Hq] fp32, optional
+ * Per item with n = len and T = T_b: the new rows go to slots n .. n+T-1 (pos = token_pos), len = n + T; token i
+ * attends over slots 0 .. n+i (without appending: 0 .. n-1), and
+ *   rel[j] = gamma^T rel[j] + sum_{i < T} gamma^(T-1-i) sum_{h in group} p_ihj      (rel of the new slots starts at 0)
+ * which is what T calls of lethe_decode_attend would leave.  Sums, softmax statistics and outputs are accumulated in
+ * fp32; the tensor-core kernels (bf16 and byte caches) round the probabilities of the output product to bf16.
+ * An item that cannot take all T tokens (len + T > cap_tokens) is left untouched, its out rows are zero-filled (lse =
+ * -inf) and LETHE_ERR_CAPACITY is recorded.  A page id outside the pool reads as zero rows and records LETHE_ERR_PAGE.
+ * If chunk_start decreases anywhere, leaves [0, n_tokens] or has a T_b above max_chunk, the call does nothing and records
+ * LETHE_ERR_INVALID_ARG.  Slots at or beyond len may hold anything.  A NaN or an infinity in a value row that some
+ * token of the chunk sees may reach the other tokens of its sequence too.
+ * Scratch: 8 bytes per (layer, token, query head), and up to about 80 MB of partial results.
+ */
+lethe_status lethe_chunk_attend(lethe_ctx *ctx, const lethe_cache *cache, int layer_begin, int layer_end,
+                                const int32_t *chunk_start, int n_tokens, int max_chunk, const void *q,
+                                const void *k_new, const void *v_new, const int32_t *token_pos, const float *scale,
+                                double gamma, const lethe_score_mod *mod, const lethe_rotary *rotary, void *out, float *lse,
+                                void *stream);
 
 /*
  * lethe_rasr_prune without a context and without any allocation.  (The paper has no counterpart: this entry

@@ -24,7 +24,7 @@ VARIANT_AUTO, VARIANT_SIMT, VARIANT_MMA4, VARIANT_MMA8 = 0, 1, 2, 3
 EXPORTS = ["lethe_create", "lethe_destroy", "lethe_last_error", "lethe_poll_status", "lethe_set_tuning", "lethe_set_wait_limit",
            "lethe_decode_attend", "lethe_decode_attend_host", "lethe_estimate_sparsity", "lethe_alloc_budgets",
            "lethe_rasr_prune", "lethe_rasr_prune_static", "lethe_segment_prune", "lethe_prefill_seed",
-           "lethe_collapsed_prune"]
+           "lethe_collapsed_prune", "lethe_chunk_attend", "lethe_rotate"]
 
 
 class LetheError(RuntimeError):
@@ -42,6 +42,17 @@ class lethe_cache(ctypes.Structure):
         ("len", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
         ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
     ]
+
+
+class lethe_score_mod(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
+                ("doc_start", ctypes.c_void_p), ("prefix_len", ctypes.c_void_p)]
+
+
+class lethe_rotary(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("style", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("pair_axis", ctypes.POINTER(ctypes.c_int32)), ("pair_freq", ctypes.POINTER(ctypes.c_double)),
+                ("axis_pos", ctypes.c_void_p)]
 
 
 _lib = None
@@ -87,6 +98,13 @@ def load() -> ctypes.CDLL:
     lib.lethe_segment_prune.argtypes = [vp, cp, i32, ctypes.c_float, i32, i32, vp, vp, i32, vp]
     lib.lethe_prefill_seed.restype = ctypes.c_int
     lib.lethe_prefill_seed.argtypes = [vp, cp, vp, i32, ctypes.POINTER(ctypes.c_float), ctypes.c_float, vp]
+    lib.lethe_chunk_attend.restype = ctypes.c_int
+    lib.lethe_chunk_attend.argtypes = [vp, cp, ctypes.c_int, ctypes.c_int, vp, ctypes.c_int, ctypes.c_int, vp, vp, vp, vp,
+                                       ctypes.POINTER(ctypes.c_float), ctypes.c_double, ctypes.POINTER(lethe_score_mod),
+                                       ctypes.POINTER(lethe_rotary), vp, vp, vp]
+    lib.lethe_rotate.restype = ctypes.c_int
+    lib.lethe_rotate.argtypes = [vp, ctypes.POINTER(lethe_rotary), i32, i32, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                 ctypes.c_int, vp, vp, i32, vp, vp, vp]
     lib.lethe_rasr_prune_static.restype = ctypes.c_int
     lib.lethe_rasr_prune_static.argtypes = [cp, vp, i32, i32, vp, i32, vp, vp]
     _lib = lib
@@ -153,6 +171,41 @@ class Cache:
     @property
     def cap_tokens(self) -> int:
         return self.capacity * self.page_tokens if self.page_table is not None else self.capacity
+
+
+class ScoreMod:
+    """lethe_score_mod: softcap, window, and device tensors slopes [Hq] fp32, doc_start [n_tokens] int32, prefix_len [B] int32
+    (each may be None).  The tensors stay owned here."""
+
+    def __init__(self, softcap: float = 0.0, window: int = 0, slopes: Optional[torch.Tensor] = None,
+                 doc_start: Optional[torch.Tensor] = None, prefix_len: Optional[torch.Tensor] = None):
+        self.slopes, self.doc_start, self.prefix_len = slopes, doc_start, prefix_len
+        for t, dt in ((slopes, torch.float32), (doc_start, torch.int32), (prefix_len, torch.int32)):
+            assert t is None or (t.is_cuda and t.is_contiguous() and t.dim() == 1 and t.dtype == dt)
+        ptr = [None if t is None else t.data_ptr() for t in (slopes, doc_start, prefix_len)]
+        self.c = lethe_score_mod(float(softcap), int(window), *ptr)
+
+
+ROT_HALVES, ROT_PAIRS = 0, 1
+
+
+class Rotary:
+    """lethe_rotary: pair_axis and pair_freq (one entry per pair; host sequences) and axis_pos, a device int32 tensor
+    [n_axes][n_tokens].  The rotated part of a row is twice as long as pair_axis."""
+
+    def __init__(self, pair_axis: Sequence[int], pair_freq: Sequence[float], axis_pos: torch.Tensor, style: int = ROT_HALVES):
+        assert len(pair_axis) == len(pair_freq)
+        assert axis_pos.is_cuda and axis_pos.is_contiguous() and axis_pos.dim() == 2 and axis_pos.dtype == torch.int32
+        n = len(pair_axis)
+        self.axis_pos = axis_pos
+        self.pair_axis = (ctypes.c_int32 * n)(*[int(x) for x in pair_axis])
+        self.pair_freq = (ctypes.c_double * n)(*[float(x) for x in pair_freq])
+        self.c = lethe_rotary(2 * n, int(style), axis_pos.shape[0], ctypes.cast(self.pair_axis, ctypes.POINTER(ctypes.c_int32)),
+                              ctypes.cast(self.pair_freq, ctypes.POINTER(ctypes.c_double)), axis_pos.data_ptr())
+
+    @property
+    def n_tokens(self) -> int:
+        return self.axis_pos.shape[1]
 
 
 def rasr_prune_static(cache: "Cache", budgets: torch.Tensor, recent: int, sink: int,
@@ -285,3 +338,43 @@ class Context:
         assert q_prompt.is_cuda and q_prompt.is_contiguous() and q_prompt.dim() == 5
         self._check(self.lib.lethe_prefill_seed(self.h, ctypes.byref(cache.c), _dp(q_prompt), q_prompt.shape[2],
                                                 self._scale(scale), gamma, _stream(self.device)))
+
+    def rotate(self, rotary: Rotary, q: torch.Tensor, k: Optional[torch.Tensor], q_out: torch.Tensor,
+               k_out: Optional[torch.Tensor], inverse: bool = False):
+        """q [nl][n_tokens][Hq][D] and k [nl][n_tokens][Hkv][D] (or None), float32 or bfloat16, into q_out, k_out (which may be
+        q, k themselves)."""
+        for x, y in ((q, q_out), (k, k_out)):
+            assert (x is None) == (y is None)
+            assert x is None or (x.is_cuda and y.is_cuda and x.is_contiguous() and y.is_contiguous() and x.dim() == 4 and x.shape == y.shape)
+            assert x is None or (x.dtype == y.dtype == q.dtype and x.shape[:2] == q.shape[:2] and x.shape[3] == q.shape[3])
+        assert rotary.n_tokens == q.shape[1]
+        dt = {torch.float32: F32, torch.bfloat16: BF16}[q.dtype]
+        self._check(self.lib.lethe_rotate(self.h, ctypes.byref(rotary.c), dt, q.shape[3], q.shape[0], q.shape[1], q.shape[2],
+                                          0 if k is None else k.shape[2], _dp(q), _dp(k), int(bool(inverse)), _dp(q_out),
+                                          _dp(k_out), _stream(self.device)))
+
+    def chunk_attend(self, cache: Cache, layer_begin: int, layer_end: int, chunk_start: torch.Tensor, max_chunk: int, q, k_new,
+                     v_new, token_pos, scale, gamma, out, lse=None, mod: Optional[ScoreMod] = None,
+                     rotary: Optional[Rotary] = None, scale_c=None):
+        """q, out [nl][n_tokens][Hq][D]; k_new, v_new [nl][n_tokens][Hkv][D] or None; chunk_start [B + 1] int32 and token_pos
+        [n_tokens] int32 on the device; lse [nl][n_tokens][Hq] float32 or None.  All contiguous."""
+        nl, n_tokens = layer_end - layer_begin, q.shape[1]
+        act, head = cache.act_dtype, (cache.n_q_heads, cache.head_dim)
+        assert chunk_start.is_cuda and chunk_start.is_contiguous() and chunk_start.dtype == torch.int32 and chunk_start.numel() == cache.batch + 1
+        for t in (q, out):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == act and tuple(t.shape) == (nl, n_tokens) + head
+        for t in (k_new, v_new):
+            assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == act and tuple(t.shape) == (nl, n_tokens, cache.n_kv_heads, cache.head_dim))
+        assert token_pos is None or (token_pos.is_cuda and token_pos.is_contiguous() and token_pos.dtype == torch.int32 and token_pos.numel() == n_tokens)
+        assert lse is None or (lse.is_cuda and lse.is_contiguous() and lse.dtype == torch.float32 and tuple(lse.shape) == (nl, n_tokens, cache.n_q_heads))
+        if mod is not None:
+            assert mod.slopes is None or mod.slopes.numel() == cache.n_q_heads
+            assert mod.doc_start is None or mod.doc_start.numel() == n_tokens
+            assert mod.prefix_len is None or mod.prefix_len.numel() == cache.batch
+        assert rotary is None or rotary.n_tokens == n_tokens
+        sc = scale_c if scale_c is not None else self._scale(scale)
+        self._check(self.lib.lethe_chunk_attend(self.h, ctypes.byref(cache.c), layer_begin, layer_end, _dp(chunk_start), n_tokens,
+                                                max_chunk, _dp(q), _dp(k_new), _dp(v_new), _dp(token_pos), sc, gamma,
+                                                None if mod is None else ctypes.byref(mod.c),
+                                                None if rotary is None else ctypes.byref(rotary.c), _dp(out), _dp(lse),
+                                                _stream(self.device)))

@@ -7,6 +7,8 @@
 
 #include "common.cuh"
 #include "prefill.cuh"
+#include "chunk.cuh"
+#include "rotate.cuh"
 
 namespace lethe {
 cudaError_t launch_attend_simt(const AttendArgs& a, int dtype, int D, bool paged, cudaStream_t stream);
@@ -1020,6 +1022,175 @@ lethe_status lethe_prefill_seed(lethe_ctx* ctx, const lethe_cache* c, const void
         e = launch_prefill_tc(a, items, c->n_layers, c->head_dim, ctx->tma_encode, allow_tma, (cudaStream_t)stream);
     }
     if (e != cudaSuccess) return cuda_fail(ctx, e, "prefill_seed launch");
+    return LETHE_OK;
+}
+
+// Checks of a rotary description, and its kernel arguments (everything but the tensors).
+static lethe_status rotary_args(lethe_ctx* ctx, const lethe_rotary* r, int32_t dtype, int32_t head_dim, int nl, int n_tokens, int Hq,
+                                int Hkv, int inverse, RotateArgs* a) {
+    if (dtype != LETHE_F32 && dtype != LETHE_BF16) return fail(ctx, LETHE_ERR_INVALID_ARG, "rotation: dtype must be LETHE_F32 or LETHE_BF16");
+    if (head_dim != 64 && head_dim != 128) return fail(ctx, LETHE_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+    if (nl < 1 || n_tokens < 0 || Hq < 1 || Hkv < 0) return fail(ctx, LETHE_ERR_INVALID_ARG, "rotation: bad sizes");
+    if (r->rot_dim < 2 || r->rot_dim > head_dim || (r->rot_dim & 1)) return fail(ctx, LETHE_ERR_INVALID_ARG, "rot_dim must be even, 2 .. head_dim");
+    if (r->style != LETHE_ROT_HALVES && r->style != LETHE_ROT_PAIRS) return fail(ctx, LETHE_ERR_INVALID_ARG, "unknown rotary style");
+    if (r->n_axes < 1 || r->n_axes > 4) return fail(ctx, LETHE_ERR_INVALID_ARG, "n_axes must be 1 .. 4");
+    if (!r->pair_axis || !r->pair_freq || !r->axis_pos) return fail(ctx, LETHE_ERR_INVALID_ARG, "rotary has a NULL table");
+    const long long rows = (long long)nl * ((long long)Hq + Hkv);
+    if (rows > 0x7fffffffLL || rows * (long long)n_tokens > 0x7fffffffLL) return fail(ctx, LETHE_ERR_UNSUPPORTED, "rotation: too many rows");
+    memset(a, 0, sizeof(*a));
+    for (int p = 0; p < r->rot_dim / 2; ++p) {
+        if (r->pair_axis[p] < 0 || r->pair_axis[p] >= r->n_axes) return fail(ctx, LETHE_ERR_INVALID_ARG, "pair_axis out of range");
+        const double f = r->pair_freq[p];
+        if (!(fabs(f) <= 6.2831853071795865)) return fail(ctx, LETHE_ERR_INVALID_ARG, "pair_freq must be at most one turn (2 pi) per position");
+        long double turns = (long double)f / 6.283185307179586476925286766559L;
+        turns -= floorl(turns);
+        a->turn[p] = turns >= 1.0L ? 0 : (unsigned long long)ldexpl(turns, 64);
+        a->axis[p] = (unsigned char)r->pair_axis[p];
+    }
+    a->axis_pos = r->axis_pos;
+    a->nl = nl; a->n_tokens = n_tokens; a->Hq = Hq; a->Hkv = Hkv; a->D = head_dim;
+    a->rot_dim = r->rot_dim;
+    a->halves = r->style == LETHE_ROT_HALVES;
+    a->inverse = inverse != 0;
+    a->rows = (int)rows;
+    return LETHE_OK;
+}
+
+// Two ranges of `na` and `nb` bytes that share some, without being the same tensor.
+static bool overlap_partly(const void* x, size_t na, const void* y, size_t nb) {
+    const uintptr_t p = (uintptr_t)x, q = (uintptr_t)y;
+    return p != q && p < q + nb && q < p + na;
+}
+
+lethe_status lethe_rotate(lethe_ctx* ctx, const lethe_rotary* rotary, int32_t dtype, int32_t head_dim, int n_layers, int n_tokens,
+                          int n_q_heads, int n_kv_heads, const void* q, const void* k, int32_t inverse, void* q_out, void* k_out,
+                          void* stream) {
+    if (!ctx) return LETHE_ERR_INVALID_ARG;
+    ctx->last_len = nullptr;  // the next decode call does not follow a decode call
+    if (!rotary || !q || !q_out) return fail(ctx, LETHE_ERR_INVALID_ARG, "rotary, q and q_out are required");
+    if ((k == nullptr) != (k_out == nullptr)) return fail(ctx, LETHE_ERR_INVALID_ARG, "k and k_out go together");
+    if (k && n_kv_heads < 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "rotation: bad sizes");
+    RotateArgs a;
+    lethe_status st = rotary_args(ctx, rotary, dtype, head_dim, n_layers, n_tokens, n_q_heads, k ? n_kv_heads : 0, inverse, &a);
+    if (st != LETHE_OK) return st;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out) & 15) return fail(ctx, LETHE_ERR_INVALID_ARG, "q, k and their outputs must be 16-byte aligned");
+    const size_t eb = dtype == LETHE_F32 ? 4 : 2;
+    const size_t nq = (size_t)n_layers * n_tokens * n_q_heads * head_dim * eb, nk = k ? (size_t)n_layers * n_tokens * n_kv_heads * head_dim * eb : 0;
+    if (overlap_partly(q, nq, q_out, nq) || (k && (overlap_partly(k, nk, k_out, nk) || overlap_partly(q, nq, k_out, nk) || overlap_partly(k, nk, q_out, nq) ||
+                                                   overlap_partly(q_out, nq, k_out, nk) || q_out == k_out || q == k_out || k == q_out)))
+        return fail(ctx, LETHE_ERR_INVALID_ARG, "an output may only be its own input");
+    if (n_tokens == 0) return LETHE_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
+    a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out;
+    cudaError_t e = launch_rotate(a, dtype == LETHE_F32, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "rotate launch");
+    return LETHE_OK;
+}
+
+lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_begin, int layer_end, const int32_t* chunk_start,
+                                int n_tokens, int max_chunk, const void* q, const void* k_new, const void* v_new,
+                                const int32_t* token_pos, const float* scale, double gamma, const lethe_score_mod* mod,
+                                const lethe_rotary* rotary, void* out, float* lse, void* stream) {
+    lethe_status st = check_cache(ctx, c);
+    if (st != LETHE_OK) return st;
+    ctx->last_len = nullptr;  // the next decode call does not follow a decode call
+    if (n_tokens < 0) return fail(ctx, LETHE_ERR_INVALID_ARG, "n_tokens must be >= 0");
+    if (n_tokens == 0) return LETHE_OK;
+    st = check_attend_args(ctx, c, layer_begin, layer_end, q, k_new, v_new, token_pos, scale, (float)gamma, out, true);
+    if (st != LETHE_OK) return st;
+    if (!chunk_start) return fail(ctx, LETHE_ERR_INVALID_ARG, "chunk_start is NULL");
+    if (max_chunk < 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "max_chunk must be positive");
+    if (mod) {
+        if (!(mod->softcap >= 0.f && mod->softcap <= 1e30f)) return fail(ctx, LETHE_ERR_INVALID_ARG, "softcap must be finite and >= 0");
+        if (mod->window < 0) return fail(ctx, LETHE_ERR_INVALID_ARG, "window must be >= 0");
+        if ((mod->slopes || mod->window > 0) && !token_pos) return fail(ctx, LETHE_ERR_INVALID_ARG, "slopes and a window need token_pos");
+    }
+    const int nl = layer_end - layer_begin, G = c->n_q_heads / c->n_kv_heads, D = c->head_dim;
+    RotateArgs rot;
+    if (rotary) {
+        st = rotary_args(ctx, rotary, c->dtype == LETHE_F32 ? LETHE_F32 : LETHE_BF16, D, nl, n_tokens, c->n_q_heads, k_new ? c->n_kv_heads : 0, 0, &rot);
+        if (st != LETHE_OK) return st;
+    }
+    if (max_chunk > n_tokens) max_chunk = n_tokens;
+
+    ChunkArgs a;
+    memset(&a, 0, sizeof(a));
+    a.k = c->k; a.v = c->v; a.rel = c->rel; a.pos = c->pos; a.len = c->len; a.page_table = c->page_table;
+    a.q = q; a.k_new = k_new; a.v_new = v_new; a.token_pos = token_pos; a.chunk_start = chunk_start; a.out = out; a.lse = lse;
+    a.status = ctx->status;
+    a.n_pages = c->n_pages;
+    a.dtype = c->dtype; a.D = D;
+    a.B = c->batch; a.Hq = c->n_q_heads; a.Hkv = c->n_kv_heads; a.G = G;
+    a.capacity = c->capacity; a.cap_tokens = cap_tokens_of(c);
+    a.paged = c->layout == LETHE_PAGED;
+    a.page_tokens = a.paged ? c->page_tokens : 1;
+    a.layer_begin = layer_begin; a.nl = nl;
+    a.n_items = nl * c->batch * c->n_kv_heads;
+    a.n_tokens = n_tokens; a.max_chunk = max_chunk;
+    a.append = k_new != nullptr;
+    a.gamma_log2 = (float)log2(gamma);
+    a.wait_limit = ctx->wait_limit;
+    bool by_pos = false;
+    if (mod) {
+        a.softcap = mod->softcap; a.window = mod->window; a.slopes = mod->slopes; a.doc_start = mod->doc_start; a.prefix_len = mod->prefix_len;
+        by_pos = mod->window > 0 || mod->doc_start || mod->prefix_len;
+    }
+    const bool bytes = c->dtype == LETHE_FP8_E4M3 || c->dtype == LETHE_FP8_E5M2;
+    for (int l = 0; l < c->n_layers; ++l) {
+        a.scale[l] = scale[l];
+        a.k_scale[l] = bytes && c->k_scale ? c->k_scale[l] : 1.f;
+        a.v_scale[l] = bytes && c->v_scale ? c->v_scale[l] : 1.f;
+    }
+    const bool simt = true;
+    a.TT = 64 / G;
+    a.TU = a.TT;
+    a.n_cta = 2 * ctx->sm_count;
+    a.min_per = 1;
+    a.QT = (max_chunk + a.TU - 1) / a.TU;
+    a.cap_tiles = (a.cap_tokens + kChunkTile - 1) / kChunkTile;
+    const long long units = (long long)a.n_items * a.QT;
+    if (units > 0x7fffffffLL / 4 || units * a.cap_tiles > 0x7fffffffLL || (long long)a.n_items * a.cap_tiles * 2 > 0x7fffffffLL)
+        return fail(ctx, LETHE_ERR_UNSUPPORTED, "chunk: too many (layer, sequence, head, block) units for one call; cover fewer layers");
+    a.n_units = (int)units;
+
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
+    size_t at = 0;
+    auto take = [&](size_t bytes_) { const size_t p = at; at += (bytes_ + 255) & ~(size_t)255; return p; };
+    const size_t act = c->dtype == LETHE_F32 ? 4 : 2;
+    const size_t o_plan = take(sizeof(ChunkPlan)), o_old = take((size_t)a.n_items * 4), o_start = take(((size_t)a.n_units + 1) * 4);
+    const size_t o_lo = by_pos ? take((size_t)a.n_units * 4) : 0, o_hi = by_pos ? take((size_t)a.n_units * 4) : 0;
+    const size_t o_bounds = by_pos ? take((size_t)a.n_items * a.cap_tiles * sizeof(int2)) : 0;
+    const size_t o_nlse = take((size_t)nl * n_tokens * a.Hq * 4);
+    const size_t o_ml = take((size_t)a.n_cta * kChunkParts * kChunkPartRows * sizeof(float2));
+    const size_t o_po = take((size_t)a.n_cta * kChunkParts * kChunkPartRows * D * sizeof(float));
+    const size_t o_q = rotary ? take((size_t)nl * n_tokens * a.Hq * D * act) : 0;
+    const size_t o_k = rotary && k_new ? take((size_t)nl * n_tokens * a.Hkv * D * act) : 0;
+    st = ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, at, "chunk scratch", stream);
+    if (st != LETHE_OK) return st;
+    char* base = (char*)ctx->scratch;
+    a.plan = (ChunkPlan*)(base + o_plan);
+    a.n_old = (int*)(base + o_old);
+    a.u_start = (int*)(base + o_start);
+    if (by_pos) {
+        a.u_lo = (int*)(base + o_lo);
+        a.u_hi = (int*)(base + o_hi);
+        a.bounds = (int2*)(base + o_bounds);
+    }
+    a.nlse2 = (float*)(base + o_nlse);
+    a.part_ml = (float2*)(base + o_ml);
+    a.part_o = (float*)(base + o_po);
+    cudaError_t e = cudaSuccess;
+    if (rotary) {
+        rot.q = q; rot.k = k_new; rot.q_out = base + o_q; rot.k_out = k_new ? base + o_k : nullptr;
+        e = launch_rotate(rot, c->dtype == LETHE_F32, (cudaStream_t)stream);
+        a.q = rot.q_out;
+        if (k_new) a.k_new = rot.k_out;
+    }
+    if (e == cudaSuccess) e = launch_chunk_append(a, (cudaStream_t)stream);
+    if (e == cudaSuccess && simt) e = launch_chunk_simt(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "chunk_attend launch");
     return LETHE_OK;
 }
 

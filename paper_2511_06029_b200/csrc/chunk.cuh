@@ -1,0 +1,166 @@
+// Arguments and device helpers shared by the kernels of lethe_chunk_attend.
+//
+// A call is a short chain of launches, each a programmatic dependent of the one before:
+//   append   new rows into the cache, pos; block 0 writes the plan
+//   range    only for masks by position: the tiles each unit can see, then the plan
+//   attend   softmax attention of the chunk, split evenly over the GPU by the plan
+//   combine  merges what the split left in parts
+//   rel      Eq. 5 for the chunk from the final softmax statistics; len
+//
+// A unit is a block of TU consecutive tokens of one sequence with the G query heads of one KV head (for the tensor-core
+// kernel two tiles of up to 128 rows).  Its cost is the number of 128-key tiles it can see.  The plan lays all units end to
+// end on a line of tiles and gives every CTA an equal stretch: lengths are only known on the device, and an even cut keeps
+// ragged batches, single long sequences and causal triangles balanced alike.  A stretch may begin or end inside a unit; such
+// a unit leaves one part per CTA, joined by `combine` in CTA order (deterministic: nothing is added atomically).
+#pragma once
+#include "common.cuh"
+
+namespace lethe {
+
+constexpr int kChunkTile = 128;    // keys per tile of the plan
+constexpr int kChunkParts = 4;     // parts a CTA can leave: (unit begun earlier, unit begun here and continued later) x two row tiles
+constexpr int kChunkPartRows = 128;
+
+struct ChunkPlan {  // head of the call's scratch
+    int total;      // tiles of all units
+    int per;        // tiles per CTA
+    int refused;    // chunk_start is malformed: nothing is done
+    int done;       // blocks of the range kernel that have finished
+};
+
+struct ChunkArgs {
+    const void* k;
+    const void* v;
+    float* rel;
+    int32_t* pos;
+    int32_t* len;
+    const int32_t* page_table;
+    const void* q;
+    const void* k_new;
+    const void* v_new;
+    const int32_t* token_pos;
+    const int32_t* chunk_start;
+    void* out;
+    float* lse;
+    int32_t* status;
+    // scratch
+    ChunkPlan* plan;
+    int* n_old;      // [items] retained tokens before the call; -1: the item is left alone
+    int* u_start;    // [n_units + 1] first tile of each unit on the line
+    int* u_lo;       // [n_units] first key tile of the unit (masks by position only, else NULL)
+    int* u_hi;       // [n_units] slots the unit can see end here (masks by position only, else NULL)
+    int2* bounds;    // [items][cap_tiles] smallest and largest pos of a key tile (masks by position only, else NULL)
+    float* nlse2;    // [nl][Hkv][n_tokens][G] minus the log-sum-exp, in log2 units; -inf for a row that sees nothing
+    float* part_o;   // [n_cta][kChunkParts][kChunkPartRows][D]
+    float2* part_ml; // [n_cta][kChunkParts][kChunkPartRows] (max in log2 units, sum)
+    long long n_pages;
+    int dtype, D;
+    int B, Hq, Hkv, G, capacity, cap_tokens, page_tokens, paged;
+    int layer_begin, nl, n_items, n_tokens, max_chunk;
+    int TT;          // tokens per row tile
+    int TU;          // tokens per unit
+    int QT;          // units per item
+    int n_units, n_cta, cap_tiles, min_per;
+    int append;
+    float gamma_log2;
+    int wait_limit;
+    // score modification
+    float softcap;
+    int window;
+    const float* slopes;
+    const int32_t* doc_start;
+    const int32_t* prefix_len;
+    float scale[kMaxLayers];    // softmax scale, by absolute layer
+    float k_scale[kMaxLayers];
+    float v_scale[kMaxLayers];
+};
+
+struct ChunkItem {
+    int li, l, b, hkv, item;  // item: absolute flat item
+    int first, T;             // first packed token and number of tokens of the sequence
+    int n_old, n;             // slots before and after the call; n_old = -1: left alone
+};
+
+// One sequence's stretch of the packed tokens is taken as chunk_start says: the append kernel has checked it (plan->refused).
+__device__ __forceinline__ ChunkItem chunk_item(const ChunkArgs& a, int idx) {
+    ChunkItem c;
+    c.hkv = idx % a.Hkv;
+    c.b = (idx / a.Hkv) % a.B;
+    c.li = idx / (a.Hkv * a.B);
+    c.l = a.layer_begin + c.li;
+    c.item = (c.l * a.B + c.b) * a.Hkv + c.hkv;
+    c.first = a.chunk_start[c.b];
+    c.T = a.chunk_start[c.b + 1] - c.first;
+    c.n_old = a.n_old[idx];
+    c.n = c.n_old + (a.append ? c.T : 0);
+    return c;
+}
+
+// Byte offset of row `slot` of an item, in rows; -1 for a page id outside the pool.
+__device__ __forceinline__ long long chunk_row(const ChunkArgs& a, int item, int slot) {
+    if (!a.paged) return (long long)item * a.capacity + slot;
+    const int page = a.page_table[(size_t)item * a.capacity + slot / a.page_tokens];
+    if (page < 0 || page >= a.n_pages) return -1;
+    return (long long)page * a.page_tokens + slot % a.page_tokens;
+}
+
+// What a query row needs to know to judge a key.
+struct ChunkRow {
+    int lim;     // slots below lim are in causal order
+    int qpos;    // original position
+    int lo;      // keys with a smaller position are hidden (window, document)
+    float slope; // distance bias, log2 units
+};
+
+__device__ __forceinline__ int chunk_lo(const ChunkArgs& a, int tok, int qpos) {
+    int lo = INT32_MIN;
+    if (a.window > 0) {
+        const long long w = (long long)qpos - a.window + 1;
+        lo = w < INT32_MIN ? INT32_MIN : (int)w;
+    }
+    if (a.doc_start) lo = max(lo, a.doc_start[tok]);
+    return lo;
+}
+
+// softcap * tanh(x / softcap) in log2 units: t = x / softcap, cap2 = softcap * log2(e).  An odd polynomial (fitted to tanh(t) / t
+// on t^2 <= 0.55^2; largest error 1e-9 before rounding) where scores usually are, 1 - 2 / (1 + e^2|t|) beyond: that form alone
+// has an absolute error of an ulp of one at small t, which times the cap would cost a score its low bits.
+__device__ __forceinline__ float capped_small(float t) {
+    const float u = t * t;
+    float p = fmaf(u, -0.006235556820094805f, 0.021039673409724794f);
+    p = fmaf(u, p, -0.05384270671952741f);
+    p = fmaf(u, p, 0.13332460742850846f);
+    p = fmaf(u, p, -0.33333310957894996f);
+    p = fmaf(u, p, 0.9999999990645916f);
+    return t * p;
+}
+__device__ __forceinline__ float capped_large(float t) {
+    const float e = fast_exp2(fabsf(t) * 2.885390081777927f);
+    return copysignf(1.f - __fdividef(2.f, 1.f + fminf(e, 1e30f)), t);
+}
+__device__ __forceinline__ float capped(float t) { return fabsf(t) <= 0.55f ? capped_small(t) : capped_large(t); }
+
+cudaError_t launch_chunk_append(const ChunkArgs& a, cudaStream_t stream);
+cudaError_t launch_chunk_combine(const ChunkArgs& a, cudaStream_t stream);
+cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t stream);
+
+// Launch with the programmatic dependency attribute: the kernel may start while the one before it is still finishing and waits
+// (griddepcontrol.wait) before it touches global memory.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
+}
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dependency_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+}  // namespace lethe

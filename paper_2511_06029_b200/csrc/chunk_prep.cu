@@ -1,0 +1,304 @@
+// lethe_chunk_attend: append of the new rows, the plan that cuts the attention evenly, and the merge of its parts.
+#include "chunk.cuh"
+
+namespace lethe {
+namespace {
+
+constexpr int kPrepThreads = 256;
+constexpr int kPrepWarps = kPrepThreads / 32;
+constexpr int kSeqShared = 1024;  // chunk_start entries kept in shared memory (longer batches read it from global memory)
+
+// Whether chunk_start never decreases, stays inside [0, n_tokens] and has no sequence above max_chunk; uniform for the block.
+__device__ bool chunk_start_ok(const ChunkArgs& a) {
+    bool ok = true;
+    for (int b = threadIdx.x; b < a.B; b += kPrepThreads) {
+        const int s0 = a.chunk_start[b], s1 = a.chunk_start[b + 1];
+        ok = ok && s0 >= 0 && s0 <= s1 && s1 <= a.n_tokens && s1 - s0 <= a.max_chunk;
+    }
+    return __syncthreads_and(ok);
+}
+
+__device__ __forceinline__ int unit_cost(const ChunkArgs& a, int u) {
+    const int idx = u / a.QT, qt = u - idx * a.QT;
+    const int n_old = a.n_old[idx];
+    if (n_old < 0) return 0;
+    const int b = (idx / a.Hkv) % a.B;
+    const int T = a.chunk_start[b + 1] - a.chunk_start[b], tok0 = qt * a.TU;
+    if (tok0 >= T) return 0;
+    if (a.u_hi) return max(1, (a.u_hi[u] + kChunkTile - 1) / kChunkTile - a.u_lo[u]);
+    const int hi = a.append ? n_old + min(T, tok0 + a.TU) : n_old;
+    return max(1, (hi + kChunkTile - 1) / kChunkTile);  // rows that see nothing still have to be written
+}
+
+// Lays the units end to end: u_start and the plan's totals.  One block.
+__device__ void make_plan(const ChunkArgs& a) {
+    __shared__ int sums[kPrepThreads];
+    const int tid = threadIdx.x;
+    const int seg = (a.n_units + kPrepThreads - 1) / kPrepThreads;
+    const int u0 = min(a.n_units, tid * seg), u1 = min(a.n_units, u0 + seg);
+    int mine = 0;
+    for (int u = u0; u < u1; ++u) mine += unit_cost(a, u);
+    sums[tid] = mine;
+    __syncthreads();
+    for (int off = 1; off < kPrepThreads; off <<= 1) {
+        const int add = tid >= off ? sums[tid - off] : 0;
+        __syncthreads();
+        sums[tid] += add;
+        __syncthreads();
+    }
+    int at = sums[tid] - mine;
+    for (int u = u0; u < u1; ++u) {
+        a.u_start[u] = at;
+        at += unit_cost(a, u);
+    }
+    if (tid == 0) {
+        const int total = sums[kPrepThreads - 1];
+        a.u_start[a.n_units] = total;
+        a.plan->total = total;
+        a.plan->per = max(a.min_per, (total + a.n_cta - 1) / a.n_cta);
+    }
+}
+
+// Two fp32 values -> two bytes of an 8-bit float, saturating (the low byte is the first).
+__device__ __forceinline__ uint32_t to_bytes(float lo, float hi, bool e5m2) {
+    uint32_t y;
+    if (e5m2) asm("{ .reg .b16 r; cvt.rn.satfinite.e5m2x2.f32 r, %2, %1; cvt.u32.u16 %0, r; }" : "=r"(y) : "f"(lo), "f"(hi));
+    else asm("{ .reg .b16 r; cvt.rn.satfinite.e4m3x2.f32 r, %2, %1; cvt.u32.u16 %0, r; }" : "=r"(y) : "f"(lo), "f"(hi));
+    return y;
+}
+__device__ __forceinline__ uint32_t quantise4(uint32_t ab, uint32_t cd, float scale, bool e5m2) {
+    const float a = __uint_as_float(ab << 16) / scale, b = __uint_as_float(ab & 0xffff0000u) / scale;
+    const float c = __uint_as_float(cd << 16) / scale, d = __uint_as_float(cd & 0xffff0000u) / scale;
+    return to_bytes(a, b, e5m2) | (to_bytes(c, d, e5m2) << 16);
+}
+
+// Blocks 1.. : one warp per (layer, token, KV head) row.  Memory-bound: each new row is read and written once with 16-byte
+// accesses.  Block 0 writes n_old, clears the call's counters and, when no mask goes by position, the plan.
+__global__ void __launch_bounds__(kPrepThreads) chunk_append_kernel(const __grid_constant__ ChunkArgs a) {
+    __shared__ int cs[kSeqShared + 1];
+    dependency_wait();
+    dependency_release();
+    const int tid = threadIdx.x, lane = tid & 31;
+    const bool ok = chunk_start_ok(a);
+    if (blockIdx.x == 0) {
+        if (tid == 0) {
+            a.plan->refused = !ok;
+            a.plan->done = 0;
+            if (!ok) record_error(a.status, LETHE_ERR_INVALID_ARG, 0);
+        }
+        for (int idx = tid; idx < a.n_items; idx += kPrepThreads) {
+            int n_old = -1;
+            if (ok) {
+                const int b = (idx / a.Hkv) % a.B, l = a.layer_begin + idx / (a.Hkv * a.B);
+                const int item = (l * a.B + b) * a.Hkv + idx % a.Hkv;
+                const int T = a.chunk_start[b + 1] - a.chunk_start[b];
+                n_old = min(max(a.len[item], 0), a.cap_tokens);
+                if (a.append && n_old + (long long)T > a.cap_tokens) {
+                    n_old = -1;
+                    record_error(a.status, LETHE_ERR_CAPACITY, item);
+                }
+            }
+            a.n_old[idx] = n_old;
+        }
+        __syncthreads();
+        if (!a.u_hi) make_plan(a);
+        return;
+    }
+    if (!ok) return;
+    const bool in_shared = a.B <= kSeqShared;
+    if (in_shared)
+        for (int b = tid; b <= a.B; b += kPrepThreads) cs[b] = a.chunk_start[b];
+    __syncthreads();
+    const int* start = in_shared ? cs : a.chunk_start;
+
+    const bool bytes = a.dtype == LETHE_FP8_E4M3 || a.dtype == LETHE_FP8_E5M2, e5m2 = a.dtype == LETHE_FP8_E5M2;
+    const int act = a.dtype == LETHE_F32 ? 4 : 2;
+    const int src_row = a.D * act, dst_row = bytes ? a.D : src_row;
+    const int chunks = src_row / 16;  // 16-byte pieces of a new row: 8 .. 32
+    const long long rows = (long long)a.nl * a.n_tokens * a.Hkv;
+    for (long long r = (long long)(blockIdx.x - 1) * kPrepWarps + (tid >> 5); r < rows; r += (long long)(gridDim.x - 1) * kPrepWarps) {
+        const int hkv = (int)(r % a.Hkv);
+        const long long lt = r / a.Hkv;
+        const int tok = (int)(lt % a.n_tokens), li = (int)(lt / a.n_tokens), l = a.layer_begin + li;
+        if (tok < start[0] || tok >= start[a.B]) continue;
+        int lo = 0, hi = a.B;  // last b with start[b] <= tok: the sequence of this token (empty ones before it are passed over)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (start[mid] <= tok) lo = mid;
+            else hi = mid;
+        }
+        const int b = lo, T = start[b + 1] - start[b];
+        const int item = (l * a.B + b) * a.Hkv + hkv;
+        const int n_old = min(max(a.len[item], 0), a.cap_tokens);
+        if (n_old + (long long)T > a.cap_tokens) {  // refused: nothing of the item changes, its outputs are zero
+            char* o = (char*)a.out + ((size_t)lt * a.Hq + (size_t)hkv * a.G) * src_row;
+            for (int i = lane; i < a.G * chunks; i += 32) reinterpret_cast<uint4*>(o)[i] = make_uint4(0, 0, 0, 0);
+            if (a.lse && lane < a.G) a.lse[(size_t)lt * a.Hq + hkv * a.G + lane] = -INFINITY;
+            continue;
+        }
+        const int slot = n_old + tok - start[b];
+        if (lane == 0) a.pos[(size_t)item * a.cap_tokens + slot] = a.token_pos[tok];
+        const long long at = chunk_row(a, item, slot);
+        if (at < 0) {
+            if (lane == 0) record_error(a.status, LETHE_ERR_PAGE, item);
+            continue;
+        }
+        for (int i = lane; i < 2 * chunks; i += 32) {
+            const bool is_v = i >= chunks;
+            const int c = is_v ? i - chunks : i;
+            const uint4 x = reinterpret_cast<const uint4*>((const char*)(is_v ? a.v_new : a.k_new) + (size_t)r * src_row)[c];
+            char* d = (char*)const_cast<void*>(is_v ? a.v : a.k) + (size_t)at * dst_row;
+            if (!bytes) reinterpret_cast<uint4*>(d)[c] = x;
+            else {
+                const float sc = is_v ? a.v_scale[l] : a.k_scale[l];
+                reinterpret_cast<uint2*>(d)[c] = make_uint2(quantise4(x.x, x.y, sc, e5m2), quantise4(x.z, x.w, sc, e5m2));
+            }
+        }
+    }
+}
+
+// Masks by position.  A block takes one item: the smallest and largest position of each of its key tiles, then for each unit the
+// first tile with a key that its farthest-reaching token may still see and the end of what the prefix opens.  Conservative
+// whatever the order of the positions is; the attention tests every key that is left.  The last block to finish plans.
+__global__ void __launch_bounds__(kPrepThreads) chunk_range_kernel(const __grid_constant__ ChunkArgs a) {
+    __shared__ int last;
+    dependency_wait();
+    dependency_release();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const ChunkItem it = chunk_item(a, blockIdx.x);
+    if (it.n_old >= 0 && it.T > 0) {
+        const int tiles = (it.n + kChunkTile - 1) / kChunkTile;
+        int2* bounds = a.bounds + (size_t)blockIdx.x * a.cap_tiles;
+        const int32_t* pos = a.pos + (size_t)it.item * a.cap_tokens;
+        for (int t = warp; t < tiles; t += kPrepWarps) {
+            int mn = INT32_MAX, mx = INT32_MIN;
+#pragma unroll
+            for (int i = 0; i < kChunkTile / 32; ++i) {
+                const int j = t * kChunkTile + i * 32 + lane;
+                if (j < it.n) {
+                    const int p = pos[j];
+                    mn = min(mn, p);
+                    mx = max(mx, p);
+                }
+            }
+            mn = __reduce_min_sync(0xffffffffu, mn);
+            mx = __reduce_max_sync(0xffffffffu, mx);
+            if (lane == 0) bounds[t] = make_int2(mn, mx);
+        }
+        __syncthreads();
+        const int units = (it.T + a.TU - 1) / a.TU;
+        for (int qt = warp; qt < units; qt += kPrepWarps) {
+            const int tok0 = qt * a.TU, tok1 = min(it.T, tok0 + a.TU);
+            int lo = INT32_MAX;
+            for (int i = tok0 + lane; i < tok1; i += 32) lo = min(lo, chunk_lo(a, it.first + i, a.window > 0 ? a.token_pos[it.first + i] : 0));
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            int hi = a.append ? it.n_old + tok1 : it.n_old;
+            int t_lo = 0;
+            bool found = false;
+            for (int t0 = 0; t0 < tiles && !found; t0 += 32) {
+                const unsigned hit = __ballot_sync(0xffffffffu, t0 + lane < tiles && bounds[t0 + lane].y >= lo);
+                if (hit) {
+                    t_lo = t0 + __ffs(hit) - 1;
+                    found = true;
+                }
+            }
+            if (a.prefix_len) {
+                const int prefix = a.prefix_len[it.b];
+                for (int t0 = (tiles - 1) & ~31; t0 >= 0; t0 -= 32) {
+                    const unsigned hit = __ballot_sync(0xffffffffu, t0 + lane < tiles && bounds[t0 + lane].x < prefix);
+                    if (hit) {
+                        hi = max(hi, min(it.n, (t0 + 32 - __clz(hit)) * kChunkTile));
+                        break;
+                    }
+                }
+            }
+            if (!found || t_lo * kChunkTile >= hi) t_lo = 0, hi = 0;
+            if (lane == 0) {
+                a.u_lo[blockIdx.x * a.QT + qt] = t_lo;
+                a.u_hi[blockIdx.x * a.QT + qt] = hi;
+            }
+        }
+    }
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) last = atomicAdd(&a.plan->done, 1) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    make_plan(a);
+}
+
+// Merges the parts of each unit that more than one CTA worked on: one block per unit, one warp per row, the parts in the
+// order of the keys they cover.
+__global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __grid_constant__ ChunkArgs a) {
+    dependency_wait();
+    dependency_release();
+    const int u = blockIdx.x;
+    const int s0 = a.u_start[u], s1 = a.u_start[u + 1];
+    if (s0 == s1) return;
+    const int per = a.plan->per;
+    const int c0 = s0 / per, c1 = (s1 - 1) / per;
+    if (c0 == c1) return;  // written by the one CTA that had it
+    const int idx = u / a.QT, tok0 = (u - idx * a.QT) * a.TU;
+    const ChunkItem it = chunk_item(a, idx);
+    const int toks = min(it.T - tok0, a.TU);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int E = a.D / 32;                      // elements per lane: 2 or 4
+    for (int row = warp; row < toks * a.G; row += kPrepWarps) {
+        const int tile = row / (a.TT * a.G), r = row - tile * a.TT * a.G;  // row tile and row in it
+        float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int c = c0; c <= c1; ++c) {
+            const size_t p = (size_t)(c * 2 + (c == c0 ? 1 : 0)) * 2 + tile;  // the unit begins in CTA c0 and was begun earlier in the others
+            const float2 ml = a.part_ml[p * kChunkPartRows + r];
+            if (ml.x == -INFINITY) continue;  // the part saw nothing of this row
+            const float mx = fmaxf(m, ml.x);
+            const float w_old = exp2_diff(m, mx), w = fast_exp2(ml.x - mx);
+            const float* src = a.part_o + (p * kChunkPartRows + r) * a.D + lane * E;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (E == 4) {
+                const float4 f = *reinterpret_cast<const float4*>(src);
+                v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+            } else {
+                const float2 f = *reinterpret_cast<const float2*>(src);
+                v[0] = f.x; v[1] = f.y;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * w_old + v[e] * w;
+            l = l * w_old + ml.y * w;
+            m = mx;
+        }
+        const float inv = l == 0.f ? 0.f : a.v_scale[it.l] / l;  // nothing seen: zero; a NaN stays one
+        const int tok = tok0 + row / a.G, h = row % a.G;
+        const size_t orow = ((size_t)it.li * a.n_tokens + it.first + tok) * a.Hq + it.hkv * a.G + h;
+        if (a.dtype == LETHE_F32) {
+            float* d = (float*)a.out + orow * a.D + lane * E;
+            for (int e = 0; e < E; ++e) d[e] = o[e] * inv;
+        } else {
+            __nv_bfloat16* d = (__nv_bfloat16*)a.out + orow * a.D + lane * E;
+            for (int e = 0; e < E; e += 2) *reinterpret_cast<__nv_bfloat162*>(d + e) = __floats2bfloat162_rn(o[e] * inv, o[e + 1] * inv);
+        }
+        if (lane == 0) {
+            const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+            if (a.lse) a.lse[orow] = lse2 * 0.6931471805599453f;
+            a.nlse2[(((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first + tok) * a.G + h] = l == 0.f ? -INFINITY : -lse2;
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_append(const ChunkArgs& a, cudaStream_t stream) {
+    // about four waves of warps: a row is a short dependent chain (sequence, length, page, row), so many are kept in flight
+    const long long rows = a.append ? (long long)a.nl * a.n_tokens * a.Hkv : 0;
+    const long long want = (rows + kPrepWarps - 1) / kPrepWarps;
+    const int blocks = 1 + (int)(want < 4736 ? want : 4736);
+    cudaError_t e = launch_dependent(chunk_append_kernel, dim3(blocks), kPrepThreads, 0, stream, a);
+    if (e == cudaSuccess && a.u_hi) e = launch_dependent(chunk_range_kernel, dim3(a.n_items), kPrepThreads, 0, stream, a);
+    return e;
+}
+
+cudaError_t launch_chunk_combine(const ChunkArgs& a, cudaStream_t stream) {
+    return launch_dependent(chunk_combine_kernel, dim3(a.n_units), kPrepThreads, 0, stream, a);
+}
+
+}  // namespace lethe
