@@ -7,7 +7,7 @@
 
 #include "common.cuh"
 #include "prefill.cuh"
-#include "chunk.cuh"
+#include "chunk_tc.cuh"
 #include "rotate.cuh"
 
 namespace lethe {
@@ -1142,11 +1142,12 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
         a.k_scale[l] = bytes && c->k_scale ? c->k_scale[l] : 1.f;
         a.v_scale[l] = bytes && c->v_scale ? c->v_scale[l] : 1.f;
     }
-    const bool simt = true;
-    a.TT = 64 / G;
-    a.TU = a.TT;
-    a.n_cta = 2 * ctx->sm_count;
-    a.min_per = 1;
+    // fp32 caches: CUDA cores, 64-row units; else the tensor cores, units of two 128-row tiles
+    const bool simt = c->dtype == LETHE_F32;
+    a.TT = (simt ? 64 : kChunkTile) / G;
+    a.TU = simt ? a.TT : 2 * a.TT;
+    a.n_cta = simt ? 2 * ctx->sm_count : ctx->sm_count;
+    a.min_per = simt ? 1 : 2;  // both softmax groups of a CTA have something to do
     a.QT = (max_chunk + a.TU - 1) / a.TU;
     a.cap_tiles = (a.cap_tokens + kChunkTile - 1) / kChunkTile;
     const long long units = (long long)a.n_items * a.QT;
@@ -1161,6 +1162,7 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     const size_t act = c->dtype == LETHE_F32 ? 4 : 2;
     const size_t o_plan = take(sizeof(ChunkPlan)), o_old = take((size_t)a.n_items * 4), o_start = take(((size_t)a.n_units + 1) * 4);
     const size_t o_lo = by_pos ? take((size_t)a.n_units * 4) : 0, o_hi = by_pos ? take((size_t)a.n_units * 4) : 0;
+    const size_t o_rel = simt ? 0 : take(((size_t)a.n_items + 1) * 4);
     const size_t o_bounds = by_pos ? take((size_t)a.n_items * a.cap_tiles * sizeof(int2)) : 0;
     const size_t o_nlse = take((size_t)nl * n_tokens * a.Hq * 4);
     const size_t o_ml = take((size_t)a.n_cta * kChunkParts * kChunkPartRows * sizeof(float2));
@@ -1178,6 +1180,7 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
         a.u_hi = (int*)(base + o_hi);
         a.bounds = (int2*)(base + o_bounds);
     }
+    if (!simt) a.rel_start = (int*)(base + o_rel);
     a.nlse2 = (float*)(base + o_nlse);
     a.part_ml = (float2*)(base + o_ml);
     a.part_o = (float*)(base + o_po);
@@ -1188,8 +1191,17 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
         a.q = rot.q_out;
         if (k_new) a.k_new = rot.k_out;
     }
+    ChunkMaps maps;
+    if (!simt && (!resolve_tma_encode(ctx) || !build_chunk_maps(ctx->tma_encode, a, c->n_layers, &maps)))
+        return fail(ctx, LETHE_ERR_CUDA, "cuTensorMapEncodeTiled failed");
     if (e == cudaSuccess) e = launch_chunk_append(a, (cudaStream_t)stream);
-    if (e == cudaSuccess && simt) e = launch_chunk_simt(a, (cudaStream_t)stream);
+    if (simt) {
+        if (e == cudaSuccess) e = launch_chunk_simt(a, (cudaStream_t)stream);
+    } else {
+        if (e == cudaSuccess) e = launch_chunk_tc(a, maps, (cudaStream_t)stream);
+        if (e == cudaSuccess) e = launch_chunk_combine(a, (cudaStream_t)stream);
+        if (e == cudaSuccess) e = launch_chunk_rel_tc(a, maps, 2 * ctx->sm_count, (cudaStream_t)stream);
+    }
     if (e != cudaSuccess) return cuda_fail(ctx, e, "chunk_attend launch");
     return LETHE_OK;
 }

@@ -57,6 +57,31 @@ __device__ void make_plan(const ChunkArgs& a) {
         a.plan->total = total;
         a.plan->per = max(a.min_per, (total + a.n_cta - 1) / a.n_cta);
     }
+    if (!a.rel_start) return;
+    // the relevance kernel's line: pairs of key tiles of every item that changes
+    const int iseg = (a.n_items + kPrepThreads - 1) / kPrepThreads;
+    const int i0 = min(a.n_items, tid * iseg), i1 = min(a.n_items, i0 + iseg);
+    auto pairs = [&](int idx) {
+        const ChunkItem it = chunk_item(a, idx);
+        return it.n_old < 0 || it.T == 0 ? 0 : (it.n + 2 * kChunkTile - 1) / (2 * kChunkTile);
+    };
+    mine = 0;
+    for (int idx = i0; idx < i1; ++idx) mine += pairs(idx);
+    __syncthreads();
+    sums[tid] = mine;
+    __syncthreads();
+    for (int off = 1; off < kPrepThreads; off <<= 1) {
+        const int add = tid >= off ? sums[tid - off] : 0;
+        __syncthreads();
+        sums[tid] += add;
+        __syncthreads();
+    }
+    at = sums[tid] - mine;
+    for (int idx = i0; idx < i1; ++idx) {
+        a.rel_start[idx] = at;
+        at += pairs(idx);
+    }
+    if (tid == 0) a.rel_start[a.n_items] = sums[kPrepThreads - 1];
 }
 
 // Two fp32 values -> two bytes of an 8-bit float, saturating (the low byte is the first).
@@ -250,7 +275,7 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
         for (int c = c0; c <= c1; ++c) {
             const size_t p = (size_t)(c * 2 + (c == c0 ? 1 : 0)) * 2 + tile;  // the unit begins in CTA c0 and was begun earlier in the others
             const float2 ml = a.part_ml[p * kChunkPartRows + r];
-            if (ml.x == -INFINITY) continue;  // the part saw nothing of this row
+            if (ml.x == -INFINITY && ml.y == 0.f) continue;  // the part saw nothing of this row
             const float mx = fmaxf(m, ml.x);
             const float w_old = exp2_diff(m, mx), w = fast_exp2(ml.x - mx);
             const float* src = a.part_o + (p * kChunkPartRows + r) * a.D + lane * E;

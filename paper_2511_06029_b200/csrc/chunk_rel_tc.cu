@@ -1,0 +1,339 @@
+// lethe_chunk_attend, Eq. 5 for the chunk, on the tensor cores: rel[j] = gamma^T rel[j] + sum over tokens and heads of
+// gamma^(T-1-i) p_ihj, from the final softmax statistics.
+//
+// The logits are formed again, transposed: S^T = K Q^T with 128 keys on the tensor-memory lanes and 128 (token, head) columns, so
+// that a thread owns a key, adds its row up in registers and stores one sum — no atomics, one order.  With the column's bias
+// (log2 of the decay weight minus the log-sum-exp) a column costs one FMA, one exponential and one add, and the exponentials are
+// the bound (16 a clock per SM, 1024 clocks a tile against 512 of products).  The alternative, writing column sums from the
+// attention kernel, would need the final maxima and sums before the last key is known.
+//
+// A unit is a pair of key tiles of one item (two groups of four warps); CTAs walk the plan's line of units round robin, two
+// CTAs to an SM covering each other's hand-offs.  Warp 8 issues the MMAs, warp 9 loads tiles by TMA; tiles that TMA cannot take
+// (byte caches, odd pages) are gathered by the softmax warps, once per unit.
+#include "chunk_tc.cuh"
+
+namespace lethe {
+namespace {
+
+constexpr int kSoftWarps = 8;
+constexpr int kMmaWarp = 8;
+constexpr int kLoadWarp = 9;
+constexpr int kThreads = 10 * 32;
+constexpr int kTmemCols = 256;  // one logit tile per group
+
+template <int D>
+constexpr size_t smem_bytes() { return 1024 + 3 * (size_t)tile_bytes<D>(); }  // two key tiles, one query tile
+
+struct ColumnMod {
+    float qpos;   // relative to the sequence's first new token
+    float slope;  // log2 units
+    int lo;
+    int pad;
+};
+
+template <bool MOD>
+struct Shared {
+    unsigned long long k_full, k_empty, q_full, q_empty;
+    unsigned long long s_full[2], s_empty[2];
+    unsigned long long drained;
+    uint32_t tmem_base;
+    int abort;
+    int k_loads, q_loads, issued;
+    alignas(16) float bias[kSoftWarps][kTile];
+    alignas(16) ColumnMod mod[MOD ? kSoftWarps : 1][MOD ? kTile : 1];
+};
+
+// The query tiles that a pair of key tiles (from slot j0) meets: f(qt) for each; f returns false to stop.
+template <typename F>
+__device__ __forceinline__ bool for_query_tiles(const ChunkArgs& a, const ChunkItem& it, int idx, int j0, F f) {
+    const int n_qt = (it.T + a.TT - 1) / a.TT;
+    int qt = 0;
+    if (!a.u_hi && a.append) qt = max(0, j0 - it.n_old) / a.TT;  // earlier tokens do not reach slot j0
+    for (; qt < n_qt; ++qt) {
+        if (a.u_hi) {  // masks by position: what the unit of this tile can see
+            const int u = idx * a.QT + qt * a.TT / a.TU;
+            if (a.u_hi[u] <= j0 || a.u_lo[u] * kTile >= j0 + 2 * kTile) continue;
+        }
+        if (!f(qt)) return false;
+    }
+    return true;
+}
+
+template <int D, bool TMA, bool MOD>
+__global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps) {
+    constexpr int TILE = tile_bytes<D>(), KS = D / 16;
+    extern __shared__ unsigned char dyn_raw[];
+    __shared__ Shared<MOD> sh;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t k_tile = (smem_u32(dyn_raw) + 1023u) & ~1023u, q_tile = k_tile + 2 * TILE;
+    volatile int* abort_flag = &sh.abort;
+    const int limit = a.wait_limit > 0 ? a.wait_limit : kChunkWaitLimit;
+    const int used = a.TT * a.G;
+
+    if (tid == 0) {
+        bar_init(&sh.k_full, TMA ? 1 : kSoftWarps);
+        bar_init(&sh.k_empty, 1);
+        bar_init(&sh.q_full, 1);
+        bar_init(&sh.q_empty, 1);
+        for (int g = 0; g < 2; ++g) {
+            bar_init(&sh.s_full[g], 1);
+            bar_init(&sh.s_empty[g], 4);
+        }
+        bar_init(&sh.drained, 1);
+        sh.abort = sh.k_loads = sh.q_loads = sh.issued = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    // columns that the query boxes never write stay zero
+    for (int i = tid; i < (kTile - used) * (D / 8); i += kThreads)
+        st_shared_16(chunk_addr(q_tile, used + i / (D / 8), i % (D / 8)), make_uint4(0, 0, 0, 0));
+    proxy_fence();
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    dependency_wait();
+    dependency_release();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = sh.tmem_base;
+    const int total = a.rel_start[a.n_items];
+
+    if (warp == kLoadWarp) {
+        if (lane == 0) {
+            bool bad = false;  // the attention has recorded bad pages
+            int k = 0, qn = 0;
+            for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
+                const int idx = find_start(a.rel_start, a.n_items, w), j0 = (w - a.rel_start[idx]) * 2 * kTile;
+                const ChunkItem it = chunk_item(a, idx);
+                if (TMA) {
+                    if (k > 0 && !bar_wait(&sh.k_empty, k - 1, abort_flag, limit)) break;
+                    const int tiles = j0 + kTile < it.n ? 2 : 1;
+                    bar_expect_tx(&sh.k_full, tiles * TILE);
+                    sh.k_loads = k + 1;
+                    for (int g = 0; g < tiles; ++g) tma_tile<D>(a, &maps.k, it.item, it.n, j0 + g * kTile, k_tile + g * TILE, &sh.k_full, &bad);
+                }
+                const bool ok = for_query_tiles(a, it, idx, j0, [&](int qt) {
+                    if (qn > 0 && !bar_wait(&sh.q_empty, qn - 1, abort_flag, limit)) return false;
+                    bar_expect_tx(&sh.q_full, (unsigned)(used * D * 2));
+                    sh.q_loads = ++qn;
+#pragma unroll
+                    for (int hf = 0; hf < D / 64; ++hf)
+                        tma_4d(q_tile + hf * kHalfBytes, &maps.q, 64 * hf, it.hkv * a.G, it.first + qt * a.TT, it.li, &sh.q_full);
+                    return true;
+                });
+                if (!ok) break;
+            }
+        }
+        __syncwarp();
+    } else if (warp == kMmaWarp) {
+        if (lane == 0) {
+            int k = 0, qn = 0;
+            int ns[2] = {0, 0};
+            for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
+                const int idx = find_start(a.rel_start, a.n_items, w), j0 = (w - a.rel_start[idx]) * 2 * kTile;
+                const ChunkItem it = chunk_item(a, idx);
+                const int tiles = j0 + kTile < it.n ? 2 : 1;
+                const uint32_t desc = mma_idesc(kTile, false, a.scale[it.l] < 0.f);
+                if (!bar_wait(&sh.k_full, k, abort_flag, limit)) break;
+                const bool ok = for_query_tiles(a, it, idx, j0, [&](int) {
+                    if (!bar_wait(&sh.q_full, qn, abort_flag, limit)) return false;
+                    for (int g = 0; g < tiles; ++g) {
+                        if (ns[g] > 0 && !bar_wait(&sh.s_empty[g], ns[g] - 1, abort_flag, limit)) return false;
+                        tc_after();
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) {
+                            const uint32_t off = (ks >> 2) * kHalfBytes + (ks & 3) * 32;
+                            mma_ss(tmem + g * kTile, smem_desc(k_tile + g * TILE + off, 16), smem_desc(q_tile + off, 16), desc, ks > 0);
+                        }
+                        sh.issued = 1;
+                        tc_commit(&sh.s_full[g]);
+                        ++ns[g];
+                    }
+                    tc_commit(&sh.q_empty);
+                    ++qn;
+                    return true;
+                });
+                if (!ok) break;
+                tc_commit(&sh.k_empty);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int g = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + g * kTile;
+        int n_s = 0, k = 0;
+        for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
+            const int idx = find_start(a.rel_start, a.n_items, w), j0 = (w - a.rel_start[idx]) * 2 * kTile;
+            const ChunkItem it = chunk_item(a, idx);
+            const int j = j0 + g * kTile + r;  // this thread's key
+            if (!TMA) {
+                bool bad = false;
+                if (k > 0 && !warp_wait(&sh.k_empty, k - 1, abort_flag, limit)) break;
+                for (int t = 0; t < (j0 + kTile < it.n ? 2 : 1); ++t) gather_tile<D>(a, a.k, it.item, it.n, j0 + t * kTile, k_tile + t * TILE, tid, kSoftWarps * 32, &bad);
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.k_full);
+            }
+            if (j0 == 0 && tid == 0 && a.append) a.len[it.item] = it.n;
+            if (j0 + g * kTile >= it.n) continue;  // the second tile does not exist
+            float* rel = a.rel + (size_t)it.item * a.cap_tokens + j;
+            const float old = j < it.n_old ? *rel : 0.f;
+            const float scale = fabsf(a.scale[it.l]) * a.k_scale[it.l], sl2 = scale * 1.4426950408889634f;
+            float cap_in = 0.f, cap2 = 0.f, kf = 0.f;
+            int kp = 0, prefix = INT32_MIN, pos0 = 0;
+            const bool mask_pos = MOD && (a.window > 0 || a.doc_start || a.prefix_len);
+            if (MOD) {
+                if (a.softcap > 0.f) {
+                    cap_in = scale / a.softcap;
+                    cap2 = a.softcap * 1.4426950408889634f;
+                }
+                if (a.token_pos) pos0 = a.token_pos[it.first];
+                if (a.prefix_len) prefix = a.prefix_len[it.b];
+                if (mask_pos || a.slopes) {
+                    kp = j < it.n ? a.pos[(size_t)it.item * a.cap_tokens + j] : 0;
+                    kf = (float)((long long)kp - pos0);
+                }
+            }
+            const float* nlse = a.nlse2 + (((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G;
+            float acc0 = 0.f, acc1 = 0.f, acc2 = 0.f, acc3 = 0.f;
+            const bool ok = for_query_tiles(a, it, idx, j0, [&](int qt) {
+                // biases of the tile's columns, one copy per warp (the warps never wait for one another)
+                const int cols = min(a.TT, it.T - qt * a.TT) * a.G;
+                int lo_max = INT32_MIN;
+                __syncwarp();
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int c = x * 32 + lane, tok = qt * a.TT + c / a.G;
+                    float bias = -INFINITY;
+                    if (c < cols) bias = nlse[qt * used + c] + (float)(it.T - 1 - tok) * a.gamma_log2;
+                    sh.bias[warp][c] = bias;
+                    if (MOD) {
+                        ColumnMod cm = {0.f, 0.f, INT32_MIN, 0};
+                        if (c < cols) {
+                            const int qp = a.token_pos ? a.token_pos[it.first + tok] : 0;
+                            cm.qpos = (float)((long long)qp - pos0);
+                            if (a.slopes) cm.slope = a.slopes[it.hkv * a.G + c % a.G] * 1.4426950408889634f;
+                            cm.lo = chunk_lo(a, it.first + tok, qp);
+                        }
+                        sh.mod[warp][c] = cm;
+                        lo_max = max(lo_max, cm.lo);
+                    }
+                }
+                if (MOD) lo_max = __reduce_max_sync(0xffffffffu, lo_max);
+                __syncwarp();
+                if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
+                tc_after();
+                // first column that reaches slot j in causal order
+                const int c_lo = a.append ? (j - it.n_old - qt * a.TT) * a.G : 0;
+                // a short tile's other columns are tokens of other sequences: whatever they hold must not count
+                const bool clean = cols == used && __all_sync(0xffffffffu, c_lo <= 0 && (!mask_pos || kp >= lo_max));
+#pragma unroll
+                for (int ch = 0; ch < kTile; ch += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(s_addr + ch, v);
+                    tmem_ld_wait();
+                    if (ch == kTile - 32) {
+                        tc_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(&sh.s_empty[g]);
+                    }
+                    float ml = sl2;
+                    if (MOD) {
+                        if (a.softcap > 0.f) {
+                            ml = 1.f;
+#pragma unroll
+                            for (int c = 0; c < 32; c += 8) {
+                                float x[8], big = 0.f;
+#pragma unroll
+                                for (int y = 0; y < 8; ++y) {
+                                    x[y] = __uint_as_float(v[c + y]) * cap_in;
+                                    big = fmaxf(big, fabsf(x[y]));
+                                    v[c + y] = __float_as_uint(cap2 * capped_small(x[y]));
+                                }
+                                if (__any_sync(0xffffffffu, big > 0.55f)) {
+#pragma unroll
+                                    for (int y = 0; y < 8; ++y)
+                                        if (fabsf(x[y]) > 0.55f) v[c + y] = __float_as_uint(cap2 * capped_large(x[y]));
+                                }
+                            }
+                        }
+                        if (a.slopes) {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                const float2 qs = *reinterpret_cast<const float2*>(&sh.mod[warp][ch + c]);
+                                v[c] = __float_as_uint(fmaf(-qs.y, fabsf(qs.x - kf), __uint_as_float(v[c]) * ml));
+                            }
+                            ml = 1.f;
+                        }
+                    }
+                    const float4* b4 = reinterpret_cast<const float4*>(sh.bias[warp] + ch);
+                    if (clean) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4) {
+                            const float4 b = b4[c / 4];
+                            acc0 += fast_exp2(fmaf(__uint_as_float(v[c]), ml, b.x));
+                            acc1 += fast_exp2(fmaf(__uint_as_float(v[c + 1]), ml, b.y));
+                            acc2 += fast_exp2(fmaf(__uint_as_float(v[c + 2]), ml, b.z));
+                            acc3 += fast_exp2(fmaf(__uint_as_float(v[c + 3]), ml, b.w));
+                        }
+                    } else if (j < it.n) {
+                        const bool open = kp < prefix;  // the prefix opens this key to every token
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            const int cc = ch + c;
+                            bool see = cc < cols && (cc >= c_lo || (MOD && open));
+                            if (MOD && mask_pos) see = see && kp >= sh.mod[warp][cc].lo;
+                            const float e = fast_exp2(fmaf(__uint_as_float(v[c]), ml, sh.bias[warp][cc]));
+                            if (see) acc0 += e;
+                        }
+                    }
+                }
+                return true;
+            });
+            if (!ok) break;
+            if (j < it.n) *rel = fmaf(exp2f((float)it.T * a.gamma_log2), old, (acc0 + acc1) + (acc2 + acc3));
+        }
+    }
+
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (sh.abort) {  // uniform for the CTA: see everything this CTA has started end
+        if (tid == 0) record_error(a.status, LETHE_ERR_TIMEOUT, blockIdx.x);
+        if (warp == kMmaWarp && lane == 0 && sh.issued) {
+            tc_commit(&sh.drained);
+            bar_drain(&sh.drained, 0);
+        }
+        if (warp == kLoadWarp && lane == 0) {
+            if (TMA && sh.k_loads > 0) bar_drain(&sh.k_full, sh.k_loads - 1);
+            if (sh.q_loads > 0) bar_drain(&sh.q_full, sh.q_loads - 1);
+        }
+        tc_before();
+        __syncthreads();
+        tc_after();
+    }
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+template <int D, bool TMA, bool MOD>
+cudaError_t launch_t(const ChunkArgs& a, const ChunkMaps& maps, int grid, cudaStream_t stream) {
+    cudaError_t e = prepare_kernel((const void*)chunk_tc_rel<D, TMA, MOD>, smem_bytes<D>());
+    if (e == cudaSuccess) e = launch_dependent(chunk_tc_rel<D, TMA, MOD>, dim3(grid), kThreads, smem_bytes<D>(), stream, a, maps);
+    return e;
+}
+
+template <int D, bool TMA>
+cudaError_t launch_m(const ChunkArgs& a, const ChunkMaps& maps, int grid, cudaStream_t stream) {
+    const bool mod = a.softcap > 0.f || a.slopes || a.window > 0 || a.doc_start || a.prefix_len;
+    return mod ? launch_t<D, TMA, true>(a, maps, grid, stream) : launch_t<D, TMA, false>(a, maps, grid, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_rel_tc(const ChunkArgs& a, const ChunkMaps& maps, int grid, cudaStream_t stream) {
+    if (tma_can_tile(a)) return a.D == 128 ? launch_m<128, true>(a, maps, grid, stream) : launch_m<64, true>(a, maps, grid, stream);
+    return a.D == 128 ? launch_m<128, false>(a, maps, grid, stream) : launch_m<64, false>(a, maps, grid, stream);
+}
+
+}  // namespace lethe

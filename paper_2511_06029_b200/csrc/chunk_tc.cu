@@ -1,0 +1,591 @@
+// lethe_chunk_attend, the attention itself, on the fifth-generation tensor cores (bf16 and byte caches).
+//
+// S = Q K^T and O += P V with tcgen05.mma: the 128 x 128 fp32 logits and the 128 x D outputs live in tensor memory, the softmax
+// threads read a row each, write the probabilities back as bf16 over the logits they came from, and those are the A operand of the
+// second product where they lie.  A CTA holds two row tiles (two softmax groups of four warps), so one group's exponentials run
+// under the other's products.  A unit with one row tile only (few new tokens) gives both groups alternate key tiles of it instead
+// and merges their halves at the end.  Row maxima are followed lazily: the outputs are rescaled only when a maximum has grown by
+// more than 2^8 since the last time, which a row's first few tiles settle; the sums stay far inside fp32.
+//
+// Roles: warps 0-7 softmax; warp 8 issues the MMAs; warp 9 fetches the query tiles; warp 10 K and V tiles by TMA (one thread) or,
+// for byte caches and odd page sizes, warps 10-13 read, convert and store them (exact: e4m3 and e5m2 are bf16 values).  K and V tiles alternate in a ring.  Negative scales flip the sign of Q inside the MMA.
+#include <string.h>
+
+#include "chunk_tc.cuh"
+
+namespace lethe {
+namespace {
+
+constexpr int kSoftWarps = 8;
+constexpr int kMmaWarp = 8;
+constexpr int kQWarp = 9;
+constexpr int kLoadWarp = 10;    // TMA
+constexpr int kGatherWarp = 10;  // four warps
+constexpr int kMaxStages = 8;
+constexpr float kLazy = 8.f;  // log2 of the growth of a row maximum that is left standing
+
+template <bool TMA>
+__host__ __device__ constexpr int tc_threads() { return (TMA ? kLoadWarp + 1 : kGatherWarp + 4) * 32; }
+template <int D>
+__host__ __device__ constexpr int stages() { return D == 128 ? 4 : 8; }
+template <int D>
+constexpr size_t smem_bytes() { return 1024 + (size_t)(2 + stages<D>()) * tile_bytes<D>(); }
+
+struct Shared {
+    unsigned long long full[kMaxStages], empty[kMaxStages];
+    unsigned long long q_full, q_done, q_soft, merge;
+    unsigned long long s_full[2], p_full[2], o_full[2];
+    unsigned long long drained;
+    uint32_t tmem_base;
+    int abort;
+    int loaded, q_loaded, issued;  // ring entries, query loads and MMAs started (for the drain after a timeout)
+    float2 merge_ml[kTile];
+    alignas(16) int kpos[kSoftWarps][kTile];     // positions of the tile's keys, one copy per warp
+    alignas(16) float kposf[kSoftWarps][kTile];  // the same relative to the unit's first query
+};
+
+// A CTA's piece of a unit, as every role derives it from the plan.
+struct Piece {
+    ChunkItem it;
+    int tok0, toks;  // tokens of the unit
+    int tile0, nt;   // key tiles
+    int hi;          // slots from here on are hidden from the whole unit
+    bool alt;        // one row tile, the groups take alternate key tiles
+    bool head, tail; // begins / ends here
+};
+
+__device__ __forceinline__ Piece piece_of(const ChunkArgs& a, int u, int at, int stop, int s0, int s1) {
+    Piece p;
+    const int idx = u / a.QT;
+    p.tok0 = (u - idx * a.QT) * a.TU;
+    p.it = chunk_item(a, idx);
+    p.toks = min(p.it.T - p.tok0, a.TU);
+    p.hi = a.u_hi ? a.u_hi[u] : (a.append ? p.it.n_old + p.tok0 + p.toks : p.it.n_old);
+    p.tile0 = (a.u_lo ? a.u_lo[u] : 0) + at - s0;
+    p.nt = stop - at;
+    p.alt = p.toks <= a.TT;
+    p.head = at == s0;
+    p.tail = stop == s1;
+    return p;
+}
+
+// Calls f(piece) for each piece of this CTA, in order; f returns false to stop.
+template <typename F>
+__device__ __forceinline__ void for_pieces(const ChunkArgs& a, F f) {
+    const int total = a.plan->total, per = a.plan->per;
+    const int begin = min(total, (int)blockIdx.x * per), end = min(total, begin + per);
+    if (begin >= end) return;
+    int u = find_start(a.u_start, a.n_units, begin), s0 = a.u_start[u];
+    for (int at = begin; at < end; ++u) {
+        const int s1 = a.u_start[u + 1];
+        if (s1 > at) {
+            const int stop = min(end, s1);
+            if (!f(piece_of(a, u, at, stop, s0, s1))) return;
+            at = stop;
+        }
+        s0 = s1;
+    }
+}
+
+template <int D, bool TMA, bool MOD>
+__global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps) {
+    constexpr int TILE = tile_bytes<D>(), NS = stages<D>(), KS = D / 16;
+    constexpr int kOCol = 256;  // tensor memory: S0 | S1 | O0 | O1, 128 columns each (P over its S)
+    extern __shared__ unsigned char dyn_raw[];
+    __shared__ Shared sh;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t q_tile = (smem_u32(dyn_raw) + 1023u) & ~1023u;
+    const uint32_t ring = q_tile + 2 * TILE;
+    unsigned char* const q_generic = dyn_raw + (q_tile - smem_u32(dyn_raw));
+    volatile int* abort_flag = &sh.abort;
+    const int limit = a.wait_limit > 0 ? a.wait_limit : kChunkWaitLimit;
+    const int used = a.TT * a.G;
+
+    if (tid == 0) {
+        for (int i = 0; i < NS; ++i) {
+            bar_init(&sh.full[i], TMA ? 1 : 4);
+            bar_init(&sh.empty[i], 1);
+        }
+        bar_init(&sh.q_full, 1);
+        bar_init(&sh.q_done, 1);
+        bar_init(&sh.q_soft, kSoftWarps);
+        bar_init(&sh.merge, 4);
+        for (int g = 0; g < 2; ++g) {
+            bar_init(&sh.s_full[g], 1);
+            bar_init(&sh.p_full[g], 4);
+            bar_init(&sh.o_full[g], 1);
+        }
+        bar_init(&sh.drained, 1);
+        sh.abort = sh.loaded = sh.q_loaded = sh.issued = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    dependency_wait();
+    dependency_release();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = sh.tmem_base;
+
+    if (warp >= kLoadWarp) {
+        // ------------------------------------------------------------------ K and V tiles
+        bool bad = false;
+        int e = 0;
+        if (TMA) {
+            if (lane == 0) {
+                for_pieces(a, [&](const Piece& p) {
+                    for (int t = 0; t < 2 * p.nt; ++t, ++e) {
+                        const int s = e % NS;
+                        if (e >= NS && !bar_wait(&sh.empty[s], e / NS - 1, abort_flag, limit)) return false;
+                        bar_expect_tx(&sh.full[s], TILE);
+                        sh.loaded = e + 1;
+                        tma_tile<D>(a, (t & 1) ? &maps.v : &maps.k, p.it.item, p.it.n, (p.tile0 + (t >> 1)) * kTile, ring + s * TILE, &sh.full[s], &bad);
+                    }
+                    if (bad) record_error(a.status, LETHE_ERR_PAGE, p.it.item);
+                    bad = false;
+                    return true;
+                });
+            }
+            __syncwarp();
+        } else {
+            for_pieces(a, [&](const Piece& p) {
+                for (int t = 0; t < 2 * p.nt; ++t, ++e) {
+                    const int s = e % NS;
+                    if (e >= NS && !warp_wait(&sh.empty[s], e / NS - 1, abort_flag, limit)) return false;
+                    gather_tile<D>(a, (t & 1) ? a.v : a.k, p.it.item, p.hi, (p.tile0 + (t >> 1)) * kTile, ring + s * TILE, tid - kGatherWarp * 32, 128, &bad);
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sh.full[s]);
+                }
+                if (bad) record_error(a.status, LETHE_ERR_PAGE, p.it.item);
+                bad = false;
+                return true;
+            });
+        }
+    } else if (warp == kQWarp) {
+        // ------------------------------------------------------------------ query tiles
+        if (lane == 0) {
+            int k = 0;
+            for_pieces(a, [&](const Piece& p) {
+                // the previous unit's products have read the tiles, and its softmax groups are done with them as merge space
+                if (k > 0 && (!bar_wait(&sh.q_done, k - 1, abort_flag, limit) || !bar_wait(&sh.q_soft, k - 1, abort_flag, limit))) return false;
+                const int tiles = p.alt ? 1 : 2;
+                bar_expect_tx(&sh.q_full, (unsigned)(tiles * used * D * 2));
+                sh.q_loaded = k + 1;
+                for (int g = 0; g < tiles; ++g)
+#pragma unroll
+                    for (int hf = 0; hf < D / 64; ++hf)
+                        tma_4d(q_tile + g * TILE + hf * kHalfBytes, &maps.q, 64 * hf, p.it.hkv * a.G, p.it.first + p.tok0 + g * a.TT, p.it.li, &sh.q_full);
+                ++k;
+                return true;
+            });
+        }
+        __syncwarp();
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------------ MMA issue
+        if (lane == 0) {
+            const uint32_t pv_desc = mma_idesc(D, true, false);
+            int k = 0, base = 0;              // pieces done, first ring entry of the piece
+            int jobs_p[2] = {0, 0};           // probabilities consumed so far, per group
+            for_pieces(a, [&](const Piece& p) {
+                const uint32_t qk_desc = mma_idesc(kTile, false, a.scale[p.it.l] < 0.f);
+                const int jobs = p.alt ? p.nt : 2 * p.nt;
+                if (!bar_wait(&sh.q_full, k, abort_flag, limit)) return false;
+                auto entry_full = [&](int e) { return bar_wait(&sh.full[e % NS], e / NS, abort_flag, limit); };
+                for (int i = 0; i < jobs + 2; ++i) {
+                    if (i >= 2) {  // P V of job i - 2
+                        const int j = i - 2, g = j & 1, t = p.alt ? j : j >> 1;
+                        if (j < jobs) {
+                            const int e = base + 2 * t + 1;
+                            if (!entry_full(e)) return false;
+                            if (!bar_wait(&sh.p_full[g], jobs_p[g]++, abort_flag, limit)) return false;
+                            tc_after();
+                            const int valid = min(kTile, p.hi - (p.tile0 + t) * kTile);
+                            const int steps = max(1, (valid + 15) / 16);
+                            const uint32_t vt = ring + (e % NS) * TILE, pt = tmem + g * 128, ot = tmem + kOCol + g * 128;
+                            const bool first = p.alt ? t < 2 : t == 0;
+#pragma unroll
+                            for (int ks = 0; ks < kTile / 16; ++ks)
+                                if (ks < steps) mma_ts(ot, pt + ks * 8, smem_desc(vt + ks * 2048, kHalfBytes), pv_desc, !first || ks > 0);
+                            sh.issued = 1;
+                            tc_commit(&sh.o_full[g]);
+                            if (p.alt || g == 1) tc_commit(&sh.empty[e % NS]);
+                        }
+                    }
+                    if (i < jobs) {  // Q K^T of job i
+                        const int g = i & 1, t = p.alt ? i : i >> 1, e = base + 2 * t;
+                        if (!entry_full(e)) return false;
+                        tc_after();
+                        const uint32_t qt = q_tile + (p.alt ? 0 : g) * TILE, kt = ring + (e % NS) * TILE;
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) {
+                            const uint32_t off = (ks >> 2) * kHalfBytes + (ks & 3) * 32;
+                            mma_ss(tmem + g * 128, smem_desc(qt + off, 16), smem_desc(kt + off, 16), qk_desc, ks > 0);
+                        }
+                        sh.issued = 1;
+                        tc_commit(&sh.s_full[g]);
+                        if (p.alt || g == 1) tc_commit(&sh.empty[e % NS]);
+                        if (i == jobs - 1) tc_commit(&sh.q_done);
+                    }
+                }
+                base += 2 * p.nt;
+                ++k;
+                return true;
+            });
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ softmax
+        const int g = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;  // group, TMEM lane
+        const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + g * 128;
+        const uint32_t o_addr = s_addr + kOCol;
+        const bool by_pos = MOD && (a.slopes || a.window > 0 || a.doc_start || a.prefix_len);
+        const bool mask_pos = MOD && (a.window > 0 || a.doc_start || a.prefix_len);
+        int n_s = 0, n_o = 0, n_v = 0, k = 0, n_m = 0;  // logit tiles, output products and ring entries so far; pieces, merged pieces
+        for_pieces(a, [&](const Piece& p) {
+            const int tile_rows = min(used, p.toks * a.G - (p.alt ? 0 : g * used));
+            const bool valid_row = r < tile_rows;
+            const bool busy = quarter * 32 < tile_rows;  // the warp has rows at all
+            const int tok = p.tok0 + (p.alt ? 0 : g * a.TT) + min(r, tile_rows - 1) / a.G, h = r % a.G;
+            // a scale of zero is a very small one here, so that a hidden key's -inf stays one
+            const float scale = fabsf(a.scale[p.it.l]) * a.k_scale[p.it.l], sl2 = fmaxf(scale * 1.4426950408889634f, 1e-36f);
+            // rows that are not there count as seeing everything: they never ask for a mask
+            const int lim = valid_row && a.append ? p.it.n_old + tok + 1 : INT32_MAX;
+            int qpos = 0, lo = INT32_MIN, pos0 = 0, prefix = INT32_MIN;
+            float slope = 0.f, qf = 0.f, cap_in = 0.f, cap2 = 0.f;
+            if (MOD) {
+                if (a.token_pos) {
+                    qpos = a.token_pos[p.it.first + tok];
+                    pos0 = a.token_pos[p.it.first + p.tok0];
+                    qf = (float)((long long)qpos - pos0);
+                }
+                if (valid_row) lo = chunk_lo(a, p.it.first + tok, qpos);
+                if (a.prefix_len) prefix = a.prefix_len[p.it.b];
+                if (a.slopes) slope = a.slopes[p.it.hkv * a.G + h] * 1.4426950408889634f;
+                if (a.softcap > 0.f) {
+                    cap_in = scale / a.softcap;
+                    cap2 = a.softcap * 1.4426950408889634f;
+                }
+            }
+            float m = -INFINITY, l = 0.f;
+            const int jobs = p.alt ? p.nt : 2 * p.nt;
+            int done = 0;  // jobs of this group in the piece
+            for (int i = g; i < jobs; i += 2, ++done) {
+                const int t = p.alt ? i : i >> 1, j0 = (p.tile0 + t) * kTile;
+                int kp_min = INT32_MIN;
+                if (MOD && by_pos && busy) {  // positions of the tile's keys, while the product runs
+                    const int32_t* pos = a.pos + (size_t)p.it.item * a.cap_tokens + j0;
+                    kp_min = INT32_MAX;
+                    __syncwarp();
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int kp = j0 + c * 32 + lane < p.it.n ? pos[c * 32 + lane] : INT32_MAX;
+                        sh.kpos[warp][c * 32 + lane] = kp;
+                        sh.kposf[warp][c * 32 + lane] = (float)((long long)kp - pos0);
+                        kp_min = min(kp_min, kp);
+                    }
+                    kp_min = __reduce_min_sync(0xffffffffu, kp_min);
+                    __syncwarp();
+                }
+                const int valid = min(kTile, p.hi - j0);
+                if (valid < kTile && (valid <= 0 || (valid & 15))) {
+                    // rows behind the last slot may hold anything, and 0 x NaN is NaN: clear those the product's last step takes in
+                    const int e = n_v + 2 * t + 1, r0 = max(valid, 0), rows = max(16, (valid + 15) & ~15) - r0;
+                    if (!warp_wait(&sh.full[e % NS], e / NS, abort_flag, limit)) return false;
+                    for (int x = r; x < rows * (D / 8); x += kTile) st_shared_16(chunk_addr(ring + (e % NS) * TILE, r0 + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
+                    proxy_fence();
+                }
+                if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
+                tc_after();
+                if (busy) {
+                    // The row in two halves of 64 logits: the first is shaped, its maximum taken and (if shaping changed it) put back,
+                    // the second stays in registers; after the maximum the second half's probabilities are formed, then the first
+                    // half is read again, then both are stored (the second half's land on the first half's logits).
+                    uint32_t v[64], pk[32];
+                    float ml = sl2;  // what a logit still has to be multiplied by to be in log2 units
+                    float top = -INFINITY;
+                    bool shaped = false;
+                    auto half_max = [&](const int c0) {
+                        if (MOD) {
+                            ml = sl2;
+                            if (a.softcap > 0.f) {
+                                ml = 1.f;
+                                shaped = true;
+#pragma unroll
+                                for (int c = 0; c < 64; c += 8) {
+                                    float x[8], big = 0.f;
+#pragma unroll
+                                    for (int y = 0; y < 8; ++y) {
+                                        x[y] = __uint_as_float(v[c + y]) * cap_in;
+                                        big = fmaxf(big, fabsf(x[y]));
+                                        v[c + y] = __float_as_uint(cap2 * capped_small(x[y]));
+                                    }
+                                    if (__any_sync(0xffffffffu, big > 0.55f)) {
+#pragma unroll
+                                        for (int y = 0; y < 8; ++y)
+                                            if (fabsf(x[y]) > 0.55f) v[c + y] = __float_as_uint(cap2 * capped_large(x[y]));
+                                    }
+                                }
+                            }
+                            if (a.slopes) {
+                                shaped = true;
+#pragma unroll
+                                for (int c = 0; c < 64; c += 4) {
+                                    const float4 kf = *reinterpret_cast<const float4*>(&sh.kposf[warp][c0 + c]);
+                                    v[c] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.x), __uint_as_float(v[c]) * ml));
+                                    v[c + 1] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.y), __uint_as_float(v[c + 1]) * ml));
+                                    v[c + 2] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.z), __uint_as_float(v[c + 2]) * ml));
+                                    v[c + 3] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.w), __uint_as_float(v[c + 3]) * ml));
+                                }
+                                ml = 1.f;
+                            }
+                        }
+                        if (MOD && mask_pos) {
+                            if (!__all_sync(0xffffffffu, kp_min >= lo && lim - j0 >= kTile && p.it.n - j0 >= kTile)) {
+                                const int nn = p.it.n - j0 - c0, nv = lim == INT32_MAX ? nn : lim - j0 - c0;
+                                shaped = true;
+#pragma unroll
+                                for (int c = 0; c < 64; c += 4) {
+                                    const int4 kp = *reinterpret_cast<const int4*>(&sh.kpos[warp][c0 + c]);
+                                    if (!((c < nv || (kp.x < prefix && c < nn)) && kp.x >= lo)) v[c] = 0xff800000u;
+                                    if (!((c + 1 < nv || (kp.y < prefix && c + 1 < nn)) && kp.y >= lo)) v[c + 1] = 0xff800000u;
+                                    if (!((c + 2 < nv || (kp.z < prefix && c + 2 < nn)) && kp.z >= lo)) v[c + 2] = 0xff800000u;
+                                    if (!((c + 3 < nv || (kp.w < prefix && c + 3 < nn)) && kp.w >= lo)) v[c + 3] = 0xff800000u;
+                                }
+                            }
+                        } else {
+                            const int nv = min(lim, p.it.n) - j0 - c0;  // keys of this half that the row sees
+                            if (__any_sync(0xffffffffu, nv < 64)) {
+                                shaped = true;
+#pragma unroll
+                                for (int c = 0; c < 64; ++c)
+                                    if (c >= nv) v[c] = 0xff800000u;
+                            }
+                        }
+                        float m0 = top, m1 = __uint_as_float(v[1]), m2 = __uint_as_float(v[2]), m3 = __uint_as_float(v[3]);
+                        m0 = fmaxf(m0, __uint_as_float(v[0]));
+#pragma unroll
+                        for (int c = 4; c < 64; c += 4) {
+                            m0 = fmaxf(m0, __uint_as_float(v[c]));
+                            m1 = fmaxf(m1, __uint_as_float(v[c + 1]));
+                            m2 = fmaxf(m2, __uint_as_float(v[c + 2]));
+                            m3 = fmaxf(m3, __uint_as_float(v[c + 3]));
+                        }
+                        top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+                    };
+                    tmem_ld32(s_addr, v);
+                    tmem_ld32(s_addr + 32, v + 32);
+                    tmem_ld_wait();
+                    half_max(0);
+                    if (shaped) {  // uniform for the warp
+                        tmem_st32(s_addr, v);
+                        tmem_st32(s_addr + 32, v + 32);
+                    }
+                    tmem_ld32(s_addr + 64, v);
+                    tmem_ld32(s_addr + 96, v + 32);
+                    tmem_ld_wait();
+                    half_max(64);
+                    const float mt = top * ml;
+                    const bool grow = valid_row && mt > m + kLazy;  // true from -inf too
+                    if (__any_sync(0xffffffffu, grow)) {
+                        const float w = grow ? exp2_diff(m, mt) : 1.f;
+                        if (grow) m = mt;
+                        l *= w;
+                        if (done > 0) {
+                            if (!warp_wait(&sh.o_full[g], n_o + done - 1, abort_flag, limit)) return false;
+                            tc_after();
+#pragma unroll
+                            for (int c = 0; c < D; c += 32) {
+                                tmem_ld32(o_addr + c, pk);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int y = 0; y < 32; ++y) pk[y] = __float_as_uint(__uint_as_float(pk[y]) * w);
+                                tmem_st32(o_addr + c, pk);
+                            }
+                        }
+                    }
+                    const float nm = m == -INFINITY ? 0.f : -m;
+                    float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+                    auto half_exp = [&]() {
+#pragma unroll
+                        for (int y = 0; y < 64; y += 4) {
+                            const float p0 = fast_exp2(fmaf(__uint_as_float(v[y]), ml, nm)), p1 = fast_exp2(fmaf(__uint_as_float(v[y + 1]), ml, nm));
+                            const float p2 = fast_exp2(fmaf(__uint_as_float(v[y + 2]), ml, nm)), p3 = fast_exp2(fmaf(__uint_as_float(v[y + 3]), ml, nm));
+                            l0 += p0;
+                            l1 += p1;
+                            l2 += p2;
+                            l3 += p3;
+                            pk[y / 2] = pack_bf16(p0, p1);
+                            pk[y / 2 + 1] = pack_bf16(p2, p3);
+                        }
+                    };
+                    half_exp();
+                    if (shaped) tmem_st_wait();
+                    tmem_ld32(s_addr, v);
+                    tmem_ld32(s_addr + 32, v + 32);
+                    tmem_ld_wait();
+                    tmem_st32(s_addr + 32, pk);
+                    half_exp();
+                    tmem_st32(s_addr, pk);
+                    l += (l0 + l1) + (l2 + l3);
+                    tmem_st_wait();
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.p_full[g]);
+            }
+            n_v += 2 * p.nt;
+            // ---- the piece's outputs
+            if (done > 0 && !warp_wait(&sh.o_full[g], n_o + done - 1, abort_flag, limit)) return false;
+            n_o += done;
+            tc_after();
+            float* const merge_o = reinterpret_cast<float*>(q_generic);  // [D][128]: the query tiles have been read by then
+            if (p.alt) {
+                if (g == 1) {
+                    if (!warp_wait(&sh.q_done, k, abort_flag, limit)) return false;
+                    if (busy) {
+                        sh.merge_ml[r] = make_float2(m, l);
+                        if (done > 0) {
+#pragma unroll
+                            for (int c = 0; c < D; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(o_addr + c, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int y = 0; y < 32; ++y) merge_o[(c + y) * kTile + r] = __uint_as_float(o[y]);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sh.merge);
+                } else if (!warp_wait(&sh.merge, n_m, abort_flag, limit)) return false;
+            }
+            n_m += p.alt;
+            if (busy && !(p.alt && g == 1)) {
+                float w0 = 1.f, w1 = 0.f;
+                if (p.alt) {
+                    const float2 other = sh.merge_ml[r];
+                    const float mx = fmaxf(m, other.x);
+                    w0 = exp2_diff(m, mx);
+                    w1 = exp2_diff(other.x, mx);
+                    l = l * w0 + other.y * w1;
+                    m = mx;
+                }
+                const bool whole = p.head && p.tail;
+                const bool add = p.alt && jobs > 1;
+                const size_t orow = ((size_t)p.it.li * a.n_tokens + p.it.first + tok) * a.Hq + p.it.hkv * a.G + h;
+                const size_t part = (((size_t)blockIdx.x * 2 + (p.head ? 1 : 0)) * 2 + (p.alt ? 0 : g)) * kChunkPartRows + r;
+                const float mul = !whole ? 1.f : (l == 0.f ? 0.f : a.v_scale[p.it.l] / l);
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(o_addr + c, o);
+                    tmem_ld_wait();
+                    float f[32];
+#pragma unroll
+                    for (int y = 0; y < 32; ++y) {
+                        float x = __uint_as_float(o[y]);
+                        if (l == 0.f) x = 0.f;
+                        if (p.alt) x = add ? (w0 == 0.f ? 0.f : x * w0) + (w1 == 0.f ? 0.f : merge_o[(c + y) * kTile + r] * w1) : x * w0;
+                        f[y] = x * mul;
+                    }
+                    if (valid_row) {
+                        if (whole) {
+                            uint4* d = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + orow * D + c);
+#pragma unroll
+                            for (int y = 0; y < 4; ++y)
+                                d[y] = make_uint4(pack_bf16(f[8 * y], f[8 * y + 1]), pack_bf16(f[8 * y + 2], f[8 * y + 3]), pack_bf16(f[8 * y + 4], f[8 * y + 5]), pack_bf16(f[8 * y + 6], f[8 * y + 7]));
+                        } else {
+                            float4* d = reinterpret_cast<float4*>(a.part_o + part * D + c);
+#pragma unroll
+                            for (int y = 0; y < 8; ++y) d[y] = make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
+                        }
+                    }
+                }
+                if (valid_row) {
+                    if (!whole) a.part_ml[part] = make_float2(m, l);
+                    else {
+                        const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+                        if (a.lse) a.lse[orow] = lse2 * 0.6931471805599453f;
+                        a.nlse2[(((size_t)p.it.li * a.Hkv + p.it.hkv) * a.n_tokens + p.it.first + tok) * a.G + h] = l == 0.f ? -INFINITY : -lse2;
+                    }
+                }
+            }
+            tc_before();   // O has been read: the next unit's first product may overwrite it (ordered by p_full)
+            proxy_fence(); // the merge space goes back to the query loads
+            __syncwarp();
+            if (lane == 0) bar_arrive(&sh.q_soft);
+            ++k;
+            return true;
+        });
+    }
+
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (sh.abort) {  // uniform for the CTA: see everything this CTA has started end
+        if (tid == 0) record_error(a.status, LETHE_ERR_TIMEOUT, blockIdx.x);
+        if (warp == kMmaWarp && lane == 0 && sh.issued) {
+            tc_commit(&sh.drained);
+            bar_drain(&sh.drained, 0);
+        }
+        if (TMA && warp == kLoadWarp && lane == 0)
+            for (int e = max(0, sh.loaded - NS); e < sh.loaded; ++e) bar_drain(&sh.full[e % NS], e / NS);
+        if (warp == kQWarp && lane == 0 && sh.q_loaded > 0) bar_drain(&sh.q_full, sh.q_loaded - 1);
+        tc_before();
+        __syncthreads();
+        tc_after();
+    }
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+template <int D, bool TMA, bool MOD>
+cudaError_t launch_t(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
+    cudaError_t e = prepare_kernel((const void*)chunk_tc_attend<D, TMA, MOD>, smem_bytes<D>());
+    if (e != cudaSuccess) return e;
+    if (e == cudaSuccess) e = launch_dependent(chunk_tc_attend<D, TMA, MOD>, dim3(a.n_cta), tc_threads<TMA>(), smem_bytes<D>(), stream, a, maps);
+    return e;
+}
+
+template <int D, bool TMA>
+cudaError_t launch_m(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
+    const bool mod = a.softcap > 0.f || a.slopes || a.window > 0 || a.doc_start || a.prefix_len;
+    return mod ? launch_t<D, TMA, true>(a, maps, stream) : launch_t<D, TMA, false>(a, maps, stream);
+}
+
+}  // namespace
+
+bool build_chunk_maps(void* encode, const ChunkArgs& a, int n_layers, ChunkMaps* maps) {
+    typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    encode_fn fn = reinterpret_cast<encode_fn>(encode);
+    memset(maps, 0, sizeof(*maps));
+    const cuuint32_t es[4] = {1, 1, 1, 1};
+    const cuuint64_t D = a.D;
+    const cuuint64_t qd[4] = {D, (cuuint64_t)a.Hq, (cuuint64_t)a.n_tokens, (cuuint64_t)a.nl};
+    const cuuint64_t qs[3] = {D * 2, a.Hq * D * 2, (cuuint64_t)a.n_tokens * a.Hq * D * 2};
+    const cuuint32_t qb[4] = {64, (cuuint32_t)a.G, (cuuint32_t)a.TT, 1};
+    if (fn(&maps->q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(a.q), qd, qs, qb, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return false;
+    if (!tma_can_tile(a)) return true;
+    const cuuint64_t rows = a.paged ? (cuuint64_t)a.page_tokens : (cuuint64_t)a.capacity;
+    const cuuint64_t kd[3] = {D, rows, a.paged ? (cuuint64_t)a.n_pages : (cuuint64_t)n_layers * a.B * a.Hkv};
+    const cuuint64_t ks[2] = {D * 2, rows * D * 2};
+    const cuuint32_t kb[3] = {64, a.paged ? (cuuint32_t)a.page_tokens : (cuuint32_t)kTile, 1};
+    for (int i = 0; i < 2; ++i)
+        if (fn(i ? &maps->v : &maps->k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(i ? a.v : a.k), kd, ks, kb, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return false;
+    return true;
+}
+
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
+    if (tma_can_tile(a)) return a.D == 128 ? launch_m<128, true>(a, maps, stream) : launch_m<64, true>(a, maps, stream);
+    return a.D == 128 ? launch_m<128, false>(a, maps, stream) : launch_m<64, false>(a, maps, stream);
+}
+
+}  // namespace lethe

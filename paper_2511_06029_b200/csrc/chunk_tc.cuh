@@ -1,0 +1,258 @@
+// PTX wrappers and operand layouts shared by the tensor-core kernels of lethe_chunk_attend (tcgen05, TMA, mbarriers).
+#pragma once
+#include <cuda.h>
+
+#include "chunk.cuh"
+#include "mma_utils.cuh"
+
+namespace lethe {
+
+// Tensor maps: K and V as [items or pages][rows][D], Q as [nl][n_tokens][Hq][D]; 64-element (128-byte) inner boxes, 128-byte swizzle.
+struct alignas(64) ChunkMaps {
+    CUtensorMap k, v, q;
+};
+
+namespace {
+
+constexpr int kTile = kChunkTile;          // rows of every operand tile
+constexpr int kHalfBytes = kTile * 128;    // 64 elements of each of a tile's rows: one swizzled region
+constexpr int kChunkWaitLimit = 400000;
+
+template <int D>
+__host__ __device__ constexpr int tile_bytes() { return kTile * D * 2; }
+
+__device__ __forceinline__ void bar_init(unsigned long long* b, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(unsigned long long* b) {
+    asm volatile("{ .reg .b64 st; mbarrier.arrive.shared::cta.b64 st, [%0]; }" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect_tx(unsigned long long* b, unsigned bytes) {
+    asm volatile("{ .reg .b64 st; mbarrier.arrive.expect_tx.shared::cta.b64 st, [%0], %1; }" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(unsigned long long* b, unsigned parity) {
+    unsigned ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool bar_test(unsigned long long* b, unsigned parity) {
+    unsigned ok;
+    asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded wait for the completion of phase `phase` (0, 1, 2, ...); false = gave up, or another thread already did.  The first look
+// never blocks.
+__device__ __forceinline__ bool bar_wait(unsigned long long* b, unsigned phase, volatile int* abort_flag, int limit) {
+    const unsigned parity = phase & 1;
+    if (bar_test(b, parity)) return true;
+    for (int it = 1; it < limit; ++it) {
+        if (bar_try(b, parity)) return true;
+        if (*abort_flag) return false;
+        if (it > 64) __nanosleep(64);
+    }
+    *abort_flag = 1;
+    return false;
+}
+// The same for a whole warp, which goes on or gives up as one (collective instructions follow).
+__device__ __forceinline__ bool warp_wait(unsigned long long* b, unsigned phase, volatile int* abort_flag, int limit) {
+    return __all_sync(0xffffffffu, bar_wait(b, phase, abort_flag, limit));
+}
+// The same with the built-in limit and no abort flag: for what a CTA has started itself and must see end before it returns.
+__device__ __forceinline__ void bar_drain(unsigned long long* b, unsigned phase) {
+    for (int it = 0; it < kChunkWaitLimit; ++it) {
+        if (bar_try(b, phase & 1)) return;
+        if (it > 64) __nanosleep(64);
+    }
+}
+
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(unsigned long long* b) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, unsigned long long* b) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, unsigned long long* b) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(b)) : "memory");
+}
+
+// Shared-memory descriptor of a tile kept as rows of 128 bytes with the 128-byte swizzle, 8-row groups 1024 bytes apart.
+// K-major (the row is the M or N axis): the leading offset is unused.  MN-major (the row is the contraction axis, 64 elements of
+// the other axis along it): the leading offset leads to the next 64 elements, one region further.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t leading) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(leading >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+// tcgen05.mma.kind::f16, bf16 x bf16 -> fp32, M = 128, N columns; B K-major or MN-major, A optionally negated.
+__device__ __forceinline__ uint32_t mma_idesc(int N, bool b_mn_major, bool negate_a) {
+    uint32_t d = 0;
+    d |= 1u << 4;
+    d |= 1u << 7;
+    d |= 1u << 10;
+    d |= (negate_a ? 1u : 0u) << 13;
+    d |= (b_mn_major ? 1u : 0u) << 16;
+    d |= (uint32_t)(N >> 3) << 17;
+    d |= (uint32_t)(kTile >> 4) << 24;
+    return d;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// 32 consecutive columns of this thread's TMEM lane (asynchronous: ld_wait before the registers are used).
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+          "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]),
+          "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]),
+          "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void st_shared_16(uint32_t addr, const uint4& x) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+// 16-byte chunk c of row r of a tile: halves of 64 elements are separate regions, chunks are swizzled by the row.
+__device__ __forceinline__ uint32_t chunk_addr(uint32_t tile, int r, int c) {
+    return tile + (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+}
+
+// One box of K or V rows [j0, j0 + 128) by TMA: a contiguous item in one box per 64 elements, a paged one page by page.  Rows past
+// the item's capacity, pages past its last slot and ids outside the pool read as zeros (coordinates outside the map).
+template <int D>
+__device__ __forceinline__ void tma_tile(const ChunkArgs& a, const CUtensorMap* map, int item, int n, int j0, uint32_t dst, unsigned long long* bar, bool* bad) {
+    if (!a.paged) {
+#pragma unroll
+        for (int hf = 0; hf < D / 64; ++hf) tma_3d(dst + hf * kHalfBytes, map, 64 * hf, j0, item, bar);
+        return;
+    }
+    const int pt = a.page_tokens, per_tile = kTile / pt;  // pt is 8 .. 128 and divides 128
+    const int32_t* table = a.page_table + (size_t)item * a.capacity + j0 / pt;
+#pragma unroll 8
+    for (int pg = 0; pg < per_tile; ++pg) {
+        int page = (int)a.n_pages;  // outside the map: zeros
+        if (j0 + pg * pt < n) {
+            page = table[pg];
+            if (page < 0 || page >= a.n_pages) {
+                *bad = true;
+                page = (int)a.n_pages;
+            }
+        }
+#pragma unroll
+        for (int hf = 0; hf < D / 64; ++hf) tma_3d(dst + hf * kHalfBytes + pg * pt * 128, map, 64 * hf, 0, page, bar);
+    }
+}
+
+// Sixteen bytes of a bf16 operand row (8 elements) from stored K or V: bf16 as it is, 8-bit floats converted (exact).
+__device__ __forceinline__ uint4 expand8(uint2 w, bool e5m2) {
+    uint32_t h[4];
+    if (e5m2) {  // an e5m2 byte is the upper byte of the half of the same value
+        h[0] = __byte_perm(w.x, 0u, 0x1404); h[1] = __byte_perm(w.x, 0u, 0x3424);
+        h[2] = __byte_perm(w.y, 0u, 0x1404); h[3] = __byte_perm(w.y, 0u, 0x3424);
+    } else {
+        asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi; }" : "=r"(h[0]), "=r"(h[1]) : "r"(w.x));
+        asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi; }" : "=r"(h[2]), "=r"(h[3]) : "r"(w.y));
+    }
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.f32.f16 %0, l; cvt.f32.f16 %1, h; }" : "=f"(lo), "=f"(hi) : "r"(h[i]));
+        o[i] = pack_bf16(lo, hi);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// The same tile by `nt` threads with plain loads: any page size, any storage type.  Rows at or beyond `end` are zeros.
+template <int D>
+__device__ __forceinline__ void gather_tile(const ChunkArgs& a, const void* base, int item, int end, int j0, uint32_t dst, int tid, int nt, bool* bad) {
+    constexpr int C = D / 8;       // 16-byte operand chunks per row
+    constexpr int U = 4;           // chunks a thread has in flight
+    const bool bytes = a.dtype != LETHE_BF16, e5m2 = a.dtype == LETHE_FP8_E5M2;
+    for (int i0 = tid; i0 < kTile * C; i0 += U * nt) {
+        uint4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * nt, r = i / C, c = i % C;
+            x[u] = make_uint4(0, 0, 0, 0);
+            if (i < kTile * C && j0 + r < end) {
+                const long long at = chunk_row(a, item, j0 + r);
+                if (at < 0) *bad = true;
+                else if (!bytes) x[u] = reinterpret_cast<const uint4*>((const char*)base + (size_t)at * (D * 2))[c];
+                else {
+                    const uint2 w = reinterpret_cast<const uint2*>((const char*)base + (size_t)at * D)[c];
+                    x[u].x = w.x;
+                    x[u].y = w.y;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * nt;
+            if (i < kTile * C) st_shared_16(chunk_addr(dst, i / C, i % C), bytes ? expand8(make_uint2(x[u].x, x[u].y), e5m2) : x[u]);
+        }
+    }
+}
+
+// First unit whose tiles reach beyond `tile` on the plan's line (u_start is non-decreasing; units without tiles are passed over).
+__device__ __forceinline__ int find_start(const int* start, int n, int tile) {
+    int lo = 0, hi = n;  // the last with start <= tile
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= tile) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Whether K and V tiles can come by TMA: bf16 rows, and pages that tile the 128 rows in whole swizzle groups.
+inline bool tma_can_tile(const ChunkArgs& a) {
+    if (a.dtype != LETHE_BF16) return false;
+    return !a.paged || (a.page_tokens >= 8 && kTile % a.page_tokens == 0 && a.n_pages <= 0x7ffffffeLL);
+}
+
+}  // namespace
+
+// encode: cuTensorMapEncodeTiled; false = a map could not be made.
+bool build_chunk_maps(void* encode, const ChunkArgs& a, int n_layers, ChunkMaps* maps);
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream);
+cudaError_t launch_chunk_rel_tc(const ChunkArgs& a, const ChunkMaps& maps, int grid, cudaStream_t stream);
+
+}  // namespace lethe
