@@ -290,16 +290,18 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     kp_min = __reduce_min_sync(0xffffffffu, kp_min);
                     __syncwarp();
                 }
+                if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
+                tc_after();
                 const int valid = min(kTile, p.hi - j0);
                 if (valid < kTile && (valid <= 0 || (valid & 15))) {
-                    // rows behind the last slot may hold anything, and 0 x NaN is NaN: clear those the product's last step takes in
+                    // Rows behind the last slot may hold anything, and 0 x NaN is NaN: clear those the product's last step takes in.  Not before
+                    // the logits are there: they show that the group's previous product, and with it the ring slot's last entry, is done
+                    // (a wait that is a whole turn of the ring early would take the last entry's phase for this one's).
                     const int e = n_v + 2 * t + 1, r0 = max(valid, 0), rows = max(16, (valid + 15) & ~15) - r0;
                     if (!warp_wait(&sh.full[e % NS], e / NS, abort_flag, limit)) return false;
                     for (int x = r; x < rows * (D / 8); x += kTile) st_shared_16(chunk_addr(ring + (e % NS) * TILE, r0 + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
                     proxy_fence();
                 }
-                if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
-                tc_after();
                 if (busy) {
                     // The row in two halves of 64 logits: the first is shaped, its maximum taken and (if shaping changed it) put back,
                     // the second stays in registers; after the maximum the second half's probabilities are formed, then the first
