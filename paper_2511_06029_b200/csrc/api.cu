@@ -1162,7 +1162,8 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     const size_t act = c->dtype == LETHE_F32 ? 4 : 2;
     const size_t o_plan = take(sizeof(ChunkPlan)), o_old = take((size_t)a.n_items * 4), o_start = take(((size_t)a.n_units + 1) * 4);
     const size_t o_lo = by_pos ? take((size_t)a.n_units * 4) : 0, o_hi = by_pos ? take((size_t)a.n_units * 4) : 0;
-    const size_t o_rel = simt ? 0 : take(((size_t)a.n_items + 1) * 4);
+    const size_t o_cta = take((size_t)a.n_cta * 4);
+    const size_t o_rel = simt ? 0 : take(((size_t)a.n_items + 1) * 4), o_ri = simt ? 0 : take((size_t)a.n_items * ((a.cap_tiles + 1) / 2) * 4);
     const size_t o_bounds = by_pos ? take((size_t)a.n_items * a.cap_tiles * sizeof(int2)) : 0;
     const size_t o_nlse = take((size_t)nl * n_tokens * a.Hq * 4);
     const size_t o_ml = take((size_t)a.n_cta * kChunkParts * kChunkPartRows * sizeof(float2));
@@ -1180,7 +1181,11 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
         a.u_hi = (int*)(base + o_hi);
         a.bounds = (int2*)(base + o_bounds);
     }
-    if (!simt) a.rel_start = (int*)(base + o_rel);
+    a.cta_unit = (int*)(base + o_cta);
+    if (!simt) {
+        a.rel_start = (int*)(base + o_rel);
+        a.rel_item = (int*)(base + o_ri);
+    }
     a.nlse2 = (float*)(base + o_nlse);
     a.part_ml = (float2*)(base + o_ml);
     a.part_o = (float*)(base + o_po);

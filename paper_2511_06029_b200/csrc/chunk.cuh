@@ -49,10 +49,12 @@ struct ChunkArgs {
     int* u_start;    // [n_units + 1] first tile of each unit on the line
     int* u_lo;       // [n_units] first key tile of the unit (masks by position only, else NULL)
     int* u_hi;       // [n_units] slots the unit can see end here (masks by position only, else NULL)
+    int* cta_unit;   // [n_cta] the unit that holds the first tile of each CTA's stretch
     int* rel_start;  // [n_items + 1] first pair of key tiles of each item on the relevance kernel's line (tensor-core kernels, else NULL)
+    int* rel_item;   // [n_items * ceil(cap_tiles / 2)] the item of each pair on that line
     int2* bounds;    // [items][cap_tiles] smallest and largest pos of a key tile (masks by position only, else NULL)
     float* nlse2;    // [nl][Hkv][n_tokens][G] minus the log-sum-exp, in log2 units; -inf for a row that sees nothing
-    float* part_o;   // [n_cta][kChunkParts][kChunkPartRows][D]
+    float* part_o;   // [n_cta][kChunkParts][D][kChunkPartRows]: a thread that owns a row writes beside its neighbours
     float2* part_ml; // [n_cta][kChunkParts][kChunkPartRows] (max in log2 units, sum)
     long long n_pages;
     int dtype, D;

@@ -46,16 +46,18 @@ __device__ void make_plan(const ChunkArgs& a) {
         sums[tid] += add;
         __syncthreads();
     }
+    const int total = sums[kPrepThreads - 1], per = max(a.min_per, (total + a.n_cta - 1) / a.n_cta);
     int at = sums[tid] - mine;
     for (int u = u0; u < u1; ++u) {
         a.u_start[u] = at;
-        at += unit_cost(a, u);
+        const int next = at + unit_cost(a, u);
+        for (int c = (at + per - 1) / per; c * per < next; ++c) a.cta_unit[c] = u;
+        at = next;
     }
     if (tid == 0) {
-        const int total = sums[kPrepThreads - 1];
         a.u_start[a.n_units] = total;
         a.plan->total = total;
-        a.plan->per = max(a.min_per, (total + a.n_cta - 1) / a.n_cta);
+        a.plan->per = per;
     }
     if (!a.rel_start) return;
     // the relevance kernel's line: pairs of key tiles of every item that changes
@@ -79,7 +81,7 @@ __device__ void make_plan(const ChunkArgs& a) {
     at = sums[tid] - mine;
     for (int idx = i0; idx < i1; ++idx) {
         a.rel_start[idx] = at;
-        at += pairs(idx);
+        for (const int next = at + pairs(idx); at < next; ++at) a.rel_item[at] = idx;
     }
     if (tid == 0) a.rel_start[a.n_items] = sums[kPrepThreads - 1];
 }
@@ -97,8 +99,7 @@ __device__ __forceinline__ uint32_t quantise4(uint32_t ab, uint32_t cd, float sc
     return to_bytes(a, b, e5m2) | (to_bytes(c, d, e5m2) << 16);
 }
 
-// Blocks 1.. : one warp per (layer, token, KV head) row.  Memory-bound: each new row is read and written once with 16-byte
-// accesses.  Block 0 writes n_old, clears the call's counters and, when no mask goes by position, the plan.
+// Blocks 1.. : the (layer, token, KV head) rows.  Memory-bound: each new row is read and written once with 16-byte accesses.  Block 0 writes n_old, clears the call's counters and, when no mask goes by position, the plan.
 __global__ void __launch_bounds__(kPrepThreads) chunk_append_kernel(const __grid_constant__ ChunkArgs a) {
     __shared__ int cs[kSeqShared + 1];
     dependency_wait();
@@ -141,43 +142,75 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_append_kernel(const __grid
     const int src_row = a.D * act, dst_row = bytes ? a.D : src_row;
     const int chunks = src_row / 16;  // 16-byte pieces of a new row: 8 .. 32
     const long long rows = (long long)a.nl * a.n_tokens * a.Hkv;
-    for (long long r = (long long)(blockIdx.x - 1) * kPrepWarps + (tid >> 5); r < rows; r += (long long)(gridDim.x - 1) * kPrepWarps) {
-        const int hkv = (int)(r % a.Hkv);
-        const long long lt = r / a.Hkv;
-        const int tok = (int)(lt % a.n_tokens), li = (int)(lt / a.n_tokens), l = a.layer_begin + li;
-        if (tok < start[0] || tok >= start[a.B]) continue;
-        int lo = 0, hi = a.B;  // last b with start[b] <= tok: the sequence of this token (empty ones before it are passed over)
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (start[mid] <= tok) lo = mid;
-            else hi = mid;
-        }
-        const int b = lo, T = start[b + 1] - start[b];
-        const int item = (l * a.B + b) * a.Hkv + hkv;
-        const int n_old = min(max(a.len[item], 0), a.cap_tokens);
-        if (n_old + (long long)T > a.cap_tokens) {  // refused: nothing of the item changes, its outputs are zero
-            char* o = (char*)a.out + ((size_t)lt * a.Hq + (size_t)hkv * a.G) * src_row;
-            for (int i = lane; i < a.G * chunks; i += 32) reinterpret_cast<uint4*>(o)[i] = make_uint4(0, 0, 0, 0);
-            if (a.lse && lane < a.G) a.lse[(size_t)lt * a.Hq + hkv * a.G + lane] = -INFINITY;
-            continue;
-        }
-        const int slot = n_old + tok - start[b];
-        if (lane == 0) a.pos[(size_t)item * a.cap_tokens + slot] = a.token_pos[tok];
-        const long long at = chunk_row(a, item, slot);
-        if (at < 0) {
-            if (lane == 0) record_error(a.status, LETHE_ERR_PAGE, item);
-            continue;
-        }
-        for (int i = lane; i < 2 * chunks; i += 32) {
-            const bool is_v = i >= chunks;
-            const int c = is_v ? i - chunks : i;
-            const uint4 x = reinterpret_cast<const uint4*>((const char*)(is_v ? a.v_new : a.k_new) + (size_t)r * src_row)[c];
-            char* d = (char*)const_cast<void*>(is_v ? a.v : a.k) + (size_t)at * dst_row;
-            if (!bytes) reinterpret_cast<uint4*>(d)[c] = x;
-            else {
-                const float sc = is_v ? a.v_scale[l] : a.k_scale[l];
-                reinterpret_cast<uint2*>(d)[c] = make_uint2(quantise4(x.x, x.y, sc, e5m2), quantise4(x.z, x.w, sc, e5m2));
+    // A half-warp takes a row at a time, first its K, then its V, U of each in flight: where a row goes is a short chain of
+    // dependent loads (length, page), so a warp works on 2 U rows at once.
+    constexpr int U = 2;
+    const int half = lane >> 4, hl = lane & 15;
+    const long long step = (long long)(gridDim.x - 1) * kPrepWarps * 2 * U;
+    for (long long r0 = ((long long)(blockIdx.x - 1) * kPrepWarps + (tid >> 5)) * 2 * U; r0 < rows; r0 += step) {
+        int item[U], slot[U], lay[U];
+        long long at[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + 2 * u + half;
+            item[u] = -1;
+            at[u] = -1;
+            if (r >= rows) continue;
+            const int hkv = (int)(r % a.Hkv);
+            const long long lt = r / a.Hkv;
+            const int tok = (int)(lt % a.n_tokens), li = (int)(lt / a.n_tokens);
+            if (tok < start[0] || tok >= start[a.B]) continue;
+            int lo = 0, hi = a.B;  // last b with start[b] <= tok: the sequence of this token (empty ones before it are passed over)
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (start[mid] <= tok) lo = mid;
+                else hi = mid;
             }
+            const int T = start[lo + 1] - start[lo];
+            lay[u] = a.layer_begin + li;
+            item[u] = (lay[u] * a.B + lo) * a.Hkv + hkv;
+            const int n_old = min(max(a.len[item[u]], 0), a.cap_tokens);
+            slot[u] = n_old + (long long)T > a.cap_tokens ? -1 : n_old + tok - start[lo];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + 2 * u + half;
+            if (item[u] < 0) continue;
+            const long long lt = r / a.Hkv;
+            const int hkv = (int)(r % a.Hkv);
+            if (slot[u] < 0) {  // refused: nothing of the item changes, its outputs are zero
+                char* o = (char*)a.out + ((size_t)lt * a.Hq + (size_t)hkv * a.G) * src_row;
+                for (int i = hl; i < a.G * chunks; i += 16) reinterpret_cast<uint4*>(o)[i] = make_uint4(0, 0, 0, 0);
+                if (a.lse && hl < a.G) a.lse[(size_t)lt * a.Hq + hkv * a.G + hl] = -INFINITY;
+                continue;
+            }
+            if (hl == 0) a.pos[(size_t)item[u] * a.cap_tokens + slot[u]] = a.token_pos[lt % a.n_tokens];
+            at[u] = chunk_row(a, item[u], slot[u]);
+            if (at[u] < 0 && hl == 0) record_error(a.status, LETHE_ERR_PAGE, item[u]);
+        }
+        for (int c = hl; c < chunks; c += 16) {
+            uint4 x[U][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (at[u] >= 0) {
+                    const size_t src = (size_t)(r0 + 2 * u + half) * src_row;
+                    x[u][0] = reinterpret_cast<const uint4*>((const char*)a.k_new + src)[c];
+                    x[u][1] = reinterpret_cast<const uint4*>((const char*)a.v_new + src)[c];
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (at[u] >= 0) {
+                    char* kd = (char*)const_cast<void*>(a.k) + (size_t)at[u] * dst_row;
+                    char* vd = (char*)const_cast<void*>(a.v) + (size_t)at[u] * dst_row;
+                    if (!bytes) {
+                        reinterpret_cast<uint4*>(kd)[c] = x[u][0];
+                        reinterpret_cast<uint4*>(vd)[c] = x[u][1];
+                    } else {
+                        const float ks = a.k_scale[lay[u]], vs = a.v_scale[lay[u]];
+                        reinterpret_cast<uint2*>(kd)[c] = make_uint2(quantise4(x[u][0].x, x[u][0].y, ks, e5m2), quantise4(x[u][0].z, x[u][0].w, ks, e5m2));
+                        reinterpret_cast<uint2*>(vd)[c] = make_uint2(quantise4(x[u][1].x, x[u][1].y, vs, e5m2), quantise4(x[u][1].z, x[u][1].w, vs, e5m2));
+                    }
+                }
         }
     }
 }
@@ -253,59 +286,69 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_range_kernel(const __grid_
     make_plan(a);
 }
 
-// Merges the parts of each unit that more than one CTA worked on: one block per unit, one warp per row, the parts in the
-// order of the keys they cover.
-__global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __grid_constant__ ChunkArgs a) {
+// Merges the parts of each unit that more than one CTA worked on.  A block takes 32 rows of the unit that lies across the beginning
+// of CTA c's stretch (the first such c of the unit speaks for it): thread (x, y) of 32 x 8 adds up elements y, y + 8, ... of row x
+// over the parts, in the order of the keys they cover, and the rows are turned in shared memory so that reads and writes are both
+// whole lines.
+constexpr int kCombineRows = 32;
+__global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __grid_constant__ ChunkArgs a, int row_blocks) {
+    __shared__ float tile[kCombineRows][128 + 1];
     dependency_wait();
     dependency_release();
-    const int u = blockIdx.x;
-    const int s0 = a.u_start[u], s1 = a.u_start[u + 1];
-    if (s0 == s1) return;
+    const int c_mid = 1 + blockIdx.x / row_blocks, row0 = (blockIdx.x % row_blocks) * kCombineRows;
     const int per = a.plan->per;
+    if ((long long)c_mid * per >= a.plan->total) return;
+    const int u = a.cta_unit[c_mid];
+    const int s0 = a.u_start[u], s1 = a.u_start[u + 1];
     const int c0 = s0 / per, c1 = (s1 - 1) / per;
-    if (c0 == c1) return;  // written by the one CTA that had it
+    if (c0 != c_mid - 1) return;  // begins here (nothing to merge) or was begun before CTA c_mid - 1
     const int idx = u / a.QT, tok0 = (u - idx * a.QT) * a.TU;
     const ChunkItem it = chunk_item(a, idx);
-    const int toks = min(it.T - tok0, a.TU);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int E = a.D / 32;                      // elements per lane: 2 or 4
-    for (int row = warp; row < toks * a.G; row += kPrepWarps) {
-        const int tile = row / (a.TT * a.G), r = row - tile * a.TT * a.G;  // row tile and row in it
-        float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    const int rows = min(it.T - tok0, a.TU) * a.G;
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    // row blocks do not lie across row tiles: a tile has TT * G <= 128 rows, four blocks
+    const int tile_idx = row0 / kChunkPartRows, r = row0 % kChunkPartRows + x;
+    const int row = tile_idx * a.TT * a.G + r;
+    const bool ok = r < a.TT * a.G && row < rows;
+    constexpr int E = 16;  // elements per thread at D = 128
+    float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    if (ok) {
         for (int c = c0; c <= c1; ++c) {
-            const size_t p = (size_t)(c * 2 + (c == c0 ? 1 : 0)) * 2 + tile;  // the unit begins in CTA c0 and was begun earlier in the others
+            const size_t p = (size_t)(c * 2 + (c == c0 ? 1 : 0)) * 2 + tile_idx;  // the unit begins in CTA c0 and was begun earlier in the others
             const float2 ml = a.part_ml[p * kChunkPartRows + r];
+            const float* src = a.part_o + (p * a.D + y) * kChunkPartRows + r;
+            float v[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = y + 8 * e < a.D ? src[(size_t)e * 8 * kChunkPartRows] : 0.f;
             if (ml.x == -INFINITY && ml.y == 0.f) continue;  // the part saw nothing of this row
             const float mx = fmaxf(m, ml.x);
             const float w_old = exp2_diff(m, mx), w = fast_exp2(ml.x - mx);
-            const float* src = a.part_o + (p * kChunkPartRows + r) * a.D + lane * E;
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            if (E == 4) {
-                const float4 f = *reinterpret_cast<const float4*>(src);
-                v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-            } else {
-                const float2 f = *reinterpret_cast<const float2*>(src);
-                v[0] = f.x; v[1] = f.y;
-            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = o[e] * w_old + v[e] * w;
+            for (int e = 0; e < E; ++e) o[e] = o[e] * w_old + v[e] * w;
             l = l * w_old + ml.y * w;
             m = mx;
         }
         const float inv = l == 0.f ? 0.f : a.v_scale[it.l] / l;  // nothing seen: zero; a NaN stays one
-        const int tok = tok0 + row / a.G, h = row % a.G;
-        const size_t orow = ((size_t)it.li * a.n_tokens + it.first + tok) * a.Hq + it.hkv * a.G + h;
-        if (a.dtype == LETHE_F32) {
-            float* d = (float*)a.out + orow * a.D + lane * E;
-            for (int e = 0; e < E; ++e) d[e] = o[e] * inv;
-        } else {
-            __nv_bfloat16* d = (__nv_bfloat16*)a.out + orow * a.D + lane * E;
-            for (int e = 0; e < E; e += 2) *reinterpret_cast<__nv_bfloat162*>(d + e) = __floats2bfloat162_rn(o[e] * inv, o[e + 1] * inv);
-        }
-        if (lane == 0) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (y + 8 * e < a.D) tile[x][y + 8 * e] = o[e] * inv;
+        if (y == 0) {
+            const int tok = it.first + tok0 + row / a.G, h = row % a.G;
             const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-            if (a.lse) a.lse[orow] = lse2 * 0.6931471805599453f;
-            a.nlse2[(((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first + tok) * a.G + h] = l == 0.f ? -INFINITY : -lse2;
+            if (a.lse) a.lse[((size_t)it.li * a.n_tokens + tok) * a.Hq + it.hkv * a.G + h] = lse2 * 0.6931471805599453f;
+            a.nlse2[(((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + tok) * a.G + h] = l == 0.f ? -INFINITY : -lse2;
+        }
+    }
+    __syncthreads();
+    for (int rr = y; rr < kCombineRows; rr += 8) {
+        const int r2 = row0 % kChunkPartRows + rr, row2 = tile_idx * a.TT * a.G + r2;
+        if (r2 >= a.TT * a.G || row2 >= rows) break;
+        const size_t orow = ((size_t)it.li * a.n_tokens + it.first + tok0 + row2 / a.G) * a.Hq + it.hkv * a.G + row2 % a.G;
+        for (int d = 2 * x; d < a.D; d += 64) {
+            if (a.dtype == LETHE_F32) *reinterpret_cast<float2*>((float*)a.out + orow * a.D + d) = make_float2(tile[rr][d], tile[rr][d + 1]);
+            else *reinterpret_cast<__nv_bfloat162*>((__nv_bfloat16*)a.out + orow * a.D + d) = __floats2bfloat162_rn(tile[rr][d], tile[rr][d + 1]);
         }
     }
 }
@@ -313,17 +356,21 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
 }  // namespace
 
 cudaError_t launch_chunk_append(const ChunkArgs& a, cudaStream_t stream) {
-    // about four waves of warps: a row is a short dependent chain (sequence, length, page, row), so many are kept in flight
+    // at most two waves of blocks
     const long long rows = a.append ? (long long)a.nl * a.n_tokens * a.Hkv : 0;
-    const long long want = (rows + kPrepWarps - 1) / kPrepWarps;
-    const int blocks = 1 + (int)(want < 4736 ? want : 4736);
+    const long long want = (rows + 4 * kPrepWarps - 1) / (4 * kPrepWarps);
+    const int blocks = 1 + (int)(want < 2368 ? want : 2368);
     cudaError_t e = launch_dependent(chunk_append_kernel, dim3(blocks), kPrepThreads, 0, stream, a);
     if (e == cudaSuccess && a.u_hi) e = launch_dependent(chunk_range_kernel, dim3(a.n_items), kPrepThreads, 0, stream, a);
     return e;
 }
 
 cudaError_t launch_chunk_combine(const ChunkArgs& a, cudaStream_t stream) {
-    return launch_dependent(chunk_combine_kernel, dim3(a.n_units), kPrepThreads, 0, stream, a);
+    if (a.n_cta < 2) return cudaSuccess;
+    // rows of a unit in the parts: one or two row tiles, each padded to whole blocks
+    const int tile_rows = min(a.TT, a.max_chunk) * a.G;
+    const int row_blocks = a.max_chunk > a.TT && a.TU > a.TT ? 2 * kChunkPartRows / kCombineRows : (tile_rows + kCombineRows - 1) / kCombineRows;
+    return launch_dependent(chunk_combine_kernel, dim3((a.n_cta - 1) * row_blocks), kPrepThreads, 0, stream, a, row_blocks);
 }
 
 }  // namespace lethe

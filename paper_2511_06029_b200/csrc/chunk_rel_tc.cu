@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
             bool bad = false;  // the attention has recorded bad pages
             int k = 0, qn = 0;
             for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
-                const int idx = find_start(a.rel_start, a.n_items, w), j0 = (w - a.rel_start[idx]) * 2 * kTile;
+                const int idx = a.rel_item[w], j0 = (w - a.rel_start[idx]) * 2 * kTile;
                 const ChunkItem it = chunk_item(a, idx);
                 if (TMA) {
                     if (k > 0 && !bar_wait(&sh.k_empty, k - 1, abort_flag, limit)) break;
@@ -127,44 +127,48 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        if (lane == 0) {
-            int k = 0, qn = 0;
-            int ns[2] = {0, 0};
-            for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
-                const int idx = find_start(a.rel_start, a.n_items, w), j0 = (w - a.rel_start[idx]) * 2 * kTile;
-                const ChunkItem it = chunk_item(a, idx);
-                const int tiles = j0 + kTile < it.n ? 2 : 1;
-                const uint32_t desc = mma_idesc(kTile, false, a.scale[it.l] < 0.f);
-                if (!bar_wait(&sh.k_full, k, abort_flag, limit)) break;
-                const bool ok = for_query_tiles(a, it, idx, j0, [&](int) {
-                    if (!bar_wait(&sh.q_full, qn, abort_flag, limit)) return false;
-                    for (int g = 0; g < tiles; ++g) {
-                        if (ns[g] > 0 && !bar_wait(&sh.s_empty[g], ns[g] - 1, abort_flag, limit)) return false;
-                        tc_after();
+        const uint64_t q_desc = smem_desc(q_tile, 16), k_desc = smem_desc(k_tile, 16);
+        int k = 0, qn = 0;
+        int ns[2] = {0, 0};
+        for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
+            const int idx = a.rel_item[w], j0 = (w - a.rel_start[idx]) * 2 * kTile;
+            const ChunkItem it = chunk_item(a, idx);
+            const int tiles = j0 + kTile < it.n ? 2 : 1;
+            const uint32_t desc = mma_idesc(kTile, false, a.scale[it.l] < 0.f);
+            if (!warp_wait(&sh.k_full, k, abort_flag, limit)) break;
+            const bool ok = for_query_tiles(a, it, idx, j0, [&](int) {
+                if (!warp_wait(&sh.q_full, qn, abort_flag, limit)) return false;
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    if (g >= tiles) break;
+                    if (ns[g] > 0 && !warp_wait(&sh.s_empty[g], ns[g] - 1, abort_flag, limit)) return false;
+                    tc_after();
+                    if (elect_one()) {
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
-                            const uint32_t off = (ks >> 2) * kHalfBytes + (ks & 3) * 32;
-                            mma_ss(tmem + g * kTile, smem_desc(k_tile + g * TILE + off, 16), smem_desc(q_tile + off, 16), desc, ks > 0);
+                            const uint32_t off = ((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4;
+                            mma_ss(tmem + g * kTile, k_desc + (g * (TILE >> 4) + off), q_desc + off, desc, ks > 0);
                         }
                         sh.issued = 1;
                         tc_commit(&sh.s_full[g]);
-                        ++ns[g];
+                        if (g == tiles - 1) tc_commit(&sh.q_empty);
                     }
-                    tc_commit(&sh.q_empty);
-                    ++qn;
-                    return true;
-                });
-                if (!ok) break;
-                tc_commit(&sh.k_empty);
-            }
+                    __syncwarp();
+                    ++ns[g];
+                }
+                ++qn;
+                return true;
+            });
+            if (!ok) break;
+            if (elect_one()) tc_commit(&sh.k_empty);
+            __syncwarp();
         }
-        __syncwarp();
     } else {
         const int g = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + g * kTile;
         int n_s = 0, k = 0;
         for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
-            const int idx = find_start(a.rel_start, a.n_items, w), j0 = (w - a.rel_start[idx]) * 2 * kTile;
+            const int idx = a.rel_item[w], j0 = (w - a.rel_start[idx]) * 2 * kTile;
             const ChunkItem it = chunk_item(a, idx);
             const int j = j0 + g * kTile + r;  // this thread's key
             if (!TMA) {
@@ -230,10 +234,11 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                 const bool clean = cols == used && __all_sync(0xffffffffu, c_lo <= 0 && (!mask_pos || kp >= lo_max));
 #pragma unroll
                 for (int ch = 0; ch < kTile; ch += 32) {
+                    if (ch >= cols) break;  // a short chunk leaves most columns empty
                     uint32_t v[32];
                     tmem_ld32(s_addr + ch, v);
                     tmem_ld_wait();
-                    if (ch == kTile - 32) {
+                    if (ch + 32 >= cols) {
                         tc_before();
                         __syncwarp();
                         if (lane == 0) bar_arrive(&sh.s_empty[g]);
@@ -301,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
     tc_after();
     if (sh.abort) {  // uniform for the CTA: see everything this CTA has started end
         if (tid == 0) record_error(a.status, LETHE_ERR_TIMEOUT, blockIdx.x);
-        if (warp == kMmaWarp && lane == 0 && sh.issued) {
+        if (warp == kMmaWarp && sh.issued && elect_one()) {  // the lane that issued them: a commit follows one's own MMAs
             tc_commit(&sh.drained);
             bar_drain(&sh.drained, 0);
         }

@@ -1,9 +1,6 @@
 // lethe_chunk_attend on fp32 caches: CUDA-core kernels (the tensor cores have no full fp32 product).  Both are bound by the fp32
 // FMA rate: 64 query rows by 32 keys per step, operands in shared memory, 4 x 2 logits and 4 x D / 16 outputs per thread, so that
 // a 16-byte shared-memory read feeds 5 to 8 FMAs per operand.
-#include <cuda_fp16.h>
-#include <cuda_fp8.h>
-
 #include "chunk.cuh"
 
 namespace lethe {
@@ -14,25 +11,6 @@ constexpr int kRows = 64;   // query rows of a unit
 constexpr int kKeys = 32;   // keys per step
 constexpr int kPad = 4;     // row padding of the staged tiles: rows start in different banks
 
-// Four consecutive elements of a stored row as floats (storage: 0 fp32, 1 bf16, 2 e4m3, 3 e5m2, the dtype codes of lethe_cache).
-__device__ __forceinline__ float4 load4(const void* base, size_t e, int storage) {
-    if (storage == LETHE_F32) return *reinterpret_cast<const float4*>((const float*)base + e);
-    if (storage == LETHE_BF16) {
-        const uint2 w = *reinterpret_cast<const uint2*>((const __nv_bfloat16*)base + e);
-        return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
-    }
-    const uint32_t w = *reinterpret_cast<const uint32_t*>((const char*)base + e);
-    float2 lo, hi;
-    if (storage == LETHE_FP8_E4M3) {
-        lo = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffff), __NV_E4M3)));
-        hi = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3)));
-    } else {
-        lo = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffff), __NV_E5M2)));
-        hi = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E5M2)));
-    }
-    return make_float4(lo.x, lo.y, hi.x, hi.y);
-}
-
 // Rows [j0, j0 + count) of K or V of an item into shared memory, missing rows (at or beyond `end`, or on a page outside the pool) as zeros.
 template <int D>
 __device__ __forceinline__ void stage_rows(const ChunkArgs& a, const void* base, int item, int j0, int end, int count, float* dst, bool* bad) {
@@ -42,7 +20,7 @@ __device__ __forceinline__ void stage_rows(const ChunkArgs& a, const void* base,
         if (j0 + r < end) {
             const long long at = chunk_row(a, item, j0 + r);
             if (at < 0) *bad = true;
-            else x = load4(base, (size_t)at * D + c * 4, a.dtype);
+            else x = reinterpret_cast<const float4*>((const float*)base + (size_t)at * D)[c];
         }
         *reinterpret_cast<float4*>(dst + r * (D + kPad) + c * 4) = x;
     }
@@ -71,14 +49,8 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
     const int total = a.plan->total, per = a.plan->per;
     const int begin = min(total, (int)blockIdx.x * per), end = min(total, begin + per);
     if (begin >= end) return;
-    int lo = 0, hi = a.n_units;  // the unit that holds tile `begin`: the last with u_start <= begin (units without tiles share a start)
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.u_start[mid] <= begin) lo = mid;
-        else hi = mid;
-    }
     bool bad = false;
-    for (int u = lo, at = begin; at < end; ++u) {
+    for (int u = a.cta_unit[blockIdx.x], at = begin; at < end; ++u) {
         const int s0 = a.u_start[u], s1 = a.u_start[u + 1];
         if (s1 <= at) continue;
         const int stop = min(end, s1);
@@ -86,7 +58,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
         const ChunkItem it = chunk_item(a, idx);
         const int rows = min(it.T - tok0, a.TU) * a.G;
         const int base_tile = (a.u_lo ? a.u_lo[u] : 0) - s0;
-        const float scale = a.scale[it.l] * a.k_scale[it.l];
+        const float scale = a.scale[it.l];
         const int prefix = a.prefix_len ? a.prefix_len[it.b] : INT32_MIN;
         const int32_t* pos = a.pos + (size_t)it.item * a.cap_tokens;
         const bool by_pos = a.slopes || a.window || a.doc_start || a.prefix_len;
@@ -95,7 +67,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
             const int r = i / (D / 4), c = i % (D / 4);
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
             if (r < rows)
-                x = load4(a.q, (((size_t)it.li * a.n_tokens + it.first + tok0 + r / a.G) * a.Hq + it.hkv * a.G + r % a.G) * D + c * 4, a.dtype == LETHE_F32 ? LETHE_F32 : LETHE_BF16);
+                x = reinterpret_cast<const float4*>((const float*)a.q + (((size_t)it.li * a.n_tokens + it.first + tok0 + r / a.G) * a.Hq + it.hkv * a.G + r % a.G) * D)[c];
             *reinterpret_cast<float4*>(sq + r * (D + kPad) + c * 4) = x;
         }
         ChunkRow row[4];
@@ -186,17 +158,13 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
             if (r >= rows) continue;
             const int tok = tok0 + r / a.G, h = r % a.G;
             const size_t orow = ((size_t)it.li * a.n_tokens + it.first + tok) * a.Hq + it.hkv * a.G + h;
-            const float mul = !whole ? 1.f : (l[i] == 0.f ? 0.f : a.v_scale[it.l] / l[i]);
-            float* d = whole ? (float*)a.out + orow * D : a.part_o + (part * kChunkPartRows + r) * D;
+            const float mul = !whole ? 1.f : (l[i] == 0.f ? 0.f : 1.f / l[i]);
 #pragma unroll
             for (int e = 0; e < D / 64; ++e) {
-                const float4 y = make_float4(o[i][4 * e] * mul, o[i][4 * e + 1] * mul, o[i][4 * e + 2] * mul, o[i][4 * e + 3] * mul);
-                if (!whole || a.dtype == LETHE_F32) *reinterpret_cast<float4*>(d + tx * 4 + 64 * e) = y;
-                else {
-                    __nv_bfloat162* b = reinterpret_cast<__nv_bfloat162*>((__nv_bfloat16*)a.out + orow * D + tx * 4 + 64 * e);
-                    b[0] = __floats2bfloat162_rn(y.x, y.y);
-                    b[1] = __floats2bfloat162_rn(y.z, y.w);
-                }
+                if (whole) *reinterpret_cast<float4*>((float*)a.out + orow * D + tx * 4 + 64 * e) = make_float4(o[i][4 * e] * mul, o[i][4 * e + 1] * mul, o[i][4 * e + 2] * mul, o[i][4 * e + 3] * mul);
+                else
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) a.part_o[(part * D + tx * 4 + 64 * e + x) * kChunkPartRows + r] = o[i][4 * e + x];
             }
             if (tx == 0) {
                 if (!whole) a.part_ml[part * kChunkPartRows + r] = make_float2(m[i], l[i]);
@@ -231,7 +199,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_rel(const __grid_cons
     if (j0 >= it.n) return;
     bool bad = false;  // the attention has recorded bad pages
     stage_rows<D>(a, a.k, it.item, j0, it.n, kRows, sk, &bad);
-    const float scale = a.scale[it.l] * a.k_scale[it.l];
+    const float scale = a.scale[it.l];
     const int prefix = a.prefix_len ? a.prefix_len[it.b] : INT32_MIN;
     const int32_t* pos = a.pos + (size_t)it.item * a.cap_tokens;
     const bool by_pos = a.slopes || a.window || a.doc_start || a.prefix_len;
@@ -249,7 +217,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_rel(const __grid_cons
             const int r = r0 + i / (D / 4), c = i % (D / 4);
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
             if (r < rows)
-                x = load4(a.q, (((size_t)it.li * a.n_tokens + it.first + r / a.G) * a.Hq + it.hkv * a.G + r % a.G) * D + c * 4, a.dtype == LETHE_F32 ? LETHE_F32 : LETHE_BF16);
+                x = reinterpret_cast<const float4*>((const float*)a.q + (((size_t)it.li * a.n_tokens + it.first + r / a.G) * a.Hq + it.hkv * a.G + r % a.G) * D)[c];
             *reinterpret_cast<float4*>(sq + (i / (D / 4)) * (D + kPad) + c * 4) = x;
         }
         __syncthreads();

@@ -31,6 +31,7 @@ __host__ __device__ constexpr int stages() { return D == 128 ? 4 : 8; }
 template <int D>
 constexpr size_t smem_bytes() { return 1024 + (size_t)(2 + stages<D>()) * tile_bytes<D>(); }
 
+template <bool MOD>
 struct Shared {
     unsigned long long full[kMaxStages], empty[kMaxStages];
     unsigned long long q_full, q_done, q_soft, merge;
@@ -40,8 +41,9 @@ struct Shared {
     int abort;
     int loaded, q_loaded, issued;  // ring entries, query loads and MMAs started (for the drain after a timeout)
     float2 merge_ml[kTile];
-    alignas(16) int kpos[kSoftWarps][kTile];     // positions of the tile's keys, one copy per warp
-    alignas(16) float kposf[kSoftWarps][kTile];  // the same relative to the unit's first query
+    alignas(16) int kpos[MOD ? kSoftWarps : 1][kTile];     // positions of the tile's keys, one copy per warp
+    alignas(16) float kposf[MOD ? kSoftWarps : 1][kTile];  // the same relative to the unit's first query
+    alignas(16) unsigned char turn[kSoftWarps][32][80];     // 32 columns of a warp's output rows on their way out (rows 16 bytes apart in the banks)
 };
 
 // A CTA's piece of a unit, as every role derives it from the plan.
@@ -75,7 +77,7 @@ __device__ __forceinline__ void for_pieces(const ChunkArgs& a, F f) {
     const int total = a.plan->total, per = a.plan->per;
     const int begin = min(total, (int)blockIdx.x * per), end = min(total, begin + per);
     if (begin >= end) return;
-    int u = find_start(a.u_start, a.n_units, begin), s0 = a.u_start[u];
+    int u = a.cta_unit[blockIdx.x], s0 = a.u_start[u];
     for (int at = begin; at < end; ++u) {
         const int s1 = a.u_start[u + 1];
         if (s1 > at) {
@@ -92,7 +94,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
     constexpr int TILE = tile_bytes<D>(), NS = stages<D>(), KS = D / 16;
     constexpr int kOCol = 256;  // tensor memory: S0 | S1 | O0 | O1, 128 columns each (P over its S)
     extern __shared__ unsigned char dyn_raw[];
-    __shared__ Shared sh;
+    __shared__ Shared<MOD> sh;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t q_tile = (smem_u32(dyn_raw) + 1023u) & ~1023u;
     const uint32_t ring = q_tile + 2 * TILE;
@@ -185,58 +187,60 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        // ------------------------------------------------------------------ MMA issue
-        if (lane == 0) {
-            const uint32_t pv_desc = mma_idesc(D, true, false);
-            int k = 0, base = 0;              // pieces done, first ring entry of the piece
-            int jobs_p[2] = {0, 0};           // probabilities consumed so far, per group
-            for_pieces(a, [&](const Piece& p) {
-                const uint32_t qk_desc = mma_idesc(kTile, false, a.scale[p.it.l] < 0.f);
-                const int jobs = p.alt ? p.nt : 2 * p.nt;
-                if (!bar_wait(&sh.q_full, k, abort_flag, limit)) return false;
-                auto entry_full = [&](int e) { return bar_wait(&sh.full[e % NS], e / NS, abort_flag, limit); };
-                for (int i = 0; i < jobs + 2; ++i) {
-                    if (i >= 2) {  // P V of job i - 2
-                        const int j = i - 2, g = j & 1, t = p.alt ? j : j >> 1;
-                        if (j < jobs) {
-                            const int e = base + 2 * t + 1;
-                            if (!entry_full(e)) return false;
-                            if (!bar_wait(&sh.p_full[g], jobs_p[g]++, abort_flag, limit)) return false;
-                            tc_after();
-                            const int valid = min(kTile, p.hi - (p.tile0 + t) * kTile);
-                            const int steps = max(1, (valid + 15) / 16);
-                            const uint32_t vt = ring + (e % NS) * TILE, pt = tmem + g * 128, ot = tmem + kOCol + g * 128;
-                            const bool first = p.alt ? t < 2 : t == 0;
+        // ------------------------------------------------------------------ MMA issue: the warp waits as one, one lane issues
+        const uint32_t pv_desc = mma_idesc(D, true, false);
+        const uint64_t q_desc = smem_desc(q_tile, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, kHalfBytes);
+        int k = 0, base = 0;              // pieces done, first ring entry of the piece
+        int jobs_p[2] = {0, 0};           // probabilities consumed so far, per group
+        for_pieces(a, [&](const Piece& p) {
+            const uint32_t qk_desc = mma_idesc(kTile, false, a.scale[p.it.l] < 0.f);
+            const int jobs = p.alt ? p.nt : 2 * p.nt;
+            if (!warp_wait(&sh.q_full, k, abort_flag, limit)) return false;
+            auto entry_full = [&](int e) { return warp_wait(&sh.full[e % NS], e / NS, abort_flag, limit); };
+            for (int i = 0; i < jobs + 2; ++i) {
+                const int g = i & 1;
+                if (i >= 2) {  // P V of job i - 2
+                    const int t = p.alt ? i - 2 : (i - 2) >> 1, e = base + 2 * t + 1;
+                    if (!entry_full(e)) return false;
+                    if (!warp_wait(&sh.p_full[g], jobs_p[g]++, abort_flag, limit)) return false;
+                    tc_after();
+                    const int steps = max(1, (min(kTile, p.hi - (p.tile0 + t) * kTile) + 15) / 16);
+                    const bool first = p.alt ? t < 2 : t == 0;
+                    if (elect_one()) {
+                        const uint64_t vd = v_desc + (uint64_t)((e % NS) * (TILE >> 4));
+                        const uint32_t pt = tmem + g * 128, ot = tmem + kOCol + g * 128;
 #pragma unroll
-                            for (int ks = 0; ks < kTile / 16; ++ks)
-                                if (ks < steps) mma_ts(ot, pt + ks * 8, smem_desc(vt + ks * 2048, kHalfBytes), pv_desc, !first || ks > 0);
-                            sh.issued = 1;
-                            tc_commit(&sh.o_full[g]);
-                            if (p.alt || g == 1) tc_commit(&sh.empty[e % NS]);
-                        }
+                        for (int ks = 0; ks < kTile / 16; ++ks)
+                            if (ks < steps) mma_ts(ot, pt + ks * 8, vd + ks * (2048 >> 4), pv_desc, !first || ks > 0);
+                        sh.issued = 1;
+                        tc_commit(&sh.o_full[g]);
+                        if (p.alt || g == 1) tc_commit(&sh.empty[e % NS]);
                     }
-                    if (i < jobs) {  // Q K^T of job i
-                        const int g = i & 1, t = p.alt ? i : i >> 1, e = base + 2 * t;
-                        if (!entry_full(e)) return false;
-                        tc_after();
-                        const uint32_t qt = q_tile + (p.alt ? 0 : g) * TILE, kt = ring + (e % NS) * TILE;
+                    __syncwarp();
+                }
+                if (i < jobs) {  // Q K^T of job i
+                    const int t = p.alt ? i : i >> 1, e = base + 2 * t;
+                    if (!entry_full(e)) return false;
+                    tc_after();
+                    if (elect_one()) {
+                        const uint64_t qd = q_desc + (uint64_t)((p.alt ? 0 : g) * (TILE >> 4)), kd = k_desc + (uint64_t)((e % NS) * (TILE >> 4));
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
-                            const uint32_t off = (ks >> 2) * kHalfBytes + (ks & 3) * 32;
-                            mma_ss(tmem + g * 128, smem_desc(qt + off, 16), smem_desc(kt + off, 16), qk_desc, ks > 0);
+                            constexpr int half16 = kHalfBytes >> 4;
+                            mma_ss(tmem + g * 128, qd + (ks >> 2) * half16 + (ks & 3) * 2, kd + (ks >> 2) * half16 + (ks & 3) * 2, qk_desc, ks > 0);
                         }
                         sh.issued = 1;
                         tc_commit(&sh.s_full[g]);
                         if (p.alt || g == 1) tc_commit(&sh.empty[e % NS]);
                         if (i == jobs - 1) tc_commit(&sh.q_done);
                     }
+                    __syncwarp();
                 }
-                base += 2 * p.nt;
-                ++k;
-                return true;
-            });
-        }
-        __syncwarp();
+            }
+            base += 2 * p.nt;
+            ++k;
+            return true;
+        });
     } else {
         // ------------------------------------------------------------------ softmax
         const int g = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;  // group, TMEM lane
@@ -451,7 +455,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     if (busy) {
                         sh.merge_ml[r] = make_float2(m, l);
                         if (done > 0) {
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < D; c += 32) {
                                 uint32_t o[32];
                                 tmem_ld32(o_addr + c, o);
@@ -479,36 +483,46 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                 const bool whole = p.head && p.tail;
                 const bool add = p.alt && jobs > 1;
                 const size_t orow = ((size_t)p.it.li * a.n_tokens + p.it.first + tok) * a.Hq + p.it.hkv * a.G + h;
-                const size_t part = (((size_t)blockIdx.x * 2 + (p.head ? 1 : 0)) * 2 + (p.alt ? 0 : g)) * kChunkPartRows + r;
+                const size_t part = ((size_t)blockIdx.x * 2 + (p.head ? 1 : 0)) * 2 + (p.alt ? 0 : g);
                 const float mul = !whole ? 1.f : (l == 0.f ? 0.f : a.v_scale[p.it.l] / l);
-#pragma unroll
+                const float mine = l == 0.f ? 0.f : w0 * mul, others = add && l != 0.f ? w1 * mul : 0.f;
+                __nv_bfloat16* const out0 = (__nv_bfloat16*)a.out + (((size_t)p.it.li * a.n_tokens + p.it.first) * a.Hq + p.it.hkv * a.G) * D;
+#pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
                     tmem_ld32(o_addr + c, o);
                     tmem_ld_wait();
-                    float f[32];
 #pragma unroll
                     for (int y = 0; y < 32; ++y) {
-                        float x = __uint_as_float(o[y]);
-                        if (l == 0.f) x = 0.f;
-                        if (p.alt) x = add ? (w0 == 0.f ? 0.f : x * w0) + (w1 == 0.f ? 0.f : merge_o[(c + y) * kTile + r] * w1) : x * w0;
-                        f[y] = x * mul;
+                        float x = mine == 0.f ? 0.f : __uint_as_float(o[y]) * mine;  // what nothing was added to may hold anything
+                        if (others != 0.f) x = fmaf(merge_o[(c + y) * kTile + r], others, x);
+                        o[y] = __float_as_uint(x);
                     }
-                    if (valid_row) {
-                        if (whole) {
-                            uint4* d = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + orow * D + c);
+                    if (!whole) {
+                        if (valid_row)
 #pragma unroll
-                            for (int y = 0; y < 4; ++y)
-                                d[y] = make_uint4(pack_bf16(f[8 * y], f[8 * y + 1]), pack_bf16(f[8 * y + 2], f[8 * y + 3]), pack_bf16(f[8 * y + 4], f[8 * y + 5]), pack_bf16(f[8 * y + 6], f[8 * y + 7]));
-                        } else {
-                            float4* d = reinterpret_cast<float4*>(a.part_o + part * D + c);
+                            for (int y = 0; y < 32; ++y) a.part_o[(part * D + c + y) * kChunkPartRows + r] = __uint_as_float(o[y]);
+                        continue;
+                    }
+                    // rows are turned through shared memory: four lanes then write 64 bytes of a row together
+                    __syncwarp();
 #pragma unroll
-                            for (int y = 0; y < 8; ++y) d[y] = make_float4(f[4 * y], f[4 * y + 1], f[4 * y + 2], f[4 * y + 3]);
+                    for (int y = 0; y < 4; ++y) {
+                        const float* f = reinterpret_cast<const float*>(o) + 8 * y;
+                        *reinterpret_cast<uint4*>(&sh.turn[warp][lane][16 * y]) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int rr = y * 8 + (lane >> 2), row = quarter * 32 + rr;
+                        if (row < tile_rows) {
+                            const int tk = p.tok0 + (p.alt ? 0 : g * a.TT) + row / a.G;
+                            *reinterpret_cast<uint4*>(out0 + ((size_t)tk * a.Hq + row % a.G) * D + c + (lane & 3) * 8) = *reinterpret_cast<const uint4*>(&sh.turn[warp][rr][16 * (lane & 3)]);
                         }
                     }
                 }
                 if (valid_row) {
-                    if (!whole) a.part_ml[part] = make_float2(m, l);
+                    if (!whole) a.part_ml[part * kChunkPartRows + r] = make_float2(m, l);
                     else {
                         const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
                         if (a.lse) a.lse[orow] = lse2 * 0.6931471805599453f;
@@ -530,7 +544,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
     tc_after();
     if (sh.abort) {  // uniform for the CTA: see everything this CTA has started end
         if (tid == 0) record_error(a.status, LETHE_ERR_TIMEOUT, blockIdx.x);
-        if (warp == kMmaWarp && lane == 0 && sh.issued) {
+        if (warp == kMmaWarp && sh.issued && elect_one()) {  // the lane that issued them: a commit follows one's own MMAs
             tc_commit(&sh.drained);
             bar_drain(&sh.drained, 0);
         }

@@ -67,6 +67,12 @@ __device__ __forceinline__ void bar_drain(unsigned long long* b, unsigned phase)
     }
 }
 
+// One lane of a converged warp: what it issues stays on the uniform datapath, where the MMA takes its descriptors from.
+__device__ __forceinline__ bool elect_one() {
+    unsigned ok;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(ok));
+    return ok != 0;
+}
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -229,17 +235,6 @@ __device__ __forceinline__ void gather_tile(const ChunkArgs& a, const void* base
             if (i < kTile * C) st_shared_16(chunk_addr(dst, i / C, i % C), bytes ? expand8(make_uint2(x[u].x, x[u].y), e5m2) : x[u]);
         }
     }
-}
-
-// First unit whose tiles reach beyond `tile` on the plan's line (u_start is non-decreasing; units without tiles are passed over).
-__device__ __forceinline__ int find_start(const int* start, int n, int tile) {
-    int lo = 0, hi = n;  // the last with start <= tile
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= tile) lo = mid;
-        else hi = mid;
-    }
-    return lo;
 }
 
 // Whether K and V tiles can come by TMA: bf16 rows, and pages that tile the 128 rows in whole swizzle groups.
