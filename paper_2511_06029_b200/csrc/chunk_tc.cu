@@ -2,13 +2,23 @@
 //
 // S = Q K^T and O += P V with tcgen05.mma: the 128 x 128 fp32 logits and the 128 x D outputs live in tensor memory, the softmax
 // threads read a row each, write the probabilities back as bf16 over the logits they came from, and those are the A operand of the
-// second product where they lie.  A CTA holds two row tiles (two softmax groups of four warps), so one group's exponentials run
-// under the other's products.  A unit with one row tile only (few new tokens) gives both groups alternate key tiles of it instead
-// and merges their halves at the end.  Row maxima are followed lazily: the outputs are rescaled only when a maximum has grown by
-// more than 2^8 since the last time, which a row's first few tiles settle; the sums stay far inside fp32.
+// second product where they lie.  A CTA holds two row tiles (two softmax groups of four warps) and each has a warp of its own that
+// issues its products, so one group's exponentials run under the other's products and neither waits for the other's hand-offs.
+// A softmax job is half a tile, 64 keys: the first half's probabilities are multiplied while the second half's are formed.  Row
+// maxima are followed lazily: the outputs are rescaled only when a maximum has grown by more than 2^8 since the last time, which
+// a row's first few tiles settle; the sums stay far inside fp32.  (Logits of 64 keys in two buffers, the next job's ahead of
+// this one's, were slower: a product with 64 columns takes as long as one with 128, it is bound by reading Q.)
 //
-// Roles: warps 0-7 softmax; warp 8 issues the MMAs; warp 9 fetches the query tiles; warp 10 K and V tiles by TMA (one thread) or,
-// for byte caches and odd page sizes, warps 10-13 read, convert and store them (exact: e4m3 and e5m2 are bf16 values).  K and V tiles alternate in a ring.  Negative scales flip the sign of Q inside the MMA.
+// What the two groups work on depends on the unit:
+//   pair  two row tiles: a group each, the same keys
+//   alt   one row tile: the groups take alternate key tiles and merge at the end
+//   quad  at most 16 rows (single tokens, drafted tokens): the rows are put into the tile four times, once per 32 lanes of tensor
+//         memory, and each of a group's four warps takes every fourth run of 16 keys (its probabilities of the others' keys are
+//         zero): all eight warps work instead of two, and the eight parts merge at the end
+//
+// Roles: warps 0-7 softmax; warps 8 and 9 issue the MMAs; warp 10 fetches the query tiles; warp 11 K and V tiles by TMA (one thread)
+// or, for byte caches and odd page sizes, warps 11-14 read, convert and store them (exact: e4m3 and e5m2 are bf16 values).  K and V
+// tiles alternate in a ring.  Negative scales flip the sign of Q inside the MMA.
 #include <string.h>
 
 #include "chunk_tc.cuh"
@@ -17,11 +27,12 @@ namespace lethe {
 namespace {
 
 constexpr int kSoftWarps = 8;
-constexpr int kMmaWarp = 8;
-constexpr int kQWarp = 9;
-constexpr int kLoadWarp = 10;    // TMA
-constexpr int kGatherWarp = 10;  // four warps
+constexpr int kMmaWarp = 8;      // and 9: one per group
+constexpr int kQWarp = 10;
+constexpr int kLoadWarp = 11;    // TMA
+constexpr int kGatherWarp = 11;  // four warps
 constexpr int kMaxStages = 8;
+constexpr int kQuadRows = 16;
 constexpr float kLazy = 8.f;  // log2 of the growth of a row maximum that is left standing
 
 template <bool TMA>
@@ -34,16 +45,21 @@ constexpr size_t smem_bytes() { return 1024 + (size_t)(2 + stages<D>()) * tile_b
 template <bool MOD>
 struct Shared {
     unsigned long long full[kMaxStages], empty[kMaxStages];
-    unsigned long long q_full, q_done, q_soft, merge;
-    unsigned long long s_full[2], p_full[2], o_full[2];
-    unsigned long long drained;
+    unsigned long long q_full, q_done, q_soft, merge, merge_all;
+    unsigned long long s_full[2], p_full[2][2], o_full[2][2];  // [group], [group][half]
+    unsigned long long drained[2];
     uint32_t tmem_base;
     int abort;
-    int loaded, q_loaded, issued;  // ring entries, query loads and MMAs started (for the drain after a timeout)
+    int loaded, q_loaded, issued[2];  // ring entries, query loads and MMAs started (for the drain after a timeout)
     float2 merge_ml[kTile];
     alignas(16) int kpos[MOD ? kSoftWarps : 1][kTile];     // positions of the tile's keys, one copy per warp
     alignas(16) float kposf[MOD ? kSoftWarps : 1][kTile];  // the same relative to the unit's first query
     alignas(16) unsigned char turn[kSoftWarps][32][80];     // 32 columns of a warp's output rows on their way out (rows 16 bytes apart in the banks)
+};
+
+template <int N>
+struct Width {
+    static constexpr int value = N;
 };
 
 // A CTA's piece of a unit, as every role derives it from the plan.
@@ -52,7 +68,8 @@ struct Piece {
     int tok0, toks;  // tokens of the unit
     int tile0, nt;   // key tiles
     int hi;          // slots from here on are hidden from the whole unit
-    bool alt;        // one row tile, the groups take alternate key tiles
+    bool alt;        // one row tile, the groups take alternate key tiles (quad included)
+    bool quad;       // at most 16 rows
     bool head, tail; // begins / ends here
 };
 
@@ -66,9 +83,42 @@ __device__ __forceinline__ Piece piece_of(const ChunkArgs& a, int u, int at, int
     p.tile0 = (a.u_lo ? a.u_lo[u] : 0) + at - s0;
     p.nt = stop - at;
     p.alt = p.toks <= a.TT;
+    p.quad = p.toks * a.G <= kQuadRows;
     p.head = at == s0;
     p.tail = stop == s1;
     return p;
+}
+
+// Jobs of group g in a piece: two halves of each of its tiles; a last tile of which only the first half is seen has one.
+__device__ __forceinline__ int piece_jobs(const Piece& p, int g) {
+    const bool short_end = p.hi - (p.tile0 + p.nt - 1) * kTile <= 64;
+    if (!p.alt) return 2 * p.nt - short_end;
+    return 2 * ((p.nt - g + 1) >> 1) - (short_end && ((p.nt - 1) & 1) == g);
+}
+
+// Ring entries of a piece's tiles.  A pair goes through K and V of one tile at a time; with alternate tiles both groups' K come first
+// (a group needs its next K before the other has let its V go: in the ring's order K0 V0 K1 V1 four slots would lock up).
+__device__ __forceinline__ int k_entry(const Piece& p, int t) { return p.alt ? 4 * (t >> 1) + (t & 1) : 2 * t; }
+__device__ __forceinline__ int v_entry(const Piece& p, int t) { return p.alt ? 4 * (t >> 1) + min(2, p.nt - (t & ~1)) + (t & 1) : 2 * t + 1; }
+__device__ __forceinline__ int entry_tile(const Piece& p, int e, bool& is_v) {
+    if (!p.alt) {
+        is_v = e & 1;
+        return e >> 1;
+    }
+    const int both = min(2, p.nt - 2 * (e >> 2)), rem = e & 3;
+    is_v = rem >= both;
+    return 2 * (e >> 2) + (is_v ? rem - both : rem);
+}
+
+// A wait for a ring entry looks at one bit of the slot's phase, so the waiter has to know that the slot's entry before has landed:
+// it has used that one itself, or a piece lies between.  The V of a last tile without a partner is the exception, it follows a K
+// of the other group; whoever waits for it first sees that the loader has got to it (which it does only once that K is used).
+__device__ __forceinline__ bool lone_v(const Piece& p, int t) { return p.alt && t + 1 == p.nt && !(t & 1); }
+__device__ __forceinline__ bool wait_issued(volatile int* loaded, int e, volatile int* abort_flag, int limit) {
+    bool ok = *loaded > e;
+    for (int it = 1; !ok && it < limit && !*abort_flag; ++it) ok = *loaded > e;
+    if (!ok) *abort_flag = 1;
+    return __all_sync(0xffffffffu, ok);
 }
 
 // Calls f(piece) for each piece of this CTA, in order; f returns false to stop.
@@ -92,7 +142,7 @@ __device__ __forceinline__ void for_pieces(const ChunkArgs& a, F f) {
 template <int D, bool TMA, bool MOD>
 __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps) {
     constexpr int TILE = tile_bytes<D>(), NS = stages<D>(), KS = D / 16;
-    constexpr int kOCol = 256;  // tensor memory: S0 | S1 | O0 | O1, 128 columns each (P over its S)
+    constexpr int kOCol = 256;  // tensor memory: S0 | S1 | O0 | O1, 128 columns each (P over its S, each half over its own)
     extern __shared__ unsigned char dyn_raw[];
     __shared__ Shared<MOD> sh;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -106,19 +156,22 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
     if (tid == 0) {
         for (int i = 0; i < NS; ++i) {
             bar_init(&sh.full[i], TMA ? 1 : 4);
-            bar_init(&sh.empty[i], 1);
+            bar_init(&sh.empty[i], 2);
         }
         bar_init(&sh.q_full, 1);
-        bar_init(&sh.q_done, 1);
+        bar_init(&sh.q_done, 2);
         bar_init(&sh.q_soft, kSoftWarps);
         bar_init(&sh.merge, 4);
+        bar_init(&sh.merge_all, kSoftWarps);
         for (int g = 0; g < 2; ++g) {
             bar_init(&sh.s_full[g], 1);
-            bar_init(&sh.p_full[g], 4);
-            bar_init(&sh.o_full[g], 1);
+            for (int hf = 0; hf < 2; ++hf) {
+                bar_init(&sh.p_full[g][hf], 4);
+                bar_init(&sh.o_full[g][hf], 1);
+            }
+            bar_init(&sh.drained[g], 1);
         }
-        bar_init(&sh.drained, 1);
-        sh.abort = sh.loaded = sh.q_loaded = sh.issued = 0;
+        sh.abort = sh.loaded = sh.q_loaded = sh.issued[0] = sh.issued[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMmaWarp) {
@@ -143,8 +196,10 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         const int s = e % NS;
                         if (e >= NS && !bar_wait(&sh.empty[s], e / NS - 1, abort_flag, limit)) return false;
                         bar_expect_tx(&sh.full[s], TILE);
-                        sh.loaded = e + 1;
-                        tma_tile<D>(a, (t & 1) ? &maps.v : &maps.k, p.it.item, p.it.n, (p.tile0 + (t >> 1)) * kTile, ring + s * TILE, &sh.full[s], &bad);
+                        *(volatile int*)&sh.loaded = e + 1;
+                        bool is_v;
+                        const int tile = p.tile0 + entry_tile(p, t, is_v);
+                        tma_tile<D>(a, is_v ? &maps.v : &maps.k, p.it.item, p.it.n, tile * kTile, ring + s * TILE, &sh.full[s], &bad);
                     }
                     if (bad) record_error(a.status, LETHE_ERR_PAGE, p.it.item);
                     bad = false;
@@ -157,7 +212,10 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                 for (int t = 0; t < 2 * p.nt; ++t, ++e) {
                     const int s = e % NS;
                     if (e >= NS && !warp_wait(&sh.empty[s], e / NS - 1, abort_flag, limit)) return false;
-                    gather_tile<D>(a, (t & 1) ? a.v : a.k, p.it.item, p.hi, (p.tile0 + (t >> 1)) * kTile, ring + s * TILE, tid - kGatherWarp * 32, 128, &bad);
+                    if (tid == kGatherWarp * 32) *(volatile int*)&sh.loaded = e + 1;
+                    bool is_v;
+                    const int tile = p.tile0 + entry_tile(p, t, is_v);
+                    gather_tile<D>(a, is_v ? a.v : a.k, p.it.item, p.hi, tile * kTile, ring + s * TILE, tid - kGatherWarp * 32, 128, &bad);
                     proxy_fence();
                     __syncwarp();
                     if (lane == 0) bar_arrive(&sh.full[s]);
@@ -174,68 +232,84 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
             for_pieces(a, [&](const Piece& p) {
                 // the previous unit's products have read the tiles, and its softmax groups are done with them as merge space
                 if (k > 0 && (!bar_wait(&sh.q_done, k - 1, abort_flag, limit) || !bar_wait(&sh.q_soft, k - 1, abort_flag, limit))) return false;
-                const int tiles = p.alt ? 1 : 2;
-                bar_expect_tx(&sh.q_full, (unsigned)(tiles * used * D * 2));
+                const int copies = p.quad ? 4 : p.alt ? 1 : 2;
+                const CUtensorMap* map = p.quad ? &maps.q16 : &maps.q;
+                bar_expect_tx(&sh.q_full, (unsigned)(copies * (p.quad ? kQuadRows / a.G * a.G : used) * D * 2));
                 sh.q_loaded = k + 1;
-                for (int g = 0; g < tiles; ++g)
+                for (int c = 0; c < copies; ++c)
 #pragma unroll
                     for (int hf = 0; hf < D / 64; ++hf)
-                        tma_4d(q_tile + g * TILE + hf * kHalfBytes, &maps.q, 64 * hf, p.it.hkv * a.G, p.it.first + p.tok0 + g * a.TT, p.it.li, &sh.q_full);
+                        tma_4d(q_tile + (p.quad ? c * 32 * 128 : c * TILE) + hf * kHalfBytes, map, 64 * hf, p.it.hkv * a.G, p.it.first + p.tok0 + (p.quad ? 0 : c * a.TT), p.it.li, &sh.q_full);
                 ++k;
                 return true;
             });
         }
         __syncwarp();
-    } else if (warp == kMmaWarp) {
+    } else if (warp >= kMmaWarp) {
         // ------------------------------------------------------------------ MMA issue: the warp waits as one, one lane issues
+        const int g = warp - kMmaWarp;
         const uint32_t pv_desc = mma_idesc(D, true, false);
         const uint64_t q_desc = smem_desc(q_tile, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, kHalfBytes);
-        int k = 0, base = 0;              // pieces done, first ring entry of the piece
-        int jobs_p[2] = {0, 0};           // probabilities consumed so far, per group
+        const uint32_t st = tmem + g * 128, ot = tmem + kOCol + g * 128;
+        int k = 0, base = 0;   // pieces done, first ring entry of the piece
+        unsigned np = 0;       // tiles whose probabilities have been consumed (first halves; second halves may be fewer)
+        unsigned np1 = 0;
         for_pieces(a, [&](const Piece& p) {
             const uint32_t qk_desc = mma_idesc(kTile, false, a.scale[p.it.l] < 0.f);
-            const int jobs = p.alt ? p.nt : 2 * p.nt;
+            const uint64_t qd = q_desc + (uint64_t)((p.alt ? 0 : g) * (TILE >> 4));
+            const int step = p.alt ? 2 : 1, t0 = p.alt ? g : 0;
             if (!warp_wait(&sh.q_full, k, abort_flag, limit)) return false;
-            auto entry_full = [&](int e) { return warp_wait(&sh.full[e % NS], e / NS, abort_flag, limit); };
-            for (int i = 0; i < jobs + 2; ++i) {
-                const int g = i & 1;
-                if (i >= 2) {  // P V of job i - 2
-                    const int t = p.alt ? i - 2 : (i - 2) >> 1, e = base + 2 * t + 1;
-                    if (!entry_full(e)) return false;
-                    if (!warp_wait(&sh.p_full[g], jobs_p[g]++, abort_flag, limit)) return false;
-                    tc_after();
-                    const int steps = max(1, (min(kTile, p.hi - (p.tile0 + t) * kTile) + 15) / 16);
-                    const bool first = p.alt ? t < 2 : t == 0;
-                    if (elect_one()) {
-                        const uint64_t vd = v_desc + (uint64_t)((e % NS) * (TILE >> 4));
-                        const uint32_t pt = tmem + g * 128, ot = tmem + kOCol + g * 128;
+            // a tile's ring entry is let go by both groups, or twice by the one that uses it
+            auto let_go = [&](int slot) {
+                tc_commit(&sh.empty[slot]);
+                if (p.alt) tc_commit(&sh.empty[slot]);
+            };
+            auto qk = [&](int t) -> bool {
+                const int e = base + k_entry(p, t), slot = e % NS;
+                if (!warp_wait(&sh.full[slot], e / NS, abort_flag, limit)) return false;
+                tc_after();
+                if (elect_one()) {
+                    const uint64_t kd = k_desc + (uint64_t)(slot * (TILE >> 4));
 #pragma unroll
-                        for (int ks = 0; ks < kTile / 16; ++ks)
-                            if (ks < steps) mma_ts(ot, pt + ks * 8, vd + ks * (2048 >> 4), pv_desc, !first || ks > 0);
-                        sh.issued = 1;
-                        tc_commit(&sh.o_full[g]);
-                        if (p.alt || g == 1) tc_commit(&sh.empty[e % NS]);
+                    for (int ks = 0; ks < KS; ++ks) {
+                        constexpr int half16 = kHalfBytes >> 4;
+                        mma_ss(st, qd + (ks >> 2) * half16 + (ks & 3) * 2, kd + (ks >> 2) * half16 + (ks & 3) * 2, qk_desc, ks > 0);
+                    }
+                    sh.issued[g] = 1;
+                    tc_commit(&sh.s_full[g]);
+                    let_go(slot);
+                    if (t + step >= p.nt) tc_commit(&sh.q_done);
+                }
+                __syncwarp();
+                return true;
+            };
+            if (t0 < p.nt) {
+                if (!qk(t0)) return false;
+            } else if (elect_one()) tc_commit(&sh.q_done);  // no tile for this group
+            __syncwarp();
+            for (int t = t0; t < p.nt; t += step) {
+                const int e = base + v_entry(p, t), slot = e % NS;
+                const int seen = p.hi - (p.tile0 + t) * kTile;
+                const bool two_halves = seen > 64 || t + 1 < p.nt;
+                const uint64_t vd = v_desc + (uint64_t)(slot * (TILE >> 4));
+                if (lone_v(p, t) && !wait_issued(&sh.loaded, e, abort_flag, limit)) return false;
+                if (!warp_wait(&sh.full[slot], e / NS, abort_flag, limit)) return false;
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    if (hf == 1 && !two_halves) break;
+                    if (!warp_wait(&sh.p_full[g][hf], hf ? np1++ : np++, abort_flag, limit)) return false;
+                    tc_after();
+                    const int steps = max(1, (min(64, seen - 64 * hf) + 15) / 16);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks)
+                            if (ks < steps) mma_ts(ot, st + 64 * hf + ks * 8, vd + (uint64_t)((hf * 4 + ks) * (2048 >> 4)), pv_desc, t > t0 || hf > 0 || ks > 0);
+                        tc_commit(&sh.o_full[g][hf]);
+                        if (hf == 1 || !two_halves) let_go(slot);
                     }
                     __syncwarp();
                 }
-                if (i < jobs) {  // Q K^T of job i
-                    const int t = p.alt ? i : i >> 1, e = base + 2 * t;
-                    if (!entry_full(e)) return false;
-                    tc_after();
-                    if (elect_one()) {
-                        const uint64_t qd = q_desc + (uint64_t)((p.alt ? 0 : g) * (TILE >> 4)), kd = k_desc + (uint64_t)((e % NS) * (TILE >> 4));
-#pragma unroll
-                        for (int ks = 0; ks < KS; ++ks) {
-                            constexpr int half16 = kHalfBytes >> 4;
-                            mma_ss(tmem + g * 128, qd + (ks >> 2) * half16 + (ks & 3) * 2, kd + (ks >> 2) * half16 + (ks & 3) * 2, qk_desc, ks > 0);
-                        }
-                        sh.issued = 1;
-                        tc_commit(&sh.s_full[g]);
-                        if (p.alt || g == 1) tc_commit(&sh.empty[e % NS]);
-                        if (i == jobs - 1) tc_commit(&sh.q_done);
-                    }
-                    __syncwarp();
-                }
+                if (t + step < p.nt && !qk(t + step)) return false;
             }
             base += 2 * p.nt;
             ++k;
@@ -243,24 +317,28 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
         });
     } else {
         // ------------------------------------------------------------------ softmax
-        const int g = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;  // group, TMEM lane
+        const int g = warp >> 2, quarter = warp & 3;
         const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + g * 128;
         const uint32_t o_addr = s_addr + kOCol;
         const bool by_pos = MOD && (a.slopes || a.window > 0 || a.doc_start || a.prefix_len);
         const bool mask_pos = MOD && (a.window > 0 || a.doc_start || a.prefix_len);
-        int n_s = 0, n_o = 0, n_v = 0, k = 0, n_m = 0;  // logit tiles, output products and ring entries so far; pieces, merged pieces
+        float* const merge_o = reinterpret_cast<float*>(q_generic);  // parts to merge, where the query tiles were
+        unsigned n_s = 0, o0 = 0, o1 = 0;         // logit tiles taken, and products asked for so far, per half
+        int n_v = 0, k = 0, n_m = 0, n_q = 0;     // ring entries so far; pieces, merged pieces, quad pieces
         for_pieces(a, [&](const Piece& p) {
-            const int tile_rows = min(used, p.toks * a.G - (p.alt ? 0 : g * used));
+            const int r = p.quad ? lane : quarter * 32 + lane;  // row of the tile
+            const int tile_rows = p.quad ? p.toks * a.G : min(used, p.toks * a.G - (p.alt ? 0 : g * used));
             const bool valid_row = r < tile_rows;
-            const bool busy = quarter * 32 < tile_rows;  // the warp has rows at all
+            const bool busy = p.quad || quarter * 32 < tile_rows;  // the warp has rows at all
             const int tok = p.tok0 + (p.alt ? 0 : g * a.TT) + min(r, tile_rows - 1) / a.G, h = r % a.G;
             // a scale of zero is a very small one here, so that a hidden key's -inf stays one
             const float scale = fabsf(a.scale[p.it.l]) * a.k_scale[p.it.l], sl2 = fmaxf(scale * 1.4426950408889634f, 1e-36f);
             // rows that are not there count as seeing everything: they never ask for a mask
             const int lim = valid_row && a.append ? p.it.n_old + tok + 1 : INT32_MAX;
-            int qpos = 0, lo = INT32_MIN, pos0 = 0, prefix = INT32_MIN;
+            int lo = INT32_MIN, pos0 = 0, prefix = INT32_MIN;
             float slope = 0.f, qf = 0.f, cap_in = 0.f, cap2 = 0.f;
             if (MOD) {
+                int qpos = 0;
                 if (a.token_pos) {
                     qpos = a.token_pos[p.it.first + tok];
                     pos0 = a.token_pos[p.it.first + p.tok0];
@@ -274,13 +352,14 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     cap2 = a.softcap * 1.4426950408889634f;
                 }
             }
+            // what a logit has to be multiplied by, once shaped, to be in log2 units
+            const float ml = MOD && (a.softcap > 0.f || a.slopes) ? 1.f : sl2;
             float m = -INFINITY, l = 0.f;
-            const int jobs = p.alt ? p.nt : 2 * p.nt;
-            int done = 0;  // jobs of this group in the piece
-            for (int i = g; i < jobs; i += 2, ++done) {
-                const int t = p.alt ? i : i >> 1, j0 = (p.tile0 + t) * kTile;
-                int kp_min = INT32_MIN;
-                if (MOD && by_pos && busy) {  // positions of the tile's keys, while the product runs
+            const int jobs = piece_jobs(p, g);
+            int kp_min = INT32_MIN;
+            for (int n = 0; n < jobs; ++n) {
+                const int buf = n & 1, t = p.alt ? 2 * (n >> 1) + g : n >> 1, j0 = (p.tile0 + t) * kTile;
+                if (MOD && by_pos && busy && buf == 0) {  // positions of the tile's keys, while the product runs
                     const int32_t* pos = a.pos + (size_t)p.it.item * a.cap_tokens + j0;
                     kp_min = INT32_MAX;
                     __syncwarp();
@@ -294,116 +373,98 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     kp_min = __reduce_min_sync(0xffffffffu, kp_min);
                     __syncwarp();
                 }
-                if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
-                tc_after();
-                const int valid = min(kTile, p.hi - j0);
-                if (valid < kTile && (valid <= 0 || (valid & 15))) {
-                    // Rows behind the last slot may hold anything, and 0 x NaN is NaN: clear those the product's last step takes in.  Not before
-                    // the logits are there: they show that the group's previous product, and with it the ring slot's last entry, is done
-                    // (a wait that is a whole turn of the ring early would take the last entry's phase for this one's).
-                    const int e = n_v + 2 * t + 1, r0 = max(valid, 0), rows = max(16, (valid + 15) & ~15) - r0;
+                if (buf == 0) {
+                    if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
+                    tc_after();
+                }
+                const int seen = p.hi - j0 - 64 * buf;  // keys of this half that the unit sees at all
+                if (seen < 64 && (seen <= 0 || (seen & 15))) {
+                    // Rows behind the last slot may hold anything, and 0 x NaN is NaN: clear those the product's last step takes in.
+                    // Not before the logits are there: they show that the tile before, and with it the ring slot's last entry, is
+                    // done (a wait that is a whole turn of the ring early would take the last entry's phase for this one's).
+                    const int e = n_v + v_entry(p, t), r0 = 64 * buf + max(seen, 0), rows = 64 * buf + max(16, (seen + 15) & ~15) - r0;
+                    if (lone_v(p, t) && !wait_issued(&sh.loaded, e, abort_flag, limit)) return false;
                     if (!warp_wait(&sh.full[e % NS], e / NS, abort_flag, limit)) return false;
-                    for (int x = r; x < rows * (D / 8); x += kTile) st_shared_16(chunk_addr(ring + (e % NS) * TILE, r0 + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
+                    for (int x = quarter * 32 + lane; x < rows * (D / 8); x += kTile) st_shared_16(chunk_addr(ring + (e % NS) * TILE, r0 + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
                     proxy_fence();
                 }
-                if (busy) {
-                    // The row in two halves of 64 logits: the first is shaped, its maximum taken and (if shaping changed it) put back,
-                    // the second stays in registers; after the maximum the second half's probabilities are formed, then the first
-                    // half is read again, then both are stored (the second half's land on the first half's logits).
-                    uint32_t v[64], pk[32];
-                    float ml = sl2;  // what a logit still has to be multiplied by to be in log2 units
-                    float top = -INFINITY;
-                    bool shaped = false;
-                    auto half_max = [&](const int c0) {
-                        if (MOD) {
-                            ml = sl2;
-                            if (a.softcap > 0.f) {
-                                ml = 1.f;
-                                shaped = true;
-#pragma unroll
-                                for (int c = 0; c < 64; c += 8) {
-                                    float x[8], big = 0.f;
-#pragma unroll
-                                    for (int y = 0; y < 8; ++y) {
-                                        x[y] = __uint_as_float(v[c + y]) * cap_in;
-                                        big = fmaxf(big, fabsf(x[y]));
-                                        v[c + y] = __float_as_uint(cap2 * capped_small(x[y]));
-                                    }
-                                    if (__any_sync(0xffffffffu, big > 0.55f)) {
-#pragma unroll
-                                        for (int y = 0; y < 8; ++y)
-                                            if (fabsf(x[y]) > 0.55f) v[c + y] = __float_as_uint(cap2 * capped_large(x[y]));
-                                    }
-                                }
-                            }
-                            if (a.slopes) {
-                                shaped = true;
-#pragma unroll
-                                for (int c = 0; c < 64; c += 4) {
-                                    const float4 kf = *reinterpret_cast<const float4*>(&sh.kposf[warp][c0 + c]);
-                                    v[c] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.x), __uint_as_float(v[c]) * ml));
-                                    v[c + 1] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.y), __uint_as_float(v[c + 1]) * ml));
-                                    v[c + 2] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.z), __uint_as_float(v[c + 2]) * ml));
-                                    v[c + 3] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.w), __uint_as_float(v[c + 3]) * ml));
-                                }
-                                ml = 1.f;
-                            }
-                        }
-                        if (MOD && mask_pos) {
-                            if (!__all_sync(0xffffffffu, kp_min >= lo && lim - j0 >= kTile && p.it.n - j0 >= kTile)) {
-                                const int nn = p.it.n - j0 - c0, nv = lim == INT32_MAX ? nn : lim - j0 - c0;
-                                shaped = true;
-#pragma unroll
-                                for (int c = 0; c < 64; c += 4) {
-                                    const int4 kp = *reinterpret_cast<const int4*>(&sh.kpos[warp][c0 + c]);
-                                    if (!((c < nv || (kp.x < prefix && c < nn)) && kp.x >= lo)) v[c] = 0xff800000u;
-                                    if (!((c + 1 < nv || (kp.y < prefix && c + 1 < nn)) && kp.y >= lo)) v[c + 1] = 0xff800000u;
-                                    if (!((c + 2 < nv || (kp.z < prefix && c + 2 < nn)) && kp.z >= lo)) v[c + 2] = 0xff800000u;
-                                    if (!((c + 3 < nv || (kp.w < prefix && c + 3 < nn)) && kp.w >= lo)) v[c + 3] = 0xff800000u;
-                                }
-                            }
-                        } else {
-                            const int nv = min(lim, p.it.n) - j0 - c0;  // keys of this half that the row sees
-                            if (__any_sync(0xffffffffu, nv < 64)) {
-                                shaped = true;
-#pragma unroll
-                                for (int c = 0; c < 64; ++c)
-                                    if (c >= nv) v[c] = 0xff800000u;
-                            }
-                        }
-                        float m0 = top, m1 = __uint_as_float(v[1]), m2 = __uint_as_float(v[2]), m3 = __uint_as_float(v[3]);
-                        m0 = fmaxf(m0, __uint_as_float(v[0]));
-#pragma unroll
-                        for (int c = 4; c < 64; c += 4) {
-                            m0 = fmaxf(m0, __uint_as_float(v[c]));
-                            m1 = fmaxf(m1, __uint_as_float(v[c + 1]));
-                            m2 = fmaxf(m2, __uint_as_float(v[c + 2]));
-                            m3 = fmaxf(m3, __uint_as_float(v[c + 3]));
-                        }
-                        top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-                    };
-                    tmem_ld32(s_addr, v);
-                    tmem_ld32(s_addr + 32, v + 32);
+                // NC logits of the thread's row from column c0 of the tile: the whole half, or a quad warp's share of it
+                auto job = [&](auto width) -> bool {
+                    constexpr int NC = decltype(width)::value;
+                    const int c0 = 64 * buf + (NC == 64 ? 0 : NC * quarter);
+                    const uint32_t s_buf = s_addr + 64 * buf;
+                    uint32_t v[NC], pk[32];
+                    if (NC == 64) {
+                        tmem_ld32(s_buf, v);
+                        tmem_ld32(s_buf + 32, v + (NC == 64 ? 32 : 0));
+                    } else tmem_ld16(s_buf + NC * quarter, v);
                     tmem_ld_wait();
-                    half_max(0);
-                    if (shaped) {  // uniform for the warp
-                        tmem_st32(s_addr, v);
-                        tmem_st32(s_addr + 32, v + 32);
+                    if (MOD) {
+                        if (a.softcap > 0.f) {
+#pragma unroll
+                            for (int c = 0; c < NC; c += 8) {
+                                float x[8], big = 0.f;
+#pragma unroll
+                                for (int y = 0; y < 8; ++y) {
+                                    x[y] = __uint_as_float(v[c + y]) * cap_in;
+                                    big = fmaxf(big, fabsf(x[y]));
+                                    v[c + y] = __float_as_uint(cap2 * capped_small(x[y]));
+                                }
+                                if (__any_sync(0xffffffffu, big > 0.55f)) {
+#pragma unroll
+                                    for (int y = 0; y < 8; ++y)
+                                        if (fabsf(x[y]) > 0.55f) v[c + y] = __float_as_uint(cap2 * capped_large(x[y]));
+                                }
+                            }
+                        }
+                        if (a.slopes) {
+                            const float in = a.softcap > 0.f ? 1.f : sl2;
+#pragma unroll
+                            for (int c = 0; c < NC; c += 4) {
+                                const float4 kf = *reinterpret_cast<const float4*>(&sh.kposf[warp][c0 + c]);
+                                v[c] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.x), __uint_as_float(v[c]) * in));
+                                v[c + 1] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.y), __uint_as_float(v[c + 1]) * in));
+                                v[c + 2] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.z), __uint_as_float(v[c + 2]) * in));
+                                v[c + 3] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.w), __uint_as_float(v[c + 3]) * in));
+                            }
+                        }
                     }
-                    tmem_ld32(s_addr + 64, v);
-                    tmem_ld32(s_addr + 96, v + 32);
-                    tmem_ld_wait();
-                    half_max(64);
-                    const float mt = top * ml;
+                    if (MOD && mask_pos) {
+                        if (!__all_sync(0xffffffffu, kp_min >= lo && lim - j0 >= kTile && p.it.n - j0 >= kTile)) {
+                            const int nn = p.it.n - j0 - c0, nv = lim == INT32_MAX ? nn : lim - j0 - c0;
+#pragma unroll
+                            for (int c = 0; c < NC; c += 4) {
+                                const int4 kp = *reinterpret_cast<const int4*>(&sh.kpos[warp][c0 + c]);
+                                if (!((c < nv || (kp.x < prefix && c < nn)) && kp.x >= lo)) v[c] = 0xff800000u;
+                                if (!((c + 1 < nv || (kp.y < prefix && c + 1 < nn)) && kp.y >= lo)) v[c + 1] = 0xff800000u;
+                                if (!((c + 2 < nv || (kp.z < prefix && c + 2 < nn)) && kp.z >= lo)) v[c + 2] = 0xff800000u;
+                                if (!((c + 3 < nv || (kp.w < prefix && c + 3 < nn)) && kp.w >= lo)) v[c + 3] = 0xff800000u;
+                            }
+                        }
+                    } else {
+                        const int nv = min(lim, p.it.n) - j0 - c0;  // of these keys the row sees so many
+                        if (__any_sync(0xffffffffu, nv < NC)) {
+#pragma unroll
+                            for (int c = 0; c < NC; ++c)
+                                if (c >= nv) v[c] = 0xff800000u;
+                        }
+                    }
+                    float m0 = __uint_as_float(v[0]), m1 = __uint_as_float(v[1]);
+#pragma unroll
+                    for (int c = 2; c + 3 < NC; c += 4) {
+                        m0 = max3(m0, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                        m1 = max3(m1, __uint_as_float(v[c + 2]), __uint_as_float(v[c + 3]));
+                    }
+                    const float mt = max3(fmaxf(m0, m1), __uint_as_float(v[NC - 2]), __uint_as_float(v[NC - 1])) * ml;
                     const bool grow = valid_row && mt > m + kLazy;  // true from -inf too
                     if (__any_sync(0xffffffffu, grow)) {
                         const float w = grow ? exp2_diff(m, mt) : 1.f;
                         if (grow) m = mt;
                         l *= w;
-                        if (done > 0) {
-                            if (!warp_wait(&sh.o_full[g], n_o + done - 1, abort_flag, limit)) return false;
+                        if (n > 0) {  // the product of the job before may still be adding
+                            if (!warp_wait(&sh.o_full[g][buf ^ 1], (buf ? o0 : o1) - 1, abort_flag, limit)) return false;
                             tc_after();
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < D; c += 32) {
                                 tmem_ld32(o_addr + c, pk);
                                 tmem_ld_wait();
@@ -413,121 +474,178 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                             }
                         }
                     }
-                    const float nm = m == -INFINITY ? 0.f : -m;
-                    float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
-                    auto half_exp = [&]() {
+                    const uint64_t ml2 = two(ml, ml), nm2 = m == -INFINITY ? 0 : two(-m, -m);
+                    uint64_t la = 0, lb = 0;
 #pragma unroll
-                        for (int y = 0; y < 64; y += 4) {
-                            const float p0 = fast_exp2(fmaf(__uint_as_float(v[y]), ml, nm)), p1 = fast_exp2(fmaf(__uint_as_float(v[y + 1]), ml, nm));
-                            const float p2 = fast_exp2(fmaf(__uint_as_float(v[y + 2]), ml, nm)), p3 = fast_exp2(fmaf(__uint_as_float(v[y + 3]), ml, nm));
-                            l0 += p0;
-                            l1 += p1;
-                            l2 += p2;
-                            l3 += p3;
-                            pk[y / 2] = pack_bf16(p0, p1);
-                            pk[y / 2 + 1] = pack_bf16(p2, p3);
+                    for (int y = 0; y < NC; y += 4) {
+                        const float2 xa = apart(fma2(two(__uint_as_float(v[y]), __uint_as_float(v[y + 1])), ml2, nm2));
+                        const float2 xb = apart(fma2(two(__uint_as_float(v[y + 2]), __uint_as_float(v[y + 3])), ml2, nm2));
+                        const float p0 = fast_exp2(xa.x), p1 = fast_exp2(xa.y), p2 = fast_exp2(xb.x), p3 = fast_exp2(xb.y);
+                        la = add2(la, two(p0, p1));
+                        lb = add2(lb, two(p2, p3));
+                        pk[y / 2] = pack_bf16(p0, p1);
+                        pk[y / 2 + 1] = pack_bf16(p2, p3);
+                    }
+                    const float2 sum = apart(add2(la, lb));
+                    l += sum.x + sum.y;
+                    if (NC == 64) tmem_st32(s_buf, pk);
+                    else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            uint32_t z[8];
+#pragma unroll
+                            for (int y = 0; y < 8; ++y) z[y] = q == quarter ? pk[y] : 0u;
+                            tmem_st8(s_buf + 8 * q, z);
                         }
-                    };
-                    half_exp();
-                    if (shaped) tmem_st_wait();
-                    tmem_ld32(s_addr, v);
-                    tmem_ld32(s_addr + 32, v + 32);
-                    tmem_ld_wait();
-                    tmem_st32(s_addr + 32, pk);
-                    half_exp();
-                    tmem_st32(s_addr, pk);
-                    l += (l0 + l1) + (l2 + l3);
+                    }
                     tmem_st_wait();
+                    return true;
+                };
+                if (p.quad) {
+                    if (!job(Width<16>())) return false;
+                } else if (busy) {
+                    if (!job(Width<64>())) return false;
                 }
+                if (buf) ++o1;
+                else ++o0;
                 tc_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(&sh.p_full[g]);
+                if (lane == 0) bar_arrive(&sh.p_full[g][buf]);
             }
             n_v += 2 * p.nt;
             // ---- the piece's outputs
-            if (done > 0 && !warp_wait(&sh.o_full[g], n_o + done - 1, abort_flag, limit)) return false;
-            n_o += done;
+            if (jobs > 0 && !warp_wait(&sh.o_full[g][(jobs - 1) & 1], ((jobs - 1) & 1 ? o1 : o0) - 1, abort_flag, limit)) return false;
             tc_after();
-            float* const merge_o = reinterpret_cast<float*>(q_generic);  // [D][128]: the query tiles have been read by then
-            if (p.alt) {
-                if (g == 1) {
-                    if (!warp_wait(&sh.q_done, k, abort_flag, limit)) return false;
-                    if (busy) {
-                        sh.merge_ml[r] = make_float2(m, l);
-                        if (done > 0) {
+            const bool whole = p.head && p.tail;
+            const size_t part = ((size_t)blockIdx.x * 2 + (p.head ? 1 : 0)) * 2 + (p.alt ? 0 : g);
+            __nv_bfloat16* const out0 = (__nv_bfloat16*)a.out + (((size_t)p.it.li * a.n_tokens + p.it.first) * a.Hq + p.it.hkv * a.G) * D;
+            auto row_stats = [&](int token, int head, int row, float mr, float lr) {
+                if (!whole) a.part_ml[part * kChunkPartRows + row] = make_float2(mr, lr);
+                else {
+                    const float lse2 = lr == 0.f ? -INFINITY : mr + log2f(lr);
+                    if (a.lse) a.lse[((size_t)p.it.li * a.n_tokens + p.it.first + token) * a.Hq + p.it.hkv * a.G + head] = lse2 * 0.6931471805599453f;
+                    a.nlse2[(((size_t)p.it.li * a.Hkv + p.it.hkv) * a.n_tokens + p.it.first + token) * a.G + head] = lr == 0.f ? -INFINITY : -lse2;
+                }
+            };
+            if (p.quad) {
+                // eight parts [warp][D][16 rows]; then every warp finishes D / 8 columns of all rows
+                if (!warp_wait(&sh.q_done, k, abort_flag, limit)) return false;
+                if (lane < kQuadRows) sh.merge_ml[warp * kQuadRows + lane] = make_float2(m, l);
+                if (jobs > 0) {
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                uint32_t o[32];
-                                tmem_ld32(o_addr + c, o);
-                                tmem_ld_wait();
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_addr + c, o);
+                        tmem_ld_wait();
+                        if (lane < kQuadRows)
 #pragma unroll
-                                for (int y = 0; y < 32; ++y) merge_o[(c + y) * kTile + r] = __uint_as_float(o[y]);
+                            for (int y = 0; y < 32; ++y) merge_o[(warp * D + c + y) * kQuadRows + lane] = __uint_as_float(o[y]);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.merge_all);
+                if (!warp_wait(&sh.merge_all, n_q++, abort_flag, limit)) return false;
+                constexpr int NE = D / 16;
+                const int row = lane & (kQuadRows - 1), d0 = warp * (D / 8) + (lane >> 4) * NE;
+                if (row < tile_rows) {
+                    float mx = -INFINITY, lt = 0.f, acc[NE] = {};
+#pragma unroll
+                    for (int i = 0; i < kSoftWarps; ++i) mx = fmaxf(mx, sh.merge_ml[i * kQuadRows + row].x);
+#pragma unroll
+                    for (int i = 0; i < kSoftWarps; ++i) {
+                        const float2 part_i = sh.merge_ml[i * kQuadRows + row];
+                        const float w = exp2_diff(part_i.x, mx);
+                        lt += part_i.y * w;
+                        if (w != 0.f)
+#pragma unroll
+                            for (int e = 0; e < NE; ++e) acc[e] = fmaf(merge_o[(i * D + d0 + e) * kQuadRows + row], w, acc[e]);
+                    }
+                    const int token = p.tok0 + row / a.G, head = row % a.G;
+                    if (whole) {
+                        const float inv = lt == 0.f ? 0.f : a.v_scale[p.it.l] / lt;
+                        uint32_t w[NE / 2];
+#pragma unroll
+                        for (int e = 0; e < NE; e += 2) w[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+                        __nv_bfloat16* d = out0 + ((size_t)token * a.Hq + head) * D + d0;
+                        if (NE == 8) *reinterpret_cast<uint4*>(d) = make_uint4(w[0], w[1], w[NE / 2 - 2], w[NE / 2 - 1]);
+                        else *reinterpret_cast<uint2*>(d) = make_uint2(w[0], w[1]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < NE; ++e) a.part_o[(part * D + d0 + e) * kChunkPartRows + row] = acc[e];
+                    }
+                    if (d0 == 0) row_stats(token, head, row, mx, lt);
+                }
+            } else {
+                if (p.alt) {
+                    if (g == 1) {
+                        if (!warp_wait(&sh.q_done, k, abort_flag, limit)) return false;
+                        if (busy) {
+                            sh.merge_ml[r] = make_float2(m, l);
+                            if (jobs > 0) {
+#pragma unroll 1
+                                for (int c = 0; c < D; c += 32) {
+                                    uint32_t o[32];
+                                    tmem_ld32(o_addr + c, o);
+                                    tmem_ld_wait();
+#pragma unroll
+                                    for (int y = 0; y < 32; ++y) merge_o[(c + y) * kTile + r] = __uint_as_float(o[y]);
+                                }
+                            }
+                        }
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(&sh.merge);
+                    } else if (!warp_wait(&sh.merge, n_m, abort_flag, limit)) return false;
+                    ++n_m;
+                }
+                if (busy && !(p.alt && g == 1)) {
+                    float w0 = 1.f, w1 = 0.f;
+                    if (p.alt) {
+                        const float2 other = sh.merge_ml[r];
+                        const float mx = fmaxf(m, other.x);
+                        w0 = exp2_diff(m, mx);
+                        w1 = exp2_diff(other.x, mx);
+                        l = l * w0 + other.y * w1;
+                        m = mx;
+                    }
+                    const float mul = !whole ? 1.f : (l == 0.f ? 0.f : a.v_scale[p.it.l] / l);
+                    const float mine = l == 0.f ? 0.f : w0 * mul, others = l == 0.f ? 0.f : w1 * mul;
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_addr + c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) {
+                            float x = mine == 0.f ? 0.f : __uint_as_float(o[y]) * mine;  // what nothing was added to may hold anything
+                            if (others != 0.f) x = fmaf(merge_o[(c + y) * kTile + r], others, x);
+                            o[y] = __float_as_uint(x);
+                        }
+                        if (!whole) {
+                            if (valid_row)
+#pragma unroll
+                                for (int y = 0; y < 32; ++y) a.part_o[(part * D + c + y) * kChunkPartRows + r] = __uint_as_float(o[y]);
+                            continue;
+                        }
+                        // rows are turned through shared memory: four lanes then write 64 bytes of a row together
+                        __syncwarp();
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const uint32_t* f = o + 8 * y;
+                            *reinterpret_cast<uint4*>(&sh.turn[warp][lane][16 * y]) =
+                                make_uint4(pack_bf16(__uint_as_float(f[0]), __uint_as_float(f[1])), pack_bf16(__uint_as_float(f[2]), __uint_as_float(f[3])),
+                                           pack_bf16(__uint_as_float(f[4]), __uint_as_float(f[5])), pack_bf16(__uint_as_float(f[6]), __uint_as_float(f[7])));
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const int rr = y * 8 + (lane >> 2), row = quarter * 32 + rr;
+                            if (row < tile_rows) {
+                                const int tk = p.tok0 + (p.alt ? 0 : g * a.TT) + row / a.G;
+                                *reinterpret_cast<uint4*>(out0 + ((size_t)tk * a.Hq + row % a.G) * D + c + (lane & 3) * 8) = *reinterpret_cast<const uint4*>(&sh.turn[warp][rr][16 * (lane & 3)]);
                             }
                         }
                     }
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(&sh.merge);
-                } else if (!warp_wait(&sh.merge, n_m, abort_flag, limit)) return false;
-            }
-            n_m += p.alt;
-            if (busy && !(p.alt && g == 1)) {
-                float w0 = 1.f, w1 = 0.f;
-                if (p.alt) {
-                    const float2 other = sh.merge_ml[r];
-                    const float mx = fmaxf(m, other.x);
-                    w0 = exp2_diff(m, mx);
-                    w1 = exp2_diff(other.x, mx);
-                    l = l * w0 + other.y * w1;
-                    m = mx;
-                }
-                const bool whole = p.head && p.tail;
-                const bool add = p.alt && jobs > 1;
-                const size_t orow = ((size_t)p.it.li * a.n_tokens + p.it.first + tok) * a.Hq + p.it.hkv * a.G + h;
-                const size_t part = ((size_t)blockIdx.x * 2 + (p.head ? 1 : 0)) * 2 + (p.alt ? 0 : g);
-                const float mul = !whole ? 1.f : (l == 0.f ? 0.f : a.v_scale[p.it.l] / l);
-                const float mine = l == 0.f ? 0.f : w0 * mul, others = add && l != 0.f ? w1 * mul : 0.f;
-                __nv_bfloat16* const out0 = (__nv_bfloat16*)a.out + (((size_t)p.it.li * a.n_tokens + p.it.first) * a.Hq + p.it.hkv * a.G) * D;
-#pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(o_addr + c, o);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int y = 0; y < 32; ++y) {
-                        float x = mine == 0.f ? 0.f : __uint_as_float(o[y]) * mine;  // what nothing was added to may hold anything
-                        if (others != 0.f) x = fmaf(merge_o[(c + y) * kTile + r], others, x);
-                        o[y] = __float_as_uint(x);
-                    }
-                    if (!whole) {
-                        if (valid_row)
-#pragma unroll
-                            for (int y = 0; y < 32; ++y) a.part_o[(part * D + c + y) * kChunkPartRows + r] = __uint_as_float(o[y]);
-                        continue;
-                    }
-                    // rows are turned through shared memory: four lanes then write 64 bytes of a row together
-                    __syncwarp();
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const float* f = reinterpret_cast<const float*>(o) + 8 * y;
-                        *reinterpret_cast<uint4*>(&sh.turn[warp][lane][16 * y]) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-                    }
-                    __syncwarp();
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int rr = y * 8 + (lane >> 2), row = quarter * 32 + rr;
-                        if (row < tile_rows) {
-                            const int tk = p.tok0 + (p.alt ? 0 : g * a.TT) + row / a.G;
-                            *reinterpret_cast<uint4*>(out0 + ((size_t)tk * a.Hq + row % a.G) * D + c + (lane & 3) * 8) = *reinterpret_cast<const uint4*>(&sh.turn[warp][rr][16 * (lane & 3)]);
-                        }
-                    }
-                }
-                if (valid_row) {
-                    if (!whole) a.part_ml[part * kChunkPartRows + r] = make_float2(m, l);
-                    else {
-                        const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-                        if (a.lse) a.lse[orow] = lse2 * 0.6931471805599453f;
-                        a.nlse2[(((size_t)p.it.li * a.Hkv + p.it.hkv) * a.n_tokens + p.it.first + tok) * a.G + h] = l == 0.f ? -INFINITY : -lse2;
-                    }
+                    if (valid_row) row_stats(tok, h, r, m, l);
                 }
             }
             tc_before();   // O has been read: the next unit's first product may overwrite it (ordered by p_full)
@@ -544,9 +662,9 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
     tc_after();
     if (sh.abort) {  // uniform for the CTA: see everything this CTA has started end
         if (tid == 0) record_error(a.status, LETHE_ERR_TIMEOUT, blockIdx.x);
-        if (warp == kMmaWarp && sh.issued && elect_one()) {  // the lane that issued them: a commit follows one's own MMAs
-            tc_commit(&sh.drained);
-            bar_drain(&sh.drained, 0);
+        if ((warp == kMmaWarp || warp == kMmaWarp + 1) && sh.issued[warp - kMmaWarp] && elect_one()) {  // the lane that issued them: a commit follows one's own MMAs
+            tc_commit(&sh.drained[warp - kMmaWarp]);
+            bar_drain(&sh.drained[warp - kMmaWarp], 0);
         }
         if (TMA && warp == kLoadWarp && lane == 0)
             for (int e = max(0, sh.loaded - NS); e < sh.loaded; ++e) bar_drain(&sh.full[e % NS], e / NS);
@@ -585,6 +703,10 @@ bool build_chunk_maps(void* encode, const ChunkArgs& a, int n_layers, ChunkMaps*
     const cuuint64_t qs[3] = {D * 2, a.Hq * D * 2, (cuuint64_t)a.n_tokens * a.Hq * D * 2};
     const cuuint32_t qb[4] = {64, (cuuint32_t)a.G, (cuuint32_t)a.TT, 1};
     if (fn(&maps->q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(a.q), qd, qs, qb, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return false;
+    const cuuint32_t qb16[4] = {64, (cuuint32_t)a.G, (cuuint32_t)(kQuadRows / a.G), 1};
+    if (fn(&maps->q16, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(a.q), qd, qs, qb16, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return false;
     if (!tma_can_tile(a)) return true;
