@@ -4,10 +4,11 @@
 // threads read a row each, write the probabilities back as bf16 over the logits they came from, and those are the A operand of the
 // second product where they lie.  A CTA holds two row tiles (two softmax groups of four warps) and each has a warp of its own that
 // issues its products, so one group's exponentials run under the other's products and neither waits for the other's hand-offs.
-// A softmax job is half a tile, 64 keys: the first half's probabilities are multiplied while the second half's are formed.  Row
-// maxima are followed lazily: the outputs are rescaled only when a maximum has grown by more than 2^8 since the last time, which
-// a row's first few tiles settle; the sums stay far inside fp32.  (Logits of 64 keys in two buffers, the next job's ahead of
-// this one's, were slower: a product with 64 columns takes as long as one with 128, it is bound by reading Q.)
+// A job is 64 keys of one group, half a tile, and a group's logits have two buffers: the logits of job n + 1 are there before job
+// n's probabilities are done, so a group's softmax does not wait for its products.  (A product with 64 columns takes as long as one
+// with 128, it is bound by reading Q; with one 128-column buffer the softmax stood still for the products and the two hand-offs,
+// 1700 of a tile's 4900 clocks.)  Row maxima are followed lazily: the outputs are rescaled only when a maximum has grown by more
+// than 2^8 since the last time, which a row's first few tiles settle; the sums stay far inside fp32.
 //
 // What the two groups work on depends on the unit:
 //   pair  two row tiles: a group each, the same keys
@@ -46,7 +47,7 @@ template <bool MOD>
 struct Shared {
     unsigned long long full[kMaxStages], empty[kMaxStages];
     unsigned long long q_full, q_done, q_soft, merge, merge_all;
-    unsigned long long s_full[2], p_full[2][2], o_full[2][2];  // [group], [group][half]
+    unsigned long long s_full[2][2], p_full[2][2], o_full[2][2];  // [group][buffer]: logits, probabilities, output product
     unsigned long long drained[2];
     uint32_t tmem_base;
     int abort;
@@ -142,7 +143,7 @@ __device__ __forceinline__ void for_pieces(const ChunkArgs& a, F f) {
 template <int D, bool TMA, bool MOD>
 __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps) {
     constexpr int TILE = tile_bytes<D>(), NS = stages<D>(), KS = D / 16;
-    constexpr int kOCol = 256;  // tensor memory: S0 | S1 | O0 | O1, 128 columns each (P over its S, each half over its own)
+    constexpr int kOCol = 256;  // tensor memory: S0 | S1 | O0 | O1, 128 columns each (two buffers of logits each, P over its logits)
     extern __shared__ unsigned char dyn_raw[];
     __shared__ Shared<MOD> sh;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -164,8 +165,8 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
         bar_init(&sh.merge, 4);
         bar_init(&sh.merge_all, kSoftWarps);
         for (int g = 0; g < 2; ++g) {
-            bar_init(&sh.s_full[g], 1);
             for (int hf = 0; hf < 2; ++hf) {
+                bar_init(&sh.s_full[g][hf], 1);
                 bar_init(&sh.p_full[g][hf], 4);
                 bar_init(&sh.o_full[g][hf], 1);
             }
@@ -251,65 +252,60 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
         const uint32_t pv_desc = mma_idesc(D, true, false);
         const uint64_t q_desc = smem_desc(q_tile, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, kHalfBytes);
         const uint32_t st = tmem + g * 128, ot = tmem + kOCol + g * 128;
-        int k = 0, base = 0;   // pieces done, first ring entry of the piece
-        unsigned np = 0;       // tiles whose probabilities have been consumed (first halves; second halves may be fewer)
-        unsigned np1 = 0;
+        int k = 0, base = 0;           // pieces done, first ring entry of the piece
+        unsigned np0 = 0, np1 = 0;     // probabilities consumed so far, per buffer
         for_pieces(a, [&](const Piece& p) {
-            const uint32_t qk_desc = mma_idesc(kTile, false, a.scale[p.it.l] < 0.f);
+            const uint32_t qk_desc = mma_idesc(64, false, a.scale[p.it.l] < 0.f);
             const uint64_t qd = q_desc + (uint64_t)((p.alt ? 0 : g) * (TILE >> 4));
-            const int step = p.alt ? 2 : 1, t0 = p.alt ? g : 0;
+            const int jobs = piece_jobs(p, g);
             if (!warp_wait(&sh.q_full, k, abort_flag, limit)) return false;
             // a tile's ring entry is let go by both groups, or twice by the one that uses it
             auto let_go = [&](int slot) {
                 tc_commit(&sh.empty[slot]);
                 if (p.alt) tc_commit(&sh.empty[slot]);
             };
-            auto qk = [&](int t) -> bool {
-                const int e = base + k_entry(p, t), slot = e % NS;
+            auto qk = [&](int n) -> bool {
+                const int buf = n & 1, e = base + k_entry(p, p.alt ? 2 * (n >> 1) + g : n >> 1), slot = e % NS;
                 if (!warp_wait(&sh.full[slot], e / NS, abort_flag, limit)) return false;
                 tc_after();
                 if (elect_one()) {
-                    const uint64_t kd = k_desc + (uint64_t)(slot * (TILE >> 4));
+                    const uint64_t kd = k_desc + (uint64_t)(slot * (TILE >> 4) + buf * (64 * 128 >> 4));
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) {
                         constexpr int half16 = kHalfBytes >> 4;
-                        mma_ss(st, qd + (ks >> 2) * half16 + (ks & 3) * 2, kd + (ks >> 2) * half16 + (ks & 3) * 2, qk_desc, ks > 0);
+                        mma_ss(st + buf * 64, qd + (ks >> 2) * half16 + (ks & 3) * 2, kd + (ks >> 2) * half16 + (ks & 3) * 2, qk_desc, ks > 0);
                     }
                     sh.issued[g] = 1;
-                    tc_commit(&sh.s_full[g]);
-                    let_go(slot);
-                    if (t + step >= p.nt) tc_commit(&sh.q_done);
+                    tc_commit(&sh.s_full[g][buf]);
+                    if (buf == 1 || n + 1 == jobs) let_go(slot);
+                    if (n + 1 == jobs) tc_commit(&sh.q_done);
                 }
                 __syncwarp();
                 return true;
             };
-            if (t0 < p.nt) {
-                if (!qk(t0)) return false;
-            } else if (elect_one()) tc_commit(&sh.q_done);  // no tile for this group
+            if (jobs > 0 && !qk(0)) return false;
+            if (jobs > 1 && !qk(1)) return false;
+            if (jobs == 0 && elect_one()) tc_commit(&sh.q_done);
             __syncwarp();
-            for (int t = t0; t < p.nt; t += step) {
-                const int e = base + v_entry(p, t), slot = e % NS;
-                const int seen = p.hi - (p.tile0 + t) * kTile;
-                const bool two_halves = seen > 64 || t + 1 < p.nt;
-                const uint64_t vd = v_desc + (uint64_t)(slot * (TILE >> 4));
-                if (lone_v(p, t) && !wait_issued(&sh.loaded, e, abort_flag, limit)) return false;
-                if (!warp_wait(&sh.full[slot], e / NS, abort_flag, limit)) return false;
-#pragma unroll
-                for (int hf = 0; hf < 2; ++hf) {
-                    if (hf == 1 && !two_halves) break;
-                    if (!warp_wait(&sh.p_full[g][hf], hf ? np1++ : np++, abort_flag, limit)) return false;
-                    tc_after();
-                    const int steps = max(1, (min(64, seen - 64 * hf) + 15) / 16);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int ks = 0; ks < 4; ++ks)
-                            if (ks < steps) mma_ts(ot, st + 64 * hf + ks * 8, vd + (uint64_t)((hf * 4 + ks) * (2048 >> 4)), pv_desc, t > t0 || hf > 0 || ks > 0);
-                        tc_commit(&sh.o_full[g][hf]);
-                        if (hf == 1 || !two_halves) let_go(slot);
-                    }
-                    __syncwarp();
+            for (int n = 0; n < jobs; ++n) {
+                const int buf = n & 1, t = p.alt ? 2 * (n >> 1) + g : n >> 1, e = base + v_entry(p, t), slot = e % NS;
+                if (buf == 0) {
+                    if (lone_v(p, t) && !wait_issued(&sh.loaded, e, abort_flag, limit)) return false;
+                    if (!warp_wait(&sh.full[slot], e / NS, abort_flag, limit)) return false;
                 }
-                if (t + step < p.nt && !qk(t + step)) return false;
+                const int steps = max(1, (min(64, p.hi - (p.tile0 + t) * kTile - 64 * buf) + 15) / 16);
+                const uint64_t vd = v_desc + (uint64_t)(slot * (TILE >> 4) + buf * (64 * 128 >> 4));
+                if (!warp_wait(&sh.p_full[g][buf], buf ? np1++ : np0++, abort_flag, limit)) return false;
+                tc_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        if (ks < steps) mma_ts(ot, st + 64 * buf + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), pv_desc, n > 0 || ks > 0);
+                    tc_commit(&sh.o_full[g][buf]);
+                    if (buf == 1 || n + 1 == jobs) let_go(slot);
+                }
+                __syncwarp();
+                if (n + 2 < jobs && !qk(n + 2)) return false;
             }
             base += 2 * p.nt;
             ++k;
@@ -323,7 +319,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
         const bool by_pos = MOD && (a.slopes || a.window > 0 || a.doc_start || a.prefix_len);
         const bool mask_pos = MOD && (a.window > 0 || a.doc_start || a.prefix_len);
         float* const merge_o = reinterpret_cast<float*>(q_generic);  // parts to merge, where the query tiles were
-        unsigned n_s = 0, o0 = 0, o1 = 0;         // logit tiles taken, and products asked for so far, per half
+        unsigned s0 = 0, s1 = 0, o0 = 0, o1 = 0;  // logits taken and products asked for so far, per buffer
         int n_v = 0, k = 0, n_m = 0, n_q = 0;     // ring entries so far; pieces, merged pieces, quad pieces
         for_pieces(a, [&](const Piece& p) {
             const int r = p.quad ? lane : quarter * 32 + lane;  // row of the tile
@@ -373,15 +369,13 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     kp_min = __reduce_min_sync(0xffffffffu, kp_min);
                     __syncwarp();
                 }
-                if (buf == 0) {
-                    if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
-                    tc_after();
-                }
+                if (!warp_wait(&sh.s_full[g][buf], buf ? s1++ : s0++, abort_flag, limit)) return false;
+                tc_after();
                 const int seen = p.hi - j0 - 64 * buf;  // keys of this half that the unit sees at all
                 if (seen < 64 && (seen <= 0 || (seen & 15))) {
                     // Rows behind the last slot may hold anything, and 0 x NaN is NaN: clear those the product's last step takes in.
-                    // Not before the logits are there: they show that the tile before, and with it the ring slot's last entry, is
-                    // done (a wait that is a whole turn of the ring early would take the last entry's phase for this one's).
+                    // Not before the logits are there: they show that the product two jobs back, and with it the ring slot's last
+                    // entry, is done (a wait that is a whole turn of the ring early would take the last entry's phase for this one's).
                     const int e = n_v + v_entry(p, t), r0 = 64 * buf + max(seen, 0), rows = 64 * buf + max(16, (seen + 15) & ~15) - r0;
                     if (lone_v(p, t) && !wait_issued(&sh.loaded, e, abort_flag, limit)) return false;
                     if (!warp_wait(&sh.full[e % NS], e / NS, abort_flag, limit)) return false;
