@@ -1151,7 +1151,7 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     a.QT = (max_chunk + a.TU - 1) / a.TU;
     a.cap_tiles = (a.cap_tokens + kChunkTile - 1) / kChunkTile;
     const long long units = (long long)a.n_items * a.QT;
-    if (units > 0x7fffffffLL / 4 || units * a.cap_tiles > 0x7fffffffLL || (long long)a.n_items * a.cap_tiles * 2 > 0x7fffffffLL)
+    if (units > 0x7fffffffLL / 4 || units * a.cap_tiles > 0x7fffffffLL || units * a.cap_tiles * 2 > 0x7fffffffLL || (long long)a.n_items * a.cap_tiles * 2 > 0x7fffffffLL)
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "chunk: too many (layer, sequence, head, block) units for one call; cover fewer layers");
     a.n_units = (int)units;
 
@@ -1163,7 +1163,11 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     const size_t o_plan = take(sizeof(ChunkPlan)), o_old = take((size_t)a.n_items * 4), o_start = take(((size_t)a.n_units + 1) * 4);
     const size_t o_lo = by_pos ? take((size_t)a.n_units * 4) : 0, o_hi = by_pos ? take((size_t)a.n_units * 4) : 0;
     const size_t o_cta = take((size_t)a.n_cta * 4);
-    const size_t o_rel = simt ? 0 : take(((size_t)a.n_items + 1) * 4), o_ri = simt ? 0 : take((size_t)a.n_items * ((a.cap_tiles + 1) / 2) * 4);
+    a.n_rel_cta = 2 * ctx->sm_count;
+    const int cap_pairs = (a.cap_tiles + 1) / 2;
+    const size_t o_rel = take(((size_t)a.n_items + 1) * 4), o_ri = take((size_t)a.n_rel_cta * 4), o_cut = take((size_t)a.n_rel_cta * sizeof(int4));
+    const size_t o_rp = take((size_t)a.n_rel_cta * 2 * 2 * kChunkTile * 4);
+    const size_t o_hull = by_pos ? take((size_t)a.n_items * cap_pairs * sizeof(int2)) : 0, o_cost = by_pos ? take((size_t)a.n_items * 4) : 0;
     const size_t o_bounds = by_pos ? take((size_t)a.n_items * a.cap_tiles * sizeof(int2)) : 0;
     const size_t o_nlse = take((size_t)nl * n_tokens * a.Hq * 4);
     const size_t o_ml = take((size_t)a.n_cta * kChunkParts * kChunkPartRows * sizeof(float2));
@@ -1185,6 +1189,12 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     if (!simt) {
         a.rel_start = (int*)(base + o_rel);
         a.rel_item = (int*)(base + o_ri);
+        a.rel_cut = (int4*)(base + o_cut);
+        a.rel_part = (float*)(base + o_rp);
+        if (by_pos) {
+            a.rel_hull = (int2*)(base + o_hull);
+            a.rel_cost = (int*)(base + o_cost);
+        }
     }
     a.nlse2 = (float*)(base + o_nlse);
     a.part_ml = (float2*)(base + o_ml);
@@ -1205,7 +1215,8 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     } else {
         if (e == cudaSuccess) e = launch_chunk_tc(a, maps, (cudaStream_t)stream);
         if (e == cudaSuccess) e = launch_chunk_combine(a, (cudaStream_t)stream);
-        if (e == cudaSuccess) e = launch_chunk_rel_tc(a, maps, 2 * ctx->sm_count, (cudaStream_t)stream);
+        if (e == cudaSuccess) e = launch_chunk_rel_tc(a, maps, (cudaStream_t)stream);
+        if (e == cudaSuccess) e = launch_chunk_rel_finish(a, (cudaStream_t)stream);
     }
     if (e != cudaSuccess) return cuda_fail(ctx, e, "chunk_attend launch");
     return LETHE_OK;

@@ -26,6 +26,8 @@ struct ChunkPlan {  // head of the call's scratch
     int per;        // tiles per CTA
     int refused;    // chunk_start is malformed: nothing is done
     int done;       // blocks of the range kernel that have finished
+    int rel_total;  // steps of the relevance kernel
+    int rel_per;    // steps per CTA
 };
 
 struct ChunkArgs {
@@ -50,8 +52,14 @@ struct ChunkArgs {
     int* u_lo;       // [n_units] first key tile of the unit (masks by position only, else NULL)
     int* u_hi;       // [n_units] slots the unit can see end here (masks by position only, else NULL)
     int* cta_unit;   // [n_cta] the unit that holds the first tile of each CTA's stretch
-    int* rel_start;  // [n_items + 1] first pair of key tiles of each item on the relevance kernel's line (tensor-core kernels, else NULL)
-    int* rel_item;   // [n_items * ceil(cap_tiles / 2)] the item of each pair on that line
+    // the relevance kernel's line (tensor-core kernels, else NULL): (pair of key tiles, query tile) steps, item by item
+    int* rel_start;  // [n_items + 1] first step of each item
+    int* rel_item;   // [n_rel_cta] the item that holds the first step of each CTA's stretch
+    int2* rel_hull;  // [n_items][ceil(cap_tiles / 2)] query tiles that meet a pair: first and end (masks by position only, else NULL)
+    int* rel_cost;   // [n_items] steps of an item (masks by position only)
+    int4* rel_cut;   // [n_rel_cta] where a CTA's stretch begins: item, pair, first step of the pair, end of it
+    float* rel_part; // [n_rel_cta][2][256] sums of a pair begun earlier, and of one begun here and continued later
+    int n_rel_cta;
     int2* bounds;    // [items][cap_tiles] smallest and largest pos of a key tile (masks by position only, else NULL)
     float* nlse2;    // [nl][Hkv][n_tokens][G] minus the log-sum-exp, in log2 units; -inf for a row that sees nothing
     float* part_o;   // [n_cta][kChunkParts][D][kChunkPartRows]: a thread that owns a row writes beside its neighbours
@@ -143,8 +151,17 @@ __device__ __forceinline__ float capped_large(float t) {
 }
 __device__ __forceinline__ float capped(float t) { return fabsf(t) <= 0.55f ? capped_small(t) : capped_large(t); }
 
+// Query tiles that a pair of key tiles (its first slot j0) meets: [lo, hi).
+__device__ __forceinline__ int2 rel_hull(const ChunkArgs& a, const ChunkItem& it, int idx, int pair) {
+    if (a.rel_hull) return a.rel_hull[(size_t)idx * ((a.cap_tiles + 1) / 2) + pair];
+    const int lo = a.append ? max(0, pair * 2 * kChunkTile - it.n_old) / a.TT : 0;  // earlier tokens do not reach the pair
+    return make_int2(lo, (it.T + a.TT - 1) / a.TT);
+}
+__device__ __forceinline__ int rel_pairs(const ChunkItem& it) { return (it.n + 2 * kChunkTile - 1) / (2 * kChunkTile); }
+
 cudaError_t launch_chunk_append(const ChunkArgs& a, cudaStream_t stream);
 cudaError_t launch_chunk_combine(const ChunkArgs& a, cudaStream_t stream);
+cudaError_t launch_chunk_rel_finish(const ChunkArgs& a, cudaStream_t stream);
 cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t stream);
 
 // Launch with the programmatic dependency attribute: the kernel may start while the one before it is still finishing and waits

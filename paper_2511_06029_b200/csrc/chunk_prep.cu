@@ -60,15 +60,24 @@ __device__ void make_plan(const ChunkArgs& a) {
         a.plan->per = per;
     }
     if (!a.rel_start) return;
-    // the relevance kernel's line: pairs of key tiles of every item that changes
+    // the relevance kernel's line, item by item
     const int iseg = (a.n_items + kPrepThreads - 1) / kPrepThreads;
     const int i0 = min(a.n_items, tid * iseg), i1 = min(a.n_items, i0 + iseg);
-    auto pairs = [&](int idx) {
+    auto steps = [&](int idx) -> int {
         const ChunkItem it = chunk_item(a, idx);
-        return it.n_old < 0 || it.T == 0 ? 0 : (it.n + 2 * kChunkTile - 1) / (2 * kChunkTile);
+        if (it.n_old < 0 || it.T == 0) return 0;
+        if (a.rel_cost) return a.rel_cost[idx];
+        const int pairs = rel_pairs(it), tiles = (it.T + a.TT - 1) / a.TT;
+        int pr = a.append ? min(pairs, it.n_old / (2 * kChunkTile) + 1) : pairs;  // these meet every query tile
+        int sum = pr * tiles;
+        for (; pr < pairs; ++pr) {
+            const int2 h = rel_hull(a, it, idx, pr);
+            sum += h.y - h.x;
+        }
+        return sum;
     };
     mine = 0;
-    for (int idx = i0; idx < i1; ++idx) mine += pairs(idx);
+    for (int idx = i0; idx < i1; ++idx) mine += steps(idx);
     __syncthreads();
     sums[tid] = mine;
     __syncthreads();
@@ -78,12 +87,19 @@ __device__ void make_plan(const ChunkArgs& a) {
         sums[tid] += add;
         __syncthreads();
     }
+    const int rel_total = sums[kPrepThreads - 1], rel_per = max(1, (rel_total + a.n_rel_cta - 1) / a.n_rel_cta);
     at = sums[tid] - mine;
     for (int idx = i0; idx < i1; ++idx) {
         a.rel_start[idx] = at;
-        for (const int next = at + pairs(idx); at < next; ++at) a.rel_item[at] = idx;
+        const int next = at + steps(idx);
+        for (int c = (at + rel_per - 1) / rel_per; c * rel_per < next; ++c) a.rel_item[c] = idx;
+        at = next;
     }
-    if (tid == 0) a.rel_start[a.n_items] = sums[kPrepThreads - 1];
+    if (tid == 0) {
+        a.rel_start[a.n_items] = rel_total;
+        a.plan->rel_total = rel_total;
+        a.plan->rel_per = rel_per;
+    }
 }
 
 // Two fp32 values -> two bytes of an 8-bit float, saturating (the low byte is the first).
@@ -277,6 +293,34 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_range_kernel(const __grid_
             }
         }
     }
+    __syncthreads();  // the item's u_lo and u_hi are there
+    if (it.n_old >= 0 && it.T > 0 && a.rel_hull) {
+        // query tiles that each pair of key tiles meets, from the ranges of their units
+        __shared__ int cost;
+        if (tid == 0) cost = 0;
+        __syncthreads();
+        const int pairs = rel_pairs(it), tiles = (it.T + a.TT - 1) / a.TT;
+        int mine = 0;
+        for (int pr = warp; pr < pairs; pr += kPrepWarps) {
+            const int j0 = pr * 2 * kChunkTile;
+            int first = INT32_MAX, end = 0;
+            for (int qt = lane; qt < tiles; qt += 32) {
+                const int u = blockIdx.x * a.QT + qt * a.TT / a.TU;
+                if (a.u_hi[u] > j0 && a.u_lo[u] * kChunkTile < j0 + 2 * kChunkTile) {
+                    first = min(first, qt);
+                    end = max(end, qt + 1);
+                }
+            }
+            first = __reduce_min_sync(0xffffffffu, first);
+            end = __reduce_max_sync(0xffffffffu, end);
+            if (end == 0) first = 0, end = 1;  // nobody sees the pair, but its relevance decays
+            if (lane == 0) a.rel_hull[(size_t)blockIdx.x * ((a.cap_tiles + 1) / 2) + pr] = make_int2(first, end);
+            mine += end - first;
+        }
+        if (lane == 0) atomicAdd(&cost, mine);  // whole numbers: any order
+        __syncthreads();
+        if (tid == 0) a.rel_cost[blockIdx.x] = cost;
+    }
     __threadfence();
     __syncthreads();
     if (tid == 0) last = atomicAdd(&a.plan->done, 1) == (int)gridDim.x - 1;
@@ -353,7 +397,31 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
     }
 }
 
+// Pairs of key tiles that more than one CTA of the relevance kernel worked on: the parts are added in the order of their tokens.
+// One block per CTA whose stretch begins inside a pair, the pair's first such CTA speaks for it.
+__global__ void __launch_bounds__(kPrepThreads) chunk_rel_finish_kernel(const __grid_constant__ ChunkArgs a) {
+    dependency_wait();
+    dependency_release();
+    const int c = 1 + blockIdx.x, per = a.plan->rel_per;
+    if ((long long)c * per >= a.plan->rel_total) return;
+    const int4 cut = a.rel_cut[c];  // item, pair, first step, end
+    const int c0 = cut.z / per, c1 = (cut.w - 1) / per;
+    if (c0 != c - 1 || cut.z == c * per) return;
+    const ChunkItem it = chunk_item(a, cut.x);
+    const int j = cut.y * 2 * kChunkTile + threadIdx.x;
+    if (j >= it.n) return;
+    float sum = 0.f;
+    for (int k = c0; k <= c1; ++k) sum += a.rel_part[((size_t)k * 2 + (k == c0 ? 1 : 0)) * (2 * kChunkTile) + threadIdx.x];
+    float* rel = a.rel + (size_t)it.item * a.cap_tokens + j;
+    *rel = fmaf(exp2f((float)it.T * a.gamma_log2), j < it.n_old ? *rel : 0.f, sum);
+}
+
 }  // namespace
+
+cudaError_t launch_chunk_rel_finish(const ChunkArgs& a, cudaStream_t stream) {
+    static_assert(kPrepThreads == 2 * kChunkTile, "one thread per key of a pair");
+    return launch_dependent(chunk_rel_finish_kernel, dim3(a.n_rel_cta - 1), kPrepThreads, 0, stream, a);
+}
 
 cudaError_t launch_chunk_append(const ChunkArgs& a, cudaStream_t stream) {
     // at most two waves of blocks

@@ -7,8 +7,9 @@
 // the bound (16 a clock per SM, 1024 clocks a tile against 512 of products).  The alternative, writing column sums from the
 // attention kernel, would need the final maxima and sums before the last key is known.
 //
-// A unit is a pair of key tiles of one item (two groups of four warps); CTAs walk the plan's line of units round robin, two
-// CTAs to an SM covering each other's hand-offs.  Warp 8 issues the MMAs, warp 9 loads tiles by TMA; tiles that TMA cannot take
+// A unit is a pair of key tiles of one item (two groups of four warps), its steps are the query tiles that meet it; the plan gives
+// every CTA an equal stretch of the line of all steps (a causal prompt's first keys meet every token, its last keys few), and the
+// parts of a unit that CTAs share are added up afterwards in order.  Two CTAs to an SM cover each other's hand-offs.  Warp 8 issues the MMAs, warp 9 loads tiles by TMA; tiles that TMA cannot take
 // (byte caches, odd pages) are gathered by the softmax warps, once per unit.
 #include "chunk_tc.cuh"
 
@@ -43,20 +44,52 @@ struct Shared {
     alignas(16) ColumnMod mod[MOD ? kSoftWarps : 1][MOD ? kTile : 1];
 };
 
-// The query tiles that a pair of key tiles (from slot j0) meets: f(qt) for each; f returns false to stop.
+// A CTA's piece of a unit: query tiles [qa, qb) of the pair of key tiles that begins at slot j0.
+struct RelPiece {
+    ChunkItem it;
+    int idx, pair, j0, qa, qb;
+    int s0, s1;      // the unit's steps on the line
+    bool head, tail; // begins / ends here
+};
+
+// Calls f(piece) for each piece of this CTA, in order; f returns false to stop.
 template <typename F>
-__device__ __forceinline__ bool for_query_tiles(const ChunkArgs& a, const ChunkItem& it, int idx, int j0, F f) {
-    const int n_qt = (it.T + a.TT - 1) / a.TT;
-    int qt = 0;
-    if (!a.u_hi && a.append) qt = max(0, j0 - it.n_old) / a.TT;  // earlier tokens do not reach slot j0
-    for (; qt < n_qt; ++qt) {
-        if (a.u_hi) {  // masks by position: what the unit of this tile can see
-            const int u = idx * a.QT + qt * a.TT / a.TU;
-            if (a.u_hi[u] <= j0 || a.u_lo[u] * kTile >= j0 + 2 * kTile) continue;
-        }
-        if (!f(qt)) return false;
+__device__ __forceinline__ void for_rel_pieces(const ChunkArgs& a, F f) {
+    const int total = a.plan->rel_total, per = a.plan->rel_per;
+    const int begin = min(total, (int)blockIdx.x * per), end = min(total, begin + per);
+    if (begin >= end) return;
+    RelPiece p;
+    p.idx = a.rel_item[blockIdx.x];
+    p.it = chunk_item(a, p.idx);
+    p.s0 = a.rel_start[p.idx];
+    p.pair = 0;
+    if (!a.rel_hull) {  // the pairs at the front all meet every query tile
+        const int tiles = (p.it.T + a.TT - 1) / a.TT;
+        const int same = a.append ? min(rel_pairs(p.it), p.it.n_old / (2 * kTile) + 1) : rel_pairs(p.it);
+        p.pair = min((begin - p.s0) / tiles, same);
+        p.s0 += p.pair * tiles;
     }
-    return true;
+    for (int at = begin; at < end;) {
+        if (p.it.n_old < 0 || p.it.T == 0 || p.pair >= rel_pairs(p.it)) {
+            p.it = chunk_item(a, ++p.idx);
+            p.pair = 0;
+            continue;
+        }
+        const int2 h = rel_hull(a, p.it, p.idx, p.pair);
+        p.s1 = p.s0 + h.y - h.x;
+        if (p.s1 > at) {
+            const int stop = min(end, p.s1);
+            p.j0 = p.pair * 2 * kTile;
+            p.qa = h.x + at - p.s0;
+            p.qb = h.x + stop - p.s0;
+            p.head = at == p.s0;
+            p.tail = stop == p.s1;
+            if (!f(p)) return;
+            at = stop;
+        }
+        p.s0 = p.s1;
+        ++p.pair;
+    }
 }
 
 template <int D, bool TMA, bool MOD>
@@ -97,46 +130,41 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
     __syncthreads();
     tc_after();
     const uint32_t tmem = sh.tmem_base;
-    const int total = a.rel_start[a.n_items];
 
     if (warp == kLoadWarp) {
         if (lane == 0) {
             bool bad = false;  // the attention has recorded bad pages
             int k = 0, qn = 0;
-            for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
-                const int idx = a.rel_item[w], j0 = (w - a.rel_start[idx]) * 2 * kTile;
-                const ChunkItem it = chunk_item(a, idx);
+            for_rel_pieces(a, [&](const RelPiece& p) {
                 if (TMA) {
-                    if (k > 0 && !bar_wait(&sh.k_empty, k - 1, abort_flag, limit)) break;
-                    const int tiles = j0 + kTile < it.n ? 2 : 1;
+                    if (k > 0 && !bar_wait(&sh.k_empty, k - 1, abort_flag, limit)) return false;
+                    const int tiles = p.j0 + kTile < p.it.n ? 2 : 1;
                     bar_expect_tx(&sh.k_full, tiles * TILE);
                     sh.k_loads = k + 1;
-                    for (int g = 0; g < tiles; ++g) tma_tile<D>(a, &maps.k, it.item, it.n, j0 + g * kTile, k_tile + g * TILE, &sh.k_full, &bad);
+                    for (int g = 0; g < tiles; ++g) tma_tile<D>(a, &maps.k, p.it.item, p.it.n, p.j0 + g * kTile, k_tile + g * TILE, &sh.k_full, &bad);
                 }
-                const bool ok = for_query_tiles(a, it, idx, j0, [&](int qt) {
+                ++k;
+                for (int qt = p.qa; qt < p.qb; ++qt) {
                     if (qn > 0 && !bar_wait(&sh.q_empty, qn - 1, abort_flag, limit)) return false;
                     bar_expect_tx(&sh.q_full, (unsigned)(used * D * 2));
                     sh.q_loads = ++qn;
 #pragma unroll
                     for (int hf = 0; hf < D / 64; ++hf)
-                        tma_4d(q_tile + hf * kHalfBytes, &maps.q, 64 * hf, it.hkv * a.G, it.first + qt * a.TT, it.li, &sh.q_full);
-                    return true;
-                });
-                if (!ok) break;
-            }
+                        tma_4d(q_tile + hf * kHalfBytes, &maps.q, 64 * hf, p.it.hkv * a.G, p.it.first + qt * a.TT, p.it.li, &sh.q_full);
+                }
+                return true;
+            });
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
         const uint64_t q_desc = smem_desc(q_tile, 16), k_desc = smem_desc(k_tile, 16);
         int k = 0, qn = 0;
         int ns[2] = {0, 0};
-        for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
-            const int idx = a.rel_item[w], j0 = (w - a.rel_start[idx]) * 2 * kTile;
-            const ChunkItem it = chunk_item(a, idx);
-            const int tiles = j0 + kTile < it.n ? 2 : 1;
-            const uint32_t desc = mma_idesc(kTile, false, a.scale[it.l] < 0.f);
-            if (!warp_wait(&sh.k_full, k, abort_flag, limit)) break;
-            const bool ok = for_query_tiles(a, it, idx, j0, [&](int) {
+        for_rel_pieces(a, [&](const RelPiece& p) {
+            const int tiles = p.j0 + kTile < p.it.n ? 2 : 1;
+            const uint32_t desc = mma_idesc(kTile, false, a.scale[p.it.l] < 0.f);
+            if (!warp_wait(&sh.k_full, k++, abort_flag, limit)) return false;
+            for (int qt = p.qa; qt < p.qb; ++qt, ++qn) {
                 if (!warp_wait(&sh.q_full, qn, abort_flag, limit)) return false;
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
@@ -152,37 +180,41 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                         sh.issued = 1;
                         tc_commit(&sh.s_full[g]);
                         if (g == tiles - 1) tc_commit(&sh.q_empty);
+                        if (g == tiles - 1 && qt + 1 == p.qb) tc_commit(&sh.k_empty);
                     }
                     __syncwarp();
                     ++ns[g];
                 }
-                ++qn;
-                return true;
-            });
-            if (!ok) break;
-            if (elect_one()) tc_commit(&sh.k_empty);
-            __syncwarp();
-        }
+            }
+            return true;
+        });
     } else {
         const int g = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + g * kTile;
         int n_s = 0, k = 0;
-        for (int w = blockIdx.x; w < total; w += gridDim.x, ++k) {
-            const int idx = a.rel_item[w], j0 = (w - a.rel_start[idx]) * 2 * kTile;
-            const ChunkItem it = chunk_item(a, idx);
-            const int j = j0 + g * kTile + r;  // this thread's key
+        if (tid == 0)  // where the stretch begins, for the merge
+            for_rel_pieces(a, [&](const RelPiece& p) {
+                a.rel_cut[blockIdx.x] = make_int4(p.idx, p.pair, p.s0, p.s1);
+                return false;
+            });
+        __syncwarp();
+        for_rel_pieces(a, [&](const RelPiece& p) {
+            const ChunkItem& it = p.it;
+            const int j0 = p.j0, j = j0 + g * kTile + r;  // this thread's key
             if (!TMA) {
                 bool bad = false;
-                if (k > 0 && !warp_wait(&sh.k_empty, k - 1, abort_flag, limit)) break;
+                if (k > 0 && !warp_wait(&sh.k_empty, k - 1, abort_flag, limit)) return false;
                 for (int t = 0; t < (j0 + kTile < it.n ? 2 : 1); ++t) gather_tile<D>(a, a.k, it.item, it.n, j0 + t * kTile, k_tile + t * TILE, tid, kSoftWarps * 32, &bad);
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) bar_arrive(&sh.k_full);
             }
-            if (j0 == 0 && tid == 0 && a.append) a.len[it.item] = it.n;
-            if (j0 + g * kTile >= it.n) continue;  // the second tile does not exist
+            ++k;
+            if (j0 == 0 && p.head && tid == 0 && a.append) a.len[it.item] = it.n;
+            if (j0 + g * kTile >= it.n) return true;  // the second tile does not exist
             float* rel = a.rel + (size_t)it.item * a.cap_tokens + j;
-            const float old = j < it.n_old ? *rel : 0.f;
+            const bool whole = p.head && p.tail;
+            const float old = whole && j < it.n_old ? *rel : 0.f;
             const float scale = fabsf(a.scale[it.l]) * a.k_scale[it.l], sl2 = scale * 1.4426950408889634f;
             float cap_in = 0.f, cap2 = 0.f, kf = 0.f;
             int kp = 0, prefix = INT32_MIN, pos0 = 0;
@@ -201,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
             }
             const float* nlse = a.nlse2 + (((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G;
             float acc0 = 0.f, acc1 = 0.f, acc2 = 0.f, acc3 = 0.f;
-            const bool ok = for_query_tiles(a, it, idx, j0, [&](int qt) {
+            for (int qt = p.qa; qt < p.qb; ++qt) {
                 // biases of the tile's columns, one copy per warp (the warps never wait for one another)
                 const int cols = min(a.TT, it.T - qt * a.TT) * a.G;
                 int lo_max = INT32_MIN;
@@ -294,11 +326,12 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                         }
                     }
                 }
-                return true;
-            });
-            if (!ok) break;
-            if (j < it.n) *rel = fmaf(exp2f((float)it.T * a.gamma_log2), old, (acc0 + acc1) + (acc2 + acc3));
-        }
+            }
+            const float sum = (acc0 + acc1) + (acc2 + acc3);
+            if (!whole) a.rel_part[((size_t)blockIdx.x * 2 + (p.head ? 1 : 0)) * (2 * kTile) + g * kTile + r] = sum;
+            else if (j < it.n) *rel = fmaf(exp2f((float)it.T * a.gamma_log2), old, sum);
+            return true;
+        });
     }
 
     tc_before();
@@ -322,23 +355,23 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
 }
 
 template <int D, bool TMA, bool MOD>
-cudaError_t launch_t(const ChunkArgs& a, const ChunkMaps& maps, int grid, cudaStream_t stream) {
+cudaError_t launch_t(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
     cudaError_t e = prepare_kernel((const void*)chunk_tc_rel<D, TMA, MOD>, smem_bytes<D>());
-    if (e == cudaSuccess) e = launch_dependent(chunk_tc_rel<D, TMA, MOD>, dim3(grid), kThreads, smem_bytes<D>(), stream, a, maps);
+    if (e == cudaSuccess) e = launch_dependent(chunk_tc_rel<D, TMA, MOD>, dim3(a.n_rel_cta), kThreads, smem_bytes<D>(), stream, a, maps);
     return e;
 }
 
 template <int D, bool TMA>
-cudaError_t launch_m(const ChunkArgs& a, const ChunkMaps& maps, int grid, cudaStream_t stream) {
+cudaError_t launch_m(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
     const bool mod = a.softcap > 0.f || a.slopes || a.window > 0 || a.doc_start || a.prefix_len;
-    return mod ? launch_t<D, TMA, true>(a, maps, grid, stream) : launch_t<D, TMA, false>(a, maps, grid, stream);
+    return mod ? launch_t<D, TMA, true>(a, maps, stream) : launch_t<D, TMA, false>(a, maps, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_chunk_rel_tc(const ChunkArgs& a, const ChunkMaps& maps, int grid, cudaStream_t stream) {
-    if (tma_can_tile(a)) return a.D == 128 ? launch_m<128, true>(a, maps, grid, stream) : launch_m<64, true>(a, maps, grid, stream);
-    return a.D == 128 ? launch_m<128, false>(a, maps, grid, stream) : launch_m<64, false>(a, maps, grid, stream);
+cudaError_t launch_chunk_rel_tc(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
+    if (tma_can_tile(a)) return a.D == 128 ? launch_m<128, true>(a, maps, stream) : launch_m<64, true>(a, maps, stream);
+    return a.D == 128 ? launch_m<128, false>(a, maps, stream) : launch_m<64, false>(a, maps, stream);
 }
 
 }  // namespace lethe

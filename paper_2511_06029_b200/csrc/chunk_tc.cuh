@@ -288,6 +288,6 @@ inline bool tma_can_tile(const ChunkArgs& a) {
 // encode: cuTensorMapEncodeTiled; false = a map could not be made.
 bool build_chunk_maps(void* encode, const ChunkArgs& a, int n_layers, ChunkMaps* maps);
 cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream);
-cudaError_t launch_chunk_rel_tc(const ChunkArgs& a, const ChunkMaps& maps, int grid, cudaStream_t stream);
+cudaError_t launch_chunk_rel_tc(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream);
 
 }  // namespace lethe
