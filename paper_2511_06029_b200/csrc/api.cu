@@ -1149,9 +1149,10 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     a.n_cta = simt ? 2 * ctx->sm_count : ctx->sm_count;
     a.min_per = simt ? 1 : 2;  // both softmax groups of a CTA have something to do
     a.QT = (max_chunk + a.TU - 1) / a.TU;
+    a.pad = simt ? 0 : 3;
     a.cap_tiles = (a.cap_tokens + kChunkTile - 1) / kChunkTile;
     const long long units = (long long)a.n_items * a.QT;
-    if (units > 0x7fffffffLL / 4 || units * a.cap_tiles > 0x7fffffffLL || units * a.cap_tiles * 2 > 0x7fffffffLL || (long long)a.n_items * a.cap_tiles * 2 > 0x7fffffffLL)
+    if (units > 0x7fffffffLL / 4 || units * (a.cap_tiles + a.pad) > 0x7fffffffLL || units * a.cap_tiles * 2 > 0x7fffffffLL || (long long)a.n_items * a.cap_tiles * 2 > 0x7fffffffLL)
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "chunk: too many (layer, sequence, head, block) units for one call; cover fewer layers");
     a.n_units = (int)units;
 

@@ -20,6 +20,7 @@ constexpr int kSoftWarps = 8;
 constexpr int kMmaWarp = 8;
 constexpr int kLoadWarp = 9;
 constexpr int kThreads = 10 * 32;
+constexpr int kFmaShare = 2;  // of eight exponentials, computed by polynomial
 constexpr int kTmemCols = 256;  // one logit tile per group
 
 template <int D>
@@ -232,11 +233,13 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                 }
             }
             const float* nlse = a.nlse2 + (((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G;
-            float acc0 = 0.f, acc1 = 0.f, acc2 = 0.f, acc3 = 0.f;
+            uint64_t acc[2] = {0, 0};
+            float acc0 = 0.f;  // of columns judged one by one
             for (int qt = p.qa; qt < p.qb; ++qt) {
                 // biases of the tile's columns, one copy per warp (the warps never wait for one another)
                 const int cols = min(a.TT, it.T - qt * a.TT) * a.G;
                 int lo_max = INT32_MIN;
+                bool nan = false;  // a token whose scores are NaN: every column is judged, so that it comes through
                 __syncwarp();
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
@@ -244,6 +247,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     float bias = -INFINITY;
                     if (c < cols) bias = nlse[qt * used + c] + (float)(it.T - 1 - tok) * a.gamma_log2;
                     sh.bias[warp][c] = bias;
+                    nan = nan || bias != bias;
                     if (MOD) {
                         ColumnMod cm = {0.f, 0.f, INT32_MIN, 0};
                         if (c < cols) {
@@ -263,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                 // first column that reaches slot j in causal order
                 const int c_lo = a.append ? (j - it.n_old - qt * a.TT) * a.G : 0;
                 // a short tile's other columns are tokens of other sequences: whatever they hold must not count
-                const bool clean = cols == used && __all_sync(0xffffffffu, c_lo <= 0 && (!mask_pos || kp >= lo_max));
+                const bool clean = cols == used && __all_sync(0xffffffffu, !nan && c_lo <= 0 && (!mask_pos || kp >= lo_max));
 #pragma unroll
                 for (int ch = 0; ch < kTile; ch += 32) {
                     if (ch >= cols) break;  // a short chunk leaves most columns empty
@@ -279,21 +283,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     if (MOD) {
                         if (a.softcap > 0.f) {
                             ml = 1.f;
-#pragma unroll
-                            for (int c = 0; c < 32; c += 8) {
-                                float x[8], big = 0.f;
-#pragma unroll
-                                for (int y = 0; y < 8; ++y) {
-                                    x[y] = __uint_as_float(v[c + y]) * cap_in;
-                                    big = fmaxf(big, fabsf(x[y]));
-                                    v[c + y] = __float_as_uint(cap2 * capped_small(x[y]));
-                                }
-                                if (__any_sync(0xffffffffu, big > 0.55f)) {
-#pragma unroll
-                                    for (int y = 0; y < 8; ++y)
-                                        if (fabsf(x[y]) > 0.55f) v[c + y] = __float_as_uint(cap2 * capped_large(x[y]));
-                                }
-                            }
+                            cap_scores<32>(v, cap_in, cap2);
                         }
                         if (a.slopes) {
 #pragma unroll
@@ -306,13 +296,17 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     }
                     const float4* b4 = reinterpret_cast<const float4*>(sh.bias[warp] + ch);
                     if (clean) {
+                        const uint64_t ml2 = two(ml, ml);
 #pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            const float4 b = b4[c / 4];
-                            acc0 += fast_exp2(fmaf(__uint_as_float(v[c]), ml, b.x));
-                            acc1 += fast_exp2(fmaf(__uint_as_float(v[c + 1]), ml, b.y));
-                            acc2 += fast_exp2(fmaf(__uint_as_float(v[c + 2]), ml, b.z));
-                            acc3 += fast_exp2(fmaf(__uint_as_float(v[c + 3]), ml, b.w));
+                        for (int c = 0; c < 32; c += 8) {
+                            const float4 b0 = b4[c / 4], b1 = b4[c / 4 + 1];
+                            const uint64_t bias[4] = {two(b0.x, b0.y), two(b0.z, b0.w), two(b1.x, b1.y), two(b1.z, b1.w)};
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                const float2 x = apart(fma2(two(__uint_as_float(v[c + 2 * z]), __uint_as_float(v[c + 2 * z + 1])), ml2, bias[z]));
+                                const float2 e = 2 * z >= 8 - kFmaShare ? exp2_fma<5>(x.x, x.y) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                                acc[z & 1] = add2(acc[z & 1], two(e.x, e.y));
+                            }
                         }
                     } else if (j < it.n) {
                         const bool open = kp < prefix;  // the prefix opens this key to every token
@@ -327,7 +321,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     }
                 }
             }
-            const float sum = (acc0 + acc1) + (acc2 + acc3);
+            const float2 both = apart(add2(acc[0], acc[1]));
+            const float sum = both.x + both.y + acc0;
             if (!whole) a.rel_part[((size_t)blockIdx.x * 2 + (p.head ? 1 : 0)) * (2 * kTile) + g * kTile + r] = sum;
             else if (j < it.n) *rel = fmaf(exp2f((float)it.T * a.gamma_log2), old, sum);
             return true;

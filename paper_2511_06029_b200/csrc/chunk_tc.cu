@@ -34,6 +34,7 @@ constexpr int kLoadWarp = 11;    // TMA
 constexpr int kGatherWarp = 11;  // four warps
 constexpr int kMaxStages = 8;
 constexpr int kQuadRows = 16;
+constexpr int kFmaShare = 2;  // of eight exponentials, computed by polynomial
 constexpr float kLazy = 8.f;  // log2 of the growth of a row maximum that is left standing
 
 template <bool TMA>
@@ -81,11 +82,12 @@ __device__ __forceinline__ Piece piece_of(const ChunkArgs& a, int u, int at, int
     p.it = chunk_item(a, idx);
     p.toks = min(p.it.T - p.tok0, a.TU);
     p.hi = a.u_hi ? a.u_hi[u] : (a.append ? p.it.n_old + p.tok0 + p.toks : p.it.n_old);
-    p.tile0 = (a.u_lo ? a.u_lo[u] : 0) + at - s0;
-    p.nt = stop - at;
+    const int before = tiles_before(a, s0, at);
+    p.tile0 = (a.u_lo ? a.u_lo[u] : 0) + before;
+    p.nt = tiles_before(a, s0, stop) - before;
     p.alt = p.toks <= a.TT;
     p.quad = p.toks * a.G <= kQuadRows;
-    p.head = at == s0;
+    p.head = before == 0;
     p.tail = stop == s1;
     return p;
 }
@@ -133,7 +135,7 @@ __device__ __forceinline__ void for_pieces(const ChunkArgs& a, F f) {
         const int s1 = a.u_start[u + 1];
         if (s1 > at) {
             const int stop = min(end, s1);
-            if (!f(piece_of(a, u, at, stop, s0, s1))) return;
+            if (tiles_before(a, s0, stop) > tiles_before(a, s0, at) && !f(piece_of(a, u, at, stop, s0, s1))) return;
             at = stop;
         }
         s0 = s1;
@@ -394,23 +396,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     } else tmem_ld16(s_buf + NC * quarter, v);
                     tmem_ld_wait();
                     if (MOD) {
-                        if (a.softcap > 0.f) {
-#pragma unroll
-                            for (int c = 0; c < NC; c += 8) {
-                                float x[8], big = 0.f;
-#pragma unroll
-                                for (int y = 0; y < 8; ++y) {
-                                    x[y] = __uint_as_float(v[c + y]) * cap_in;
-                                    big = fmaxf(big, fabsf(x[y]));
-                                    v[c + y] = __float_as_uint(cap2 * capped_small(x[y]));
-                                }
-                                if (__any_sync(0xffffffffu, big > 0.55f)) {
-#pragma unroll
-                                    for (int y = 0; y < 8; ++y)
-                                        if (fabsf(x[y]) > 0.55f) v[c + y] = __float_as_uint(cap2 * capped_large(x[y]));
-                                }
-                            }
-                        }
+                        if (a.softcap > 0.f) cap_scores<NC>(v, cap_in, cap2);
                         if (a.slopes) {
                             const float in = a.softcap > 0.f ? 1.f : sl2;
 #pragma unroll
@@ -449,8 +435,8 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         m0 = max3(m0, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
                         m1 = max3(m1, __uint_as_float(v[c + 2]), __uint_as_float(v[c + 3]));
                     }
-                    const float mt = max3(fmaxf(m0, m1), __uint_as_float(v[NC - 2]), __uint_as_float(v[NC - 1])) * ml;
-                    const bool grow = valid_row && mt > m + kLazy;  // true from -inf too
+                    const float mt = max3(max3(m0, m1, m1), __uint_as_float(v[NC - 2]), __uint_as_float(v[NC - 1])) * ml;
+                    const bool grow = valid_row && !(mt <= m + kLazy);  // true from -inf, and for a NaN, which the row then keeps
                     if (__any_sync(0xffffffffu, grow)) {
                         const float w = grow ? exp2_diff(m, mt) : 1.f;
                         if (grow) m = mt;
@@ -471,14 +457,24 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     const uint64_t ml2 = two(ml, ml), nm2 = m == -INFINITY ? 0 : two(-m, -m);
                     uint64_t la = 0, lb = 0;
 #pragma unroll
-                    for (int y = 0; y < NC; y += 4) {
-                        const float2 xa = apart(fma2(two(__uint_as_float(v[y]), __uint_as_float(v[y + 1])), ml2, nm2));
-                        const float2 xb = apart(fma2(two(__uint_as_float(v[y + 2]), __uint_as_float(v[y + 3])), ml2, nm2));
-                        const float p0 = fast_exp2(xa.x), p1 = fast_exp2(xa.y), p2 = fast_exp2(xb.x), p3 = fast_exp2(xb.y);
-                        la = add2(la, two(p0, p1));
-                        lb = add2(lb, two(p2, p3));
-                        pk[y / 2] = pack_bf16(p0, p1);
-                        pk[y / 2 + 1] = pack_bf16(p2, p3);
+                    for (int y = 0; y < NC; y += 8) {
+                        float p[8];
+#pragma unroll
+                        for (int z = 0; z < 8; z += 2) {
+                            const float2 x = apart(fma2(two(__uint_as_float(v[y + z]), __uint_as_float(v[y + z + 1])), ml2, nm2));
+                            if (NC == 64 && z >= 8 - kFmaShare) {
+                                const float2 e = exp2_fma<4>(x.x, x.y);
+                                p[z] = e.x;
+                                p[z + 1] = e.y;
+                            } else {
+                                p[z] = fast_exp2(x.x);
+                                p[z + 1] = fast_exp2(x.y);
+                            }
+                        }
+                        la = add2(add2(la, two(p[0], p[1])), two(p[4], p[5]));
+                        lb = add2(add2(lb, two(p[2], p[3])), two(p[6], p[7]));
+#pragma unroll
+                        for (int z = 0; z < 8; z += 2) pk[(y + z) / 2] = pack_bf16(p[z], p[z + 1]);
                     }
                     const float2 sum = apart(add2(la, lb));
                     l += sum.x + sum.y;

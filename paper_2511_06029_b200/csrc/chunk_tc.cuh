@@ -165,7 +165,7 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* v) {
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Two fp32 operations in one instruction, and the three-way maximum.
+// Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t two(float lo, float hi) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
@@ -186,10 +186,70 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// A NaN among them comes through.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
+}
+
+// 2^x of two values on the FMA pipes, for a share of the exponentials that the special-function unit (16 a clock per SM) is the bound
+// of: x = n + r with n the nearest whole number (the low bits of x + 1.5 * 2^23) and r in [-1/2, 1/2], 2^r by a polynomial fitted
+// to the relative error (degree 4: 2.7e-6, degree 5: 2.1e-7 in fp32), n added to the exponent.  x is at most 127 here; below
+// -126 the result is 0 (for a NaN too: the callers look for those).
+template <int DEG>
+__device__ __forceinline__ float2 exp2_fma(float lo, float hi) {
+    constexpr float c4[6] = {0.9999992614236742f, 0.6931218147800758f, 0.24024744901073158f, 0.05591786008673926f, 0.009570098946574577f, 0.f};
+    constexpr float c5[6] = {1.0000000716545048f, 0.6931469670591965f, 0.2402211972442394f, 0.05550713282584675f, 0.009675541310994419f, 0.0013276469054922968f};
+    const uint64_t x = two(fmaxf(lo, -126.f), fmaxf(hi, -126.f));
+    const uint64_t t = add2(x, two(12582912.f, 12582912.f));
+    const uint64_t r = fma2(add2(t, two(-12582912.f, -12582912.f)), two(-1.f, -1.f), x);
+    const float* c = DEG == 4 ? c4 : c5;
+    uint64_t p = two(c[DEG], c[DEG]);
+#pragma unroll
+    for (int i = DEG - 1; i >= 0; --i) p = fma2(p, r, two(c[i], c[i]));
+    const float2 pf = apart(p), tf = apart(t);
+    const float a = __int_as_float(__float_as_int(pf.x) + (__float_as_int(tf.x) << 23)), b = __int_as_float(__float_as_int(pf.y) + (__float_as_int(tf.y) << 23));
+    return make_float2(lo >= -126.f ? a : 0.f, hi >= -126.f ? b : 0.f);
+}
+
+// softcap * tanh(t) in log2 units (cap2 = softcap * log2(e)) of NC logits, t = v * cap_in.
+template <int NC>
+__device__ __forceinline__ void cap_scores(uint32_t* v, float cap_in, float cap2) {
+    const uint64_t in2 = two(cap_in, cap_in), out2 = two(cap2, cap2);
+#pragma unroll
+    for (int c = 0; c < NC; c += 16) {
+        float big = 0.f;
+        uint64_t t[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+            t[y] = mul2(two(__uint_as_float(v[c + 2 * y]), __uint_as_float(v[c + 2 * y + 1])), in2);
+            const float2 f = apart(t[y]);
+            big = max3(big, fabsf(f.x), fabsf(f.y));
+            const uint64_t u = mul2(t[y], t[y]);
+            uint64_t p = fma2(u, two(-0.006235556820094805f, -0.006235556820094805f), two(0.021039673409724794f, 0.021039673409724794f));
+            p = fma2(u, p, two(-0.05384270671952741f, -0.05384270671952741f));
+            p = fma2(u, p, two(0.13332460742850846f, 0.13332460742850846f));
+            p = fma2(u, p, two(-0.33333310957894996f, -0.33333310957894996f));
+            p = fma2(u, p, two(0.9999999990645916f, 0.9999999990645916f));
+            const float2 r = apart(mul2(mul2(t[y], out2), p));
+            v[c + 2 * y] = __float_as_uint(r.x);
+            v[c + 2 * y + 1] = __float_as_uint(r.y);
+        }
+        if (__any_sync(0xffffffffu, !(big <= 0.55f))) {  // some are outside the polynomial's range (or NaN, behind the last slot)
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const float2 f = apart(t[y]);
+                if (fabsf(f.x) > 0.55f) v[c + 2 * y] = __float_as_uint(cap2 * capped_large(f.x));
+                if (fabsf(f.y) > 0.55f) v[c + 2 * y + 1] = __float_as_uint(cap2 * capped_large(f.y));
+            }
+        }
+    }
 }
 
 __device__ __forceinline__ void st_shared_16(uint32_t addr, const uint4& x) {
