@@ -1149,7 +1149,10 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     a.n_cta = simt ? 2 * ctx->sm_count : ctx->sm_count;
     a.min_per = simt ? 1 : 2;  // both softmax groups of a CTA have something to do
     a.QT = (max_chunk + a.TU - 1) / a.TU;
-    a.pad = simt ? 0 : 3;
+    // Beginning and ending a unit with two row tiles costs as much as about three of its tiles (8192-token prompt: 970 us with 3,
+    // 1036 with 1, 1080 with none; documents 654 / 658 / 664), about one where the scores are capped (528 / 520 / 515 us), nothing beside
+    // tiles that threads convert (218 / 211 / 208).
+    a.pad = simt || c->dtype != LETHE_BF16 ? 0 : a.softcap > 0.f ? 1 : 3;
     a.cap_tiles = (a.cap_tokens + kChunkTile - 1) / kChunkTile;
     const long long units = (long long)a.n_items * a.QT;
     if (units > 0x7fffffffLL / 4 || units * (a.cap_tiles + a.pad) > 0x7fffffffLL || units * a.cap_tiles * 2 > 0x7fffffffLL || (long long)a.n_items * a.cap_tiles * 2 > 0x7fffffffLL)

@@ -48,7 +48,7 @@ struct ChunkArgs {
     // scratch
     ChunkPlan* plan;
     int* n_old;      // [items] retained tokens before the call; -1: the item is left alone
-    int* u_start;    // [n_units + 1] where each unit begins on the line: `pad` steps, then its tiles
+    int* u_start;    // [n_units + 1] where each unit begins on the line: its pad, then its tiles
     int* u_lo;       // [n_units] first key tile of the unit (masks by position only, else NULL)
     int* u_hi;       // [n_units] slots the unit can see end here (masks by position only, else NULL)
     int* cta_unit;   // [n_cta] the unit that holds the first tile of each CTA's stretch
@@ -72,7 +72,7 @@ struct ChunkArgs {
     int TU;          // tokens per unit
     int QT;          // units per item
     int n_units, n_cta, cap_tiles, min_per;
-    int pad;         // tiles' worth of time that beginning and ending a unit takes, laid on the line before its tiles
+    int pad;         // tiles' worth of time that beginning and ending a unit takes (unit_pad), laid on the line before its tiles
     int append;
     float gamma_log2;
     int wait_limit;
@@ -152,8 +152,10 @@ __device__ __forceinline__ float capped_large(float t) {
 }
 __device__ __forceinline__ float capped(float t) { return fabsf(t) <= 0.55f ? capped_small(t) : capped_large(t); }
 
+// Tiles' worth of time that beginning and ending a unit of `toks` tokens takes (a unit with two row tiles of outputs).
+__device__ __forceinline__ int unit_pad(const ChunkArgs& a, int toks) { return toks > a.TT ? a.pad : 0; }
 // Tiles of a unit that begins at s0 on the line which lie before point x of the line.
-__device__ __forceinline__ int tiles_before(const ChunkArgs& a, int s0, int x) { return max(0, x - s0 - a.pad); }
+__device__ __forceinline__ int tiles_before(const ChunkArgs& a, int toks, int s0, int x) { return max(0, x - s0 - unit_pad(a, toks)); }
 
 // Query tiles that a pair of key tiles (its first slot j0) meets: [lo, hi).
 __device__ __forceinline__ int2 rel_hull(const ChunkArgs& a, const ChunkItem& it, int idx, int pair) {

@@ -25,9 +25,9 @@ __device__ __forceinline__ int unit_cost(const ChunkArgs& a, int u) {
     const int b = (idx / a.Hkv) % a.B;
     const int T = a.chunk_start[b + 1] - a.chunk_start[b], tok0 = qt * a.TU;
     if (tok0 >= T) return 0;
-    if (a.u_hi) return a.pad + max(1, (a.u_hi[u] + kChunkTile - 1) / kChunkTile - a.u_lo[u]);
+    if (a.u_hi) return unit_pad(a, T - tok0) + max(1, (a.u_hi[u] + kChunkTile - 1) / kChunkTile - a.u_lo[u]);
     const int hi = a.append ? n_old + min(T, tok0 + a.TU) : n_old;
-    return a.pad + max(1, (hi + kChunkTile - 1) / kChunkTile);  // rows that see nothing still have to be written
+    return unit_pad(a, T - tok0) + max(1, (hi + kChunkTile - 1) / kChunkTile);  // rows that see nothing still have to be written
 }
 
 // Lays the units end to end: u_start and the plan's totals.  One block.
@@ -346,12 +346,12 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
     const int s0 = a.u_start[u], s1 = a.u_start[u + 1];
     const int c0 = s0 / per, c1 = (s1 - 1) / per;
     if (c0 != c_mid - 1) return;  // begins here (nothing to merge) or was begun before CTA c_mid - 1
-    int with_tiles = 0;
-    for (int c = c0; c <= c1 && with_tiles < 2; ++c) with_tiles += tiles_before(a, s0, min(s1, (c + 1) * per)) > tiles_before(a, s0, max(s0, c * per));
-    if (with_tiles < 2) return;   // one CTA had all of its tiles and has written the outputs
     const int idx = u / a.QT, tok0 = (u - idx * a.QT) * a.TU;
     const ChunkItem it = chunk_item(a, idx);
-    const int rows = min(it.T - tok0, a.TU) * a.G;
+    const int toks = min(it.T - tok0, a.TU), rows = toks * a.G;
+    int with_tiles = 0;
+    for (int c = c0; c <= c1 && with_tiles < 2; ++c) with_tiles += tiles_before(a, toks, s0, min(s1, (c + 1) * per)) > tiles_before(a, toks, s0, max(s0, c * per));
+    if (with_tiles < 2) return;  // one CTA had all of its tiles and has written the outputs
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     // row blocks do not lie across row tiles: a tile has TT * G <= 128 rows, four blocks
     const int tile_idx = row0 / kChunkPartRows, r = row0 % kChunkPartRows + x;
@@ -363,8 +363,8 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
     for (int e = 0; e < E; ++e) o[e] = 0.f;
     if (ok) {
         for (int c = c0; c <= c1; ++c) {
-            const int before = tiles_before(a, s0, max(s0, c * per));
-            if (before == tiles_before(a, s0, min(s1, (c + 1) * per))) continue;  // only the unit's pad lies in this CTA
+            const int before = tiles_before(a, toks, s0, max(s0, c * per));
+            if (before == tiles_before(a, toks, s0, min(s1, (c + 1) * per))) continue;  // only the unit's pad lies in this CTA
             const size_t p = (size_t)(c * 2 + (before == 0 ? 1 : 0)) * 2 + tile_idx;
             const float2 ml = a.part_ml[p * kChunkPartRows + r];
             const float* src = a.part_o + (p * a.D + y) * kChunkPartRows + r;

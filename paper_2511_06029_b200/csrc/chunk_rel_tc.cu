@@ -26,13 +26,6 @@ constexpr int kTmemCols = 256;  // one logit tile per group
 template <int D>
 constexpr size_t smem_bytes() { return 1024 + 3 * (size_t)tile_bytes<D>(); }  // two key tiles, one query tile
 
-struct ColumnMod {
-    float qpos;   // relative to the sequence's first new token
-    float slope;  // log2 units
-    int lo;
-    int pad;
-};
-
 template <bool MOD>
 struct Shared {
     unsigned long long k_full, k_empty, q_full, q_empty;
@@ -42,7 +35,9 @@ struct Shared {
     int abort;
     int k_loads, q_loads, issued;
     alignas(16) float bias[kSoftWarps][kTile];
-    alignas(16) ColumnMod mod[MOD ? kSoftWarps : 1][MOD ? kTile : 1];
+    alignas(16) float qpos[MOD ? kSoftWarps : 1][kTile];   // relative to the sequence's first new token
+    alignas(16) float slope[MOD ? kSoftWarps : 1][kTile];  // log2 units
+    alignas(16) int lo[MOD ? kSoftWarps : 1][kTile];
 };
 
 // A CTA's piece of a unit: query tiles [qa, qb) of the pair of key tiles that begins at slot j0.
@@ -193,6 +188,9 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
         const int g = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + g * kTile;
         int n_s = 0, k = 0;
+        int col_tok[4];  // token of the tile that lane's columns lane, lane + 32, ... belong to
+#pragma unroll
+        for (int x = 0; x < 4; ++x) col_tok[x] = (x * 32 + lane) / a.G;
         if (tid == 0)  // where the stretch begins, for the merge
             for_rel_pieces(a, [&](const RelPiece& p) {
                 a.rel_cut[blockIdx.x] = make_int4(p.idx, p.pair, p.s0, p.s1);
@@ -205,7 +203,12 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
             if (!TMA) {
                 bool bad = false;
                 if (k > 0 && !warp_wait(&sh.k_empty, k - 1, abort_flag, limit)) return false;
-                for (int t = 0; t < (j0 + kTile < it.n ? 2 : 1); ++t) gather_tile<D>(a, a.k, it.item, it.n, j0 + t * kTile, k_tile + t * TILE, tid, kSoftWarps * 32, &bad);
+                for (int t = 0; t < (j0 + kTile < it.n ? 2 : 1); ++t)
+                    for (int half = 0; half < (a.dtype == LETHE_BF16 ? 2 : 1); ++half) {
+                        Gather<D, kSoftWarps * 32> x;
+                        x.load(a, a.k, it.item, it.n, j0 + t * kTile, tid, half, &bad);
+                        x.store(a, k_tile + t * TILE, tid, half);
+                    }
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) bar_arrive(&sh.k_full);
@@ -232,43 +235,77 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     kf = (float)((long long)kp - pos0);
                 }
             }
+            float col_slope[4];
+            if (MOD)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) col_slope[x] = a.slopes ? a.slopes[it.hkv * a.G + (x * 32 + lane) % a.G] * 1.4426950408889634f : 0.f;
             const float* nlse = a.nlse2 + (((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G;
             uint64_t acc[2] = {0, 0};
             float acc0 = 0.f;  // of columns judged one by one
+            // what the tile's columns bring along, fetched a tile ahead: lane x has columns x, x + 32, ...
+            float next_bias[4];
+            int next_pos[4], next_doc[4];
+            auto fetch = [&](int qt) {
+                const int cols = min(a.TT, it.T - qt * a.TT) * a.G;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int c = x * 32 + lane;
+                    next_bias[x] = c < cols ? nlse[qt * used + c] : -INFINITY;
+                    if (MOD) {
+                        const int tok = it.first + qt * a.TT + col_tok[x];
+                        next_pos[x] = c < cols && a.token_pos ? a.token_pos[tok] : 0;
+                        next_doc[x] = c < cols && a.doc_start ? a.doc_start[tok] : INT32_MIN;
+                    }
+                }
+            };
+            fetch(p.qa);
             for (int qt = p.qa; qt < p.qb; ++qt) {
-                // biases of the tile's columns, one copy per warp (the warps never wait for one another)
+                // one copy per warp (the warps never wait for one another)
                 const int cols = min(a.TT, it.T - qt * a.TT) * a.G;
                 int lo_max = INT32_MIN;
                 bool nan = false;  // a token whose scores are NaN: every column is judged, so that it comes through
                 __syncwarp();
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int c = x * 32 + lane, tok = qt * a.TT + c / a.G;
-                    float bias = -INFINITY;
-                    if (c < cols) bias = nlse[qt * used + c] + (float)(it.T - 1 - tok) * a.gamma_log2;
+                    const int c = x * 32 + lane;
+                    const float bias = next_bias[x] + (float)(it.T - 1 - qt * a.TT - col_tok[x]) * a.gamma_log2;
                     sh.bias[warp][c] = bias;
                     nan = nan || bias != bias;
                     if (MOD) {
-                        ColumnMod cm = {0.f, 0.f, INT32_MIN, 0};
-                        if (c < cols) {
-                            const int qp = a.token_pos ? a.token_pos[it.first + tok] : 0;
-                            cm.qpos = (float)((long long)qp - pos0);
-                            if (a.slopes) cm.slope = a.slopes[it.hkv * a.G + c % a.G] * 1.4426950408889634f;
-                            cm.lo = chunk_lo(a, it.first + tok, qp);
-                        }
-                        sh.mod[warp][c] = cm;
-                        lo_max = max(lo_max, cm.lo);
+                        int lo = next_doc[x];
+                        if (a.window > 0) lo = (int)max((long long)lo, (long long)next_pos[x] - a.window + 1);
+                        sh.qpos[warp][c] = (float)((long long)next_pos[x] - pos0);
+                        sh.slope[warp][c] = col_slope[x];
+                        sh.lo[warp][c] = c < cols ? lo : INT32_MAX;  // columns that are not there see nothing
+                        if (c < cols) lo_max = max(lo_max, lo);
                     }
                 }
                 if (MOD) lo_max = __reduce_max_sync(0xffffffffu, lo_max);
+                if (qt + 1 < p.qb) fetch(qt + 1);
                 __syncwarp();
+                // the columns [from, to) see this thread's key: they reach it in causal order (or a prefix opens it to all), and their
+                // windows and documents, which grow with the tokens, have not left it behind
+                int from = a.append && !(MOD && kp < prefix) ? (j - it.n_old - qt * a.TT) * a.G : 0, to = cols;
+                bool run = true;
+                // a short tile's other columns are tokens of other sequences: whatever they hold must not count
+                const bool clean = cols == used && __all_sync(0xffffffffu, !nan && from <= 0 && (!mask_pos || kp >= lo_max));
+                if (MOD && mask_pos && !clean) {
+                    bool up = true;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) up = up && (x * 32 + lane + 1 >= kTile || sh.lo[warp][x * 32 + lane] <= sh.lo[warp][x * 32 + lane + 1]);
+                    run = __all_sync(0xffffffffu, up);
+                    int end = 0;
+#pragma unroll
+                    for (int half = kTile / 2; half >= 1; half >>= 1)
+                        if (sh.lo[warp][end + half - 1] <= kp) end += half;
+                    end += sh.lo[warp][end] <= kp;
+                    to = min(to, end);
+                }
+                if (j >= it.n) to = 0;
                 if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
                 tc_after();
-                // first column that reaches slot j in causal order
-                const int c_lo = a.append ? (j - it.n_old - qt * a.TT) * a.G : 0;
-                // a short tile's other columns are tokens of other sequences: whatever they hold must not count
-                const bool clean = cols == used && __all_sync(0xffffffffu, !nan && c_lo <= 0 && (!mask_pos || kp >= lo_max));
-#pragma unroll
+                // rolled where scores are shaped: unrolled, the code outgrows the instruction cache
+#pragma unroll (MOD ? 1 : 4)
                 for (int ch = 0; ch < kTile; ch += 32) {
                     if (ch >= cols) break;  // a short chunk leaves most columns empty
                     uint32_t v[32];
@@ -287,9 +324,12 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                         }
                         if (a.slopes) {
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) {
-                                const float2 qs = *reinterpret_cast<const float2*>(&sh.mod[warp][ch + c]);
-                                v[c] = __float_as_uint(fmaf(-qs.y, fabsf(qs.x - kf), __uint_as_float(v[c]) * ml));
+                            for (int c = 0; c < 32; c += 4) {
+                                const float4 qp = *reinterpret_cast<const float4*>(&sh.qpos[warp][ch + c]), sl = *reinterpret_cast<const float4*>(&sh.slope[warp][ch + c]);
+                                v[c] = __float_as_uint(fmaf(-sl.x, fabsf(qp.x - kf), __uint_as_float(v[c]) * ml));
+                                v[c + 1] = __float_as_uint(fmaf(-sl.y, fabsf(qp.y - kf), __uint_as_float(v[c + 1]) * ml));
+                                v[c + 2] = __float_as_uint(fmaf(-sl.z, fabsf(qp.z - kf), __uint_as_float(v[c + 2]) * ml));
+                                v[c + 3] = __float_as_uint(fmaf(-sl.w, fabsf(qp.w - kf), __uint_as_float(v[c + 3]) * ml));
                             }
                             ml = 1.f;
                         }
@@ -308,15 +348,25 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                                 acc[z & 1] = add2(acc[z & 1], two(e.x, e.y));
                             }
                         }
-                    } else if (j < it.n) {
-                        const bool open = kp < prefix;  // the prefix opens this key to every token
+                    } else if (run) {
+                        if (__any_sync(0xffffffffu, from < ch + 32 && to > ch)) {
+                            const int c0 = from - ch, c1 = to - ch;
+#pragma unroll
+                            for (int c = 0; c < 32; c += 4) {
+                                const float4 b = b4[c / 4];
+                                const float e0 = fast_exp2(fmaf(__uint_as_float(v[c]), ml, b.x)), e1 = fast_exp2(fmaf(__uint_as_float(v[c + 1]), ml, b.y));
+                                const float e2 = fast_exp2(fmaf(__uint_as_float(v[c + 2]), ml, b.z)), e3 = fast_exp2(fmaf(__uint_as_float(v[c + 3]), ml, b.w));
+                                if (c >= c0 && c < c1) acc0 += e0;
+                                if (c + 1 >= c0 && c + 1 < c1) acc0 += e1;
+                                if (c + 2 >= c0 && c + 2 < c1) acc0 += e2;
+                                if (c + 3 >= c0 && c + 3 < c1) acc0 += e3;
+                            }
+                        }
+                    } else if (MOD) {  // documents that do not grow with the tokens: every column by itself
 #pragma unroll
                         for (int c = 0; c < 32; ++c) {
-                            const int cc = ch + c;
-                            bool see = cc < cols && (cc >= c_lo || (MOD && open));
-                            if (MOD && mask_pos) see = see && kp >= sh.mod[warp][cc].lo;
-                            const float e = fast_exp2(fmaf(__uint_as_float(v[c]), ml, sh.bias[warp][cc]));
-                            if (see) acc0 += e;
+                            const float e = fast_exp2(fmaf(__uint_as_float(v[c]), ml, sh.bias[warp][ch + c]));
+                            if (j < it.n && ch + c >= from && ch + c < cols && kp >= sh.lo[warp][ch + c]) acc0 += e;
                         }
                     }
                 }

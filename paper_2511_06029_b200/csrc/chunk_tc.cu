@@ -82,9 +82,9 @@ __device__ __forceinline__ Piece piece_of(const ChunkArgs& a, int u, int at, int
     p.it = chunk_item(a, idx);
     p.toks = min(p.it.T - p.tok0, a.TU);
     p.hi = a.u_hi ? a.u_hi[u] : (a.append ? p.it.n_old + p.tok0 + p.toks : p.it.n_old);
-    const int before = tiles_before(a, s0, at);
+    const int before = tiles_before(a, p.toks, s0, at);
     p.tile0 = (a.u_lo ? a.u_lo[u] : 0) + before;
-    p.nt = tiles_before(a, s0, stop) - before;
+    p.nt = tiles_before(a, p.toks, s0, stop) - before;
     p.alt = p.toks <= a.TT;
     p.quad = p.toks * a.G <= kQuadRows;
     p.head = before == 0;
@@ -135,7 +135,8 @@ __device__ __forceinline__ void for_pieces(const ChunkArgs& a, F f) {
         const int s1 = a.u_start[u + 1];
         if (s1 > at) {
             const int stop = min(end, s1);
-            if (tiles_before(a, s0, stop) > tiles_before(a, s0, at) && !f(piece_of(a, u, at, stop, s0, s1))) return;
+            const Piece p = piece_of(a, u, at, stop, s0, s1);
+            if (p.nt > 0 && !f(p)) return;
             at = stop;
         }
         s0 = s1;
@@ -211,17 +212,31 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
             }
             __syncwarp();
         } else {
+            // bf16 tiles take two register tiles; the next one's loads are under way while this one waits for its slot
+            const int gt = tid - kGatherWarp * 32, halves = a.dtype == LETHE_BF16 ? 2 : 1;
             for_pieces(a, [&](const Piece& p) {
-                for (int t = 0; t < 2 * p.nt; ++t, ++e) {
-                    const int s = e % NS;
-                    if (e >= NS && !warp_wait(&sh.empty[s], e / NS - 1, abort_flag, limit)) return false;
-                    if (tid == kGatherWarp * 32) *(volatile int*)&sh.loaded = e + 1;
+                Gather<D, 128> now, next;
+                auto load = [&](Gather<D, 128>& x, int i) {  // i-th register tile of the piece
                     bool is_v;
-                    const int tile = p.tile0 + entry_tile(p, t, is_v);
-                    gather_tile<D>(a, is_v ? a.v : a.k, p.it.item, p.hi, tile * kTile, ring + s * TILE, tid - kGatherWarp * 32, 128, &bad);
-                    proxy_fence();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(&sh.full[s]);
+                    const int tile = p.tile0 + entry_tile(p, i / halves, is_v);
+                    x.load(a, is_v ? a.v : a.k, p.it.item, p.hi, tile * kTile, gt, i % halves, &bad);
+                };
+                load(now, 0);
+                for (int i = 0; i < 2 * p.nt * halves; ++i) {
+                    if (i + 1 < 2 * p.nt * halves) load(next, i + 1);
+                    const int s = e % NS;
+                    if (i % halves == 0) {
+                        if (e >= NS && !warp_wait(&sh.empty[s], e / NS - 1, abort_flag, limit)) return false;
+                        if (gt == 0) *(volatile int*)&sh.loaded = e + 1;
+                    }
+                    now.store(a, ring + s * TILE, gt, i % halves);
+                    if ((i + 1) % halves == 0) {
+                        proxy_fence();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(&sh.full[s]);
+                        ++e;
+                    }
+                    now = next;
                 }
                 if (bad) record_error(a.status, LETHE_ERR_PAGE, p.it.item);
                 bad = false;
@@ -354,7 +369,8 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
             const float ml = MOD && (a.softcap > 0.f || a.slopes) ? 1.f : sl2;
             float m = -INFINITY, l = 0.f;
             const int jobs = piece_jobs(p, g);
-            int kp_min = INT32_MIN;
+            int kp_min, from = 0, to = 0;  // masks by position, per tile
+            bool clean = true, run = true;
             for (int n = 0; n < jobs; ++n) {
                 const int buf = n & 1, t = p.alt ? 2 * (n >> 1) + g : n >> 1, j0 = (p.tile0 + t) * kTile;
                 if (MOD && by_pos && busy && buf == 0) {  // positions of the tile's keys, while the product runs
@@ -368,8 +384,33 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         sh.kposf[warp][c * 32 + lane] = (float)((long long)kp - pos0);
                         kp_min = min(kp_min, kp);
                     }
-                    kp_min = __reduce_min_sync(0xffffffffu, kp_min);
                     __syncwarp();
+                    if (mask_pos) {
+                        kp_min = __reduce_min_sync(0xffffffffu, kp_min);
+                        const int nn = p.it.n - j0;
+                        clean = __all_sync(0xffffffffu, kp_min >= lo && lim - j0 >= kTile && nn >= kTile);
+                        if (!clean) {
+                            // Positions that grow with the slot (any cache that was only appended to and pruned): what a row sees of
+                            // the tile is a run of columns [from, to), found by halving.  Else every key is judged by itself.
+                            bool up = true;
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const int x = c * 32 + lane;
+                                up = up && (x + 1 >= kTile || sh.kpos[warp][x] <= sh.kpos[warp][x + 1]);
+                            }
+                            run = __all_sync(0xffffffffu, up);
+                            from = 0;
+                            int opened = 0;  // keys before the prefix's end
+#pragma unroll
+                            for (int half = kTile / 2; half >= 1; half >>= 1) {
+                                if (sh.kpos[warp][from + half - 1] < lo) from += half;
+                                if (sh.kpos[warp][opened + half - 1] < prefix) opened += half;
+                            }
+                            from += sh.kpos[warp][from] < lo;
+                            opened += sh.kpos[warp][opened] < prefix;
+                            to = lim == INT32_MAX ? nn : max(lim - j0, min(opened, nn));
+                        }
+                    }
                 }
                 if (!warp_wait(&sh.s_full[g][buf], buf ? s1++ : s0++, abort_flag, limit)) return false;
                 tc_after();
@@ -390,38 +431,56 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     const int c0 = 64 * buf + (NC == 64 ? 0 : NC * quarter);
                     const uint32_t s_buf = s_addr + 64 * buf;
                     uint32_t v[NC], pk[32];
+                    if (MOD) {
+                        // Scores are shaped sixteen columns at a time and put back: unrolled over the whole row the code outgrows the
+                        // instruction cache (a job took 8000 clocks instead of 2500).
+                        const float in = a.softcap > 0.f ? 1.f : sl2;
+                        const int nv = min(lim, p.it.n) - j0;
+                        const bool masked = mask_pos ? !clean : __any_sync(0xffffffffu, nv < c0 + NC);
+                        if (masked || a.softcap > 0.f || a.slopes) {
+#pragma unroll 1
+                            for (int c = 0; c < NC; c += 16) {
+                                const uint32_t at = s_buf + (NC == 64 ? c : NC * quarter);
+                                uint32_t w[16];
+                                tmem_ld16(at, w);
+                                tmem_ld_wait();
+                                if (a.softcap > 0.f) cap_scores<16>(w, cap_in, cap2);
+                                if (a.slopes) {
+#pragma unroll
+                                    for (int y = 0; y < 16; y += 4) {
+                                        const float4 kf = *reinterpret_cast<const float4*>(&sh.kposf[warp][c0 + c + y]);
+                                        w[y] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.x), __uint_as_float(w[y]) * in));
+                                        w[y + 1] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.y), __uint_as_float(w[y + 1]) * in));
+                                        w[y + 2] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.z), __uint_as_float(w[y + 2]) * in));
+                                        w[y + 3] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.w), __uint_as_float(w[y + 3]) * in));
+                                    }
+                                }
+                                if (masked) {
+                                    if (!mask_pos || run) {
+                                        const int y0 = (mask_pos ? from : 0) - c0 - c, y1 = (mask_pos ? to : nv) - c0 - c;
+#pragma unroll
+                                        for (int y = 0; y < 16; ++y)
+                                            if (y < y0 || y >= y1) w[y] = 0xff800000u;
+                                    } else {
+                                        const int nn = p.it.n - j0 - c0 - c, nl = lim == INT32_MAX ? nn : lim - j0 - c0 - c;
+#pragma unroll
+                                        for (int y = 0; y < 16; ++y) {
+                                            const int kp = sh.kpos[warp][c0 + c + y];
+                                            if (!((y < nl || (kp < prefix && y < nn)) && kp >= lo)) w[y] = 0xff800000u;
+                                        }
+                                    }
+                                }
+                                tmem_st16(at, w);
+                            }
+                            tmem_st_wait();
+                        }
+                    }
                     if (NC == 64) {
                         tmem_ld32(s_buf, v);
                         tmem_ld32(s_buf + 32, v + (NC == 64 ? 32 : 0));
                     } else tmem_ld16(s_buf + NC * quarter, v);
                     tmem_ld_wait();
-                    if (MOD) {
-                        if (a.softcap > 0.f) cap_scores<NC>(v, cap_in, cap2);
-                        if (a.slopes) {
-                            const float in = a.softcap > 0.f ? 1.f : sl2;
-#pragma unroll
-                            for (int c = 0; c < NC; c += 4) {
-                                const float4 kf = *reinterpret_cast<const float4*>(&sh.kposf[warp][c0 + c]);
-                                v[c] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.x), __uint_as_float(v[c]) * in));
-                                v[c + 1] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.y), __uint_as_float(v[c + 1]) * in));
-                                v[c + 2] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.z), __uint_as_float(v[c + 2]) * in));
-                                v[c + 3] = __float_as_uint(fmaf(-slope, fabsf(qf - kf.w), __uint_as_float(v[c + 3]) * in));
-                            }
-                        }
-                    }
-                    if (MOD && mask_pos) {
-                        if (!__all_sync(0xffffffffu, kp_min >= lo && lim - j0 >= kTile && p.it.n - j0 >= kTile)) {
-                            const int nn = p.it.n - j0 - c0, nv = lim == INT32_MAX ? nn : lim - j0 - c0;
-#pragma unroll
-                            for (int c = 0; c < NC; c += 4) {
-                                const int4 kp = *reinterpret_cast<const int4*>(&sh.kpos[warp][c0 + c]);
-                                if (!((c < nv || (kp.x < prefix && c < nn)) && kp.x >= lo)) v[c] = 0xff800000u;
-                                if (!((c + 1 < nv || (kp.y < prefix && c + 1 < nn)) && kp.y >= lo)) v[c + 1] = 0xff800000u;
-                                if (!((c + 2 < nv || (kp.z < prefix && c + 2 < nn)) && kp.z >= lo)) v[c + 2] = 0xff800000u;
-                                if (!((c + 3 < nv || (kp.w < prefix && c + 3 < nn)) && kp.w >= lo)) v[c + 3] = 0xff800000u;
-                            }
-                        }
-                    } else {
+                    if (!MOD) {
                         const int nv = min(lim, p.it.n) - j0 - c0;  // of these keys the row sees so many
                         if (__any_sync(0xffffffffu, nv < NC)) {
 #pragma unroll

@@ -157,6 +157,13 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* v) {
         : "r"(taddr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+          "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
                  ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr)
@@ -306,36 +313,43 @@ __device__ __forceinline__ uint4 expand8(uint2 w, bool e5m2) {
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// The same tile by `nt` threads with plain loads: any page size, any storage type.  Rows at or beyond `end` are zeros.
-template <int D>
-__device__ __forceinline__ void gather_tile(const ChunkArgs& a, const void* base, int item, int end, int j0, uint32_t dst, int tid, int nt, bool* bad) {
-    constexpr int C = D / 8;       // 16-byte operand chunks per row
-    constexpr int U = 4;           // chunks a thread has in flight
-    const bool bytes = a.dtype != LETHE_BF16, e5m2 = a.dtype == LETHE_FP8_E5M2;
-    for (int i0 = tid; i0 < kTile * C; i0 += U * nt) {
-        uint4 x[U];
+// The same tile by NT threads with plain loads: any page size, any storage type.  A thread holds its 16-byte pieces of a stored tile in
+// registers between `load` and `store`, so that the next tile's loads run under this one's conversion and the wait for its slot.
+// Rows at or beyond `end` are zeros.
+template <int D, int NT>
+struct Gather {
+    static constexpr int kByteLoads = kTile * D / 16 / NT;  // 16 bytes: 16 elements of a byte cache, 8 of a bf16 one (two loads then)
+    uint4 x[kByteLoads];
+
+    // half: which half of the columns (bf16: a register tile is half a tile wide)
+    __device__ __forceinline__ void load(const ChunkArgs& a, const void* base, int item, int end, int j0, int tid, int half, bool* bad) {
+        const bool bytes = a.dtype != LETHE_BF16;
+        constexpr int C = D / 16;  // 16-byte pieces of a row of bytes, or of half a bf16 row
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * nt, r = i / C, c = i % C;
+        for (int u = 0; u < kByteLoads; ++u) {
+            const int i = tid + u * NT, r = i / C, c = i % C;
             x[u] = make_uint4(0, 0, 0, 0);
-            if (i < kTile * C && j0 + r < end) {
+            if (j0 + r < end) {
                 const long long at = chunk_row(a, item, j0 + r);
                 if (at < 0) *bad = true;
-                else if (!bytes) x[u] = reinterpret_cast<const uint4*>((const char*)base + (size_t)at * (D * 2))[c];
-                else {
-                    const uint2 w = reinterpret_cast<const uint2*>((const char*)base + (size_t)at * D)[c];
-                    x[u].x = w.x;
-                    x[u].y = w.y;
-                }
+                else x[u] = reinterpret_cast<const uint4*>((const char*)base + (size_t)at * (bytes ? D : 2 * D))[bytes ? c : half * C + c];
             }
         }
+    }
+    __device__ __forceinline__ void store(const ChunkArgs& a, uint32_t dst, int tid, int half) const {
+        constexpr int C = D / 16;
+        const bool e5m2 = a.dtype == LETHE_FP8_E5M2;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * nt;
-            if (i < kTile * C) st_shared_16(chunk_addr(dst, i / C, i % C), bytes ? expand8(make_uint2(x[u].x, x[u].y), e5m2) : x[u]);
+        for (int u = 0; u < kByteLoads; ++u) {
+            const int i = tid + u * NT, r = i / C, c = i % C;
+            if (a.dtype == LETHE_BF16) st_shared_16(chunk_addr(dst, r, half * C + c), x[u]);
+            else {
+                st_shared_16(chunk_addr(dst, r, 2 * c), expand8(make_uint2(x[u].x, x[u].y), e5m2));
+                st_shared_16(chunk_addr(dst, r, 2 * c + 1), expand8(make_uint2(x[u].z, x[u].w), e5m2));
+            }
         }
     }
-}
+};
 
 // Whether K and V tiles can come by TMA: bf16 rows, and pages that tile the 128 rows in whole swizzle groups.
 inline bool tma_can_tile(const ChunkArgs& a) {
