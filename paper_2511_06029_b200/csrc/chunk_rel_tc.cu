@@ -128,29 +128,33 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
     const uint32_t tmem = sh.tmem_base;
 
     if (warp == kLoadWarp) {
-        if (lane == 0) {
-            bool bad = false;  // the attention has recorded bad pages
-            int k = 0, qn = 0;
-            for_rel_pieces(a, [&](const RelPiece& p) {
-                if (TMA) {
-                    if (k > 0 && !bar_wait(&sh.k_empty, k - 1, abort_flag, limit)) return false;
-                    const int tiles = p.j0 + kTile < p.it.n ? 2 : 1;
+        TileLoader<D> loader;  // bad pages: the attention has recorded them
+        int k = 0, qn = 0;
+        for_rel_pieces(a, [&](const RelPiece& p) {
+            if (TMA) {
+                if (k > 0 && !warp_wait(&sh.k_empty, k - 1, abort_flag, limit)) return false;
+                const int tiles = p.j0 + kTile < p.it.n ? 2 : 1;
+                if (lane == 0) {
                     bar_expect_tx(&sh.k_full, tiles * TILE);
                     sh.k_loads = k + 1;
-                    for (int g = 0; g < tiles; ++g) tma_tile<D>(a, &maps.k, p.it.item, p.it.n, p.j0 + g * kTile, k_tile + g * TILE, &sh.k_full, &bad);
                 }
-                ++k;
-                for (int qt = p.qa; qt < p.qb; ++qt) {
-                    if (qn > 0 && !bar_wait(&sh.q_empty, qn - 1, abort_flag, limit)) return false;
+                __syncwarp();
+                loader.reset();
+                for (int g = tiles - 1; g >= 0; --g) loader.load(a, &maps.k, p.it.item, p.it.n, p.j0 + g * kTile, k_tile + g * TILE, &sh.k_full);
+            }
+            ++k;
+            for (int qt = p.qa; qt < p.qb; ++qt) {
+                if (qn > 0 && !warp_wait(&sh.q_empty, qn - 1, abort_flag, limit)) return false;
+                ++qn;
+                if (lane == 0) {
                     bar_expect_tx(&sh.q_full, (unsigned)(used * D * 2));
-                    sh.q_loads = ++qn;
-#pragma unroll
-                    for (int hf = 0; hf < D / 64; ++hf)
-                        tma_4d(q_tile + hf * kHalfBytes, &maps.q, 64 * hf, p.it.hkv * a.G, p.it.first + qt * a.TT, p.it.li, &sh.q_full);
+                    sh.q_loads = qn;
                 }
-                return true;
-            });
-        }
+                __syncwarp();
+                if (lane < D / 64) tma_4d(q_tile + lane * kHalfBytes, &maps.q, 64 * lane, p.it.hkv * a.G, p.it.first + qt * a.TT, p.it.li, &sh.q_full);
+            }
+            return true;
+        });
         __syncwarp();
     } else if (warp == kMmaWarp) {
         const uint64_t q_desc = smem_desc(q_tile, 16), k_desc = smem_desc(k_tile, 16);

@@ -92,14 +92,16 @@ __device__ __forceinline__ Piece piece_of(const ChunkArgs& a, int u, int at, int
     return p;
 }
 
-// Jobs of group g in a piece: two halves of each of its tiles; a last tile of which only the first half is seen has one.
-__device__ __forceinline__ int piece_jobs(const Piece& p, int g) {
-    const bool short_end = p.hi - (p.tile0 + p.nt - 1) * kTile <= 64;
-    if (!p.alt) return 2 * p.nt - short_end;
-    return 2 * ((p.nt - g + 1) >> 1) - (short_end && ((p.nt - 1) & 1) == g);
-}
+// A piece's tiles are taken last first: the nearest keys of a causal row, which a distance bias favours, set its maximum at once
+// (first to last, steep slopes made it grow, and the outputs be rescaled, with every job: 7000 clocks of each).  Job n of a group is
+// half 1 - (n & 1) of its (n / 2)-th tile; jobs run from first_job to job_end.
+__device__ __forceinline__ int seq_tile(const Piece& p, int s) { return p.tile0 + p.nt - 1 - s; }
+// Where the piece's last tile has nothing to see in its second half, that job is left out.
+__device__ __forceinline__ int first_job(const Piece& p, int g) { return (!p.alt || g == 0) && p.hi - (p.tile0 + p.nt - 1) * kTile <= 64; }
+__device__ __forceinline__ int job_end(const Piece& p, int g) { return p.alt ? 2 * ((p.nt - g + 1) >> 1) : 2 * p.nt; }
+__device__ __forceinline__ int job_seq(const Piece& p, int g, int n) { return p.alt ? 2 * (n >> 1) + g : n >> 1; }
 
-// Ring entries of a piece's tiles.  A pair goes through K and V of one tile at a time; with alternate tiles both groups' K come first
+// Ring entries of a piece's tiles, by their place in that order.  A pair goes through K and V of one tile at a time; with alternate tiles both groups' K come first
 // (a group needs its next K before the other has let its V go: in the ring's order K0 V0 K1 V1 four slots would lock up).
 __device__ __forceinline__ int k_entry(const Piece& p, int t) { return p.alt ? 4 * (t >> 1) + (t & 1) : 2 * t; }
 __device__ __forceinline__ int v_entry(const Piece& p, int t) { return p.alt ? 4 * (t >> 1) + min(2, p.nt - (t & ~1)) + (t & 1) : 2 * t + 1; }
@@ -191,34 +193,38 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
 
     if (warp >= kLoadWarp) {
         // ------------------------------------------------------------------ K and V tiles
-        bool bad = false;
         int e = 0;
         if (TMA) {
-            if (lane == 0) {
-                for_pieces(a, [&](const Piece& p) {
-                    for (int t = 0; t < 2 * p.nt; ++t, ++e) {
-                        const int s = e % NS;
-                        if (e >= NS && !bar_wait(&sh.empty[s], e / NS - 1, abort_flag, limit)) return false;
+            TileLoader<D> loader;
+            int item = -1;
+            for_pieces(a, [&](const Piece& p) {
+                if (p.it.item != item) loader.reset();
+                item = p.it.item;
+                for (int t = 0; t < 2 * p.nt; ++t, ++e) {
+                    const int s = e % NS;
+                    if (e >= NS && !warp_wait(&sh.empty[s], e / NS - 1, abort_flag, limit)) return false;
+                    if (lane == 0) {
                         bar_expect_tx(&sh.full[s], TILE);
                         *(volatile int*)&sh.loaded = e + 1;
-                        bool is_v;
-                        const int tile = p.tile0 + entry_tile(p, t, is_v);
-                        tma_tile<D>(a, is_v ? &maps.v : &maps.k, p.it.item, p.it.n, tile * kTile, ring + s * TILE, &sh.full[s], &bad);
                     }
-                    if (bad) record_error(a.status, LETHE_ERR_PAGE, p.it.item);
-                    bad = false;
-                    return true;
-                });
-            }
-            __syncwarp();
+                    __syncwarp();
+                    bool is_v;
+                    const int tile = seq_tile(p, entry_tile(p, t, is_v));
+                    loader.load(a, is_v ? &maps.v : &maps.k, p.it.item, p.it.n, tile * kTile, ring + s * TILE, &sh.full[s]);
+                }
+                if (loader.bad) record_error(a.status, LETHE_ERR_PAGE, p.it.item);
+                loader.bad = false;
+                return true;
+            });
         } else {
+            bool bad = false;
             // bf16 tiles take two register tiles; the next one's loads are under way while this one waits for its slot
             const int gt = tid - kGatherWarp * 32, halves = a.dtype == LETHE_BF16 ? 2 : 1;
             for_pieces(a, [&](const Piece& p) {
                 Gather<D, 128> now, next;
                 auto load = [&](Gather<D, 128>& x, int i) {  // i-th register tile of the piece
                     bool is_v;
-                    const int tile = p.tile0 + entry_tile(p, i / halves, is_v);
+                    const int tile = seq_tile(p, entry_tile(p, i / halves, is_v));
                     x.load(a, is_v ? a.v : a.k, p.it.item, p.hi, tile * kTile, gt, i % halves, &bad);
                 };
                 load(now, 0);
@@ -274,7 +280,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
         for_pieces(a, [&](const Piece& p) {
             const uint32_t qk_desc = mma_idesc(64, false, a.scale[p.it.l] < 0.f);
             const uint64_t qd = q_desc + (uint64_t)((p.alt ? 0 : g) * (TILE >> 4));
-            const int jobs = piece_jobs(p, g);
+            const int n0 = first_job(p, g), end = job_end(p, g);
             if (!warp_wait(&sh.q_full, k, abort_flag, limit)) return false;
             // a tile's ring entry is let go by both groups, or twice by the one that uses it
             auto let_go = [&](int slot) {
@@ -282,11 +288,11 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                 if (p.alt) tc_commit(&sh.empty[slot]);
             };
             auto qk = [&](int n) -> bool {
-                const int buf = n & 1, e = base + k_entry(p, p.alt ? 2 * (n >> 1) + g : n >> 1), slot = e % NS;
+                const int buf = n & 1, e = base + k_entry(p, job_seq(p, g, n)), slot = e % NS;
                 if (!warp_wait(&sh.full[slot], e / NS, abort_flag, limit)) return false;
                 tc_after();
                 if (elect_one()) {
-                    const uint64_t kd = k_desc + (uint64_t)(slot * (TILE >> 4) + buf * (64 * 128 >> 4));
+                    const uint64_t kd = k_desc + (uint64_t)(slot * (TILE >> 4) + (1 - buf) * (64 * 128 >> 4));
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) {
                         constexpr int half16 = kHalfBytes >> 4;
@@ -294,35 +300,35 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     }
                     sh.issued[g] = 1;
                     tc_commit(&sh.s_full[g][buf]);
-                    if (buf == 1 || n + 1 == jobs) let_go(slot);
-                    if (n + 1 == jobs) tc_commit(&sh.q_done);
+                    if (buf == 1) let_go(slot);
+                    if (n + 1 == end) tc_commit(&sh.q_done);
                 }
                 __syncwarp();
                 return true;
             };
-            if (jobs > 0 && !qk(0)) return false;
-            if (jobs > 1 && !qk(1)) return false;
-            if (jobs == 0 && elect_one()) tc_commit(&sh.q_done);
+            if (n0 < end && !qk(n0)) return false;
+            if (n0 + 1 < end && !qk(n0 + 1)) return false;
+            if (n0 >= end && elect_one()) tc_commit(&sh.q_done);
             __syncwarp();
-            for (int n = 0; n < jobs; ++n) {
-                const int buf = n & 1, t = p.alt ? 2 * (n >> 1) + g : n >> 1, e = base + v_entry(p, t), slot = e % NS;
-                if (buf == 0) {
+            for (int n = n0; n < end; ++n) {
+                const int buf = n & 1, half = 1 - buf, t = job_seq(p, g, n), e = base + v_entry(p, t), slot = e % NS;
+                if (buf == 0 || n == n0) {
                     if (lone_v(p, t) && !wait_issued(&sh.loaded, e, abort_flag, limit)) return false;
                     if (!warp_wait(&sh.full[slot], e / NS, abort_flag, limit)) return false;
                 }
-                const int steps = max(1, (min(64, p.hi - (p.tile0 + t) * kTile - 64 * buf) + 15) / 16);
-                const uint64_t vd = v_desc + (uint64_t)(slot * (TILE >> 4) + buf * (64 * 128 >> 4));
+                const int steps = max(1, (min(64, p.hi - seq_tile(p, t) * kTile - 64 * half) + 15) / 16);
+                const uint64_t vd = v_desc + (uint64_t)(slot * (TILE >> 4) + half * (64 * 128 >> 4));
                 if (!warp_wait(&sh.p_full[g][buf], buf ? np1++ : np0++, abort_flag, limit)) return false;
                 tc_after();
                 if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        if (ks < steps) mma_ts(ot, st + 64 * buf + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), pv_desc, n > 0 || ks > 0);
+                        if (ks < steps) mma_ts(ot, st + 64 * buf + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), pv_desc, n > n0 || ks > 0);
                     tc_commit(&sh.o_full[g][buf]);
-                    if (buf == 1 || n + 1 == jobs) let_go(slot);
+                    if (buf == 1) let_go(slot);
                 }
                 __syncwarp();
-                if (n + 2 < jobs && !qk(n + 2)) return false;
+                if (n + 2 < end && !qk(n + 2)) return false;
             }
             base += 2 * p.nt;
             ++k;
@@ -368,23 +374,32 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
             // what a logit has to be multiplied by, once shaped, to be in log2 units
             const float ml = MOD && (a.softcap > 0.f || a.slopes) ? 1.f : sl2;
             float m = -INFINITY, l = 0.f;
-            const int jobs = piece_jobs(p, g);
+            const int n0 = first_job(p, g), end = job_end(p, g);
             int kp_min, from = 0, to = 0;  // masks by position, per tile
             bool clean = true, run = true;
-            for (int n = 0; n < jobs; ++n) {
-                const int buf = n & 1, t = p.alt ? 2 * (n >> 1) + g : n >> 1, j0 = (p.tile0 + t) * kTile;
-                if (MOD && by_pos && busy && buf == 0) {  // positions of the tile's keys, while the product runs
-                    const int32_t* pos = a.pos + (size_t)p.it.item * a.cap_tokens + j0;
+            int kp_next[4];  // positions of the next tile's keys, fetched a tile ahead
+            auto fetch_pos = [&](int t) {
+                const int j0 = seq_tile(p, t) * kTile;
+                const int32_t* pos = a.pos + (size_t)p.it.item * a.cap_tokens + j0;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) kp_next[c] = j0 + c * 32 + lane < p.it.n ? pos[c * 32 + lane] : INT32_MAX;
+            };
+            if (MOD && by_pos && busy && n0 < end) fetch_pos(job_seq(p, g, n0));
+            for (int n = n0; n < end; ++n) {
+                const int buf = n & 1, half = 1 - buf, t = job_seq(p, g, n), j0 = seq_tile(p, t) * kTile;
+                if (MOD && by_pos && busy && (buf == 0 || n == n0)) {  // while the product runs
                     kp_min = INT32_MAX;
                     __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const int kp = j0 + c * 32 + lane < p.it.n ? pos[c * 32 + lane] : INT32_MAX;
+                        const int kp = kp_next[c];
                         sh.kpos[warp][c * 32 + lane] = kp;
                         sh.kposf[warp][c * 32 + lane] = (float)((long long)kp - pos0);
                         kp_min = min(kp_min, kp);
                     }
                     __syncwarp();
+                    const int ahead = (n | 1) + 1;
+                    if (ahead < end) fetch_pos(job_seq(p, g, ahead));
                     if (mask_pos) {
                         kp_min = __reduce_min_sync(0xffffffffu, kp_min);
                         const int nn = p.it.n - j0;
@@ -402,9 +417,9 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                             from = 0;
                             int opened = 0;  // keys before the prefix's end
 #pragma unroll
-                            for (int half = kTile / 2; half >= 1; half >>= 1) {
-                                if (sh.kpos[warp][from + half - 1] < lo) from += half;
-                                if (sh.kpos[warp][opened + half - 1] < prefix) opened += half;
+                            for (int by = kTile / 2; by >= 1; by >>= 1) {
+                                if (sh.kpos[warp][from + by - 1] < lo) from += by;
+                                if (sh.kpos[warp][opened + by - 1] < prefix) opened += by;
                             }
                             from += sh.kpos[warp][from] < lo;
                             opened += sh.kpos[warp][opened] < prefix;
@@ -414,12 +429,12 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                 }
                 if (!warp_wait(&sh.s_full[g][buf], buf ? s1++ : s0++, abort_flag, limit)) return false;
                 tc_after();
-                const int seen = p.hi - j0 - 64 * buf;  // keys of this half that the unit sees at all
+                const int seen = p.hi - j0 - 64 * half;  // keys of this half that the unit sees at all
                 if (seen < 64 && (seen <= 0 || (seen & 15))) {
                     // Rows behind the last slot may hold anything, and 0 x NaN is NaN: clear those the product's last step takes in.
                     // Not before the logits are there: they show that the product two jobs back, and with it the ring slot's last
                     // entry, is done (a wait that is a whole turn of the ring early would take the last entry's phase for this one's).
-                    const int e = n_v + v_entry(p, t), r0 = 64 * buf + max(seen, 0), rows = 64 * buf + max(16, (seen + 15) & ~15) - r0;
+                    const int e = n_v + v_entry(p, t), r0 = 64 * half + max(seen, 0), rows = 64 * half + max(16, (seen + 15) & ~15) - r0;
                     if (lone_v(p, t) && !wait_issued(&sh.loaded, e, abort_flag, limit)) return false;
                     if (!warp_wait(&sh.full[e % NS], e / NS, abort_flag, limit)) return false;
                     for (int x = quarter * 32 + lane; x < rows * (D / 8); x += kTile) st_shared_16(chunk_addr(ring + (e % NS) * TILE, r0 + x / (D / 8), x % (D / 8)), make_uint4(0, 0, 0, 0));
@@ -428,7 +443,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                 // NC logits of the thread's row from column c0 of the tile: the whole half, or a quad warp's share of it
                 auto job = [&](auto width) -> bool {
                     constexpr int NC = decltype(width)::value;
-                    const int c0 = 64 * buf + (NC == 64 ? 0 : NC * quarter);
+                    const int c0 = 64 * half + (NC == 64 ? 0 : NC * quarter);
                     const uint32_t s_buf = s_addr + 64 * buf;
                     uint32_t v[NC], pk[32];
                     if (MOD) {
@@ -500,7 +515,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         const float w = grow ? exp2_diff(m, mt) : 1.f;
                         if (grow) m = mt;
                         l *= w;
-                        if (n > 0) {  // the product of the job before may still be adding
+                        if (n > n0) {  // the product of the job before may still be adding
                             if (!warp_wait(&sh.o_full[g][buf ^ 1], (buf ? o0 : o1) - 1, abort_flag, limit)) return false;
                             tc_after();
 #pragma unroll 1
@@ -563,7 +578,8 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
             }
             n_v += 2 * p.nt;
             // ---- the piece's outputs
-            if (jobs > 0 && !warp_wait(&sh.o_full[g][(jobs - 1) & 1], ((jobs - 1) & 1 ? o1 : o0) - 1, abort_flag, limit)) return false;
+            const bool worked = n0 < end;
+            if (worked && !warp_wait(&sh.o_full[g][1], o1 - 1, abort_flag, limit)) return false;  // the last job is a first half, buffer 1
             tc_after();
             const bool whole = p.head && p.tail;
             const size_t part = ((size_t)blockIdx.x * 2 + (p.head ? 1 : 0)) * 2 + (p.alt ? 0 : g);
@@ -580,7 +596,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                 // eight parts [warp][D][16 rows]; then every warp finishes D / 8 columns of all rows
                 if (!warp_wait(&sh.q_done, k, abort_flag, limit)) return false;
                 if (lane < kQuadRows) sh.merge_ml[warp * kQuadRows + lane] = make_float2(m, l);
-                if (jobs > 0) {
+                if (worked) {
 #pragma unroll 1
                     for (int c = 0; c < D; c += 32) {
                         uint32_t o[32];
@@ -630,7 +646,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         if (!warp_wait(&sh.q_done, k, abort_flag, limit)) return false;
                         if (busy) {
                             sh.merge_ml[r] = make_float2(m, l);
-                            if (jobs > 0) {
+                            if (worked) {
 #pragma unroll 1
                                 for (int c = 0; c < D; c += 32) {
                                     uint32_t o[32];

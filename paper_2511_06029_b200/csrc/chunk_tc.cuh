@@ -267,35 +267,68 @@ __device__ __forceinline__ uint32_t chunk_addr(uint32_t tile, int r, int c) {
     return tile + (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
 }
 
-// One box of K or V rows [j0, j0 + 128) by TMA: a contiguous item in one box per 64 elements, a paged one page by page.  Rows past
-// the item's capacity, pages past its last slot and ids outside the pool read as zeros (coordinates outside the map).
+// K or V rows [j0, j0 + 128) by TMA, issued by a converged warp: a contiguous item in one box per 64 elements, a paged one page by
+// page, each lane its own.  Rows past the item's capacity, pages past its last slot and ids outside the pool read as zeros
+// (coordinates outside the map).
 template <int D>
-__device__ __forceinline__ void tma_tile(const ChunkArgs& a, const CUtensorMap* map, int item, int n, int j0, uint32_t dst, unsigned long long* bar, bool* bad) {
-    if (!a.paged) {
-#pragma unroll
-        for (int hf = 0; hf < D / 64; ++hf) tma_3d(dst + hf * kHalfBytes, map, 64 * hf, j0, item, bar);
-        return;
-    }
-    const int pt = a.page_tokens, per_tile = kTile / pt;  // pt is 8 .. 128 and divides 128
-    const int32_t* table = a.page_table + (size_t)item * a.capacity + j0 / pt;
-#pragma unroll 8
-    for (int pg = 0; pg < per_tile; ++pg) {
-        int page = (int)a.n_pages;  // outside the map: zeros
-        if (j0 + pg * pt < n) {
-            page = table[pg];
-            if (page < 0 || page >= a.n_pages) {
-                *bad = true;
-                page = (int)a.n_pages;
-            }
-        }
-#pragma unroll
-        for (int hf = 0; hf < D / 64; ++hf) tma_3d(dst + hf * kHalfBytes + pg * pt * 128, map, 64 * hf, 0, page, bar);
-    }
-}
+struct TileLoader {
+    int window = INT32_MIN, pages;        // page ids of 32 consecutive table entries, one per lane
+    int ahead_at = INT32_MIN, ahead;      // and of the 32 before them, where a piece goes on
+    bool bad = false;
 
-// Sixteen bytes of a bf16 operand row (8 elements) from stored K or V: bf16 as it is, 8-bit floats converted (exact).
+    __device__ __forceinline__ int fetch(const ChunkArgs& a, int item, int n, int at) {
+        const int i = at + (threadIdx.x & 31);
+        if (i < 0 || (long long)i * a.page_tokens >= n) return (int)a.n_pages;  // outside the map: zeros
+        const int page = a.page_table[(size_t)item * a.capacity + i];
+        if (page >= 0 && page < a.n_pages) return page;
+        bad = true;
+        return (int)a.n_pages;
+    }
+    // a new item: nothing kept is of use
+    __device__ __forceinline__ void reset() { window = ahead_at = INT32_MIN; }
+    __device__ __forceinline__ void load(const ChunkArgs& a, const CUtensorMap* map, int item, int n, int j0, uint32_t dst, unsigned long long* bar) {
+        const int lane = threadIdx.x & 31;
+        if (!a.paged) {
+            if (lane < D / 64) tma_3d(dst + lane * kHalfBytes, map, 64 * lane, j0, item, bar);
+            return;
+        }
+        const int pt = a.page_tokens, per_tile = kTile / pt;  // pt is 8 .. 128 and divides 128: 1 .. 16 pages
+        const int first = j0 / pt, want = first & ~31;        // tiles do not lie across windows
+        if (want != window) {
+            if (want == ahead_at) pages = ahead;
+            else pages = fetch(a, item, n, want);
+            window = want;
+            ahead_at = want - 32;                             // tiles come last first
+            ahead = fetch(a, item, n, ahead_at);
+        }
+        const int page = __shfl_sync(0xffffffffu, pages, (first & 31) + (lane & (per_tile - 1)));
+        if (lane < per_tile)
+#pragma unroll
+            for (int hf = 0; hf < D / 64; ++hf) tma_3d(dst + hf * kHalfBytes + lane * pt * 128, map, 64 * hf, 0, page, bar);
+    }
+};
+
+// Eight stored 8-bit floats as bf16 (exact).  The bits go where bf16 has them, sign on top and the exponent's and mantissa's bits
+// joined below, and a multiplication by a power of two moves the exponent's bias over; zeros and subnormals come out right.  That
+// takes five full-rate instructions for two elements; conversion instructions (through f16 and fp32) are fewer but run at a
+// fraction of the rate.  Not for NaN and e5m2's infinities, whose exponent does not fit: `expand8_any`.
 __device__ __forceinline__ uint4 expand8(uint2 w, bool e5m2) {
-    uint32_t h[4];
+    const uint32_t mul = e5m2 ? 0x77807780u : 0x7b807b80u;  // 2^112, 2^120
+    const uint32_t keep = e5m2 ? 0x0fe00fe0u : 0x07f007f0u;
+    const int shift = e5m2 ? 3 : 4;
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t v = __byte_perm(i < 2 ? w.x : w.y, 0u, i & 1 ? 0x3424 : 0x1404);  // each byte on top of its 16 bits
+        const uint32_t x = (v & 0x80008000u) | ((v >> shift) & keep);
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(x), "r"(mul));
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+// Nonzero where a byte of w has the largest exponent (e4m3: is NaN).
+__device__ __forceinline__ uint32_t special_bytes(uint32_t w, bool e5m2) { return ((w & 0x7f7f7f7fu) + (e5m2 ? 0x04040404u : 0x01010101u)) & 0x80808080u; }
+__device__ __noinline__ uint4 expand8_any(uint2 w, bool e5m2) {
+    uint32_t h[4], o[4];
     if (e5m2) {  // an e5m2 byte is the upper byte of the half of the same value
         h[0] = __byte_perm(w.x, 0u, 0x1404); h[1] = __byte_perm(w.x, 0u, 0x3424);
         h[2] = __byte_perm(w.y, 0u, 0x1404); h[3] = __byte_perm(w.y, 0u, 0x3424);
@@ -303,7 +336,6 @@ __device__ __forceinline__ uint4 expand8(uint2 w, bool e5m2) {
         asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi; }" : "=r"(h[0]), "=r"(h[1]) : "r"(w.x));
         asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi; }" : "=r"(h[2]), "=r"(h[3]) : "r"(w.y));
     }
-    uint32_t o[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float lo, hi;
@@ -339,13 +371,30 @@ struct Gather {
     __device__ __forceinline__ void store(const ChunkArgs& a, uint32_t dst, int tid, int half) const {
         constexpr int C = D / 16;
         const bool e5m2 = a.dtype == LETHE_FP8_E5M2;
+        if (a.dtype == LETHE_BF16) {
 #pragma unroll
-        for (int u = 0; u < kByteLoads; ++u) {
-            const int i = tid + u * NT, r = i / C, c = i % C;
-            if (a.dtype == LETHE_BF16) st_shared_16(chunk_addr(dst, r, half * C + c), x[u]);
-            else {
+            for (int u = 0; u < kByteLoads; ++u) {
+                const int i = tid + u * NT;
+                st_shared_16(chunk_addr(dst, i / C, half * C + i % C), x[u]);
+            }
+            return;
+        }
+        uint32_t special = 0;
+#pragma unroll
+        for (int u = 0; u < kByteLoads; ++u) special |= special_bytes(x[u].x, e5m2) | special_bytes(x[u].y, e5m2) | special_bytes(x[u].z, e5m2) | special_bytes(x[u].w, e5m2);
+        if (!special) {
+#pragma unroll
+            for (int u = 0; u < kByteLoads; ++u) {
+                const int i = tid + u * NT, r = i / C, c = i % C;
                 st_shared_16(chunk_addr(dst, r, 2 * c), expand8(make_uint2(x[u].x, x[u].y), e5m2));
                 st_shared_16(chunk_addr(dst, r, 2 * c + 1), expand8(make_uint2(x[u].z, x[u].w), e5m2));
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < kByteLoads; ++u) {
+                const int i = tid + u * NT, r = i / C, c = i % C;
+                st_shared_16(chunk_addr(dst, r, 2 * c), expand8_any(make_uint2(x[u].x, x[u].y), e5m2));
+                st_shared_16(chunk_addr(dst, r, 2 * c + 1), expand8_any(make_uint2(x[u].z, x[u].w), e5m2));
             }
         }
     }
