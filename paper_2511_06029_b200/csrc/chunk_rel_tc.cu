@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     if (MOD) {
                         if (a.softcap > 0.f) {
                             ml = 1.f;
-                            cap_scores<32>(v, cap_in, cap2);
+                            cap_scores<32>(v, cap_in, cap2, j < it.n);
                         }
                         if (a.slopes) {
 #pragma unroll

@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                                 uint32_t w[16];
                                 tmem_ld16(at, w);
                                 tmem_ld_wait();
-                                if (a.softcap > 0.f) cap_scores<16>(w, cap_in, cap2);
+                                if (a.softcap > 0.f) cap_scores<16>(w, cap_in, cap2, valid_row);
                                 if (a.slopes) {
 #pragma unroll
                                     for (int y = 0; y < 16; y += 4) {

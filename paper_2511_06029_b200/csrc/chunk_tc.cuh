@@ -225,9 +225,10 @@ __device__ __forceinline__ float2 exp2_fma(float lo, float hi) {
     return make_float2(lo >= -126.f ? a : 0.f, hi >= -126.f ? b : 0.f);
 }
 
-// softcap * tanh(t) in log2 units (cap2 = softcap * log2(e)) of NC logits, t = v * cap_in.
+// softcap * tanh(t) in log2 units (cap2 = softcap * log2(e)) of NC logits, t = v * cap_in.  `care`: what this lane holds counts (rows
+// that are not there may hold anything, which must not send the warp down the longer path).
 template <int NC>
-__device__ __forceinline__ void cap_scores(uint32_t* v, float cap_in, float cap2) {
+__device__ __forceinline__ void cap_scores(uint32_t* v, float cap_in, float cap2, bool care) {
     const uint64_t in2 = two(cap_in, cap_in), out2 = two(cap2, cap2);
 #pragma unroll
     for (int c = 0; c < NC; c += 16) {
@@ -248,7 +249,7 @@ __device__ __forceinline__ void cap_scores(uint32_t* v, float cap_in, float cap2
             v[c + 2 * y] = __float_as_uint(r.x);
             v[c + 2 * y + 1] = __float_as_uint(r.y);
         }
-        if (__any_sync(0xffffffffu, !(big <= 0.55f))) {  // some are outside the polynomial's range (or NaN, behind the last slot)
+        if (__any_sync(0xffffffffu, care && !(big <= 0.55f))) {  // some are outside the polynomial's range (or NaN, behind the last slot)
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
                 const float2 f = apart(t[y]);
