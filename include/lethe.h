@@ -395,7 +395,8 @@ lethe_status lethe_rotate(lethe_ctx *ctx, const lethe_rotary *rotary, int32_t dt
  * If chunk_start decreases anywhere, leaves [0, n_tokens] or has a T_b above max_chunk, the call does nothing and records
  * LETHE_ERR_INVALID_ARG.  Slots at or beyond len may hold anything.  A NaN or an infinity in a value row that some
  * token of the chunk sees may reach the other tokens of its sequence too.
- * Scratch: 8 bytes per (layer, token, query head), and up to about 80 MB of partial results.
+ * Scratch: 4 bytes per (layer, token, query head), up to about 80 MB of partial results, and for chunks of at most 16
+ * (token, head of a group) rows up to 1 GB of parked logits (64 bytes per slot at most).
  */
 lethe_status lethe_chunk_attend(lethe_ctx *ctx, const lethe_cache *cache, int layer_begin, int layer_end,
                                 const int32_t *chunk_start, int n_tokens, int max_chunk, const void *q,

@@ -1173,6 +1173,11 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     const size_t o_rp = take((size_t)a.n_rel_cta * 2 * 2 * kChunkTile * 4);
     const size_t o_hull = by_pos ? take((size_t)a.n_items * cap_pairs * sizeof(int2)) : 0, o_cost = by_pos ? take((size_t)a.n_items * 4) : 0;
     const size_t o_bounds = by_pos ? take((size_t)a.n_items * a.cap_tiles * sizeof(int2)) : 0;
+    // Short chunks park their logits (at most 16 rows of 4 bytes for each slot), where that is not more than a gigabyte.
+    const int park_pitch = a.cap_tiles * kChunkTile;
+    const size_t park_bytes = (size_t)a.n_items * max_chunk * G * park_pitch * 4;
+    const bool park = !simt && max_chunk * G <= kChunkQuadRows && park_bytes <= ((size_t)1 << 30);
+    const size_t o_park = park ? take(park_bytes) : 0;
     const size_t o_nlse = take((size_t)nl * n_tokens * a.Hq * 4);
     const size_t o_ml = take((size_t)a.n_cta * kChunkParts * kChunkPartRows * sizeof(float2));
     const size_t o_po = take((size_t)a.n_cta * kChunkParts * kChunkPartRows * D * sizeof(float));
@@ -1190,7 +1195,12 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
         a.bounds = (int2*)(base + o_bounds);
     }
     a.cta_unit = (int*)(base + o_cta);
-    if (!simt) {
+    if (park) {
+        a.park = (float*)(base + o_park);
+        a.park_rows = max_chunk * G;
+        a.park_pitch = park_pitch;
+    }
+    if (!simt && !park) {
         a.rel_start = (int*)(base + o_rel);
         a.rel_item = (int*)(base + o_ri);
         a.rel_cut = (int4*)(base + o_cut);
@@ -1219,8 +1229,12 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     } else {
         if (e == cudaSuccess) e = launch_chunk_tc(a, maps, (cudaStream_t)stream);
         if (e == cudaSuccess) e = launch_chunk_combine(a, (cudaStream_t)stream);
-        if (e == cudaSuccess) e = launch_chunk_rel_tc(a, maps, (cudaStream_t)stream);
-        if (e == cudaSuccess) e = launch_chunk_rel_finish(a, (cudaStream_t)stream);
+        if (park) {
+            if (e == cudaSuccess) e = launch_chunk_rel_parked(a, (cudaStream_t)stream);
+        } else {
+            if (e == cudaSuccess) e = launch_chunk_rel_tc(a, maps, (cudaStream_t)stream);
+            if (e == cudaSuccess) e = launch_chunk_rel_finish(a, (cudaStream_t)stream);
+        }
     }
     if (e != cudaSuccess) return cuda_fail(ctx, e, "chunk_attend launch");
     return LETHE_OK;

@@ -5,7 +5,8 @@
 //   range    only for masks by position: the tiles each unit can see, then the plan
 //   attend   softmax attention of the chunk, split evenly over the GPU by the plan
 //   combine  merges what the split left in parts
-//   rel      Eq. 5 for the chunk from the final softmax statistics; len
+//   rel      Eq. 5 for the chunk from the final softmax statistics; len.  Chunks of at most 16 rows (single tokens, drafted tokens):
+//            from the logits that `attend` has parked; longer ones: from a second, transposed product
 //
 // A unit is a block of TU consecutive tokens of one sequence with the G query heads of one KV head (for the tensor-core
 // kernel two tiles of up to 128 rows).  Its cost is the number of 128-key tiles it can see.  The plan lays all units end to
@@ -20,6 +21,7 @@ namespace lethe {
 constexpr int kChunkTile = 128;    // keys per tile of the plan
 constexpr int kChunkParts = 4;     // parts a CTA can leave: (unit begun earlier, unit begun here and continued later) x two row tiles
 constexpr int kChunkPartRows = 128;
+constexpr int kChunkQuadRows = 16; // rows of a short chunk that all softmax warps work on together
 
 struct ChunkPlan {  // head of the call's scratch
     int total;      // tiles of all units
@@ -61,6 +63,8 @@ struct ChunkArgs {
     float* rel_part; // [n_rel_cta][2][256] sums of a pair begun earlier, and of one begun here and continued later
     int n_rel_cta;
     int2* bounds;    // [items][cap_tiles] smallest and largest pos of a key tile (masks by position only, else NULL)
+    float* park;     // [n_items][park_rows][park_pitch] shaped logits in log2 units, -inf where masked (short chunks, else NULL)
+    int park_rows, park_pitch;
     float* nlse2;    // [nl][Hkv][n_tokens][G] minus the log-sum-exp, in log2 units; -inf for a row that sees nothing
     float* part_o;   // [n_cta][kChunkParts][D][kChunkPartRows]: a thread that owns a row writes beside its neighbours
     float2* part_ml; // [n_cta][kChunkParts][kChunkPartRows] (max in log2 units, sum)
@@ -157,16 +161,18 @@ __device__ __forceinline__ int unit_pad(const ChunkArgs& a, int toks) { return t
 // Tiles of a unit that begins at s0 on the line which lie before point x of the line.
 __device__ __forceinline__ int tiles_before(const ChunkArgs& a, int toks, int s0, int x) { return max(0, x - s0 - unit_pad(a, toks)); }
 
-// Query tiles that a pair of key tiles (its first slot j0) meets: [lo, hi).
+// Query tiles that a pair of key tiles (its first slot j0) meets: [lo, hi); none where masks hide it from all.
 __device__ __forceinline__ int2 rel_hull(const ChunkArgs& a, const ChunkItem& it, int idx, int pair) {
     if (a.rel_hull) return a.rel_hull[(size_t)idx * ((a.cap_tiles + 1) / 2) + pair];
     const int lo = a.append ? max(0, pair * 2 * kChunkTile - it.n_old) / a.TT : 0;  // earlier tokens do not reach the pair
     return make_int2(lo, (it.T + a.TT - 1) / a.TT);
 }
+__device__ __forceinline__ int rel_steps(int2 hull) { return max(1, hull.y - hull.x); }  // a pair that nobody sees still decays
 __device__ __forceinline__ int rel_pairs(const ChunkItem& it) { return (it.n + 2 * kChunkTile - 1) / (2 * kChunkTile); }
 
 cudaError_t launch_chunk_append(const ChunkArgs& a, cudaStream_t stream);
 cudaError_t launch_chunk_combine(const ChunkArgs& a, cudaStream_t stream);
+cudaError_t launch_chunk_rel_parked(const ChunkArgs& a, cudaStream_t stream);
 cudaError_t launch_chunk_rel_finish(const ChunkArgs& a, cudaStream_t stream);
 cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t stream);
 

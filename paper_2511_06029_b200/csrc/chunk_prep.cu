@@ -30,76 +30,79 @@ __device__ __forceinline__ int unit_cost(const ChunkArgs& a, int u) {
     return unit_pad(a, T - tok0) + max(1, (hi + kChunkTile - 1) / kChunkTile);  // rows that see nothing still have to be written
 }
 
-// Lays the units end to end: u_start and the plan's totals.  One block.
-__device__ void make_plan(const ChunkArgs& a) {
-    __shared__ int sums[kPrepThreads];
-    const int tid = threadIdx.x;
-    const int seg = (a.n_units + kPrepThreads - 1) / kPrepThreads;
-    const int u0 = min(a.n_units, tid * seg), u1 = min(a.n_units, u0 + seg);
-    int mine = 0;
-    for (int u = u0; u < u1; ++u) mine += unit_cost(a, u);
-    sums[tid] = mine;
-    __syncthreads();
-    for (int off = 1; off < kPrepThreads; off <<= 1) {
-        const int add = tid >= off ? sums[tid - off] : 0;
-        __syncthreads();
-        sums[tid] += add;
-        __syncthreads();
+// Exclusive prefix sum over the block's threads; `total` is the sum.
+__device__ int block_scan(int mine, int* total) {
+    __shared__ int sums[kPrepWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int x = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
     }
-    const int total = sums[kPrepThreads - 1], per = max(a.min_per, (total + a.n_cta - 1) / a.n_cta);
-    int at = sums[tid] - mine;
-    for (int u = u0; u < u1; ++u) {
-        a.u_start[u] = at;
-        const int next = at + unit_cost(a, u);
-        for (int c = (at + per - 1) / per; c * per < next; ++c) a.cta_unit[c] = u;
+    __syncthreads();  // the last call's readers are done
+    if (lane == 31) sums[warp] = x;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kPrepWarps; ++w) {
+        if (w < warp) before += sums[w];
+        all += sums[w];
+    }
+    *total = all;
+    return before + x - mine;
+}
+
+// Lays `n` costs end to end: starts, the whole, equal stretches for `n_cta` CTAs, and for each CTA the entry that its stretch begins in.
+// The whole launch waits for this one block: every cost is computed once, the loads of neighbouring threads side by side, and the
+// loops stay rolled, because code that runs once is paid for by fetching it.
+template <typename Cost>
+__device__ void lay_line(int n, int n_cta, int min_per, int* start, int* cta_entry, int* total_out, int* per_out, Cost cost) {
+    constexpr int kShared = 2048;
+    __shared__ int few[kShared];
+    int* costs = n <= kShared ? few : start;  // long lines keep them where the starts go
+    const int tid = threadIdx.x;
+    __syncthreads();  // the last line's readers are done
+#pragma unroll 1
+    for (int i = tid; i < n; i += kPrepThreads) costs[i] = cost(i);
+    __syncthreads();
+    const int seg = (n + kPrepThreads - 1) / kPrepThreads;
+    const int i0 = min(n, tid * seg), i1 = min(n, i0 + seg);
+    int mine = 0, total;
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) mine += costs[i];
+    int at = block_scan(mine, &total);
+    const int per = max(min_per, (total + n_cta - 1) / n_cta);
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) {
+        const int next = at + costs[i];
+        start[i] = at;
+#pragma unroll 1
+        for (int k = (at + per - 1) / per; k * per < next; ++k) cta_entry[k] = i;
         at = next;
     }
     if (tid == 0) {
-        a.u_start[a.n_units] = total;
-        a.plan->total = total;
-        a.plan->per = per;
+        start[n] = total;
+        *total_out = total;
+        *per_out = per;
     }
+}
+
+// The plan: the units' line for the attention, the items' line for the relevance.  One block.
+__device__ void make_plan(const ChunkArgs& a) {
+    lay_line(a.n_units, a.n_cta, a.min_per, a.u_start, a.cta_unit, &a.plan->total, &a.plan->per, [&](int u) { return unit_cost(a, u); });
     if (!a.rel_start) return;
-    // the relevance kernel's line, item by item
-    const int iseg = (a.n_items + kPrepThreads - 1) / kPrepThreads;
-    const int i0 = min(a.n_items, tid * iseg), i1 = min(a.n_items, i0 + iseg);
-    auto steps = [&](int idx) -> int {
+    lay_line(a.n_items, a.n_rel_cta, 1, a.rel_start, a.rel_item, &a.plan->rel_total, &a.plan->rel_per, [&](int idx) -> int {
         const ChunkItem it = chunk_item(a, idx);
         if (it.n_old < 0 || it.T == 0) return 0;
         if (a.rel_cost) return a.rel_cost[idx];
         const int pairs = rel_pairs(it), tiles = (it.T + a.TT - 1) / a.TT;
         int pr = a.append ? min(pairs, it.n_old / (2 * kChunkTile) + 1) : pairs;  // these meet every query tile
         int sum = pr * tiles;
-        for (; pr < pairs; ++pr) {
-            const int2 h = rel_hull(a, it, idx, pr);
-            sum += h.y - h.x;
-        }
+#pragma unroll 1
+        for (; pr < pairs; ++pr) sum += rel_steps(rel_hull(a, it, idx, pr));
         return sum;
-    };
-    mine = 0;
-    for (int idx = i0; idx < i1; ++idx) mine += steps(idx);
-    __syncthreads();
-    sums[tid] = mine;
-    __syncthreads();
-    for (int off = 1; off < kPrepThreads; off <<= 1) {
-        const int add = tid >= off ? sums[tid - off] : 0;
-        __syncthreads();
-        sums[tid] += add;
-        __syncthreads();
-    }
-    const int rel_total = sums[kPrepThreads - 1], rel_per = max(1, (rel_total + a.n_rel_cta - 1) / a.n_rel_cta);
-    at = sums[tid] - mine;
-    for (int idx = i0; idx < i1; ++idx) {
-        a.rel_start[idx] = at;
-        const int next = at + steps(idx);
-        for (int c = (at + rel_per - 1) / rel_per; c * rel_per < next; ++c) a.rel_item[c] = idx;
-        at = next;
-    }
-    if (tid == 0) {
-        a.rel_start[a.n_items] = rel_total;
-        a.plan->rel_total = rel_total;
-        a.plan->rel_per = rel_per;
-    }
+    });
 }
 
 // Two fp32 values -> two bytes of an 8-bit float, saturating (the low byte is the first).
@@ -313,9 +316,9 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_range_kernel(const __grid_
             }
             first = __reduce_min_sync(0xffffffffu, first);
             end = __reduce_max_sync(0xffffffffu, end);
-            if (end == 0) first = 0, end = 1;  // nobody sees the pair, but its relevance decays
+            if (end == 0) first = 0;  // nobody sees the pair
             if (lane == 0) a.rel_hull[(size_t)blockIdx.x * ((a.cap_tiles + 1) / 2) + pr] = make_int2(first, end);
-            mine += end - first;
+            mine += rel_steps(make_int2(first, end));
         }
         if (lane == 0) atomicAdd(&cost, mine);  // whole numbers: any order
         __syncthreads();
@@ -402,6 +405,46 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
     }
 }
 
+// Eq. 5 from parked logits: a thread takes four keys, adds up exp2(logit - lse + log2 of the row's decay weight) over the chunk's rows.
+// Bound by memory: 4 bytes per row and key read, against 2 D of the key itself for the transposed product.
+constexpr int kParkKeys = 4 * kPrepThreads;
+__global__ void __launch_bounds__(kPrepThreads) chunk_rel_parked_kernel(const __grid_constant__ ChunkArgs a) {
+    __shared__ float bias[kChunkQuadRows];
+    dependency_wait();
+    dependency_release();
+    const int per_item = (a.cap_tokens + kParkKeys - 1) / kParkKeys;
+    const int idx = blockIdx.x / per_item, block = blockIdx.x - idx * per_item;
+    const ChunkItem it = chunk_item(a, idx);
+    if (it.n_old < 0 || it.T == 0 || block * kParkKeys >= it.n) return;
+    const int tid = threadIdx.x, rows = it.T * a.G;
+    if (block == 0 && tid == 0 && a.append) a.len[it.item] = it.n;
+    if (tid < rows) bias[tid] = a.nlse2[(((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G + tid] + (float)(it.T - 1 - tid / a.G) * a.gamma_log2;
+    // what the attention has gone through, and so written: one unit per item
+    const int lo = a.u_hi ? a.u_lo[idx] * kChunkTile : 0, hi = a.u_hi ? a.u_hi[idx] : it.n;
+    const int j0 = block * kParkKeys + 4 * tid;
+    float* rel = a.rel + (size_t)it.item * a.cap_tokens + j0;
+    float old[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) old[k] = j0 + k < it.n_old ? rel[k] : 0.f;
+    __syncthreads();
+    if (j0 < hi && j0 + 4 > lo) {  // lo is a multiple of four; keys from hi on are -inf or left out below
+        const float* src = a.park + (size_t)idx * a.park_rows * a.park_pitch + j0;
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+            const float4 x = *reinterpret_cast<const float4*>(src + (size_t)r * a.park_pitch);
+            const float b = bias[r];
+            if (x.x != -INFINITY) sum[0] += fast_exp2(x.x + b);
+            if (x.y != -INFINITY) sum[1] += fast_exp2(x.y + b);
+            if (x.z != -INFINITY) sum[2] += fast_exp2(x.z + b);
+            if (x.w != -INFINITY) sum[3] += fast_exp2(x.w + b);
+        }
+    }
+    const float decay = exp2f((float)it.T * a.gamma_log2);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (j0 + k < it.n) rel[k] = fmaf(decay, old[k], j0 + k < hi ? sum[k] : 0.f);
+}
+
 // Pairs of key tiles that more than one CTA of the relevance kernel worked on: the parts are added in the order of their tokens.
 // One block per CTA whose stretch begins inside a pair, the pair's first such CTA speaks for it.
 __global__ void __launch_bounds__(kPrepThreads) chunk_rel_finish_kernel(const __grid_constant__ ChunkArgs a) {
@@ -422,6 +465,11 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_rel_finish_kernel(const __
 }
 
 }  // namespace
+
+cudaError_t launch_chunk_rel_parked(const ChunkArgs& a, cudaStream_t stream) {
+    const int per_item = (a.cap_tokens + kParkKeys - 1) / kParkKeys;
+    return launch_dependent(chunk_rel_parked_kernel, dim3(per_item * a.n_items), kPrepThreads, 0, stream, a);
+}
 
 cudaError_t launch_chunk_rel_finish(const ChunkArgs& a, cudaStream_t stream) {
     static_assert(kPrepThreads == 2 * kChunkTile, "one thread per key of a pair");

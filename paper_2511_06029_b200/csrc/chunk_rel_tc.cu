@@ -72,12 +72,12 @@ __device__ __forceinline__ void for_rel_pieces(const ChunkArgs& a, F f) {
             continue;
         }
         const int2 h = rel_hull(a, p.it, p.idx, p.pair);
-        p.s1 = p.s0 + h.y - h.x;
+        p.s1 = p.s0 + rel_steps(h);
         if (p.s1 > at) {
             const int stop = min(end, p.s1);
             p.j0 = p.pair * 2 * kTile;
             p.qa = h.x + at - p.s0;
-            p.qb = h.x + stop - p.s0;
+            p.qb = min(h.y, h.x + stop - p.s0);  // qb <= qa: nobody sees the pair
             p.head = at == p.s0;
             p.tail = stop == p.s1;
             if (!f(p)) return;
@@ -131,6 +131,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
         TileLoader<D> loader;  // bad pages: the attention has recorded them
         int k = 0, qn = 0;
         for_rel_pieces(a, [&](const RelPiece& p) {
+            if (p.qb <= p.qa) return true;
             if (TMA) {
                 if (k > 0 && !warp_wait(&sh.k_empty, k - 1, abort_flag, limit)) return false;
                 const int tiles = p.j0 + kTile < p.it.n ? 2 : 1;
@@ -161,6 +162,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
         int k = 0, qn = 0;
         int ns[2] = {0, 0};
         for_rel_pieces(a, [&](const RelPiece& p) {
+            if (p.qb <= p.qa) return true;
             const int tiles = p.j0 + kTile < p.it.n ? 2 : 1;
             const uint32_t desc = mma_idesc(kTile, false, a.scale[p.it.l] < 0.f);
             if (!warp_wait(&sh.k_full, k++, abort_flag, limit)) return false;
@@ -204,6 +206,12 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
         for_rel_pieces(a, [&](const RelPiece& p) {
             const ChunkItem& it = p.it;
             const int j0 = p.j0, j = j0 + g * kTile + r;  // this thread's key
+            if (p.qb <= p.qa) {  // only the decay
+                float* rel = a.rel + (size_t)it.item * a.cap_tokens + j;
+                if (j < it.n) *rel = j < it.n_old ? exp2f((float)it.T * a.gamma_log2) * *rel : 0.f;
+                if (j0 == 0 && tid == 0 && a.append) a.len[it.item] = it.n;
+                return true;
+            }
             if (!TMA) {
                 bool bad = false;
                 if (k > 0 && !warp_wait(&sh.k_empty, k - 1, abort_flag, limit)) return false;

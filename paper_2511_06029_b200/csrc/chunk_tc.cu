@@ -33,7 +33,7 @@ constexpr int kQWarp = 10;
 constexpr int kLoadWarp = 11;    // TMA
 constexpr int kGatherWarp = 11;  // four warps
 constexpr int kMaxStages = 8;
-constexpr int kQuadRows = 16;
+constexpr int kQuadRows = kChunkQuadRows;
 constexpr int kFmaShare = 2;  // of eight exponentials, computed by polynomial
 constexpr float kLazy = 8.f;  // log2 of the growth of a row maximum that is left standing
 
@@ -67,6 +67,7 @@ struct Width {
 // A CTA's piece of a unit, as every role derives it from the plan.
 struct Piece {
     ChunkItem it;
+    int idx;         // item of the call
     int tok0, toks;  // tokens of the unit
     int tile0, nt;   // key tiles
     int hi;          // slots from here on are hidden from the whole unit
@@ -77,9 +78,9 @@ struct Piece {
 
 __device__ __forceinline__ Piece piece_of(const ChunkArgs& a, int u, int at, int stop, int s0, int s1) {
     Piece p;
-    const int idx = u / a.QT;
-    p.tok0 = (u - idx * a.QT) * a.TU;
-    p.it = chunk_item(a, idx);
+    p.idx = u / a.QT;
+    p.tok0 = (u - p.idx * a.QT) * a.TU;
+    p.it = chunk_item(a, p.idx);
     p.toks = min(p.it.T - p.tok0, a.TU);
     p.hi = a.u_hi ? a.u_hi[u] : (a.append ? p.it.n_old + p.tok0 + p.toks : p.it.n_old);
     const int before = tiles_before(a, p.toks, s0, at);
@@ -502,6 +503,12 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                             for (int c = 0; c < NC; ++c)
                                 if (c >= nv) v[c] = 0xff800000u;
                         }
+                    }
+                    if (NC == 16 && a.park && valid_row) {
+                        float4* d = reinterpret_cast<float4*>(a.park + ((size_t)p.idx * a.park_rows + r) * a.park_pitch + j0 + c0);
+#pragma unroll
+                        for (int y = 0; y < 16; y += 4)
+                            d[y / 4] = make_float4(__uint_as_float(v[y]) * ml, __uint_as_float(v[y + 1]) * ml, __uint_as_float(v[y + 2]) * ml, __uint_as_float(v[y + 3]) * ml);
                     }
                     float m0 = __uint_as_float(v[0]), m1 = __uint_as_float(v[1]);
 #pragma unroll
