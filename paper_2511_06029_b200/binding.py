@@ -202,10 +202,8 @@ class Rotary:
         self.pair_freq = (ctypes.c_double * n)(*[float(x) for x in pair_freq])
         self.c = lethe_rotary(2 * n, int(style), axis_pos.shape[0], ctypes.cast(self.pair_axis, ctypes.POINTER(ctypes.c_int32)),
                               ctypes.cast(self.pair_freq, ctypes.POINTER(ctypes.c_double)), axis_pos.data_ptr())
-
-    @property
-    def n_tokens(self) -> int:
-        return self.axis_pos.shape[1]
+        self.ref = ctypes.byref(self.c)
+        self.n_tokens = axis_pos.shape[1]
 
 
 def rasr_prune_static(cache: "Cache", budgets: torch.Tensor, recent: int, sink: int,
@@ -343,15 +341,19 @@ class Context:
                k_out: Optional[torch.Tensor], inverse: bool = False):
         """q [nl][n_tokens][Hq][D] and k [nl][n_tokens][Hkv][D] (or None), float32 or bfloat16, into q_out, k_out (which may be
         q, k themselves)."""
-        for x, y in ((q, q_out), (k, k_out)):
-            assert (x is None) == (y is None)
-            assert x is None or (x.is_cuda and y.is_cuda and x.is_contiguous() and y.is_contiguous() and x.dim() == 4 and x.shape == y.shape)
-            assert x is None or (x.dtype == y.dtype == q.dtype and x.shape[:2] == q.shape[:2] and x.shape[3] == q.shape[3])
-        assert rotary.n_tokens == q.shape[1]
-        dt = {torch.float32: F32, torch.bfloat16: BF16}[q.dtype]
-        self._check(self.lib.lethe_rotate(self.h, ctypes.byref(rotary.c), dt, q.shape[3], q.shape[0], q.shape[1], q.shape[2],
-                                          0 if k is None else k.shape[2], _dp(q), _dp(k), int(bool(inverse)), _dp(q_out),
-                                          _dp(k_out), _stream(self.device)))
+        shape, dt = q.shape, q.dtype
+        assert q.is_cuda and q_out.is_cuda and q.is_contiguous() and q_out.is_contiguous() and q_out.shape == shape and q_out.dtype == dt
+        nl, n, hq, d = shape
+        assert rotary.n_tokens == n and (k is None) == (k_out is None)
+        hkv, kp, ko = 0, None, None
+        if k is not None:
+            ks = k.shape
+            assert k.is_cuda and k_out.is_cuda and k.is_contiguous() and k_out.is_contiguous() and k_out.shape == ks and k.dtype == k_out.dtype == dt
+            assert ks[0] == nl and ks[1] == n and ks[3] == d
+            hkv, kp, ko = ks[2], k.data_ptr(), k_out.data_ptr()
+        code = F32 if dt == torch.float32 else BF16 if dt == torch.bfloat16 else -1
+        self._check(self.lib.lethe_rotate(self.h, rotary.ref, code, d, nl, n, hq, hkv, q.data_ptr(), kp, 1 if inverse else 0, q_out.data_ptr(), ko,
+                                          torch.cuda.current_stream(self.device).cuda_stream))
 
     def chunk_attend(self, cache: Cache, layer_begin: int, layer_end: int, chunk_start: torch.Tensor, max_chunk: int, q, k_new,
                      v_new, token_pos, scale, gamma, out, lse=None, mod: Optional[ScoreMod] = None,

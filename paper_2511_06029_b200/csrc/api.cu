@@ -1042,9 +1042,14 @@ static lethe_status rotary_args(lethe_ctx* ctx, const lethe_rotary* r, int32_t d
         if (r->pair_axis[p] < 0 || r->pair_axis[p] >= r->n_axes) return fail(ctx, LETHE_ERR_INVALID_ARG, "pair_axis out of range");
         const double f = r->pair_freq[p];
         if (!(fabs(f) <= 6.2831853071795865)) return fail(ctx, LETHE_ERR_INVALID_ARG, "pair_freq must be at most one turn (2 pi) per position");
-        long double turns = (long double)f / 6.283185307179586476925286766559L;
-        turns -= floorl(turns);
-        a->turn[p] = turns >= 1.0L ? 0 : (unsigned long long)ldexpl(turns, 64);
+        // f / (2 pi) as a fraction of 2^64: the double's 53-bit whole number times 2^66 / (2 pi), shifted into place (whole numbers
+        // keep all 64 bits and are ten times as fast as extended precision, which shows in a call of a few microseconds)
+        int ex;
+        const long long m = (long long)ldexp(frexp(fabs(f), &ex), 53);
+        const unsigned __int128 prod = (unsigned __int128)(unsigned long long)m * 0xa2f9836e4e44152aULL;
+        const int down = 2 - (ex - 53);
+        const unsigned long long turn = down < 128 ? (unsigned long long)(prod >> down) : 0;
+        a->turn[p] = f < 0 ? 0 - turn : turn;
         a->axis[p] = (unsigned char)r->pair_axis[p];
     }
     a->axis_pos = r->axis_pos;
@@ -1147,13 +1152,14 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     a.TT = (simt ? 64 : kChunkTile) / G;
     a.TU = simt ? a.TT : 2 * a.TT;
     a.n_cta = simt ? 2 * ctx->sm_count : ctx->sm_count;
-    a.min_per = simt ? 1 : 2;  // both softmax groups of a CTA have something to do
+    a.min_per = simt ? 3 : 2;  // every part costs its merge; and both softmax groups of a CTA have something to do
     a.QT = (max_chunk + a.TU - 1) / a.TU;
     // Beginning and ending a unit with two row tiles costs as much as about three of its tiles (8192-token prompt: 970 us with 3,
     // 1036 with 1, 1080 with none; documents 654 / 658 / 664), about one where the scores are capped (528 / 520 / 515 us), nothing beside
     // tiles that threads convert (218 / 211 / 208).
     a.pad = simt || c->dtype != LETHE_BF16 ? 0 : a.softcap > 0.f ? 1 : 3;
-    a.cap_tiles = (a.cap_tokens + kChunkTile - 1) / kChunkTile;
+    a.tile = simt ? 32 : kChunkTile;
+    a.cap_tiles = (a.cap_tokens + a.tile - 1) / a.tile;
     const long long units = (long long)a.n_items * a.QT;
     if (units > 0x7fffffffLL / 4 || units * (a.cap_tiles + a.pad) > 0x7fffffffLL || units * a.cap_tiles * 2 > 0x7fffffffLL || (long long)a.n_items * a.cap_tiles * 2 > 0x7fffffffLL)
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "chunk: too many (layer, sequence, head, block) units for one call; cover fewer layers");
@@ -1174,7 +1180,7 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     const size_t o_hull = by_pos ? take((size_t)a.n_items * cap_pairs * sizeof(int2)) : 0, o_cost = by_pos ? take((size_t)a.n_items * 4) : 0;
     const size_t o_bounds = by_pos ? take((size_t)a.n_items * a.cap_tiles * sizeof(int2)) : 0;
     // Short chunks park their logits (at most 16 rows of 4 bytes for each slot), where that is not more than a gigabyte.
-    const int park_pitch = a.cap_tiles * kChunkTile;
+    const int park_pitch = a.cap_tiles * a.tile;
     const size_t park_bytes = (size_t)a.n_items * max_chunk * G * park_pitch * 4;
     const bool park = !simt && max_chunk * G <= kChunkQuadRows && park_bytes <= ((size_t)1 << 30);
     const size_t o_park = park ? take(park_bytes) : 0;

@@ -18,7 +18,7 @@
 
 namespace lethe {
 
-constexpr int kChunkTile = 128;    // keys per tile of the plan
+constexpr int kChunkTile = 128;    // keys per tile of the tensor-core kernels
 constexpr int kChunkParts = 4;     // parts a CTA can leave: (unit begun earlier, unit begun here and continued later) x two row tiles
 constexpr int kChunkPartRows = 128;
 constexpr int kChunkQuadRows = 16; // rows of a short chunk that all softmax warps work on together
@@ -75,6 +75,7 @@ struct ChunkArgs {
     int TT;          // tokens per row tile
     int TU;          // tokens per unit
     int QT;          // units per item
+    int tile;        // keys per tile of the plan: 128 for the tensor cores, fewer for the CUDA cores
     int n_units, n_cta, cap_tiles, min_per;
     int pad;         // tiles' worth of time that beginning and ending a unit takes (unit_pad), laid on the line before its tiles
     int append;

@@ -6,6 +6,8 @@ namespace {
 
 constexpr int kPrepThreads = 256;
 constexpr int kPrepWarps = kPrepThreads / 32;
+constexpr int kRangeThreads = 1024;  // one block per item: its tiles, units and pairs are gone through by warps
+constexpr int kRangeWarps = kRangeThreads / 32;
 constexpr int kSeqShared = 1024;  // chunk_start entries kept in shared memory (longer batches read it from global memory)
 
 // Whether chunk_start never decreases, stays inside [0, n_tokens] and has no sequence above max_chunk; uniform for the block.
@@ -25,15 +27,15 @@ __device__ __forceinline__ int unit_cost(const ChunkArgs& a, int u) {
     const int b = (idx / a.Hkv) % a.B;
     const int T = a.chunk_start[b + 1] - a.chunk_start[b], tok0 = qt * a.TU;
     if (tok0 >= T) return 0;
-    if (a.u_hi) return unit_pad(a, T - tok0) + max(1, (a.u_hi[u] + kChunkTile - 1) / kChunkTile - a.u_lo[u]);
+    if (a.u_hi) return unit_pad(a, T - tok0) + max(1, (a.u_hi[u] + a.tile - 1) / a.tile - a.u_lo[u]);
     const int hi = a.append ? n_old + min(T, tok0 + a.TU) : n_old;
-    return unit_pad(a, T - tok0) + max(1, (hi + kChunkTile - 1) / kChunkTile);  // rows that see nothing still have to be written
+    return unit_pad(a, T - tok0) + max(1, (hi + a.tile - 1) / a.tile);  // rows that see nothing still have to be written
 }
 
 // Exclusive prefix sum over the block's threads; `total` is the sum.
 __device__ int block_scan(int mine, int* total) {
-    __shared__ int sums[kPrepWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ int sums[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     int x = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -43,14 +45,9 @@ __device__ int block_scan(int mine, int* total) {
     __syncthreads();  // the last call's readers are done
     if (lane == 31) sums[warp] = x;
     __syncthreads();
-    int before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < kPrepWarps; ++w) {
-        if (w < warp) before += sums[w];
-        all += sums[w];
-    }
-    *total = all;
-    return before + x - mine;
+    const int of_warp = lane < warps ? sums[lane] : 0;
+    *total = __reduce_add_sync(0xffffffffu, of_warp);
+    return __reduce_add_sync(0xffffffffu, lane < warp ? of_warp : 0) + x - mine;
 }
 
 // Lays `n` costs end to end: starts, the whole, equal stretches for `n_cta` CTAs, and for each CTA the entry that its stretch begins in.
@@ -64,9 +61,9 @@ __device__ void lay_line(int n, int n_cta, int min_per, int* start, int* cta_ent
     const int tid = threadIdx.x;
     __syncthreads();  // the last line's readers are done
 #pragma unroll 1
-    for (int i = tid; i < n; i += kPrepThreads) costs[i] = cost(i);
+    for (int i = tid; i < n; i += (int)blockDim.x) costs[i] = cost(i);
     __syncthreads();
-    const int seg = (n + kPrepThreads - 1) / kPrepThreads;
+    const int seg = (n + (int)blockDim.x - 1) / (int)blockDim.x;
     const int i0 = min(n, tid * seg), i1 = min(n, i0 + seg);
     int mine = 0, total;
 #pragma unroll 1
@@ -237,22 +234,22 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_append_kernel(const __grid
 // Masks by position.  A block takes one item: the smallest and largest position of each of its key tiles, then for each unit the
 // first tile with a key that its farthest-reaching token may still see and the end of what the prefix opens.  Conservative
 // whatever the order of the positions is; the attention tests every key that is left.  The last block to finish plans.
-__global__ void __launch_bounds__(kPrepThreads) chunk_range_kernel(const __grid_constant__ ChunkArgs a) {
+__global__ void __launch_bounds__(kRangeThreads) chunk_range_kernel(const __grid_constant__ ChunkArgs a) {
     __shared__ int last;
     dependency_wait();
     dependency_release();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const ChunkItem it = chunk_item(a, blockIdx.x);
     if (it.n_old >= 0 && it.T > 0) {
-        const int tiles = (it.n + kChunkTile - 1) / kChunkTile;
+        const int tiles = (it.n + a.tile - 1) / a.tile;
         int2* bounds = a.bounds + (size_t)blockIdx.x * a.cap_tiles;
         const int32_t* pos = a.pos + (size_t)it.item * a.cap_tokens;
-        for (int t = warp; t < tiles; t += kPrepWarps) {
+        for (int t = warp; t < tiles; t += kRangeWarps) {
             int mn = INT32_MAX, mx = INT32_MIN;
 #pragma unroll
             for (int i = 0; i < kChunkTile / 32; ++i) {
-                const int j = t * kChunkTile + i * 32 + lane;
-                if (j < it.n) {
+                const int j = t * a.tile + i * 32 + lane;
+                if (j < it.n && i * 32 < a.tile) {
                     const int p = pos[j];
                     mn = min(mn, p);
                     mx = max(mx, p);
@@ -264,7 +261,7 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_range_kernel(const __grid_
         }
         __syncthreads();
         const int units = (it.T + a.TU - 1) / a.TU;
-        for (int qt = warp; qt < units; qt += kPrepWarps) {
+        for (int qt = warp; qt < units; qt += kRangeWarps) {
             const int tok0 = qt * a.TU, tok1 = min(it.T, tok0 + a.TU);
             int lo = INT32_MAX;
             for (int i = tok0 + lane; i < tok1; i += 32) lo = min(lo, chunk_lo(a, it.first + i, a.window > 0 ? a.token_pos[it.first + i] : 0));
@@ -284,12 +281,12 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_range_kernel(const __grid_
                 for (int t0 = (tiles - 1) & ~31; t0 >= 0; t0 -= 32) {
                     const unsigned hit = __ballot_sync(0xffffffffu, t0 + lane < tiles && bounds[t0 + lane].x < prefix);
                     if (hit) {
-                        hi = max(hi, min(it.n, (t0 + 32 - __clz(hit)) * kChunkTile));
+                        hi = max(hi, min(it.n, (t0 + 32 - __clz(hit)) * a.tile));
                         break;
                     }
                 }
             }
-            if (!found || t_lo * kChunkTile >= hi) t_lo = 0, hi = 0;
+            if (!found || t_lo * a.tile >= hi) t_lo = 0, hi = 0;
             if (lane == 0) {
                 a.u_lo[blockIdx.x * a.QT + qt] = t_lo;
                 a.u_hi[blockIdx.x * a.QT + qt] = hi;
@@ -304,7 +301,7 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_range_kernel(const __grid_
         __syncthreads();
         const int pairs = rel_pairs(it), tiles = (it.T + a.TT - 1) / a.TT;
         int mine = 0;
-        for (int pr = warp; pr < pairs; pr += kPrepWarps) {
+        for (int pr = warp; pr < pairs; pr += kRangeWarps) {
             const int j0 = pr * 2 * kChunkTile;
             int first = INT32_MAX, end = 0;
             for (int qt = lane; qt < tiles; qt += 32) {
@@ -352,9 +349,8 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
     const int idx = u / a.QT, tok0 = (u - idx * a.QT) * a.TU;
     const ChunkItem it = chunk_item(a, idx);
     const int toks = min(it.T - tok0, a.TU), rows = toks * a.G;
-    int with_tiles = 0;
-    for (int c = c0; c <= c1 && with_tiles < 2; ++c) with_tiles += tiles_before(a, toks, s0, min(s1, (c + 1) * per)) > tiles_before(a, toks, s0, max(s0, c * per));
-    if (with_tiles < 2) return;  // one CTA had all of its tiles and has written the outputs
+    const int cf = (s0 + unit_pad(a, toks)) / per;  // the first CTA that has some of its tiles; all after it have
+    if (cf == c1) return;                            // one CTA had all of its tiles and has written the outputs
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     // row blocks do not lie across row tiles: a tile has TT * G <= 128 rows, four blocks
     const int tile_idx = row0 / kChunkPartRows, r = row0 % kChunkPartRows + x;
@@ -365,10 +361,9 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
     if (ok) {
-        for (int c = c0; c <= c1; ++c) {
-            const int before = tiles_before(a, toks, s0, max(s0, c * per));
-            if (before == tiles_before(a, toks, s0, min(s1, (c + 1) * per))) continue;  // only the unit's pad lies in this CTA
-            const size_t p = (size_t)(c * 2 + (before == 0 ? 1 : 0)) * 2 + tile_idx;
+#pragma unroll 1
+        for (int c = cf; c <= c1; ++c) {  // rolled: code that runs once is paid for by fetching it
+            const size_t p = (size_t)(c * 2 + (c == cf ? 1 : 0)) * 2 + tile_idx;  // begun in cf, earlier in the rest
             const float2 ml = a.part_ml[p * kChunkPartRows + r];
             const float* src = a.part_o + (p * a.D + y) * kChunkPartRows + r;
             float v[E];
@@ -482,7 +477,7 @@ cudaError_t launch_chunk_append(const ChunkArgs& a, cudaStream_t stream) {
     const long long want = (rows + 4 * kPrepWarps - 1) / (4 * kPrepWarps);
     const int blocks = 1 + (int)(want < 2368 ? want : 2368);
     cudaError_t e = launch_dependent(chunk_append_kernel, dim3(blocks), kPrepThreads, 0, stream, a);
-    if (e == cudaSuccess && a.u_hi) e = launch_dependent(chunk_range_kernel, dim3(a.n_items), kPrepThreads, 0, stream, a);
+    if (e == cudaSuccess && a.u_hi) e = launch_dependent(chunk_range_kernel, dim3(a.n_items), kRangeThreads, 0, stream, a);
     return e;
 }
 

@@ -316,14 +316,16 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                 if (j >= it.n) to = 0;
                 if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
                 tc_after();
-                // rolled where scores are shaped: unrolled, the code outgrows the instruction cache
+                // in narrow pieces and rolled where scores are shaped: unrolled, the code outgrows the instruction cache, and 32 columns spill
+                constexpr int W = MOD ? 16 : 32;
 #pragma unroll (MOD ? 1 : 4)
-                for (int ch = 0; ch < kTile; ch += 32) {
+                for (int ch = 0; ch < kTile; ch += W) {
                     if (ch >= cols) break;  // a short chunk leaves most columns empty
-                    uint32_t v[32];
-                    tmem_ld32(s_addr + ch, v);
+                    uint32_t v[W];
+                    if (W == 32) tmem_ld32(s_addr + ch, v);
+                    else tmem_ld16(s_addr + ch, v);
                     tmem_ld_wait();
-                    if (ch + 32 >= cols) {
+                    if (ch + W >= cols) {
                         tc_before();
                         __syncwarp();
                         if (lane == 0) bar_arrive(&sh.s_empty[g]);
@@ -332,11 +334,11 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     if (MOD) {
                         if (a.softcap > 0.f) {
                             ml = 1.f;
-                            cap_scores<32>(v, cap_in, cap2, j < it.n);
+                            cap_scores<W>(v, cap_in, cap2, j < it.n);
                         }
                         if (a.slopes) {
 #pragma unroll
-                            for (int c = 0; c < 32; c += 4) {
+                            for (int c = 0; c < W; c += 4) {
                                 const float4 qp = *reinterpret_cast<const float4*>(&sh.qpos[warp][ch + c]), sl = *reinterpret_cast<const float4*>(&sh.slope[warp][ch + c]);
                                 v[c] = __float_as_uint(fmaf(-sl.x, fabsf(qp.x - kf), __uint_as_float(v[c]) * ml));
                                 v[c + 1] = __float_as_uint(fmaf(-sl.y, fabsf(qp.y - kf), __uint_as_float(v[c + 1]) * ml));
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     if (clean) {
                         const uint64_t ml2 = two(ml, ml);
 #pragma unroll
-                        for (int c = 0; c < 32; c += 8) {
+                        for (int c = 0; c < W; c += 8) {
                             const float4 b0 = b4[c / 4], b1 = b4[c / 4 + 1];
                             const uint64_t bias[4] = {two(b0.x, b0.y), two(b0.z, b0.w), two(b1.x, b1.y), two(b1.z, b1.w)};
 #pragma unroll
@@ -361,10 +363,10 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                             }
                         }
                     } else if (run) {
-                        if (__any_sync(0xffffffffu, from < ch + 32 && to > ch)) {
+                        if (__any_sync(0xffffffffu, from < ch + W && to > ch)) {
                             const int c0 = from - ch, c1 = to - ch;
 #pragma unroll
-                            for (int c = 0; c < 32; c += 4) {
+                            for (int c = 0; c < W; c += 4) {
                                 const float4 b = b4[c / 4];
                                 const float e0 = fast_exp2(fmaf(__uint_as_float(v[c]), ml, b.x)), e1 = fast_exp2(fmaf(__uint_as_float(v[c + 1]), ml, b.y));
                                 const float e2 = fast_exp2(fmaf(__uint_as_float(v[c + 2]), ml, b.z)), e3 = fast_exp2(fmaf(__uint_as_float(v[c + 3]), ml, b.w));
@@ -376,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                         }
                     } else if (MOD) {  // documents that do not grow with the tokens: every column by itself
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) {
+                        for (int c = 0; c < W; ++c) {
                             const float e = fast_exp2(fmaf(__uint_as_float(v[c]), ml, sh.bias[warp][ch + c]));
                             if (j < it.n && ch + c >= from && ch + c < cols && kp >= sh.lo[warp][ch + c]) acc0 += e;
                         }

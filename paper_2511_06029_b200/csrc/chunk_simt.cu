@@ -2,6 +2,7 @@
 // FMA rate: 64 query rows by 32 keys per step, operands in shared memory, 4 x 2 logits and 4 x D / 16 outputs per thread, so that
 // a 16-byte shared-memory read feeds 5 to 8 FMAs per operand.
 #include "chunk.cuh"
+#include "mma_utils.cuh"
 
 namespace lethe {
 namespace {
@@ -11,18 +12,27 @@ constexpr int kRows = 64;   // query rows of a unit
 constexpr int kKeys = 32;   // keys per step
 constexpr int kPad = 4;     // row padding of the staged tiles: rows start in different banks
 
-// Rows [j0, j0 + count) of K or V of an item into shared memory, missing rows (at or beyond `end`, or on a page outside the pool) as zeros.
+// Rows [j0, j0 + count) of K or V of an item on their way into shared memory, missing rows (at or beyond `end`, or on a page outside
+// the pool) as zeros.
 template <int D>
 __device__ __forceinline__ void stage_rows(const ChunkArgs& a, const void* base, int item, int j0, int end, int count, float* dst, bool* bad) {
     for (int i = threadIdx.x; i < count * (D / 4); i += kSimtThreads) {
         const int r = i / (D / 4), c = i % (D / 4);
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        long long at = -1;
         if (j0 + r < end) {
-            const long long at = chunk_row(a, item, j0 + r);
+            at = chunk_row(a, item, j0 + r);
             if (at < 0) *bad = true;
-            else x = reinterpret_cast<const float4*>((const float*)base + (size_t)at * D)[c];
         }
-        *reinterpret_cast<float4*>(dst + r * (D + kPad) + c * 4) = x;
+        cp_async16(smem_u32(dst + r * (D + kPad) + c * 4), (const float*)base + (size_t)max(at, 0LL) * D + c * 4, at >= 0 ? 16 : 0);
+    }
+}
+// The same of query rows [r0, r0 + count) of a sequence's packed tokens, from token `tok`.
+template <int D>
+__device__ __forceinline__ void stage_queries(const ChunkArgs& a, const ChunkItem& it, int tok, int r0, int rows, int count, float* dst) {
+    for (int i = threadIdx.x; i < count * (D / 4); i += kSimtThreads) {
+        const int r = r0 + i / (D / 4), c = i % (D / 4), rr = min(r, rows - 1);
+        const float* src = (const float*)a.q + (((size_t)it.li * a.n_tokens + it.first + tok + rr / a.G) * a.Hq + it.hkv * a.G + rr % a.G) * D + c * 4;
+        cp_async16(smem_u32(dst + (i / (D / 4)) * (D + kPad) + c * 4), src, r < rows ? 16 : 0);
     }
 }
 
@@ -40,9 +50,8 @@ template <int D>
 __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_constant__ ChunkArgs a) {
     extern __shared__ __align__(16) float smem[];
     float* sq = smem;                        // [kRows][D + kPad]
-    float* sk = sq + kRows * (D + kPad);     // [kKeys][D + kPad]
-    float* sv = sk + kKeys * (D + kPad);
-    float* sp = sv + kKeys * (D + kPad);     // [kRows][kKeys + 1] probabilities
+    float* skv = sq + kRows * (D + kPad);    // two stages of K [kKeys][D + kPad] and V
+    float* sp = skv + 4 * kKeys * (D + kPad);  // [kRows][kKeys + 1] probabilities
     dependency_wait();
     dependency_release();
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;  // thread: rows 4 ty .. + 3; keys tx, tx + 16; elements 4 tx + 64 i
@@ -63,13 +72,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
         const int32_t* pos = a.pos + (size_t)it.item * a.cap_tokens;
         const bool by_pos = a.slopes || a.window || a.doc_start || a.prefix_len;
         __syncthreads();  // the previous unit's readers are done
-        for (int i = tid; i < kRows * (D / 4); i += kSimtThreads) {
-            const int r = i / (D / 4), c = i % (D / 4);
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < rows)
-                x = reinterpret_cast<const float4*>((const float*)a.q + (((size_t)it.li * a.n_tokens + it.first + tok0 + r / a.G) * a.Hq + it.hkv * a.G + r % a.G) * D)[c];
-            *reinterpret_cast<float4*>(sq + r * (D + kPad) + c * 4) = x;
-        }
+        stage_queries<D>(a, it, tok0, 0, rows, kRows, sq);
         ChunkRow row[4];
         float m[4], l[4], o[4][D / 16];
         int slot_end = 0;  // slots from here on are hidden from the whole unit
@@ -86,12 +89,24 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
 #pragma unroll
             for (int e = 0; e < D / 16; ++e) o[i][e] = 0.f;
         }
-        for (int t = at; t < stop; ++t) {
-            for (int j0 = (base_tile + t) * kChunkTile; j0 < min((base_tile + t + 1) * kChunkTile, slot_end); j0 += kKeys) {
+        // steps of kKeys keys, the next one's rows under way while this one is worked on
+        const int j_begin = (base_tile + at) * a.tile, j_end = min((base_tile + stop) * a.tile, slot_end);
+        auto stage = [&](int j0, int buf) {
+            float* sk = skv + buf * 2 * kKeys * (D + kPad);
+            stage_rows<D>(a, a.k, it.item, j0, slot_end, kKeys, sk, &bad);
+            stage_rows<D>(a, a.v, it.item, j0, slot_end, kKeys, sk + kKeys * (D + kPad), &bad);
+        };
+        if (j_begin < j_end) stage(j_begin, 0);
+        cp_async_commit();
+        {
+            int buf = 0;
+            for (int j0 = j_begin; j0 < j_end; j0 += kKeys, buf ^= 1) {
+                cp_async_wait<0>();
                 __syncthreads();
-                stage_rows<D>(a, a.k, it.item, j0, slot_end, kKeys, sk, &bad);
-                stage_rows<D>(a, a.v, it.item, j0, slot_end, kKeys, sv, &bad);
-                __syncthreads();
+                if (j0 + kKeys < j_end) stage(j0 + kKeys, buf ^ 1);
+                cp_async_commit();
+                const float* sk = skv + buf * 2 * kKeys * (D + kPad);
+                const float* sv = sk + kKeys * (D + kPad);
                 float s[4][2] = {};
 #pragma unroll 4
                 for (int d = 0; d < D; d += 4) {
@@ -147,6 +162,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
                 }
                 __syncwarp();
             }
+            cp_async_wait<0>();
         }
         const bool whole = at == s0 && stop == s1;
         const size_t part = ((size_t)blockIdx.x * 2 + (at == s0 ? 1 : 0)) * 2;
@@ -181,98 +197,97 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
     }
 }
 
-// Eq. 5 for the chunk: one block per (item, 64 keys); threads own 4 keys x 2 of 32 query rows per step and add up
+// Eq. 5 for the chunk: one block per (item, 32 keys); threads own 2 keys x 4 of 64 query rows per step and add up
 // exp2(logit - lse + log2 of the row's decay weight).  The last launch that reads len: block 0 of an item stores the new one.
 template <int D>
 __global__ void __launch_bounds__(kSimtThreads) chunk_simt_rel(const __grid_constant__ ChunkArgs a) {
     extern __shared__ __align__(16) float smem[];
-    float* sk = smem;                        // [64][D + kPad]
-    float* sq = sk + kRows * (D + kPad);     // [32][D + kPad]
+    float* sk = smem;                        // [kKeys][D + kPad]
+    float* sqs = sk + kKeys * (D + kPad);    // two stages of [kRows][D + kPad]
     dependency_wait();
-    const int per_item = (a.cap_tokens + kRows - 1) / kRows;
+    const int per_item = (a.cap_tokens + kKeys - 1) / kKeys;
     const int idx = blockIdx.x / per_item, block = blockIdx.x - idx * per_item;
     const ChunkItem it = chunk_item(a, idx);
     if (it.n_old < 0 || it.T == 0) return;
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;  // thread: keys ty, ty + 16; rows tx + 16 i
     if (block == 0 && tid == 0 && a.append) a.len[it.item] = it.n;
-    const int j0 = block * kRows;
+    const int j0 = block * kKeys;
     if (j0 >= it.n) return;
     bool bad = false;  // the attention has recorded bad pages
-    stage_rows<D>(a, a.k, it.item, j0, it.n, kRows, sk, &bad);
-    const float scale = a.scale[it.l];
-    const int prefix = a.prefix_len ? a.prefix_len[it.b] : INT32_MIN;
-    const int32_t* pos = a.pos + (size_t)it.item * a.cap_tokens;
-    const bool by_pos = a.slopes || a.window || a.doc_start || a.prefix_len;
-    int kp[4];
-    float acc[4] = {};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) kp[i] = by_pos && j0 + ty * 4 + i < it.n ? pos[j0 + ty * 4 + i] : 0;
+    stage_rows<D>(a, a.k, it.item, j0, it.n, kKeys, sk, &bad);
     const int rows = it.T * a.G;
     // rows before the first that reaches key j0 in causal order see nothing here, unless a prefix opens it to all
-    int first = a.append && !a.prefix_len ? max(0, j0 - it.n_old) * a.G : 0;
-    first &= ~31;
-    for (int r0 = first; r0 < rows; r0 += 32) {
+    const int first = a.append && !a.prefix_len ? max(0, j0 - it.n_old) * a.G & ~(kRows - 1) : 0;
+    if (first < rows) stage_queries<D>(a, it, 0, first, rows, kRows, sqs);
+    cp_async_commit();
+    const float scale = a.scale[it.l];
+    const int prefix = a.prefix_len ? a.prefix_len[it.b] : INT32_MIN;
+    const bool by_pos = a.slopes || a.window || a.doc_start || a.prefix_len;
+    int kp[2];
+    float acc[2] = {}, old[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int j = j0 + ty + 16 * k;
+        kp[k] = by_pos && j < it.n ? a.pos[(size_t)it.item * a.cap_tokens + j] : 0;
+        old[k] = j < it.n_old ? a.rel[(size_t)it.item * a.cap_tokens + j] : 0.f;
+    }
+    int buf = 0;
+    for (int r0 = first; r0 < rows; r0 += kRows, buf ^= 1) {
+        cp_async_wait<0>();
         __syncthreads();
-        for (int i = tid; i < 32 * (D / 4); i += kSimtThreads) {
-            const int r = r0 + i / (D / 4), c = i % (D / 4);
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < rows)
-                x = reinterpret_cast<const float4*>((const float*)a.q + (((size_t)it.li * a.n_tokens + it.first + r / a.G) * a.Hq + it.hkv * a.G + r % a.G) * D)[c];
-            *reinterpret_cast<float4*>(sq + (i / (D / 4)) * (D + kPad) + c * 4) = x;
+        if (r0 + kRows < rows) stage_queries<D>(a, it, 0, r0 + kRows, rows, kRows, sqs + (buf ^ 1) * kRows * (D + kPad));
+        cp_async_commit();
+        const float* sq = sqs + buf * kRows * (D + kPad);
+        ChunkRow row[4];
+        float bias[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = min(r0 + tx + 16 * i, rows - 1), tok = r / a.G;
+            row[i].lim = r0 + tx + 16 * i < rows ? it.n_old + (a.append ? tok + 1 : 0) : INT32_MIN;
+            row[i].qpos = a.token_pos ? a.token_pos[it.first + tok] : 0;
+            row[i].lo = r0 + tx + 16 * i < rows ? chunk_lo(a, it.first + tok, row[i].qpos) : INT32_MAX;
+            row[i].slope = a.slopes ? a.slopes[it.hkv * a.G + r % a.G] * 1.4426950408889634f : 0.f;
+            bias[i] = a.nlse2[(((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G + r] + (float)(it.T - 1 - tok) * a.gamma_log2;
         }
-        __syncthreads();
-        float s[4][2] = {};
+        float s[2][4] = {};
 #pragma unroll 4
         for (int d = 0; d < D; d += 4) {
-            const float4 q0 = *reinterpret_cast<const float4*>(sq + tx * (D + kPad) + d);
-            const float4 q1 = *reinterpret_cast<const float4*>(sq + (tx + 16) * (D + kPad) + d);
+            const float4 k0 = *reinterpret_cast<const float4*>(sk + ty * (D + kPad) + d);
+            const float4 k1 = *reinterpret_cast<const float4*>(sk + (ty + 16) * (D + kPad) + d);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float4 x = *reinterpret_cast<const float4*>(sk + (ty * 4 + i) * (D + kPad) + d);
-                s[i][0] = fmaf(x.x, q0.x, fmaf(x.y, q0.y, fmaf(x.z, q0.z, fmaf(x.w, q0.w, s[i][0]))));
-                s[i][1] = fmaf(x.x, q1.x, fmaf(x.y, q1.y, fmaf(x.z, q1.z, fmaf(x.w, q1.w, s[i][1]))));
+                const float4 x = *reinterpret_cast<const float4*>(sq + (tx + 16 * i) * (D + kPad) + d);
+                s[0][i] = fmaf(x.x, k0.x, fmaf(x.y, k0.y, fmaf(x.z, k0.z, fmaf(x.w, k0.w, s[0][i]))));
+                s[1][i] = fmaf(x.x, k1.x, fmaf(x.y, k1.y, fmaf(x.z, k1.z, fmaf(x.w, k1.w, s[1][i]))));
             }
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = r0 + tx + 16 * h;
-            if (r >= rows) continue;
-            const int tok = r / a.G;
-            ChunkRow row;
-            row.lim = it.n_old + (a.append ? tok + 1 : 0);
-            row.qpos = a.token_pos ? a.token_pos[it.first + tok] : 0;
-            row.lo = chunk_lo(a, it.first + tok, row.qpos);
-            row.slope = a.slopes ? a.slopes[it.hkv * a.G + r % a.G] * 1.4426950408889634f : 0.f;
-            const float bias = a.nlse2[(((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G + r] + (float)(it.T - 1 - tok) * a.gamma_log2;
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float x = judge(a, row, s[i][h], j0 + ty * 4 + i, it.n, kp[i], scale, prefix);
-                if (x != -INFINITY) acc[i] += fast_exp2(x + bias);
+                const float x = judge(a, row[i], s[k][i], j0 + ty + 16 * k, it.n, kp[k], scale, prefix);
+                if (x != -INFINITY) acc[k] += fast_exp2(x + bias[i]);
             }
-        }
     }
+    cp_async_wait<0>();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int k = 0; k < 2; ++k) {
 #pragma unroll
-        for (int off = 8; off > 0; off >>= 1) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], off);
-        const int j = j0 + ty * 4 + i;
-        if (tx == 0 && j < it.n) {
-            float* rel = a.rel + (size_t)it.item * a.cap_tokens + j;
-            const float old = j < it.n_old ? *rel : 0.f;
-            *rel = fmaf(exp2f((float)it.T * a.gamma_log2), old, acc[i]);
-        }
+        for (int off = 8; off > 0; off >>= 1) acc[k] += __shfl_xor_sync(0xffffffffu, acc[k], off);
+        const int j = j0 + ty + 16 * k;
+        if (tx == 0 && j < it.n) a.rel[(size_t)it.item * a.cap_tokens + j] = fmaf(exp2f((float)it.T * a.gamma_log2), old[k], acc[k]);
     }
 }
 
 template <int D>
 cudaError_t launch_t(const ChunkArgs& a, cudaStream_t stream) {
-    const size_t smem = ((size_t)(kRows + 2 * kKeys) * (D + kPad) + kRows * (kKeys + 1)) * sizeof(float);
-    const size_t smem_rel = (size_t)(kRows + 32) * (D + kPad) * sizeof(float);
+    const size_t smem = ((size_t)(kRows + 4 * kKeys) * (D + kPad) + kRows * (kKeys + 1)) * sizeof(float);
+    const size_t smem_rel = (size_t)(kKeys + 2 * kRows) * (D + kPad) * sizeof(float);
     cudaError_t e = prepare_kernel((const void*)chunk_simt_attend<D>, smem);
     if (e == cudaSuccess) e = prepare_kernel((const void*)chunk_simt_rel<D>, smem_rel);
     if (e == cudaSuccess) e = launch_dependent(chunk_simt_attend<D>, dim3(a.n_cta), kSimtThreads, smem, stream, a);
     if (e == cudaSuccess) e = launch_chunk_combine(a, stream);
-    if (e == cudaSuccess) e = launch_dependent(chunk_simt_rel<D>, dim3((a.cap_tokens + kRows - 1) / kRows * a.n_items), kSimtThreads, smem_rel, stream, a);
+    if (e == cudaSuccess) e = launch_dependent(chunk_simt_rel<D>, dim3((a.cap_tokens + kKeys - 1) / kKeys * a.n_items), kSimtThreads, smem_rel, stream, a);
     return e;
 }
 
