@@ -331,7 +331,7 @@ lethe_status lethe_prefill_seed(lethe_ctx *ctx, const lethe_cache *cache, const 
  * A token that no slot is visible to gets out = 0, lse = -inf and adds nothing to the relevance.
  */
 typedef struct {
-    float softcap;             /* 0 = off; finite, >= 0                        */
+    float softcap;             /* 0 = off; else 1e-4 .. 1e30                   */
     int32_t window;            /* 0 = off; >= 0                                */
     const float *slopes;       /* DEVICE [Hq] or NULL                          */
     const int32_t *doc_start;  /* DEVICE [n_tokens] or NULL                    */
@@ -393,8 +393,9 @@ lethe_status lethe_rotate(lethe_ctx *ctx, const lethe_rotary *rotary, int32_t dt
  * An item that cannot take all T tokens (len + T > cap_tokens) is left untouched, its out rows are zero-filled (lse =
  * -inf) and LETHE_ERR_CAPACITY is recorded.  A page id outside the pool reads as zero rows and records LETHE_ERR_PAGE.
  * If chunk_start decreases anywhere, leaves [0, n_tokens] or has a T_b above max_chunk, the call does nothing and records
- * LETHE_ERR_INVALID_ARG.  Slots at or beyond len may hold anything.  A NaN or an infinity in a value row that some
- * token of the chunk sees may reach the other tokens of its sequence too.
+ * LETHE_ERR_INVALID_ARG.  Slots at or beyond len may hold anything, and a hidden key may be NaN or infinite.  A value row
+ * below len must be finite even where it is hidden: it is multiplied by probabilities that are zero, and a NaN or an
+ * infinity in it can reach every token of its sequence.  out must not overlap q.
  * Scratch: 4 bytes per (layer, token, query head), up to about 80 MB of partial results, and for chunks of at most 16
  * (token, head of a group) rows up to 1 GB of parked logits (64 bytes per slot at most).
  */

@@ -1107,11 +1107,14 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     if (!chunk_start) return fail(ctx, LETHE_ERR_INVALID_ARG, "chunk_start is NULL");
     if (max_chunk < 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "max_chunk must be positive");
     if (mod) {
-        if (!(mod->softcap >= 0.f && mod->softcap <= 1e30f)) return fail(ctx, LETHE_ERR_INVALID_ARG, "softcap must be finite and >= 0");
+        if (!(mod->softcap == 0.f || (mod->softcap >= 1e-4f && mod->softcap <= 1e30f))) return fail(ctx, LETHE_ERR_INVALID_ARG, "softcap must be 0 or 1e-4 .. 1e30");
         if (mod->window < 0) return fail(ctx, LETHE_ERR_INVALID_ARG, "window must be >= 0");
         if ((mod->slopes || mod->window > 0) && !token_pos) return fail(ctx, LETHE_ERR_INVALID_ARG, "slopes and a window need token_pos");
     }
     const int nl = layer_end - layer_begin, G = c->n_q_heads / c->n_kv_heads, D = c->head_dim;
+    // the queries are read again after outputs have been written
+    const size_t act = c->dtype == LETHE_F32 ? 4 : 2, q_bytes = (size_t)nl * n_tokens * c->n_q_heads * D * act;
+    if (q == out || overlap_partly(q, q_bytes, out, q_bytes)) return fail(ctx, LETHE_ERR_INVALID_ARG, "out must not overlap q");
     RotateArgs rot;
     if (rotary) {
         st = rotary_args(ctx, rotary, c->dtype == LETHE_F32 ? LETHE_F32 : LETHE_BF16, D, nl, n_tokens, c->n_q_heads, k_new ? c->n_kv_heads : 0, 0, &rot);
@@ -1161,7 +1164,7 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     a.tile = simt ? 32 : kChunkTile;
     a.cap_tiles = (a.cap_tokens + a.tile - 1) / a.tile;
     const long long units = (long long)a.n_items * a.QT;
-    if (units > 0x7fffffffLL / 4 || units * (a.cap_tiles + a.pad) > 0x7fffffffLL || units * a.cap_tiles * 2 > 0x7fffffffLL || (long long)a.n_items * a.cap_tiles * 2 > 0x7fffffffLL)
+    if (units > 0x3fffffffLL / (a.cap_tiles + a.pad + 1))  // steps of the plan's lines, with room for their rounding
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "chunk: too many (layer, sequence, head, block) units for one call; cover fewer layers");
     a.n_units = (int)units;
 
@@ -1169,7 +1172,6 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
     size_t at = 0;
     auto take = [&](size_t bytes_) { const size_t p = at; at += (bytes_ + 255) & ~(size_t)255; return p; };
-    const size_t act = c->dtype == LETHE_F32 ? 4 : 2;
     const size_t o_plan = take(sizeof(ChunkPlan)), o_old = take((size_t)a.n_items * 4), o_start = take(((size_t)a.n_units + 1) * 4);
     const size_t o_lo = by_pos ? take((size_t)a.n_units * 4) : 0, o_hi = by_pos ? take((size_t)a.n_units * 4) : 0;
     const size_t o_cta = take((size_t)a.n_cta * 4);

@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
             const bool mask_pos = MOD && (a.window > 0 || a.doc_start || a.prefix_len);
             if (MOD) {
                 if (a.softcap > 0.f) {
-                    cap_in = scale / a.softcap;
+                    cap_in = fminf(scale / a.softcap, 1e15f);  // its square has to stay finite
                     cap2 = a.softcap * 1.4426950408889634f;
                 }
                 if (a.token_pos) pos0 = a.token_pos[it.first];

@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                 if (a.prefix_len) prefix = a.prefix_len[p.it.b];
                 if (a.slopes) slope = a.slopes[p.it.hkv * a.G + h] * 1.4426950408889634f;
                 if (a.softcap > 0.f) {
-                    cap_in = scale / a.softcap;
+                    cap_in = fminf(scale / a.softcap, 1e15f);  // its square has to stay finite
                     cap2 = a.softcap * 1.4426950408889634f;
                 }
             }
@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         const float in = a.softcap > 0.f ? 1.f : sl2;
                         const int nv = min(lim, p.it.n) - j0;
                         const bool masked = mask_pos ? !clean : __any_sync(0xffffffffu, nv < c0 + NC);
-                        if (masked || a.softcap > 0.f || a.slopes) {
+                        if ((masked && mask_pos && !run) || a.softcap > 0.f || a.slopes) {
 #pragma unroll 1
                             for (int c = 0; c < NC; c += 16) {
                                 const uint32_t at = s_buf + (NC == 64 ? c : NC * quarter);
@@ -502,6 +502,13 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
 #pragma unroll
                             for (int c = 0; c < NC; ++c)
                                 if (c >= nv) v[c] = 0xff800000u;
+                        }
+                    } else if (mask_pos && !clean && run && !(a.softcap > 0.f || a.slopes)) {  // a run, and nothing else to shape
+                        const int y0 = from - c0, y1 = to - c0;
+                        if (__any_sync(0xffffffffu, y0 > 0 || y1 < NC)) {
+#pragma unroll
+                            for (int c = 0; c < NC; ++c)
+                                if (c < y0 || c >= y1) v[c] = 0xff800000u;
                         }
                     }
                     if (NC == 16 && a.park && valid_row) {
@@ -681,6 +688,12 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     }
                     const float mul = !whole ? 1.f : (l == 0.f ? 0.f : a.v_scale[p.it.l] / l);
                     const float mine = l == 0.f ? 0.f : w0 * mul, others = l == 0.f ? 0.f : w1 * mul;
+                    __nv_bfloat16* dst[4];  // where the rows go that this lane writes a piece of
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int row = quarter * 32 + y * 8 + (lane >> 2), tk = p.tok0 + (p.alt ? 0 : g * a.TT) + row / a.G;
+                        dst[y] = row < tile_rows ? out0 + ((size_t)tk * a.Hq + row % a.G) * D + (lane & 3) * 8 : nullptr;
+                    }
 #pragma unroll 1
                     for (int c = 0; c < D; c += 32) {
                         uint32_t o[32];
@@ -688,10 +701,12 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         tmem_ld_wait();
 #pragma unroll
                         for (int y = 0; y < 32; ++y) {
-                            float x = mine == 0.f ? 0.f : __uint_as_float(o[y]) * mine;  // what nothing was added to may hold anything
-                            if (others != 0.f) x = fmaf(merge_o[(c + y) * kTile + r], others, x);
-                            o[y] = __float_as_uint(x);
+                            // what nothing was added to may hold anything
+                            o[y] = mine == 0.f ? 0u : __float_as_uint(__uint_as_float(o[y]) * mine);
                         }
+                        if (p.alt && others != 0.f)
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(fmaf(merge_o[(c + y) * kTile + r], others, __uint_as_float(o[y])));
                         if (!whole) {
                             if (valid_row)
 #pragma unroll
@@ -709,13 +724,8 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         }
                         __syncwarp();
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const int rr = y * 8 + (lane >> 2), row = quarter * 32 + rr;
-                            if (row < tile_rows) {
-                                const int tk = p.tok0 + (p.alt ? 0 : g * a.TT) + row / a.G;
-                                *reinterpret_cast<uint4*>(out0 + ((size_t)tk * a.Hq + row % a.G) * D + c + (lane & 3) * 8) = *reinterpret_cast<const uint4*>(&sh.turn[warp][rr][16 * (lane & 3)]);
-                            }
-                        }
+                        for (int y = 0; y < 4; ++y)
+                            if (dst[y]) *reinterpret_cast<uint4*>(dst[y] + c) = *reinterpret_cast<const uint4*>(&sh.turn[warp][y * 8 + (lane >> 2)][16 * (lane & 3)]);
                     }
                     if (valid_row) row_stats(tok, h, r, m, l);
                 }

@@ -225,36 +225,35 @@ __device__ __forceinline__ float2 exp2_fma(float lo, float hi) {
     return make_float2(lo >= -126.f ? a : 0.f, hi >= -126.f ? b : 0.f);
 }
 
-// softcap * tanh(t) in log2 units (cap2 = softcap * log2(e)) of NC logits, t = v * cap_in.  `care`: what this lane holds counts (rows
-// that are not there may hold anything, which must not send the warp down the longer path).
+// softcap * tanh(t) in log2 units (cap2 = softcap * log2(e)) of NC logits, t = v * cap_in: v times a polynomial in t^2 (five
+// coefficients: 1.4e-7 of tanh in fp32) while |t| <= 0.55.  `care`: what this lane holds counts (rows that are not there may hold
+// anything, which must not send the warp down the longer path).
 template <int NC>
 __device__ __forceinline__ void cap_scores(uint32_t* v, float cap_in, float cap2, bool care) {
-    const uint64_t in2 = two(cap_in, cap_in), out2 = two(cap2, cap2);
+    const float k = cap2 * cap_in, far = 0.55f / cap_in;
+    const uint64_t sq = two(cap_in * cap_in, cap_in * cap_in);
+    const uint64_t c0 = two(0.9999999676367849f * k, 0.9999999676367849f * k), c1 = two(-0.3333279501836578f * k, -0.3333279501836578f * k);
+    const uint64_t c2 = two(0.13318876828366036f * k, 0.13318876828366036f * k), c3 = two(-0.052589315256801286f * k, -0.052589315256801286f * k);
+    const uint64_t c4 = two(0.01631543615226489f * k, 0.01631543615226489f * k);
 #pragma unroll
     for (int c = 0; c < NC; c += 16) {
         float big = 0.f;
-        uint64_t t[8];
+        uint64_t x[8];
 #pragma unroll
         for (int y = 0; y < 8; ++y) {
-            t[y] = mul2(two(__uint_as_float(v[c + 2 * y]), __uint_as_float(v[c + 2 * y + 1])), in2);
-            const float2 f = apart(t[y]);
-            big = max3(big, fabsf(f.x), fabsf(f.y));
-            const uint64_t u = mul2(t[y], t[y]);
-            uint64_t p = fma2(u, two(-0.006235556820094805f, -0.006235556820094805f), two(0.021039673409724794f, 0.021039673409724794f));
-            p = fma2(u, p, two(-0.05384270671952741f, -0.05384270671952741f));
-            p = fma2(u, p, two(0.13332460742850846f, 0.13332460742850846f));
-            p = fma2(u, p, two(-0.33333310957894996f, -0.33333310957894996f));
-            p = fma2(u, p, two(0.9999999990645916f, 0.9999999990645916f));
-            const float2 r = apart(mul2(mul2(t[y], out2), p));
+            big = max3(big, fabsf(__uint_as_float(v[c + 2 * y])), fabsf(__uint_as_float(v[c + 2 * y + 1])));
+            x[y] = two(__uint_as_float(v[c + 2 * y]), __uint_as_float(v[c + 2 * y + 1]));
+            const uint64_t u = mul2(mul2(x[y], x[y]), sq);
+            const float2 r = apart(mul2(x[y], fma2(u, fma2(u, fma2(u, fma2(u, c4, c3), c2), c1), c0)));
             v[c + 2 * y] = __float_as_uint(r.x);
             v[c + 2 * y + 1] = __float_as_uint(r.y);
         }
-        if (__any_sync(0xffffffffu, care && !(big <= 0.55f))) {  // some are outside the polynomial's range (or NaN, behind the last slot)
+        if (__any_sync(0xffffffffu, care && !(big <= far))) {  // some are outside the polynomial's range (or NaN, behind the last slot)
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-                const float2 f = apart(t[y]);
-                if (fabsf(f.x) > 0.55f) v[c + 2 * y] = __float_as_uint(cap2 * capped_large(f.x));
-                if (fabsf(f.y) > 0.55f) v[c + 2 * y + 1] = __float_as_uint(cap2 * capped_large(f.y));
+                const float2 f = apart(x[y]);
+                if (fabsf(f.x) > far) v[c + 2 * y] = __float_as_uint(cap2 * capped_large(f.x * cap_in));
+                if (fabsf(f.y) > far) v[c + 2 * y + 1] = __float_as_uint(cap2 * capped_large(f.y * cap_in));
             }
         }
     }
@@ -355,28 +354,43 @@ struct Gather {
     uint4 x[kByteLoads];
 
     // half: which half of the columns (bf16: a register tile is half a tile wide)
-    __device__ __forceinline__ void load(const ChunkArgs& a, const void* base, int item, int end, int j0, int tid, int half, bool* bad) {
+    __device__ __forceinline__ void load(const ChunkArgs& a, const void* base, int item, int end, int j0, unsigned tid, int half, bool* bad) {
         const bool bytes = a.dtype != LETHE_BF16;
-        constexpr int C = D / 16;  // 16-byte pieces of a row of bytes, or of half a bf16 row
+        constexpr unsigned C = D / 16;       // 16-byte pieces of a row of bytes, or of half a bf16 row
+        constexpr unsigned kStep = NT / C;   // rows from one piece of a thread to its next
+        const unsigned r0 = tid / C, c = tid % C;
+        const size_t row_bytes = bytes ? D : 2 * D;
+        const char* col = (const char*)base + (bytes ? c : half * C + c) * 16;
+        const int left = end - j0 - (int)r0;  // rows of the tile from this thread's first on that there are
+        if (!a.paged) {
+            const char* src = col + ((size_t)item * a.capacity + j0 + r0) * row_bytes;
+#pragma unroll
+            for (int u = 0; u < kByteLoads; ++u)
+                x[u] = (int)(u * kStep) < left ? *reinterpret_cast<const uint4*>(src + u * kStep * row_bytes) : make_uint4(0, 0, 0, 0);
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < kByteLoads; ++u) {
-            const int i = tid + u * NT, r = i / C, c = i % C;
             x[u] = make_uint4(0, 0, 0, 0);
-            if (j0 + r < end) {
-                const long long at = chunk_row(a, item, j0 + r);
+            if ((int)(u * kStep) < left) {
+                long long at;
+                if (bytes) {  // 16-token pages
+                    const unsigned slot = j0 + r0 + u * kStep;
+                    const int page = a.page_table[(size_t)item * a.capacity + (slot >> 4)];
+                    at = page < 0 || page >= a.n_pages ? -1 : (long long)page * 16 + (slot & 15);
+                } else at = chunk_row(a, item, j0 + r0 + u * kStep);
                 if (at < 0) *bad = true;
-                else x[u] = reinterpret_cast<const uint4*>((const char*)base + (size_t)at * (bytes ? D : 2 * D))[bytes ? c : half * C + c];
+                else x[u] = *reinterpret_cast<const uint4*>(col + (size_t)at * row_bytes);
             }
         }
     }
-    __device__ __forceinline__ void store(const ChunkArgs& a, uint32_t dst, int tid, int half) const {
-        constexpr int C = D / 16;
+    __device__ __forceinline__ void store(const ChunkArgs& a, uint32_t dst, unsigned tid, int half) const {
+        constexpr unsigned C = D / 16;
         const bool e5m2 = a.dtype == LETHE_FP8_E5M2;
         if (a.dtype == LETHE_BF16) {
 #pragma unroll
             for (int u = 0; u < kByteLoads; ++u) {
-                const int i = tid + u * NT;
-                st_shared_16(chunk_addr(dst, i / C, half * C + i % C), x[u]);
+                st_shared_16(chunk_addr(dst, tid / C + u * (NT / C), half * C + tid % C), x[u]);
             }
             return;
         }
@@ -386,14 +400,14 @@ struct Gather {
         if (!special) {
 #pragma unroll
             for (int u = 0; u < kByteLoads; ++u) {
-                const int i = tid + u * NT, r = i / C, c = i % C;
+                const unsigned r = tid / C + u * (NT / C), c = tid % C;
                 st_shared_16(chunk_addr(dst, r, 2 * c), expand8(make_uint2(x[u].x, x[u].y), e5m2));
                 st_shared_16(chunk_addr(dst, r, 2 * c + 1), expand8(make_uint2(x[u].z, x[u].w), e5m2));
             }
         } else {
 #pragma unroll
             for (int u = 0; u < kByteLoads; ++u) {
-                const int i = tid + u * NT, r = i / C, c = i % C;
+                const unsigned r = tid / C + u * (NT / C), c = tid % C;
                 st_shared_16(chunk_addr(dst, r, 2 * c), expand8_any(make_uint2(x[u].x, x[u].y), e5m2));
                 st_shared_16(chunk_addr(dst, r, 2 * c + 1), expand8_any(make_uint2(x[u].z, x[u].w), e5m2));
             }

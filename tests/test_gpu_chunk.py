@@ -355,7 +355,8 @@ def test_refusals(ctx):
     assert call(start=None) == I and call(q=None) == I and call(out=None) == I and call(k=None) == I and call(v=None) == I and call(tp=None) == I
     assert call(mx=0) == I and call(n=-1) == I and call(gamma=0.0) == I and call(gamma=1.5) == I and call(layers=(0, 2)) == I and call(layers=(1, 1)) == I
     assert call(scale=float("nan")) == I and call(mod=M(-1.0, 0, None, None, None)) == I and call(mod=M(float("nan"), 0, None, None, None)) == I
-    assert call(mod=M(0.0, -1, None, None, None)) == I
+    assert call(mod=M(0.0, -1, None, None, None)) == I and call(mod=M(1e-6, 0, None, None, None)) == I
+    assert call(out=x["q"]) == I and call(out=x["q"].view(-1)[64:]) == I
     assert call(k=None, v=None, tp=None, mod=M(0.0, 5, None, None, None)) == I
     q1 = x["q"].view(-1)[1:]
     assert call(q=q1) == I
@@ -454,3 +455,59 @@ def test_several_tiles_per_cta(ctx, dtype, gain, page, T):
     ch = ref.make_chunk(st, [T] * B)
     for _ in range(2):
         check(ctx, copy.deepcopy(st), ch)
+
+
+@pytest.mark.parametrize("dtype,page", [(BF16, 0), (BF16, 16), (E4M3, 0)])
+@pytest.mark.parametrize("new", [[1, 1], [300, 20]])
+def test_waits_run_out_and_the_context_recovers(ctx, dtype, page, new):
+    """With a poll limit of one the tensor-core kernels' first hand-offs give up: the launches return, LETHE_ERR_TIMEOUT is recorded,
+    and the next ordinary call on the same context is right."""
+    from paper_2511_06029_b200 import binding
+    st = ref.State(1, 2, 32, 8, 128, 1600, 1200, dtype, page=page, seed=3)
+    ch = ref.make_chunk(st, new)
+    broken = st.device_cache()
+    try:
+        ctx.set_wait_limit(1)
+        run_device(ctx, st, broken, ch, [0.09], 0.9)
+        assert ctx.poll_status()[0] == binding.ERR_TIMEOUT
+        assert ctx.poll_status()[0] == 0
+    finally:
+        ctx.set_wait_limit(0)
+    check(ctx, st, ch, scale=[0.09], gamma=0.9)
+
+
+def test_two_contexts_on_two_streams(ctx):
+    """Calls through two contexts may overlap on the device: each has scratch of its own."""
+    from paper_2511_06029_b200 import binding
+    other = binding.Context(0)
+    st = ref.State(1, 2, 32, 8, 128, 3000, torch.tensor([2500, 900]).view(1, 2, 1).expand(1, 2, 8), BF16, seed=8)
+    ch = ref.make_chunk(st, [120, 300])
+    caches = [st.device_cache() for _ in range(6)]
+    x = {k: dev(ch[k]) for k in ("q", "k_new", "v_new", "token_pos", "chunk_start")}
+    outs = [(torch.zeros_like(x["q"]), torch.zeros(ch["q"].shape[:3], device="cuda")) for _ in caches]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for i, (gc, (o, z)) in enumerate(zip(caches, outs)):
+        with torch.cuda.stream(streams[i % 2]):
+            (ctx, other)[i % 2].chunk_attend(gc, 0, 1, x["chunk_start"], ch["max_chunk"], x["q"], x["k_new"], x["v_new"], x["token_pos"], [0.09], 0.9, o, z)
+    torch.cuda.synchronize()
+    assert ctx.poll_status()[0] == 0 and other.poll_status()[0] == 0
+    live = torch.arange(3000, device="cuda") < caches[0].len[..., None]
+    for gc, (o, z) in zip(caches[1:], outs[1:]):
+        assert torch.equal(o, outs[0][0]) and torch.equal(z, outs[0][1]) and torch.equal(gc.rel[live], caches[0].rel[live])
+    other.close()
+
+
+def test_empty_and_padded_batches(ctx):
+    """Sequences without tokens between others, all of them empty with padding rows around, one sequence only."""
+    for dtype in (F32, BF16, E4M3):
+        st = ref.State(1, 5, 8, 2, 64, 200, torch.tensor([0, 50, 100, 7, 150]).view(1, 5, 1).expand(1, 5, 2), dtype, seed=3)
+        check(ctx, copy.deepcopy(st), ref.make_chunk(st, [0, 3, 0, 0, 50], lead=1, trail=2))
+        ch = ref.make_chunk(st, [0, 0, 0, 0, 0], lead=3, trail=1)
+        check(ctx, copy.deepcopy(st), ch)
+
+
+def test_long_chunk_of_many_units(ctx):
+    """A chunk of several units per item on both sides of every split, odd group size, against the reference."""
+    st = ref.State(1, 1, 14, 2, 128, 1500, 333, BF16, page=16 if 1500 % 16 == 0 else 0, seed=5)
+    check(ctx, st, ref.make_chunk(st, [1111]))
