@@ -1164,7 +1164,8 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     a.tile = simt ? 32 : kChunkTile;
     a.cap_tiles = (a.cap_tokens + a.tile - 1) / a.tile;
     const long long units = (long long)a.n_items * a.QT;
-    if (units > 0x3fffffffLL / (a.cap_tiles + a.pad + 1))  // steps of the plan's lines, with room for their rounding
+    // Steps of the plan's lines, with room for their rounding, and rows of a call are counted in 32 bits.
+    if (units > 0x3fffffffLL / (a.cap_tiles + a.pad + 1) || (long long)nl * n_tokens * c->n_q_heads > 0x3fffffffLL)
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "chunk: too many (layer, sequence, head, block) units for one call; cover fewer layers");
     a.n_units = (int)units;
 

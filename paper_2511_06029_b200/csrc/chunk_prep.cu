@@ -157,50 +157,51 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_append_kernel(const __grid
     const int act = a.dtype == LETHE_F32 ? 4 : 2;
     const int src_row = a.D * act, dst_row = bytes ? a.D : src_row;
     const int chunks = src_row / 16;  // 16-byte pieces of a new row: 8 .. 32
-    const long long rows = (long long)a.nl * a.n_tokens * a.Hkv;
     // A half-warp takes a row at a time, first its K, then its V, U of each in flight: where a row goes is a short chain of
-    // dependent loads (length, page), so a warp works on 2 U rows at once.
+    // dependent loads (length, page), so a warp works on 2 U rows at once.  Rows are counted in 32 bits: the divisions of a
+    // 64-bit count took longer than the copy.
     constexpr int U = 2;
-    const int half = lane >> 4, hl = lane & 15;
-    const long long step = (long long)(gridDim.x - 1) * kPrepWarps * 2 * U;
-    for (long long r0 = ((long long)(blockIdx.x - 1) * kPrepWarps + (tid >> 5)) * 2 * U; r0 < rows; r0 += step) {
+    const unsigned rows = (unsigned)a.nl * a.n_tokens * a.Hkv, hkvs = a.Hkv, tokens = a.n_tokens;
+    const unsigned half = lane >> 4, hl = lane & 15;
+    const unsigned step = (gridDim.x - 1) * kPrepWarps * 2 * U;
+    const int first = start[0], last = start[a.B];
+    for (unsigned r0 = ((blockIdx.x - 1) * kPrepWarps + (tid >> 5)) * 2 * U; r0 < rows; r0 += step) {
         int item[U], slot[U], lay[U];
+        unsigned tok[U], lt[U];
         long long at[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const long long r = r0 + 2 * u + half;
+            const unsigned r = r0 + 2 * u + half;
             item[u] = -1;
             at[u] = -1;
             if (r >= rows) continue;
-            const int hkv = (int)(r % a.Hkv);
-            const long long lt = r / a.Hkv;
-            const int tok = (int)(lt % a.n_tokens), li = (int)(lt / a.n_tokens);
-            if (tok < start[0] || tok >= start[a.B]) continue;
+            lt[u] = r / hkvs;
+            const unsigned hkv = r - lt[u] * hkvs, li = lt[u] / tokens;
+            tok[u] = lt[u] - li * tokens;
+            if ((int)tok[u] < first || (int)tok[u] >= last) continue;
             int lo = 0, hi = a.B;  // last b with start[b] <= tok: the sequence of this token (empty ones before it are passed over)
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (start[mid] <= tok) lo = mid;
+                if (start[mid] <= (int)tok[u]) lo = mid;
                 else hi = mid;
             }
             const int T = start[lo + 1] - start[lo];
             lay[u] = a.layer_begin + li;
             item[u] = (lay[u] * a.B + lo) * a.Hkv + hkv;
             const int n_old = min(max(a.len[item[u]], 0), a.cap_tokens);
-            slot[u] = n_old + (long long)T > a.cap_tokens ? -1 : n_old + tok - start[lo];
+            slot[u] = n_old + (long long)T > a.cap_tokens ? -1 : n_old + (int)tok[u] - start[lo];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const long long r = r0 + 2 * u + half;
             if (item[u] < 0) continue;
-            const long long lt = r / a.Hkv;
-            const int hkv = (int)(r % a.Hkv);
             if (slot[u] < 0) {  // refused: nothing of the item changes, its outputs are zero
-                char* o = (char*)a.out + ((size_t)lt * a.Hq + (size_t)hkv * a.G) * src_row;
+                const unsigned head = (r0 + 2 * u + half - lt[u] * hkvs) * a.G;
+                char* o = (char*)a.out + ((size_t)lt[u] * a.Hq + head) * src_row;
                 for (int i = hl; i < a.G * chunks; i += 16) reinterpret_cast<uint4*>(o)[i] = make_uint4(0, 0, 0, 0);
-                if (a.lse && hl < a.G) a.lse[(size_t)lt * a.Hq + hkv * a.G + hl] = -INFINITY;
+                if (a.lse && hl < a.G) a.lse[(size_t)lt[u] * a.Hq + head + hl] = -INFINITY;
                 continue;
             }
-            if (hl == 0) a.pos[(size_t)item[u] * a.cap_tokens + slot[u]] = a.token_pos[lt % a.n_tokens];
+            if (hl == 0) a.pos[(size_t)item[u] * a.cap_tokens + slot[u]] = a.token_pos[tok[u]];
             at[u] = chunk_row(a, item[u], slot[u]);
             if (at[u] < 0 && hl == 0) record_error(a.status, LETHE_ERR_PAGE, item[u]);
         }
