@@ -1176,7 +1176,7 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     const size_t o_plan = take(sizeof(ChunkPlan)), o_old = take((size_t)a.n_items * 4), o_start = take(((size_t)a.n_units + 1) * 4);
     const size_t o_lo = by_pos ? take((size_t)a.n_units * 4) : 0, o_hi = by_pos ? take((size_t)a.n_units * 4) : 0;
     const size_t o_cta = take((size_t)a.n_cta * 4);
-    a.n_rel_cta = 2 * ctx->sm_count;
+    a.n_rel_cta = (a.slopes ? 1 : 2) * ctx->sm_count;  // as many as are resident, see the kernel
     const int cap_pairs = (a.cap_tiles + 1) / 2;
     const size_t o_rel = take(((size_t)a.n_items + 1) * 4), o_ri = take((size_t)a.n_rel_cta * 4), o_cut = take((size_t)a.n_rel_cta * sizeof(int4));
     const size_t o_rp = take((size_t)a.n_rel_cta * 2 * 2 * kChunkTile * 4);

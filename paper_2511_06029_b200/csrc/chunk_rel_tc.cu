@@ -9,7 +9,9 @@
 //
 // A unit is a pair of key tiles of one item (two groups of four warps), its steps are the query tiles that meet it; the plan gives
 // every CTA an equal stretch of the line of all steps (a causal prompt's first keys meet every token, its last keys few), and the
-// parts of a unit that CTAs share are added up afterwards in order.  Two CTAs to an SM cover each other's hand-offs.  Warp 8 issues the MMAs, warp 9 loads tiles by TMA; tiles that TMA cannot take
+// parts of a unit that CTAs share are added up afterwards in order.  Two CTAs to an SM cover each other's hand-offs; with slopes one,
+// which then has registers for all that its columns bring along (512-token chunks with a cap and slopes 65 us with two that spill, 54
+// with one; a cap alone 70 us with two, 88 with one).  Warp 8 issues the MMAs, warp 9 loads tiles by TMA; tiles that TMA cannot take
 // (byte caches, odd pages) are gathered by the softmax warps, once per unit.
 #include "chunk_tc.cuh"
 
@@ -26,7 +28,7 @@ constexpr int kTmemCols = 256;  // one logit tile per group
 template <int D>
 constexpr size_t smem_bytes() { return 1024 + 3 * (size_t)tile_bytes<D>(); }  // two key tiles, one query tile
 
-template <bool MOD>
+template <int MOD>
 struct Shared {
     unsigned long long k_full, k_empty, q_full, q_empty;
     unsigned long long s_full[2], s_empty[2];
@@ -35,8 +37,8 @@ struct Shared {
     int abort;
     int k_loads, q_loads, issued;
     alignas(16) float bias[kSoftWarps][kTile];
-    alignas(16) float qpos[MOD ? kSoftWarps : 1][kTile];   // relative to the sequence's first new token
-    alignas(16) float slope[MOD ? kSoftWarps : 1][kTile];  // log2 units
+    alignas(16) float qpos[MOD == kSloped ? kSoftWarps : 1][kTile];   // relative to the sequence's first new token
+    alignas(16) float slope[MOD == kSloped ? kSoftWarps : 1][kTile];  // log2 units
     alignas(16) int lo[MOD ? kSoftWarps : 1][kTile];
 };
 
@@ -88,8 +90,8 @@ __device__ __forceinline__ void for_rel_pieces(const ChunkArgs& a, F f) {
     }
 }
 
-template <int D, bool TMA, bool MOD>
-__global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps) {
+template <int D, bool TMA, int MOD>
+__global__ void __launch_bounds__(kThreads, MOD == kSloped ? 1 : 2) chunk_tc_rel(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps) {
     constexpr int TILE = tile_bytes<D>(), KS = D / 16;
     extern __shared__ unsigned char dyn_raw[];
     __shared__ Shared<MOD> sh;
@@ -234,15 +236,17 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
             const float scale = fabsf(a.scale[it.l]) * a.k_scale[it.l], sl2 = scale * 1.4426950408889634f;
             float cap_in = 0.f, cap2 = 0.f, kf = 0.f;
             int kp = 0, prefix = INT32_MIN, pos0 = 0;
+            constexpr bool sloped = MOD == kSloped;
+            const bool cap = MOD == kCapped || (sloped && a.softcap > 0.f);
             const bool mask_pos = MOD && (a.window > 0 || a.doc_start || a.prefix_len);
             if (MOD) {
-                if (a.softcap > 0.f) {
+                if (cap) {
                     cap_in = fminf(scale / a.softcap, 1e15f);  // its square has to stay finite
                     cap2 = a.softcap * 1.4426950408889634f;
                 }
                 if (a.token_pos) pos0 = a.token_pos[it.first];
                 if (a.prefix_len) prefix = a.prefix_len[it.b];
-                if (mask_pos || a.slopes) {
+                if (mask_pos || sloped) {
                     kp = j < it.n ? a.pos[(size_t)it.item * a.cap_tokens + j] : 0;
                     kf = (float)((long long)kp - pos0);
                 }
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
             float col_slope[4];
             if (MOD)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) col_slope[x] = a.slopes ? a.slopes[it.hkv * a.G + (x * 32 + lane) % a.G] * 1.4426950408889634f : 0.f;
+                for (int x = 0; x < 4; ++x) col_slope[x] = sloped ? a.slopes[it.hkv * a.G + (x * 32 + lane) % a.G] * 1.4426950408889634f : 0.f;
             const float* nlse = a.nlse2 + (((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G;
             uint64_t acc[2] = {0, 0};
             float acc0 = 0.f;  // of columns judged one by one
@@ -286,8 +290,10 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     if (MOD) {
                         int lo = next_doc[x];
                         if (a.window > 0) lo = (int)max((long long)lo, (long long)next_pos[x] - a.window + 1);
-                        sh.qpos[warp][c] = (float)((long long)next_pos[x] - pos0);
-                        sh.slope[warp][c] = col_slope[x];
+                        if (sloped) {
+                            sh.qpos[warp][c] = (float)((long long)next_pos[x] - pos0);
+                            sh.slope[warp][c] = col_slope[x];
+                        }
                         sh.lo[warp][c] = c < cols ? lo : INT32_MAX;  // columns that are not there see nothing
                         if (c < cols) lo_max = max(lo_max, lo);
                     }
@@ -316,8 +322,9 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                 if (j >= it.n) to = 0;
                 if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
                 tc_after();
-                // in narrow pieces and rolled where scores are shaped: unrolled, the code outgrows the instruction cache, and 32 columns spill
-                constexpr int W = MOD ? 16 : 32;
+                // rolled where there is more than the causal mask: unrolled, the code outgrows the instruction cache (packed documents 287
+                // -> 301 us); in narrow pieces where scores are shaped: 32 columns spill
+                constexpr int W = shaped(MOD) ? 16 : 32;
 #pragma unroll (MOD ? 1 : 4)
                 for (int ch = 0; ch < kTile; ch += W) {
                     if (ch >= cols) break;  // a short chunk leaves most columns empty
@@ -332,11 +339,11 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
                     }
                     float ml = sl2;
                     if (MOD) {
-                        if (a.softcap > 0.f) {
+                        if (cap) {
                             ml = 1.f;
                             cap_scores<W>(v, cap_in, cap2, j < it.n);
                         }
-                        if (a.slopes) {
+                        if (sloped) {
 #pragma unroll
                             for (int c = 0; c < W; c += 4) {
                                 const float4 qp = *reinterpret_cast<const float4*>(&sh.qpos[warp][ch + c]), sl = *reinterpret_cast<const float4*>(&sh.slope[warp][ch + c]);
@@ -413,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_tc_rel(const __grid_constan
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
-template <int D, bool TMA, bool MOD>
+template <int D, bool TMA, int MOD>
 cudaError_t launch_t(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
     cudaError_t e = prepare_kernel((const void*)chunk_tc_rel<D, TMA, MOD>, smem_bytes<D>());
     if (e == cudaSuccess) e = launch_dependent(chunk_tc_rel<D, TMA, MOD>, dim3(a.n_rel_cta), kThreads, smem_bytes<D>(), stream, a, maps);
@@ -422,8 +429,12 @@ cudaError_t launch_t(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t str
 
 template <int D, bool TMA>
 cudaError_t launch_m(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
-    const bool mod = a.softcap > 0.f || a.slopes || a.window > 0 || a.doc_start || a.prefix_len;
-    return mod ? launch_t<D, TMA, true>(a, maps, stream) : launch_t<D, TMA, false>(a, maps, stream);
+    switch (score_kind(a)) {
+        case kPlain: return launch_t<D, TMA, kPlain>(a, maps, stream);
+        case kMasked: return launch_t<D, TMA, kMasked>(a, maps, stream);
+        case kCapped: return launch_t<D, TMA, kCapped>(a, maps, stream);
+        default: return launch_t<D, TMA, kSloped>(a, maps, stream);
+    }
 }
 
 }  // namespace

@@ -44,7 +44,7 @@ __host__ __device__ constexpr int stages() { return D == 128 ? 4 : 8; }
 template <int D>
 constexpr size_t smem_bytes() { return 1024 + (size_t)(2 + stages<D>()) * tile_bytes<D>(); }
 
-template <bool MOD>
+template <int MOD>
 struct Shared {
     unsigned long long full[kMaxStages], empty[kMaxStages];
     unsigned long long q_full, q_done, q_soft, merge, merge_all;
@@ -146,7 +146,7 @@ __device__ __forceinline__ void for_pieces(const ChunkArgs& a, F f) {
     }
 }
 
-template <int D, bool TMA, bool MOD>
+template <int D, bool TMA, int MOD>
 __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __grid_constant__ ChunkArgs a, const __grid_constant__ ChunkMaps maps) {
     constexpr int TILE = tile_bytes<D>(), NS = stages<D>(), KS = D / 16;
     constexpr int kOCol = 256;  // tensor memory: S0 | S1 | O0 | O1, 128 columns each (two buffers of logits each, P over its logits)
@@ -340,7 +340,9 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
         const int g = warp >> 2, quarter = warp & 3;
         const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + g * 128;
         const uint32_t o_addr = s_addr + kOCol;
-        const bool by_pos = MOD && (a.slopes || a.window > 0 || a.doc_start || a.prefix_len);
+        constexpr bool sloped = MOD == kSloped;
+        const bool cap = MOD == kCapped || (sloped && a.softcap > 0.f);
+        const bool by_pos = MOD && (sloped || a.window > 0 || a.doc_start || a.prefix_len);
         const bool mask_pos = MOD && (a.window > 0 || a.doc_start || a.prefix_len);
         float* const merge_o = reinterpret_cast<float*>(q_generic);  // parts to merge, where the query tiles were
         unsigned s0 = 0, s1 = 0, o0 = 0, o1 = 0;  // logits taken and products asked for so far, per buffer
@@ -366,14 +368,14 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                 }
                 if (valid_row) lo = chunk_lo(a, p.it.first + tok, qpos);
                 if (a.prefix_len) prefix = a.prefix_len[p.it.b];
-                if (a.slopes) slope = a.slopes[p.it.hkv * a.G + h] * 1.4426950408889634f;
-                if (a.softcap > 0.f) {
+                if (sloped) slope = a.slopes[p.it.hkv * a.G + h] * 1.4426950408889634f;
+                if (cap) {
                     cap_in = fminf(scale / a.softcap, 1e15f);  // its square has to stay finite
                     cap2 = a.softcap * 1.4426950408889634f;
                 }
             }
             // what a logit has to be multiplied by, once shaped, to be in log2 units
-            const float ml = MOD && (a.softcap > 0.f || a.slopes) ? 1.f : sl2;
+            const float ml = cap || sloped ? 1.f : sl2;
             float m = -INFINITY, l = 0.f;
             const int n0 = first_job(p, g), end = job_end(p, g);
             int kp_min, from = 0, to = 0;  // masks by position, per tile
@@ -450,18 +452,18 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                     if (MOD) {
                         // Scores are shaped sixteen columns at a time and put back: unrolled over the whole row the code outgrows the
                         // instruction cache (a job took 8000 clocks instead of 2500).
-                        const float in = a.softcap > 0.f ? 1.f : sl2;
+                        const float in = cap ? 1.f : sl2;
                         const int nv = min(lim, p.it.n) - j0;
                         const bool masked = mask_pos ? !clean : __any_sync(0xffffffffu, nv < c0 + NC);
-                        if ((masked && mask_pos && !run) || a.softcap > 0.f || a.slopes) {
+                        if ((masked && mask_pos && !run) || cap || sloped) {
 #pragma unroll 1
                             for (int c = 0; c < NC; c += 16) {
                                 const uint32_t at = s_buf + (NC == 64 ? c : NC * quarter);
                                 uint32_t w[16];
                                 tmem_ld16(at, w);
                                 tmem_ld_wait();
-                                if (a.softcap > 0.f) cap_scores<16>(w, cap_in, cap2, valid_row);
-                                if (a.slopes) {
+                                if (cap) cap_scores<16>(w, cap_in, cap2, valid_row);
+                                if (sloped) {
 #pragma unroll
                                     for (int y = 0; y < 16; y += 4) {
                                         const float4 kf = *reinterpret_cast<const float4*>(&sh.kposf[warp][c0 + c + y]);
@@ -503,7 +505,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                             for (int c = 0; c < NC; ++c)
                                 if (c >= nv) v[c] = 0xff800000u;
                         }
-                    } else if (mask_pos && !clean && run && !(a.softcap > 0.f || a.slopes)) {  // a run, and nothing else to shape
+                    } else if (mask_pos && !clean && run && !(cap || sloped)) {  // a run, and nothing else to shape
                         const int y0 = from - c0, y1 = to - c0;
                         if (__any_sync(0xffffffffu, y0 > 0 || y1 < NC)) {
 #pragma unroll
@@ -758,7 +760,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-template <int D, bool TMA, bool MOD>
+template <int D, bool TMA, int MOD>
 cudaError_t launch_t(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
     cudaError_t e = prepare_kernel((const void*)chunk_tc_attend<D, TMA, MOD>, smem_bytes<D>());
     if (e != cudaSuccess) return e;
@@ -768,8 +770,12 @@ cudaError_t launch_t(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t str
 
 template <int D, bool TMA>
 cudaError_t launch_m(const ChunkArgs& a, const ChunkMaps& maps, cudaStream_t stream) {
-    const bool mod = a.softcap > 0.f || a.slopes || a.window > 0 || a.doc_start || a.prefix_len;
-    return mod ? launch_t<D, TMA, true>(a, maps, stream) : launch_t<D, TMA, false>(a, maps, stream);
+    switch (score_kind(a)) {
+        case kPlain: return launch_t<D, TMA, kPlain>(a, maps, stream);
+        case kMasked: return launch_t<D, TMA, kMasked>(a, maps, stream);
+        case kCapped: return launch_t<D, TMA, kCapped>(a, maps, stream);
+        default: return launch_t<D, TMA, kSloped>(a, maps, stream);
+    }
 }
 
 }  // namespace
