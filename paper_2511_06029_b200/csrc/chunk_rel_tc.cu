@@ -12,7 +12,8 @@
 // parts of a unit that CTAs share are added up afterwards in order.  Two CTAs to an SM cover each other's hand-offs; with slopes one,
 // which then has registers for all that its columns bring along (512-token chunks with a cap and slopes 65 us with two that spill, 54
 // with one; a cap alone 70 us with two, 88 with one).  Warp 8 issues the MMAs, warp 9 loads tiles by TMA; tiles that TMA cannot take
-// (byte caches, odd pages) are gathered by the softmax warps, once per unit.
+// (byte caches, odd pages) are gathered by the softmax warps, once per unit.  An 8192-token prompt of 32 heads over 8: about 360 us,
+// 1250 clocks of a tile, of which the special-function unit has 768 with a quarter of the exponentials on the FMA pipes.
 #include "chunk_tc.cuh"
 
 namespace lethe {
@@ -22,7 +23,8 @@ constexpr int kSoftWarps = 8;
 constexpr int kMmaWarp = 8;
 constexpr int kLoadWarp = 9;
 constexpr int kThreads = 10 * 32;
-constexpr int kFmaShare = 2;  // of eight exponentials, computed by polynomial
+// Of eight exponentials, computed by polynomial: an 8192-token prompt takes 925 us with none, 907 with two, 1000 with four.
+constexpr int kFmaShare = 2;
 constexpr int kTmemCols = 256;  // one logit tile per group
 
 template <int D>
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, MOD == kSloped ? 1 : 2) chunk_tc_rel
 #pragma unroll
                             for (int z = 0; z < 4; ++z) {
                                 const float2 x = apart(fma2(two(__uint_as_float(v[c + 2 * z]), __uint_as_float(v[c + 2 * z + 1])), ml2, bias[z]));
-                                const float2 e = 2 * z >= 8 - kFmaShare ? exp2_fma<5>(x.x, x.y) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                                const float2 e = 2 * z >= 8 - kFmaShare ? exp2_fma(x.x, x.y) : make_float2(fast_exp2(x.x), fast_exp2(x.y));
                                 acc[z & 1] = add2(acc[z & 1], two(e.x, e.y));
                             }
                         }

@@ -207,19 +207,16 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // 2^x of two values on the FMA pipes, for a share of the exponentials that the special-function unit (16 a clock per SM) is the bound
 // of: x = n + r with n the nearest whole number (the low bits of x + 1.5 * 2^23) and r in [-1/2, 1/2], 2^r by a polynomial fitted
-// to the relative error (degree 4: 2.7e-6, degree 5: 2.1e-7 in fp32), n added to the exponent.  x is at most 127 here; below
+// to the relative error (2.1e-7 in fp32), n added to the exponent.  x is at most 127 here; below
 // -126 the result is 0 (for a NaN too: the callers look for those).
-template <int DEG>
 __device__ __forceinline__ float2 exp2_fma(float lo, float hi) {
-    constexpr float c4[6] = {0.9999992614236742f, 0.6931218147800758f, 0.24024744901073158f, 0.05591786008673926f, 0.009570098946574577f, 0.f};
-    constexpr float c5[6] = {1.0000000716545048f, 0.6931469670591965f, 0.2402211972442394f, 0.05550713282584675f, 0.009675541310994419f, 0.0013276469054922968f};
+    constexpr float c[6] = {1.0000000716545048f, 0.6931469670591965f, 0.2402211972442394f, 0.05550713282584675f, 0.009675541310994419f, 0.0013276469054922968f};
     const uint64_t x = two(fmaxf(lo, -126.f), fmaxf(hi, -126.f));
     const uint64_t t = add2(x, two(12582912.f, 12582912.f));
     const uint64_t r = fma2(add2(t, two(-12582912.f, -12582912.f)), two(-1.f, -1.f), x);
-    const float* c = DEG == 4 ? c4 : c5;
-    uint64_t p = two(c[DEG], c[DEG]);
+    uint64_t p = two(c[5], c[5]);
 #pragma unroll
-    for (int i = DEG - 1; i >= 0; --i) p = fma2(p, r, two(c[i], c[i]));
+    for (int i = 4; i >= 0; --i) p = fma2(p, r, two(c[i], c[i]));
     const float2 pf = apart(p), tf = apart(t);
     const float a = __int_as_float(__float_as_int(pf.x) + (__float_as_int(tf.x) << 23)), b = __int_as_float(__float_as_int(pf.y) + (__float_as_int(tf.y) << 23));
     return make_float2(lo >= -126.f ? a : 0.f, hi >= -126.f ? b : 0.f);
