@@ -121,7 +121,7 @@ __device__ __forceinline__ long long chunk_row(const ChunkArgs& a, int item, int
     return (long long)page * a.page_tokens + slot % a.page_tokens;
 }
 
-// What a query row needs to know to judge a key.
+// What a query row needs to know to test a key.
 struct ChunkRow {
     int lim;     // slots below lim are in causal order
     int qpos;    // original position

@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, MOD == kSloped ? 1 : 2) chunk_tc_rel
                 for (int x = 0; x < 4; ++x) col_slope[x] = sloped ? a.slopes[it.hkv * a.G + (x * 32 + lane) % a.G] * 1.4426950408889634f : 0.f;
             const float* nlse = a.nlse2 + (((size_t)it.li * a.Hkv + it.hkv) * a.n_tokens + it.first) * a.G;
             uint64_t acc[2] = {0, 0};
-            float acc0 = 0.f;  // of columns judged one by one
+            float acc0 = 0.f;  // of columns tested one by one
             // what the tile's columns bring along, fetched a tile ahead: lane x has columns x, x + 32, ...
             float next_bias[4];
             int next_pos[4], next_doc[4];
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, MOD == kSloped ? 1 : 2) chunk_tc_rel
                 // one copy per warp (the warps never wait for one another)
                 const int cols = min(a.TT, it.T - qt * a.TT) * a.G;
                 int lo_max = INT32_MIN;
-                bool nan = false;  // a token whose scores are NaN: every column is judged, so that it comes through
+                bool nan = false;  // a token whose scores are NaN: every column is tested, so that it comes through
                 __syncwarp();
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {

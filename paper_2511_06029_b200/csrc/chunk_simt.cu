@@ -38,7 +38,7 @@ __device__ __forceinline__ void stage_queries(const ChunkArgs& a, const ChunkIte
 }
 
 // The logit of a visible key in log2 units, -inf for a hidden one.
-__device__ __forceinline__ float judge(const ChunkArgs& a, const ChunkRow& row, float s, int j, int n, int kpos, float scale, int prefix) {
+__device__ __forceinline__ float shaped_logit(const ChunkArgs& a, const ChunkRow& row, float s, int j, int n, int kpos, float scale, int prefix) {
     if (!((j < row.lim || (kpos < prefix && j < n)) && kpos >= row.lo)) return -INFINITY;
     float x = s * scale;
     if (a.softcap > 0.f) x = a.softcap * capped(x / a.softcap);
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_attend(const __grid_c
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int j = j0 + tx + 16 * h;
-                        s[i][h] = j < slot_end ? judge(a, row[i], s[i][h], j, it.n, kp[h], scale, prefix) : -INFINITY;
+                        s[i][h] = j < slot_end ? shaped_logit(a, row[i], s[i][h], j, it.n, kp[h], scale, prefix) : -INFINITY;
                     }
                     float mx = fmaxf(s[i][0], s[i][1]);
 #pragma unroll
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_rel(const __grid_cons
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float x = judge(a, row[i], s[k][i], j0 + ty + 16 * k, it.n, kp[k], scale, prefix);
+                const float x = shaped_logit(a, row[i], s[k][i], j0 + ty + 16 * k, it.n, kp[k], scale, prefix);
                 if (x != -INFINITY) acc[k] += fast_exp2(x + bias[i]);
             }
     }

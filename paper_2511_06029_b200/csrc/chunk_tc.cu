@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
                         clean = __all_sync(0xffffffffu, kp_min >= lo && lim - j0 >= kTile && nn >= kTile);
                         if (!clean) {
                             // Positions that grow with the slot (any cache that was only appended to and pruned): what a row sees of
-                            // the tile is a run of columns [from, to), found by halving.  Else every key is judged by itself.
+                            // the tile is a run of columns [from, to), found by halving.  Else every key is tested by itself.
                             bool up = true;
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {

@@ -156,6 +156,27 @@ def test_modified_scores(ctx, dtype, kind, new):
     check(ctx, st, ch, scale=[3.0 / math.sqrt(D)], **kw)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, E5M2])
+@pytest.mark.parametrize("order", ["grown", "any"])
+@pytest.mark.parametrize("kind", ["softcap", "slopes"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_shaped_scores_with_masks(ctx, dtype, order, kind, D):
+    """A cap alone, or slopes alone, together with every mask by position; positions that grow with the slot and others; logits on
+    both sides of the cap's bend."""
+    Hq, Hkv, B = 10, 2, 2
+    st = ref.State(1, B, Hq, Hkv, D, 512, torch.tensor([330, 60]).view(1, B, 1).expand(1, B, Hkv), dtype, page=16 if D == 128 else 0, seed=D + len(kind))
+    if order == "any":
+        g = torch.Generator().manual_seed(3)
+        st.pos[...] = torch.randint(0, 1200, st.pos.shape, generator=g, dtype=torch.int32)
+    ch = ref.make_chunk(st, [70, 37], seed=8, first_pos=[1000, 180])
+    kw = {"window": 500, "prefix_len": torch.tensor([90, 30], dtype=torch.int32), "doc_start": (ch["token_pos"] // 400 * 400).to(torch.int32)}
+    if kind == "softcap":
+        kw["softcap"] = 4.0
+    else:
+        kw["slopes"] = torch.tensor([2.0 ** (-0.8 * (h + 1)) for h in range(Hq)])
+    check(ctx, st, ch, scale=[3.0 / math.sqrt(D)], **kw)
+
+
 def test_positions_in_any_order(ctx):
     """Masks by position do not lean on positions that grow with the slot."""
     st = ref.State(1, 1, 8, 2, 128, 900, 700, BF16, seed=2)
