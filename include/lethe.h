@@ -103,11 +103,12 @@ typedef struct {
  * scored before they are quantised). */
 
 /* Create a context on CUDA device `device`.  scratch_bytes_hint (0 = default) sizes the
- * device scratch the calls may use; it grows on demand.  Growth synchronises the device, frees the
- * old buffer and allocates a larger one: a CUDA graph captured from earlier calls may still name the
- * old buffer and must be captured again, and a call that would have to grow scratch while its stream
- * is being captured is refused with LETHE_ERR_UNSUPPORTED (size the scratch with scratch_bytes_hint,
- * or make the same call once before capturing).
+ * device scratch the calls may use; it grows on demand.  Growth synchronises the device and allocates a
+ * larger buffer; the old one is freed, unless calls of the context have been captured into CUDA graphs: such
+ * graphs go on using it, and it stays allocated until lethe_destroy.  A call that would have to grow scratch
+ * while its stream is being captured is refused with LETHE_ERR_UNSUPPORTED (size the scratch with
+ * scratch_bytes_hint, or make the same call once before capturing).  Calls and graph replays of one context
+ * share its scratch: order them on one stream or by events.
  * Returns LETHE_ERR_CUDA if no usable sm_100 device / runtime is present. */
 lethe_status lethe_create(lethe_ctx **ctx, int device, size_t scratch_bytes_hint);
 void lethe_destroy(lethe_ctx *ctx);

@@ -82,6 +82,11 @@ cudaError_t prepare_kernel(const void* func, size_t smem_needed) {
 }
 }  // namespace lethe
 
+struct Outgrown {  // a buffer that captured graphs may still name
+    void* buf;
+    Outgrown* next;
+};
+
 struct lethe_ctx {
     int device;
     int sm_count;
@@ -90,6 +95,8 @@ struct lethe_ctx {
     unsigned int* sched;  // device: {next ticket, CTAs finished}; zero whenever no attend launch is running
     void* scratch;
     size_t scratch_bytes;
+    bool captured;       // calls have been captured: buffers that they may have been given stay allocated
+    Outgrown* outgrown;  // until lethe_destroy
     // longest-first item order written by the last lethe_rasr_prune, and the cache it describes
     int32_t* order;
     size_t order_bytes;
@@ -150,18 +157,28 @@ struct DeviceGuard {
     }
 };
 
-// Grow a context-owned buffer.  Growth synchronises the device and frees the old buffer, so it must not happen
-// while `stream` is being captured (the capture would be invalidated, and a graph captured earlier may still name
-// the old buffer): that case is refused.
+// Grow a context-owned buffer.  Growth synchronises the device, so it must not happen while `stream` is being captured (the
+// capture would be invalidated): that case is refused.  The old buffer is freed unless a call has been captured with it; a graph
+// captured earlier then goes on using it.
 lethe_status ensure(lethe_ctx* ctx, void** buf, size_t* have, size_t need, const char* what, void* stream = nullptr) {
-    if (need <= *have) return LETHE_OK;
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing((cudaStream_t)stream, &cap) != cudaSuccess) cudaGetLastError();
-    else if (cap != cudaStreamCaptureStatusNone)
+    if (cudaStreamIsCapturing((cudaStream_t)stream, &cap) != cudaSuccess) {
+        cudaGetLastError();
+        cap = cudaStreamCaptureStatusNone;
+    }
+    if (need <= *have) {
+        if (cap != cudaStreamCaptureStatusNone) ctx->captured = true;
+        return LETHE_OK;
+    }
+    if (cap != cudaStreamCaptureStatusNone)
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "%s would have to grow while the stream is being captured", what);
     cudaError_t e = cudaDeviceSynchronize();  // the old buffer may still be in use
     if (e != cudaSuccess) return cuda_fail(ctx, e, what);
-    if (*buf) cudaFree(*buf);
+    if (*buf && ctx->captured) {
+        Outgrown* kept = new (std::nothrow) Outgrown{*buf, ctx->outgrown};
+        if (!kept) return fail(ctx, LETHE_ERR_CUDA, "%s: out of host memory", what);
+        ctx->outgrown = kept;
+    } else if (*buf) cudaFree(*buf);
     *buf = nullptr;
     *have = 0;
     size_t sz = need + need / 4;
@@ -258,6 +275,11 @@ void lethe_destroy(lethe_ctx* ctx) {
     if (ctx->status) cudaFree(ctx->status);
     if (ctx->scratch) cudaFree(ctx->scratch);
     if (ctx->staging) cudaFree(ctx->staging);
+    while (Outgrown* o = ctx->outgrown) {
+        ctx->outgrown = o->next;
+        cudaFree(o->buf);
+        delete o;
+    }
     if (ctx->host_pipeline_ready) {
         cudaStreamDestroy(ctx->up_stream);
         cudaStreamDestroy(ctx->down_stream);

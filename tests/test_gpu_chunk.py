@@ -356,6 +356,42 @@ def test_other_stream_graph_and_two_calls(ctx):
         del graph
 
 
+def test_graph_outlives_growth_of_the_scratch():
+    """A captured call is replayed after a larger one has made the context's scratch grow."""
+    from paper_2511_06029_b200 import binding
+    own = binding.Context(0)
+    st = ref.State(1, 1, 8, 2, 128, 300, 100, BF16, page=0, seed=3)
+    ch = ref.make_chunk(st, [30])
+    x = {k: dev(ch[k]) for k in ("q", "k_new", "v_new", "token_pos", "chunk_start")}
+    gc = st.device_cache()
+    length, rel = gc.len.clone(), gc.rel.clone()
+    out = torch.zeros_like(x["q"])
+
+    def call():
+        own.chunk_attend(gc, 0, 1, x["chunk_start"], ch["max_chunk"], x["q"], x["k_new"], x["v_new"], x["token_pos"], [0.1], 0.9, out)
+
+    call()
+    want, want_rel = out.clone(), gc.rel.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    big = ref.State(2, 4, 32, 8, 128, 4000, 100, BF16, page=0, seed=4)
+    many = ref.make_chunk(big, [3000, 1, 2000, 7])
+    y = {k: dev(many[k]) for k in ("q", "k_new", "v_new", "token_pos", "chunk_start")}
+    own.chunk_attend(big.device_cache(), 0, 2, y["chunk_start"], many["max_chunk"], y["q"], y["k_new"], y["v_new"], y["token_pos"], [0.1, 0.1], 0.9,
+                     torch.zeros_like(y["q"]))
+    filler = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")  # what a freed buffer could have become
+    gc.len.copy_(length)
+    gc.rel.copy_(rel)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert own.poll_status()[0] == 0
+    assert torch.equal(out, want) and torch.equal(gc.rel[0, 0, :, :130], want_rel[0, 0, :, :130])
+    assert bool((filler == 255).all())
+    del graph
+
+
 def test_refusals(ctx):
     from paper_2511_06029_b200 import binding
     st = ref.State(1, 2, 8, 2, 64, 130, 60, BF16, seed=1)
