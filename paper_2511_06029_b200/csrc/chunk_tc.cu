@@ -395,6 +395,10 @@ __global__ void __launch_bounds__(tc_threads<TMA>(), 1) chunk_tc_attend(const __
 #pragma unroll
                 for (int c = 0; c < 4; ++c) kp_next[c] = j0 + c * 32 + lane < p.it.n ? pos[c * 32 + lane] : INT32_MAX;
             };
+            // A group without a job here (one key tile, alternate tiles) would see nothing of the piece before its merge, and after a pair,
+            // whose end it does not wait for either, q_done's phase before the piece's could still be open: its wait would pass at
+            // once, and the group's arrivals on merge and q_soft would count for a piece too early.  The queries come after both.
+            if (n0 >= end && !warp_wait(&sh.q_full, k, abort_flag, limit)) return false;
             if (MOD && by_pos && busy && n0 < end) fetch_pos(job_seq(p, g, n0));
             for (int n = n0; n < end; ++n) {
                 const int buf = n & 1, half = 1 - buf, t = job_seq(p, g, n), j0 = seq_tile(p, t) * kTile;

@@ -568,3 +568,24 @@ def test_long_chunk_of_many_units(ctx):
     """A chunk of several units per item on both sides of every split, odd group size, against the reference."""
     st = ref.State(1, 1, 14, 2, 128, 1500, 333, BF16, page=16 if 1500 % 16 == 0 else 0, seed=5)
     check(ctx, st, ref.make_chunk(st, [1111]))
+
+
+@pytest.mark.parametrize("D,softcap", [(64, 0.0), (64, 20.0), (128, 0.0)])
+def test_single_tile_units_after_pairs(ctx, D, softcap):
+    """Units of two row tiles with several key tiles, each followed by two of one row tile and one key tile (in which a CTA's second
+    softmax group has nothing to do), so that most CTAs walk pair, short, short.  The second group must not run ahead of the first."""
+    L, groups, Hq = 2, 100, 4
+    new = [64, 20, 9] * groups
+    B = len(new)
+    cached = torch.tensor([600, 100, 3] * groups).view(1, B, 1).expand(L, B, 1)
+    st = ref.State(L, B, Hq, 1, D, 664, cached, BF16, seed=D)
+    ch = ref.make_chunk(st, new, seed=4)
+    first = st.device_cache()
+    scale = [0.1, 0.07]
+    out, lse = run_device(ctx, st, first, ch, scale, 0.97, mod_kw={"softcap": softcap} if softcap else None)
+    for _ in range(8):                                               # the same bits however the warps meet
+        again = st.device_cache()
+        o, z = run_device(ctx, st, again, ch, scale, 0.97, mod_kw={"softcap": softcap} if softcap else None)
+        assert torch.equal(o, out) and torch.equal(z, lse) and torch.equal(torch.nan_to_num(again.rel), torch.nan_to_num(first.rel))
+    assert ctx.poll_status()[0] == 0
+    compare(st, first, ch, out, lse, ref.chunk_attend(st, ch, scale, 0.97, softcap=softcap))
