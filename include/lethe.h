@@ -105,9 +105,13 @@ typedef struct {
 /* Create a context on CUDA device `device`.  scratch_bytes_hint (0 = default) sizes the
  * device scratch the calls may use; it grows on demand.  Growth synchronises the device and allocates a
  * larger buffer; the old one is freed, unless calls of the context have been captured into CUDA graphs: such
- * graphs go on using it, and it stays allocated until lethe_destroy.  A call that would have to grow scratch
+ * graphs go on using it, and it stays allocated until lethe_destroy (a buffer grows by a quarter at least, so all
+ * that it has outgrown is less than four times what it has).  A call that would have to grow scratch
  * while its stream is being captured is refused with LETHE_ERR_UNSUPPORTED (size the scratch with
- * scratch_bytes_hint, or make the same call once before capturing).  Calls and graph replays of one context
+ * scratch_bytes_hint, or make the same call once before capturing).  A prune round also leaves the order of the
+ * items' lengths for the decode calls on all layers of that cache: 4 bytes per item, one list for each number of
+ * items, kept until lethe_destroy, so that captured decode calls stay valid whatever is pruned between their replays
+ * (a captured round whose number of items no earlier round had leaves none).  Calls and graph replays of one context
  * share its scratch: order them on one stream or by events.
  * Returns LETHE_ERR_CUDA if no usable sm_100 device / runtime is present. */
 lethe_status lethe_create(lethe_ctx **ctx, int device, size_t scratch_bytes_hint);

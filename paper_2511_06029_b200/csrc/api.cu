@@ -87,6 +87,16 @@ struct Outgrown {  // a buffer that captured graphs may still name
     Outgrown* next;
 };
 
+// The longest-first order that the last prune round of a cache with `items` items has written.  One array for each number of items,
+// kept until lethe_destroy: whatever cache wrote it last, its content is a permutation of 0 .. items - 1, so a captured decode call
+// that names it stays valid (any order gives the same results) however caches are pruned between replays.
+struct ItemOrder {
+    int items;
+    int32_t* order;
+    const int32_t* len;  // cache.len the order was computed from
+    ItemOrder* next;
+};
+
 struct lethe_ctx {
     int device;
     int sm_count;
@@ -97,11 +107,7 @@ struct lethe_ctx {
     size_t scratch_bytes;
     bool captured;       // calls have been captured: buffers that they may have been given stay allocated
     Outgrown* outgrown;  // until lethe_destroy
-    // longest-first item order written by the last lethe_rasr_prune, and the cache it describes
-    int32_t* order;
-    size_t order_bytes;
-    const int32_t* order_len;  // cache.len the order was computed from
-    int order_items;
+    ItemOrder* orders;   // until lethe_destroy
     void* flat;  // scratch-merged split mode: arrival counters (zero between launches), partials, logits
     size_t flat_bytes;
     void* staging;  // device staging of lethe_decode_attend_host
@@ -157,20 +163,25 @@ struct DeviceGuard {
     }
 };
 
-// Grow a context-owned buffer.  Growth synchronises the device, so it must not happen while `stream` is being captured (the
-// capture would be invalidated): that case is refused.  The old buffer is freed unless a call has been captured with it; a graph
-// captured earlier then goes on using it.
-lethe_status ensure(lethe_ctx* ctx, void** buf, size_t* have, size_t need, const char* what, void* stream = nullptr) {
+bool capturing(void* stream) {
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     if (cudaStreamIsCapturing((cudaStream_t)stream, &cap) != cudaSuccess) {
         cudaGetLastError();
-        cap = cudaStreamCaptureStatusNone;
+        return false;
     }
+    return cap != cudaStreamCaptureStatusNone;
+}
+
+// Grow a context-owned buffer.  Every call that hands one to a kernel comes through here, because this is where a capture is noticed.
+// Growth synchronises the device, so it must not happen while `stream` is being captured (the capture would be invalidated): that
+// case is refused.  The old buffer is freed unless a call has been captured; a graph captured earlier then goes on using it.
+lethe_status ensure(lethe_ctx* ctx, void** buf, size_t* have, size_t need, const char* what, void* stream = nullptr) {
+    const bool cap = capturing(stream);
     if (need <= *have) {
-        if (cap != cudaStreamCaptureStatusNone) ctx->captured = true;
+        if (cap) ctx->captured = true;
         return LETHE_OK;
     }
-    if (cap != cudaStreamCaptureStatusNone)
+    if (cap)
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "%s would have to grow while the stream is being captured", what);
     cudaError_t e = cudaDeviceSynchronize();  // the old buffer may still be in use
     if (e != cudaSuccess) return cuda_fail(ctx, e, what);
@@ -290,7 +301,11 @@ void lethe_destroy(lethe_ctx* ctx) {
             cudaEventDestroy(ctx->ev_done[i]);
         }
     }
-    if (ctx->order) cudaFree(ctx->order);
+    while (ItemOrder* o = ctx->orders) {
+        ctx->orders = o->next;
+        cudaFree(o->order);
+        delete o;
+    }
     if (ctx->flat) cudaFree(ctx->flat);
     delete ctx;
 }
@@ -387,6 +402,12 @@ lethe_status lethe_set_wait_limit(lethe_ctx* ctx, int32_t polls) {
     return LETHE_OK;
 }
 
+static ItemOrder* order_of(lethe_ctx* ctx, int items) {
+    ItemOrder* o = ctx->orders;
+    while (o && o->items != items) o = o->next;
+    return o;
+}
+
 lethe_status lethe_decode_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_begin, int layer_end, const void* q,
                                  const void* k_new, const void* v_new, const int32_t* token_pos, const float* scale,
                                  float gamma, void* out, float* lse, void* stream) {
@@ -405,9 +426,10 @@ lethe_status lethe_decode_attend(lethe_ctx* ctx, const lethe_cache* c, int layer
     a.sched = ctx->sched;
     // Work-queue order from the last prune round: usable while the call covers the same items (all layers of the
     // same cache).  Appends lengthen every item alike, so the order stays longest-first between rounds.
-    if (ctx->order && ctx->order_len == c->len && layer_begin == 0 && layer_end == c->n_layers &&
-        ctx->order_items == c->n_layers * c->batch * c->n_kv_heads)
-        a.order = ctx->order;
+    if (layer_begin == 0 && layer_end == c->n_layers) {
+        const ItemOrder* o = order_of(ctx, c->n_layers * c->batch * c->n_kv_heads);
+        if (o && o->len == c->len) a.order = o->order;
+    }
     a.n_pages = c->n_pages;
     a.B = c->batch; a.Hq = c->n_q_heads; a.Hkv = c->n_kv_heads; a.G = G; a.GP = (G + 1) & ~1;
     a.capacity = c->capacity; a.cap_tokens = cap_tokens_of(c);
@@ -604,9 +626,10 @@ lethe_status lethe_decode_attend(lethe_ctx* ctx, const lethe_cache* c, int layer
         const size_t part_bytes = up((size_t)a.n_items * S * (16 + (size_t)G * c->head_dim) * sizeof(float));
         const size_t lg_bytes = up((size_t)a.n_items * a.flat_pitch * a.GP * sizeof(float));
         const size_t need = cnt_bytes + part_bytes + lg_bytes;
-        if (need > ctx->flat_bytes) {
-            st = ensure(ctx, &ctx->flat, &ctx->flat_bytes, need, "scratch-merge buffers", stream);
-            if (st != LETHE_OK) return st;
+        const size_t had = ctx->flat_bytes;
+        st = ensure(ctx, &ctx->flat, &ctx->flat_bytes, need, "scratch-merge buffers", stream);
+        if (st != LETHE_OK) return st;
+        if (ctx->flat_bytes != had) {
             if (cudaMemsetAsync(ctx->flat, 0, ctx->flat_bytes, (cudaStream_t)stream) != cudaSuccess)
                 return fail(ctx, LETHE_ERR_CUDA, "clearing the scratch-merge buffers failed");
         }
@@ -907,16 +930,33 @@ static lethe_status prune_scratch(lethe_ctx* ctx, const CacheView& v, int* smem_
 static lethe_status refresh_order(lethe_ctx* ctx, const lethe_cache* c, const CacheView& v, void* stream) {
     // longest-first order of the items for the persistent attend kernels' work queue
     const long long items = (long long)v.L * v.B * v.Hkv;
-    ctx->order_len = nullptr;
-    if (items >= 2LL * ctx->sm_count && items <= (1 << 20)) {
-        void* buf = ctx->order;
-        lethe_status st = ensure(ctx, &buf, &ctx->order_bytes, (size_t)items * sizeof(int32_t), "item order", stream);
-        ctx->order = (int32_t*)buf;
-        if (st != LETHE_OK) return st;
-        cudaError_t e = launch_order(c->len, (int)items, v.cap_tokens, ctx->order, (cudaStream_t)stream);
-        if (e != cudaSuccess) return cuda_fail(ctx, e, "item order launch");
-        ctx->order_len = c->len;
-        ctx->order_items = (int)items;
+    if (items < 2LL * ctx->sm_count || items > (1 << 20)) return LETHE_OK;
+    ItemOrder* o = order_of(ctx, (int)items);
+    const bool fresh = !o;
+    if (fresh) {
+        // An array holds a permutation before anybody is given it, which a captured launch does not see to: such a round goes without.
+        if (capturing(stream)) return LETHE_OK;
+        int32_t* buf = nullptr;
+        const cudaError_t e = cudaMalloc((void**)&buf, (size_t)items * sizeof(int32_t));
+        if (e != cudaSuccess) return cuda_fail(ctx, e, "item order");
+        o = new (std::nothrow) ItemOrder{(int)items, buf, nullptr, nullptr};
+        if (!o) {
+            cudaFree(buf);
+            return fail(ctx, LETHE_ERR_CUDA, "item order: out of host memory");
+        }
+    }
+    const cudaError_t e = launch_order(c->len, (int)items, v.cap_tokens, o->order, (cudaStream_t)stream);
+    if (e != cudaSuccess) {
+        if (fresh) {
+            cudaFree(o->order);
+            delete o;
+        }
+        return cuda_fail(ctx, e, "item order launch");
+    }
+    o->len = c->len;
+    if (fresh) {
+        o->next = ctx->orders;
+        ctx->orders = o;
     }
     return LETHE_OK;
 }
