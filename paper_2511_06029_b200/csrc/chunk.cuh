@@ -153,7 +153,8 @@ __device__ __forceinline__ float capped_small(float t) {
 }
 __device__ __forceinline__ float capped_large(float t) {
     const float e = fast_exp2(fabsf(t) * 2.885390081777927f);
-    return copysignf(1.f - __fdividef(2.f, 1.f + fminf(e, 1e30f)), t);
+    const float r = copysignf(1.f - __fdividef(2.f, 1.f + fminf(e, 1e30f)), t);
+    return t == t ? r : t;  // the minimum would turn a NaN into a cap
 }
 __device__ __forceinline__ float capped(float t) { return fabsf(t) <= 0.55f ? capped_small(t) : capped_large(t); }
 

@@ -589,3 +589,45 @@ def test_single_tile_units_after_pairs(ctx, D, softcap):
         assert torch.equal(o, out) and torch.equal(z, lse) and torch.equal(torch.nan_to_num(again.rel), torch.nan_to_num(first.rel))
     assert ctx.poll_status()[0] == 0
     compare(st, first, ch, out, lse, ref.chunk_attend(st, ch, scale, 0.97, softcap=softcap))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, E4M3])
+@pytest.mark.parametrize("T", [3, 40])
+@pytest.mark.parametrize("sloped", [False, True])
+def test_nan_comes_through_the_cap(ctx, dtype, T, sloped):
+    """Capped scores: a NaN query makes its own row NaN and what that row sees NaN in the relevance; a NaN key makes the rows NaN that see
+    it.  Everything else is as without it."""
+    n, at, head = 300, T // 2, 5                                     # a token in the middle, a head of the second group
+    Hq, Hkv, D = 8, 2, 128
+    scale, gamma = [0.2], 0.97
+    kw = {"softcap": 20.0}
+    if sloped:
+        kw["slopes"] = torch.tensor([2.0 ** (-0.8 * (h + 1)) for h in range(Hq)])
+
+    def run(where):
+        st = ref.State(1, 1, Hq, Hkv, D, n + T, n, dtype, seed=11)
+        ch = ref.make_chunk(st, [T], seed=12)
+        want = ref.chunk_attend(copy.deepcopy(st), ch, scale, gamma, **kw)
+        clean = copy.deepcopy(st)
+        ref.chunk_attend(clean, ch, scale, gamma, **kw)
+        ch[where] = ch[where].clone()
+        ch[where][0, at, head if where == "q" else 1, 3] = float("nan")
+        gc = st.device_cache()
+        out, lse = run_device(ctx, st, gc, ch, scale, gamma, True, kw)
+        assert ctx.poll_status()[0] == 0
+        o, z, tol_o, tol_z, tol_r, _ = want
+        hit = torch.zeros((1, T, Hq), dtype=torch.bool)
+        if where == "q":
+            hit[0, at, head] = True
+        else:
+            hit[0, at:, 4:] = True
+        gone = torch.zeros((1, 1, Hkv, n + T), dtype=torch.bool)
+        gone[0, 0, 1, :n + at + 1 if where == "q" else n + T] = True
+        out, lse, rel = out.cpu().double(), lse.cpu().double(), gc.rel.cpu().double()
+        assert torch.equal(torch.isnan(lse), hit) and torch.equal(torch.isnan(rel), gone)
+        assert torch.equal(torch.isnan(out), hit[..., None].expand_as(out))
+        assert bool(((out - o).abs() <= tol_o)[~hit].all()) and bool(((lse - z).abs() <= tol_z)[~hit].all())
+        assert bool(((rel - clean.rel).abs() <= tol_r)[~gone].all())
+
+    run("q")
+    run("k_new")
