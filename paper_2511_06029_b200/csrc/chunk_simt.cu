@@ -43,7 +43,7 @@ __device__ __forceinline__ float shaped_logit(const ChunkArgs& a, const ChunkRow
     float x = s * scale;
     if (a.softcap > 0.f) x = a.softcap * capped(x / a.softcap);
     x *= 1.4426950408889634f;
-    if (a.slopes) x -= row.slope * (float)abs(row.qpos - kpos);
+    if (a.slopes) x -= row.slope * fabsf((float)((long long)row.qpos - kpos));
     return x;
 }
 

@@ -631,3 +631,13 @@ def test_nan_comes_through_the_cap(ctx, dtype, T, sloped):
 
     run("q")
     run("k_new")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, E4M3])
+def test_slopes_over_the_whole_range_of_positions(ctx, dtype):
+    """Distances of up to 2^32 - 1: tiny slopes, half of the keys at the lower end of int32, the others near the tokens at its upper end."""
+    st = ref.State(1, 1, 4, 1, 64, 300, 200, dtype, seed=2)
+    st.pos[...] = torch.arange(300, dtype=torch.int32) - 2 ** 31
+    st.pos[..., 100:] = 2 ** 31 - 1000 + torch.arange(200, dtype=torch.int32)
+    ch = ref.make_chunk(st, [20], first_pos=[2 ** 31 - 30])
+    check(ctx, st, ch, slopes=torch.tensor([2.0 ** -30, 2.0 ** -31, 2.0 ** -32, 2.0 ** -40]))
