@@ -241,10 +241,11 @@ __device__ __forceinline__ float fast_rcp(float x) {
     return y;
 }
 // softcap * tanh(t) in log2 units (cap2 = softcap * log2(e)) of NC logits, t = v * cap_in: v times a polynomial in t^2 (five
-// coefficients: 1.4e-7 of tanh in fp32) while |t| <= 0.55; a piece with a larger one takes 1 - 2 / (1 + 2^(2 t log2 e)) for all of its
-// logits, two special-function calls each but no branch (chosen one by one: 512-token chunks with a cap and slopes 305 us instead of
-// 270).  `care`: what this lane holds counts (rows that are not there may hold anything, which must not send the warp down the
-// longer path).
+// coefficients: 1.4e-7 of tanh in fp32) while |t| <= 0.55, else 1 - 2 / (1 + 2^(2 t log2 e)), which alone has an absolute error of an
+// ulp of one: at small t that times the cap would cost a score its low bits, and so each logit takes its own form, whatever its
+// neighbours are.  The second form is computed for a piece of sixteen columns that has a larger one, and chosen without a branch
+// (512-token chunks with a cap and slopes 243 us; 234 when the whole piece took it).
+// `care`: what this lane holds counts (rows that are not there may hold anything, which must not send the warp down the longer path).
 template <int NC>
 __device__ __forceinline__ void cap_scores(uint32_t* v, float cap_in, float cap2, bool care) {
     const float k = cap2 * cap_in, far = 0.55f / cap_in;
@@ -266,14 +267,14 @@ __device__ __forceinline__ void cap_scores(uint32_t* v, float cap_in, float cap2
             v[c + 2 * y] = __float_as_uint(r.x);
             v[c + 2 * y + 1] = __float_as_uint(r.y);
         }
-        if (__any_sync(0xffffffffu, care && !(big <= far))) {  // some are outside the polynomial's range (or NaN, behind the last slot)
+        if (__any_sync(0xffffffffu, care && !(big <= far))) {  // some are outside the polynomial's range (or NaN)
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-                const float2 t = apart(mul2(x[y], far2));
+                const float2 raw = apart(x[y]), t = apart(mul2(x[y], far2));
                 const float2 e = apart(add2(two(fast_exp2(t.x), fast_exp2(t.y)), two(1.f, 1.f)));
                 const float2 r = apart(fma2(two(fast_rcp(e.x), fast_rcp(e.y)), two(-2.f * cap2, -2.f * cap2), two(cap2, cap2)));
-                v[c + 2 * y] = __float_as_uint(r.x);
-                v[c + 2 * y + 1] = __float_as_uint(r.y);
+                if (!(fabsf(raw.x) <= far)) v[c + 2 * y] = __float_as_uint(r.x);
+                if (!(fabsf(raw.y) <= far)) v[c + 2 * y + 1] = __float_as_uint(r.y);
             }
         }
     }

@@ -641,3 +641,72 @@ def test_slopes_over_the_whole_range_of_positions(ctx, dtype):
     st.pos[..., 100:] = 2 ** 31 - 1000 + torch.arange(200, dtype=torch.int32)
     ch = ref.make_chunk(st, [20], first_pos=[2 ** 31 - 30])
     check(ctx, st, ch, slopes=torch.tensor([2.0 ** -30, 2.0 ** -31, 2.0 ** -32, 2.0 ** -40]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, E4M3])
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("sloped", [False, True])
+def test_capped_scores_do_not_depend_on_what_is_not_seen(ctx, dtype, T, sloped):
+    """The same bits whatever lies behind the last slot and in rows that are nobody's tokens."""
+    Hq, Hkv, D = 8, 2, 128
+    results = []
+    for junk in (0.0, float("nan"), 300.0):
+        st = ref.State(1, 1, Hq, Hkv, D, 400, 301, dtype, seed=5, junk=junk, k_scale=[0.02], v_scale=[0.015])
+        st.rel[..., 301:] = 0
+        ch = ref.make_chunk(st, [T], seed=6, trail=30, first_pos=[1000])
+        ch["q"][:, T:] = junk
+        kw = {"softcap": 30.0}
+        if sloped:
+            kw["slopes"] = torch.tensor([2.0 ** (-0.8 * (h + 4)) for h in range(Hq)])
+        gc = st.device_cache()
+        out, lse = run_device(ctx, st, gc, ch, [0.09], 0.97, True, kw)
+        assert ctx.poll_status()[0] == 0
+        results.append((out[:, :T].clone(), lse[:, :T].clone(), gc.rel[..., :301 + T].clone()))
+    for other in results[1:]:
+        for x, y in zip(results[0], other):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [2, 40])
+@pytest.mark.parametrize("sloped", [False, True])
+def test_far_score_leaves_its_neighbours_exact(ctx, dtype, T, sloped):
+    """A cap of 1e5 and one key in sixteen whose scores are near minus the cap: it weighs nothing, and the others have to be as exact as
+    scores of their own size are, not as the cap's size allows."""
+    Hq, Hkv, D, n, cap, s = 8, 2, 128, 320, 1e5, 0.0884
+    st = ref.State(1, 1, Hq, Hkv, D, n, n, dtype, seed=5)
+    far = torch.arange(n) % 16 == 3
+    st.k[..., 0] = 0.0
+    st.k[0, 0, :, far, 0] = -56576.0                                 # exact in bf16
+    ch = ref.make_chunk(st, [T], seed=6, first_pos=[1000])
+    ch["q"][..., 0] = 16.0                                           # scores of -8e4, tanh(-0.8) of the cap
+    slopes = torch.tensor([2.0 ** (-h - 4) for h in range(Hq)]) if sloped else torch.zeros(Hq)
+    gc = st.device_cache()
+    out, lse = run_device(ctx, st, gc, ch, [s], 0.97, False, {"softcap": cap, **({"slopes": slopes} if sloped else {})})
+    assert ctx.poll_status()[0] == 0
+    u, s32 = 2.0 ** -23, float(torch.tensor(s, dtype=torch.float32))
+    rel, rel_err = st.rel.double() * 0.97 ** T, st.rel.double() * 0.97 ** T * (8 + 4 * T * abs(math.log2(0.97))) * u
+    for h in range(Hkv):
+        K, V = st.k[0, 0, h, ~far].double(), st.v[0, 0, h, ~far].double()
+        for g in range(Hq // Hkv):
+            hq = h * (Hq // Hkv) + g
+            q = ch["q"][0, :, hq].double()
+            x = cap * torch.tanh(q @ K.T * s32 / cap)
+            # the product, accumulated in fp32; the cap: eight half steps of the argument, the polynomial and its factors, relative to the score
+            err = (q.abs() @ K.abs().T * s32) * (D + 4) * u + x.abs() * (2.0 ** -21 + 4 * u)
+            bias = float(slopes[hq]) * (ch["token_pos"].long()[:, None] - st.pos[0, 0, h, ~far].long()[None]).abs().double()
+            x, err = x - bias, err + (bias + (x - bias).abs()) * 4 * u
+            z = torch.logsumexp(x, 1)
+            e_z = err.amax(1) + (z.abs() + 8) * 4 * u + (n / 16 + 16) * u   # as in chunk_reference.py
+            assert bool(((lse[0, :, hq].cpu().double() - z).abs() <= e_z).all())
+            p = torch.exp(x - z[:, None])
+            e_p = 2 * (2 * err.amax(1) + (z.abs() + 8) * 4 * u + (n / 16 + 16) * u)
+            half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+            o = p @ V
+            tol = (p @ V.abs()) * (e_p + (half if dtype == BF16 else 0) + (n / 16 + 16) * u)[:, None] + o.abs() * half
+            assert bool(((out[0, :, hq].cpu().double() - o).abs() <= tol).all())
+            wt = 0.97 ** (T - 1 - torch.arange(T)).double()
+            rel[0, 0, h, ~far] += wt @ p
+            rel_err[0, 0, h, ~far] += (wt * (e_p + 4 * u * T * abs(math.log2(0.97)) + (T * Hq / 16 + 16) * u)) @ p
+    rel_err += rel.abs() * (8 + 4 * T * abs(math.log2(0.97))) * u
+    assert bool(((gc.rel.cpu().double() - rel).abs() <= rel_err + 1e-30).all())
