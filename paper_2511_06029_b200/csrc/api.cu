@@ -1164,7 +1164,8 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     ctx->last_len = nullptr;  // the next decode call does not follow a decode call
     if (n_tokens < 0) return fail(ctx, LETHE_ERR_INVALID_ARG, "n_tokens must be >= 0");
     if (n_tokens == 0) return LETHE_OK;
-    st = check_attend_args(ctx, c, layer_begin, layer_end, q, k_new, v_new, token_pos, scale, (float)gamma, out, true);
+    if (!(gamma > 0.0 && gamma <= 1.0)) return fail(ctx, LETHE_ERR_INVALID_ARG, "gamma must be in (0, 1]");
+    st = check_attend_args(ctx, c, layer_begin, layer_end, q, k_new, v_new, token_pos, scale, 1.f, out, true);
     if (st != LETHE_OK) return st;
     if (!chunk_start) return fail(ctx, LETHE_ERR_INVALID_ARG, "chunk_start is NULL");
     if (max_chunk < 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "max_chunk must be positive");

@@ -710,3 +710,26 @@ def test_far_score_leaves_its_neighbours_exact(ctx, dtype, T, sloped):
             rel_err[0, 0, h, ~far] += (wt * (e_p + 4 * u * T * abs(math.log2(0.97)) + (T * Hq / 16 + 16) * u)) @ p
     rel_err += rel.abs() * (8 + 4 * T * abs(math.log2(0.97))) * u
     assert bool(((gc.rel.cpu().double() - rel).abs() <= rel_err + 1e-30).all())
+
+
+def test_gamma_is_checked_as_a_double(ctx):
+    """What fp32 would round into or out of (0, 1]."""
+    from paper_2511_06029_b200 import binding
+    st = ref.State(1, 1, 8, 2, 64, 130, 60, BF16, seed=1)
+    gc = st.device_cache()
+    ch = ref.make_chunk(st, [20])
+    x = {k: dev(ch[k]) for k in ("q", "k_new", "v_new", "token_pos", "chunk_start")}
+    out = torch.zeros_like(x["q"])
+
+    def call(gamma):
+        p = binding._dp
+        return ctx.lib.lethe_chunk_attend(ctx.h, ctypes.byref(gc.c), 0, 1, p(x["chunk_start"]), 20, 20, p(x["q"]), p(x["k_new"]), p(x["v_new"]),
+                                          p(x["token_pos"]), (ctypes.c_float * 1)(0.1), gamma, None, None, p(out), None, binding._stream(0))
+
+    for bad in (1.0 + 1e-9, 0.0, -1e-60, float("nan")):
+        assert call(bad) == binding.ERR_INVALID_ARG
+    assert torch.equal(gc.len.cpu(), st.len) and bool((out == 0).all())
+    assert call(1e-60) == binding.OK and ctx.poll_status()[0] == 0
+    ref.chunk_attend(st, ch, [0.1], 1e-60)
+    assert torch.equal(gc.len.cpu(), st.len)
+    assert torch.allclose(gc.rel.cpu()[..., :80].double(), st.rel[..., :80], rtol=1e-4, atol=1e-30)  # only the last token's weights are left
