@@ -108,8 +108,10 @@ struct lethe_ctx {
     bool captured;       // calls have been captured: buffers that they may have been given stay allocated
     Outgrown* outgrown;  // until lethe_destroy
     ItemOrder* orders;   // until lethe_destroy
-    void* flat;  // scratch-merged split mode: arrival counters (zero between launches), partials, logits
+    void* flat;  // scratch-merged split mode: partials, logits
     size_t flat_bytes;
+    void* flat_cnt;  // its arrival counters: zero between launches, so nothing else is ever kept there
+    size_t flat_cnt_bytes;
     void* staging;  // device staging of lethe_decode_attend_host
     size_t staging_bytes;
     // lethe_decode_attend_host: upload / download streams and the events that chain them to the caller's stream
@@ -307,6 +309,7 @@ void lethe_destroy(lethe_ctx* ctx) {
         delete o;
     }
     if (ctx->flat) cudaFree(ctx->flat);
+    if (ctx->flat_cnt) cudaFree(ctx->flat_cnt);
     delete ctx;
 }
 
@@ -625,18 +628,16 @@ lethe_status lethe_decode_attend(lethe_ctx* ctx, const lethe_cache* c, int layer
         const size_t cnt_bytes = up((size_t)a.n_items * sizeof(int));
         const size_t part_bytes = up((size_t)a.n_items * S * (16 + (size_t)G * c->head_dim) * sizeof(float));
         const size_t lg_bytes = up((size_t)a.n_items * a.flat_pitch * a.GP * sizeof(float));
-        const size_t need = cnt_bytes + part_bytes + lg_bytes;
-        const size_t had = ctx->flat_bytes;
-        st = ensure(ctx, &ctx->flat, &ctx->flat_bytes, need, "scratch-merge buffers", stream);
+        st = ensure(ctx, &ctx->flat, &ctx->flat_bytes, part_bytes + lg_bytes, "scratch-merge buffers", stream);
         if (st != LETHE_OK) return st;
-        if (ctx->flat_bytes != had) {
-            if (cudaMemsetAsync(ctx->flat, 0, ctx->flat_bytes, (cudaStream_t)stream) != cudaSuccess)
-                return fail(ctx, LETHE_ERR_CUDA, "clearing the scratch-merge buffers failed");
-        }
-        // counters sit at the front: they stay zero between launches whatever n_items later calls use
-        a.flat_cnt = (int*)ctx->flat;
-        a.flat_part = (float*)((char*)ctx->flat + cnt_bytes);
-        a.flat_lg = (float*)((char*)ctx->flat + cnt_bytes + part_bytes);
+        const size_t had = ctx->flat_cnt_bytes;
+        st = ensure(ctx, &ctx->flat_cnt, &ctx->flat_cnt_bytes, cnt_bytes, "scratch-merge counters", stream);
+        if (st != LETHE_OK) return st;
+        if (ctx->flat_cnt_bytes != had && cudaMemsetAsync(ctx->flat_cnt, 0, ctx->flat_cnt_bytes, (cudaStream_t)stream) != cudaSuccess)
+            return fail(ctx, LETHE_ERR_CUDA, "clearing the scratch-merge counters failed");
+        a.flat_cnt = (int*)ctx->flat_cnt;
+        a.flat_part = (float*)ctx->flat;
+        a.flat_lg = (float*)((char*)ctx->flat + part_bytes);
         e = launch_attend_mma(a, c->head_dim, shape, paged, (cudaStream_t)stream);
     } else if (variant >= 16 && variant < 32) {  // persistent, asynchronous epilogue: both logit buffers (item parity) share what is left
         if (ctx->splits > 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "the persistent variants do not split items");

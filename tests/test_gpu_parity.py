@@ -638,3 +638,20 @@ def test_layer_by_layer_launches_with_pipelining(ctx, variant, splits):
     finally:
         ctx.set_tuning(50, 0)
         ctx.set_tuning(0, 0)
+
+
+def test_scratch_merge_with_changing_item_counts():
+    """The arrival counters of the scratch-merged variants stay zero between launches whatever the launches before covered: one layer,
+    then all, then one again, through a context of its own."""
+    own = gpu_context()
+    L, B, Hq, Hkv, D, cap = 3, 8, 16, 8, 64, 200
+    oc = random_cache(L, B, Hq, Hkv, D, cap, _lens(L, B, Hkv, cap - 8, seed=5), dtype=torch.bfloat16, seed=5, rel_init="rand")
+    gc = to_device(oc)
+    scale = torch.tensor([0.1, 0.12, 0.08])
+    g = torch.Generator().manual_seed(6)
+    own.set_tuning(32, 4)
+    for i, (l0, l1) in enumerate([(0, 1), (0, 3), (2, 3), (1, 3), (0, 3)]):
+        rn = lambda h: torch.randn((l1 - l0, B, h, D), generator=g).to(torch.bfloat16)  # noqa: E731
+        _step(own, oc, gc, rn(Hq), rn(Hkv), rn(Hkv), torch.full((B,), cap + i, dtype=torch.int32), scale, 0.95, l0, l1)
+        sync_state(gc, oc)
+    own.close()
