@@ -334,6 +334,9 @@ lethe_status lethe_prefill_seed(lethe_ctx *ctx, const lethe_cache *cache, const 
  *   window > 0  : of these only slots with token_pos[i] - pos[j] < window
  *   doc_start   : of these only slots with pos[j] >= doc_start[i] (packed documents: where token i's document begins)
  * A token that no slot is visible to gets out = 0, lse = -inf and adds nothing to the relevance.
+ * Distances are formed in 64 bits.  On fp32 caches they are rounded to fp32 as they are; on the others a position is first
+ * rounded relative to the sequence's new tokens: exact where the new tokens of a sequence lie within 2^24 of one another
+ * and the keys within 2^24 of them, else a distance is off by up to 2^-23 of the farthest position's.
  */
 typedef struct {
     float softcap;             /* 0 = off; else 1e-4 .. 1e30                   */
@@ -401,8 +404,13 @@ lethe_status lethe_rotate(lethe_ctx *ctx, const lethe_rotary *rotary, int32_t dt
  * LETHE_ERR_INVALID_ARG.  Slots at or beyond len may hold anything, and a hidden key may be NaN or infinite.  A value row
  * below len must be finite even where it is hidden: it is multiplied by probabilities that are zero, and a NaN or an
  * infinity in it can reach every token of its sequence.  out must not overlap q.
- * Scratch: 4 bytes per (layer, token, query head), up to about 80 MB of partial results, and for chunks of at most 16
- * (token, head of a group) rows up to 1 GB of parked logits (64 bytes per slot at most).
+ * Scratch: 4 bytes per (layer, token, query head); up to about 80 MB of partial results; some 16 bytes per item and block of
+ * max_chunk tokens (a block is 8 tokens at least); with a window, doc_start or prefix_len 12 bytes per item and 32 slots of
+ * capacity (fp32 caches; 128 slots on the others); with `rotary` a copy of q and of k_new; and for chunks of at
+ * most 16 (token, head of a group) rows their logits, 4 bytes per row and slot of capacity, where that is no more than 1 GB
+ * (beyond, the relevance is computed from the keys again, which takes longer: 107 us instead of 79 for single tokens of 32
+ * sequences).
+ * On a quantised cache the rounding of the probabilities (2^-8 of each weight at most) is coarser than lethe_decode_attend's.
  */
 lethe_status lethe_chunk_attend(lethe_ctx *ctx, const lethe_cache *cache, int layer_begin, int layer_end,
                                 const int32_t *chunk_start, int n_tokens, int max_chunk, const void *q,

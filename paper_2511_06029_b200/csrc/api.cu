@@ -1221,9 +1221,10 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
     a.n_cta = simt ? 2 * ctx->sm_count : ctx->sm_count;
     a.min_per = simt ? 3 : 2;  // every part costs its merge; and both softmax groups of a CTA have something to do
     a.QT = (max_chunk + a.TU - 1) / a.TU;
-    // Beginning and ending a unit with two row tiles costs as much as about three of its tiles (8192-token prompt: 970 us with 3,
-    // 1036 with 1, 1080 with none; documents 654 / 658 / 664), about one where the scores are capped (528 / 520 / 515 us), nothing beside
-    // tiles that threads convert (218 / 211 / 208).
+    // Beginning and ending a unit with two row tiles costs as much as about three of its tiles (8192-token prompt: 999 us with 3,
+    // 1025 with 1, 1054 with none; documents 274 / 280 / 284).  Less where scores are capped, whose tiles take longer, and nothing beside
+    // tiles that threads convert; there one count is as good as another by now (capped chunks with slopes 242 us with 3, 1 and none, an
+    // e4m3 chunk 142 to 150 either way).
     a.pad = simt || c->dtype != LETHE_BF16 ? 0 : a.softcap > 0.f ? 1 : 3;
     a.tile = simt ? 32 : kChunkTile;
     a.cap_tiles = (a.cap_tokens + a.tile - 1) / a.tile;

@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_append_kernel(const __grid
 // first tile with a key that its farthest-reaching token may still see and the end of what the prefix opens.  Conservative
 // whatever the order of the positions is; the attention tests every key that is left.  The last block to finish plans.  Bound by
 // latency (256 items of about 2000 slots: 8 us, most of it the plan and the code's first fetch); 32 warps to an item because a long
-// prompt has one item per KV head only (8 warps: packed documents of 4096 tokens 424 us instead of 372).
+// prompt has one item per KV head only (8 warps: packed documents of 4096 tokens 298 us instead of 274).
 __global__ void __launch_bounds__(kRangeThreads) chunk_range_kernel(const __grid_constant__ ChunkArgs a) {
     __shared__ int last;
     dependency_wait();
@@ -408,8 +408,8 @@ __global__ void __launch_bounds__(kPrepThreads) chunk_combine_kernel(const __gri
 
 // Eq. 5 from parked logits: a thread takes four keys, adds up exp2(logit - lse + log2 of the row's decay weight) over the chunk's rows.
 // Bound by memory: 4 bytes per row and key read, against 2 D of the key itself for the transposed product.  Chunks of up to 16 rows
-// take it: single tokens of 32 sequences with a window and a cap 80 us for the call, 167 with the transposed product; four drafted
-// tokens of 8 sequences 42 against 48.
+// take it: single tokens of 32 sequences with a window and a cap 79 us for the call, 107 with the transposed product; four drafted
+// tokens of 8 sequences 39 against 48.
 constexpr int kParkKeys = 4 * kPrepThreads;
 __global__ void __launch_bounds__(kPrepThreads) chunk_rel_parked_kernel(const __grid_constant__ ChunkArgs a) {
     __shared__ float bias[kChunkQuadRows];

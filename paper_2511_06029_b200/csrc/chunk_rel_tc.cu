@@ -10,8 +10,8 @@
 // A unit is a pair of key tiles of one item (two groups of four warps), its steps are the query tiles that meet it; the plan gives
 // every CTA an equal stretch of the line of all steps (a causal prompt's first keys meet every token, its last keys few), and the
 // parts of a unit that CTAs share are added up afterwards in order.  Two CTAs to an SM cover each other's hand-offs; with slopes one,
-// which then has registers for all that its columns bring along (512-token chunks with a cap and slopes 65 us with two that spill, 54
-// with one; a cap alone 70 us with two, 88 with one).  Warp 8 issues the MMAs, warp 9 loads tiles by TMA; tiles that TMA cannot take
+// which then has registers for all that its columns bring along (calls of 512-token chunks with a cap and slopes 262 us with two that
+// spill, 242 with one; with a cap alone 205 us with two, 217 with one).  Warp 8 issues the MMAs, warp 9 loads tiles by TMA; tiles that TMA cannot take
 // (byte caches, odd pages) are gathered by the softmax warps, once per unit.  An 8192-token prompt of 32 heads over 8: about 360 us,
 // 1250 clocks of a tile, of which the special-function unit has 768 with a quarter of the exponentials on the FMA pipes.
 #include "chunk_tc.cuh"
@@ -23,7 +23,8 @@ constexpr int kSoftWarps = 8;
 constexpr int kMmaWarp = 8;
 constexpr int kLoadWarp = 9;
 constexpr int kThreads = 10 * 32;
-// Of eight exponentials, computed by polynomial: an 8192-token prompt takes 925 us with none, 907 with two, 1000 with four.
+// Of eight exponentials, computed by polynomial: an 8192-token prompt takes 925 us with none, 907 with two, 1000 with four in runs short
+// enough that the clock holds; where the power cap lowers it 996, 999 and 1058.
 constexpr int kFmaShare = 2;
 constexpr int kTmemCols = 256;  // one logit tile per group
 
@@ -324,8 +325,8 @@ __global__ void __launch_bounds__(kThreads, MOD == kSloped ? 1 : 2) chunk_tc_rel
                 if (j >= it.n) to = 0;
                 if (!warp_wait(&sh.s_full[g], n_s++, abort_flag, limit)) return false;
                 tc_after();
-                // rolled where there is more than the causal mask: unrolled, the code outgrows the instruction cache (packed documents 287
-                // -> 301 us); in narrow pieces where scores are shaped: 32 columns spill
+                // rolled where there is more than the causal mask: unrolled, the code outgrows the instruction cache (packed documents 274
+                // -> 287 us); in narrow pieces where scores are shaped: 32 columns spill
                 constexpr int W = shaped(MOD) ? 16 : 32;
 #pragma unroll (MOD ? 1 : 4)
                 for (int ch = 0; ch < kTile; ch += W) {

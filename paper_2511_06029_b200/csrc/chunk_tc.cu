@@ -24,8 +24,8 @@
 // Measured (bf16, 32 query over 8 KV heads of 128): an 8192-token prompt in 525 us, 1.05 PFLOP/s on the two products, 0.64 of a large
 // GEMM's rate; 512 tokens behind 1024 of 8 sequences 105 us.  A step of a pair takes about 3950 clocks: 2950 are the tensor pipe's (the
 // 64-column products bound by reading Q), the rest is where both groups' exponentials (1000 of a 64-column job) and hand-offs do
-// not fit under it.  (A quarter of the exponentials on the FMA pipes, as in the relevance kernel, gains nothing
-// here and costs code: packed documents 286 us instead of 278.)
+// not fit under it.  (A quarter of the exponentials on the FMA pipes, as in the relevance kernel, gained nothing
+// here and cost code.)
 //
 // Roundings: the probabilities to bf16 (the products' operands share a type; half a step is 2^-8 of a weight, and the sum l is taken
 // before, in fp32), the outputs to bf16 last.

@@ -4,8 +4,8 @@
 // queries first, then keys), so the cosines and sines of the token's pairs are computed once per block, while the rows it has
 // already asked for are on their way.  Angles: position x frequency is formed in turns as a 64-bit fraction, where the integer
 // product's overflow is the reduction modulo one turn; the fraction is rounded to fp32 last.
-// Measured: 8192 tokens of 32 + 8 heads of 128 in bf16, 168 MB both ways, 31 us = 5.4 TB/s, 0.83 of the copy rate (41 us with one
-// task per thread); eight tokens 2.6 us on the device, 8 for a call.
+// Measured: 8192 tokens of 32 + 8 heads of 128 in bf16, 168 MB both ways, 31 us = 5.4 TB/s, 0.83 of the copy rate (46 us with 16 rows
+// per block and one task per thread); eight tokens 2.6 us on the device, 8 for a call.
 #include "common.cuh"
 #include "rotate.cuh"
 
@@ -172,7 +172,9 @@ cudaError_t launch_t(const RotateArgs& a, cudaStream_t stream) {
 cudaError_t launch_rotate(const RotateArgs& args, bool f32, cudaStream_t stream) {
     RotateArgs a = args;
     // Few tokens: many small blocks, for the latency.  Many: more bytes in flight per thread and the angles once per token (8192
-    // tokens of 32 + 8 heads of 128: 31 us = 5.4 TB/s, against 41 us with 16 rows and one task, 36 us with 24 or 48 rows).
+    // tokens of 32 + 8 heads of 128: 31 us = 5.4 TB/s, against 46 us with 16 rows and one task, 36 us with 24 or 48 rows).  The bound
+    // between the two lies somewhere between 8 and 8192 tokens, where they were measured.  A block has one token's rows only, so a
+    // model of few or narrow heads leaves some of its threads idle.
     a.rows_per_block = a.n_tokens < 1024 ? kFewRows : kManyRows;
     return f32 ? launch_t<float>(a, stream) : launch_t<__nv_bfloat16>(a, stream);
 }
