@@ -570,15 +570,16 @@ def test_long_chunk_of_many_units(ctx):
     check(ctx, st, ref.make_chunk(st, [1111]))
 
 
-@pytest.mark.parametrize("D,softcap", [(64, 0.0), (64, 20.0), (128, 0.0)])
-def test_single_tile_units_after_pairs(ctx, D, softcap):
+@pytest.mark.parametrize("D,softcap,dtype", [(64, 0.0, BF16), (64, 20.0, BF16), (128, 0.0, BF16), (128, 0.0, E4M3)])
+@pytest.mark.parametrize("short", [(20, 9), (3, 2), (3, 20)])        # one row tile each, or at most 16 rows
+def test_single_tile_units_after_pairs(ctx, D, softcap, dtype, short):
     """Units of two row tiles with several key tiles, each followed by two of one row tile and one key tile (in which a CTA's second
     softmax group has nothing to do), so that most CTAs walk pair, short, short.  The second group must not run ahead of the first."""
     L, groups, Hq = 2, 100, 4
-    new = [64, 20, 9] * groups
+    new = [64, *short] * groups
     B = len(new)
     cached = torch.tensor([600, 100, 3] * groups).view(1, B, 1).expand(L, B, 1)
-    st = ref.State(L, B, Hq, 1, D, 664, cached, BF16, seed=D)
+    st = ref.State(L, B, Hq, 1, D, 664, cached, dtype, seed=D)
     ch = ref.make_chunk(st, new, seed=4)
     first = st.device_cache()
     scale = [0.1, 0.07]
