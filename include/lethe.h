@@ -23,6 +23,10 @@
  *   lethe_chunk_attend       a step of several new tokens per sequence (chunks of prompts, drafted tokens, mixed
  *                            batches), also with modified scores
  *   lethe_rotate             rotary positions with several axes for the queries and keys of such a step
+ *   lethe_append             new rows into a cache without attending, rotated on the way
+ *   lethe_block_append, lethe_block_attend, lethe_block_select, lethe_block_read
+ *                            a cache in 8 bits with a scale for each block of tokens: filling it, a decode step over
+ *                            it or over the blocks that a cheap score selects, and reading it back
  *
  * General conventions
  *   - Unless marked HOST, every pointer is a DEVICE pointer to memory owned by the
@@ -417,6 +421,102 @@ lethe_status lethe_chunk_attend(lethe_ctx *ctx, const lethe_cache *cache, int la
                                 const void *k_new, const void *v_new, const int32_t *token_pos, const float *scale,
                                 double gamma, const lethe_score_mod *mod, const lethe_rotary *rotary, void *out, float *lse,
                                 void *stream);
+
+/*
+ * New rows into the cache without attending: a prompt whose attention another kernel computes (lethe_prefill_seed wants its
+ * keys in the cache), tokens of a step that is attended later.  Layers [layer_begin, layer_end); chunk_start, n_tokens,
+ * max_chunk, k_new, v_new and token_pos as in lethe_chunk_attend (all required).  Per item with n = len and T = T_b: rows go to
+ * slots n .. n+T-1 in the cache's storage type, pos = token_pos, rel = 0, len = n + T.
+ *   rotary      NULL: k_new comes rotated; else it is rotated on the way, as by lethe_rotate
+ *   q, q_out    [nl][n_tokens][Hq][D], both NULL or both given (with rotary): the same tokens' queries, rotated in the same
+ *               launch.  q_out may be q; it must not overlap anything else.
+ * What the device refuses is refused as in lethe_chunk_attend: an item that cannot take its T tokens stays as it is
+ * (LETHE_ERR_CAPACITY; its queries are rotated all the same), a row whose page id lies outside the pool is dropped (LETHE_ERR_PAGE),
+ * a malformed chunk_start makes the call do nothing (LETHE_ERR_INVALID_ARG).  No scratch.
+ */
+lethe_status lethe_append(lethe_ctx *ctx, const lethe_cache *cache, int layer_begin, int layer_end, const int32_t *chunk_start,
+                          int n_tokens, int max_chunk, const void *q, const void *k_new, const void *v_new,
+                          const int32_t *token_pos, const lethe_rotary *rotary, void *q_out, void *stream);
+
+/*
+ * A cache held in 8 bits with one scale for each block of block_tokens tokens of a KV head, keys and values apart: the
+ * counterpart of pruning, where every token stays, at half the bytes, and a query may read a selection of the blocks.  (The
+ * paper has no such cache.)
+ *   - Slot j of an item belongs to block j / block_tokens.  The first len / block_tokens blocks are full; a full block is
+ *     written once, when its last token arrives, and never changes afterwards.  It holds whole numbers x in -127 .. 127 that
+ *     stand for scale * x.  The len % block_tokens newest tokens lie in the item's open block, as bf16 rows.
+ *   - A block's scale is amax / 127 in fp32, amax its largest finite magnitude (taken from the rows as bf16); x =
+ *     rint(row * (127 / amax)), limited to -127 .. 127; NaN is stored as 0, an infinity as the largest value of its sign.  Where
+ *     amax < 2^-100 scale and block are 0.  So a value is off by at most scale * (0.5 + 2^-16).  What a cache holds does not
+ *     depend on how its tokens were split over calls.
+ *   - k_range holds the least and the greatest x of each element over a full block's keys.
+ * A caller that fills a cache itself keeps to this: scales finite and not negative (those of one item's value blocks within a
+ * factor of 2^100 of one another, zeros apart).
+ */
+typedef struct {
+    int32_t n_layers, batch, n_q_heads, n_kv_heads;
+    int32_t head_dim;       /* 64 or 128; q, k_new, v_new, out and the open blocks are bf16                       */
+    int32_t layout;         /* LETHE_CONTIG or LETHE_PAGED: a page is a block                                     */
+    int32_t capacity;       /* blocks (page-table entries) per item; an item holds capacity * block_tokens tokens */
+    int32_t block_tokens;   /* 16, 32, 64 or 128                                                                  */
+    int8_t *k, *v;          /* CONTIG [L][B][Hkv][capacity][block_tokens][D], PAGED [n_pages][block_tokens][D]    */
+    float *k_scale, *v_scale; /* CONTIG [L][B][Hkv][capacity], PAGED [n_pages]                                    */
+    int8_t *k_range;        /* CONTIG [L][B][Hkv][capacity][2][D], PAGED [n_pages][2][D]: least, greatest; may be NULL
+                               where nothing is selected                                                          */
+    void *k_open, *v_open;  /* [L][B][Hkv][block_tokens][D] bf16: row i is slot len / block_tokens * block_tokens + i */
+    int32_t *len;           /* [L][B][Hkv] tokens per item                                                        */
+    const int32_t *page_table; /* PAGED: [L][B][Hkv][capacity] page ids (never written by the library)            */
+    int64_t n_pages;        /* PAGED: pages in the pools                                                          */
+} lethe_block_cache;
+/* k, v, k_range, k_open and v_open must be 16-byte aligned.  Items may share full blocks (one page in several tables); calls
+ * that append must give every new block a page of its own. */
+
+/*
+ * lethe_append for a block cache: new rows, rotated on the way, go to the open block; a block that they fill is quantised in
+ * the same launch.  Arguments as in lethe_append.  Rows of the open block from len % block_tokens on stay as they were.  A
+ * block whose page id lies outside the pool is dropped (LETHE_ERR_PAGE; len grows all the same).
+ */
+lethe_status lethe_block_append(lethe_ctx *ctx, const lethe_block_cache *cache, int layer_begin, int layer_end,
+                                const int32_t *chunk_start, int n_tokens, int max_chunk, const void *q, const void *k_new,
+                                const void *v_new, const lethe_rotary *rotary, void *q_out, void *stream);
+
+/*
+ * Reads slots back as bf16 (for what works on ordinary caches: the result has the layout of a contiguous one).
+ *   slot_begin [B] int32 (DEVICE) or NULL (0): first slot to read of each sequence
+ *   k_out, v_out [nl][B][Hkv][n_slots][D] bf16: scale * x rounded once, or the open row; slots below 0 and from len on, and
+ *   blocks whose page id lies outside the pool (LETHE_ERR_PAGE), read as zeros
+ */
+lethe_status lethe_block_read(lethe_ctx *ctx, const lethe_block_cache *cache, int layer_begin, int layer_end,
+                              const int32_t *slot_begin, int n_slots, void *k_out, void *v_out, void *stream);
+
+/*
+ * Chooses, for the query token of each (layer, sequence, KV head), n_select of the item's full blocks.  With G the heads of
+ * the KV head's group, amax the largest finite magnitude of their queries and qx = rint(q * (127 / amax)) limited to -127 .. 127
+ * (0 where amax < 2^-100 and for NaN), a block's score is
+ *     k_scale * sum over the group's heads and elements of max(qx * least, qx * greatest)
+ * an upper bound of what its keys can reach, summed over the heads (for a positive softmax scale).  The sum is a whole number
+ * below 2^24 and the product is rounded once, in fp32: the choice has one correct value.
+ *   n_select, sink, recent   the first `sink` and the last `recent` full blocks are always chosen; sink + recent <= n_select
+ *   selected [nl][B][Hkv][n_select] int32   the chosen blocks in ascending order (equal scores: the lower block first), then -1
+ * An item with at most n_select full blocks has them all.  q [nl][B][Hq][D] bf16.  A block whose page id lies outside the pool
+ * scores as zero (LETHE_ERR_PAGE).  Scratch: 4 bytes for each block of capacity of each item of the call.
+ */
+lethe_status lethe_block_select(lethe_ctx *ctx, const lethe_block_cache *cache, int layer_begin, int layer_end, const void *q,
+                                int n_select, int sink, int recent, int32_t *selected, void *stream);
+
+/*
+ * Softmax attention of one query token per sequence over a block cache: q, scale, out and lse as in lethe_decode_attend
+ * (nothing is appended, no relevance is kept: nothing is evicted from such a cache).
+ *   selected  NULL: over all of the item's tokens; else [nl][B][Hkv][n_select] as lethe_block_select leaves it: over the full
+ *             blocks that the first min(n_select, full blocks) entries name (a negative entry names none, a repeated one counts
+ *             again, one that is not a full block is left out and records LETHE_ERR_INVALID_ARG), and the open block
+ * An item with nothing to attend over gives out = 0, lse = -inf.  A block whose page id lies outside the pool is left out
+ * (LETHE_ERR_PAGE).  Sums, softmax statistics and outputs are held in fp32; full blocks take part as exact f16 values with
+ * probabilities rounded to f16, open rows with probabilities in two bf16 terms.  Scratch: 4 bytes per item and up to 25 MB of
+ * partial results.  The same inputs give the same bits.
+ */
+lethe_status lethe_block_attend(lethe_ctx *ctx, const lethe_block_cache *cache, int layer_begin, int layer_end, const void *q,
+                                const float *scale, const int32_t *selected, int n_select, void *out, float *lse, void *stream);
 
 /*
  * lethe_rasr_prune without a context and without any allocation.  (The paper has no counterpart: this entry

@@ -24,7 +24,8 @@ VARIANT_AUTO, VARIANT_SIMT, VARIANT_MMA4, VARIANT_MMA8 = 0, 1, 2, 3
 EXPORTS = ["lethe_create", "lethe_destroy", "lethe_last_error", "lethe_poll_status", "lethe_set_tuning", "lethe_set_wait_limit",
            "lethe_decode_attend", "lethe_decode_attend_host", "lethe_estimate_sparsity", "lethe_alloc_budgets",
            "lethe_rasr_prune", "lethe_rasr_prune_static", "lethe_segment_prune", "lethe_prefill_seed",
-           "lethe_collapsed_prune", "lethe_chunk_attend", "lethe_rotate"]
+           "lethe_collapsed_prune", "lethe_chunk_attend", "lethe_rotate", "lethe_append", "lethe_block_append", "lethe_block_read",
+           "lethe_block_select", "lethe_block_attend"]
 
 
 class LetheError(RuntimeError):
@@ -53,6 +54,17 @@ class lethe_rotary(ctypes.Structure):
     _fields_ = [("rot_dim", ctypes.c_int32), ("style", ctypes.c_int32), ("n_axes", ctypes.c_int32),
                 ("pair_axis", ctypes.POINTER(ctypes.c_int32)), ("pair_freq", ctypes.POINTER(ctypes.c_double)),
                 ("axis_pos", ctypes.c_void_p)]
+
+
+class lethe_block_cache(ctypes.Structure):
+    _fields_ = [
+        ("n_layers", ctypes.c_int32), ("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+        ("capacity", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("k_range", ctypes.c_void_p), ("k_open", ctypes.c_void_p), ("v_open", ctypes.c_void_p), ("len", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+    ]
 
 
 _lib = None
@@ -105,6 +117,17 @@ def load() -> ctypes.CDLL:
     lib.lethe_rotate.restype = ctypes.c_int
     lib.lethe_rotate.argtypes = [vp, ctypes.POINTER(lethe_rotary), i32, i32, ctypes.c_int, ctypes.c_int, ctypes.c_int,
                                  ctypes.c_int, vp, vp, i32, vp, vp, vp]
+    bp, rp, fp = ctypes.POINTER(lethe_block_cache), ctypes.POINTER(lethe_rotary), ctypes.POINTER(ctypes.c_float)
+    lib.lethe_append.restype = ctypes.c_int
+    lib.lethe_append.argtypes = [vp, cp, ctypes.c_int, ctypes.c_int, vp, ctypes.c_int, ctypes.c_int, vp, vp, vp, vp, rp, vp, vp]
+    lib.lethe_block_append.restype = ctypes.c_int
+    lib.lethe_block_append.argtypes = [vp, bp, ctypes.c_int, ctypes.c_int, vp, ctypes.c_int, ctypes.c_int, vp, vp, vp, rp, vp, vp]
+    lib.lethe_block_read.restype = ctypes.c_int
+    lib.lethe_block_read.argtypes = [vp, bp, ctypes.c_int, ctypes.c_int, vp, ctypes.c_int, vp, vp, vp]
+    lib.lethe_block_select.restype = ctypes.c_int
+    lib.lethe_block_select.argtypes = [vp, bp, ctypes.c_int, ctypes.c_int, vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, vp]
+    lib.lethe_block_attend.restype = ctypes.c_int
+    lib.lethe_block_attend.argtypes = [vp, bp, ctypes.c_int, ctypes.c_int, vp, fp, vp, ctypes.c_int, vp, vp, vp]
     lib.lethe_rasr_prune_static.restype = ctypes.c_int
     lib.lethe_rasr_prune_static.argtypes = [cp, vp, i32, i32, vp, i32, vp, vp]
     _lib = lib
@@ -171,6 +194,48 @@ class Cache:
     @property
     def cap_tokens(self) -> int:
         return self.capacity * self.page_tokens if self.page_table is not None else self.capacity
+
+
+class BlockCache:
+    """Device tensors of a cache in 8 bits with a scale for each block of tokens, plus the C descriptor that points at them (the
+    tensors stay owned here)."""
+
+    def __init__(self, n_q_heads: int, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                 k_range: Optional[torch.Tensor], k_open: torch.Tensor, v_open: torch.Tensor, len_: torch.Tensor,
+                 page_table: Optional[torch.Tensor] = None):
+        """k, v int8 [L][B][Hkv][capacity][block_tokens][D], or pools [pages][block_tokens][D] with page_table [L][B][Hkv][capacity]
+        int32; k_scale, v_scale float32 and k_range int8 [..][2][D] (or None) by block likewise; k_open, v_open bfloat16
+        [L][B][Hkv][block_tokens][D]; len_ int32 [L][B][Hkv]."""
+        self.k, self.v, self.k_scale, self.v_scale, self.k_range = k, v, k_scale, v_scale, k_range
+        self.k_open, self.v_open, self.len, self.page_table = k_open, v_open, len_, page_table
+        for t in (k, v, k_scale, v_scale, k_range, k_open, v_open, len_, page_table):
+            assert t is None or (t.is_cuda and t.is_contiguous() and t.device == k.device)
+        assert k.dtype == v.dtype == torch.int8 and k.shape == v.shape and (k_range is None or k_range.dtype == torch.int8)
+        assert k_scale.dtype == v_scale.dtype == torch.float32 and k_open.dtype == v_open.dtype == torch.bfloat16
+        assert len_.dtype == torch.int32 and len_.dim() == 3
+        L, B, Hkv = len_.shape
+        lead, (T, D) = tuple(k.shape[:-2]), k.shape[-2:]
+        if page_table is None:
+            assert len(lead) == 4 and lead[:3] == (L, B, Hkv)
+            cap, layout, n_pages = lead[3], CONTIG, 0
+        else:
+            assert len(lead) == 1 and page_table.dtype == torch.int32 and page_table.dim() == 4 and tuple(page_table.shape[:3]) == (L, B, Hkv)
+            cap, layout, n_pages = page_table.shape[3], PAGED, lead[0]
+        assert tuple(k_scale.shape) == tuple(v_scale.shape) == lead and (k_range is None or tuple(k_range.shape) == lead + (2, D))
+        assert tuple(k_open.shape) == tuple(v_open.shape) == (L, B, Hkv, T, D)
+        self.n_layers, self.batch, self.n_kv_heads, self.n_q_heads, self.head_dim = L, B, Hkv, n_q_heads, D
+        self.capacity, self.block_tokens = cap, T
+        ptr = [None if t is None else t.data_ptr() for t in (k, v, k_scale, v_scale, k_range, k_open, v_open, len_, page_table)]
+        self.c = lethe_block_cache(L, B, n_q_heads, Hkv, D, layout, cap, T, *ptr, n_pages)
+        self.ref = ctypes.byref(self.c)
+
+    @property
+    def device(self):
+        return self.k.device
+
+    @property
+    def cap_tokens(self) -> int:
+        return self.capacity * self.block_tokens
 
 
 class ScoreMod:
@@ -380,3 +445,71 @@ class Context:
                                                 None if mod is None else ctypes.byref(mod.c),
                                                 None if rotary is None else ctypes.byref(rotary.c), _dp(out), _dp(lse),
                                                 _stream(self.device)))
+
+    def _append_args(self, cache, nl, chunk_start, act, k_new, v_new, rotary, q, q_out):
+        """Checks what append and block_append have in common; the number of tokens."""
+        n = k_new.shape[1]
+        assert chunk_start.is_cuda and chunk_start.is_contiguous() and chunk_start.dtype == torch.int32 and chunk_start.numel() == cache.batch + 1
+        for t in (k_new, v_new):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == act and tuple(t.shape) == (nl, n, cache.n_kv_heads, cache.head_dim)
+        assert (q is None) == (q_out is None)
+        for t in (q, q_out):
+            assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == act and tuple(t.shape) == (nl, n, cache.n_q_heads, cache.head_dim))
+        assert rotary is None or rotary.n_tokens == n
+        return n
+
+    def append(self, cache: Cache, layer_begin: int, layer_end: int, chunk_start: torch.Tensor, max_chunk: int, k_new, v_new, token_pos,
+               rotary: Optional[Rotary] = None, q=None, q_out=None):
+        """k_new, v_new [nl][n_tokens][Hkv][D]; chunk_start [B + 1] and token_pos [n_tokens] int32; q, q_out [nl][n_tokens][Hq][D] (with
+        rotary) or None.  All contiguous device tensors."""
+        n = self._append_args(cache, layer_end - layer_begin, chunk_start, cache.act_dtype, k_new, v_new, rotary, q, q_out)
+        assert token_pos.is_cuda and token_pos.is_contiguous() and token_pos.dtype == torch.int32 and token_pos.numel() == n
+        self._check(self.lib.lethe_append(self.h, ctypes.byref(cache.c), layer_begin, layer_end, chunk_start.data_ptr(), n, max_chunk,
+                                          None if q is None else q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), token_pos.data_ptr(),
+                                          None if rotary is None else rotary.ref, None if q is None else q_out.data_ptr(),
+                                          torch.cuda.current_stream(self.device).cuda_stream))
+
+    def block_append(self, cache: BlockCache, layer_begin: int, layer_end: int, chunk_start: torch.Tensor, max_chunk: int, k_new, v_new,
+                     rotary: Optional[Rotary] = None, q=None, q_out=None):
+        """As append, all bfloat16."""
+        n = self._append_args(cache, layer_end - layer_begin, chunk_start, torch.bfloat16, k_new, v_new, rotary, q, q_out)
+        self._check(self.lib.lethe_block_append(self.h, cache.ref, layer_begin, layer_end, chunk_start.data_ptr(), n, max_chunk,
+                                                None if q is None else q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+                                                None if rotary is None else rotary.ref, None if q is None else q_out.data_ptr(),
+                                                torch.cuda.current_stream(self.device).cuda_stream))
+
+    def block_read(self, cache: BlockCache, layer_begin: int, layer_end: int, slot_begin: Optional[torch.Tensor], k_out, v_out):
+        """k_out, v_out bfloat16 [nl][B][Hkv][n_slots][D]; slot_begin [B] int32 on the device, or None for slot 0."""
+        lead = (layer_end - layer_begin, cache.batch, cache.n_kv_heads)
+        for t in (k_out, v_out):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16 and t.dim() == 5 and tuple(t.shape[:3]) == lead
+            assert t.shape[3] == k_out.shape[3] and t.shape[4] == cache.head_dim
+        assert slot_begin is None or (slot_begin.is_cuda and slot_begin.is_contiguous() and slot_begin.dtype == torch.int32 and slot_begin.numel() == cache.batch)
+        self._check(self.lib.lethe_block_read(self.h, cache.ref, layer_begin, layer_end, None if slot_begin is None else slot_begin.data_ptr(),
+                                              k_out.shape[3], k_out.data_ptr(), v_out.data_ptr(), torch.cuda.current_stream(self.device).cuda_stream))
+
+    def _block_query(self, cache, layer_begin, layer_end, selected, *tensors):
+        lead = (layer_end - layer_begin, cache.batch)
+        for t in tensors:
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16 and tuple(t.shape) == lead + (cache.n_q_heads, cache.head_dim)
+        if selected is not None:
+            assert selected.is_cuda and selected.is_contiguous() and selected.dtype == torch.int32 and selected.dim() == 4
+            assert tuple(selected.shape[:3]) == lead + (cache.n_kv_heads,)
+
+    def block_select(self, cache: BlockCache, layer_begin: int, layer_end: int, q, sink: int, recent: int, selected: torch.Tensor):
+        """selected [nl][B][Hkv][n_select] int32 is written: the chosen blocks in ascending order, then -1."""
+        self._block_query(cache, layer_begin, layer_end, selected, q)
+        self._check(self.lib.lethe_block_select(self.h, cache.ref, layer_begin, layer_end, q.data_ptr(), selected.shape[3], sink, recent,
+                                                selected.data_ptr(), torch.cuda.current_stream(self.device).cuda_stream))
+
+    def block_attend(self, cache: BlockCache, layer_begin: int, layer_end: int, q, scale, out, lse=None, selected: Optional[torch.Tensor] = None,
+                     scale_c=None):
+        """q, out [nl][B][Hq][D] bfloat16; scale one float per layer of the cache; lse [nl][B][Hq] float32 or None; selected as
+        block_select leaves it, or None for all blocks."""
+        self._block_query(cache, layer_begin, layer_end, selected, q, out)
+        assert lse is None or (lse.is_cuda and lse.is_contiguous() and lse.dtype == torch.float32 and tuple(lse.shape) == tuple(q.shape[:3]))
+        sc = scale_c if scale_c is not None else self._scale(scale)
+        self._check(self.lib.lethe_block_attend(self.h, cache.ref, layer_begin, layer_end, q.data_ptr(), sc,
+                                                None if selected is None else selected.data_ptr(), 0 if selected is None else selected.shape[3],
+                                                out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                                torch.cuda.current_stream(self.device).cuda_stream))

@@ -9,6 +9,7 @@
 #include "prefill.cuh"
 #include "chunk_tc.cuh"
 #include "rotate.cuh"
+#include "block_attend.cuh"
 
 namespace lethe {
 cudaError_t launch_attend_simt(const AttendArgs& a, int dtype, int D, bool paged, cudaStream_t stream);
@@ -112,6 +113,8 @@ struct lethe_ctx {
     size_t flat_bytes;
     void* flat_cnt;  // its arrival counters: zero between launches, so nothing else is ever kept there
     size_t flat_cnt_bytes;
+    void* block_cnt;  // arrival counters of the block-cache kernels: zero between launches, so nothing else is ever kept there
+    size_t block_cnt_bytes;
     void* staging;  // device staging of lethe_decode_attend_host
     size_t staging_bytes;
     // lethe_decode_attend_host: upload / download streams and the events that chain them to the caller's stream
@@ -310,6 +313,7 @@ void lethe_destroy(lethe_ctx* ctx) {
     }
     if (ctx->flat) cudaFree(ctx->flat);
     if (ctx->flat_cnt) cudaFree(ctx->flat_cnt);
+    if (ctx->block_cnt) cudaFree(ctx->block_cnt);
     delete ctx;
 }
 
@@ -1311,6 +1315,231 @@ lethe_status lethe_chunk_attend(lethe_ctx* ctx, const lethe_cache* c, int layer_
         }
     }
     if (e != cudaSuccess) return cuda_fail(ctx, e, "chunk_attend launch");
+    return LETHE_OK;
+}
+
+// What lethe_append and lethe_block_append ask of their new rows; fills `in`.  kv_heads rows of K per token.
+static lethe_status new_rows(lethe_ctx* ctx, int32_t dtype, int head_dim, int nl, int B, int Hq, int Hkv, const int32_t* chunk_start, int n_tokens,
+                             int max_chunk, const void* q, const void* k_new, const void* v_new, const lethe_rotary* rotary, void* q_out, NewRows* in) {
+    if (!chunk_start || !k_new || !v_new) return fail(ctx, LETHE_ERR_INVALID_ARG, "chunk_start, k_new and v_new are required");
+    if (max_chunk < 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "max_chunk must be positive");
+    if ((q == nullptr) != (q_out == nullptr)) return fail(ctx, LETHE_ERR_INVALID_ARG, "q and q_out go together");
+    if (q && !rotary) return fail(ctx, LETHE_ERR_INVALID_ARG, "queries are taken along to be rotated: rotary is required with q");
+    if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)q_out) & 15)
+        return fail(ctx, LETHE_ERR_INVALID_ARG, "q, k_new, v_new and q_out must be 16-byte aligned");
+    const long long rows = (long long)nl * ((q ? (long long)Hq : 0) + 2LL * Hkv);
+    if (rows > 0x7fffffffLL || rows * n_tokens > 0x7fffffffLL || (long long)nl * B * Hkv > 0x7fffffffLL / 16)
+        return fail(ctx, LETHE_ERR_UNSUPPORTED, "append: too many rows for one call; cover fewer layers");
+    const size_t eb = dtype == LETHE_F32 ? 4 : 2;
+    const size_t nq = (size_t)nl * n_tokens * Hq * head_dim * eb, nk = (size_t)nl * n_tokens * Hkv * head_dim * eb;
+    if (q && (overlap_partly(q, nq, q_out, nq) || q_out == k_new || q_out == v_new || overlap_partly(k_new, nk, q_out, nq) || overlap_partly(v_new, nk, q_out, nq)))
+        return fail(ctx, LETHE_ERR_INVALID_ARG, "q_out may only be q");
+    memset(in, 0, sizeof(*in));
+    if (rotary) {
+        RotateArgs rot;
+        lethe_status st = rotary_args(ctx, rotary, dtype, head_dim, nl, n_tokens, Hq, Hkv, 0, &rot);
+        if (st != LETHE_OK) return st;
+        in->axis_pos = rot.axis_pos;
+        in->rot_dim = rot.rot_dim;
+        in->halves = rot.halves;
+        memcpy(in->turn, rot.turn, sizeof(in->turn));
+        memcpy(in->axis, rot.axis, sizeof(in->axis));
+    }
+    in->chunk_start = chunk_start; in->q = q; in->q_out = q_out; in->k = k_new; in->v = v_new;
+    in->n_tokens = n_tokens;
+    in->max_chunk = max_chunk < n_tokens ? max_chunk : n_tokens;
+    return LETHE_OK;
+}
+
+lethe_status lethe_append(lethe_ctx* ctx, const lethe_cache* c, int layer_begin, int layer_end, const int32_t* chunk_start, int n_tokens, int max_chunk,
+                          const void* q, const void* k_new, const void* v_new, const int32_t* token_pos, const lethe_rotary* rotary, void* q_out,
+                          void* stream) {
+    lethe_status st = check_cache(ctx, c);
+    if (st != LETHE_OK) return st;
+    ctx->last_len = nullptr;  // the next decode call does not follow a decode call
+    if (layer_begin < 0 || layer_end > c->n_layers || layer_begin >= layer_end) return fail(ctx, LETHE_ERR_INVALID_ARG, "bad layer range");
+    if (c->n_layers > kMaxLayers) return fail(ctx, LETHE_ERR_UNSUPPORTED, "more than 128 layers");
+    if (n_tokens < 0) return fail(ctx, LETHE_ERR_INVALID_ARG, "n_tokens must be >= 0");
+    if (n_tokens == 0) return LETHE_OK;
+    if (!token_pos) return fail(ctx, LETHE_ERR_INVALID_ARG, "token_pos is NULL");
+    AppendArgs a;
+    memset(&a, 0, sizeof(a));
+    const int nl = layer_end - layer_begin;
+    st = new_rows(ctx, c->dtype == LETHE_F32 ? LETHE_F32 : LETHE_BF16, c->head_dim, nl, c->batch, c->n_q_heads, c->n_kv_heads, chunk_start, n_tokens,
+                  max_chunk, q, k_new, v_new, rotary, q_out, &a.in);
+    if (st != LETHE_OK) return st;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
+    a.k = c->k; a.v = c->v; a.rel = c->rel; a.pos = c->pos; a.len = c->len; a.page_table = c->page_table; a.token_pos = token_pos;
+    a.status = ctx->status;
+    a.n_pages = c->n_pages;
+    a.dtype = c->dtype; a.D = c->head_dim; a.B = c->batch; a.Hq = c->n_q_heads; a.Hkv = c->n_kv_heads;
+    a.capacity = c->capacity; a.cap_tokens = cap_tokens_of(c);
+    a.paged = c->layout == LETHE_PAGED;
+    a.page_tokens = a.paged ? c->page_tokens : 1;
+    a.layer_begin = layer_begin; a.nl = nl;
+    const bool bytes = c->dtype == LETHE_FP8_E4M3 || c->dtype == LETHE_FP8_E5M2;
+    for (int l = 0; l < c->n_layers; ++l) {
+        a.k_scale[l] = bytes && c->k_scale ? c->k_scale[l] : 1.f;
+        a.v_scale[l] = bytes && c->v_scale ? c->v_scale[l] : 1.f;
+    }
+    const cudaError_t e = launch_append(a, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "append launch");
+    return LETHE_OK;
+}
+
+// Checks of a block cache and a layer range; fills the view.
+static lethe_status block_view(lethe_ctx* ctx, const lethe_block_cache* c, int layer_begin, int layer_end, BlockView* v) {
+    if (!ctx) return LETHE_ERR_INVALID_ARG;
+    ctx->last_len = nullptr;  // the next decode call does not follow a decode call
+    if (!c) return fail(ctx, LETHE_ERR_INVALID_ARG, "cache is NULL");
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->k_open || !c->v_open || !c->len) return fail(ctx, LETHE_ERR_INVALID_ARG, "cache has a NULL tensor");
+    if (c->n_layers < 1 || c->batch < 1 || c->n_kv_heads < 1 || c->n_q_heads < 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "cache dimensions must be positive");
+    if (c->n_q_heads % c->n_kv_heads) return fail(ctx, LETHE_ERR_INVALID_ARG, "n_q_heads must be a multiple of n_kv_heads");
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(ctx, LETHE_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+    if (c->layout != LETHE_CONTIG && c->layout != LETHE_PAGED) return fail(ctx, LETHE_ERR_INVALID_ARG, "unknown layout");
+    if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64 && c->block_tokens != 128)
+        return fail(ctx, LETHE_ERR_UNSUPPORTED, "block_tokens must be 16, 32, 64 or 128");
+    if (c->capacity < 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "capacity must be positive");
+    const bool paged = c->layout == LETHE_PAGED;
+    if (paged && (!c->page_table || c->n_pages < 1)) return fail(ctx, LETHE_ERR_INVALID_ARG, "paged layout needs page_table and n_pages");
+    if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->k_range | (uintptr_t)c->k_open | (uintptr_t)c->v_open) & 15)
+        return fail(ctx, LETHE_ERR_INVALID_ARG, "k, v, k_range, k_open, v_open must be 16-byte aligned");
+    if (layer_begin < 0 || layer_end > c->n_layers || layer_begin >= layer_end) return fail(ctx, LETHE_ERR_INVALID_ARG, "bad layer range");
+    if (c->n_layers > kMaxLayers) return fail(ctx, LETHE_ERR_UNSUPPORTED, "more than 128 layers");
+    const long long heads = (long long)c->batch * c->n_kv_heads;  // below 2^62
+    if (heads > 0x7fffffffLL / 16 || heads * c->n_layers > 0x7fffffffLL / 16) return fail(ctx, LETHE_ERR_UNSUPPORTED, "too many (layer, sequence, head) items");
+    if ((long long)c->capacity * c->block_tokens > 0x7fffffffLL) return fail(ctx, LETHE_ERR_INVALID_ARG, "capacity too large");
+    memset(v, 0, sizeof(*v));
+    v->n_pages = paged ? c->n_pages : heads * c->n_layers * c->capacity;
+    // rows of the pools and blocks of a call's items are counted in 32 bits
+    if (v->n_pages > 0x7fffffffLL / c->block_tokens) return fail(ctx, LETHE_ERR_UNSUPPORTED, "too many blocks: 2^31 rows at most");
+    v->k = c->k; v->v = c->v; v->k_scale = c->k_scale; v->v_scale = c->v_scale; v->k_range = c->k_range;
+    v->k_open = (__nv_bfloat16*)c->k_open; v->v_open = (__nv_bfloat16*)c->v_open;
+    v->len = c->len; v->page_table = paged ? c->page_table : nullptr;
+    v->status = ctx->status;
+    v->B = c->batch; v->Hq = c->n_q_heads; v->Hkv = c->n_kv_heads; v->G = c->n_q_heads / c->n_kv_heads;
+    v->D = c->head_dim; v->T = c->block_tokens;
+    v->t_shift = c->block_tokens == 16 ? 4 : c->block_tokens == 32 ? 5 : c->block_tokens == 64 ? 6 : 7;
+    v->capacity = c->capacity; v->cap_tokens = c->capacity * c->block_tokens;
+    v->layer_begin = layer_begin; v->nl = layer_end - layer_begin;
+    v->n_items = (int)(v->nl * heads);
+    return LETHE_OK;
+}
+
+// Arrival counters of a call's items, zero between launches.
+static lethe_status block_counters(lethe_ctx* ctx, int n_items, int** counters, void* stream) {
+    const size_t had = ctx->block_cnt_bytes;
+    lethe_status st = ensure(ctx, &ctx->block_cnt, &ctx->block_cnt_bytes, (size_t)n_items * sizeof(int), "block counters", stream);
+    if (st != LETHE_OK) return st;
+    if (ctx->block_cnt_bytes != had && cudaMemsetAsync(ctx->block_cnt, 0, ctx->block_cnt_bytes, (cudaStream_t)stream) != cudaSuccess)
+        return fail(ctx, LETHE_ERR_CUDA, "clearing the block counters failed");
+    *counters = (int*)ctx->block_cnt;
+    return LETHE_OK;
+}
+
+lethe_status lethe_block_append(lethe_ctx* ctx, const lethe_block_cache* c, int layer_begin, int layer_end, const int32_t* chunk_start, int n_tokens,
+                                int max_chunk, const void* q, const void* k_new, const void* v_new, const lethe_rotary* rotary, void* q_out,
+                                void* stream) {
+    BlockView v;
+    lethe_status st = block_view(ctx, c, layer_begin, layer_end, &v);
+    if (st != LETHE_OK) return st;
+    if (n_tokens < 0) return fail(ctx, LETHE_ERR_INVALID_ARG, "n_tokens must be >= 0");
+    if (n_tokens == 0) return LETHE_OK;
+    NewRows in;
+    st = new_rows(ctx, LETHE_BF16, v.D, v.nl, v.B, v.Hq, v.Hkv, chunk_start, n_tokens, max_chunk, q, k_new, v_new, rotary, q_out, &in);
+    if (st != LETHE_OK) return st;
+    if ((long long)v.n_items * (in.max_chunk / v.T + 1) + (long long)n_tokens * v.nl * v.Hq > 0x7fffffffLL)
+        return fail(ctx, LETHE_ERR_UNSUPPORTED, "append: too many blocks for one call; cover fewer layers");
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
+    const cudaError_t e = launch_block_append(v, in, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "block_append launch");
+    return LETHE_OK;
+}
+
+lethe_status lethe_block_read(lethe_ctx* ctx, const lethe_block_cache* c, int layer_begin, int layer_end, const int32_t* slot_begin, int n_slots,
+                              void* k_out, void* v_out, void* stream) {
+    BlockView v;
+    lethe_status st = block_view(ctx, c, layer_begin, layer_end, &v);
+    if (st != LETHE_OK) return st;
+    if (n_slots < 0) return fail(ctx, LETHE_ERR_INVALID_ARG, "n_slots must be >= 0");
+    if (n_slots == 0) return LETHE_OK;
+    if (!k_out || !v_out) return fail(ctx, LETHE_ERR_INVALID_ARG, "k_out and v_out are required");
+    if (((uintptr_t)k_out | (uintptr_t)v_out) & 15) return fail(ctx, LETHE_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+    if ((long long)v.n_items * n_slots > 0x7fffffffLL / 16) return fail(ctx, LETHE_ERR_UNSUPPORTED, "block_read: too many rows for one call; cover fewer layers");
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
+    const cudaError_t e = launch_block_read(v, slot_begin, n_slots, k_out, v_out, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "block_read launch");
+    return LETHE_OK;
+}
+
+lethe_status lethe_block_select(lethe_ctx* ctx, const lethe_block_cache* c, int layer_begin, int layer_end, const void* q, int n_select, int sink,
+                                int recent, int32_t* selected, void* stream) {
+    BlockView v;
+    lethe_status st = block_view(ctx, c, layer_begin, layer_end, &v);
+    if (st != LETHE_OK) return st;
+    if (!q || !selected) return fail(ctx, LETHE_ERR_INVALID_ARG, "q and selected are required");
+    if ((uintptr_t)q & 15) return fail(ctx, LETHE_ERR_INVALID_ARG, "q must be 16-byte aligned");
+    if (!v.k_range) return fail(ctx, LETHE_ERR_INVALID_ARG, "selecting blocks needs k_range");
+    if (v.G > kMaxGroup) return fail(ctx, LETHE_ERR_UNSUPPORTED, "more than 8 query heads per KV head");
+    if (n_select < 1 || sink < 0 || recent < 0 || (long long)sink + recent > n_select)
+        return fail(ctx, LETHE_ERR_INVALID_ARG, "n_select must be positive, sink and recent >= 0 and together at most n_select");
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
+    // Thread blocks per item: about four for each SM, of 128 blocks at least.
+    const long long most = (v.capacity + 127) / 128;
+    int splits = (int)((4LL * ctx->sm_count + v.n_items - 1) / v.n_items);
+    if (splits > most) splits = (int)most;
+    if (splits > 64) splits = 64;
+    st = ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, (size_t)v.n_items * v.capacity * sizeof(float), "block scores", stream);
+    if (st != LETHE_OK) return st;
+    int* counters;
+    st = block_counters(ctx, v.n_items, &counters, stream);
+    if (st != LETHE_OK) return st;
+    const cudaError_t e = launch_block_select(v, q, n_select, sink, recent, (float*)ctx->scratch, counters, splits, selected, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "block_select launch");
+    return LETHE_OK;
+}
+
+lethe_status lethe_block_attend(lethe_ctx* ctx, const lethe_block_cache* c, int layer_begin, int layer_end, const void* q, const float* scale,
+                                const int32_t* selected, int n_select, void* out, float* lse, void* stream) {
+    BlockAttendArgs a;
+    memset(&a, 0, sizeof(a));
+    lethe_status st = block_view(ctx, c, layer_begin, layer_end, &a.c);
+    if (st != LETHE_OK) return st;
+    if (!q || !out || !scale) return fail(ctx, LETHE_ERR_INVALID_ARG, "q, out and scale are required");
+    if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(ctx, LETHE_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+    if (a.c.G > kMaxGroup) return fail(ctx, LETHE_ERR_UNSUPPORTED, "more than 8 query heads per KV head");
+    if (selected && n_select < 1) return fail(ctx, LETHE_ERR_INVALID_ARG, "n_select must be positive with selected");
+    const size_t q_bytes = (size_t)a.c.nl * a.c.B * a.c.Hq * a.c.D * 2;
+    if (q == out || overlap_partly(q, q_bytes, out, q_bytes)) return fail(ctx, LETHE_ERR_INVALID_ARG, "out must not overlap q");  // other CTAs read q late
+    for (int l = layer_begin; l < layer_end; ++l) {
+        if (!(fabsf(scale[l]) <= 1e30f)) return fail(ctx, LETHE_ERR_INVALID_ARG, "scale must be finite");
+        a.c.scale_log2[l] = scale[l] * 1.4426950408889634f;
+    }
+    // the line of 16-token groups is counted in 32 bits
+    const long long most = selected && n_select < c->capacity ? n_select : c->capacity;
+    if (a.c.n_items * (most * (a.c.T / 16) + 2 * (a.c.T / 16) + 1) > 0x3fffffffLL)
+        return fail(ctx, LETHE_ERR_UNSUPPORTED, "block_attend: too many blocks for one call; cover fewer layers");
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
+    BlockMaps maps;
+    if (!resolve_tma_encode(ctx) || !build_block_maps(ctx->tma_encode, a.c, &maps)) return fail(ctx, LETHE_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+    a.q = (const __nv_bfloat16*)q; a.selected = selected; a.out = (__nv_bfloat16*)out; a.lse = lse;
+    a.n_select = selected ? n_select : 0;
+    a.n_cta = ctx->sm_count;
+    a.wait_limit = ctx->wait_limit ? ctx->wait_limit : 400000;
+    const size_t warp_bytes = (size_t)a.n_cta * kBlockWarps * kBlockPart * sizeof(float), cta_bytes = (size_t)a.n_cta * 2 * kBlockPart * sizeof(float);
+    st = ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, warp_bytes + cta_bytes, "block attention scratch", stream);
+    if (st != LETHE_OK) return st;
+    a.warp_part = (float*)ctx->scratch;
+    a.cta_part = (float*)((char*)ctx->scratch + warp_bytes);
+    st = block_counters(ctx, a.c.n_items, &a.counters, stream);
+    if (st != LETHE_OK) return st;
+    const cudaError_t e = launch_block_attend(a, maps, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "block_attend launch");
     return LETHE_OK;
 }
 

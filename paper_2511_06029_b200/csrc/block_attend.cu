@@ -1,0 +1,655 @@
+// lethe_block_attend: softmax attention of single query tokens over a cache in 8 bits with a scale for each block of tokens.
+//
+// Bound by memory: 2 D bytes per token and KV head.  The groups of 16 tokens of all items lie end to end on a line (an item's full
+// blocks, or those its list names, then its open rows), which is cut evenly over the warps of the GPU, since lengths are known on the
+// device only: ragged batches, one long sequence and many short ones are balanced alike.  A warp goes through its stretch alone, with a
+// ring of TMA tiles of its own and no barrier with the others.  What a warp has of an item that others share is merged by the CTA when
+// all its warps are done (adjacent stretches belong to adjacent warps), and what a CTA has of an item that other CTAs share by the last
+// of them to finish, in the order of the line: nothing is added atomically.
+//
+// Per group: S^T = K Q^T (tokens on M, the group's heads on N), the probabilities turned by movmatrix, O^T += V^T P^T; m16n8k16 f16 MMAs.
+// A code becomes the f16 of the same value by bit operations (1024 + 128 + x is 0x6400 | (x ^ 0x80)) and one subtraction, exactly.  The
+// scale of the key block is a factor of the logits; the scale of the value block goes into the exponent, p' = exp2(s + log2 vs - m),
+// so that the probabilities meet plain codes in the MMA, and the sum of probabilities takes p' / vs.  m is the largest s + log2 vs up to
+// a factor of 2^6: it only moves when a logit outgrows it by that, and p' is kept 2^9 up, so that f16 (up to 2^15 in use) holds
+// probabilities down to 2^-23 of the largest with full precision.  Rows of open blocks are bf16 and may have any range: they take bf16 MMAs
+// with the probabilities in two terms.
+#include <string.h>
+
+#include "block_attend.cuh"
+#include "chunk_tc.cuh"
+#include "kv8_utils.cuh"
+
+namespace lethe {
+namespace {
+
+constexpr int kThreads = kBlockWarps * 32;
+constexpr int kTailWeight = 2;  // length on the line of 16 open rows, which are fetched without a ring
+constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
+constexpr float kLift = 9.f;    // p' is kept up by this (log2)
+
+template <int D>
+__host__ __device__ constexpr int stage_bytes() { return 16 * D * 2; }
+template <int D>
+__host__ __device__ constexpr int stages() { return D == 128 ? 3 : 6; }
+
+// One end of a warp's stretch that is not a whole item.
+struct Rec {
+    int idx;       // item of the call, -1: none
+    int start, w;  // where the item lies on the line
+    bool begins, ends;
+    float m[8], l[8];
+};
+
+template <int D>
+struct __align__(1024) Smem {
+    unsigned char ring[kBlockWarps][stages<D>()][stage_bytes<D>()];
+    float4 meta[kBlockWarps][stages<D>()];  // key scale, log2 of the value scale, its inverse, whether there is a block
+    unsigned long long bars[kBlockWarps][stages<D>()];
+    int prefix[kThreads + 1], totals[kBlockWarps];
+    Rec rec[2 * kBlockWarps];
+    int chain_first[2 * kBlockWarps + 1], n_chains;
+    int finish[2];  // chains whose other parts are all there
+    int abort;
+};
+
+struct Span {
+    int n, full, blocks, groups, open, w;
+};
+__device__ __forceinline__ Span span_of(const BlockAttendArgs& a, int item) {
+    Span s;
+    s.n = block_len(a.c, item);
+    s.full = s.n >> a.c.t_shift;
+    s.blocks = a.selected ? min(a.n_select, s.full) : s.full;
+    s.groups = s.blocks << (a.c.t_shift - 4);
+    s.open = s.n & (a.c.T - 1);
+    s.w = max(1, s.groups + kTailWeight * ((s.open + 15) >> 4));
+    return s;
+}
+
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, unsigned long long* b, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(smem_u32(b)), "l"(policy) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+// Bytes 0 and 2 of x, whole numbers in two's complement, as two halves.
+__device__ __forceinline__ uint32_t halves_of(uint32_t x) {
+    uint32_t y;
+    asm("lop3.b32 %0, %1, 0x00ff00ff, 0x64806480, 0x6a;" : "=r"(y) : "r"(x));  // (x & mask) ^ bias
+    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&y), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// State of a stretch: lane = 4 g + t has heads 2t and 2t + 1; o[i] = (d, 2t), (d, 2t + 1), (d + 1, 2t), (d + 1, 2t + 1) with d = first_d + 2 i.
+template <int D>
+struct Acc {
+    float o[D / 16][4];
+    float m[2], l[2];  // l: this lane's tokens only
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+        m[0] = m[1] = -INFINITY;
+        l[0] = l[1] = 0.f;
+    }
+    // x: logits of tokens (row g: x[0], x[1]; row g + 8: x[2], x[3]) -> p', and m moved where it has to be
+    __device__ __forceinline__ void softmax(float (&x)[4], float inv_vs) {
+        const float a = fmaxf(x[0], x[2]), b = fmaxf(x[1], x[3]);
+        if (__any_sync(0xffffffffu, a > m[0] + kLazy || b > m[1] + kLazy)) {
+            float na = a, nb = b;
+#pragma unroll
+            for (int s = 4; s < 32; s <<= 1) {
+                na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, s));
+                nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, s));
+            }
+            na = fmaxf(na, m[0]);
+            nb = fmaxf(nb, m[1]);
+            const float fa = exp2_diff(m[0], na), fb = exp2_diff(m[1], nb);
+            m[0] = na;
+            m[1] = nb;
+            l[0] *= fa;
+            l[1] *= fb;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                o[i][0] *= fa;
+                o[i][1] *= fb;
+                o[i][2] *= fa;
+                o[i][3] *= fb;
+            }
+        }
+        const float ma = m[0] == -INFINITY ? 0.f : m[0] - kLift, mb = m[1] == -INFINITY ? 0.f : m[1] - kLift;
+        x[0] = fast_exp2(x[0] - ma);
+        x[1] = fast_exp2(x[1] - mb);
+        x[2] = fast_exp2(x[2] - ma);
+        x[3] = fast_exp2(x[3] - mb);
+        l[0] = fmaf(x[0] + x[2], inv_vs, l[0]);
+        l[1] = fmaf(x[1] + x[3], inv_vs, l[1]);
+    }
+};
+
+// Elements that a lane reads of a key row (16 bytes at each of D / 64 places) and of a value row, and the order of a tile's tokens among
+// the MMA's rows: chosen so that eight neighbouring lanes touch eight different 16-byte columns of the swizzled tile at D = 128.
+template <int D>
+__device__ __forceinline__ int token_row(int r) {  // row 0 .. 7 of the MMA -> token of the tile
+    return D == 128 ? ((r >> 1) | ((r & 1) << 2)) : r;
+}
+template <int D>
+__device__ __forceinline__ int first_d(int g) { return D == 128 ? 16 * ((g >> 1) | ((g & 1) << 2)) : 8 * g; }
+template <int D>
+__device__ __forceinline__ uint32_t swizzled(int row, int byte) {
+    return D == 128 ? row * 128 + (byte ^ ((row & 7) << 4)) : row * 64 + (byte ^ (((row >> 1) & 3) << 4));
+}
+
+// O^T += V^T P^T for rows a, b (tokens of k = 2t, 2t + 1) and c, d (k = 2t + 8, 2t + 9), words of four codes.
+template <int D>
+__device__ __forceinline__ void value_word(float (*o)[4], uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t p0, uint32_t p1) {
+    const uint32_t ab = __byte_perm(a, b, 0x5410), cd = __byte_perm(c, d, 0x5410);
+    const uint32_t f0[4] = {halves_of(ab), halves_of(ab >> 8), halves_of(cd), halves_of(cd >> 8)};
+    mma_f16(o[0], f0, p0, p1);
+    const uint32_t ef = __byte_perm(a, b, 0x7632), gh = __byte_perm(c, d, 0x7632);
+    const uint32_t f1[4] = {halves_of(ef), halves_of(ef >> 8), halves_of(gh), halves_of(gh >> 8)};
+    mma_f16(o[1], f1, p0, p1);
+}
+
+// 16 open rows from row r0 on: keys and values straight from memory, bf16.
+template <int D>
+__device__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float v_ref, float inv_ref_log2) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const __nv_bfloat16* K = a.c.k_open + (size_t)it.item * a.c.T * D;
+    const __nv_bfloat16* V = a.c.v_open + (size_t)it.item * a.c.T * D;
+    const __nv_bfloat16* Q = a.q + (((size_t)it.li * a.c.B + it.b) * a.c.Hkv + it.h) * a.c.G * D;
+    const bool in0 = r0 + g < n_open, in1 = r0 + g + 8 < n_open;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {  // 8 elements of a lane: two steps of 16
+        const int d = j * 32 + 8 * t;
+        const uint4 q = g < a.c.G ? *reinterpret_cast<const uint4*>(Q + (size_t)g * D + d) : zero;
+        const uint4 x = in0 ? *reinterpret_cast<const uint4*>(K + (size_t)(r0 + g) * D + d) : zero;
+        const uint4 y = in1 ? *reinterpret_cast<const uint4*>(K + (size_t)(r0 + g + 8) * D + d) : zero;
+        const uint32_t f0[4] = {x.x, y.x, x.y, y.y}, f1[4] = {x.z, y.z, x.w, y.w};
+        mma_bf16(s, f0, q.x, q.y);
+        mma_bf16(s, f1, q.z, q.w);
+    }
+    s[0] = in0 ? fmaf(s[0], scale2[0], inv_ref_log2) : -INFINITY;
+    s[1] = in0 ? fmaf(s[1], scale2[1], inv_ref_log2) : -INFINITY;
+    s[2] = in1 ? fmaf(s[2], scale2[0], inv_ref_log2) : -INFINITY;
+    s[3] = in1 ? fmaf(s[3], scale2[1], inv_ref_log2) : -INFINITY;
+    acc.softmax(s, v_ref);
+    uint32_t p[2][2];  // [term][rows 0 .. 7, 8 .. 15]
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float u = s[2 * k], w = s[2 * k + 1];
+        const uint32_t big = pack_bf16(u, w);
+        p[0][k] = movmatrix_trans(big);
+        p[1][k] = movmatrix_trans(pack_bf16(u - __uint_as_float(big << 16), w - __uint_as_float(big & 0xffff0000u)));
+    }
+    const int d0 = first_d<D>(g);
+    uint4 v[4][D / 64];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = r0 + 2 * t + (k & 1) + (k >> 1) * 8;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) v[k][j] = r < n_open ? *reinterpret_cast<const uint4*>(V + (size_t)r * D + d0 + 8 * j) : zero;
+    }
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+        const uint32_t x[4][4] = {{v[0][j].x, v[0][j].y, v[0][j].z, v[0][j].w}, {v[1][j].x, v[1][j].y, v[1][j].z, v[1][j].w},
+                                  {v[2][j].x, v[2][j].y, v[2][j].z, v[2][j].w}, {v[3][j].x, v[3][j].y, v[3][j].z, v[3][j].w}};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {  // elements 2 w and 2 w + 1 of the eight
+            const uint32_t f[4] = {__byte_perm(x[0][w], x[1][w], 0x5410), __byte_perm(x[0][w], x[1][w], 0x7632),
+                                   __byte_perm(x[2][w], x[3][w], 0x5410), __byte_perm(x[2][w], x[3][w], 0x7632)};
+            mma_bf16(acc.o[4 * j + w], f, p[0][0], p[0][1]);
+            mma_bf16(acc.o[4 * j + w], f, p[1][0], p[1][1]);
+        }
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_constant__ BlockAttendArgs a, const __grid_constant__ BlockMaps maps) {
+    constexpr int NS = stages<D>(), SB = stage_bytes<D>(), C = D / 64;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    Smem<D>& sm = *reinterpret_cast<Smem<D>*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, g = lane >> 2, t = lane & 3;
+    const BlockView& c = a.c;
+    if (lane == 0) {
+        for (int s = 0; s < NS; ++s) bar_init(&sm.bars[w][s], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        sm.rec[2 * w].idx = sm.rec[2 * w + 1].idx = -1;
+    }
+    if (tid == 0) sm.abort = 0;
+    dependency_wait();
+    dependency_release();
+
+    // the line: where each thread's run of items begins
+    const int run = (c.n_items + kThreads - 1) / kThreads;
+    int mine = 0;
+    for (int i = tid * run; i < min(c.n_items, (tid + 1) * run); ++i) mine += span_of(a, block_item(c.layer_begin, c.B, c.Hkv, i).item).w;
+    {
+        int x = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) sm.totals[w] = x;
+        __syncthreads();
+        int base = 0;
+#pragma unroll
+        for (int i = 0; i < kBlockWarps; ++i)
+            if (i < w) base += sm.totals[i];
+        sm.prefix[tid] = base + x - mine;
+        if (tid == kThreads - 1) sm.prefix[kThreads] = base + x;
+        __syncthreads();
+    }
+    const long long total = sm.prefix[kThreads];
+    // warps in use: at least two groups each, as far as there are
+    const long long warps = min((long long)a.n_cta * kBlockWarps, (total + 1) / 2);
+    if ((long long)blockIdx.x * kBlockWarps >= warps) return;
+    const int wid = blockIdx.x * kBlockWarps + w;
+    const int at0 = wid < warps ? (int)(wid * total / warps) : 0, at1 = wid < warps ? (int)((wid + 1) * total / warps) : 0;
+
+    if (at0 < at1) {
+        // the item that holds at0
+        int lo = 0, hi = kThreads;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (sm.prefix[mid] <= at0) lo = mid;
+            else hi = mid;
+        }
+        int idx = lo * run, start = sm.prefix[lo];
+        for (;;) {
+            const int i = idx + lane;
+            int x = i < c.n_items ? span_of(a, block_item(c.layer_begin, c.B, c.Hkv, i).item).w : 0x3fffffff / 32;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += y;
+            }
+            const unsigned past = __ballot_sync(0xffffffffu, x > at0 - start);
+            const int skip = past ? __ffs(past) - 1 : 32;
+            const int before = __shfl_sync(0xffffffffu, x, max(skip - 1, 0));
+            if (skip) start += before;
+            idx += skip;
+            if (skip < 32) break;
+        }
+
+        const uint64_t policy = l2_evict_first_policy();
+        const uint32_t ring = smem_u32(sm.ring[w]);
+        int stage = 0;
+        unsigned phase = 0;      // of `stage`
+        int put = 0;             // stage that is filled next
+        bool aborted = false;
+        int at = at0;
+        while (at < at1) {
+            const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, idx);
+            const Span sp = span_of(a, it.item);
+            const int p0 = at - start, p1 = min(at1 - start, sp.w);
+            const int g0 = min(p0, sp.groups), g1 = aborted ? g0 : min(p1, sp.groups);
+            const int gshift = c.t_shift - 4;
+
+            // a run of up to 32 blocks whose pages and scales the lanes hold
+            int run0 = -64;
+            int page = -1;
+            float ks = 0.f, lv = 0.f, iv = 0.f, v_ref = 1.f, inv_ref = 1.f;
+            bool have_ref = false;
+            auto fetch_run = [&](int e0) {
+                run0 = e0;
+                page = -1;
+                ks = 0.f;
+                float vs = 0.f;
+                const int e = e0 + lane;
+                if (e < sp.blocks) {
+                    int blk = e;
+                    if (a.selected) {
+                        blk = a.selected[(size_t)idx * a.n_select + e];
+                        if (blk >= sp.full) {
+                            record_error(c.status, LETHE_ERR_INVALID_ARG, it.item);
+                            blk = -1;
+                        }
+                    }
+                    if (blk >= 0) {
+                        page = (int)block_page(c, it.item, blk);
+                        if (page < 0) record_error(c.status, LETHE_ERR_PAGE, it.item);
+                    }
+                    if (page >= 0) {
+                        ks = c.k_scale[page];
+                        vs = c.v_scale[page];
+                    }
+                }
+                if (!have_ref) {
+                    // a power of two near the first value scale: the others are taken relative to it
+                    const unsigned some = __ballot_sync(0xffffffffu, vs > 0.f && vs < INFINITY);
+                    if (some) {
+                        const float v0 = __shfl_sync(0xffffffffu, vs, __ffs(some) - 1);
+                        const int ex = min(max((int)(__float_as_uint(v0) >> 23), 1), 252);
+                        v_ref = __uint_as_float((uint32_t)ex << 23);
+                        inv_ref = __uint_as_float((uint32_t)(254 - ex) << 23);
+                        have_ref = true;
+                    }
+                }
+                const float rel = vs * inv_ref;
+                lv = vs == 0.f ? 0.f : __log2f(rel);
+                iv = vs == 0.f ? 1.f : __fdividef(1.f, rel);
+                if (vs == 0.f) page = page < 0 ? page : page | 0x40000000;  // the block's values are zero
+            };
+            auto issue = [&](int gi) {
+                const int e = gi >> gshift, sub = gi & ((1 << gshift) - 1);
+                if (e >= run0 + 32 || run0 < 0) fetch_run(e);
+                const int src = e - run0;
+                const int pg = __shfl_sync(0xffffffffu, page, src);
+                const float k_ = __shfl_sync(0xffffffffu, ks, src), l_ = __shfl_sync(0xffffffffu, lv, src), i_ = __shfl_sync(0xffffffffu, iv, src);
+                if (lane == 0) {
+                    sm.meta[w][put] = make_float4(k_, l_, i_, pg < 0 ? 0.f : (pg & 0x40000000) ? 2.f : 1.f);
+                    unsigned long long* bar = &sm.bars[w][put];
+                    bar_expect_tx(bar, pg < 0 ? 0 : SB);
+                    if (pg >= 0) {
+                        const int row = ((pg & 0x3fffffff) << c.t_shift) + 16 * sub;
+                        const uint32_t dst = ring + put * SB;
+                        tma_2d(dst, &maps.k, 0, row, bar, policy);
+                        tma_2d(dst + SB / 2, &maps.v, 0, row, bar, policy);
+                    }
+                }
+                put = put + 1 == NS ? 0 : put + 1;
+            };
+
+            // queries: bf16 -> f16 within range, in the order of the key codes (bytes 0, 2 and 1, 3 of each word)
+            uint32_t qf[4 * C][2];
+            float scale2[2], open2[2];
+            int queued = min(g1, g0 + NS);
+            {
+                const __nv_bfloat16* Q = a.q + (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G * D + (size_t)g * D;
+                uint4 x[C][2];
+#pragma unroll
+                for (int k = 0; k < C; ++k)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        x[k][j] = g < c.G ? *reinterpret_cast<const uint4*>(Q + 64 * k + 16 * t + 8 * j) : make_uint4(0, 0, 0, 0);
+                for (int i = g0; i < queued; ++i) issue(i);
+                float big = 0.f;
+                float f[C][16];
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    Piece<__nv_bfloat16>::unpack(x[k][0], f[k]);
+                    Piece<__nv_bfloat16>::unpack(x[k][1], f[k] + 8);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) big = fmaxf(big, fabsf(f[k][j]));
+                }
+                big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+                big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+                int ex = (int)((__float_as_uint(big) >> 23) & 0xffu) - 7;  // the largest magnitude to [128, 256)
+                ex = big > 0.f && big < INFINITY ? min(max(ex, 2), 252) : 127;
+                const float mul = __uint_as_float((uint32_t)(254 - ex) << 23), div = __uint_as_float((uint32_t)ex << 23);
+#pragma unroll
+                for (int k = 0; k < C; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        qf[4 * k + j][0] = pack_f16(f[k][4 * j] * mul, f[k][4 * j + 2] * mul);
+                        qf[4 * k + j][1] = pack_f16(f[k][4 * j + 1] * mul, f[k][4 * j + 3] * mul);
+                    }
+                const float sc = c.scale_log2[c.layer_begin + it.li];
+                open2[0] = open2[1] = sc;
+                scale2[0] = sc * __shfl_sync(0xffffffffu, div, 8 * t);
+                scale2[1] = sc * __shfl_sync(0xffffffffu, div, 8 * t + 4);
+            }
+            Acc<D> acc;
+            acc.clear();
+            for (int gi = g0; gi < g1; ++gi) {
+                unsigned long long* bar = &sm.bars[w][stage];
+                if (!warp_wait(bar, phase, &sm.abort, a.wait_limit)) {
+                    if (lane == 0) record_error(c.status, LETHE_ERR_TIMEOUT, blockIdx.x);
+                    // what is in flight lands before the CTA goes on
+                    for (int k = gi; k < queued; ++k) {
+                        bar_drain(&sm.bars[w][stage], phase);
+                        stage = stage + 1 == NS ? 0 : stage + 1;
+                        phase ^= stage == 0;
+                    }
+                    aborted = true;
+                    break;
+                }
+                const float4 meta = sm.meta[w][stage];
+                const uint32_t tile = ring + stage * SB;
+                uint4 kx[2][C], vx[4];
+                uint2 vy[4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int k = 0; k < C; ++k) kx[r][k] = lds128(tile + swizzled<D>(token_row<D>(g) + 8 * r, 64 * k + 16 * t));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int row = token_row<D>(2 * t + (k & 1)) + (k >> 1) * 8;
+                    if (D == 128) vx[k] = lds128(tile + SB / 2 + swizzled<D>(row, first_d<D>(g)));
+                    else vy[k] = lds64(tile + SB / 2 + swizzled<D>(row, first_d<D>(g)));
+                }
+                __syncwarp();
+                stage = stage + 1 == NS ? 0 : stage + 1;
+                phase ^= stage == 0;
+                if (queued < g1) issue(queued++);
+                if (meta.w == 0.f) continue;
+
+                float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    const uint32_t x[4] = {kx[0][k].x, kx[0][k].y, kx[0][k].z, kx[0][k].w}, y[4] = {kx[1][k].x, kx[1][k].y, kx[1][k].z, kx[1][k].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t f[4] = {halves_of(x[j]), halves_of(y[j]), halves_of(x[j] >> 8), halves_of(y[j] >> 8)};
+                        mma_f16(j & 1 ? s1 : s0, f, qf[4 * k + j][0], qf[4 * k + j][1]);
+                    }
+                }
+                const float ka = meta.x * scale2[0], kb = meta.x * scale2[1];
+                float p[4] = {fmaf(s0[0] + s1[0], ka, meta.y), fmaf(s0[1] + s1[1], kb, meta.y), fmaf(s0[2] + s1[2], ka, meta.y), fmaf(s0[3] + s1[3], kb, meta.y)};
+                acc.softmax(p, meta.z);
+                if (meta.w == 2.f) continue;  // values of zero
+                const uint32_t b0 = movmatrix_trans(pack_f16(p[0], p[1])), b1 = movmatrix_trans(pack_f16(p[2], p[3]));
+                if (D == 128) {
+                    value_word<D>(acc.o, vx[0].x, vx[1].x, vx[2].x, vx[3].x, b0, b1);
+                    value_word<D>(acc.o + 2, vx[0].y, vx[1].y, vx[2].y, vx[3].y, b0, b1);
+                    value_word<D>(acc.o + D / 32, vx[0].z, vx[1].z, vx[2].z, vx[3].z, b0, b1);
+                    value_word<D>(acc.o + D / 32 + 2, vx[0].w, vx[1].w, vx[2].w, vx[3].w, b0, b1);
+                } else {
+                    value_word<D>(acc.o, vy[0].x, vy[1].x, vy[2].x, vy[3].x, b0, b1);
+                    value_word<D>(acc.o + 2, vy[0].y, vy[1].y, vy[2].y, vy[3].y, b0, b1);
+                }
+            }
+            // open rows whose place on the line lies in the stretch
+            const int tail0 = (max(p0 - sp.groups, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - sp.groups, 0) + kTailWeight - 1) / kTailWeight;
+            for (int j = tail0; j < tail1 && 16 * j < sp.open; ++j) open_rows<D>(a, acc, it, 16 * j, sp.open, open2, v_ref, __log2f(inv_ref));
+
+#pragma unroll
+            for (int s = 4; s < 32; s <<= 1) {
+                acc.l[0] += __shfl_xor_sync(0xffffffffu, acc.l[0], s);
+                acc.l[1] += __shfl_xor_sync(0xffffffffu, acc.l[1], s);
+            }
+            const bool begins = p0 == 0, ends = p1 == sp.w;
+            const int d0 = first_d<D>(g);
+            if (begins && ends) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int head = 2 * t + k;
+                    if (head >= c.G) continue;
+                    const size_t row = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G + head;
+                    const float inv = acc.l[k] == 0.f ? 0.f : v_ref / acc.l[k];
+                    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D + d0);
+#pragma unroll
+                    for (int i = 0; i < D / 16; i += 2)
+                        *reinterpret_cast<uint2*>(dst + i) = make_uint2(pack_bf16(acc.o[i][k] * inv, acc.o[i][2 + k] * inv), pack_bf16(acc.o[i + 1][k] * inv, acc.o[i + 1][2 + k] * inv));
+                    if (a.lse && g == 0) a.lse[row] = acc.l[k] == 0.f ? -INFINITY : (acc.m[k] - kLift + log2f(acc.l[k])) * 0.6931471805599453f;
+                }
+            } else {
+                const bool last = at1 <= start + sp.w;  // nothing of this warp comes after it: the ring is free
+                Rec& rec = sm.rec[2 * w + (last ? 1 : 0)];
+                if (lane == 0) {
+                    rec.idx = idx;
+                    rec.start = start;
+                    rec.w = sp.w;
+                    rec.begins = begins;
+                    rec.ends = ends;
+                }
+                if (g == 0) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        rec.m[2 * t + k] = acc.l[k] == 0.f ? -INFINITY : acc.m[k] - kLift;
+                        rec.l[2 * t + k] = acc.l[k];
+                    }
+                }
+                float* part = last ? reinterpret_cast<float*>(sm.ring[w]) : a.warp_part + ((size_t)blockIdx.x * kBlockWarps + w) * kBlockPart;
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+                        *reinterpret_cast<float2*>(part + (2 * t + k) * D + d0 + 2 * i) = make_float2(acc.o[i][k] * v_ref, acc.o[i][2 + k] * v_ref);
+            }
+            at = start + p1;
+            start += sp.w;
+            ++idx;
+        }
+    }
+    __syncthreads();
+
+    // chains of parts of one item, in the order of the line
+    if (w == 0) {
+        const int mine_idx = sm.rec[lane].idx;
+        const unsigned have = __ballot_sync(0xffffffffu, mine_idx >= 0);
+        const unsigned below = have & ((1u << lane) - 1);
+        const int prev = __shfl_sync(0xffffffffu, mine_idx, below ? 31 - __clz(below) : 0);
+        const bool heads = mine_idx >= 0 && (!below || prev != mine_idx);
+        const unsigned firsts = __ballot_sync(0xffffffffu, heads);
+        if (heads) sm.chain_first[__popc(firsts & ((1u << lane) - 1))] = lane;
+        if (lane == 0) {
+            sm.n_chains = __popc(firsts);
+            sm.chain_first[__popc(firsts)] = 2 * kBlockWarps;
+        }
+    }
+    if (tid < 2) sm.finish[tid] = -1;
+    __syncthreads();
+    const int chains = sm.n_chains;
+    int teams = 1;
+    while (teams < chains && teams < kBlockWarps) teams *= 2;
+    const int team_threads = kThreads / teams, team = tid / team_threads, tt = tid - team * team_threads;
+    for (int ch = team; ch < chains; ch += teams) {
+        const int r0 = sm.chain_first[ch], r1 = sm.chain_first[ch + 1];
+        int r_last = r0;
+        for (int r = r0; r < r1; ++r)
+            if (sm.rec[r].idx >= 0) r_last = r;
+        const bool whole = sm.rec[r0].begins && sm.rec[r_last].ends;
+        const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, sm.rec[r0].idx);
+        float* part = a.cta_part + ((size_t)blockIdx.x * 2 + (sm.rec[r0].begins ? 1 : 0)) * kBlockPart;
+        for (int e = tt; e < c.G * D / 2; e += team_threads) {
+            const int head = e / (D / 2), d = 2 * (e - head * (D / 2));
+            float m = -INFINITY, l = 0.f;
+            for (int r = r0; r <= r_last; ++r)
+                if (sm.rec[r].idx >= 0) m = fmaxf(m, sm.rec[r].m[head]);
+            float2 o = make_float2(0.f, 0.f);
+#pragma unroll 4
+            for (int r = r0; r <= r_last; ++r) {
+                if (sm.rec[r].idx < 0) continue;
+                const float f = exp2_diff(sm.rec[r].m[head], m);
+                const float* src = (r & 1 ? reinterpret_cast<const float*>(sm.ring[r >> 1]) : a.warp_part + ((size_t)blockIdx.x * kBlockWarps + (r >> 1)) * kBlockPart) + head * D + d;
+                const float2 x = *reinterpret_cast<const float2*>(src);
+                l = fmaf(sm.rec[r].l[head], f, l);
+                o.x = fmaf(x.x, f, o.x);
+                o.y = fmaf(x.y, f, o.y);
+            }
+            if (whole) {
+                const size_t row = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G + head;
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                *reinterpret_cast<uint32_t*>(a.out + row * D + d) = pack_bf16(o.x * inv, o.y * inv);
+                if (a.lse && d == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            } else {
+                *reinterpret_cast<float2*>(part + 16 + head * D + d) = o;
+                if (d == 0) *reinterpret_cast<float2*>(part + 2 * head) = make_float2(m, l);
+            }
+        }
+    }
+    __threadfence();
+    __syncthreads();
+    // items that other CTAs share: at most the first chain and the last
+    if (tid < 2 && chains > 0 && (tid == 0 || chains > 1)) {
+        const int ch = tid == 0 ? 0 : chains - 1;
+        const int r0 = sm.chain_first[ch], r1 = sm.chain_first[ch + 1];
+        int r_last = r0;
+        for (int r = r0; r < r1; ++r)
+            if (sm.rec[r].idx >= 0) r_last = r;
+        const Rec& rec = sm.rec[r0];
+        if (!(rec.begins && sm.rec[r_last].ends)) {
+            const int c0 = (int)(((rec.start + 1LL) * warps - 1) / total) / kBlockWarps;
+            const int c1 = (int)(((long long)(rec.start + rec.w) * warps - 1) / total) / kBlockWarps;
+            const int seen = atomicAdd(&a.counters[rec.idx], 1);
+            if (seen == c1 - c0) {
+                a.counters[rec.idx] = 0;
+                sm.finish[tid] = r0;
+            }
+        }
+    }
+    __syncthreads();
+    for (int k = 0; k < 2; ++k) {
+        if (sm.finish[k] < 0) continue;
+        __threadfence();
+        const Rec& rec = sm.rec[sm.finish[k]];
+        const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, rec.idx);
+        const int c0 = (int)(((rec.start + 1LL) * warps - 1) / total) / kBlockWarps;
+        const int c1 = (int)(((long long)(rec.start + rec.w) * warps - 1) / total) / kBlockWarps;
+        for (int e = tid; e < c.G * D / 2; e += kThreads) {
+            const int head = e / (D / 2), d = 2 * (e - head * (D / 2));
+            float m = -INFINITY, l = 0.f;
+            float2 o = make_float2(0.f, 0.f);
+#pragma unroll 4
+            for (int cta = c0; cta <= c1; ++cta) {
+                const float* src = a.cta_part + ((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * kBlockPart;
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 2 * head)), x = __ldcg(reinterpret_cast<const float2*>(src + 16 + head * D + d));
+                const float nm = fmaxf(m, ml.x), f = exp2_diff(m, nm), h = exp2_diff(ml.x, nm);
+                l = l * f + ml.y * h;
+                o.x = o.x * f + x.x * h;
+                o.y = o.y * f + x.y * h;
+                m = nm;
+            }
+            const size_t row = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G + head;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            *reinterpret_cast<uint32_t*>(a.out + row * D + d) = pack_bf16(o.x * inv, o.y * inv);
+            if (a.lse && d == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        }
+    }
+}
+
+template <int D>
+cudaError_t launch_d(const BlockAttendArgs& a, const BlockMaps& maps, cudaStream_t stream) {
+    const size_t smem = sizeof(Smem<D>) + 1024;
+    cudaError_t e = prepare_kernel((const void*)block_attend_kernel<D>, smem);
+    return e != cudaSuccess ? e : launch_dependent(block_attend_kernel<D>, dim3(a.n_cta), kThreads, smem, stream, a, maps);
+}
+
+}  // namespace
+
+bool build_block_maps(void* encode, const BlockView& c, BlockMaps* maps) {
+    typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    encode_fn fn = reinterpret_cast<encode_fn>(encode);
+    const cuuint64_t dims[2] = {(cuuint64_t)c.D, (cuuint64_t)c.n_pages * c.T};
+    const cuuint64_t pitch[1] = {(cuuint64_t)c.D};
+    const cuuint32_t box[2] = {(cuuint32_t)c.D, 16}, es[2] = {1, 1};
+    const CUtensorMapSwizzle swizzle = c.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+    for (int i = 0; i < 2; ++i)
+        if (fn(i ? &maps->v : &maps->k, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, i ? c.v : c.k, dims, pitch, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return false;
+    return true;
+}
+
+cudaError_t launch_block_attend(const BlockAttendArgs& a, const BlockMaps& maps, cudaStream_t stream) {
+    return a.c.D == 128 ? launch_d<128>(a, maps, stream) : launch_d<64>(a, maps, stream);
+}
+
+}  // namespace lethe
