@@ -1521,7 +1521,7 @@ lethe_status lethe_block_attend(lethe_ctx* ctx, const lethe_block_cache* c, int 
     }
     // the line of 16-token groups is counted in 32 bits
     const long long most = selected && n_select < c->capacity ? n_select : c->capacity;
-    if (a.c.n_items * (most * (a.c.T / 16) + 2 * (a.c.T / 16) + 1) > 0x3fffffffLL)
+    if (a.c.n_items * (most * (a.c.T / 16) + 2 * (a.c.T / 16) + 4) > 0x3fffffffLL)
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "block_attend: too many blocks for one call; cover fewer layers");
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");
@@ -1531,12 +1531,10 @@ lethe_status lethe_block_attend(lethe_ctx* ctx, const lethe_block_cache* c, int 
     a.n_select = selected ? n_select : 0;
     a.n_cta = ctx->sm_count;
     a.wait_limit = ctx->wait_limit ? ctx->wait_limit : 400000;
-    const size_t warp_bytes = (size_t)a.n_cta * kBlockWarps * kBlockPart * sizeof(float), cta_bytes = (size_t)a.n_cta * 2 * kBlockPart * sizeof(float);
-    st = ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, warp_bytes + cta_bytes, "block attention scratch", stream);
+    st = ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, (size_t)a.n_cta * 16 * kBlockPart * sizeof(float), "block attention scratch", stream);
     if (st != LETHE_OK) return st;
-    a.warp_part = (float*)ctx->scratch;
-    a.cta_part = (float*)((char*)ctx->scratch + warp_bytes);
-    st = block_counters(ctx, a.c.n_items, &a.counters, stream);
+    a.cta_part = (float*)ctx->scratch;
+    st = block_counters(ctx, a.c.n_items * 8, &a.counters, stream);
     if (st != LETHE_OK) return st;
     const cudaError_t e = launch_block_attend(a, maps, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "block_attend launch");

@@ -25,45 +25,46 @@ namespace {
 
 constexpr int kThreads = kBlockWarps * 32;
 constexpr int kTailWeight = 2;  // length on the line of 16 open rows, which are fetched without a ring
+constexpr int kPad = 3;         // and of an item's beginning: its length, first pages, queries and first tile come one after the other
+constexpr int kLine = 2048;     // items whose places on the line are kept in shared memory; of more, only every so many-th is
 constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
 constexpr float kLift = 9.f;    // p' is kept up by this (log2)
 
 template <int D>
 __host__ __device__ constexpr int stage_bytes() { return 16 * D * 2; }
 template <int D>
-__host__ __device__ constexpr int stages() { return D == 128 ? 3 : 6; }
+__host__ __device__ constexpr int stages() { return kBlockStages * 128 / D; }
 
 // One end of a warp's stretch that is not a whole item.
 struct Rec {
     int idx;       // item of the call, -1: none
     int start, w;  // where the item lies on the line
     bool begins, ends;
-    float m[8], l[8];
 };
 
 template <int D>
 struct __align__(1024) Smem {
     unsigned char ring[kBlockWarps][stages<D>()][stage_bytes<D>()];
-    float4 meta[kBlockWarps][stages<D>()];  // key scale, log2 of the value scale, its inverse, whether there is a block
+    float first[kBlockWarps][8 * D];        // O of a warp's first stretch, when it has others after it (the last one's goes to its ring)
     unsigned long long bars[kBlockWarps][stages<D>()];
+    int line[kLine + 1], len[kLine];
     int prefix[kThreads + 1], totals[kBlockWarps];
-    Rec rec[2 * kBlockWarps];
-    int chain_first[2 * kBlockWarps + 1], n_chains;
-    int finish[2];  // chains whose other parts are all there
+    Rec rec[32];                            // warp w: 2 w its first stretch, 2 w + 1 its last
+    float m[32][8], l[32][8];
     int abort;
 };
 
 struct Span {
     int n, full, blocks, groups, open, w;
 };
-__device__ __forceinline__ Span span_of(const BlockAttendArgs& a, int item) {
+__device__ __forceinline__ Span span_of(const BlockAttendArgs& a, int n) {
     Span s;
-    s.n = block_len(a.c, item);
+    s.n = n;
     s.full = s.n >> a.c.t_shift;
     s.blocks = a.selected ? min(a.n_select, s.full) : s.full;
     s.groups = s.blocks << (a.c.t_shift - 4);
     s.open = s.n & (a.c.T - 1);
-    s.w = max(1, s.groups + kTailWeight * ((s.open + 15) >> 4));
+    s.w = kPad + s.groups + kTailWeight * ((s.open + 15) >> 4);
     return s;
 }
 
@@ -172,6 +173,14 @@ __device__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem
     const bool in0 = r0 + g < n_open, in1 = r0 + g + 8 < n_open;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     const uint4 zero = make_uint4(0, 0, 0, 0);
+    const int d0 = first_d<D>(g);
+    uint4 v[4][D / 64];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = r0 + 2 * t + (k & 1) + (k >> 1) * 8;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) v[k][j] = r < n_open ? *reinterpret_cast<const uint4*>(V + (size_t)r * D + d0 + 8 * j) : zero;
+    }
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {  // 8 elements of a lane: two steps of 16
         const int d = j * 32 + 8 * t;
@@ -195,14 +204,6 @@ __device__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem
         p[0][k] = movmatrix_trans(big);
         p[1][k] = movmatrix_trans(pack_bf16(u - __uint_as_float(big << 16), w - __uint_as_float(big & 0xffff0000u)));
     }
-    const int d0 = first_d<D>(g);
-    uint4 v[4][D / 64];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int r = r0 + 2 * t + (k & 1) + (k >> 1) * 8;
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) v[k][j] = r < n_open ? *reinterpret_cast<const uint4*>(V + (size_t)r * D + d0 + 8 * j) : zero;
-    }
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
         const uint32_t x[4][4] = {{v[0][j].x, v[0][j].y, v[0][j].z, v[0][j].w}, {v[1][j].x, v[1][j].y, v[1][j].z, v[1][j].w},
@@ -217,6 +218,19 @@ __device__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem
     }
 }
 
+// The last place of an ascending table (its first entry is at most x) that holds at most x; a warp, 32 places at a time.
+__device__ __forceinline__ int last_at_most(const int* table, int n, int x, int lane) {
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 31) / 32, i = lane * step;
+        const unsigned ok = __ballot_sync(0xffffffffu, i < n && table[lo + i] <= x);
+        const int k = 31 - __clz(ok);
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_constant__ BlockAttendArgs a, const __grid_constant__ BlockMaps maps) {
     constexpr int NS = stages<D>(), SB = stage_bytes<D>(), C = D / 64;
@@ -227,16 +241,30 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
     if (lane == 0) {
         for (int s = 0; s < NS; ++s) bar_init(&sm.bars[w][s], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        sm.rec[2 * w].idx = sm.rec[2 * w + 1].idx = -1;
     }
-    if (tid == 0) sm.abort = 0;
+    if (tid < 32) sm.rec[tid].idx = -1;
+    if (tid == 0) {
+        sm.abort = 0;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v) : "memory");
+    }
     dependency_wait();
     dependency_release();
 
-    // the line: where each thread's run of items begins
-    const int run = (c.n_items + kThreads - 1) / kThreads;
+    // the line: a run of items to each thread
+    auto len_of = [&](int idx) { return block_len(c, block_item(c.layer_begin, c.B, c.Hkv, idx).item); };
+    const bool fits = c.n_items <= kLine;
+    const int run = (c.n_items + kThreads - 1) / kThreads, i0 = min(c.n_items, tid * run), i1 = min(c.n_items, i0 + run);
     int mine = 0;
-    for (int i = tid * run; i < min(c.n_items, (tid + 1) * run); ++i) mine += span_of(a, block_item(c.layer_begin, c.B, c.Hkv, i).item).w;
+#pragma unroll 4
+    for (int i = i0; i < i1; ++i) {
+        const int n = len_of(i), wt = span_of(a, n).w;
+        if (fits) {
+            sm.len[i] = n;
+            sm.line[i] = wt;
+        }
+        mine += wt;
+    }
     {
         int x = mine;
 #pragma unroll
@@ -250,40 +278,50 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
 #pragma unroll
         for (int i = 0; i < kBlockWarps; ++i)
             if (i < w) base += sm.totals[i];
-        sm.prefix[tid] = base + x - mine;
+        int at = base + x - mine;
+        sm.prefix[tid] = at;
         if (tid == kThreads - 1) sm.prefix[kThreads] = base + x;
+        if (fits)
+            for (int i = i0; i < i1; ++i) {
+                const int wt = sm.line[i];
+                sm.line[i] = at;
+                at += wt;
+            }
         __syncthreads();
     }
     const long long total = sm.prefix[kThreads];
-    // warps in use: at least two groups each, as far as there are
+    // warps in use: at least two groups each (or an item's beginning), as far as there are
     const long long warps = min((long long)a.n_cta * kBlockWarps, (total + 1) / 2);
     if ((long long)blockIdx.x * kBlockWarps >= warps) return;
+    auto cta_at = [&](int pos) { return (int)(((pos + 1LL) * warps - 1) / total) / kBlockWarps; };
     const int wid = blockIdx.x * kBlockWarps + w;
     const int at0 = wid < warps ? (int)(wid * total / warps) : 0, at1 = wid < warps ? (int)((wid + 1) * total / warps) : 0;
 
     if (at0 < at1) {
         // the item that holds at0
-        int lo = 0, hi = kThreads;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (sm.prefix[mid] <= at0) lo = mid;
-            else hi = mid;
-        }
-        int idx = lo * run, start = sm.prefix[lo];
-        for (;;) {
-            const int i = idx + lane;
-            int x = i < c.n_items ? span_of(a, block_item(c.layer_begin, c.B, c.Hkv, i).item).w : 0x3fffffff / 32;
+        int idx, start;
+        if (fits) {
+            idx = last_at_most(sm.line, c.n_items, at0, lane);
+            start = sm.line[idx];
+        } else {
+            const int chunk = last_at_most(sm.prefix, kThreads, at0, lane);
+            idx = chunk * run;
+            start = sm.prefix[chunk];
+            for (;;) {
+                const int i = idx + lane;
+                int x = i < c.n_items ? span_of(a, len_of(i)).w : 0x3fffffff / 32;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, x, o);
+                    if (lane >= o) x += y;
+                }
+                const unsigned past = __ballot_sync(0xffffffffu, x > at0 - start);
+                const int skip = past ? __ffs(past) - 1 : 32;
+                const int before = __shfl_sync(0xffffffffu, x, max(skip - 1, 0));
+                if (skip) start += before;
+                idx += skip;
+                if (skip < 32) break;
             }
-            const unsigned past = __ballot_sync(0xffffffffu, x > at0 - start);
-            const int skip = past ? __ffs(past) - 1 : 32;
-            const int before = __shfl_sync(0xffffffffu, x, max(skip - 1, 0));
-            if (skip) start += before;
-            idx += skip;
-            if (skip < 32) break;
         }
 
         const uint64_t policy = l2_evict_first_policy();
@@ -295,21 +333,21 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
         int at = at0;
         while (at < at1) {
             const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, idx);
-            const Span sp = span_of(a, it.item);
+            const Span sp = span_of(a, fits ? sm.len[idx] : len_of(idx));
             const int p0 = at - start, p1 = min(at1 - start, sp.w);
-            const int g0 = min(p0, sp.groups), g1 = aborted ? g0 : min(p1, sp.groups);
+            const int g0 = min(max(p0 - kPad, 0), sp.groups), g1 = aborted ? g0 : min(max(p1 - kPad, 0), sp.groups);
             const int gshift = c.t_shift - 4;
 
-            // a run of up to 32 blocks whose pages and scales the lanes hold
-            int run0 = -64;
-            int page = -1;
-            float ks = 0.f, lv = 0.f, iv = 0.f, v_ref = 1.f, inv_ref = 1.f;
+            // runs of up to 32 blocks, one to a lane: the one that is being asked for (its scales are still on their way) and the one
+            // that is worked on.  The former is ahead by less than a run.
+            int ask0 = -64, ask_page = -1, use0 = -64;
+            float ask_ks = 0.f, ask_vs = 0.f, ks = 0.f, lv = 0.f, iv = 0.f;  // iv: v_ref / vs, 0: no block, -1: a block whose values are zero
+            float v_ref = 1.f, inv_ref = 1.f;
             bool have_ref = false;
-            auto fetch_run = [&](int e0) {
-                run0 = e0;
-                page = -1;
-                ks = 0.f;
-                float vs = 0.f;
+            auto ask_run = [&](int e0) {
+                ask0 = e0;
+                ask_page = -1;
+                ask_ks = ask_vs = 0.f;
                 const int e = e0 + lane;
                 if (e < sp.blocks) {
                     int blk = e;
@@ -321,42 +359,42 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                         }
                     }
                     if (blk >= 0) {
-                        page = (int)block_page(c, it.item, blk);
-                        if (page < 0) record_error(c.status, LETHE_ERR_PAGE, it.item);
+                        ask_page = (int)block_page(c, it.item, blk);
+                        if (ask_page < 0) record_error(c.status, LETHE_ERR_PAGE, it.item);
                     }
-                    if (page >= 0) {
-                        ks = c.k_scale[page];
-                        vs = c.v_scale[page];
+                    if (ask_page >= 0) {
+                        ask_ks = c.k_scale[ask_page];
+                        ask_vs = c.v_scale[ask_page];
                     }
                 }
+            };
+            auto use_run = [&]() {
+                use0 = ask0;
+                ks = ask_ks;
                 if (!have_ref) {
                     // a power of two near the first value scale: the others are taken relative to it
-                    const unsigned some = __ballot_sync(0xffffffffu, vs > 0.f && vs < INFINITY);
+                    const unsigned some = __ballot_sync(0xffffffffu, ask_vs > 0.f && ask_vs < INFINITY);
                     if (some) {
-                        const float v0 = __shfl_sync(0xffffffffu, vs, __ffs(some) - 1);
+                        const float v0 = __shfl_sync(0xffffffffu, ask_vs, __ffs(some) - 1);
                         const int ex = min(max((int)(__float_as_uint(v0) >> 23), 1), 252);
                         v_ref = __uint_as_float((uint32_t)ex << 23);
                         inv_ref = __uint_as_float((uint32_t)(254 - ex) << 23);
                         have_ref = true;
                     }
                 }
-                const float rel = vs * inv_ref;
-                lv = vs == 0.f ? 0.f : __log2f(rel);
-                iv = vs == 0.f ? 1.f : __fdividef(1.f, rel);
-                if (vs == 0.f) page = page < 0 ? page : page | 0x40000000;  // the block's values are zero
+                const float rel = ask_vs * inv_ref;
+                lv = ask_vs == 0.f ? 0.f : __log2f(rel);
+                iv = ask_page < 0 ? 0.f : ask_vs == 0.f ? -1.f : __fdividef(1.f, rel);
             };
             auto issue = [&](int gi) {
                 const int e = gi >> gshift, sub = gi & ((1 << gshift) - 1);
-                if (e >= run0 + 32 || run0 < 0) fetch_run(e);
-                const int src = e - run0;
-                const int pg = __shfl_sync(0xffffffffu, page, src);
-                const float k_ = __shfl_sync(0xffffffffu, ks, src), l_ = __shfl_sync(0xffffffffu, lv, src), i_ = __shfl_sync(0xffffffffu, iv, src);
+                if (e >= ask0 + 32 || ask0 < 0) ask_run(e);
+                const int pg = __shfl_sync(0xffffffffu, ask_page, e - ask0);
                 if (lane == 0) {
-                    sm.meta[w][put] = make_float4(k_, l_, i_, pg < 0 ? 0.f : (pg & 0x40000000) ? 2.f : 1.f);
                     unsigned long long* bar = &sm.bars[w][put];
                     bar_expect_tx(bar, pg < 0 ? 0 : SB);
                     if (pg >= 0) {
-                        const int row = ((pg & 0x3fffffff) << c.t_shift) + 16 * sub;
+                        const int row = (pg << c.t_shift) + 16 * sub;
                         const uint32_t dst = ring + put * SB;
                         tma_2d(dst, &maps.k, 0, row, bar, policy);
                         tma_2d(dst + SB / 2, &maps.v, 0, row, bar, policy);
@@ -406,7 +444,15 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             }
             Acc<D> acc;
             acc.clear();
+            float b_ks = 0.f, b_lv = 0.f, b_iv = 0.f;  // of the block at hand
             for (int gi = g0; gi < g1; ++gi) {
+                const int e = gi >> gshift;
+                if (e >= use0 + 32 || use0 < 0) use_run();
+                if (gi == g0 || !(gi & ((1 << gshift) - 1))) {
+                    b_ks = __shfl_sync(0xffffffffu, ks, e - use0);
+                    b_lv = __shfl_sync(0xffffffffu, lv, e - use0);
+                    b_iv = __shfl_sync(0xffffffffu, iv, e - use0);
+                }
                 unsigned long long* bar = &sm.bars[w][stage];
                 if (!warp_wait(bar, phase, &sm.abort, a.wait_limit)) {
                     if (lane == 0) record_error(c.status, LETHE_ERR_TIMEOUT, blockIdx.x);
@@ -419,7 +465,6 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     aborted = true;
                     break;
                 }
-                const float4 meta = sm.meta[w][stage];
                 const uint32_t tile = ring + stage * SB;
                 uint4 kx[2][C], vx[4];
                 uint2 vy[4];
@@ -437,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 stage = stage + 1 == NS ? 0 : stage + 1;
                 phase ^= stage == 0;
                 if (queued < g1) issue(queued++);
-                if (meta.w == 0.f) continue;
+                if (b_iv == 0.f) continue;  // no block
 
                 float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -449,10 +494,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                         mma_f16(j & 1 ? s1 : s0, f, qf[4 * k + j][0], qf[4 * k + j][1]);
                     }
                 }
-                const float ka = meta.x * scale2[0], kb = meta.x * scale2[1];
-                float p[4] = {fmaf(s0[0] + s1[0], ka, meta.y), fmaf(s0[1] + s1[1], kb, meta.y), fmaf(s0[2] + s1[2], ka, meta.y), fmaf(s0[3] + s1[3], kb, meta.y)};
-                acc.softmax(p, meta.z);
-                if (meta.w == 2.f) continue;  // values of zero
+                const float ka = b_ks * scale2[0], kb = b_ks * scale2[1];
+                float p[4] = {fmaf(s0[0] + s1[0], ka, b_lv), fmaf(s0[1] + s1[1], kb, b_lv), fmaf(s0[2] + s1[2], ka, b_lv), fmaf(s0[3] + s1[3], kb, b_lv)};
+                acc.softmax(p, fabsf(b_iv));
+                if (b_iv < 0.f) continue;  // values of zero
                 const uint32_t b0 = movmatrix_trans(pack_f16(p[0], p[1])), b1 = movmatrix_trans(pack_f16(p[2], p[3]));
                 if (D == 128) {
                     value_word<D>(acc.o, vx[0].x, vx[1].x, vx[2].x, vx[3].x, b0, b1);
@@ -465,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 }
             }
             // open rows whose place on the line lies in the stretch
-            const int tail0 = (max(p0 - sp.groups, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - sp.groups, 0) + kTailWeight - 1) / kTailWeight;
+            const int tail0 = (max(p0 - kPad - sp.groups, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - kPad - sp.groups, 0) + kTailWeight - 1) / kTailWeight;
             for (int j = tail0; j < tail1 && 16 * j < sp.open; ++j) open_rows<D>(a, acc, it, 16 * j, sp.open, open2, v_ref, __log2f(inv_ref));
 
 #pragma unroll
@@ -490,7 +535,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 }
             } else {
                 const bool last = at1 <= start + sp.w;  // nothing of this warp comes after it: the ring is free
-                Rec& rec = sm.rec[2 * w + (last ? 1 : 0)];
+                const int which = 2 * w + (last ? 1 : 0);
+                Rec& rec = sm.rec[which];
                 if (lane == 0) {
                     rec.idx = idx;
                     rec.start = start;
@@ -501,11 +547,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 if (g == 0) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        rec.m[2 * t + k] = acc.l[k] == 0.f ? -INFINITY : acc.m[k] - kLift;
-                        rec.l[2 * t + k] = acc.l[k];
+                        sm.m[which][2 * t + k] = acc.l[k] == 0.f ? -INFINITY : acc.m[k] - kLift;
+                        sm.l[which][2 * t + k] = acc.l[k];
                     }
                 }
-                float* part = last ? reinterpret_cast<float*>(sm.ring[w]) : a.warp_part + ((size_t)blockIdx.x * kBlockWarps + w) * kBlockPart;
+                float* part = last ? reinterpret_cast<float*>(sm.ring[w]) : sm.first[w];
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -519,107 +565,92 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
     }
     __syncthreads();
 
-    // chains of parts of one item, in the order of the line
-    if (w == 0) {
-        const int mine_idx = sm.rec[lane].idx;
-        const unsigned have = __ballot_sync(0xffffffffu, mine_idx >= 0);
-        const unsigned below = have & ((1u << lane) - 1);
-        const int prev = __shfl_sync(0xffffffffu, mine_idx, below ? 31 - __clz(below) : 0);
-        const bool heads = mine_idx >= 0 && (!below || prev != mine_idx);
-        const unsigned firsts = __ballot_sync(0xffffffffu, heads);
-        if (heads) sm.chain_first[__popc(firsts & ((1u << lane) - 1))] = lane;
-        if (lane == 0) {
-            sm.n_chains = __popc(firsts);
-            sm.chain_first[__popc(firsts)] = 2 * kBlockWarps;
-        }
-    }
-    if (tid < 2) sm.finish[tid] = -1;
-    __syncthreads();
-    const int chains = sm.n_chains;
-    int teams = 1;
-    while (teams < chains && teams < kBlockWarps) teams *= 2;
-    const int team_threads = kThreads / teams, team = tid / team_threads, tt = tid - team * team_threads;
-    for (int ch = team; ch < chains; ch += teams) {
-        const int r0 = sm.chain_first[ch], r1 = sm.chain_first[ch + 1];
-        int r_last = r0;
-        for (int r = r0; r < r1; ++r)
-            if (sm.rec[r].idx >= 0) r_last = r;
-        const bool whole = sm.rec[r0].begins && sm.rec[r_last].ends;
-        const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, sm.rec[r0].idx);
-        float* part = a.cta_part + ((size_t)blockIdx.x * 2 + (sm.rec[r0].begins ? 1 : 0)) * kBlockPart;
-        for (int e = tt; e < c.G * D / 2; e += team_threads) {
-            const int head = e / (D / 2), d = 2 * (e - head * (D / 2));
-            float m = -INFINITY, l = 0.f;
-            for (int r = r0; r <= r_last; ++r)
-                if (sm.rec[r].idx >= 0) m = fmaxf(m, sm.rec[r].m[head]);
-            float2 o = make_float2(0.f, 0.f);
-#pragma unroll 4
-            for (int r = r0; r <= r_last; ++r) {
-                if (sm.rec[r].idx < 0) continue;
-                const float f = exp2_diff(sm.rec[r].m[head], m);
-                const float* src = (r & 1 ? reinterpret_cast<const float*>(sm.ring[r >> 1]) : a.warp_part + ((size_t)blockIdx.x * kBlockWarps + (r >> 1)) * kBlockPart) + head * D + d;
-                const float2 x = *reinterpret_cast<const float2*>(src);
-                l = fmaf(sm.rec[r].l[head], f, l);
-                o.x = fmaf(x.x, f, o.x);
-                o.y = fmaf(x.y, f, o.y);
-            }
-            if (whole) {
-                const size_t row = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G + head;
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                *reinterpret_cast<uint32_t*>(a.out + row * D + d) = pack_bf16(o.x * inv, o.y * inv);
-                if (a.lse && d == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-            } else {
-                *reinterpret_cast<float2*>(part + 16 + head * D + d) = o;
-                if (d == 0) *reinterpret_cast<float2*>(part + 2 * head) = make_float2(m, l);
-            }
-        }
-    }
-    __threadfence();
-    __syncthreads();
-    // items that other CTAs share: at most the first chain and the last
-    if (tid < 2 && chains > 0 && (tid == 0 || chains > 1)) {
-        const int ch = tid == 0 ? 0 : chains - 1;
-        const int r0 = sm.chain_first[ch], r1 = sm.chain_first[ch + 1];
-        int r_last = r0;
-        for (int r = r0; r < r1; ++r)
-            if (sm.rec[r].idx >= 0) r_last = r;
+    // The parts there are, in the order of the line; those of one item follow one another.  A lane stands for a part; every warp finds out.
+    const int part_idx = lane < 2 * kBlockWarps ? sm.rec[lane].idx : -1;
+    const unsigned have = __ballot_sync(0xffffffffu, part_idx >= 0), below = have & ((1u << lane) - 1);
+    const int prev = __shfl_sync(0xffffffffu, part_idx, below ? 31 - __clz(below) : 0);
+    const unsigned firsts = __ballot_sync(0xffffffffu, part_idx >= 0 && (!below || prev != part_idx));
+    // A warp merges one head of one item at a time, D / 32 elements to a lane.  The CTA's first and last item, which other CTAs may share, come
+    // first and fall to different warps: they take a round trip or two more.
+    constexpr int E = D / 32;
+    const int items = __popc(firsts);
+#pragma unroll 1
+    for (int unit = w; unit < items * c.G; unit += kBlockWarps) {
+        const int order = unit / c.G, head = unit - order * c.G;
+        unsigned rest = firsts;
+        for (int k = order == 0 ? 0 : order == 1 ? items - 1 : order - 1; k > 0; --k) rest &= rest - 1;
+        const int r0 = __ffs(rest) - 1;
+        const unsigned later = rest & (rest - 1);
+        const unsigned chain = have & ~((1u << r0) - 1) & (later ? (1u << (__ffs(later) - 1)) - 1 : 0xffffffffu);
         const Rec& rec = sm.rec[r0];
-        if (!(rec.begins && sm.rec[r_last].ends)) {
-            const int c0 = (int)(((rec.start + 1LL) * warps - 1) / total) / kBlockWarps;
-            const int c1 = (int)(((long long)(rec.start + rec.w) * warps - 1) / total) / kBlockWarps;
-            const int seen = atomicAdd(&a.counters[rec.idx], 1);
-            if (seen == c1 - c0) {
-                a.counters[rec.idx] = 0;
-                sm.finish[tid] = r0;
-            }
-        }
-    }
-    __syncthreads();
-    for (int k = 0; k < 2; ++k) {
-        if (sm.finish[k] < 0) continue;
-        __threadfence();
-        const Rec& rec = sm.rec[sm.finish[k]];
+        const bool whole = rec.begins && sm.rec[31 - __clz(chain)].ends;
         const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, rec.idx);
-        const int c0 = (int)(((rec.start + 1LL) * warps - 1) / total) / kBlockWarps;
-        const int c1 = (int)(((long long)(rec.start + rec.w) * warps - 1) / total) / kBlockWarps;
-        for (int e = tid; e < c.G * D / 2; e += kThreads) {
-            const int head = e / (D / 2), d = 2 * (e - head * (D / 2));
-            float m = -INFINITY, l = 0.f;
-            float2 o = make_float2(0.f, 0.f);
+        {
+            const bool in = chain >> lane & 1;
+            float m = in ? sm.m[lane][head] : -INFINITY;
+            float l = in ? sm.l[lane][head] : 0.f;
+            const float mine_m = m;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const float f = exp2_diff(mine_m, m);
+            l *= f;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+            float o[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll 4
-            for (int cta = c0; cta <= c1; ++cta) {
-                const float* src = a.cta_part + ((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * kBlockPart;
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + 2 * head)), x = __ldcg(reinterpret_cast<const float2*>(src + 16 + head * D + d));
-                const float nm = fmaxf(m, ml.x), f = exp2_diff(m, nm), h = exp2_diff(ml.x, nm);
-                l = l * f + ml.y * h;
-                o.x = o.x * f + x.x * h;
-                o.y = o.y * f + x.y * h;
-                m = nm;
+            for (unsigned k = chain; k; k &= k - 1) {
+                const int r = __ffs(k) - 1;
+                const float* src = (r & 1 ? reinterpret_cast<const float*>(sm.ring[r >> 1]) : sm.first[r >> 1]) + head * D + E * lane;
+                const float fr = __shfl_sync(0xffffffffu, f, r);
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = fmaf(src[e], fr, o[e]);
+            }
+            if (!whole) {
+                // the item goes on in other CTAs: the last of them to come here merges
+                float* part = a.cta_part + (((size_t)blockIdx.x * 2 + (rec.begins ? 1 : 0)) * 8 + head) * kBlockPart;
+#pragma unroll
+                for (int e = 0; e < E; ++e) part[4 + E * lane + e] = o[e];
+                if (lane == 0) *reinterpret_cast<float2*>(part) = make_float2(m, l);
+                __syncwarp();
+                const int c0 = cta_at(rec.start), c1 = cta_at(rec.start + rec.w - 1);
+                int seen = 0;
+                if (lane == 0) {
+                    int* counter = a.counters + (size_t)rec.idx * 8 + head;
+                    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(seen) : "l"(counter) : "memory");  // the warp's part lies before
+                    if (seen == c1 - c0) *counter = 0;
+                }
+                if (__shfl_sync(0xffffffffu, seen, 0) != c1 - c0) continue;
+                m = -INFINITY;
+                l = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 4
+                for (int cta = c0; cta <= c1; ++cta) {
+                    const float* src = a.cta_part + (((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * 8 + head) * kBlockPart;
+                    const float2 ml = __ldcg(reinterpret_cast<const float2*>(src));
+                    float x[E];
+                    if constexpr (E == 4) {
+                        const float4 v = __ldcg(reinterpret_cast<const float4*>(src + 4) + lane);
+                        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+                    } else {
+                        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + 4) + lane);
+                        x[0] = v.x, x[1] = v.y;
+                    }
+                    const float nm = fmaxf(m, ml.x), g0 = exp2_diff(m, nm), g1 = exp2_diff(ml.x, nm);
+                    l = l * g0 + ml.y * g1;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = o[e] * g0 + x[e] * g1;
+                    m = nm;
+                }
             }
             const size_t row = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G + head;
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            *reinterpret_cast<uint32_t*>(a.out + row * D + d) = pack_bf16(o.x * inv, o.y * inv);
-            if (a.lse && d == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D) + E / 2 * lane;
+            if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+            else *dst = pack_bf16(o[0] * inv, o[1] * inv);
+            if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
         }
     }
 }

@@ -6,7 +6,8 @@
 
 namespace lethe {
 
-constexpr int kBlockWarps = 16;  // warps of a CTA, each with a ring of its own; one CTA per SM
+constexpr int kBlockWarps = 12;  // warps of a CTA, each with a ring of its own; one CTA per SM
+constexpr int kBlockStages = 2;  // groups of 16 tokens in a ring at D = 128
 
 struct alignas(64) BlockMaps {
     CUtensorMap k, v;  // [blocks * block_tokens][D] bytes, boxes of 16 rows
@@ -18,12 +19,11 @@ struct BlockAttendArgs {
     const int32_t* selected;  // NULL: all blocks
     __nv_bfloat16* out;
     float* lse;
-    float* warp_part;         // [CTAs][kBlockWarps][kBlockPart]: a warp's first stretch, when it has others after it
-    float* cta_part;          // [CTAs][2][kBlockPart]: items that begin before / go on behind the CTA
-    int* counters;            // [items] CTAs that have left a part, zero between launches
+    float* cta_part;          // [CTAs][2][8 heads][kBlockPart]: items that begin before / go on behind the CTA
+    int* counters;            // [items][8 heads] CTAs that have left a part, zero between launches
     int n_select, n_cta, wait_limit;
 };
-constexpr int kBlockPart = 16 + 8 * 128;  // 8 x (max, sum), then O by head
+constexpr int kBlockPart = 4 + 128;  // max, sum, two unused, then O
 
 bool build_block_maps(void* encode, const BlockView& c, BlockMaps* maps);
 cudaError_t launch_block_attend(const BlockAttendArgs& a, const BlockMaps& maps, cudaStream_t stream);
