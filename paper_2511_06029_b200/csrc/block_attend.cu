@@ -1,19 +1,20 @@
 // lethe_block_attend: softmax attention of single query tokens over a cache in 8 bits with a scale for each block of tokens.
 //
-// Bound by memory: 2 D bytes per token and KV head.  The groups of 16 tokens of all items lie end to end on a line (an item's full
+// Bound by memory: 2 D bytes per token and KV head.  The steps of 32 tokens of all items lie end to end on a line (an item's full
 // blocks, or those its list names, then its open rows), which is cut evenly over the warps of the GPU, since lengths are known on the
 // device only: ragged batches, one long sequence and many short ones are balanced alike.  A warp goes through its stretch alone, with a
-// ring of TMA tiles of its own and no barrier with the others.  What a warp has of an item that others share is merged by the CTA when
-// all its warps are done (adjacent stretches belong to adjacent warps), and what a CTA has of an item that other CTAs share by the last
-// of them to finish, in the order of the line: nothing is added atomically.
+// ring of TMA tiles of its own and no barrier with the others.  What a CTA's warps have of one item is merged when all of them are done
+// (adjacent stretches belong to adjacent warps), and what a CTA has of an item that other CTAs share by the last of them to finish, in
+// the order of the line: nothing is added atomically.
 //
-// Per group: S^T = K Q^T (tokens on M, the group's heads on N), the probabilities turned by movmatrix, O^T += V^T P^T; m16n8k16 f16 MMAs.
-// A code becomes the f16 of the same value by bit operations (1024 + 128 + x is 0x6400 | (x ^ 0x80)) and one subtraction, exactly.  The
-// scale of the key block is a factor of the logits; the scale of the value block goes into the exponent, p' = exp2(s + log2 vs - m),
-// so that the probabilities meet plain codes in the MMA, and the sum of probabilities takes p' / vs.  m is the largest s + log2 vs up to
-// a factor of 2^6: it only moves when a logit outgrows it by that, and p' is kept 2^9 up, so that f16 (up to 2^15 in use) holds
-// probabilities down to 2^-23 of the largest with full precision.  Rows of open blocks are bf16 and may have any range: they take bf16 MMAs
-// with the probabilities in two terms.
+// S^T = K Q^T (tokens on M, the group's heads on N) on the codes themselves: m16n8k32 s8 MMAs, a query row as a whole number of 21 bits
+// relative to its largest element, in three digits of 7 bits, so that the sums are exact.  The scale of the key block is a factor of the
+// logits; the scale of the value block goes into the exponent, p' = exp2(s + log2 vs - m), so that the probabilities meet plain codes
+// in O^T += V^T P^T (m16n8k16 f16 MMAs, the probabilities turned by movmatrix), and the sum of probabilities takes p' / vs.  A value code
+// becomes the f16 of the same value by bit operations (1024 + 128 + x is 0x6400 | (x ^ 0x80)) and one subtraction, exactly.  m is the
+// largest s + log2 vs up to a factor of 2^6: it only moves when a logit outgrows it by that, and p' is kept 2^9 up, so that f16 (up to
+// 2^15 in use) holds probabilities down to 2^-23 of the largest with full precision.  Rows of open blocks are bf16 and may have any
+// range: they take bf16 MMAs with the probabilities in two terms.
 #include <string.h>
 
 #include "block_attend.cuh"
@@ -24,6 +25,7 @@ namespace lethe {
 namespace {
 
 constexpr int kThreads = kBlockWarps * 32;
+constexpr int kStep = 32;       // tokens of a step
 constexpr int kTailWeight = 2;  // length on the line of 16 open rows, which are fetched without a ring
 constexpr int kPad = 3;         // and of an item's beginning: its length, first pages, queries and first tile come one after the other
 constexpr int kLine = 2048;     // items whose places on the line are kept in shared memory; of more, only every so many-th is
@@ -31,7 +33,7 @@ constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
 constexpr float kLift = 9.f;    // p' is kept up by this (log2)
 
 template <int D>
-__host__ __device__ constexpr int stage_bytes() { return 16 * D * 2; }
+__host__ __device__ constexpr int stage_bytes() { return kStep * D * 2; }
 template <int D>
 __host__ __device__ constexpr int stages() { return kBlockStages * 128 / D; }
 
@@ -55,16 +57,16 @@ struct __align__(1024) Smem {
 };
 
 struct Span {
-    int n, full, blocks, groups, open, w;
+    int n, full, blocks, steps, open, w;
 };
 __device__ __forceinline__ Span span_of(const BlockAttendArgs& a, int n) {
     Span s;
     s.n = n;
     s.full = s.n >> a.c.t_shift;
     s.blocks = a.selected ? min(a.n_select, s.full) : s.full;
-    s.groups = s.blocks << (a.c.t_shift - 4);
+    s.steps = ((s.blocks << a.c.t_shift) + kStep - 1) / kStep;
     s.open = s.n & (a.c.T - 1);
-    s.w = kPad + s.groups + kTailWeight * ((s.open + 15) >> 4);
+    s.w = kPad + s.steps + kTailWeight * ((s.open + 15) >> 4);
     return s;
 }
 
@@ -82,6 +84,12 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
     uint2 v;
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
     return v;
+}
+// d = a b + c, 8-bit whole numbers.
+__device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, const int (&c)[4]) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
 }
 // Bytes 0 and 2 of x, whole numbers in two's complement, as two halves.
 __device__ __forceinline__ uint32_t halves_of(uint32_t x) {
@@ -104,9 +112,15 @@ struct Acc {
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
     }
-    // x: logits of tokens (row g: x[0], x[1]; row g + 8: x[2], x[3]) -> p', and m moved where it has to be
-    __device__ __forceinline__ void softmax(float (&x)[4], float inv_vs) {
-        const float a = fmaxf(x[0], x[2]), b = fmaxf(x[1], x[3]);
+    // x: logits of H x 16 tokens (row g: x[h][0], x[h][1]; row g + 8: x[h][2], x[h][3]) -> p', and m moved where it has to be
+    template <int H>
+    __device__ __forceinline__ void softmax(float (&x)[H][4], const float (&inv_vs)[H]) {
+        float a = fmaxf(x[0][0], x[0][2]), b = fmaxf(x[0][1], x[0][3]);
+#pragma unroll
+        for (int h = 1; h < H; ++h) {
+            a = fmaxf(a, fmaxf(x[h][0], x[h][2]));
+            b = fmaxf(b, fmaxf(x[h][1], x[h][3]));
+        }
         if (__any_sync(0xffffffffu, a > m[0] + kLazy || b > m[1] + kLazy)) {
             float na = a, nb = b;
 #pragma unroll
@@ -130,12 +144,15 @@ struct Acc {
             }
         }
         const float ma = m[0] == -INFINITY ? 0.f : m[0] - kLift, mb = m[1] == -INFINITY ? 0.f : m[1] - kLift;
-        x[0] = fast_exp2(x[0] - ma);
-        x[1] = fast_exp2(x[1] - mb);
-        x[2] = fast_exp2(x[2] - ma);
-        x[3] = fast_exp2(x[3] - mb);
-        l[0] = fmaf(x[0] + x[2], inv_vs, l[0]);
-        l[1] = fmaf(x[1] + x[3], inv_vs, l[1]);
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            x[h][0] = fast_exp2(x[h][0] - ma);
+            x[h][1] = fast_exp2(x[h][1] - mb);
+            x[h][2] = fast_exp2(x[h][2] - ma);
+            x[h][3] = fast_exp2(x[h][3] - mb);
+            l[0] = fmaf(x[h][0] + x[h][2], inv_vs[h], l[0]);
+            l[1] = fmaf(x[h][1] + x[h][3], inv_vs[h], l[1]);
+        }
     }
 };
 
@@ -171,7 +188,8 @@ __device__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem
     const __nv_bfloat16* V = a.c.v_open + (size_t)it.item * a.c.T * D;
     const __nv_bfloat16* Q = a.q + (((size_t)it.li * a.c.B + it.b) * a.c.Hkv + it.h) * a.c.G * D;
     const bool in0 = r0 + g < n_open, in1 = r0 + g + 8 < n_open;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    float x2[1][4] = {{0.f, 0.f, 0.f, 0.f}};
+    float(&s)[4] = x2[0];
     const uint4 zero = make_uint4(0, 0, 0, 0);
     const int d0 = first_d<D>(g);
     uint4 v[4][D / 64];
@@ -195,7 +213,8 @@ __device__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem
     s[1] = in0 ? fmaf(s[1], scale2[1], inv_ref_log2) : -INFINITY;
     s[2] = in1 ? fmaf(s[2], scale2[0], inv_ref_log2) : -INFINITY;
     s[3] = in1 ? fmaf(s[3], scale2[1], inv_ref_log2) : -INFINITY;
-    acc.softmax(s, v_ref);
+    const float inv[1] = {v_ref};
+    acc.template softmax<1>(x2, inv);
     uint32_t p[2][2];  // [term][rows 0 .. 7, 8 .. 15]
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -325,6 +344,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
         }
 
         const uint64_t policy = l2_evict_first_policy();
+        uint32_t k_at[C], v_at[2];  // this lane's places in a tile's first 16 tokens; eight rows further nothing but 8 D is added
+#pragma unroll
+        for (int k = 0; k < C; ++k) k_at[k] = swizzled<D>(token_row<D>(g), 64 * k + 16 * t);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) v_at[k] = swizzled<D>(token_row<D>(2 * t + k), first_d<D>(g));
         const uint32_t ring = smem_u32(sm.ring[w]);
         int stage = 0;
         unsigned phase = 0;      // of `stage`
@@ -335,13 +359,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, idx);
             const Span sp = span_of(a, fits ? sm.len[idx] : len_of(idx));
             const int p0 = at - start, p1 = min(at1 - start, sp.w);
-            const int g0 = min(max(p0 - kPad, 0), sp.groups), g1 = aborted ? g0 : min(max(p1 - kPad, 0), sp.groups);
-            const int gshift = c.t_shift - 4;
+            const int g0 = min(max(p0 - kPad, 0), sp.steps), g1 = aborted ? g0 : min(max(p1 - kPad, 0), sp.steps);
 
             // runs of up to 32 blocks, one to a lane: the one that is being asked for (its scales are still on their way) and the one
             // that is worked on.  The former is ahead by less than a run.
             int ask0 = -64, ask_page = -1, use0 = -64;
-            float ask_ks = 0.f, ask_vs = 0.f, ks = 0.f, lv = 0.f, iv = 0.f;  // iv: v_ref / vs, 0: no block, -1: a block whose values are zero
+            float ask_ks = 0.f, ask_vs = 0.f, ks = 0.f, lv = 0.f, iv = 0.f;  // iv: v_ref / vs, negative: a block whose values are zero
             float v_ref = 1.f, inv_ref = 1.f;
             bool have_ref = false;
             auto ask_run = [&](int e0) {
@@ -383,28 +406,45 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     }
                 }
                 const float rel = ask_vs * inv_ref;
-                lv = ask_vs == 0.f ? 0.f : __log2f(rel);
-                iv = ask_page < 0 ? 0.f : ask_vs == 0.f ? -1.f : __fdividef(1.f, rel);
+                lv = ask_page < 0 ? -INFINITY : ask_vs == 0.f ? 0.f : __log2f(rel);  // no block: no weight
+                iv = ask_vs == 0.f ? -1.f : __fdividef(1.f, rel);
             };
+            // step gi: one tile of a block of 32 tokens or more, or two blocks of 16
             auto issue = [&](int gi) {
-                const int e = gi >> gshift, sub = gi & ((1 << gshift) - 1);
-                if (e >= ask0 + 32 || ask0 < 0) ask_run(e);
-                const int pg = __shfl_sync(0xffffffffu, ask_page, e - ask0);
-                if (lane == 0) {
-                    unsigned long long* bar = &sm.bars[w][put];
-                    bar_expect_tx(bar, pg < 0 ? 0 : SB);
-                    if (pg >= 0) {
-                        const int row = (pg << c.t_shift) + 16 * sub;
-                        const uint32_t dst = ring + put * SB;
-                        tma_2d(dst, &maps.k, 0, row, bar, policy);
-                        tma_2d(dst + SB / 2, &maps.v, 0, row, bar, policy);
+                unsigned long long* bar = &sm.bars[w][put];
+                const uint32_t dst = ring + put * SB;
+                if (c.t_shift > 4) {
+                    const int e = gi >> (c.t_shift - 5);
+                    if (e >= ask0 + 32 || ask0 < 0) ask_run(e);
+                    const int pg = __shfl_sync(0xffffffffu, ask_page, e - ask0);
+                    if (lane == 0) {
+                        bar_expect_tx(bar, pg < 0 ? 0 : SB);
+                        if (pg >= 0) {
+                            const int row = (pg << c.t_shift) + ((gi * kStep) & (c.T - 1));
+                            tma_2d(dst, &maps.k, 0, row, bar, policy);
+                            tma_2d(dst + SB / 2, &maps.v, 0, row, bar, policy);
+                        }
+                    }
+                } else {
+                    if (2 * gi >= ask0 + 32 || ask0 < 0) ask_run(2 * gi);  // runs begin at even blocks
+                    const int p0 = __shfl_sync(0xffffffffu, ask_page, 2 * gi - ask0), p1 = __shfl_sync(0xffffffffu, ask_page, 2 * gi + 1 - ask0);
+                    if (lane == 0) {
+                        bar_expect_tx(bar, (p0 < 0 ? 0 : SB / 2) + (p1 < 0 ? 0 : SB / 2));
+                        if (p0 >= 0) {
+                            tma_2d(dst, &maps.k, 0, p0 * 16, bar, policy);
+                            tma_2d(dst + SB / 2, &maps.v, 0, p0 * 16, bar, policy);
+                        }
+                        if (p1 >= 0) {
+                            tma_2d(dst + SB / 4, &maps.k, 0, p1 * 16, bar, policy);
+                            tma_2d(dst + 3 * (SB / 4), &maps.v, 0, p1 * 16, bar, policy);
+                        }
                     }
                 }
                 put = put + 1 == NS ? 0 : put + 1;
             };
 
-            // queries: bf16 -> f16 within range, in the order of the key codes (bytes 0, 2 and 1, 3 of each word)
-            uint32_t qf[4 * C][2];
+            // queries: whole numbers below 2^20, in three digits, in the order of the key codes
+            uint32_t qf[3][4 * C];
             float scale2[2], open2[2];
             int queued = min(g1, g0 + NS);
             {
@@ -415,6 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
                         x[k][j] = g < c.G ? *reinterpret_cast<const uint4*>(Q + 64 * k + 16 * t + 8 * j) : make_uint4(0, 0, 0, 0);
+#pragma unroll 1
                 for (int i = g0; i < queued; ++i) issue(i);
                 float big = 0.f;
                 float f[C][16];
@@ -427,16 +468,31 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 }
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-                int ex = (int)((__float_as_uint(big) >> 23) & 0xffu) - 7;  // the largest magnitude to [128, 256)
+                // a power of two brings the largest magnitude to [2^19, 2^20)
+                int ex = (int)((__float_as_uint(big) >> 23) & 0xffu) - 19;
                 ex = big > 0.f && big < INFINITY ? min(max(ex, 2), 252) : 127;
-                const float mul = __uint_as_float((uint32_t)(254 - ex) << 23), div = __uint_as_float((uint32_t)ex << 23);
+                const float mul = __uint_as_float((uint32_t)(254 - ex) << 23);
+                float div = __uint_as_float((uint32_t)ex << 23);
+                bool bad = false;  // a query with a NaN or an infinity has no whole numbers: all its logits are NaN
 #pragma unroll
                 for (int k = 0; k < C; ++k)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        qf[4 * k + j][0] = pack_f16(f[k][4 * j] * mul, f[k][4 * j + 2] * mul);
-                        qf[4 * k + j][1] = pack_f16(f[k][4 * j + 1] * mul, f[k][4 * j + 3] * mul);
+                        uint32_t digit[3] = {0, 0, 0};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float y = f[k][4 * j + i];
+                            bad = bad || !(fabsf(y) < INFINITY);
+                            const int v = __float2int_rn(y * mul), d2 = (v + 8192) >> 14, r = v - (d2 << 14), d1 = (r + 64) >> 7, d0 = r - (d1 << 7);
+                            digit[2] |= (uint32_t)(d2 & 0xff) << (8 * i);
+                            digit[1] |= (uint32_t)(d1 & 0xff) << (8 * i);
+                            digit[0] |= (uint32_t)(d0 & 0xff) << (8 * i);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) qf[i][4 * k + j] = digit[i];
                     }
+                const unsigned bads = __ballot_sync(0xffffffffu, bad);
+                if (bads >> (4 * g) & 15u) div = __uint_as_float(0x7fc00000u);
                 const float sc = c.scale_log2[c.layer_begin + it.li];
                 open2[0] = open2[1] = sc;
                 scale2[0] = sc * __shfl_sync(0xffffffffu, div, 8 * t);
@@ -444,14 +500,19 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             }
             Acc<D> acc;
             acc.clear();
-            float b_ks = 0.f, b_lv = 0.f, b_iv = 0.f;  // of the block at hand
+            float b_ks[2] = {0.f, 0.f}, b_lv[2] = {0.f, 0.f}, b_iv[2] = {0.f, 0.f};  // of the blocks at hand
             for (int gi = g0; gi < g1; ++gi) {
-                const int e = gi >> gshift;
+                const int e = (gi * kStep) >> c.t_shift;
                 if (e >= use0 + 32 || use0 < 0) use_run();
-                if (gi == g0 || !(gi & ((1 << gshift) - 1))) {
-                    b_ks = __shfl_sync(0xffffffffu, ks, e - use0);
-                    b_lv = __shfl_sync(0xffffffffu, lv, e - use0);
-                    b_iv = __shfl_sync(0xffffffffu, iv, e - use0);
+                if (c.t_shift <= 5 || gi == g0 || !((gi * kStep) & (c.T - 1))) {
+                    b_ks[0] = b_ks[1] = __shfl_sync(0xffffffffu, ks, e - use0);
+                    b_lv[0] = b_lv[1] = __shfl_sync(0xffffffffu, lv, e - use0);
+                    b_iv[0] = b_iv[1] = __shfl_sync(0xffffffffu, iv, e - use0);
+                    if (c.t_shift == 4) {
+                        b_ks[1] = __shfl_sync(0xffffffffu, ks, e + 1 - use0);
+                        b_lv[1] = __shfl_sync(0xffffffffu, lv, e + 1 - use0);
+                        b_iv[1] = __shfl_sync(0xffffffffu, iv, e + 1 - use0);
+                    }
                 }
                 unsigned long long* bar = &sm.bars[w][stage];
                 if (!warp_wait(bar, phase, &sm.abort, a.wait_limit)) {
@@ -466,51 +527,73 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     break;
                 }
                 const uint32_t tile = ring + stage * SB;
-                uint4 kx[2][C], vx[4];
-                uint2 vy[4];
+                uint4 kx[2][C][2];
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int k = 0; k < C; ++k) kx[r][k] = lds128(tile + swizzled<D>(token_row<D>(g) + 8 * r, 64 * k + 16 * t));
+                    for (int k = 0; k < C; ++k)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int row = token_row<D>(2 * t + (k & 1)) + (k >> 1) * 8;
-                    if (D == 128) vx[k] = lds128(tile + SB / 2 + swizzled<D>(row, first_d<D>(g)));
-                    else vy[k] = lds64(tile + SB / 2 + swizzled<D>(row, first_d<D>(g)));
+                        for (int r = 0; r < 2; ++r) kx[h][k][r] = lds128(tile + k_at[k] + h * (SB / 4) + r * 8 * D);
+                float p[2][4];
+                {
+                    constexpr int kMagic = 0x4b400000;  // 1.5 x 2^23 as bits: a whole number added to it is the fraction of that float
+                    const int from[4] = {kMagic, kMagic, kMagic, kMagic};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        int sums[3][4];
+#pragma unroll
+                        for (int k = 0; k < C; ++k) {
+                            const uint4 x = kx[h][k][0], y = kx[h][k][1];
+#pragma unroll
+                            for (int i = 0; i < 3; ++i) {
+                                if (k == 0) mma_s8(sums[i], x.x, y.x, x.y, y.y, qf[i][0], qf[i][1], from);
+                                else mma_s8(sums[i], x.x, y.x, x.y, y.y, qf[i][4 * k], qf[i][4 * k + 1], sums[i]);
+                                mma_s8(sums[i], x.z, y.z, x.w, y.w, qf[i][4 * k + 2], qf[i][4 * k + 3], sums[i]);
+                            }
+                        }
+                        const float ka = b_ks[h] * scale2[0], kb = b_ks[h] * scale2[1];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            constexpr float kOff = 12582912.f;
+                            const float s2 = __int_as_float(sums[2][i]) - kOff, s1 = __int_as_float(sums[1][i]) - kOff, s0 = __int_as_float(sums[0][i]) - kOff;
+                            p[h][i] = fmaf(fmaf(fmaf(s2, 128.f, s1), 128.f, s0), i & 1 ? kb : ka, b_lv[h]);
+                        }
+                    }
                 }
+                uint4 vx[2][4];
+                uint2 vy[2][4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t at = tile + SB / 2 + h * (SB / 4) + v_at[k & 1] + (k >> 1) * 8 * D;
+                        if (D == 128) vx[h][k] = lds128(at);
+                        else vy[h][k] = lds64(at);
+                    }
                 __syncwarp();
                 stage = stage + 1 == NS ? 0 : stage + 1;
                 phase ^= stage == 0;
                 if (queued < g1) issue(queued++);
-                if (b_iv == 0.f) continue;  // no block
 
-                float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+                const float inv[2] = {fabsf(b_iv[0]), fabsf(b_iv[1])};
+                acc.template softmax<2>(p, inv);
 #pragma unroll
-                for (int k = 0; k < C; ++k) {
-                    const uint32_t x[4] = {kx[0][k].x, kx[0][k].y, kx[0][k].z, kx[0][k].w}, y[4] = {kx[1][k].x, kx[1][k].y, kx[1][k].z, kx[1][k].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t f[4] = {halves_of(x[j]), halves_of(y[j]), halves_of(x[j] >> 8), halves_of(y[j] >> 8)};
-                        mma_f16(j & 1 ? s1 : s0, f, qf[4 * k + j][0], qf[4 * k + j][1]);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t b0 = movmatrix_trans(pack_f16(p[h][0], p[h][1])), b1 = movmatrix_trans(pack_f16(p[h][2], p[h][3]));
+                    if (b_iv[h] < 0.f) b0 = b1 = 0;  // values of zero
+                    if (D == 128) {
+                        value_word<D>(acc.o, vx[h][0].x, vx[h][1].x, vx[h][2].x, vx[h][3].x, b0, b1);
+                        value_word<D>(acc.o + 2, vx[h][0].y, vx[h][1].y, vx[h][2].y, vx[h][3].y, b0, b1);
+                        value_word<D>(acc.o + D / 32, vx[h][0].z, vx[h][1].z, vx[h][2].z, vx[h][3].z, b0, b1);
+                        value_word<D>(acc.o + D / 32 + 2, vx[h][0].w, vx[h][1].w, vx[h][2].w, vx[h][3].w, b0, b1);
+                    } else {
+                        value_word<D>(acc.o, vy[h][0].x, vy[h][1].x, vy[h][2].x, vy[h][3].x, b0, b1);
+                        value_word<D>(acc.o + 2, vy[h][0].y, vy[h][1].y, vy[h][2].y, vy[h][3].y, b0, b1);
                     }
-                }
-                const float ka = b_ks * scale2[0], kb = b_ks * scale2[1];
-                float p[4] = {fmaf(s0[0] + s1[0], ka, b_lv), fmaf(s0[1] + s1[1], kb, b_lv), fmaf(s0[2] + s1[2], ka, b_lv), fmaf(s0[3] + s1[3], kb, b_lv)};
-                acc.softmax(p, fabsf(b_iv));
-                if (b_iv < 0.f) continue;  // values of zero
-                const uint32_t b0 = movmatrix_trans(pack_f16(p[0], p[1])), b1 = movmatrix_trans(pack_f16(p[2], p[3]));
-                if (D == 128) {
-                    value_word<D>(acc.o, vx[0].x, vx[1].x, vx[2].x, vx[3].x, b0, b1);
-                    value_word<D>(acc.o + 2, vx[0].y, vx[1].y, vx[2].y, vx[3].y, b0, b1);
-                    value_word<D>(acc.o + D / 32, vx[0].z, vx[1].z, vx[2].z, vx[3].z, b0, b1);
-                    value_word<D>(acc.o + D / 32 + 2, vx[0].w, vx[1].w, vx[2].w, vx[3].w, b0, b1);
-                } else {
-                    value_word<D>(acc.o, vy[0].x, vy[1].x, vy[2].x, vy[3].x, b0, b1);
-                    value_word<D>(acc.o + 2, vy[0].y, vy[1].y, vy[2].y, vy[3].y, b0, b1);
                 }
             }
             // open rows whose place on the line lies in the stretch
-            const int tail0 = (max(p0 - kPad - sp.groups, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - kPad - sp.groups, 0) + kTailWeight - 1) / kTailWeight;
+            const int tail0 = (max(p0 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight;
             for (int j = tail0; j < tail1 && 16 * j < sp.open; ++j) open_rows<D>(a, acc, it, 16 * j, sp.open, open2, v_ref, __log2f(inv_ref));
 
 #pragma unroll
@@ -626,23 +709,39 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 l = 0.f;
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 4
-                for (int cta = c0; cta <= c1; ++cta) {
-                    const float* src = a.cta_part + (((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * 8 + head) * kBlockPart;
-                    const float2 ml = __ldcg(reinterpret_cast<const float2*>(src));
-                    float x[E];
-                    if constexpr (E == 4) {
-                        const float4 v = __ldcg(reinterpret_cast<const float4*>(src + 4) + lane);
-                        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-                    } else {
-                        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + 4) + lane);
-                        x[0] = v.x, x[1] = v.y;
-                    }
-                    const float nm = fmaxf(m, ml.x), g0 = exp2_diff(m, nm), g1 = exp2_diff(ml.x, nm);
-                    l = l * g0 + ml.y * g1;
+#pragma unroll 1
+                for (int base = c0; base <= c1; base += 32) {  // the statistics of 32 parts at once, then their O
+                    auto part_of = [&](int cta) { return a.cta_part + (((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * 8 + head) * kBlockPart; };
+                    const int n = min(32, c1 - base + 1);
+                    const float2 ml = lane < n ? __ldcg(reinterpret_cast<const float2*>(part_of(base + lane))) : make_float2(-INFINITY, 0.f);
+                    float nm = ml.x;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = o[e] * g0 + x[e] * g1;
+                    for (int k = 16; k; k >>= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, k));
+                    nm = fmaxf(nm, m);
+                    const float f = exp2_diff(m, nm), g = exp2_diff(ml.x, nm);
+                    float sum = ml.y * g;
+#pragma unroll
+                    for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+                    l = l * f + sum;
                     m = nm;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll 8
+                    for (int k = 0; k < n; ++k) {
+                        const float* src = part_of(base + k) + 4 + E * lane;
+                        const float gk = __shfl_sync(0xffffffffu, g, k);
+                        if constexpr (E == 4) {
+                            const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
+                            o[0] = fmaf(x.x, gk, o[0]);
+                            o[1] = fmaf(x.y, gk, o[1]);
+                            o[2] = fmaf(x.z, gk, o[2]);
+                            o[3] = fmaf(x.w, gk, o[3]);
+                        } else {
+                            const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
+                            o[0] = fmaf(x.x, gk, o[0]);
+                            o[1] = fmaf(x.y, gk, o[1]);
+                        }
+                    }
                 }
             }
             const size_t row = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G + head;
@@ -670,7 +769,7 @@ bool build_block_maps(void* encode, const BlockView& c, BlockMaps* maps) {
     encode_fn fn = reinterpret_cast<encode_fn>(encode);
     const cuuint64_t dims[2] = {(cuuint64_t)c.D, (cuuint64_t)c.n_pages * c.T};
     const cuuint64_t pitch[1] = {(cuuint64_t)c.D};
-    const cuuint32_t box[2] = {(cuuint32_t)c.D, 16}, es[2] = {1, 1};
+    const cuuint32_t box[2] = {(cuuint32_t)c.D, (cuuint32_t)(c.T < kStep ? c.T : kStep)}, es[2] = {1, 1};
     const CUtensorMapSwizzle swizzle = c.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
     for (int i = 0; i < 2; ++i)
         if (fn(i ? &maps->v : &maps->k, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, i ? c.v : c.k, dims, pitch, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,

@@ -6,8 +6,8 @@
 
 namespace lethe {
 
-constexpr int kBlockWarps = 12;  // warps of a CTA, each with a ring of its own; one CTA per SM
-constexpr int kBlockStages = 2;  // groups of 16 tokens in a ring at D = 128
+constexpr int kBlockWarps = 8;  // warps of a CTA, each with a ring of its own; one CTA per SM
+constexpr int kBlockStages = 2;  // steps of 32 tokens in a ring at D = 128
 
 struct alignas(64) BlockMaps {
     CUtensorMap k, v;  // [blocks * block_tokens][D] bytes, boxes of 16 rows
