@@ -427,7 +427,8 @@ lethe_status lethe_chunk_attend(lethe_ctx *ctx, const lethe_cache *cache, int la
  * keys in the cache), tokens of a step that is attended later.  Layers [layer_begin, layer_end); chunk_start, n_tokens,
  * max_chunk, k_new, v_new and token_pos as in lethe_chunk_attend (all required).  Per item with n = len and T = T_b: rows go to
  * slots n .. n+T-1 in the cache's storage type, pos = token_pos, rel = 0, len = n + T.
- *   rotary      NULL: k_new comes rotated; else it is rotated on the way, as by lethe_rotate
+ *   rotary      NULL: k_new comes rotated; else it is rotated on the way, as by lethe_rotate up to the last bits (cosines and
+ *               sines are off by at most 2^-23; arithmetic in fp32, one rounding to the type of k_new)
  *   q, q_out    [nl][n_tokens][Hq][D], both NULL or both given (with rotary): the same tokens' queries, rotated in the same
  *               launch.  q_out may be q; it must not overlap anything else.
  * What the device refuses is refused as in lethe_chunk_attend: an item that cannot take its T tokens stays as it is

@@ -85,21 +85,50 @@ __device__ __forceinline__ long long block_page(const BlockView& c, int item, in
 }
 __device__ __forceinline__ int block_len(const BlockView& c, int item) { return min(max(c.len[item], 0), c.cap_tokens); }
 
-// Whether chunk_start is well-formed (the same answer in every thread of the block; a barrier).
-__device__ __forceinline__ bool starts_ok(const int32_t* start, int B, int n_tokens, int max_chunk) {
+// Whether chunk_start is well-formed (the same answer in every thread of the block; a barrier).  `kept`: a table of kStartsKept entries in
+// shared memory that takes it, where there are fewer sequences than that.
+constexpr int kStartsKept = 512;
+__device__ __forceinline__ bool starts_ok(const int32_t* start, int B, int n_tokens, int max_chunk, int* kept) {
     bool ok = true;
     for (int b = threadIdx.x; b < B; b += blockDim.x) {
         const int s0 = start[b], s1 = start[b + 1];
         ok = ok && s0 >= 0 && s1 >= s0 && s1 <= n_tokens && s1 - s0 <= max_chunk;
+        if (kept && B < kStartsKept) {
+            kept[b] = s0;
+            if (b == B - 1) kept[B] = s1;
+        }
     }
     return __syncthreads_and(ok);
 }
+// The sequence of a token: the last b with start[b] <= tok (empty ones before it are passed over).
+__device__ __forceinline__ int sequence_of(const int32_t* start, int B, int tok) {
+    int b = 0, hi = B;
+    while (hi - b > 1) {
+        const int mid = (b + hi) >> 1;
+        if (start[mid] <= tok) b = mid;
+        else hi = mid;
+    }
+    return b;
+}
 
-// cos and sin of one pair's angle, position x frequency taken in turns as a 64-bit fraction (whose overflow is the reduction).
-__device__ __forceinline__ void pair_turn(const NewRows& in, int pair, int pos, float& c, float& s) {
-    const unsigned long long turn = (unsigned long long)(long long)pos * in.turn[pair];
-    const int top = (int)((turn + 0x80000000ull) >> 32);  // the nearest 2^-32 turn, as a signed fraction
-    sincospif((float)top * 4.656612873077393e-10f, &s, &c);  // 2^-31: half turns
+// cos and sin of one pair's angle, position x frequency taken in turns as a 64-bit fraction (whose overflow is the reduction).  The nearest
+// quarter turn is taken off exactly; on the eighth of a turn either side that is left, z = -1 .. 1, sin(pi z / 4) / z and
+// (cos(pi z / 4) - 1) / z^2 are cubics in z^2 fitted for the smallest largest error (2.4e-9 and 1.9e-10): about 25 instructions, largest error
+// with all roundings 1.02e-7 (2^-23 is 1.19e-7), 2e-8 on average; an angle rounded to fp32 before its reduction has three times that.
+// A pair's frequency comes from the kernel's parameters: a thread that makes several angles of a pair keeps it, since lanes that read
+// different parameters are served one after the other.
+__device__ __forceinline__ void turn_by(unsigned long long per_pos, int pos, float& c, float& s) {
+    const unsigned long long turn = (unsigned long long)(long long)pos * per_pos;
+    const unsigned top = (unsigned)((turn + 0x80000000ull) >> 32) + 0x20000000u;  // the nearest 2^-32 turn, an eighth of a turn on
+    const float z = (float)((int)(top & 0x3fffffffu) - 0x20000000) * 1.862645149230957e-9f;  // 2^-29
+    const float u = z * z;
+    const float si = z * fmaf(fmaf(fmaf(-3.595450834836811e-05f, u, 0.002490007085725665f), u, -0.08074543625116348f), u, 0.7853981852531433f);
+    const float co = fmaf(fmaf(fmaf(fmaf(3.5419668620306766e-06f, u, -0.00032596138771623373f), u, 0.01585433818399906f), u, -0.3084251284599304f), u, 1.f);
+    const unsigned quarter = top >> 30;
+    c = quarter & 1 ? si : co;
+    s = quarter & 1 ? co : si;
+    if ((quarter + 1) & 2) c = -c;
+    if (quarter & 2) s = -s;
 }
 
 // 16 bytes of a row as floats, and back.
@@ -155,38 +184,46 @@ inline bool rotation_in_pieces(const NewRows& in) {
     return in.rot_dim % (2 * Piece<T>::N) == 0;
 }
 
-// Rotates the two pieces of a task; cs / sn of pair p by the caller's look-up.
-template <typename T, typename Look>
-__device__ __forceinline__ void turn_pieces(const NewRows& in, int at0, uint4& x, uint4& y, Look look) {
+// The first of the N pairs of a rotated task.
+__device__ __forceinline__ int first_pair(const NewRows& in, int at0) { return in.halves ? at0 : at0 / 2; }
+
+// Rotates the two pieces of a task by the cosines and sines of its N pairs.
+template <typename T>
+__device__ __forceinline__ void turn_pieces(const NewRows& in, uint4& x, uint4& y, const float (&c)[Piece<T>::N], const float (&s)[Piece<T>::N]) {
     using P = Piece<T>;
-    float f[P::N], g[P::N];
+    constexpr int N = P::N;
+    float f[N], g[N];
     P::unpack(x, f);
     P::unpack(y, g);
     if (in.halves) {
 #pragma unroll
-        for (int i = 0; i < P::N; ++i) {
-            float c, s;
-            look(at0 + i, c, s);
+        for (int i = 0; i < N; ++i) {
             const float v = f[i], w = g[i];
-            f[i] = v * c - w * s;
-            g[i] = v * s + w * c;
+            f[i] = v * c[i] - w * s[i];
+            g[i] = v * s[i] + w * c[i];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < P::N; i += 2) {
-            float c, s;
-            look((at0 + i) / 2, c, s);
+        for (int i = 0; i < N; i += 2) {
             float v = f[i], w = f[i + 1];
-            f[i] = v * c - w * s;
-            f[i + 1] = v * s + w * c;
-            look((at0 + P::N + i) / 2, c, s);
+            f[i] = v * c[i / 2] - w * s[i / 2];
+            f[i + 1] = v * s[i / 2] + w * c[i / 2];
             v = g[i], w = g[i + 1];
-            g[i] = v * c - w * s;
-            g[i + 1] = v * s + w * c;
+            g[i] = v * c[N / 2 + i / 2] - w * s[N / 2 + i / 2];
+            g[i + 1] = v * s[N / 2 + i / 2] + w * c[N / 2 + i / 2];
         }
     }
     x = P::pack(f);
     y = P::pack(g);
+}
+// N cosines or sines from a table in shared memory (16-byte aligned, as the task's first pair is).
+template <int N>
+__device__ __forceinline__ void look_up(const float* table, float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(table + i);
+        v[i] = x.x, v[i + 1] = x.y, v[i + 2] = x.z, v[i + 3] = x.w;
+    }
 }
 
 // One element of a rotated row, from memory (rotations whose pairs do not come in whole pieces).
@@ -202,28 +239,20 @@ __device__ __forceinline__ float turned_element(const NewRows& in, const T* src,
     // one product rounded, the other fused with the sum: as the compiler forms it where both elements are made at once
     return d == i0 ? fmaf(v, c, -__fmul_rn(w, s)) : fmaf(v, s, __fmul_rn(w, c));
 }
-// The two pieces of a task, rotated or copied.
-template <typename T, bool VEC, typename Look>
-__device__ __forceinline__ void load_task(const NewRows& in, const T* src, int task, bool rotated_row, Look look, int& at0, int& at1, uint4& x, uint4& y) {
-    bool turned;
-    if (VEC || !rotated_row) {
-        piece_pair<T>(in, task, rotated_row, at0, at1, turned);
-        x = *reinterpret_cast<const uint4*>(src + at0);
-        y = *reinterpret_cast<const uint4*>(src + at1);
-        if (turned) turn_pieces<T>(in, at0, x, y, look);
-    } else {
-        constexpr int N = Piece<T>::N;
-        at0 = 2 * task * N;
-        at1 = at0 + N;
-        float f[N], g[N];
+// The two pieces of a task of a row whose pairs do not come in whole pieces.
+template <typename T, typename Look>
+__device__ __forceinline__ void load_by_element(const NewRows& in, const T* src, int task, Look look, int& at0, int& at1, uint4& x, uint4& y) {
+    constexpr int N = Piece<T>::N;
+    at0 = 2 * task * N;
+    at1 = at0 + N;
+    float f[N], g[N];
 #pragma unroll 1
-        for (int i = 0; i < N; ++i) {
-            f[i] = turned_element<T>(in, src, at0 + i, look);
-            g[i] = turned_element<T>(in, src, at1 + i, look);
-        }
-        x = Piece<T>::pack(f);
-        y = Piece<T>::pack(g);
+    for (int i = 0; i < N; ++i) {
+        f[i] = turned_element<T>(in, src, at0 + i, look);
+        g[i] = turned_element<T>(in, src, at1 + i, look);
     }
+    x = Piece<T>::pack(f);
+    y = Piece<T>::pack(g);
 }
 
 }  // namespace lethe

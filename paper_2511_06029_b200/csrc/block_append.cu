@@ -4,10 +4,13 @@
 namespace lethe {
 cudaError_t launch_append_len(const int32_t* chunk_start, int32_t* len, int B, int Hkv, int layer_begin, int n_items, int n_tokens, int max_chunk,
                               int cap_tokens, cudaStream_t stream);
+cudaError_t launch_append_queries(const NewRows& in, int nl, int B, int Hq, int D, int32_t* status, cudaStream_t stream);
 namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kQueryRows = 16;
+constexpr int kPlenty = 1184;  // blocks to fill: eight for each of 148 SMs
+constexpr int kFewTokens = 4;  // tokens to a sequence that a warp takes one after the other
 
 __device__ __forceinline__ float finite_top(const uint4& w, float top) {
     float f[8];
@@ -31,33 +34,84 @@ __device__ __forceinline__ uint2 codes8(const uint4& w, float inv) {
     return make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
 }
 
-// The first n_items * units blocks: unit u of an item quantises the u-th of the blocks that the call fills; unit 0 also moves what is
-// left over to the open block (it has read the rows that were there by then).  The rest rotate queries, kQueryRows rows of a token each.
+// What a call does to an item.
+struct Filled {
+    int li, h, item;
+    int s0, n0, n1;  // first new token; tokens before and after; n1 = 0: no tokens, -1: no room for them
+};
+__device__ __forceinline__ Filled filled(const BlockView& c, const NewRows& in, int idx) {
+    const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, idx);
+    Filled f = {it.li, it.h, it.item, in.chunk_start[it.b], 0, 0};
+    const int n_new = max(in.chunk_start[it.b + 1] - f.s0, 0);  // before chunk_start has been looked over: it may hold anything
+    f.n0 = block_len(c, it.item);
+    if (n_new > 0 && f.n0 + (long long)n_new <= c.cap_tokens) f.n1 = f.n0 + n_new;
+    else if (n_new > 0) f.n1 = -1;
+    return f;
+}
+
+// Blocks of threads: first those of the items.
+// FEW (calls of a few tokens to a sequence): one to as many items as it has warps, since mostly a few rows go to open blocks, a warp's
+// work; items that fill a block then have all warps, one after the other.
+// Else: `units` to `heads` (1 .. 8) KV heads of a sequence, which share the cosines and sines of their tokens (where they have the same length, as
+// they mostly do).  Unit u quantises the u-th of the blocks that the call fills; unit 0 also moves what is left over to the open block (it
+// has read the rows that were there by then).
+// The rest of the blocks rotate queries, kQueryRows rows of a token each.
 // Bound by memory: rows are read once and kept packed in registers between the search for the largest magnitude and the rounding.
-template <int D, int TPT, bool VEC>  // TPT: tasks of 16 elements per thread, of K and of V
-__global__ void __launch_bounds__(256) block_append_kernel(const __grid_constant__ BlockView c, const __grid_constant__ NewRows in, int units) {
-    extern __shared__ __align__(16) unsigned char tile[];  // [T][D] key codes
-    __shared__ unsigned long long turn[64];
-    __shared__ unsigned char axis[64];
-    __shared__ float cs[64], sn[64];
+template <int D, int TPT, bool VEC, bool FEW>  // TPT: tasks of 16 elements per thread, of K and of V
+__global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_append_kernel(const __grid_constant__ BlockView c, const __grid_constant__ NewRows in, int units, int heads, unsigned kv_blocks) {
+    extern __shared__ __align__(16) unsigned char tile[];  // [T][D] key codes; then cosines [T][D / 2] and sines of a block's new tokens
+    float* cos_at = reinterpret_cast<float*>(tile + c.T * D);
+    float* sin_at = cos_at + c.T * (D / 2);
+    __shared__ __align__(16) float cs[FEW ? 8 : 1][64], sn[FEW ? 8 : 1][64];  // of one token: queries, or a warp's row
     __shared__ float tops[2][8];
     __shared__ uint32_t least[8][32], greatest[8][32];
+    __shared__ Filled some[8];
     dependency_wait();
     dependency_release();
-    const int tid = threadIdx.x, nt = blockDim.x;
+    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, w = tid >> 5;
     constexpr int kPerRow = D / 16;
     const int half = in.rot_dim / 2;
-    const bool ok = starts_ok(in.chunk_start, c.B, in.n_tokens, in.max_chunk);
-    if (!ok) {
+    // the items of the block, one to a warp (FEW) or one after the other; their lengths are asked for together with chunk_start
+    const int groups = (c.Hkv + heads - 1) / heads, g = blockIdx.x / units, u = blockIdx.x - g * units;
+    if (blockIdx.x < kv_blocks) {
+        const int i = FEW ? w : tid;
+        const int idx = FEW ? blockIdx.x * (nt / 32) + i : g / groups * c.Hkv + g % groups * heads + i;
+        if (FEW ? lane == 0 : i < heads) {
+            some[i] = Filled{0, 0, 0, 0, 0, 0};
+            if (FEW ? idx < c.n_items : g % groups * heads + i < c.Hkv) some[i] = filled(c, in, idx);
+        }
+    }
+    if (!starts_ok(in.chunk_start, c.B, in.n_tokens, in.max_chunk, nullptr)) {
         if (blockIdx.x == 0 && tid == 0) record_error(c.status, LETHE_ERR_INVALID_ARG, 0);
         return;
     }
-    const unsigned kv_blocks = (unsigned)c.n_items * units;
+    // the pieces of a row's task; rotated by a row of cosines and sines
+    auto load_row = [&](const bf16* src, int task, bool rotated, const float* co_row, const float* si_row, int& at0, int& at1, uint4& x, uint4& y) {
+        if (VEC || !rotated) {
+            bool turned;
+            piece_pair<bf16>(in, task, rotated, at0, at1, turned);
+            x = *reinterpret_cast<const uint4*>(src + at0);
+            y = *reinterpret_cast<const uint4*>(src + at1);
+        } else {
+            load_by_element<bf16>(in, src, task, [&](int p, float& co, float& si) { co = co_row[p], si = si_row[p]; }, at0, at1, x, y);
+        }
+    };
+    auto turn_row = [&](int task, const float* co_row, const float* si_row, uint4& x, uint4& y) {
+        int at0, at1;
+        bool turned;
+        piece_pair<bf16>(in, task, true, at0, at1, turned);
+        if (turned) {
+            float co[8], si[8];
+            look_up(co_row + first_pair(in, at0), co);
+            look_up(si_row + first_pair(in, at0), si);
+            turn_pieces<bf16>(in, x, y, co, si);
+        }
+    };
     if (blockIdx.x >= kv_blocks) {
         const int rows_total = c.nl * c.Hq, per_tok = (rows_total + kQueryRows - 1) / kQueryRows;
         const int qb = blockIdx.x - kv_blocks, tok = qb / per_tok, r0 = (qb - tok * per_tok) * kQueryRows;
         if (tok < in.chunk_start[0] || tok >= in.chunk_start[c.B]) return;
-        for (int p = tid; p < half; p += nt) pair_turn(in, p, in.axis_pos[(size_t)in.axis[p] * in.n_tokens + tok], cs[p], sn[p]);
+        if (tid < half) turn_by(in.turn[tid], in.axis_pos[(size_t)in.axis[tid] * in.n_tokens + tok], cs[0][tid], sn[0][tid]);  // half <= 64 <= nt
         __syncthreads();
         const int tasks = min(rows_total - r0, kQueryRows) * kPerRow;
         for (int t0 = 0; t0 < tasks; t0 += nt) {  // uniform for the block
@@ -65,8 +119,10 @@ __global__ void __launch_bounds__(256) block_append_kernel(const __grid_constant
             const size_t off = (((size_t)li * in.n_tokens + tok) * c.Hq + r - li * c.Hq) * D;
             int at0, at1;
             uint4 x, y;
-            if (t < tasks)
-                load_task<bf16, VEC>(in, (const bf16*)in.q + off, t % kPerRow, true, [&](int p, float& co, float& si) { co = cs[p], si = sn[p]; }, at0, at1, x, y);
+            if (t < tasks) {
+                load_row((const bf16*)in.q + off, t % kPerRow, true, cs[0], sn[0], at0, at1, x, y);
+                if (VEC) turn_row(t % kPerRow, cs[0], sn[0], x, y);
+            }
             if (!VEC) __syncwarp();  // q_out may be q: a row's tasks lie in one warp, all have read before one writes
             if (t < tasks) {
                 *reinterpret_cast<uint4*>((bf16*)in.q_out + off + at0) = x;
@@ -75,224 +131,327 @@ __global__ void __launch_bounds__(256) block_append_kernel(const __grid_constant
         }
         return;
     }
-    const int idx = blockIdx.x / units, u = blockIdx.x - idx * units;
-    const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, idx);
-    const int s0 = in.chunk_start[it.b], n_new = in.chunk_start[it.b + 1] - s0;
-    if (n_new == 0) return;
-    const int n0 = block_len(c, it.item);
-    if (n0 + (long long)n_new > c.cap_tokens) {
-        if (u == 0 && tid == 0) record_error(c.status, LETHE_ERR_CAPACITY, it.item);
-        return;
-    }
-    const int n1 = n0 + n_new, b0 = n0 >> c.t_shift, b1 = n1 >> c.t_shift;
-    if (u > 0 && b0 + u >= b1) return;
-    if (in.axis_pos) {
-        for (int p = tid; p < half; p += nt) {
-            turn[p] = in.turn[p];
-            axis[p] = in.axis[p];
-        }
-        __syncthreads();
-    }
-    const size_t open = (size_t)it.item * c.T;
-    const bf16* new_k = (const bf16*)in.k + ((size_t)it.li * in.n_tokens * c.Hkv + it.h) * D;
-    const bf16* new_v = (const bf16*)in.v + ((size_t)it.li * in.n_tokens * c.Hkv + it.h) * D;
-    const size_t tok_pitch = (size_t)c.Hkv * D;
-    auto load_new = [&](int tok, int task, int& at0, int& at1, uint4& kx, uint4& ky, uint4& vx, uint4& vy) {
-        auto look = [&](int p, float& co, float& si) {
-            const int pos = in.axis_pos[(size_t)axis[p] * in.n_tokens + tok];
-            const unsigned long long full = (unsigned long long)(long long)pos * turn[p];
-            sincospif((float)(int)((full + 0x80000000ull) >> 32) * 4.656612873077393e-10f, &si, &co);  // as pair_turn
-        };
-        load_task<bf16, VEC>(in, new_k + tok * tok_pitch, task, in.axis_pos != nullptr, look, at0, at1, kx, ky);
-        const bf16* v = new_v + tok * tok_pitch;
-        vx = *reinterpret_cast<const uint4*>(v + at0);
-        vy = *reinterpret_cast<const uint4*>(v + at1);
+    const bool rotated = in.axis_pos != nullptr;
+    auto row_of = [&](const Filled& f, int slot) { return (((size_t)f.li * in.n_tokens + f.s0 + slot - f.n0) * c.Hkv + f.h) * D; };
+    auto put = [&](const Filled& f, int slot, int at0, int at1, const uint4& kx, const uint4& ky, const uint4& vx, const uint4& vy) {
+        const size_t off = ((size_t)f.item * c.T + (slot & (c.T - 1))) * D;
+        *reinterpret_cast<uint4*>(c.k_open + off + at0) = kx;
+        *reinterpret_cast<uint4*>(c.k_open + off + at1) = ky;
+        *reinterpret_cast<uint4*>(c.v_open + off + at0) = vx;
+        *reinterpret_cast<uint4*>(c.v_open + off + at1) = vy;
     };
-    if (b0 + u < b1) {
-        const int blk = b0 + u;
+    unsigned long long per_pos = 0;  // of pair tid % 64
+    size_t axis_at = 0;
+    if (rotated && (tid & 63) < half) {
+        per_pos = in.turn[tid & 63];
+        axis_at = (size_t)in.axis[tid & 63] * in.n_tokens;
+    }
+    // cosines and sines of the new tokens of slots s_first .. s_end - 1 of a block
+    auto angles = [&](const Filled& f, int s_first, int s_end) {
+        const int p = tid & 63, step = nt >> 6;
+        if (p >= half) return;
+        const int32_t* pos = in.axis_pos + axis_at + f.s0 - f.n0;
+        int at = s_first + (tid >> 6) < s_end ? pos[s_first + (tid >> 6)] : 0;
+#pragma unroll 1
+        for (int slot = s_first + (tid >> 6); slot < s_end; slot += step) {
+            const int next = slot + step < s_end ? pos[slot + step] : 0;
+            const int to = (slot & (c.T - 1)) * (D / 2) + p;
+            turn_by(per_pos, at, cos_at[to], sin_at[to]);
+            at = next;
+        }
+    };
+    // new rows from slot s_first on to the item's open block, by all threads
+    auto to_open = [&](const Filled& f, int s_first) {
+        if (s_first >= f.n1) return;
+        if (rotated) {
+            __syncthreads();
+            angles(f, s_first, f.n1);
+            __syncthreads();
+        }
+        for (int t = tid; t < (f.n1 - s_first) * kPerRow; t += nt) {
+            const int slot = s_first + t / kPerRow, task = t % kPerRow, row = (slot & (c.T - 1)) * (D / 2);
+            int at0, at1;
+            uint4 kx, ky;
+            load_row((const bf16*)in.k + row_of(f, slot), task, rotated, cos_at + row, sin_at + row, at0, at1, kx, ky);
+            const bf16* v = (const bf16*)in.v + row_of(f, slot);
+            const uint4 vx = *reinterpret_cast<const uint4*>(v + at0), vy = *reinterpret_cast<const uint4*>(v + at1);
+            if (VEC && rotated) turn_row(task, cos_at + row, sin_at + row, kx, ky);
+            put(f, slot, at0, at1, kx, ky, vx, vy);
+        }
+    };
+    // a block that the call fills, by all threads; `known`: the angles of its new tokens are there already
+    auto to_block = [&](const Filled& f, int blk, bool known) {
+        const size_t open = (size_t)f.item * c.T;
+        const int slot0 = blk << c.t_shift;
         uint4 kx[TPT], ky[TPT], vx[TPT], vy[TPT];
+        auto fetch = [&]() {
+#pragma unroll
+            for (int i = 0; i < TPT; ++i) {
+                const int t = tid + i * nt, r = t / kPerRow, task = t % kPerRow, slot = slot0 + r;
+                int at0, at1;
+                const bool old = slot < f.n0;
+                const bf16* k = old ? c.k_open + (open + r) * D : (const bf16*)in.k + row_of(f, slot);
+                const bf16* v = old ? c.v_open + (open + r) * D : (const bf16*)in.v + row_of(f, slot);
+                if (VEC || !rotated || !old) {
+                    load_row(k, task, rotated, cos_at + r * (D / 2), sin_at + r * (D / 2), at0, at1, kx[i], ky[i]);
+                } else {  // the pieces as load_by_element takes them
+                    at0 = 16 * task;
+                    at1 = at0 + 8;
+                    kx[i] = *reinterpret_cast<const uint4*>(k + at0);
+                    ky[i] = *reinterpret_cast<const uint4*>(k + at1);
+                }
+                vx[i] = *reinterpret_cast<const uint4*>(v + at0);
+                vy[i] = *reinterpret_cast<const uint4*>(v + at1);
+            }
+        };
+        if (VEC || !rotated) fetch();
+        __syncthreads();  // the tables of the block before have been read
+        if (rotated && !known) {
+            angles(f, max(slot0, f.n0), slot0 + c.T);
+            __syncthreads();
+        }
+        if (!VEC && rotated) fetch();
         float top_k = 0.f, top_v = 0.f;
 #pragma unroll
         for (int i = 0; i < TPT; ++i) {
-            const int t = tid + i * nt, r = t / kPerRow, slot = (blk << c.t_shift) + r;
-            int at0, at1;
-            if (slot < n0) {
-                bool turned;
-                piece_pair<bf16>(in, t % kPerRow, VEC && in.axis_pos, at0, at1, turned);
-                const size_t off = (open + r) * D;
-                kx[i] = *reinterpret_cast<const uint4*>(c.k_open + off + at0);
-                ky[i] = *reinterpret_cast<const uint4*>(c.k_open + off + at1);
-                vx[i] = *reinterpret_cast<const uint4*>(c.v_open + off + at0);
-                vy[i] = *reinterpret_cast<const uint4*>(c.v_open + off + at1);
-            } else {
-                load_new(s0 + slot - n0, t % kPerRow, at0, at1, kx[i], ky[i], vx[i], vy[i]);
-            }
+            const int t = tid + i * nt, r = t / kPerRow;
+            if (VEC && rotated && slot0 + r >= f.n0) turn_row(t % kPerRow, cos_at + r * (D / 2), sin_at + r * (D / 2), kx[i], ky[i]);
             top_k = finite_top(ky[i], finite_top(kx[i], top_k));
             top_v = finite_top(vy[i], finite_top(vx[i], top_v));
         }
+        const long long page = block_page(c, f.item, blk);
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
             top_k = fmaxf(top_k, __shfl_xor_sync(0xffffffffu, top_k, o));
             top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
         }
-        if ((tid & 31) == 0) {
-            tops[0][tid >> 5] = top_k;
-            tops[1][tid >> 5] = top_v;
+        if (lane == 0) {
+            tops[0][w] = top_k;
+            tops[1][w] = top_v;
         }
         __syncthreads();
-        for (int w = 0; w < nt / 32; ++w) {
-            top_k = fmaxf(top_k, tops[0][w]);
-            top_v = fmaxf(top_v, tops[1][w]);
+        for (int i = 0; i < nt / 32; ++i) {
+            top_k = fmaxf(top_k, tops[0][i]);
+            top_v = fmaxf(top_v, tops[1][i]);
+        }
+        if (page < 0) {
+            if (tid == 0) record_error(c.status, LETHE_ERR_PAGE, f.item);
+            return;
         }
         const float inv_k = top_k >= kBlockTiny ? __fdiv_rn(127.f, top_k) : 0.f, inv_v = top_v >= kBlockTiny ? __fdiv_rn(127.f, top_v) : 0.f;
-        const long long page = block_page(c, it.item, blk);
-        if (page < 0) {
-            if (tid == 0) record_error(c.status, LETHE_ERR_PAGE, it.item);
-        } else {
-            int8_t* kd = c.k + (size_t)page * c.T * D;
-            int8_t* vd = c.v + (size_t)page * c.T * D;
+        int8_t* kd = c.k + (size_t)page * c.T * D;
+        int8_t* vd = c.v + (size_t)page * c.T * D;
 #pragma unroll
-            for (int i = 0; i < TPT; ++i) {
-                const int t = tid + i * nt, r = t / kPerRow;
-                int at0, at1;
-                bool turned;
-                piece_pair<bf16>(in, t % kPerRow, VEC && in.axis_pos, at0, at1, turned);
-                const uint2 a = codes8(kx[i], inv_k), b = codes8(ky[i], inv_k);
-                *reinterpret_cast<uint2*>(kd + r * D + at0) = a;
-                *reinterpret_cast<uint2*>(kd + r * D + at1) = b;
-                *reinterpret_cast<uint2*>(tile + r * D + at0) = a;
-                *reinterpret_cast<uint2*>(tile + r * D + at1) = b;
-                *reinterpret_cast<uint2*>(vd + r * D + at0) = codes8(vx[i], inv_v);
-                *reinterpret_cast<uint2*>(vd + r * D + at1) = codes8(vy[i], inv_v);
-            }
-            if (tid == 0) {
-                c.k_scale[page] = top_k >= kBlockTiny ? __fdiv_rn(top_k, 127.f) : 0.f;
-                c.v_scale[page] = top_v >= kBlockTiny ? __fdiv_rn(top_v, 127.f) : 0.f;
-            }
-            if (c.k_range) {
-                // four elements to a thread, the rows in turn among the groups of threads
-                constexpr int W = D / 4;
-                const int groups = nt / W, w = tid % W, gr = tid / W;
-                __syncthreads();
-                uint32_t lo = 0x7f7f7f7fu, hi = 0x81818181u;
-                for (int r = gr; r < c.T; r += groups) {
-                    const uint32_t x = *reinterpret_cast<const uint32_t*>(tile + r * D + 4 * w);
-                    lo = __vmins4(lo, x);
-                    hi = __vmaxs4(hi, x);
-                }
-                // at D = 64 there may be more groups than rows of the table: they fold by shuffles (W = 16 lanes apart)
-                if (W == 16) {
-                    lo = __vmins4(lo, __shfl_xor_sync(0xffffffffu, lo, 16));
-                    hi = __vmaxs4(hi, __shfl_xor_sync(0xffffffffu, hi, 16));
-                }
-                least[tid >> 5][tid & 31] = lo;
-                greatest[tid >> 5][tid & 31] = hi;
-                __syncthreads();
-                if (tid < W) {
-                    for (int g = 1; g < nt / 32; ++g) {
-                        lo = __vmins4(lo, least[g][w]);
-                        hi = __vmaxs4(hi, greatest[g][w]);
-                    }
-                    uint32_t* range = reinterpret_cast<uint32_t*>(c.k_range + (size_t)page * 2 * D);
-                    range[w] = lo;
-                    range[W + w] = hi;
-                }
-            }
-        }
-    }
-    if (u == 0) {
-        // what is left over; all reads of open rows lie before the barrier
-        __syncthreads();
-        const int s_first = b1 > b0 ? b1 << c.t_shift : n0;
-        for (int t = tid; t < (n1 - s_first) * kPerRow; t += nt) {
-            const int slot = s_first + t / kPerRow;
+        for (int i = 0; i < TPT; ++i) {
+            const int t = tid + i * nt, r = t / kPerRow;
             int at0, at1;
-            uint4 kx, ky, vx, vy;
-            load_new(s0 + slot - n0, t % kPerRow, at0, at1, kx, ky, vx, vy);
-            const size_t off = (open + (slot & (c.T - 1))) * D;
-            *reinterpret_cast<uint4*>(c.k_open + off + at0) = kx;
-            *reinterpret_cast<uint4*>(c.k_open + off + at1) = ky;
-            *reinterpret_cast<uint4*>(c.v_open + off + at0) = vx;
-            *reinterpret_cast<uint4*>(c.v_open + off + at1) = vy;
+            bool turned;
+            piece_pair<bf16>(in, t % kPerRow, VEC && rotated, at0, at1, turned);
+            const uint2 a = codes8(kx[i], inv_k), b = codes8(ky[i], inv_k);
+            *reinterpret_cast<uint2*>(kd + r * D + at0) = a;
+            *reinterpret_cast<uint2*>(kd + r * D + at1) = b;
+            *reinterpret_cast<uint2*>(tile + r * D + at0) = a;
+            *reinterpret_cast<uint2*>(tile + r * D + at1) = b;
+            *reinterpret_cast<uint2*>(vd + r * D + at0) = codes8(vx[i], inv_v);
+            *reinterpret_cast<uint2*>(vd + r * D + at1) = codes8(vy[i], inv_v);
         }
-        if (units == 1 && tid == 0) c.len[it.item] = n1;  // no other block needs the item's old length
+        if (tid == 0) {
+            c.k_scale[page] = top_k >= kBlockTiny ? __fdiv_rn(top_k, 127.f) : 0.f;
+            c.v_scale[page] = top_v >= kBlockTiny ? __fdiv_rn(top_v, 127.f) : 0.f;
+        }
+        if (!c.k_range) return;
+        // four elements to a thread, the rows in turn among the groups of threads
+        constexpr int W = D / 4;
+        const int groups = nt / W, x4 = tid % W, gr = tid / W;
+        __syncthreads();
+        uint32_t lo = 0x7f7f7f7fu, hi = 0x81818181u;
+        for (int r = gr; r < c.T; r += groups) {
+            const uint32_t x = *reinterpret_cast<const uint32_t*>(tile + r * D + 4 * x4);
+            lo = __vmins4(lo, x);
+            hi = __vmaxs4(hi, x);
+        }
+        if (W == 16) {  // D = 64: two groups in a warp
+            lo = __vmins4(lo, __shfl_xor_sync(0xffffffffu, lo, 16));
+            hi = __vmaxs4(hi, __shfl_xor_sync(0xffffffffu, hi, 16));
+        }
+        least[w][lane] = lo;
+        greatest[w][lane] = hi;
+        __syncthreads();
+        if (tid < W) {
+            for (int g = 1; g < nt / 32; ++g) {
+                lo = __vmins4(lo, least[g][x4]);
+                hi = __vmaxs4(hi, greatest[g][x4]);
+            }
+            uint32_t* range = reinterpret_cast<uint32_t*>(c.k_range + (size_t)page * 2 * D);
+            range[x4] = lo;
+            range[W + x4] = hi;
+        }
+    };
+
+    if constexpr (!FEW) {
+        int known = -1;  // the length before the call of the item that the angles were made for
+        for (int i = 0; i < heads; ++i) {
+            const Filled f = some[i];
+            const int b0 = f.n0 >> c.t_shift, b1 = f.n1 >> c.t_shift;
+            if (f.n1 < 0 && u == 0 && tid == 0) record_error(c.status, LETHE_ERR_CAPACITY, f.item);
+            if (f.n1 <= 0 || (u > 0 && b0 + u >= b1)) continue;
+            if (b0 + u < b1) {
+                to_block(f, b0 + u, known == f.n0);
+                known = f.n0;
+            }
+            if (u == 0) {
+                __syncthreads();  // the open rows have been read
+                const int s_first = b1 > b0 ? b1 << c.t_shift : f.n0;
+                if (s_first < f.n1) known = -1;
+                to_open(f, s_first);
+                if (units == 1 && tid == 0) c.len[f.item] = f.n1;  // no other block needs the item's old length
+            }
+        }
+    } else {
+        const Filled f = some[w];
+        const bool fills = f.n1 > 0 && f.n1 >> c.t_shift > f.n0 >> c.t_shift;
+        if (f.n1 < 0 && lane == 0) record_error(c.status, LETHE_ERR_CAPACITY, f.item);
+        if (f.n1 > 0 && !fills)
+            for (int slot = f.n0; slot < f.n1; ++slot) {
+                if (rotated) {
+                    __syncwarp();
+                    for (int p = lane; p < half; p += 32) turn_by(in.turn[p], in.axis_pos[(size_t)in.axis[p] * in.n_tokens + f.s0 + slot - f.n0], cs[w][p], sn[w][p]);
+                    __syncwarp();
+                }
+                if (lane < kPerRow) {
+                    int at0, at1;
+                    uint4 kx, ky;
+                    load_row((const bf16*)in.k + row_of(f, slot), lane, rotated, cs[w], sn[w], at0, at1, kx, ky);
+                    const bf16* v = (const bf16*)in.v + row_of(f, slot);
+                    const uint4 vx = *reinterpret_cast<const uint4*>(v + at0), vy = *reinterpret_cast<const uint4*>(v + at1);
+                    if (VEC && rotated) turn_row(lane, cs[w], sn[w], kx, ky);
+                    put(f, slot, at0, at1, kx, ky, vx, vy);
+                }
+            }
+        if (__syncthreads_or(fills))
+            for (int i = 0; i < nt / 32; ++i) {
+                const Filled o = some[i];
+                const int b0 = o.n0 >> c.t_shift, b1 = o.n1 >> c.t_shift;
+                if (o.n1 <= 0 || b1 == b0) continue;
+                to_block(o, b0, false);
+                __syncthreads();  // the open rows have been read
+                to_open(o, b1 << c.t_shift);
+            }
+        if (lane == 0 && f.n1 > 0) c.len[f.item] = f.n1;
     }
 }
 
-// A thread takes 8 elements of a slot, of K and of V.
+// A thread takes 8 elements, of K and of V, of kReadRows slots that lie a block of threads apart.
+constexpr int kReadRows = 4;
 template <int D>
-__global__ void __launch_bounds__(256) block_read_kernel(const __grid_constant__ BlockView c, const int32_t* slot_begin, int n_slots, bf16* k_out, bf16* v_out, unsigned total) {
+__global__ void __launch_bounds__(256) block_read_kernel(const __grid_constant__ BlockView c, const int32_t* slot_begin, int n_slots, int per_item, bf16* k_out, bf16* v_out) {
     dependency_wait();
     dependency_release();
-    const unsigned t = blockIdx.x * 256u + threadIdx.x;
-    if (t >= total) return;
-    constexpr int kPieces = D / 8;
-    const unsigned row = t / kPieces;
-    const int d = (t % kPieces) * 8;
-    const int idx = row / n_slots, i = row - (unsigned)idx * n_slots;
+    constexpr int kPieces = D / 8, kApart = 256 / kPieces;
+    const int idx = blockIdx.x / per_item, chunk = blockIdx.x - idx * per_item;
     const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, idx);
     const int n = block_len(c, it.item);
-    const long long slot = (slot_begin ? (long long)slot_begin[it.b] : 0) + i;
-    uint4 x = make_uint4(0, 0, 0, 0), y = x;
-    if (slot >= 0 && slot < n) {
-        const int r = (int)slot & (c.T - 1), blk = (int)slot >> c.t_shift;
-        if (blk == n >> c.t_shift) {
-            const size_t off = ((size_t)it.item * c.T + r) * D + d;
-            x = *reinterpret_cast<const uint4*>(c.k_open + off);
-            y = *reinterpret_cast<const uint4*>(c.v_open + off);
-        } else {
-            const long long page = block_page(c, it.item, blk);
-            if (page < 0) {
-                if (d == 0 && r == 0) record_error(c.status, LETHE_ERR_PAGE, it.item);
-            } else {
-                const size_t off = ((size_t)page * c.T + r) * D + d;
-                const uint2 a = *reinterpret_cast<const uint2*>(c.k + off), b = *reinterpret_cast<const uint2*>(c.v + off);
-                const float ks = c.k_scale[page], vs = c.v_scale[page];
-                float f[8], g[8];
+    const long long begin = slot_begin ? slot_begin[it.b] : 0;
+    const int d = (threadIdx.x % kPieces) * 8, i0 = chunk * kReadRows * kApart + threadIdx.x / kPieces;
+    long long page[kReadRows];
+    uint4 x[kReadRows], y[kReadRows];
+    float ks[kReadRows], vs[kReadRows];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t wa = e < 4 ? a.x : a.y, wb = e < 4 ? b.x : b.y;
-                    f[e] = (float)(int8_t)(wa >> (8 * (e & 3))) * ks;
-                    g[e] = (float)(int8_t)(wb >> (8 * (e & 3))) * vs;
-                }
-                x = Piece<bf16>::pack(f);
-                y = Piece<bf16>::pack(g);
-            }
+    for (int u = 0; u < kReadRows; ++u) {
+        const int i = i0 + u * kApart;
+        const long long slot = begin + i;
+        page[u] = -1;
+        if (i < n_slots && slot >= 0 && slot < n >> c.t_shift << c.t_shift) {
+            page[u] = block_page(c, it.item, (int)slot >> c.t_shift);
+            if (page[u] < 0 && d == 0 && ((int)slot & (c.T - 1)) == 0) record_error(c.status, LETHE_ERR_PAGE, it.item);
         }
     }
-    reinterpret_cast<uint4*>(k_out)[t] = x;
-    reinterpret_cast<uint4*>(v_out)[t] = y;
+#pragma unroll
+    for (int u = 0; u < kReadRows; ++u) {
+        const int i = i0 + u * kApart;
+        const long long slot = begin + i;
+        const int r = (int)slot & (c.T - 1);
+        x[u] = y[u] = make_uint4(0, 0, 0, 0);
+        if (page[u] >= 0) {
+            const size_t off = ((size_t)page[u] * c.T + r) * D + d;
+            const uint2 a = *reinterpret_cast<const uint2*>(c.k + off), b = *reinterpret_cast<const uint2*>(c.v + off);
+            x[u].x = a.x, x[u].y = a.y, y[u].x = b.x, y[u].y = b.y;
+            ks[u] = c.k_scale[page[u]];
+            vs[u] = c.v_scale[page[u]];
+        } else if (i < n_slots && slot >= n >> c.t_shift << c.t_shift && slot < n) {
+            const size_t off = ((size_t)it.item * c.T + r) * D + d;
+            x[u] = *reinterpret_cast<const uint4*>(c.k_open + off);
+            y[u] = *reinterpret_cast<const uint4*>(c.v_open + off);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kReadRows; ++u) {
+        const int i = i0 + u * kApart;
+        if (i >= n_slots) continue;
+        if (page[u] >= 0) {
+            float f[8], g[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t wa = e < 4 ? x[u].x : x[u].y, wb = e < 4 ? y[u].x : y[u].y;
+                f[e] = (float)(int8_t)(wa >> (8 * (e & 3))) * ks[u];
+                g[e] = (float)(int8_t)(wb >> (8 * (e & 3))) * vs[u];
+            }
+            x[u] = Piece<bf16>::pack(f);
+            y[u] = Piece<bf16>::pack(g);
+        }
+        const size_t to = ((size_t)idx * n_slots + i) * D + d;
+        *reinterpret_cast<uint4*>(k_out + to) = x[u];
+        *reinterpret_cast<uint4*>(v_out + to) = y[u];
+    }
 }
 
+struct Shape {
+    int units, heads, threads;
+    unsigned kv_blocks, grid;
+    bool few;
+};
 template <int D, int TPT>
-cudaError_t launch_d(const BlockView& c, const NewRows& in, int units, unsigned grid, int threads, cudaStream_t stream) {
+cudaError_t launch_d(const BlockView& c, const NewRows& in, const Shape& sh, cudaStream_t stream) {
     const bool vec = !in.axis_pos || rotation_in_pieces<bf16>(in);
-    return vec ? launch_dependent(block_append_kernel<D, TPT, true>, dim3(grid), threads, (size_t)c.T * D, stream, c, in, units)
-               : launch_dependent(block_append_kernel<D, TPT, false>, dim3(grid), threads, (size_t)c.T * D, stream, c, in, units);
+    const size_t smem = (size_t)c.T * D * (in.axis_pos ? 5 : 1);
+    auto go = [&](auto kern) {
+        const cudaError_t e = prepare_kernel((const void*)kern, smem);
+        return e != cudaSuccess ? e : launch_dependent(kern, dim3(sh.grid), sh.threads, smem, stream, c, in, sh.units, sh.heads, sh.kv_blocks);
+    };
+    if (sh.few) return vec ? go(block_append_kernel<D, TPT, true, true>) : go(block_append_kernel<D, TPT, false, true>);
+    return vec ? go(block_append_kernel<D, TPT, true, false>) : go(block_append_kernel<D, TPT, false, false>);
 }
 
 }  // namespace
 
 cudaError_t launch_block_append(const BlockView& c, const NewRows& in, cudaStream_t stream) {
+    const int tasks = c.T * c.D / 16, threads = min(256, tasks), per = tasks / threads, group = threads / 32;
+    Shape sh;
+    sh.threads = threads;
+    sh.few = in.max_chunk <= kFewTokens;
     // blocks that a sequence's tokens can fill: all but a last one that the call leaves open
-    const int units = max(1, (int)(((long long)in.max_chunk + c.T - 1) / c.T));
-    const unsigned q_blocks = in.q ? (unsigned)in.n_tokens * (unsigned)((c.nl * c.Hq + kQueryRows - 1) / kQueryRows) : 0;
-    const unsigned grid = (unsigned)c.n_items * units + q_blocks;
-    const int tasks = c.T * c.D / 16, threads = min(256, tasks), per = tasks / threads;
-    cudaError_t e;
-    if (c.D == 128) e = per == 1 ? launch_d<128, 1>(c, in, units, grid, threads, stream) : per == 2 ? launch_d<128, 2>(c, in, units, grid, threads, stream)
-                                                                                                   : launch_d<128, 4>(c, in, units, grid, threads, stream);
-    else e = per == 1 ? launch_d<64, 1>(c, in, units, grid, threads, stream) : launch_d<64, 2>(c, in, units, grid, threads, stream);
-    if (e == cudaSuccess && units > 1)
+    sh.units = max(1, (int)(((long long)in.max_chunk + c.T - 1) / c.T));
+    // Two heads share their angles where there are blocks enough to fill the GPU all the same.
+    const long long to_fill = (long long)c.nl * c.Hkv * (in.n_tokens / c.T + c.B);
+    sh.heads = to_fill >= kPlenty ? 2 : 1;
+    sh.kv_blocks = sh.few ? (unsigned)((c.n_items + group - 1) / group) : (unsigned)c.nl * c.B * ((c.Hkv + sh.heads - 1) / sh.heads) * sh.units;
+    // many tokens: their queries have a launch of their own, with more bytes in flight
+    const bool apart = in.q && in.n_tokens >= 1024;
+    sh.grid = sh.kv_blocks + (in.q && !apart ? (unsigned)in.n_tokens * (unsigned)((c.nl * c.Hq + kQueryRows - 1) / kQueryRows) : 0);
+    cudaError_t e = apart ? launch_append_queries(in, c.nl, c.B, c.Hq, c.D, c.status, stream) : cudaSuccess;
+    if (e != cudaSuccess) return e;
+    if (c.D == 128) e = per == 1 ? launch_d<128, 1>(c, in, sh, stream) : per == 2 ? launch_d<128, 2>(c, in, sh, stream) : launch_d<128, 4>(c, in, sh, stream);
+    else e = per == 1 ? launch_d<64, 1>(c, in, sh, stream) : launch_d<64, 2>(c, in, sh, stream);
+    if (e == cudaSuccess && !sh.few && sh.units > 1)
         e = launch_append_len(in.chunk_start, c.len, c.B, c.Hkv, c.layer_begin, c.n_items, in.n_tokens, in.max_chunk, c.cap_tokens, stream);
     return e;
 }
 
 cudaError_t launch_block_read(const BlockView& c, const int32_t* slot_begin, int n_slots, void* k_out, void* v_out, cudaStream_t stream) {
-    const unsigned total = (unsigned)c.n_items * n_slots * (c.D / 8);
-    const unsigned grid = (total + 255) / 256;
-    return c.D == 128 ? launch_dependent(block_read_kernel<128>, dim3(grid), 256, 0, stream, c, slot_begin, n_slots, (bf16*)k_out, (bf16*)v_out, total)
-                      : launch_dependent(block_read_kernel<64>, dim3(grid), 256, 0, stream, c, slot_begin, n_slots, (bf16*)k_out, (bf16*)v_out, total);
+    const int rows = kReadRows * 256 / (c.D / 8), per_item = (n_slots + rows - 1) / rows;
+    const unsigned grid = (unsigned)c.n_items * per_item;
+    return c.D == 128 ? launch_dependent(block_read_kernel<128>, dim3(grid), 256, 0, stream, c, slot_begin, n_slots, per_item, (bf16*)k_out, (bf16*)v_out)
+                      : launch_dependent(block_read_kernel<64>, dim3(grid), 256, 0, stream, c, slot_begin, n_slots, per_item, (bf16*)k_out, (bf16*)v_out);
 }
 
 }  // namespace lethe

@@ -80,32 +80,93 @@ def test_append(ctx, dtype, L, B, Hq, Hkv, D, page, lens, chunks):
     assert ctx.poll_status()[0] == 0
 
 
+def rotated(ctx, r, k):
+    """Keys [L][n][Hkv][D] as the call rotates them: appended to an empty cache of their own type."""
+    from paper_2511_06029_b200 import binding
+    L, n, H, D = k.shape
+    x = torch.empty((L, 1, H, n, D), dtype=k.dtype, device="cuda")
+    c = binding.Cache(H, x, torch.empty_like(x), torch.zeros((L, 1, H, n), device="cuda"), torch.zeros((L, 1, H, n), dtype=torch.int32, device="cuda"),
+                      torch.zeros((L, 1, H), dtype=torch.int32, device="cuda"))
+    ctx.append(c, 0, L, starts([n]).cuda(), n, k.cuda(), k.cuda(), torch.zeros(n, dtype=torch.int32, device="cuda"), rotary=r)
+    return x[:, 0].transpose(1, 2).contiguous()
+
+
+def angles(rot, axes, n, far=10 ** 6):
+    half = rot // 2
+    pos = torch.randint(-far, far, (axes, n), dtype=torch.int32)
+    return [p % axes for p in range(half)], [10000.0 ** (-p / half) for p in range(half)], pos
+
+
+def off_by(want, size, dtype):
+    """Cosines and sines are off by 2^-23 at most (and the angle by half of 2^-32 turn), one product and the sum round, then the output
+    by half a step of its type."""
+    half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    return size * (2.0 ** -23 + 2.0 ** -30 + 2 * 2.0 ** -24) + want.abs() * half + 1e-30
+
+
+@pytest.mark.parametrize("rot", [0, 64, 42])
+def test_single_tokens_of_many_sequences(ctx, rot):
+    """More sequences than a block keeps the starts of, one token each (some none)."""
+    from paper_2511_06029_b200 import binding
+    B, Hkv, D = 1500, 1, 64
+    st, cache = state_and_cache(1, B, 2, Hkv, D, 16, 3, BF16, 0)
+    chunks = [0 if b % 7 == 3 else 1 for b in range(B)]
+    n = sum(chunks)
+    _, k, v = rows(1, n, 2, Hkv, D, BF16)
+    pos = torch.arange(n, dtype=torch.int32)
+    r, kr = None, k
+    if rot:
+        r = binding.Rotary([0] * (rot // 2), [0.01 * p for p in range(rot // 2)], pos[None].contiguous().cuda())
+        kr = rotated(ctx, r, k)
+    start = starts(chunks)
+    want = expected(st, cache, 0, start, kr.cpu(), v, pos)
+    ctx.append(cache, 0, 1, start.cuda(), 1, k.cuda(), v.cuda(), pos.cuda(), rotary=r)
+    same(cache, want)
+    assert ctx.poll_status()[0] == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,rot,pairs,axes,far", [(64, 64, False, 1, 5000), (128, 128, True, 3, 10 ** 6), (64, 32, False, 2, 2 ** 31 - 1), (128, 42, False, 4, 100),
+                                                  (64, 6, True, 2, 10 ** 9), (128, 96, True, 1, 3)])
+@pytest.mark.parametrize("n", [7, 1500])
+def test_rotation_against_definition(ctx, dtype, D, rot, pairs, axes, far, n):
+    from paper_2511_06029_b200 import binding
+    q, k, v = rows(1, n, 4, 2, D, dtype, seed=rot)
+    axis, freq, pos = angles(rot, axes, n, far)
+    r = binding.Rotary(axis, freq, pos.cuda(), style=binding.ROT_PAIRS if pairs else binding.ROT_HALVES)
+    st, cache = state_and_cache(1, 1, 4, 2, D, n + 3, 2, dtype, 0)
+    q_out = torch.empty_like(q, device="cuda")
+    ctx.append(cache, 0, 1, starts([n]).cuda(), n, k.cuda(), v.cuda(), pos[0].cuda(), rotary=r, q=q.cuda(), q_out=q_out)
+    for x, y in ((q, q_out), (k, cache.k[:, 0, :, 2:2 + n].transpose(1, 2))):
+        want, size = ref.rotate(x, axis, freq, pos, pairs, False)
+        d = (y.cpu().double() - want).abs()
+        assert bool((d <= off_by(want, size, dtype)).all()), f"worst {float((d / off_by(want, size, dtype)).max()):.3g}"
+        assert torch.equal(y.cpu()[..., rot:], x[..., rot:])
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, E4M3])
 @pytest.mark.parametrize("rot,pairs,axes", [(64, False, 1), (64, True, 3), (32, False, 2), (42, False, 4), (6, True, 2)])
 @pytest.mark.parametrize("chunks", [[1, 1], [600, 700]])
-def test_rotated_is_rotate_then_append(ctx, dtype, rot, pairs, axes, chunks):
+def test_rotated_on_the_way_is_rotated_before(ctx, dtype, rot, pairs, axes, chunks):
     from paper_2511_06029_b200 import binding
     L, B, Hq, Hkv, D = 2, 2, 6, 2, 64
-    act = F32 if dtype == F32 else BF16
     st, ca = state_and_cache(L, B, Hq, Hkv, D, 800, 20, dtype, 16)
     cb = st.device_cache()
     n = sum(chunks)
     q, k, v = (x.cuda() for x in rows(L, n, Hq, Hkv, D, dtype))
-    pos = torch.randint(0, 10 ** 6, (axes, n), dtype=torch.int32).cuda()
-    half = rot // 2
-    r = binding.Rotary([p % axes for p in range(half)], [10000.0 ** (-p / half) for p in range(half)], pos, style=binding.ROT_PAIRS if pairs else binding.ROT_HALVES)
-    qr, kr, q_out = torch.empty_like(q), torch.empty_like(k), torch.empty_like(q)
-    ctx.rotate(r, q, k, qr, kr)
-    start = starts(chunks).cuda()
+    axis, freq, pos = angles(rot, axes, n)
+    pos = pos.cuda()
+    r = binding.Rotary(axis, freq, pos, style=binding.ROT_PAIRS if pairs else binding.ROT_HALVES)
+    q_out, start = torch.empty_like(q), starts(chunks).cuda()
     ctx.append(ca, 0, L, start, max(chunks), k, v, pos[0], rotary=r, q=q, q_out=q_out)
-    ctx.append(cb, 0, L, start, max(chunks), kr, v, pos[0])
-    assert torch.equal(q_out, qr) and q_out.dtype == act
+    ctx.append(cb, 0, L, start, max(chunks), rotated(ctx, r, k), v, pos[0])
+    assert torch.equal(q_out, rotated(ctx, r, q))
     for name in ("k", "v", "rel", "pos", "len"):
         assert torch.equal(raw(getattr(ca, name)), raw(getattr(cb, name))), name
     cc = st.device_cache()
     keep = q.clone()
     ctx.append(cc, 0, L, start, max(chunks), k, v, pos[0], rotary=r, q=keep, q_out=keep)    # in place
-    assert torch.equal(keep, qr) and torch.equal(raw(cc.k), raw(ca.k))
+    assert torch.equal(keep, q_out) and torch.equal(raw(cc.k), raw(ca.k))
 
 
 def test_prompt_then_relevance(ctx):

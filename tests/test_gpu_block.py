@@ -93,30 +93,30 @@ def test_append_extreme_values(ctx):
 
 
 @pytest.mark.parametrize("rot,pairs,axes", [(128, False, 1), (128, True, 3), (64, False, 2), (90, False, 4), (34, True, 2), (2, False, 1)])
-@pytest.mark.parametrize("chunks", [[1, 1, 0], [70, 3, 33]])
-def test_append_rotated_is_rotate_then_append(ctx, rot, pairs, axes, chunks):
+@pytest.mark.parametrize("chunks", [[1, 1, 0], [70, 3, 33], [2, 4, 3], [500, 900, 1]])
+def test_append_rotated_on_the_way_is_rotated_before(ctx, rot, pairs, axes, chunks):
     from paper_2511_06029_b200 import binding
-    a, b = (BlockState(2, 3, 8, 2, 128, 32, 6, [[[31], [40], [0]]] * 2, True, seed=7) for _ in range(2))
-    ca, cb = a.device_cache(), b.device_cache()
+    from test_gpu_append import angles, rotated
+    lens = [[[31, 31], [40, 39], [0, 5]]] * 2       # heads of a sequence may differ in length
+    a = BlockState(2, 3, 8, 2, 128, 32, 32, lens, True, seed=7)
+    ca, cb, cc = (a.device_cache() for _ in range(3))
     n = sum(chunks)
     q, k, v = (x.cuda() for x in new_rows(a, 2, n, seed=rot))
     start = starts(chunks).cuda()
-    half = rot // 2
-    pos = torch.randint(0, 10 ** 6, (axes, n), dtype=torch.int32).cuda()
-    r = binding.Rotary([p % axes for p in range(half)], [10000.0 ** (-p / half) for p in range(half)], pos, style=binding.ROT_PAIRS if pairs else binding.ROT_HALVES)
-    qr, kr = torch.empty_like(q), torch.empty_like(k)
-    ctx.rotate(r, q, k, qr, kr)
-    q_out = torch.empty_like(q)
+    axis, freq, pos = angles(rot, axes, n)
+    r = binding.Rotary(axis, freq, pos.cuda(), style=binding.ROT_PAIRS if pairs else binding.ROT_HALVES)
+    q_out, kr = torch.empty_like(q), rotated(ctx, r, k)
     ctx.block_append(ca, 0, 2, start, max(chunks), k, v, rotary=r, q=q, q_out=q_out)
     ctx.block_append(cb, 0, 2, start, max(chunks), kr, v)
-    assert torch.equal(q_out, qr)
+    assert torch.equal(q_out, rotated(ctx, r, q))
     for name in ("k", "v", "k_scale", "v_scale", "k_range", "k_open", "v_open", "len"):
         x, y = getattr(ca, name), getattr(cb, name)
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), name
+    a.append(0, starts(chunks), kr.cpu(), v.cpu())
+    same_cache(a, ca)
     keep = q.clone()                                                       # in place
-    cc = a.device_cache()
     ctx.block_append(cc, 0, 2, start, max(chunks), k, v, rotary=r, q=keep, q_out=keep)
-    assert torch.equal(keep, qr)
+    assert torch.equal(keep, q_out)
 
 
 def test_append_layers_and_rows_outside(ctx):
