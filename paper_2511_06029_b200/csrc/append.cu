@@ -3,8 +3,6 @@
 // Bound by memory: each new row is read and written once.  A block takes a few tokens and a run of their rows, K and V of the (layer, KV
 // head) pairs first, then the queries, so the cosines and sines of a token's pairs are computed once per block, while the rows and the
 // chain of loads that says where a row goes (sequence, length, page) are on their way.
-#include <string.h>
-
 #include "block.cuh"
 #include "kv8_utils.cuh"
 
@@ -72,8 +70,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
         static_assert(kAppendThreads % 64 == 0, "a thread's angles are all of one pair");
         const int p = tid & 63;
         if (a.in.axis_pos && p < a.in.rot_dim / 2) {
-            const int32_t* pos = a.in.axis_pos + (size_t)a.in.axis[p] * a.in.n_tokens + tok0;
-            const unsigned long long per_pos = a.in.turn[p];
+            const int32_t* pos = a.in.axis_pos + (size_t)axis_of(a.in, p) * a.in.n_tokens + tok0;
+            const unsigned long long per_pos = turn_of(a.in, p);
             for (int ti = tid >> 6; ti < n_tok; ti += kAppendThreads / 64) turn_by(per_pos, pos[ti], cs[ti][p], sn[ti][p]);
         }
         const int32_t* start = a.B < kStartsKept ? starts : a.in.chunk_start;
@@ -221,16 +219,6 @@ cudaError_t launch_append_len(const int32_t* chunk_start, int32_t* len, int B, i
                               int cap_tokens, cudaStream_t stream) {
     return launch_dependent(append_len_kernel, dim3((n_items + 255) / 256), 256, 0, stream, chunk_start, len, B, Hkv, layer_begin, n_items, n_tokens, max_chunk,
                             cap_tokens);
-}
-
-// The queries alone (lethe_block_append of many tokens).
-cudaError_t launch_append_queries(const NewRows& in, int nl, int B, int Hq, int D, int32_t* status, cudaStream_t stream) {
-    AppendArgs a;
-    memset(&a, 0, sizeof(a));
-    a.in = in;
-    a.dtype = LETHE_BF16; a.D = D; a.B = B; a.Hq = Hq; a.nl = nl;
-    a.status = status;
-    return launch_t<__nv_bfloat16, kSame>(a, stream);
 }
 
 cudaError_t launch_append(const AppendArgs& a, cudaStream_t stream) {

@@ -115,8 +115,6 @@ __device__ __forceinline__ int sequence_of(const int32_t* start, int B, int tok)
 // quarter turn is taken off exactly; on the eighth of a turn either side that is left, z = -1 .. 1, sin(pi z / 4) / z and
 // (cos(pi z / 4) - 1) / z^2 are cubics in z^2 fitted for the smallest largest error (2.4e-9 and 1.9e-10): about 25 instructions, largest error
 // with all roundings 1.02e-7 (2^-23 is 1.19e-7), 2e-8 on average; an angle rounded to fp32 before its reduction has three times that.
-// A pair's frequency comes from the kernel's parameters: a thread that makes several angles of a pair keeps it, since lanes that read
-// different parameters are served one after the other.
 __device__ __forceinline__ void turn_by(unsigned long long per_pos, int pos, float& c, float& s) {
     const unsigned long long turn = (unsigned long long)(long long)pos * per_pos;
     const unsigned top = (unsigned)((turn + 0x80000000ull) >> 32) + 0x20000000u;  // the nearest 2^-32 turn, an eighth of a turn on
@@ -129,6 +127,19 @@ __device__ __forceinline__ void turn_by(unsigned long long per_pos, int pos, flo
     s = quarter & 1 ? co : si;
     if ((quarter + 1) & 2) c = -c;
     if (quarter & 2) s = -s;
+}
+
+// A pair's frequency and axis, which are among the kernel's parameters.  Lanes that read different parameters through the constant cache are
+// served one after the other (2 us at the head of every block); by their address they are read like other memory.
+__device__ __forceinline__ unsigned long long turn_of(const NewRows& in, int pair) {
+    unsigned long long v;
+    asm("ld.u64 %0, [%1];" : "=l"(v) : "l"(in.turn + pair));
+    return v;
+}
+__device__ __forceinline__ int axis_of(const NewRows& in, int pair) {
+    unsigned v;
+    asm("ld.u8 %0, [%1];" : "=r"(v) : "l"(in.axis + pair));
+    return (int)v;
 }
 
 // 16 bytes of a row as floats, and back.

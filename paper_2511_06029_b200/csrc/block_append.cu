@@ -4,11 +4,10 @@
 namespace lethe {
 cudaError_t launch_append_len(const int32_t* chunk_start, int32_t* len, int B, int Hkv, int layer_begin, int n_items, int n_tokens, int max_chunk,
                               int cap_tokens, cudaStream_t stream);
-cudaError_t launch_append_queries(const NewRows& in, int nl, int B, int Hq, int D, int32_t* status, cudaStream_t stream);
 namespace {
 
 using bf16 = __nv_bfloat16;
-constexpr int kQueryRows = 16;
+constexpr int kQueryRows = 16, kManyQueryRows = 32, kQueryTokens = 2;
 constexpr int kPlenty = 1184;  // blocks to fill: eight for each of 148 SMs
 constexpr int kFewTokens = 4;  // tokens to a sequence that a warp takes one after the other
 
@@ -55,14 +54,15 @@ __device__ __forceinline__ Filled filled(const BlockView& c, const NewRows& in, 
 // Else: `units` to `heads` (1 .. 8) KV heads of a sequence, which share the cosines and sines of their tokens (where they have the same length, as
 // they mostly do).  Unit u quantises the u-th of the blocks that the call fills; unit 0 also moves what is left over to the open block (it
 // has read the rows that were there by then).
-// The rest of the blocks rotate queries, kQueryRows rows of a token each.
+// The rest of the blocks rotate queries: kQueryRows rows of a token each (FEW), or kManyQueryRows of kQueryTokens tokens.  They lie between the
+// others, one of those to every `stride` blocks: the queries' stream goes on while the others wait for one load after the other.
 // Bound by memory: rows are read once and kept packed in registers between the search for the largest magnitude and the rounding.
 template <int D, int TPT, bool VEC, bool FEW>  // TPT: tasks of 16 elements per thread, of K and of V
-__global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_append_kernel(const __grid_constant__ BlockView c, const __grid_constant__ NewRows in, int units, int heads, unsigned kv_blocks) {
+__global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_append_kernel(const __grid_constant__ BlockView c, const __grid_constant__ NewRows in, int units, int heads, unsigned kv_blocks, unsigned stride) {
     extern __shared__ __align__(16) unsigned char tile[];  // [T][D] key codes; then cosines [T][D / 2] and sines of a block's new tokens
     float* cos_at = reinterpret_cast<float*>(tile + c.T * D);
     float* sin_at = cos_at + c.T * (D / 2);
-    __shared__ __align__(16) float cs[FEW ? 8 : 1][64], sn[FEW ? 8 : 1][64];  // of one token: queries, or a warp's row
+    __shared__ __align__(16) float cs[FEW ? 8 : kQueryTokens][64], sn[FEW ? 8 : kQueryTokens][64];  // of the queries' tokens, or of a warp's row
     __shared__ float tops[2][8];
     __shared__ uint32_t least[8][32], greatest[8][32];
     __shared__ Filled some[8];
@@ -72,10 +72,12 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
     constexpr int kPerRow = D / 16;
     const int half = in.rot_dim / 2;
     // the items of the block, one to a warp (FEW) or one after the other; their lengths are asked for together with chunk_start
-    const int groups = (c.Hkv + heads - 1) / heads, g = blockIdx.x / units, u = blockIdx.x - g * units;
-    if (blockIdx.x < kv_blocks) {
+    const unsigned turn_no = blockIdx.x / stride;
+    const bool is_kv = turn_no * stride == blockIdx.x && turn_no < kv_blocks;
+    const int groups = (c.Hkv + heads - 1) / heads, g = turn_no / units, u = turn_no - g * units;
+    if (is_kv) {
         const int i = FEW ? w : tid;
-        const int idx = FEW ? blockIdx.x * (nt / 32) + i : g / groups * c.Hkv + g % groups * heads + i;
+        const int idx = FEW ? turn_no * (nt / 32) + i : g / groups * c.Hkv + g % groups * heads + i;
         if (FEW ? lane == 0 : i < heads) {
             some[i] = Filled{0, 0, 0, 0, 0, 0};
             if (FEW ? idx < c.n_items : g % groups * heads + i < c.Hkv) some[i] = filled(c, in, idx);
@@ -107,27 +109,42 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
             turn_pieces<bf16>(in, x, y, co, si);
         }
     };
-    if (blockIdx.x >= kv_blocks) {
-        const int rows_total = c.nl * c.Hq, per_tok = (rows_total + kQueryRows - 1) / kQueryRows;
-        const int qb = blockIdx.x - kv_blocks, tok = qb / per_tok, r0 = (qb - tok * per_tok) * kQueryRows;
-        if (tok < in.chunk_start[0] || tok >= in.chunk_start[c.B]) return;
-        if (tid < half) turn_by(in.turn[tid], in.axis_pos[(size_t)in.axis[tid] * in.n_tokens + tok], cs[0][tid], sn[0][tid]);  // half <= 64 <= nt
-        __syncthreads();
-        const int tasks = min(rows_total - r0, kQueryRows) * kPerRow;
+    if (!is_kv) {
+        constexpr int TQ = FEW ? 1 : kQueryTokens, kRows = FEW ? kQueryRows : kManyQueryRows;
+        const int rows_total = c.nl * c.Hq, per_tok = (rows_total + kRows - 1) / kRows;
+        const int qb = blockIdx.x - min(turn_no + 1, kv_blocks), tok0 = qb / per_tok * TQ, r0 = qb % per_tok * kRows;
+        const int first = in.chunk_start[0], last = in.chunk_start[c.B];
+        for (int i = tid; i < TQ * 64; i += nt) {
+            const int p = i & 63, ti = i >> 6;
+            if (p < half && tok0 + ti < in.n_tokens) turn_by(turn_of(in, p), in.axis_pos[(size_t)axis_of(in, p) * in.n_tokens + tok0 + ti], cs[ti][p], sn[ti][p]);
+        }
+        const int tasks = min(rows_total - r0, kRows) * kPerRow;
         for (int t0 = 0; t0 < tasks; t0 += nt) {  // uniform for the block
-            const int t = t0 + tid, r = r0 + t / kPerRow, li = r / c.Hq;
-            const size_t off = (((size_t)li * in.n_tokens + tok) * c.Hq + r - li * c.Hq) * D;
-            int at0, at1;
-            uint4 x, y;
-            if (t < tasks) {
-                load_row((const bf16*)in.q + off, t % kPerRow, true, cs[0], sn[0], at0, at1, x, y);
-                if (VEC) turn_row(t % kPerRow, cs[0], sn[0], x, y);
+            const int t = t0 + tid, r = r0 + t / kPerRow, li = r / c.Hq, task = t % kPerRow;
+            const size_t off = (((size_t)li * in.n_tokens + tok0) * c.Hq + r - li * c.Hq) * D, pitch = (size_t)c.Hq * D;
+            int at0 = 0, at1 = 0;
+            uint4 x[TQ], y[TQ];
+            bool there[TQ];
+#pragma unroll
+            for (int k = 0; k < TQ; ++k) {
+                there[k] = t < tasks && tok0 + k >= first && tok0 + k < last;
+                if (VEC && there[k]) load_row((const bf16*)in.q + off + k * pitch, task, true, nullptr, nullptr, at0, at1, x[k], y[k]);
             }
+            if (t0 == 0) __syncthreads();  // the angles
+#pragma unroll
+            for (int k = 0; k < TQ; ++k)
+                if (there[k]) {
+                    if (VEC) turn_row(task, cs[k], sn[k], x[k], y[k]);
+                    else load_row((const bf16*)in.q + off + k * pitch, task, true, cs[k], sn[k], at0, at1, x[k], y[k]);
+                }
             if (!VEC) __syncwarp();  // q_out may be q: a row's tasks lie in one warp, all have read before one writes
-            if (t < tasks) {
-                *reinterpret_cast<uint4*>((bf16*)in.q_out + off + at0) = x;
-                *reinterpret_cast<uint4*>((bf16*)in.q_out + off + at1) = y;
-            }
+#pragma unroll
+            for (int k = 0; k < TQ; ++k)
+                if (there[k]) {
+                    bf16* to = (bf16*)in.q_out + off + k * pitch;
+                    *reinterpret_cast<uint4*>(to + at0) = x[k];
+                    *reinterpret_cast<uint4*>(to + at1) = y[k];
+                }
         }
         return;
     }
@@ -143,8 +160,8 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
     unsigned long long per_pos = 0;  // of pair tid % 64
     size_t axis_at = 0;
     if (rotated && (tid & 63) < half) {
-        per_pos = in.turn[tid & 63];
-        axis_at = (size_t)in.axis[tid & 63] * in.n_tokens;
+        per_pos = turn_of(in, tid & 63);
+        axis_at = (size_t)axis_of(in, tid & 63) * in.n_tokens;
     }
     // cosines and sines of the new tokens of slots s_first .. s_end - 1 of a block
     auto angles = [&](const Filled& f, int s_first, int s_end) {
@@ -315,7 +332,7 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
             for (int slot = f.n0; slot < f.n1; ++slot) {
                 if (rotated) {
                     __syncwarp();
-                    for (int p = lane; p < half; p += 32) turn_by(in.turn[p], in.axis_pos[(size_t)in.axis[p] * in.n_tokens + f.s0 + slot - f.n0], cs[w][p], sn[w][p]);
+                    for (int p = lane; p < half; p += 32) turn_by(turn_of(in, p), in.axis_pos[(size_t)axis_of(in, p) * in.n_tokens + f.s0 + slot - f.n0], cs[w][p], sn[w][p]);
                     __syncwarp();
                 }
                 if (lane < kPerRow) {
@@ -342,7 +359,7 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
 }
 
 // A thread takes 8 elements, of K and of V, of kReadRows slots that lie a block of threads apart.
-constexpr int kReadRows = 4;
+constexpr int kReadRows = 2;
 template <int D>
 __global__ void __launch_bounds__(256) block_read_kernel(const __grid_constant__ BlockView c, const int32_t* slot_begin, int n_slots, int per_item, bf16* k_out, bf16* v_out) {
     dependency_wait();
@@ -407,7 +424,7 @@ __global__ void __launch_bounds__(256) block_read_kernel(const __grid_constant__
 
 struct Shape {
     int units, heads, threads;
-    unsigned kv_blocks, grid;
+    unsigned kv_blocks, grid, stride;
     bool few;
 };
 template <int D, int TPT>
@@ -416,7 +433,7 @@ cudaError_t launch_d(const BlockView& c, const NewRows& in, const Shape& sh, cud
     const size_t smem = (size_t)c.T * D * (in.axis_pos ? 5 : 1);
     auto go = [&](auto kern) {
         const cudaError_t e = prepare_kernel((const void*)kern, smem);
-        return e != cudaSuccess ? e : launch_dependent(kern, dim3(sh.grid), sh.threads, smem, stream, c, in, sh.units, sh.heads, sh.kv_blocks);
+        return e != cudaSuccess ? e : launch_dependent(kern, dim3(sh.grid), sh.threads, smem, stream, c, in, sh.units, sh.heads, sh.kv_blocks, sh.stride);
     };
     if (sh.few) return vec ? go(block_append_kernel<D, TPT, true, true>) : go(block_append_kernel<D, TPT, false, true>);
     return vec ? go(block_append_kernel<D, TPT, true, false>) : go(block_append_kernel<D, TPT, false, false>);
@@ -435,11 +452,10 @@ cudaError_t launch_block_append(const BlockView& c, const NewRows& in, cudaStrea
     const long long to_fill = (long long)c.nl * c.Hkv * (in.n_tokens / c.T + c.B);
     sh.heads = to_fill >= kPlenty ? 2 : 1;
     sh.kv_blocks = sh.few ? (unsigned)((c.n_items + group - 1) / group) : (unsigned)c.nl * c.B * ((c.Hkv + sh.heads - 1) / sh.heads) * sh.units;
-    // many tokens: their queries have a launch of their own, with more bytes in flight
-    const bool apart = in.q && in.n_tokens >= 1024;
-    sh.grid = sh.kv_blocks + (in.q && !apart ? (unsigned)in.n_tokens * (unsigned)((c.nl * c.Hq + kQueryRows - 1) / kQueryRows) : 0);
-    cudaError_t e = apart ? launch_append_queries(in, c.nl, c.B, c.Hq, c.D, c.status, stream) : cudaSuccess;
-    if (e != cudaSuccess) return e;
+    const int q_tok = sh.few ? 1 : kQueryTokens, q_rows = sh.few ? kQueryRows : kManyQueryRows;
+    sh.grid = sh.kv_blocks + (in.q ? (unsigned)((in.n_tokens + q_tok - 1) / q_tok) * (unsigned)((c.nl * c.Hq + q_rows - 1) / q_rows) : 0);
+    sh.stride = sh.grid / sh.kv_blocks;
+    cudaError_t e;
     if (c.D == 128) e = per == 1 ? launch_d<128, 1>(c, in, sh, stream) : per == 2 ? launch_d<128, 2>(c, in, sh, stream) : launch_d<128, 4>(c, in, sh, stream);
     else e = per == 1 ? launch_d<64, 1>(c, in, sh, stream) : launch_d<64, 2>(c, in, sh, stream);
     if (e == cudaSuccess && !sh.few && sh.units > 1)
