@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kThreads = kBlockWarps * 32;
 constexpr int kStep = 32;       // tokens of a step
-constexpr int kTailWeight = 2;  // length on the line of 16 open rows, which are fetched without a ring
+constexpr int kTailWeight = 3;  // length on the line of 32 open rows, which are fetched without a ring
 constexpr int kPad = 3;         // and of an item's beginning: its length, first pages, queries and first tile come one after the other
 constexpr int kLine = 2048;     // items whose places on the line are kept in shared memory; of more, only every so many-th is
 constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
@@ -66,7 +66,7 @@ __device__ __forceinline__ Span span_of(const BlockAttendArgs& a, int n) {
     s.blocks = a.selected ? min(a.n_select, s.full) : s.full;
     s.steps = ((s.blocks << a.c.t_shift) + kStep - 1) / kStep;
     s.open = s.n & (a.c.T - 1);
-    s.w = kPad + s.steps + kTailWeight * ((s.open + 15) >> 4);
+    s.w = kPad + s.steps + kTailWeight * ((s.open + 31) >> 5);
     return s;
 }
 
@@ -180,59 +180,75 @@ __device__ __forceinline__ void value_word(float (*o)[4], uint32_t a, uint32_t b
     mma_f16(o[1], f1, p0, p1);
 }
 
-// 16 open rows from row r0 on: keys and values straight from memory, bf16.
+// 32 open rows from row r0 on: keys and values straight from memory, bf16, all asked for before anything is used.
 template <int D>
-__device__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float v_ref, float inv_ref_log2) {
+__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float scale2, float v_ref, float inv_ref_log2) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const __nv_bfloat16* K = a.c.k_open + (size_t)it.item * a.c.T * D;
     const __nv_bfloat16* V = a.c.v_open + (size_t)it.item * a.c.T * D;
     const __nv_bfloat16* Q = a.q + (((size_t)it.li * a.c.B + it.b) * a.c.Hkv + it.h) * a.c.G * D;
-    const bool in0 = r0 + g < n_open, in1 = r0 + g + 8 < n_open;
-    float x2[1][4] = {{0.f, 0.f, 0.f, 0.f}};
-    float(&s)[4] = x2[0];
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    const int d0 = first_d<D>(g);
-    uint4 v[4][D / 64];
+    constexpr int J = D / 32;  // 8 elements of a lane each
+    uint4 q[J], k[2][2][J], v[2][4][D / 64];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int r = r0 + 2 * t + (k & 1) + (k >> 1) * 8;
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) v[k][j] = r < n_open ? *reinterpret_cast<const uint4*>(V + (size_t)r * D + d0 + 8 * j) : zero;
-    }
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) {  // 8 elements of a lane: two steps of 16
+    for (int j = 0; j < J; ++j) {
         const int d = j * 32 + 8 * t;
-        const uint4 q = g < a.c.G ? *reinterpret_cast<const uint4*>(Q + (size_t)g * D + d) : zero;
-        const uint4 x = in0 ? *reinterpret_cast<const uint4*>(K + (size_t)(r0 + g) * D + d) : zero;
-        const uint4 y = in1 ? *reinterpret_cast<const uint4*>(K + (size_t)(r0 + g + 8) * D + d) : zero;
-        const uint32_t f0[4] = {x.x, y.x, x.y, y.y}, f1[4] = {x.z, y.z, x.w, y.w};
-        mma_bf16(s, f0, q.x, q.y);
-        mma_bf16(s, f1, q.z, q.w);
+        q[j] = g < a.c.G ? *reinterpret_cast<const uint4*>(Q + (size_t)g * D + d) : zero;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int row = r0 + 16 * h + 8 * r + g;
+                k[h][r][j] = row < n_open ? *reinterpret_cast<const uint4*>(K + (size_t)row * D + d) : zero;
+            }
     }
-    s[0] = in0 ? fmaf(s[0], scale2[0], inv_ref_log2) : -INFINITY;
-    s[1] = in0 ? fmaf(s[1], scale2[1], inv_ref_log2) : -INFINITY;
-    s[2] = in1 ? fmaf(s[2], scale2[0], inv_ref_log2) : -INFINITY;
-    s[3] = in1 ? fmaf(s[3], scale2[1], inv_ref_log2) : -INFINITY;
-    const float inv[1] = {v_ref};
-    acc.template softmax<1>(x2, inv);
-    uint32_t p[2][2];  // [term][rows 0 .. 7, 8 .. 15]
+    const int d0 = first_d<D>(g);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const float u = s[2 * k], w = s[2 * k + 1];
-        const uint32_t big = pack_bf16(u, w);
-        p[0][k] = movmatrix_trans(big);
-        p[1][k] = movmatrix_trans(pack_bf16(u - __uint_as_float(big << 16), w - __uint_as_float(big & 0xffff0000u)));
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = r0 + 16 * h + 2 * t + (i & 1) + (i >> 1) * 8;
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) v[h][i][j] = row < n_open ? *reinterpret_cast<const uint4*>(V + (size_t)row * D + d0 + 8 * j) : zero;
+        }
+    float s[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[h][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const uint4 x = k[h][0][j], y = k[h][1][j];
+            const uint32_t f0[4] = {x.x, y.x, x.y, y.y}, f1[4] = {x.z, y.z, x.w, y.w};
+            mma_bf16(s[h], f0, q[j].x, q[j].y);
+            mma_bf16(s[h], f1, q[j].z, q[j].w);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[h][i] = r0 + 16 * h + 8 * (i >> 1) + g < n_open ? fmaf(s[h][i], scale2, inv_ref_log2) : -INFINITY;
     }
+    const float inv[2] = {v_ref, v_ref};
+    acc.template softmax<2>(s, inv);
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) {
-        const uint32_t x[4][4] = {{v[0][j].x, v[0][j].y, v[0][j].z, v[0][j].w}, {v[1][j].x, v[1][j].y, v[1][j].z, v[1][j].w},
-                                  {v[2][j].x, v[2][j].y, v[2][j].z, v[2][j].w}, {v[3][j].x, v[3][j].y, v[3][j].z, v[3][j].w}};
+    for (int h = 0; h < 2; ++h) {
+        uint32_t p[2][2];  // [term][rows 0 .. 7, 8 .. 15]
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {  // elements 2 w and 2 w + 1 of the eight
-            const uint32_t f[4] = {__byte_perm(x[0][w], x[1][w], 0x5410), __byte_perm(x[0][w], x[1][w], 0x7632),
-                                   __byte_perm(x[2][w], x[3][w], 0x5410), __byte_perm(x[2][w], x[3][w], 0x7632)};
-            mma_bf16(acc.o[4 * j + w], f, p[0][0], p[0][1]);
-            mma_bf16(acc.o[4 * j + w], f, p[1][0], p[1][1]);
+        for (int i = 0; i < 2; ++i) {
+            const float u = s[h][2 * i], w = s[h][2 * i + 1];
+            const uint32_t big = pack_bf16(u, w);
+            p[0][i] = movmatrix_trans(big);
+            p[1][i] = movmatrix_trans(pack_bf16(u - __uint_as_float(big << 16), w - __uint_as_float(big & 0xffff0000u)));
+        }
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            const uint32_t x[4][4] = {{v[h][0][j].x, v[h][0][j].y, v[h][0][j].z, v[h][0][j].w}, {v[h][1][j].x, v[h][1][j].y, v[h][1][j].z, v[h][1][j].w},
+                                      {v[h][2][j].x, v[h][2][j].y, v[h][2][j].z, v[h][2][j].w}, {v[h][3][j].x, v[h][3][j].y, v[h][3][j].z, v[h][3][j].w}};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {  // elements 2 w and 2 w + 1 of the eight
+                const uint32_t f[4] = {__byte_perm(x[0][w], x[1][w], 0x5410), __byte_perm(x[0][w], x[1][w], 0x7632),
+                                       __byte_perm(x[2][w], x[3][w], 0x5410), __byte_perm(x[2][w], x[3][w], 0x7632)};
+                mma_bf16(acc.o[4 * j + w], f, p[0][0], p[0][1]);
+                mma_bf16(acc.o[4 * j + w], f, p[1][0], p[1][1]);
+            }
         }
     }
 }
@@ -445,7 +461,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
 
             // queries: whole numbers below 2^20, in three digits, in the order of the key codes
             uint32_t qf[3][4 * C];
-            float scale2[2], open2[2];
+            float scale2[2];
+            const float scale = c.scale_log2[c.layer_begin + it.li];
             int queued = min(g1, g0 + NS);
             {
                 const __nv_bfloat16* Q = a.q + (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G * D + (size_t)g * D;
@@ -493,10 +510,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     }
                 const unsigned bads = __ballot_sync(0xffffffffu, bad);
                 if (bads >> (4 * g) & 15u) div = __uint_as_float(0x7fc00000u);
-                const float sc = c.scale_log2[c.layer_begin + it.li];
-                open2[0] = open2[1] = sc;
-                scale2[0] = sc * __shfl_sync(0xffffffffu, div, 8 * t);
-                scale2[1] = sc * __shfl_sync(0xffffffffu, div, 8 * t + 4);
+                scale2[0] = scale * __shfl_sync(0xffffffffu, div, 8 * t);
+                scale2[1] = scale * __shfl_sync(0xffffffffu, div, 8 * t + 4);
             }
             Acc<D> acc;
             acc.clear();
@@ -594,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             }
             // open rows whose place on the line lies in the stretch
             const int tail0 = (max(p0 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight;
-            for (int j = tail0; j < tail1 && 16 * j < sp.open; ++j) open_rows<D>(a, acc, it, 16 * j, sp.open, open2, v_ref, __log2f(inv_ref));
+            for (int j = tail0; j < tail1 && 32 * j < sp.open; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, scale, v_ref, __log2f(inv_ref));
 
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) {
@@ -713,7 +728,24 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 for (int base = c0; base <= c1; base += 32) {  // the statistics of 32 parts at once, then their O
                     auto part_of = [&](int cta) { return a.cta_part + (((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * 8 + head) * kBlockPart; };
                     const int n = min(32, c1 - base + 1);
+                    constexpr int U = 8;  // parts that are asked for together, the first of them with the statistics
+                    float x[U][E];
+                    auto ask = [&](int k0) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            if (k0 + u >= n) continue;
+                            const float* src = part_of(base + k0 + u) + 4 + E * lane;
+                            if constexpr (E == 4) {
+                                const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
+                                x[u][0] = v.x, x[u][1] = v.y, x[u][2] = v.z, x[u][3] = v.w;
+                            } else {
+                                const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
+                                x[u][0] = v.x, x[u][1] = v.y;
+                            }
+                        }
+                    };
                     const float2 ml = lane < n ? __ldcg(reinterpret_cast<const float2*>(part_of(base + lane))) : make_float2(-INFINITY, 0.f);
+                    ask(0);
                     float nm = ml.x;
 #pragma unroll
                     for (int k = 16; k; k >>= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, k));
@@ -726,20 +758,15 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     m = nm;
 #pragma unroll
                     for (int e = 0; e < E; ++e) o[e] *= f;
-#pragma unroll 8
-                    for (int k = 0; k < n; ++k) {
-                        const float* src = part_of(base + k) + 4 + E * lane;
-                        const float gk = __shfl_sync(0xffffffffu, g, k);
-                        if constexpr (E == 4) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
-                            o[0] = fmaf(x.x, gk, o[0]);
-                            o[1] = fmaf(x.y, gk, o[1]);
-                            o[2] = fmaf(x.z, gk, o[2]);
-                            o[3] = fmaf(x.w, gk, o[3]);
-                        } else {
-                            const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
-                            o[0] = fmaf(x.x, gk, o[0]);
-                            o[1] = fmaf(x.y, gk, o[1]);
+#pragma unroll 1
+                    for (int k0 = 0; k0 < n; k0 += U) {
+                        if (k0) ask(k0);
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            const float gk = __shfl_sync(0xffffffffu, g, (k0 + u) & 31);
+                            if (k0 + u >= n) continue;
+#pragma unroll
+                            for (int e = 0; e < E; ++e) o[e] = fmaf(x[u][e], gk, o[e]);
                         }
                     }
                 }

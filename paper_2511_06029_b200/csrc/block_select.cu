@@ -68,6 +68,32 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
     }
     const int per = (full + splits - 1) / splits, blk0 = split * per, blk1 = min(full, blk0 + per);
 
+    // D / 16 lanes to a block, each with 16 elements of both bounds; U blocks of a lane in flight, the first of them before the queries
+    constexpr int kLanes = D / 16, kTeams = kThreads / kLanes, U = 2;
+    const int part = tid % kLanes, team = tid / kLanes;
+    long long page[U];
+    uint4 down_to[U], up_to[U];
+    float ks[U];
+    auto ask = [&](int base) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int blk = base + k * kTeams + team;
+            page[k] = blk < blk1 ? block_page(c, it.item, blk) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            down_to[k] = up_to[k] = make_uint4(0, 0, 0, 0);
+            ks[k] = 0.f;
+            if (page[k] >= 0) {
+                const uint4* r = reinterpret_cast<const uint4*>(c.k_range + (size_t)page[k] * 2 * D) + part;
+                down_to[k] = __ldg(r);
+                up_to[k] = __ldg(r + D / 16);
+                ks[k] = __ldg(c.k_scale + page[k]);
+            }
+        }
+    };
+    ask(blk0);
+
     // the group's queries as codes, summed over the heads by sign
     const __nv_bfloat16* qi = q + (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G * D;
     float top = 0.f;
@@ -94,9 +120,6 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
     }
     __syncthreads();
 
-    // scores: D / 16 lanes to a block, each with 16 elements of both bounds
-    constexpr int kLanes = D / 16, kTeams = kThreads / kLanes, U = 4;
-    const int part = tid % kLanes, team = tid / kLanes;
     int cu[8], cd[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -104,29 +127,12 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
         cd[i] = reinterpret_cast<const int*>(down)[part * 8 + i];
     }
     float* mine = scores + (size_t)idx * c.capacity;
+#pragma unroll 1
     for (int base = blk0; base < blk1; base += U * kTeams) {
-        long long page[U];
-        uint4 lo[U], hi[U];
-        float ks[U];
+        if (base > blk0) ask(base);
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int blk = base + k * kTeams + team;
-            page[k] = blk < blk1 ? block_page(c, it.item, blk) : -1;
-        }
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            lo[k] = hi[k] = make_uint4(0, 0, 0, 0);
-            ks[k] = 0.f;
-            if (page[k] >= 0) {
-                const uint4* r = reinterpret_cast<const uint4*>(c.k_range + (size_t)page[k] * 2 * D) + part;
-                lo[k] = __ldg(r);
-                hi[k] = __ldg(r + D / 16);
-                ks[k] = __ldg(c.k_scale + page[k]);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const uint32_t h[4] = {hi[k].x, hi[k].y, hi[k].z, hi[k].w}, l[4] = {lo[k].x, lo[k].y, lo[k].z, lo[k].w};
+            const uint32_t h[4] = {up_to[k].x, up_to[k].y, up_to[k].z, up_to[k].w}, l[4] = {down_to[k].x, down_to[k].y, down_to[k].z, down_to[k].w};
             int sum = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -143,15 +149,15 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
         }
     }
     if (splits > 1) {
-        __threadfence();
         __syncthreads();
         if (tid == 0) {
-            last = atomicAdd(&counters[idx], 1) == splits - 1;
+            int seen;
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(seen) : "l"(counters + idx) : "memory");  // the block's scores lie before
+            last = seen == splits - 1;
             if (last) counters[idx] = 0;
         }
         __syncthreads();
         if (!last) return;
-        __threadfence();
     } else {
         __syncthreads();
     }
