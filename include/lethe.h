@@ -500,7 +500,7 @@ lethe_status lethe_block_read(lethe_ctx *ctx, const lethe_block_cache *cache, in
  *   n_select, sink, recent   the first `sink` and the last `recent` full blocks are always chosen; sink + recent <= n_select
  *   selected [nl][B][Hkv][n_select] int32   the chosen blocks in ascending order (equal scores: the lower block first), then -1
  * An item with at most n_select full blocks has them all.  q [nl][B][Hq][D] bf16.  A block whose page id lies outside the pool
- * scores as zero (LETHE_ERR_PAGE).  Scratch: 4 bytes for each block of capacity of each item of the call.
+ * scores as zero (LETHE_ERR_PAGE).  Scratch: 4 bytes for each block of capacity of each item of the call, and 4 bytes per item.
  */
 lethe_status lethe_block_select(lethe_ctx *ctx, const lethe_block_cache *cache, int layer_begin, int layer_end, const void *q,
                                 int n_select, int sink, int recent, int32_t *selected, void *stream);
@@ -512,9 +512,10 @@ lethe_status lethe_block_select(lethe_ctx *ctx, const lethe_block_cache *cache, 
  *             blocks that the first min(n_select, full blocks) entries name (a negative entry names none, a repeated one counts
  *             again, one that is not a full block is left out and records LETHE_ERR_INVALID_ARG), and the open block
  * An item with nothing to attend over gives out = 0, lse = -inf.  A block whose page id lies outside the pool is left out
- * (LETHE_ERR_PAGE).  Sums, softmax statistics and outputs are held in fp32; full blocks take part as exact f16 values with
- * probabilities rounded to f16, open rows with probabilities in two bf16 terms.  Scratch: 4 bytes per item and up to 25 MB of
- * partial results.  The same inputs give the same bits.
+ * (LETHE_ERR_PAGE).  Sums, softmax statistics and outputs are held in fp32.  Over full blocks a query row takes part as whole numbers of
+ * 21 bits relative to its largest element (their products with the stored numbers are summed exactly) and the probabilities are rounded
+ * to f16; over open rows the query takes part as it is and the probabilities in two bf16 terms.  A query row with a NaN or an infinity
+ * gives NaN.  Scratch: 32 bytes per item and 1.3 MB of partial results.  The same inputs give the same bits.
  */
 lethe_status lethe_block_attend(lethe_ctx *ctx, const lethe_block_cache *cache, int layer_begin, int layer_end, const void *q,
                                 const float *scale, const int32_t *selected, int n_select, void *out, float *lse, void *stream);

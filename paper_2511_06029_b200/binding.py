@@ -142,6 +142,11 @@ def _stream(device) -> ctypes.c_void_p:
     return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
 
+def _raw_stream(device: int) -> int:
+    """The current stream's handle (without the Stream object around it, which takes longer to make than a small call)."""
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 class Cache:
     """Device tensors of the cache plus the C descriptor that points at them (the tensors stay owned here)."""
 
@@ -446,16 +451,19 @@ class Context:
                                                 None if rotary is None else ctypes.byref(rotary.c), _dp(out), _dp(lse),
                                                 _stream(self.device)))
 
-    def _append_args(self, cache, nl, chunk_start, act, k_new, v_new, rotary, q, q_out):
+    @staticmethod
+    def _append_args(cache, nl, chunk_start, act, k_new, v_new, rotary, q, q_out):
         """Checks what append and block_append have in common; the number of tokens."""
         n = k_new.shape[1]
         assert chunk_start.is_cuda and chunk_start.is_contiguous() and chunk_start.dtype == torch.int32 and chunk_start.numel() == cache.batch + 1
+        want = (nl, n, cache.n_kv_heads, cache.head_dim)
         for t in (k_new, v_new):
-            assert t.is_cuda and t.is_contiguous() and t.dtype == act and tuple(t.shape) == (nl, n, cache.n_kv_heads, cache.head_dim)
-        assert (q is None) == (q_out is None)
-        for t in (q, q_out):
-            assert t is None or (t.is_cuda and t.is_contiguous() and t.dtype == act and tuple(t.shape) == (nl, n, cache.n_q_heads, cache.head_dim))
-        assert rotary is None or rotary.n_tokens == n
+            assert t.is_cuda and t.dtype == act and t.shape == want and t.is_contiguous()
+        assert (q is None) == (q_out is None) and (rotary is None or rotary.n_tokens == n)
+        if q is not None:
+            want = (nl, n, cache.n_q_heads, cache.head_dim)
+            assert q.is_cuda and q.dtype == act and q.shape == want and q.is_contiguous()
+            assert q_out is q or (q_out.is_cuda and q_out.dtype == act and q_out.shape == want and q_out.is_contiguous())
         return n
 
     def append(self, cache: Cache, layer_begin: int, layer_end: int, chunk_start: torch.Tensor, max_chunk: int, k_new, v_new, token_pos,
@@ -467,7 +475,7 @@ class Context:
         self._check(self.lib.lethe_append(self.h, ctypes.byref(cache.c), layer_begin, layer_end, chunk_start.data_ptr(), n, max_chunk,
                                           None if q is None else q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), token_pos.data_ptr(),
                                           None if rotary is None else rotary.ref, None if q is None else q_out.data_ptr(),
-                                          torch.cuda.current_stream(self.device).cuda_stream))
+                                          _raw_stream(self.device)))
 
     def block_append(self, cache: BlockCache, layer_begin: int, layer_end: int, chunk_start: torch.Tensor, max_chunk: int, k_new, v_new,
                      rotary: Optional[Rotary] = None, q=None, q_out=None):
@@ -476,40 +484,40 @@ class Context:
         self._check(self.lib.lethe_block_append(self.h, cache.ref, layer_begin, layer_end, chunk_start.data_ptr(), n, max_chunk,
                                                 None if q is None else q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
                                                 None if rotary is None else rotary.ref, None if q is None else q_out.data_ptr(),
-                                                torch.cuda.current_stream(self.device).cuda_stream))
+                                                _raw_stream(self.device)))
 
     def block_read(self, cache: BlockCache, layer_begin: int, layer_end: int, slot_begin: Optional[torch.Tensor], k_out, v_out):
         """k_out, v_out bfloat16 [nl][B][Hkv][n_slots][D]; slot_begin [B] int32 on the device, or None for slot 0."""
-        lead = (layer_end - layer_begin, cache.batch, cache.n_kv_heads)
+        lead = (layer_end - layer_begin, cache.batch, cache.n_kv_heads, k_out.shape[3], cache.head_dim)
         for t in (k_out, v_out):
-            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16 and t.dim() == 5 and tuple(t.shape[:3]) == lead
-            assert t.shape[3] == k_out.shape[3] and t.shape[4] == cache.head_dim
+            assert t.is_cuda and t.dtype == torch.bfloat16 and t.shape == lead and t.is_contiguous()
         assert slot_begin is None or (slot_begin.is_cuda and slot_begin.is_contiguous() and slot_begin.dtype == torch.int32 and slot_begin.numel() == cache.batch)
         self._check(self.lib.lethe_block_read(self.h, cache.ref, layer_begin, layer_end, None if slot_begin is None else slot_begin.data_ptr(),
-                                              k_out.shape[3], k_out.data_ptr(), v_out.data_ptr(), torch.cuda.current_stream(self.device).cuda_stream))
+                                              k_out.shape[3], k_out.data_ptr(), v_out.data_ptr(), _raw_stream(self.device)))
 
-    def _block_query(self, cache, layer_begin, layer_end, selected, *tensors):
-        lead = (layer_end - layer_begin, cache.batch)
+    @staticmethod
+    def _block_query(cache, layer_begin, layer_end, selected, *tensors):
+        want = (layer_end - layer_begin, cache.batch, cache.n_q_heads, cache.head_dim)
         for t in tensors:
-            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16 and tuple(t.shape) == lead + (cache.n_q_heads, cache.head_dim)
+            assert t.is_cuda and t.dtype == torch.bfloat16 and t.shape == want and t.is_contiguous()
         if selected is not None:
-            assert selected.is_cuda and selected.is_contiguous() and selected.dtype == torch.int32 and selected.dim() == 4
-            assert tuple(selected.shape[:3]) == lead + (cache.n_kv_heads,)
+            assert selected.is_cuda and selected.dtype == torch.int32 and selected.is_contiguous() and selected.dim() == 4
+            assert selected.shape[:3] == (want[0], cache.batch, cache.n_kv_heads) and selected.shape[3] > 0
 
     def block_select(self, cache: BlockCache, layer_begin: int, layer_end: int, q, sink: int, recent: int, selected: torch.Tensor):
         """selected [nl][B][Hkv][n_select] int32 is written: the chosen blocks in ascending order, then -1."""
         self._block_query(cache, layer_begin, layer_end, selected, q)
         self._check(self.lib.lethe_block_select(self.h, cache.ref, layer_begin, layer_end, q.data_ptr(), selected.shape[3], sink, recent,
-                                                selected.data_ptr(), torch.cuda.current_stream(self.device).cuda_stream))
+                                                selected.data_ptr(), _raw_stream(self.device)))
 
     def block_attend(self, cache: BlockCache, layer_begin: int, layer_end: int, q, scale, out, lse=None, selected: Optional[torch.Tensor] = None,
                      scale_c=None):
         """q, out [nl][B][Hq][D] bfloat16; scale one float per layer of the cache; lse [nl][B][Hq] float32 or None; selected as
         block_select leaves it, or None for all blocks."""
         self._block_query(cache, layer_begin, layer_end, selected, q, out)
-        assert lse is None or (lse.is_cuda and lse.is_contiguous() and lse.dtype == torch.float32 and tuple(lse.shape) == tuple(q.shape[:3]))
+        assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.shape == q.shape[:3] and lse.is_contiguous())
         sc = scale_c if scale_c is not None else self._scale(scale)
         self._check(self.lib.lethe_block_attend(self.h, cache.ref, layer_begin, layer_end, q.data_ptr(), sc,
                                                 None if selected is None else selected.data_ptr(), 0 if selected is None else selected.shape[3],
                                                 out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                                torch.cuda.current_stream(self.device).cuda_stream))
+                                                _raw_stream(self.device)))

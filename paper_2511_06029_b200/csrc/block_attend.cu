@@ -182,7 +182,7 @@ __device__ __forceinline__ void value_word(float (*o)[4], uint32_t a, uint32_t b
 
 // 32 open rows from row r0 on: keys and values straight from memory, bf16, all asked for before anything is used.
 template <int D>
-__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float scale2, float v_ref, float inv_ref_log2) {
+__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float v_ref, float inv_ref_log2) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const __nv_bfloat16* K = a.c.k_open + (size_t)it.item * a.c.T * D;
     const __nv_bfloat16* V = a.c.v_open + (size_t)it.item * a.c.T * D;
@@ -224,7 +224,7 @@ __device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc,
             mma_bf16(s[h], f1, q[j].z, q[j].w);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[h][i] = r0 + 16 * h + 8 * (i >> 1) + g < n_open ? fmaf(s[h][i], scale2, inv_ref_log2) : -INFINITY;
+        for (int i = 0; i < 4; ++i) s[h][i] = r0 + 16 * h + 8 * (i >> 1) + g < n_open ? fmaf(s[h][i], scale2[i & 1], inv_ref_log2) : -INFINITY;
     }
     const float inv[2] = {v_ref, v_ref};
     acc.template softmax<2>(s, inv);
@@ -461,8 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
 
             // queries: whole numbers below 2^20, in three digits, in the order of the key codes
             uint32_t qf[3][4 * C];
-            float scale2[2];
-            const float scale = c.scale_log2[c.layer_begin + it.li];
+            float scale2[2], open2[2];
             int queued = min(g1, g0 + NS);
             {
                 const __nv_bfloat16* Q = a.q + (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G * D + (size_t)g * D;
@@ -489,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 int ex = (int)((__float_as_uint(big) >> 23) & 0xffu) - 19;
                 ex = big > 0.f && big < INFINITY ? min(max(ex, 2), 252) : 127;
                 const float mul = __uint_as_float((uint32_t)(254 - ex) << 23);
-                float div = __uint_as_float((uint32_t)ex << 23);
+                const float div = __uint_as_float((uint32_t)ex << 23);
                 bool bad = false;  // a query with a NaN or an infinity has no whole numbers: all its logits are NaN
 #pragma unroll
                 for (int k = 0; k < C; ++k)
@@ -509,9 +508,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                         for (int i = 0; i < 3; ++i) qf[i][4 * k + j] = digit[i];
                     }
                 const unsigned bads = __ballot_sync(0xffffffffu, bad);
-                if (bads >> (4 * g) & 15u) div = __uint_as_float(0x7fc00000u);
-                scale2[0] = scale * __shfl_sync(0xffffffffu, div, 8 * t);
-                scale2[1] = scale * __shfl_sync(0xffffffffu, div, 8 * t + 4);
+                float scale = c.scale_log2[c.layer_begin + it.li];
+                if (bads >> (4 * g) & 15u) scale = __uint_as_float(0x7fc00000u);
+                open2[0] = __shfl_sync(0xffffffffu, scale, 8 * t);
+                open2[1] = __shfl_sync(0xffffffffu, scale, 8 * t + 4);
+                scale2[0] = open2[0] * __shfl_sync(0xffffffffu, div, 8 * t);
+                scale2[1] = open2[1] * __shfl_sync(0xffffffffu, div, 8 * t + 4);
             }
             Acc<D> acc;
             acc.clear();
@@ -609,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             }
             // open rows whose place on the line lies in the stretch
             const int tail0 = (max(p0 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight;
-            for (int j = tail0; j < tail1 && 32 * j < sp.open; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, scale, v_ref, __log2f(inv_ref));
+            for (int j = tail0; j < tail1 && 32 * j < sp.open; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, open2, v_ref, __log2f(inv_ref));
 
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) {

@@ -268,6 +268,35 @@ def test_attend_ragged_with_empty_items(ctx):
     check_attend(ctx, st, st.device_cache(), 0, q, [0.1, 0.09, 0.2])
 
 
+def test_attend_more_items_than_the_table_of_places(ctx):
+    """Beyond 2048 items a CTA keeps the places of every so many-th only."""
+    g = torch.Generator().manual_seed(2)
+    lens = torch.randint(0, 70, (5, 60, 8), generator=g)
+    st = BlockState(5, 60, 8, 8, 64, 16, 5, lens, True, seed=3)
+    q, _, _ = new_rows(st, 5, 60)
+    check_attend(ctx, st, st.device_cache(), 0, q, [0.1, 0.2, 0.125, 0.09, 0.3])
+    assert ctx.poll_status()[0] == 0
+
+
+def test_attend_queries_that_are_not_finite(ctx):
+    """A head's NaN or infinity stays with that head; a zero query gives the mean of the values."""
+    st = BlockState(1, 2, 8, 1, 128, 32, 8, [[[200], [9]]], False, seed=14)
+    q, _, _ = new_rows(st, 1, 2)
+    cache = st.device_cache()
+    plain = check_attend(ctx, st, cache, 0, q, [0.1])[0]
+    bad = q.clone()
+    bad[0, :, 2, 5] = float("nan")
+    bad[0, :, 6, 100] = -float("inf")
+    bad[0, :, 3] = 0
+    out = torch.empty_like(q, device="cuda")
+    ctx.block_attend(cache, 0, 1, bad.cuda(), [0.1], out)
+    assert bool(out[0, :, [2, 6]].isnan().all())
+    keep = [0, 1, 4, 5, 7]
+    assert torch.equal(out[0, :, keep], plain[0, :, keep])
+    want, _, bound, _ = st.attend(0, torch.where(bad.isfinite(), bad, 0), [0.1])
+    assert bool(((out[0, :, 3].cpu().double() - want[0, :, 3]).abs() <= bound[0, :, 3]).all())
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_attend_wide_ranges(ctx, D):
     """Scales of blocks far apart, large and small queries, blocks of zeros, logits that rise along the cache."""
