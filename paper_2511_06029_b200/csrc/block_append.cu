@@ -11,26 +11,41 @@ constexpr int kQueryRows = 16, kManyQueryRows = 32, kQueryTokens = 2;
 constexpr int kPlenty = 1184;  // blocks to fill: eight for each of 148 SMs
 constexpr int kFewTokens = 4;  // tokens to a sequence that a warp takes one after the other
 
-__device__ __forceinline__ float finite_top(const uint4& w, float top) {
-    float f[8];
-    Piece<bf16>::unpack(w, f);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float m = fabsf(f[i]);
-        if (m < INFINITY) top = fmaxf(top, m);  // false for NaN too
-    }
-    return top;
+// Magnitudes of two bf16 are two 16-bit whole numbers in the same order; from kNotFinite on they are infinities and NaN.
+constexpr unsigned kNotFinite = 0x7f80;
+__device__ __forceinline__ uint32_t top_of(const uint4& w, uint32_t top) {
+    top = __vmaxu2(top, w.x & 0x7fff7fffu);
+    top = __vmaxu2(top, w.y & 0x7fff7fffu);
+    top = __vmaxu2(top, w.z & 0x7fff7fffu);
+    return __vmaxu2(top, w.w & 0x7fff7fffu);
 }
-__device__ __forceinline__ uint32_t code(float x, float inv) {
-    return (uint32_t)min(max(__float2int_rn(x * inv), -127), 127) & 0xffu;  // NaN converts to 0
+// The same without those that are not finite.
+__device__ __noinline__ uint32_t finite_top_of(uint4 w, uint32_t top) {
+    auto finite = [](uint32_t x) {
+        x &= 0x7fff7fffu;
+        return ((x & 0xffffu) >= kNotFinite ? 0u : x & 0xffffu) | (x >= kNotFinite << 16 ? 0u : x & 0xffff0000u);
+    };
+    return __vmaxu2(__vmaxu2(__vmaxu2(top, finite(w.x)), finite(w.y)), __vmaxu2(finite(w.z), finite(w.w)));
 }
+// Codes of eight values of at most the largest magnitude: 1.5 x 2^23 added to a product rounds it to the nearest whole number (ties to
+// even), which the sum's lowest byte holds.
 __device__ __forceinline__ uint2 codes8(const uint4& w, float inv) {
     float f[8];
     Piece<bf16>::unpack(w, f);
     uint32_t c[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = code(f[i], inv);
-    return make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+    for (int i = 0; i < 8; ++i) c[i] = __float_as_uint(__fadd_rn(__fmul_rn(f[i], inv), 12582912.f));
+    auto four = [](uint32_t a, uint32_t b, uint32_t x, uint32_t y) { return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(x, y, 0x0040), 0x5410); };
+    return make_uint2(four(c[0], c[1], c[2], c[3]), four(c[4], c[5], c[6], c[7]));
+}
+// Of any eight: limited to -127 .. 127, NaN 0.
+__device__ __noinline__ uint2 any_codes8(uint4 w, float inv) {
+    float f[8];
+    Piece<bf16>::unpack(w, f);
+    uint32_t c[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i / 4] |= ((uint32_t)min(max(__float2int_rn(f[i] * inv), -127), 127) & 0xffu) << (8 * (i & 3));
+    return make_uint2(c[0], c[1]);
 }
 
 // What a call does to an item.
@@ -63,7 +78,7 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
     float* cos_at = reinterpret_cast<float*>(tile + c.T * D);
     float* sin_at = cos_at + c.T * (D / 2);
     __shared__ __align__(16) float cs[FEW ? 8 : kQueryTokens][64], sn[FEW ? 8 : kQueryTokens][64];  // of the queries' tokens, or of a warp's row
-    __shared__ float tops[2][8];
+    __shared__ unsigned tops[2][8];
     __shared__ uint32_t least[8][32], greatest[8][32];
     __shared__ Filled some[8];
     dependency_wait();
@@ -228,29 +243,42 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
             __syncthreads();
         }
         if (!VEC && rotated) fetch();
-        float top_k = 0.f, top_v = 0.f;
+        uint32_t packed_k = 0, packed_v = 0;
 #pragma unroll
         for (int i = 0; i < TPT; ++i) {
             const int t = tid + i * nt, r = t / kPerRow;
             if (VEC && rotated && slot0 + r >= f.n0) turn_row(t % kPerRow, cos_at + r * (D / 2), sin_at + r * (D / 2), kx[i], ky[i]);
-            top_k = finite_top(ky[i], finite_top(kx[i], top_k));
-            top_v = finite_top(vy[i], finite_top(vx[i], top_v));
+            packed_k = top_of(ky[i], top_of(kx[i], packed_k));
+            packed_v = top_of(vy[i], top_of(vx[i], packed_v));
         }
         const long long page = block_page(c, f.item, blk);
+        unsigned bits_k, bits_v;  // the largest magnitudes, as bf16
+        auto over_block = [&]() {
+            bits_k = __reduce_max_sync(0xffffffffu, max(packed_k & 0xffffu, packed_k >> 16));
+            bits_v = __reduce_max_sync(0xffffffffu, max(packed_v & 0xffffu, packed_v >> 16));
+            if (lane == 0) {
+                tops[0][w] = bits_k;
+                tops[1][w] = bits_v;
+            }
+            __syncthreads();
+            for (int i = 0; i < nt / 32; ++i) {
+                bits_k = max(bits_k, tops[0][i]);
+                bits_v = max(bits_v, tops[1][i]);
+            }
+        };
+        over_block();
+        const bool any = max(bits_k, bits_v) >= kNotFinite;  // the same in all threads
+        if (any) {
+            packed_k = packed_v = 0;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            top_k = fmaxf(top_k, __shfl_xor_sync(0xffffffffu, top_k, o));
-            top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
+            for (int i = 0; i < TPT; ++i) {
+                packed_k = finite_top_of(ky[i], finite_top_of(kx[i], packed_k));
+                packed_v = finite_top_of(vy[i], finite_top_of(vx[i], packed_v));
+            }
+            __syncthreads();  // the table has been read
+            over_block();
         }
-        if (lane == 0) {
-            tops[0][w] = top_k;
-            tops[1][w] = top_v;
-        }
-        __syncthreads();
-        for (int i = 0; i < nt / 32; ++i) {
-            top_k = fmaxf(top_k, tops[0][i]);
-            top_v = fmaxf(top_v, tops[1][i]);
-        }
+        const float top_k = __uint_as_float(bits_k << 16), top_v = __uint_as_float(bits_v << 16);
         if (page < 0) {
             if (tid == 0) record_error(c.status, LETHE_ERR_PAGE, f.item);
             return;
@@ -264,13 +292,20 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
             int at0, at1;
             bool turned;
             piece_pair<bf16>(in, t % kPerRow, VEC && rotated, at0, at1, turned);
-            const uint2 a = codes8(kx[i], inv_k), b = codes8(ky[i], inv_k);
+            uint2 a, b, x, y;
+            if (any) {
+                a = any_codes8(kx[i], inv_k), b = any_codes8(ky[i], inv_k);
+                x = any_codes8(vx[i], inv_v), y = any_codes8(vy[i], inv_v);
+            } else {
+                a = codes8(kx[i], inv_k), b = codes8(ky[i], inv_k);
+                x = codes8(vx[i], inv_v), y = codes8(vy[i], inv_v);
+            }
             *reinterpret_cast<uint2*>(kd + r * D + at0) = a;
             *reinterpret_cast<uint2*>(kd + r * D + at1) = b;
             *reinterpret_cast<uint2*>(tile + r * D + at0) = a;
             *reinterpret_cast<uint2*>(tile + r * D + at1) = b;
-            *reinterpret_cast<uint2*>(vd + r * D + at0) = codes8(vx[i], inv_v);
-            *reinterpret_cast<uint2*>(vd + r * D + at1) = codes8(vy[i], inv_v);
+            *reinterpret_cast<uint2*>(vd + r * D + at0) = x;
+            *reinterpret_cast<uint2*>(vd + r * D + at1) = y;
         }
         if (tid == 0) {
             c.k_scale[page] = top_k >= kBlockTiny ? __fdiv_rn(top_k, 127.f) : 0.f;
