@@ -3,6 +3,9 @@
 // Bound by memory: each new row is read and written once.  A block takes a few tokens and a run of their rows, K and V of the (layer, KV
 // head) pairs first, then the queries, so the cosines and sines of a token's pairs are computed once per block, while the rows and the
 // chain of loads that says where a row goes (sequence, length, page) are on their way.
+// Measured: 8192 tokens of 32 + 8 + 8 heads of 128 in bf16, 202 MB both ways, 40 us = 5.1 TB/s, 0.77 of the copy rate (one token to a block
+// 45, four 43, 384 threads 49; a block lives about 7 us, of which 2 until it knows where its rows go); single tokens of 8 sequences and 32
+// layers 4.4 us on the device.
 #include "block.cuh"
 #include "kv8_utils.cuh"
 

@@ -15,6 +15,12 @@
 // largest s + log2 vs up to a factor of 2^6: it only moves when a logit outgrows it by that, and p' is kept 2^9 up, so that f16 (up to
 // 2^15 in use) holds probabilities down to 2^-23 of the largest with full precision.  Rows of open blocks are bf16 and may have any
 // range: they take bf16 MMAs with the probabilities in two terms.
+//
+// Measured (us): a step of the Llama-8B shape, 571 MB, 101 = 5.7 TB/s, 0.86 of the copy rate; one sequence of 131072 tokens, 268 MB, 48 = 0.85;
+// a ragged batch in blocks of 16 61 = 0.80; one layer of the first 13 (3.5 until the first tiles are asked for, 2 to 5 for two or three steps
+// a warp, 4 for the merges).  8 warps with two tiles each: the more is in flight the further apart the warps of an SM end (16 warps of
+// three 16-token tiles: 78 to 105 us, 113 in all; 12 of two: 83 to 95, 105), and fewer warps leave no time for a conversion of the keys,
+// which is why the logits come from the codes (f16 keys on 8 warps: 124).  Letting warps that are ahead wait for the others: 155.
 #include <string.h>
 
 #include "block_attend.cuh"

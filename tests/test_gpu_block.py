@@ -410,6 +410,41 @@ def test_captured_and_replayed(ctx):
     assert ctx.poll_status()[0] == 0
 
 
+def test_graph_outlives_growing_scratch(ctx):
+    """A graph captured before a larger call is replayed after it: the scratch and the counters it names are still its own."""
+    from paper_2511_06029_b200 import binding
+    own = binding.Context(0)
+    small = BlockState(1, 2, 4, 1, 64, 16, 20, 300, False, seed=31)
+    large = BlockState(2, 12, 16, 8, 64, 16, 40, 600, True, seed=32)
+    cs, cl = small.device_cache(), large.device_cache()
+    qs, ql = new_rows(small, 1, 2)[0], new_rows(large, 2, 12)[0]
+    q = qs.cuda()
+    sel, out = torch.empty((1, 2, 1, 5), dtype=torch.int32, device="cuda"), torch.empty_like(q)
+
+    def step():
+        own.block_select(cs, 0, 1, q, 1, 1, sel)
+        own.block_attend(cs, 0, 1, q, [0.125], out, selected=sel)
+
+    step()
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        got = torch.empty((2, 12, 8, 7), dtype=torch.int32, device="cuda")
+        own.block_select(cl, 0, 2, ql.cuda(), 1, 0, got)
+        assert torch.equal(got.cpu(), large.select(0, ql, 7, 1, 0))
+        check_attend(own, large, cl, 0, ql, [0.1, 0.2], got.cpu())
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    assert own.poll_status()[0] == 0
+    del graph
+    own.close()
+
+
 def test_other_stream_and_read_into_a_chunk(ctx):
     """A run of the operators on a side stream: a prompt is appended, read back as a contiguous cache, and drafted tokens attend over
     that with lethe_chunk_attend; single tokens attend over the block cache itself."""
