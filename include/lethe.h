@@ -507,7 +507,7 @@ lethe_status lethe_block_select(lethe_ctx *ctx, const lethe_block_cache *cache, 
 
 /*
  * Softmax attention of one query token per sequence over a block cache: q, scale, out and lse as in lethe_decode_attend
- * (nothing is appended, no relevance is kept: nothing is evicted from such a cache).
+ * (nothing is appended, no relevance is kept: nothing is evicted from such a cache); out must not overlap q.
  *   selected  NULL: over all of the item's tokens; else [nl][B][Hkv][n_select] as lethe_block_select leaves it: over the full
  *             blocks that the first min(n_select, full blocks) entries name (a negative entry names none, a repeated one counts
  *             again, one that is not a full block is left out and records LETHE_ERR_INVALID_ARG), and the open block

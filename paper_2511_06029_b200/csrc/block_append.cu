@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(256) block_read_kernel(const __grid_constant__
         page[u] = -1;
         if (i < n_slots && slot >= 0 && slot < n >> c.t_shift << c.t_shift) {
             page[u] = block_page(c, it.item, (int)slot >> c.t_shift);
-            if (page[u] < 0 && d == 0 && ((int)slot & (c.T - 1)) == 0) record_error(c.status, LETHE_ERR_PAGE, it.item);
+            if (page[u] < 0 && d == 0 && (i == 0 || ((int)slot & (c.T - 1)) == 0)) record_error(c.status, LETHE_ERR_PAGE, it.item);
         }
     }
 #pragma unroll

@@ -368,6 +368,9 @@ def test_bad_pages_are_left_out(ctx):
     vo = torch.empty_like(ko)
     ctx.block_read(cache, 0, 1, None, ko, vo)
     assert ctx.poll_status()[0] == binding.ERR_PAGE and not bool(ko[0, 0, 0, 64:80].any()) and not bool(vo[0, 1, 0, 32:48].any())
+    short = torch.full((1, 2, 1, 5, 64), 3.0, dtype=torch.bfloat16, device="cuda")     # from inside the block without a page
+    ctx.block_read(cache, 0, 1, torch.tensor([70, 0], dtype=torch.int32, device="cuda"), short, torch.empty_like(short))
+    assert ctx.poll_status()[0] == binding.ERR_PAGE and not bool(short[0, 0].any()) and bool(short[0, 1].any())
 
 
 def test_captured_and_replayed(ctx):
