@@ -331,7 +331,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
         __syncthreads();
     }
     const long long total = sm.prefix[kThreads];
-    // warps in use: at least two groups each (or an item's beginning), as far as there are
+    // Warps in use: at least two steps each (or an item's beginning), as far as there are.  Few short items behind a selection take 21.2 us with
+    // two, 21.5 with one, 22.8 with three and 23.8 with four.
     const long long warps = min((long long)a.n_cta * kBlockWarps, (total + 1) / 2);
     if ((long long)blockIdx.x * kBlockWarps >= warps) return;
     auto cta_at = [&](int pos) { return (int)(((pos + 1LL) * warps - 1) / total) / kBlockWarps; };
