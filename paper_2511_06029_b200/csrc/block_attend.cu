@@ -729,6 +729,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     if (seen == c1 - c0) *counter = 0;
                 }
                 if (__shfl_sync(0xffffffffu, seen, 0) != c1 - c0) continue;
+                __syncwarp();  // lane 0 has seen the other CTAs' parts; a shuffle alone would not order the other lanes' loads behind that
                 m = -INFINITY;
                 l = 0.f;
 #pragma unroll
