@@ -89,9 +89,10 @@ __global__ void __launch_bounds__(kThreads) block_select_kernel(const __grid_con
             ks[k] = 0.f;
             if (page[k] >= 0) {
                 const uint4* r = reinterpret_cast<const uint4*>(c.k_range + (size_t)page[k] * 2 * D) + part;
-                down_to[k] = __ldg(r);
-                up_to[k] = __ldg(r + D / 16);
-                ks[k] = __ldg(c.k_scale + page[k]);
+                // not the read-only path: this grid may be alive while the append before it still writes them
+                down_to[k] = __ldcg(r);
+                up_to[k] = __ldcg(r + D / 16);
+                ks[k] = __ldcg(c.k_scale + page[k]);
             }
         }
     };
