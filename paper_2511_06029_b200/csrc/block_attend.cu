@@ -58,7 +58,7 @@ struct __align__(1024) Smem {
     int line[kLine + 1], len[kLine];
     int prefix[kThreads + 1], totals[kBlockWarps];
     Rec rec[32];                            // warp w: 2 w its first stretch, 2 w + 1 its last
-    float m[32][8], l[32][8];
+    float m[32][8], l[32][8];               // a part's weight is l 2^m; its O is divided by that
     int abort;
 };
 
@@ -625,6 +625,18 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 acc.l[0] += __shfl_xor_sync(0xffffffffu, acc.l[0], s);
                 acc.l[1] += __shfl_xor_sync(0xffffffffu, acc.l[1], s);
             }
+            // What leaves the stretch is divided by its sum: a mean of values is as large as they are, and a part's weight is its sum.
+            float top[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float inv = acc.l[k] == 0.f ? 0.f : 1.f / acc.l[k];
+                top[k] = acc.l[k] == 0.f ? -INFINITY : acc.m[k] - kLift;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    acc.o[i][k] = acc.o[i][k] * inv * v_ref;
+                    acc.o[i][2 + k] = acc.o[i][2 + k] * inv * v_ref;
+                }
+            }
             const bool begins = p0 == 0, ends = p1 == sp.w;
             const int d0 = first_d<D>(g);
             if (begins && ends) {
@@ -633,12 +645,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     const int head = 2 * t + k;
                     if (head >= c.G) continue;
                     const size_t row = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G + head;
-                    const float inv = acc.l[k] == 0.f ? 0.f : v_ref / acc.l[k];
                     uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D + d0);
 #pragma unroll
                     for (int i = 0; i < D / 16; i += 2)
-                        *reinterpret_cast<uint2*>(dst + i) = make_uint2(pack_bf16(acc.o[i][k] * inv, acc.o[i][2 + k] * inv), pack_bf16(acc.o[i + 1][k] * inv, acc.o[i + 1][2 + k] * inv));
-                    if (a.lse && g == 0) a.lse[row] = acc.l[k] == 0.f ? -INFINITY : (acc.m[k] - kLift + log2f(acc.l[k])) * 0.6931471805599453f;
+                        *reinterpret_cast<uint2*>(dst + i) = make_uint2(pack_bf16(acc.o[i][k], acc.o[i][2 + k]), pack_bf16(acc.o[i + 1][k], acc.o[i + 1][2 + k]));
+                    if (a.lse && g == 0) a.lse[row] = acc.l[k] == 0.f ? -INFINITY : (top[k] + log2f(acc.l[k])) * 0.6931471805599453f;
                 }
             } else {
                 const bool last = at1 <= start + sp.w;  // nothing of this warp comes after it: the ring is free
@@ -654,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 if (g == 0) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        sm.m[which][2 * t + k] = acc.l[k] == 0.f ? -INFINITY : acc.m[k] - kLift;
+                        sm.m[which][2 * t + k] = top[k];
                         sm.l[which][2 * t + k] = acc.l[k];
                     }
                 }
@@ -663,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i)
-                        *reinterpret_cast<float2*>(part + (2 * t + k) * D + d0 + 2 * i) = make_float2(acc.o[i][k] * v_ref, acc.o[i][2 + k] * v_ref);
+                        *reinterpret_cast<float2*>(part + (2 * t + k) * D + d0 + 2 * i) = make_float2(acc.o[i][k], acc.o[i][2 + k]);
             }
             at = start + p1;
             start += sp.w;
@@ -699,10 +710,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             const float mine_m = m;
 #pragma unroll
             for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            const float f = exp2_diff(mine_m, m);
-            l *= f;
+            l *= exp2_diff(mine_m, m);
+            const float mine_l = l;
 #pragma unroll
             for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+            const float f = l == 0.f ? 0.f : mine_l / l;  // shares of the sum
             float o[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -760,12 +772,13 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
 #pragma unroll
                     for (int k = 16; k; k >>= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, k));
                     nm = fmaxf(nm, m);
-                    const float f = exp2_diff(m, nm), g = exp2_diff(ml.x, nm);
-                    float sum = ml.y * g;
+                    const float old = l * exp2_diff(m, nm), mine = ml.y * exp2_diff(ml.x, nm);
+                    float sum = mine;
 #pragma unroll
                     for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-                    l = l * f + sum;
+                    l = old + sum;
                     m = nm;
+                    const float f = l == 0.f ? 0.f : old / l, g = l == 0.f ? 0.f : mine / l;
 #pragma unroll
                     for (int e = 0; e < E; ++e) o[e] *= f;
 #pragma unroll 1
@@ -782,10 +795,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 }
             }
             const size_t row = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G + head;
-            const float inv = l == 0.f ? 0.f : 1.f / l;
             uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + row * D) + E / 2 * lane;
-            if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-            else *dst = pack_bf16(o[0] * inv, o[1] * inv);
+            if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+            else *dst = pack_bf16(o[0], o[1]);
             if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
         }
     }

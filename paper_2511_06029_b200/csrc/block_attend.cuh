@@ -23,7 +23,7 @@ struct BlockAttendArgs {
     int* counters;            // [items][8 heads] CTAs that have left a part, zero between launches
     int n_select, n_cta, wait_limit;
 };
-constexpr int kBlockPart = 4 + 128;  // max, sum, two unused, then O
+constexpr int kBlockPart = 4 + 128;  // m, l (the part's weight is l 2^m), two unused, then O divided by the weight
 
 bool build_block_maps(void* encode, const BlockView& c, BlockMaps* maps);
 cudaError_t launch_block_attend(const BlockAttendArgs& a, const BlockMaps& maps, cudaStream_t stream);
