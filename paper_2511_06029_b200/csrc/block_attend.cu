@@ -14,7 +14,7 @@
 // becomes the f16 of the same value by bit operations (1024 + 128 + x is 0x6400 | (x ^ 0x80)) and one subtraction, exactly.  m is the
 // largest s + log2 vs up to a factor of 2^6: it only moves when a logit outgrows it by that, and p' is kept 2^9 up, so that f16 (up to
 // 2^15 in use) holds probabilities down to 2^-23 of the largest with full precision.  Rows of open blocks are bf16 and may have any
-// range: they take bf16 MMAs with the probabilities in two terms.
+// range: they take bf16 MMAs with the probabilities in two terms, their values relative to a power of two in the place of a scale.
 //
 // Measured (us): a step of the Llama-8B shape, 571 MB, 101 = 5.7 TB/s, 0.86 of the copy rate; one sequence of 131072 tokens, 268 MB, 48 = 0.85;
 // a ragged batch in blocks of 16 61 = 0.80; one layer of the first 13 (3.5 until the first tiles are asked for, 2 to 5 for two or three steps
@@ -186,9 +186,14 @@ __device__ __forceinline__ void value_word(float (*o)[4], uint32_t a, uint32_t b
     mma_f16(o[1], f1, p0, p1);
 }
 
-// 32 open rows from row r0 on: keys and values straight from memory, bf16, all asked for before anything is used.
+// The exponent field of a power of two, a float's or a bf16's.
+__device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 0xffu); }
+__device__ __forceinline__ float power_of_two(int field) { return __uint_as_float((uint32_t)field << 23); }
+
+// 32 open rows from row r0 on: keys and values straight from memory, bf16, all asked for before anything is used.  The values are taken
+// like codes, relative to a power of two of their own (which leaves a bf16 as exact as it is): the largest of them below 2^7.
 template <int D>
-__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float v_ref, float inv_ref_log2) {
+__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float& v_ref, bool& have_ref) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const __nv_bfloat16* K = a.c.k_open + (size_t)it.item * a.c.T * D;
     const __nv_bfloat16* V = a.c.v_open + (size_t)it.item * a.c.T * D;
@@ -217,6 +222,37 @@ __device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc,
 #pragma unroll
             for (int j = 0; j < D / 64; ++j) v[h][i][j] = row < n_open ? *reinterpret_cast<const uint4*>(V + (size_t)row * D + d0 + 8 * j) : zero;
         }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8 * (D / 64); ++i) top = top_of(v[i & 1][i >> 1 & 3][i >> 3], top);
+    unsigned bits = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+    if (bits >= kNotFinite) {  // the same in all lanes
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < 8 * (D / 64); ++i) top = finite_top_of(v[i & 1][i >> 1 & 3][i >> 3], top);
+        bits = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+    }
+    // 2^-100 and less are taken relative to the same power (as blocks are, nothing smaller counts as large)
+    const int own = max((int)(bits >> 7), 127 - 100) - 6;
+    if (!have_ref) {
+        v_ref = power_of_two(own);
+        have_ref = true;
+    }
+    const int apart = own - exponent_of(v_ref);
+    const float lv = (float)apart, iv = power_of_two(min(max(127 - apart, 1), 254));
+    const __nv_bfloat162 by = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((254 - own) << 7)));
+    auto relative = [&](uint32_t& w) {
+        const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w), by);
+        w = *reinterpret_cast<const uint32_t*>(&x);
+    };
+#pragma unroll
+    for (int i = 0; i < 8 * (D / 64); ++i) {
+        uint4& x = v[i & 1][i >> 1 & 3][i >> 3];
+        relative(x.x);
+        relative(x.y);
+        relative(x.z);
+        relative(x.w);
+    }
     float s[2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -230,9 +266,9 @@ __device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc,
             mma_bf16(s[h], f1, q[j].z, q[j].w);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[h][i] = r0 + 16 * h + 8 * (i >> 1) + g < n_open ? fmaf(s[h][i], scale2[i & 1], inv_ref_log2) : -INFINITY;
+        for (int i = 0; i < 4; ++i) s[h][i] = r0 + 16 * h + 8 * (i >> 1) + g < n_open ? fmaf(s[h][i], scale2[i & 1], lv) : -INFINITY;
     }
-    const float inv[2] = {v_ref, v_ref};
+    const float inv[2] = {iv, iv};
     acc.template softmax<2>(s, inv);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -618,7 +654,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             }
             // open rows whose place on the line lies in the stretch
             const int tail0 = (max(p0 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight;
-            for (int j = tail0; j < tail1 && 32 * j < sp.open; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, open2, v_ref, __log2f(inv_ref));
+            for (int j = tail0; j < tail1 && 32 * j < sp.open; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, open2, v_ref, have_ref);
 
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) {

@@ -65,3 +65,34 @@ def test_values_of_one_size(ctx, L, B, lens, D, T, by):
     st.v_scale *= by
     scale_open(st, by)
     check(ctx, st, queries(st, L), 1 / math.sqrt(D))
+
+
+# ------------------------------------------------------------------------------------------------- open rows
+
+@pytest.mark.parametrize("L,B,lens", LENS + [(1, 3, 31)])
+@pytest.mark.parametrize("D,T", [(128, 32), (64, 128)])
+@pytest.mark.parametrize("by", [1e37, 2.0 ** 100, 2.0 ** -35, 2.0 ** -99])
+def test_open_rows_of_any_size(ctx, L, B, lens, D, T, by):
+    """Open rows far larger or smaller than the full blocks (which are as large where that fits the sums of the full blocks)."""
+    st = state(L, B, lens, D, T, seed=D + 1)
+    scale_open(st, by)
+    st.v_scale *= min(max(by, 2.0 ** -30), 2.0 ** 60) if by > 1 else by
+    check(ctx, st, queries(st, L), 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("rows", [1, 33, 127])
+def test_open_rows_with_zeros_and_infinities(ctx, rows):
+    """Rows of zeros have their share of the sum; a value that is not finite makes its element of out not finite, and only that."""
+    st = state(1, 2, 128 + rows, 64, 128, seed=rows)
+    st.v_open[0, 0, 0, :rows] = 0
+    check(ctx, st, queries(st, 1), 0.125)
+    st.v_open[0, 1, 0, 0, 3], st.v_open[0, 1, 0, 0, 9], st.v_open[0, 1, 0, 0, 60] = float("inf"), -float("inf"), float("nan")
+    q = queries(st, 1)
+    out = torch.empty_like(q, device="cuda")
+    ctx.block_attend(st.device_cache(with_range=False), 0, 1, q.cuda(), [0.125], out)
+    want, _, bound, _ = st.attend(0, q, [0.125])
+    bad = torch.zeros(64, dtype=torch.bool)
+    bad[[3, 9, 60]] = True
+    assert not bool(out[0, 1][:, bad.cuda()].isfinite().any())
+    d = (out.cpu().double() - want).abs()
+    assert bool((d[0, 0] <= bound[0, 0]).all()) and bool((d[0, 1][:, ~bad] <= bound[0, 1][:, ~bad]).all())
