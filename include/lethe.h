@@ -451,8 +451,7 @@ lethe_status lethe_append(lethe_ctx *ctx, const lethe_cache *cache, int layer_be
  *     amax < 2^-100 scale and block are 0.  So a value is off by at most scale * (0.5 + 2^-16).  What a cache holds does not
  *     depend on how its tokens were split over calls.
  *   - k_range holds the least and the greatest x of each element over a full block's keys.
- * A caller that fills a cache itself keeps to this: scales finite and not negative (those of one item's value blocks within a
- * factor of 2^100 of one another, zeros apart).
+ * A caller that fills a cache itself keeps to this: scales finite and not negative.
  */
 typedef struct {
     int32_t n_layers, batch, n_q_heads, n_kv_heads;

@@ -13,7 +13,8 @@
 // in O^T += V^T P^T (m16n8k16 f16 MMAs, the probabilities turned by movmatrix), and the sum of probabilities takes p' / vs.  A value code
 // becomes the f16 of the same value by bit operations (1024 + 128 + x is 0x6400 | (x ^ 0x80)) and one subtraction, exactly.  m is the
 // largest s + log2 vs up to a factor of 2^6: it only moves when a logit outgrows it by that, and p' is kept 2^9 up, so that f16 (up to
-// 2^15 in use) holds probabilities down to 2^-23 of the largest with full precision.  Rows of open blocks are bf16 and may have any
+// 2^15 in use) holds probabilities down to 2^-23 of the largest with full precision.  Where the scales of a stretch lie more than 2^40
+// apart the sum has a reference of its own, since m no longer says how large p' / vs is.  Rows of open blocks are bf16 and may have any
 // range: they take bf16 MMAs with the probabilities in two terms, their values relative to a power of two in the place of a scale.
 //
 // Measured (us): a step of the Llama-8B shape, 571 MB, 101 = 5.7 TB/s, 0.86 of the copy rate; one sequence of 131072 tokens, 268 MB, 48 = 0.85;
@@ -37,6 +38,9 @@ constexpr int kPad = 3;         // and of an item's beginning: its length, first
 constexpr int kLine = 2048;     // items whose places on the line are kept in shared memory; of more, only every so many-th is
 constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
 constexpr float kLift = 9.f;    // p' is kept up by this (log2)
+// Value scales of a stretch up to this far (log2) from its reference: the sums of p' / vs and O can have one m.  Further apart the sum
+// of probabilities has a reference of its own (sums_apart), since p' / vs would leave the range of fp32.
+constexpr float kApart = 40.f, kFar = 1099511627776.f;  // 2^kApart
 
 template <int D>
 __host__ __device__ constexpr int stage_bytes() { return kStep * D * 2; }
@@ -58,6 +62,7 @@ struct __align__(1024) Smem {
     int line[kLine + 1], len[kLine];
     int prefix[kThreads + 1], totals[kBlockWarps];
     Rec rec[32];                            // warp w: 2 w its first stretch, 2 w + 1 its last
+    float4 apart[kBlockWarps][32];          // stretches whose scales lie far apart: per lane the sums' references and sums (two heads)
     float m[32][8], l[32][8];               // a part's weight is l 2^m; its O is divided by that
     int abort;
 };
@@ -118,6 +123,8 @@ struct Acc {
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
     }
+    // references and sums of their own (sums_apart), with the lift of p' taken into the reference
+    __device__ __forceinline__ float4 sums() const { return make_float4(m[0] - kLift, m[1] - kLift, l[0], l[1]); }
     // x: logits of H x 16 tokens (row g: x[h][0], x[h][1]; row g + 8: x[h][2], x[h][3]) -> p', and m moved where it has to be
     template <int H>
     __device__ __forceinline__ void softmax(float (&x)[H][4], const float (&inv_vs)[H]) {
@@ -162,6 +169,41 @@ struct Acc {
     }
 };
 
+// The root of exp2(a - b): a part that is 2^228 times as large as another may count for as much with a weight as small as that.
+__device__ __forceinline__ float root_diff(float a, float b) { return a == -INFINITY ? 0.f : fast_exp2(0.5f * (a - b)); }
+
+// The sums of probabilities of H x 16 tokens where value scales lie far apart: `at` holds {reference, reference, sum, sum} of the lane's
+// heads, x the logits with log2 vs = lv added.  Tokens whose values are zero (iv < 0) have no part in O: their x becomes -inf.
+template <int H>
+__device__ __forceinline__ void sums_apart(float4* at, float (&x)[H][4], const float (&lv)[H], const float (&iv)[H]) {
+    const float4 old = *at;
+    float s[H][4], a = -INFINITY, b = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[h][i] = x[h][i] == -INFINITY ? -INFINITY : x[h][i] - lv[h];
+            if (iv[h] < 0.f) x[h][i] = -INFINITY;
+        }
+        a = fmaxf(a, fmaxf(s[h][0], s[h][2]));
+        b = fmaxf(b, fmaxf(s[h][1], s[h][3]));
+    }
+#pragma unroll
+    for (int k = 4; k < 32; k <<= 1) {
+        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, k));
+        b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, k));
+    }
+    a = fmaxf(a, old.x);
+    b = fmaxf(b, old.y);
+    float la = old.z * exp2_diff(old.x, a), lb = old.w * exp2_diff(old.y, b);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        la += exp2_diff(s[h][0], a) + exp2_diff(s[h][2], a);
+        lb += exp2_diff(s[h][1], b) + exp2_diff(s[h][3], b);
+    }
+    *at = make_float4(a, b, la, lb);
+}
+
 // Elements that a lane reads of a key row (16 bytes at each of D / 64 places) and of a value row, and the order of a tile's tokens among
 // the MMA's rows: chosen so that eight neighbouring lanes touch eight different 16-byte columns of the swizzled tile at D = 128.
 template <int D>
@@ -193,7 +235,7 @@ __device__ __forceinline__ float power_of_two(int field) { return __uint_as_floa
 // 32 open rows from row r0 on: keys and values straight from memory, bf16, all asked for before anything is used.  The values are taken
 // like codes, relative to a power of two of their own (which leaves a bf16 as exact as it is): the largest of them below 2^7.
 template <int D>
-__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float& v_ref, bool& have_ref) {
+__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float& v_ref, bool& have_ref, float4* sums, bool& apart) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const __nv_bfloat16* K = a.c.k_open + (size_t)it.item * a.c.T * D;
     const __nv_bfloat16* V = a.c.v_open + (size_t)it.item * a.c.T * D;
@@ -238,8 +280,12 @@ __device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc,
         v_ref = power_of_two(own);
         have_ref = true;
     }
-    const int apart = own - exponent_of(v_ref);
-    const float lv = (float)apart, iv = power_of_two(min(max(127 - apart, 1), 254));
+    const int off = own - exponent_of(v_ref);
+    const float lv = (float)off, iv = power_of_two(min(max(127 - off, 1), 254));
+    if (!apart && fabsf(lv) > kApart) {
+        *sums = acc.sums();
+        apart = true;
+    }
     const __nv_bfloat162 by = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((254 - own) << 7)));
     auto relative = [&](uint32_t& w) {
         const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w), by);
@@ -268,7 +314,8 @@ __device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc,
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[h][i] = r0 + 16 * h + 8 * (i >> 1) + g < n_open ? fmaf(s[h][i], scale2[i & 1], lv) : -INFINITY;
     }
-    const float inv[2] = {iv, iv};
+    const float inv[2] = {iv, iv}, lvs[2] = {lv, lv};
+    if (apart) sums_apart<2>(sums, s, lvs, inv);
     acc.template softmax<2>(s, inv);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -425,7 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             int ask0 = -64, ask_page = -1, use0 = -64;
             float ask_ks = 0.f, ask_vs = 0.f, ks = 0.f, lv = 0.f, iv = 0.f;  // iv: v_ref / vs, negative: a block whose values are zero
             float v_ref = 1.f, inv_ref = 1.f;
-            bool have_ref = false;
+            bool have_ref = false, apart = false;
+            float4* const sums = &sm.apart[w][lane];
             auto ask_run = [&](int e0) {
                 ask0 = e0;
                 ask_page = -1;
@@ -450,6 +498,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     }
                 }
             };
+            Acc<D> acc;
+            acc.clear();
             auto use_run = [&]() {
                 use0 = ask0;
                 ks = ask_ks;
@@ -465,7 +515,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     }
                 }
                 const float rel = ask_vs * inv_ref;
-                lv = ask_page < 0 ? -INFINITY : ask_vs == 0.f ? 0.f : __log2f(rel);  // no block: no weight
+                if (!apart && __any_sync(0xffffffffu, ask_vs > 0.f && !(rel <= kFar && rel >= 1.f / kFar))) {
+                    *sums = acc.sums();
+                    apart = true;
+                }
+                lv = ask_page < 0 ? -INFINITY : ask_vs == 0.f ? 0.f : apart ? log2f(ask_vs) - log2f(v_ref) : __log2f(rel);  // no block: no weight
                 iv = ask_vs == 0.f ? -1.f : __fdividef(1.f, rel);
             };
             // step gi: one tile of a block of 32 tokens or more, or two blocks of 16
@@ -558,8 +612,6 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 scale2[0] = open2[0] * __shfl_sync(0xffffffffu, div, 8 * t);
                 scale2[1] = open2[1] * __shfl_sync(0xffffffffu, div, 8 * t + 4);
             }
-            Acc<D> acc;
-            acc.clear();
             float b_ks[2] = {0.f, 0.f}, b_lv[2] = {0.f, 0.f}, b_iv[2] = {0.f, 0.f};  // of the blocks at hand
             for (int gi = g0; gi < g1; ++gi) {
                 const int e = (gi * kStep) >> c.t_shift;
@@ -635,6 +687,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 phase ^= stage == 0;
                 if (queued < g1) issue(queued++);
 
+                if (apart) sums_apart<2>(sums, p, b_lv, b_iv);
                 const float inv[2] = {fabsf(b_iv[0]), fabsf(b_iv[1])};
                 acc.template softmax<2>(p, inv);
 #pragma unroll
@@ -654,8 +707,18 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             }
             // open rows whose place on the line lies in the stretch
             const int tail0 = (max(p0 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight;
-            for (int j = tail0; j < tail1 && 32 * j < sp.open; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, open2, v_ref, have_ref);
+            for (int j = tail0; j < tail1 && 32 * j < sp.open; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, open2, v_ref, have_ref, sums, apart);
 
+            float4 own = acc.sums();
+            float by[2] = {v_ref, v_ref};  // what brings O to the sum's reference, and to the values' size
+            if (apart) {
+                const float ref = (float)(exponent_of(v_ref) - 127);
+                by[0] = acc.m[0] == -INFINITY ? 0.f : fast_exp2(0.5f * (own.x - sums->x + ref));  // half of it: the whole may have no place in fp32
+                by[1] = acc.m[1] == -INFINITY ? 0.f : fast_exp2(0.5f * (own.y - sums->y + ref));
+                own = *sums;
+                acc.l[0] = own.z;
+                acc.l[1] = own.w;
+            }
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) {
                 acc.l[0] += __shfl_xor_sync(0xffffffffu, acc.l[0], s);
@@ -666,11 +729,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const float inv = acc.l[k] == 0.f ? 0.f : 1.f / acc.l[k];
-                top[k] = acc.l[k] == 0.f ? -INFINITY : acc.m[k] - kLift;
+                top[k] = acc.l[k] == 0.f ? -INFINITY : k ? own.y : own.x;
+                const float again = apart ? by[k] : 1.f;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    acc.o[i][k] = acc.o[i][k] * inv * v_ref;
-                    acc.o[i][2 + k] = acc.o[i][2 + k] * inv * v_ref;
+                    acc.o[i][k] = acc.o[i][k] * inv * by[k] * again;
+                    acc.o[i][2 + k] = acc.o[i][2 + k] * inv * by[k] * again;
                 }
             }
             const bool begins = p0 == 0, ends = p1 == sp.w;
@@ -746,11 +810,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             const float mine_m = m;
 #pragma unroll
             for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            l *= exp2_diff(mine_m, m);
-            const float mine_l = l;
+            const float half = root_diff(mine_m, m), mine_l = l * half;
+            l = mine_l * half;
 #pragma unroll
             for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-            const float f = l == 0.f ? 0.f : mine_l / l;  // shares of the sum
+            const float f = l == 0.f ? 0.f : mine_l / l;  // a part's share of the sum is half x f
             float o[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -758,9 +822,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             for (unsigned k = chain; k; k &= k - 1) {
                 const int r = __ffs(k) - 1;
                 const float* src = (r & 1 ? reinterpret_cast<const float*>(sm.ring[r >> 1]) : sm.first[r >> 1]) + head * D + E * lane;
-                const float fr = __shfl_sync(0xffffffffu, f, r);
+                const float hr = __shfl_sync(0xffffffffu, half, r), fr = __shfl_sync(0xffffffffu, f, r);
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = fmaf(src[e], fr, o[e]);
+                for (int e = 0; e < E; ++e) o[e] = fmaf(src[e] * hr, fr, o[e]);
             }
             if (!whole) {
                 // the item goes on in other CTAs: the last of them to come here merges
@@ -808,24 +872,24 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
 #pragma unroll
                     for (int k = 16; k; k >>= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, k));
                     nm = fmaxf(nm, m);
-                    const float old = l * exp2_diff(m, nm), mine = ml.y * exp2_diff(ml.x, nm);
-                    float sum = mine;
+                    const float old_half = root_diff(m, nm), old = l * old_half, half = root_diff(ml.x, nm), mine = ml.y * half;
+                    float sum = mine * half;
 #pragma unroll
                     for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-                    l = old + sum;
+                    l = fmaf(old, old_half, sum);
                     m = nm;
                     const float f = l == 0.f ? 0.f : old / l, g = l == 0.f ? 0.f : mine / l;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] *= f;
+                    for (int e = 0; e < E; ++e) o[e] = o[e] * old_half * f;
 #pragma unroll 1
                     for (int k0 = 0; k0 < n; k0 += U) {
                         if (k0) ask(k0);
 #pragma unroll
                         for (int u = 0; u < U; ++u) {
-                            const float gk = __shfl_sync(0xffffffffu, g, (k0 + u) & 31);
+                            const float hk = __shfl_sync(0xffffffffu, half, (k0 + u) & 31), gk = __shfl_sync(0xffffffffu, g, (k0 + u) & 31);
                             if (k0 + u >= n) continue;
 #pragma unroll
-                            for (int e = 0; e < E; ++e) o[e] = fmaf(x[u][e], gk, o[e]);
+                            for (int e = 0; e < E; ++e) o[e] = fmaf(x[u][e] * hk, gk, o[e]);
                         }
                     }
                 }

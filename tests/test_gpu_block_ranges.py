@@ -45,7 +45,7 @@ def check(ctx, st, q, scale, room=0.0):
     if room:
         st.v_scale, st.v_open = st.v_scale.abs(), st.v_open.abs()
         st.v = st.v.abs()
-        b_out = b_out + room * st.attend(0, q, [scale] * L)[0]
+        b_out = b_out + room * st.attend(0, q, [scale] * L)[0] + unseen(st, q, scale)
         b_lse = b_lse + room
     # the smallest normal number is 2^-126; steps below it are 2^-133 for bf16
     d = (out.cpu().double() - want).abs()
@@ -96,3 +96,87 @@ def test_open_rows_with_zeros_and_infinities(ctx, rows):
     assert not bool(out[0, 1][:, bad.cuda()].isfinite().any())
     d = (out.cpu().double() - want).abs()
     assert bool((d[0, 0] <= bound[0, 0]).all()) and bool((d[0, 1][:, ~bad] <= bound[0, 1][:, ~bad]).all())
+
+
+# ------------------------------------------------------------------------------- blocks far apart in one item
+
+APART = 2.0 ** -14
+"""Where scales lie far apart a share is formed from logits with the scale's logarithm added: numbers below 2^9, in fp32 a rounding of
+2^-16 each for the sum, for taking the logarithm off again and, below 2^8, three times 2^-17 for the logarithm and the two halves of
+the factor that joins O and the sum: 3.5 x 2^-16 in the exponent of 2, times log 2."""
+
+
+def unseen(st, q, scale):
+    """What f16 does not hold of small shares: a share times its scale is kept 2^9 times as large as the largest of them at least, and
+    below 2^-14 it is off by half of f16's smallest number, 2^-25.  So 2^-34 of the largest for each token and unit of its code, which
+    counts where the tokens of the largest shares have small codes in an element.  [nl][B][Hq][1]"""
+    room = torch.zeros(q.shape[:3] + (1,), dtype=torch.float64)
+    for li in range(q.shape[0]):
+        for b in range(st.B):
+            for h in range(st.Hkv):
+                K, V = st.rows((li, b, h))
+                n, hs = int(st.len[li, b, h]) // st.T, slice(h * st.G, (h + 1) * st.G)
+                p = torch.softmax(q[li, b, hs].double() @ K.T * scale, 1)
+                size = torch.cat([st.v_scale[li, b, h, :n].double().repeat_interleave(st.T), V[n * st.T:].abs().amax(1) / 64])
+                room[li, b, hs, 0] = (p * size).amax(1) * 127 * n * st.T * 2.0 ** -34
+    return room
+
+
+@pytest.mark.parametrize("L,B,lens", LENS)
+@pytest.mark.parametrize("D,T", [(128, 32), (128, 16), (64, 64)])
+@pytest.mark.parametrize("sizes", [(1e-30, 1e9), (1e9, 1e-30), (1.0, 2.0 ** 119), (2.0 ** 119, 1.0, 2.0 ** -99), (1.0, 2.0 ** 45), (1e30, 1e30, 1e-30)])
+@pytest.mark.parametrize("spread", [1.0, 40.0])
+def test_value_blocks_far_apart(ctx, L, B, lens, D, T, sizes, spread):
+    """Blocks of very different size in turn.  With a wide spread of logits the small ones may outweigh the others, and do in some heads."""
+    blocks_in_turn(ctx, L, B, lens, D, T, sizes, spread)
+
+
+def blocks_in_turn(ctx, L, B, lens, D, T, sizes, spread):
+    st = state(L, B, lens, D, T, seed=D + T)
+    by = torch.tensor(sizes, dtype=torch.float64)[torch.arange(st.capacity) % len(sizes)]
+    top = st.v_scale.nan_to_num(1).max()
+    st.v_scale = (st.v_scale.double() / top * by / 127).float()        # the largest value of a block is at most its size
+    scale_open(st, sizes[-1] / 8)
+    check(ctx, st, queries(st, L, spread), 1 / math.sqrt(D), APART)
+
+
+@pytest.mark.parametrize("small,large", [(2.0 ** -90, 2.0 ** 100), (1.0, 2.0 ** 60)])
+def test_small_blocks_that_outweigh_large_ones(ctx, small, large):
+    """One key direction: the blocks' logits are known.  Large values at logits lower by the ratio of the sizes: both matter in out, only
+    the small ones in the sum; then the other way round."""
+    T, D = 32, 128
+    for up in (1, -1):
+        st = state(1, 2, 32 * 60 + 9, D, T, seed=3)
+        st.k.zero_()
+        st.k[..., 0] = 100
+        gap = math.log(large / small) * up / 2
+        odd = torch.arange(61) % 2 == 1
+        st.k_scale[:] = torch.where(odd, gap / 100, -gap / 100).float()      # logits gap and -gap
+        st.v_scale[:] = torch.where(odd, small / 127, large / 127).float()
+        st.k_open.zero_()
+        scale_open(st, small)
+        q = torch.zeros((1, 2, 8, D), dtype=torch.bfloat16)
+        q[..., 0] = 1.0
+        check(ctx, st, q, 1.0, APART)
+
+
+def test_appended_values_far_apart(ctx):
+    """Rows that the append takes, of all sizes that it holds, block by block."""
+    from block_reference import starts
+    st = BlockState(1, 2, 8, 2, 128, 16, 40, 0, True, seed=9)
+    cache = st.device_cache()
+    n = 16 * 37 + 5
+    g = torch.Generator().manual_seed(2)
+    k, v = (torch.randn((1, 2 * n, 2, 128), generator=g) for _ in range(2))
+    exponent = torch.randint(-96, 120, (2 * n // 16 + 1,), generator=g).double().repeat_interleave(16)[:2 * n]
+    v = (v.double() * 2.0 ** exponent[None, :, None, None]).to(torch.bfloat16)
+    k = k.to(torch.bfloat16)
+    ctx.block_append(cache, 0, 1, starts([n, n]).cuda(), n, k.cuda(), v.cuda())
+    st.append(0, starts([n, n]), k, v)
+    q = queries(st, 1, 20.0)
+    out = torch.empty_like(q, device="cuda")
+    ctx.block_attend(cache, 0, 1, q.cuda(), [0.1], out)
+    want, _, bound, _ = st.attend(0, q, [0.1])
+    st.v, st.v_open = st.v.abs(), st.v_open.abs()
+    bound = bound + APART * st.attend(0, q, [0.1])[0] + unseen(st, q, 0.1)
+    assert bool(((out.cpu().double() - want).abs() <= bound).all())
