@@ -14,7 +14,8 @@
 // becomes the f16 of the same value by bit operations (1024 + 128 + x is 0x6400 | (x ^ 0x80)) and one subtraction, exactly.  m is the
 // largest s + log2 vs up to a factor of 2^6: it only moves when a logit outgrows it by that, and p' is kept 2^9 up, so that f16 (up to
 // 2^15 in use) holds probabilities down to 2^-23 of the largest with full precision.  Where the scales of a stretch lie more than 2^40
-// apart the sum has a reference of its own, since m no longer says how large p' / vs is.  Rows of open blocks are bf16 and may have any
+// apart the sum has a reference of its own, since m no longer says how large p' / vs is;
+// blocks of zeros count as far apart and have a part in that sum only.  Rows of open blocks are bf16 and may have any
 // range: they take bf16 MMAs with the probabilities in two terms, their values relative to a power of two in the place of a scale.
 //
 // Measured (us): a step of the Llama-8B shape, 571 MB, 101 = 5.7 TB/s, 0.86 of the copy rate; one sequence of 131072 tokens, 268 MB, 48 = 0.85;
@@ -276,13 +277,13 @@ __device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc,
     }
     // 2^-100 and less are taken relative to the same power (as blocks are, nothing smaller counts as large)
     const int own = max((int)(bits >> 7), 127 - 100) - 6;
-    if (!have_ref) {
+    if (!have_ref && bits) {
         v_ref = power_of_two(own);
         have_ref = true;
     }
     const int off = own - exponent_of(v_ref);
-    const float lv = (float)off, iv = power_of_two(min(max(127 - off, 1), 254));
-    if (!apart && fabsf(lv) > kApart) {
+    const float lv = (float)off, iv = bits ? power_of_two(min(max(127 - off, 1), 254)) : -1.f;
+    if (!apart && (!bits || fabsf(lv) > kApart)) {
         *sums = acc.sums();
         apart = true;
     }
@@ -515,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     }
                 }
                 const float rel = ask_vs * inv_ref;
-                if (!apart && __any_sync(0xffffffffu, ask_vs > 0.f && !(rel <= kFar && rel >= 1.f / kFar))) {
+                if (!apart && __any_sync(0xffffffffu, ask_page >= 0 && (rel > kFar || rel < 1.f / kFar))) {  // a scale of zero among them
                     *sums = acc.sums();
                     apart = true;
                 }
@@ -692,8 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 acc.template softmax<2>(p, inv);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    uint32_t b0 = movmatrix_trans(pack_f16(p[h][0], p[h][1])), b1 = movmatrix_trans(pack_f16(p[h][2], p[h][3]));
-                    if (b_iv[h] < 0.f) b0 = b1 = 0;  // values of zero
+                    const uint32_t b0 = movmatrix_trans(pack_f16(p[h][0], p[h][1])), b1 = movmatrix_trans(pack_f16(p[h][2], p[h][3]));
                     if (D == 128) {
                         value_word<D>(acc.o, vx[h][0].x, vx[h][1].x, vx[h][2].x, vx[h][3].x, b0, b1);
                         value_word<D>(acc.o + 2, vx[h][0].y, vx[h][1].y, vx[h][2].y, vx[h][3].y, b0, b1);

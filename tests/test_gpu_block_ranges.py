@@ -180,3 +180,35 @@ def test_appended_values_far_apart(ctx):
     st.v, st.v_open = st.v.abs(), st.v_open.abs()
     bound = bound + APART * st.attend(0, q, [0.1])[0] + unseen(st, q, 0.1)
     assert bool(((out.cpu().double() - want).abs() <= bound).all())
+
+
+# ----------------------------------------------------------------------------------------------- blocks of zeros
+
+@pytest.mark.parametrize("L,B,lens", LENS)
+@pytest.mark.parametrize("T", [16, 32])
+def test_blocks_of_zeros_among_small_ones(ctx, L, B, lens, T):
+    """A large block that no query looks at, then blocks of zeros, then small ones at the same logits as the zeros: out is the small ones'
+    share, to the precision that it has without the others."""
+    D = 128
+    st = state(L, B, lens, D, T, seed=T)
+    n = st.capacity
+    st.k.zero_()
+    st.k[..., 0] = 127
+    odd = torch.arange(n) % 2 == 1
+    st.v_scale[:] = torch.where(odd, 2.0 ** -37 / 127, 0.0).float()
+    st.v_scale[..., 0] = 1 / 127
+    st.k_scale[..., 0] = 200 / 127     # logit -200 with a query of -1
+    st.k_scale[..., 1:] = 1e-3
+    st.k_open.zero_()
+    scale_open(st, 2.0 ** -37)
+    q = torch.zeros((L, B, 8, D), dtype=torch.bfloat16)
+    q[..., 0] = -1.0
+    check(ctx, st, q, 1.0)
+
+
+@pytest.mark.parametrize("L,B,lens", LENS)
+@pytest.mark.parametrize("D,T", [(128, 16), (64, 64)])
+@pytest.mark.parametrize("sizes", [(2.0 ** 119, 1.0, 0.0, 2.0 ** -99), (0.0, 2.0 ** -99, 2.0 ** 119), (0.0, 1.0), (0.0,), (1.0, 0.0, 0.0)])
+@pytest.mark.parametrize("spread", [1.0, 40.0])
+def test_blocks_of_zeros_and_others_in_turn(ctx, L, B, lens, D, T, sizes, spread):
+    blocks_in_turn(ctx, L, B, lens, D, T, sizes, spread)
