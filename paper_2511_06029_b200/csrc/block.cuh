@@ -172,23 +172,6 @@ struct Piece<__nv_bfloat16> {
     }
 };
 
-// Magnitudes of two bf16 are two 16-bit whole numbers in the same order; from kNotFinite on they are infinities and NaN.
-constexpr unsigned kNotFinite = 0x7f80;
-__device__ __forceinline__ uint32_t top_of(const uint4& w, uint32_t top) {
-    top = __vmaxu2(top, w.x & 0x7fff7fffu);
-    top = __vmaxu2(top, w.y & 0x7fff7fffu);
-    top = __vmaxu2(top, w.z & 0x7fff7fffu);
-    return __vmaxu2(top, w.w & 0x7fff7fffu);
-}
-// The same without those that are not finite.
-static __device__ __noinline__ uint32_t finite_top_of(uint4 w, uint32_t top) {
-    auto finite = [](uint32_t x) {
-        x &= 0x7fff7fffu;
-        return ((x & 0xffffu) >= kNotFinite ? 0u : x & 0xffffu) | (x >= kNotFinite << 16 ? 0u : x & 0xffff0000u);
-    };
-    return __vmaxu2(__vmaxu2(__vmaxu2(top, finite(w.x)), finite(w.y)), __vmaxu2(finite(w.z), finite(w.w)));
-}
-
 // A row of D elements is taken as D / (2 N) tasks of two 16-byte pieces, which hold both halves of their pairs: with pairs half a
 // rotation apart, pieces (c, c + half / N); with neighbouring pairs, (2c, 2c + 1); behind the rotated part, (2c, 2c + 1).
 // `turned` says whether the task's pieces are rotated.  `vec`: the style's pieces are whole (rotation_in_pieces).

@@ -15,6 +15,22 @@ constexpr int kQueryRows = 16, kManyQueryRows = 32, kQueryTokens = 2;
 constexpr int kPlenty = 1184;  // blocks to fill: eight for each of 148 SMs
 constexpr int kFewTokens = 4;  // tokens to a sequence that a warp takes one after the other
 
+// Magnitudes of two bf16 are two 16-bit whole numbers in the same order; from kNotFinite on they are infinities and NaN.
+constexpr unsigned kNotFinite = 0x7f80;
+__device__ __forceinline__ uint32_t top_of(const uint4& w, uint32_t top) {
+    top = __vmaxu2(top, w.x & 0x7fff7fffu);
+    top = __vmaxu2(top, w.y & 0x7fff7fffu);
+    top = __vmaxu2(top, w.z & 0x7fff7fffu);
+    return __vmaxu2(top, w.w & 0x7fff7fffu);
+}
+// The same without those that are not finite.
+__device__ __noinline__ uint32_t finite_top_of(uint4 w, uint32_t top) {
+    auto finite = [](uint32_t x) {
+        x &= 0x7fff7fffu;
+        return ((x & 0xffffu) >= kNotFinite ? 0u : x & 0xffffu) | (x >= kNotFinite << 16 ? 0u : x & 0xffff0000u);
+    };
+    return __vmaxu2(__vmaxu2(__vmaxu2(top, finite(w.x)), finite(w.y)), __vmaxu2(finite(w.z), finite(w.w)));
+}
 // Codes of eight values of at most the largest magnitude: 1.5 x 2^23 added to a product rounds it to the nearest whole number (ties to
 // even), which the sum's lowest byte holds.
 __device__ __forceinline__ uint2 codes8(const uint4& w, float inv) {

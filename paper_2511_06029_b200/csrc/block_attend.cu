@@ -13,10 +13,9 @@
 // in O^T += V^T P^T (m16n8k16 f16 MMAs, the probabilities turned by movmatrix), and the sum of probabilities takes p' / vs.  A value code
 // becomes the f16 of the same value by bit operations (1024 + 128 + x is 0x6400 | (x ^ 0x80)) and one subtraction, exactly.  m is the
 // largest s + log2 vs up to a factor of 2^6: it only moves when a logit outgrows it by that, and p' is kept 2^9 up, so that f16 (up to
-// 2^15 in use) holds probabilities down to 2^-23 of the largest with full precision.  Where the scales of a stretch lie more than 2^40
-// apart the sum has a reference of its own, since m no longer says how large p' / vs is;
-// blocks of zeros count as far apart and have a part in that sum only.  Rows of open blocks are bf16 and may have any
-// range: they take bf16 MMAs with the probabilities in two terms, their values relative to a power of two in the place of a scale.
+// 2^15 in use) holds probabilities down to 2^-23 of the largest with full precision.  Rows of open blocks take bf16 MMAs with the
+// probabilities in two terms.  Stretches whose value scales leave the range that one m can serve, or whose open rows overflow, are done once
+// more by far_stretch, plainly.
 //
 // Measured (us): a step of the Llama-8B shape, 571 MB, 101 = 5.7 TB/s, 0.86 of the copy rate; one sequence of 131072 tokens, 268 MB, 48 = 0.85;
 // a ragged batch in blocks of 16 61 = 0.80; one layer of the first 13 (3.5 until the first tiles are asked for, 2 to 5 for two or three steps
@@ -39,9 +38,10 @@ constexpr int kPad = 3;         // and of an item's beginning: its length, first
 constexpr int kLine = 2048;     // items whose places on the line are kept in shared memory; of more, only every so many-th is
 constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
 constexpr float kLift = 9.f;    // p' is kept up by this (log2)
-// Value scales of a stretch up to this far (log2) from its reference: the sums of p' / vs and O can have one m.  Further apart the sum
-// of probabilities has a reference of its own (sums_apart), since p' / vs would leave the range of fp32.
-constexpr float kApart = 40.f, kFar = 1099511627776.f;  // 2^kApart
+// Value scales that a stretch takes with one m: up to 2^40 either side of the first of them, which lies between 2^-40 and 2^60.  The sum
+// of p' / vs lies between 2^-31 and 2^72 then, with 2^17 tokens, and O, up to 2^39, stays in fp32 with that and the scale as factors.
+constexpr float kFar = 0x1p40f, kLeastRef = 0x1p-40f, kMostRef = 0x1p60f;
+constexpr float kZeroLog2 = -40.f;  // where a block of zeros, which only the sum of probabilities knows, counts for m
 
 template <int D>
 __host__ __device__ constexpr int stage_bytes() { return kStep * D * 2; }
@@ -63,7 +63,6 @@ struct __align__(1024) Smem {
     int line[kLine + 1], len[kLine];
     int prefix[kThreads + 1], totals[kBlockWarps];
     Rec rec[32];                            // warp w: 2 w its first stretch, 2 w + 1 its last
-    float4 apart[kBlockWarps][32];          // stretches whose scales lie far apart: per lane the sums' references and sums (two heads)
     float m[32][8], l[32][8];               // a part's weight is l 2^m; its O is divided by that
     int abort;
 };
@@ -124,8 +123,6 @@ struct Acc {
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
     }
-    // references and sums of their own (sums_apart), with the lift of p' taken into the reference
-    __device__ __forceinline__ float4 sums() const { return make_float4(m[0] - kLift, m[1] - kLift, l[0], l[1]); }
     // x: logits of H x 16 tokens (row g: x[h][0], x[h][1]; row g + 8: x[h][2], x[h][3]) -> p', and m moved where it has to be
     template <int H>
     __device__ __forceinline__ void softmax(float (&x)[H][4], const float (&inv_vs)[H]) {
@@ -173,36 +170,107 @@ struct Acc {
 // The root of exp2(a - b): a part that is 2^228 times as large as another may count for as much with a weight as small as that.
 __device__ __forceinline__ float root_diff(float a, float b) { return a == -INFINITY ? 0.f : fast_exp2(0.5f * (a - b)); }
 
-// The sums of probabilities of H x 16 tokens where value scales lie far apart: `at` holds {reference, reference, sum, sum} of the lane's
-// heads, x the logits with log2 vs = lv added.  Tokens whose values are zero (iv < 0) have no part in O: their x becomes -inf.
-template <int H>
-__device__ __forceinline__ void sums_apart(float4* at, float (&x)[H][4], const float (&lv)[H], const float (&iv)[H]) {
-    const float4 old = *at;
-    float s[H][4], a = -INFINITY, b = -INFINITY;
+// Tokens of an item for values of any size: full blocks of the steps g0 .. g1 - 1 and open rows r0 .. r1 - 1, a warp, a token at a time with
+// D / 32 elements to a lane.  Leaves m, l (weight l 2^m) and O / l of each head in shared memory, or, with part = NULL, the item's output.
+// Everything is held in the values' own size: O is a mean at all times.  A thirtieth of the kernel's speed (a step of the Llama-8B shape, all
+// of it by this function, 3.4 ms), for values that no model has; in a function of its own it costs ordinary calls nothing, in the kernel's
+// loop 4 us of that step.
+template <int D>
+__device__ __noinline__ void far_stretch(const BlockAttendArgs& a, int idx, int g0, int g1, int r0, int r1, float* part, float* part_m, float* part_l) {
+    constexpr int E = D / 32, U = 8;
+    const BlockView& c = a.c;
+    const int lane = threadIdx.x & 31;
+    const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, idx);
+    const int full = block_len(c, it.item) >> c.t_shift;
+    const size_t row0 = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G;
+    float q[8][E], o[8][E], m[8], l[8], scale[8];
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
+    for (int h = 0; h < 8; ++h) {
+        bool bad = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s[h][i] = x[h][i] == -INFINITY ? -INFINITY : x[h][i] - lv[h];
-            if (iv[h] < 0.f) x[h][i] = -INFINITY;
+        for (int e = 0; e < E; ++e) {
+            q[h][e] = h < c.G ? __bfloat162float(a.q[(row0 + h) * D + E * lane + e]) : 0.f;
+            bad = bad || !(fabsf(q[h][e]) < INFINITY);
+            o[h][e] = 0.f;
         }
-        a = fmaxf(a, fmaxf(s[h][0], s[h][2]));
-        b = fmaxf(b, fmaxf(s[h][1], s[h][3]));
+        scale[h] = __any_sync(0xffffffffu, bad) ? __uint_as_float(0x7fc00000u) : c.scale_log2[c.layer_begin + it.li];
+        m[h] = -INFINITY;
+        l[h] = 0.f;
+    }
+    auto token = [&](const float (&k)[E], const float (&v)[E], float k_scale) {
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+            float s = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) s = fmaf(q[h][e], k[e], s);
+#pragma unroll
+            for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
+            s *= k_scale * scale[h];
+            const float top = fmaxf(m[h], s), old = root_diff(m[h], top), now = root_diff(s, top);
+            const float was = l[h] * old, sum = fmaf(was, old, now * now), inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[h][e] = o[h][e] * old * (was * inv) + v[e] * now * (now * inv);
+            m[h] = top;
+            l[h] = sum;
+        }
+    };
+    const int group = min(c.T, kStep);  // tokens of a step that lie in one block
+#pragma unroll 1
+    for (int j = g0 * kStep; j < g1 * kStep; j += group) {
+        const int e0 = j >> c.t_shift;
+        int blk = e0;
+        if (a.selected) blk = e0 < min(a.n_select, full) ? a.selected[(size_t)idx * a.n_select + e0] : -1;
+        const long long page = blk >= 0 && blk < full ? block_page(c, it.item, blk) : -1;
+        if (page < 0) continue;
+        const float ks = c.k_scale[page], vs = c.v_scale[page];
+        const size_t at = ((size_t)page * c.T + (j & (c.T - 1))) * D + E * lane;
+#pragma unroll 1
+        for (int i0 = 0; i0 < group; i0 += U) {
+            uint32_t kw[U], vw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int8_t *kp = c.k + at + (size_t)(i0 + u) * D, *vp = c.v + at + (size_t)(i0 + u) * D;
+                kw[u] = E == 4 ? *reinterpret_cast<const uint32_t*>(kp) : *reinterpret_cast<const uint16_t*>(kp);
+                vw[u] = E == 4 ? *reinterpret_cast<const uint32_t*>(vp) : *reinterpret_cast<const uint16_t*>(vp);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float k[E], v[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    k[e] = (float)(int8_t)(kw[u] >> (8 * e));
+                    v[e] = (float)(int8_t)(vw[u] >> (8 * e)) * vs;
+                }
+                token(k, v, ks);
+            }
+        }
+    }
+#pragma unroll 1
+    for (int r = r0; r < r1; ++r) {
+        const size_t at = ((size_t)it.item * c.T + r) * D + E * lane;
+        float k[E], v[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            k[e] = __bfloat162float(c.k_open[at + e]);
+            v[e] = __bfloat162float(c.v_open[at + e]);
+        }
+        token(k, v, 1.f);
     }
 #pragma unroll
-    for (int k = 4; k < 32; k <<= 1) {
-        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, k));
-        b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, k));
-    }
-    a = fmaxf(a, old.x);
-    b = fmaxf(b, old.y);
-    float la = old.z * exp2_diff(old.x, a), lb = old.w * exp2_diff(old.y, b);
+    for (int h = 0; h < 8; ++h) {
+        if (part) {
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-        la += exp2_diff(s[h][0], a) + exp2_diff(s[h][2], a);
-        lb += exp2_diff(s[h][1], b) + exp2_diff(s[h][3], b);
+            for (int e = 0; e < E; ++e) part[h * D + E * lane + e] = o[h][e];
+            if (lane == 0) {
+                part_m[h] = m[h];
+                part_l[h] = l[h];
+            }
+        } else if (h < c.G) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) a.out[(row0 + h) * D + E * lane + e] = __float2bfloat16(o[h][e]);
+            if (a.lse && lane == 0) a.lse[row0 + h] = l[h] == 0.f ? -INFINITY : (m[h] + log2f(l[h])) * 0.6931471805599453f;
+        }
     }
-    *at = make_float4(a, b, la, lb);
 }
 
 // Elements that a lane reads of a key row (16 bytes at each of D / 64 places) and of a value row, and the order of a tile's tokens among
@@ -229,14 +297,9 @@ __device__ __forceinline__ void value_word(float (*o)[4], uint32_t a, uint32_t b
     mma_f16(o[1], f1, p0, p1);
 }
 
-// The exponent field of a power of two, a float's or a bf16's.
-__device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 0xffu); }
-__device__ __forceinline__ float power_of_two(int field) { return __uint_as_float((uint32_t)field << 23); }
-
-// 32 open rows from row r0 on: keys and values straight from memory, bf16, all asked for before anything is used.  The values are taken
-// like codes, relative to a power of two of their own (which leaves a bf16 as exact as it is): the largest of them below 2^7.
+// 32 open rows from row r0 on: keys and values straight from memory, bf16, all asked for before anything is used.
 template <int D>
-__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float& v_ref, bool& have_ref, float4* sums, bool& apart) {
+__device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc, const BlockItem& it, int r0, int n_open, const float (&scale2)[2], float v_ref, float inv_ref_log2) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const __nv_bfloat16* K = a.c.k_open + (size_t)it.item * a.c.T * D;
     const __nv_bfloat16* V = a.c.v_open + (size_t)it.item * a.c.T * D;
@@ -265,41 +328,6 @@ __device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc,
 #pragma unroll
             for (int j = 0; j < D / 64; ++j) v[h][i][j] = row < n_open ? *reinterpret_cast<const uint4*>(V + (size_t)row * D + d0 + 8 * j) : zero;
         }
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8 * (D / 64); ++i) top = top_of(v[i & 1][i >> 1 & 3][i >> 3], top);
-    unsigned bits = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-    if (bits >= kNotFinite) {  // the same in all lanes
-        top = 0;
-#pragma unroll
-        for (int i = 0; i < 8 * (D / 64); ++i) top = finite_top_of(v[i & 1][i >> 1 & 3][i >> 3], top);
-        bits = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-    }
-    // 2^-100 and less are taken relative to the same power (as blocks are, nothing smaller counts as large)
-    const int own = max((int)(bits >> 7), 127 - 100) - 6;
-    if (!have_ref && bits) {
-        v_ref = power_of_two(own);
-        have_ref = true;
-    }
-    const int off = own - exponent_of(v_ref);
-    const float lv = (float)off, iv = bits ? power_of_two(min(max(127 - off, 1), 254)) : -1.f;
-    if (!apart && (!bits || fabsf(lv) > kApart)) {
-        *sums = acc.sums();
-        apart = true;
-    }
-    const __nv_bfloat162 by = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((254 - own) << 7)));
-    auto relative = [&](uint32_t& w) {
-        const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w), by);
-        w = *reinterpret_cast<const uint32_t*>(&x);
-    };
-#pragma unroll
-    for (int i = 0; i < 8 * (D / 64); ++i) {
-        uint4& x = v[i & 1][i >> 1 & 3][i >> 3];
-        relative(x.x);
-        relative(x.y);
-        relative(x.z);
-        relative(x.w);
-    }
     float s[2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -313,10 +341,9 @@ __device__ __forceinline__ void open_rows(const BlockAttendArgs& a, Acc<D>& acc,
             mma_bf16(s[h], f1, q[j].z, q[j].w);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[h][i] = r0 + 16 * h + 8 * (i >> 1) + g < n_open ? fmaf(s[h][i], scale2[i & 1], lv) : -INFINITY;
+        for (int i = 0; i < 4; ++i) s[h][i] = r0 + 16 * h + 8 * (i >> 1) + g < n_open ? fmaf(s[h][i], scale2[i & 1], inv_ref_log2) : -INFINITY;
     }
-    const float inv[2] = {iv, iv}, lvs[2] = {lv, lv};
-    if (apart) sums_apart<2>(sums, s, lvs, inv);
+    const float inv[2] = {v_ref, v_ref};
     acc.template softmax<2>(s, inv);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -473,8 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             int ask0 = -64, ask_page = -1, use0 = -64;
             float ask_ks = 0.f, ask_vs = 0.f, ks = 0.f, lv = 0.f, iv = 0.f;  // iv: v_ref / vs, negative: a block whose values are zero
             float v_ref = 1.f, inv_ref = 1.f;
-            bool have_ref = false, apart = false;
-            float4* const sums = &sm.apart[w][lane];
+            bool have_ref = false, far = false;
             auto ask_run = [&](int e0) {
                 ask0 = e0;
                 ask_page = -1;
@@ -499,8 +525,6 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     }
                 }
             };
-            Acc<D> acc;
-            acc.clear();
             auto use_run = [&]() {
                 use0 = ask0;
                 ks = ask_ks;
@@ -513,15 +537,13 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                         v_ref = __uint_as_float((uint32_t)ex << 23);
                         inv_ref = __uint_as_float((uint32_t)(254 - ex) << 23);
                         have_ref = true;
+                        far = v_ref < kLeastRef || v_ref > kMostRef;
                     }
                 }
                 const float rel = ask_vs * inv_ref;
-                if (!apart && __any_sync(0xffffffffu, ask_page >= 0 && (rel > kFar || rel < 1.f / kFar))) {  // a scale of zero among them
-                    *sums = acc.sums();
-                    apart = true;
-                }
-                lv = ask_page < 0 ? -INFINITY : ask_vs == 0.f ? 0.f : apart ? log2f(ask_vs) - log2f(v_ref) : __log2f(rel);  // no block: no weight
-                iv = ask_vs == 0.f ? -1.f : __fdividef(1.f, rel);
+                far = far || __any_sync(0xffffffffu, ask_vs > 0.f && (rel > kFar || rel < 1.f / kFar));
+                lv = ask_page < 0 ? -INFINITY : ask_vs == 0.f ? kZeroLog2 : __log2f(rel);  // no block: no weight
+                iv = ask_vs == 0.f ? -kFar : __fdividef(1.f, rel);
             };
             // step gi: one tile of a block of 32 tokens or more, or two blocks of 16
             auto issue = [&](int gi) {
@@ -613,10 +635,16 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 scale2[0] = open2[0] * __shfl_sync(0xffffffffu, div, 8 * t);
                 scale2[1] = open2[1] * __shfl_sync(0xffffffffu, div, 8 * t + 4);
             }
+            Acc<D> acc;
+            acc.clear();
             float b_ks[2] = {0.f, 0.f}, b_lv[2] = {0.f, 0.f}, b_iv[2] = {0.f, 0.f};  // of the blocks at hand
-            for (int gi = g0; gi < g1; ++gi) {
+            int done = g0;
+            for (int gi = g0; gi < g1; done = ++gi) {
                 const int e = (gi * kStep) >> c.t_shift;
-                if (e >= use0 + 32 || use0 < 0) use_run();
+                if (e >= use0 + 32 || use0 < 0) {
+                    use_run();
+                    if (far) break;
+                }
                 if (c.t_shift <= 5 || gi == g0 || !((gi * kStep) & (c.T - 1))) {
                     b_ks[0] = b_ks[1] = __shfl_sync(0xffffffffu, ks, e - use0);
                     b_lv[0] = b_lv[1] = __shfl_sync(0xffffffffu, lv, e - use0);
@@ -630,12 +658,6 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 unsigned long long* bar = &sm.bars[w][stage];
                 if (!warp_wait(bar, phase, &sm.abort, a.wait_limit)) {
                     if (lane == 0) record_error(c.status, LETHE_ERR_TIMEOUT, blockIdx.x);
-                    // what is in flight lands before the CTA goes on
-                    for (int k = gi; k < queued; ++k) {
-                        bar_drain(&sm.bars[w][stage], phase);
-                        stage = stage + 1 == NS ? 0 : stage + 1;
-                        phase ^= stage == 0;
-                    }
                     aborted = true;
                     break;
                 }
@@ -688,12 +710,12 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 phase ^= stage == 0;
                 if (queued < g1) issue(queued++);
 
-                if (apart) sums_apart<2>(sums, p, b_lv, b_iv);
                 const float inv[2] = {fabsf(b_iv[0]), fabsf(b_iv[1])};
                 acc.template softmax<2>(p, inv);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t b0 = movmatrix_trans(pack_f16(p[h][0], p[h][1])), b1 = movmatrix_trans(pack_f16(p[h][2], p[h][3]));
+                    uint32_t b0 = movmatrix_trans(pack_f16(p[h][0], p[h][1])), b1 = movmatrix_trans(pack_f16(p[h][2], p[h][3]));
+                    if (b_iv[h] < 0.f) b0 = b1 = 0;  // values of zero
                     if (D == 128) {
                         value_word<D>(acc.o, vx[h][0].x, vx[h][1].x, vx[h][2].x, vx[h][3].x, b0, b1);
                         value_word<D>(acc.o + 2, vx[h][0].y, vx[h][1].y, vx[h][2].y, vx[h][3].y, b0, b1);
@@ -705,41 +727,53 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     }
                 }
             }
+            // after a break: what is in flight lands before the warp goes on
+            for (; done < queued; ++done) {
+                bar_drain(&sm.bars[w][stage], phase);
+                stage = stage + 1 == NS ? 0 : stage + 1;
+                phase ^= stage == 0;
+            }
             // open rows whose place on the line lies in the stretch
             const int tail0 = (max(p0 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight, tail1 = (max(p1 - kPad - sp.steps, 0) + kTailWeight - 1) / kTailWeight;
-            for (int j = tail0; j < tail1 && 32 * j < sp.open; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, open2, v_ref, have_ref, sums, apart);
+            for (int j = tail0; j < tail1 && 32 * j < sp.open && !far; ++j) open_rows<D>(a, acc, it, 32 * j, sp.open, open2, v_ref, __log2f(inv_ref));
 
-            float4 own = acc.sums();
-            float by[2] = {v_ref, v_ref};  // what brings O to the sum's reference, and to the values' size
-            if (apart) {
-                const float ref = (float)(exponent_of(v_ref) - 127);
-                by[0] = acc.m[0] == -INFINITY ? 0.f : fast_exp2(0.5f * (own.x - sums->x + ref));  // half of it: the whole may have no place in fp32
-                by[1] = acc.m[1] == -INFINITY ? 0.f : fast_exp2(0.5f * (own.y - sums->y + ref));
-                own = *sums;
-                acc.l[0] = own.z;
-                acc.l[1] = own.w;
-            }
 #pragma unroll
             for (int s = 4; s < 32; s <<= 1) {
                 acc.l[0] += __shfl_xor_sync(0xffffffffu, acc.l[0], s);
                 acc.l[1] += __shfl_xor_sync(0xffffffffu, acc.l[1], s);
             }
             // What leaves the stretch is divided by its sum: a mean of values is as large as they are, and a part's weight is its sum.
-            float top[2];
+            float top[2], all = 0.f;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const float inv = acc.l[k] == 0.f ? 0.f : 1.f / acc.l[k];
-                top[k] = acc.l[k] == 0.f ? -INFINITY : k ? own.y : own.x;
-                const float again = apart ? by[k] : 1.f;
+                const float f = acc.l[k] == 0.f ? 0.f : __fdividef(v_ref, acc.l[k]);
+                top[k] = acc.l[k] == 0.f ? -INFINITY : acc.m[k] - kLift;
+                float sizes = 0.f;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    acc.o[i][k] = acc.o[i][k] * inv * by[k] * again;
-                    acc.o[i][2 + k] = acc.o[i][2 + k] * inv * by[k] * again;
+                    acc.o[i][k] *= f;
+                    acc.o[i][2 + k] *= f;
+                    sizes += fabsf(acc.o[i][k]) + fabsf(acc.o[i][2 + k]);
                 }
+                if (acc.l[k] < INFINITY) all += sizes;  // a query that is not finite has a sum that is not, and gives NaN either way
             }
+            far = far || (tail0 < tail1 && __any_sync(0xffffffffu, !(all < INFINITY)));  // open rows may hold anything
             const bool begins = p0 == 0, ends = p1 == sp.w;
+            const bool last = at1 <= start + sp.w;  // nothing of this warp comes after it: the ring is free
+            const int which = 2 * w + (last ? 1 : 0);
+            float* const part = begins && ends ? nullptr : last ? reinterpret_cast<float*>(sm.ring[w]) : sm.first[w];
+            if (part && lane == 0) {
+                Rec& rec = sm.rec[which];
+                rec.idx = idx;
+                rec.start = start;
+                rec.w = sp.w;
+                rec.begins = begins;
+                rec.ends = ends;
+            }
             const int d0 = first_d<D>(g);
-            if (begins && ends) {
+            if (far) {
+                far_stretch<D>(a, idx, g0, aborted ? g0 : g1, min(32 * tail0, sp.open), min(32 * tail1, sp.open), part, sm.m[which], sm.l[which]);
+            } else if (!part) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int head = 2 * t + k;
@@ -752,16 +786,6 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     if (a.lse && g == 0) a.lse[row] = acc.l[k] == 0.f ? -INFINITY : (top[k] + log2f(acc.l[k])) * 0.6931471805599453f;
                 }
             } else {
-                const bool last = at1 <= start + sp.w;  // nothing of this warp comes after it: the ring is free
-                const int which = 2 * w + (last ? 1 : 0);
-                Rec& rec = sm.rec[which];
-                if (lane == 0) {
-                    rec.idx = idx;
-                    rec.start = start;
-                    rec.w = sp.w;
-                    rec.begins = begins;
-                    rec.ends = ends;
-                }
                 if (g == 0) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
@@ -769,12 +793,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                         sm.l[which][2 * t + k] = acc.l[k];
                     }
                 }
-                float* part = last ? reinterpret_cast<float*>(sm.ring[w]) : sm.first[w];
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i)
-                        *reinterpret_cast<float2*>(part + (2 * t + k) * D + d0 + 2 * i) = make_float2(acc.o[i][k], acc.o[i][2 + k]);
+                    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<float2*>(part + (2 * t + k) * D + d0 + 2 * i) = make_float2(acc.o[i][k], acc.o[i][2 + k]);
             }
             at = start + p1;
             start += sp.w;
@@ -814,7 +836,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             l = mine_l * half;
 #pragma unroll
             for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-            const float f = l == 0.f ? 0.f : mine_l / l;  // a part's share of the sum is half x f
+            const float f = l == 0.f ? 0.f : __fdividef(mine_l, l);  // a part's share of the sum is half x f
             float o[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -878,7 +900,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
                     l = fmaf(old, old_half, sum);
                     m = nm;
-                    const float f = l == 0.f ? 0.f : old / l, g = l == 0.f ? 0.f : mine / l;
+                    const float inv = l == 0.f ? 0.f : __fdividef(1.f, l), f = old * inv, g = mine * inv;
 #pragma unroll
                     for (int e = 0; e < E; ++e) o[e] = o[e] * old_half * f;
 #pragma unroll 1

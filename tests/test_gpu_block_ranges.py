@@ -109,7 +109,18 @@ the factor that joins O and the sum: 3.5 x 2^-16 in the exponent of 2, times log
 def unseen(st, q, scale):
     """What f16 does not hold of small shares: a share times its scale is kept 2^9 times as large as the largest of them at least, and
     below 2^-14 it is off by half of f16's smallest number, 2^-25.  So 2^-34 of the largest for each token and unit of its code, which
-    counts where the tokens of the largest shares have small codes in an element.  [nl][B][Hq][1]"""
+    counts where the tokens of the largest shares have small codes in an element.  Open rows have two bf16 terms in its place: below 2^-126
+    a share vanishes, below 2^-117 its second term, half a step of 2^-9, does: 2 x 2^-135 of the largest share of a full block times its
+    scale, for each token and |x|, the largest open value.
+
+    Values of zero have a share but no size, and nothing says against what they should be held.  Full blocks of zeros count among the
+    shares like blocks of 2^-40 of the reference r, the first scale (1 where there is none, 2^60 at most), open rows of zeros like others,
+    that is like blocks of scale 1; a factor of 2^6 is how far m may lag.  What they outweigh so far that it leaves fp32 vanishes:
+        full blocks before open zeros, rescaled:  p vs < p0 2^-126 2^6, times 127            -> p0 2^-113
+        full blocks before full zeros, rescaled:  p vs < p0 2^-126 2^6 2^-40 r, times 127    -> p0 2^-153 r
+        full blocks behind full zeros:            p vs < p0 2^-126 2^-9 2^-40 r, times 127   -> less than the line above
+        open rows behind full zeros:              p < p0 2^-126 2^-9 2^-40 r, times |x|      -> p0 2^-175 r |x|
+    for each token.  [nl][B][Hq][1]"""
     room = torch.zeros(q.shape[:3] + (1,), dtype=torch.float64)
     for li in range(q.shape[0]):
         for b in range(st.B):
@@ -117,8 +128,17 @@ def unseen(st, q, scale):
                 K, V = st.rows((li, b, h))
                 n, hs = int(st.len[li, b, h]) // st.T, slice(h * st.G, (h + 1) * st.G)
                 p = torch.softmax(q[li, b, hs].double() @ K.T * scale, 1)
-                size = torch.cat([st.v_scale[li, b, h, :n].double().repeat_interleave(st.T), V[n * st.T:].abs().amax(1) / 64])
+                scales, largest = st.v_scale[li, b, h, :n].double(), V[n * st.T:].abs().amax(1)
+                r = max([1.0] + [min(float(x), 2.0 ** 60) for x in scales])
+                size = torch.cat([torch.where(scales == 0, r * 2.0 ** -40, scales).repeat_interleave(st.T), largest / 64])
                 room[li, b, hs, 0] = (p * size).amax(1) * 127 * n * st.T * 2.0 ** -34
+                if len(largest) and n:
+                    full = (p[:, :n * st.T] * size[:n * st.T]).amax(1)
+                    room[li, b, hs, 0] += full * float(largest.max()) * len(largest) * 2.0 ** -134
+                zero = V.abs().amax(1) == 0
+                if bool(zero.any()):
+                    gone = 2.0 ** -113 + 2.0 ** -153 * r + 2.0 ** -175 * r * float(largest.max() if len(largest) else 0)
+                    room[li, b, hs, 0] += p[:, zero].amax(1) * gone * len(V)
     return room
 
 
