@@ -515,7 +515,8 @@ lethe_status lethe_block_select(lethe_ctx *ctx, const lethe_block_cache *cache, 
  * 21 bits relative to its largest element (their products with the stored numbers are summed exactly) and the probabilities are rounded
  * to f16; over open rows the query takes part as it is and the probabilities in two bf16 terms.  A query row with a NaN or an infinity
  * gives NaN; an open row's value that is not finite makes its element of out not finite.  Values of any size are taken; where an
- * item's value scales are more than 2^40 apart or not between 2^-40 and 2^60, or open values overflow, at a thirtieth of the speed.  Scratch: 32 bytes per item and 1.3 MB of partial results.  The same inputs give the same bits.
+ * item's value scales are more than 2^40 apart or not between 2^-40 and 2^60, or open values overflow, at a thirtieth of
+ * the speed.  Scratch: 32 bytes per item and 1.3 MB of partial results.  The same inputs give the same bits.
  */
 lethe_status lethe_block_attend(lethe_ctx *ctx, const lethe_block_cache *cache, int layer_begin, int layer_end, const void *q,
                                 const float *scale, const int32_t *selected, int n_select, void *out, float *lse, void *stream);

@@ -181,7 +181,7 @@ __device__ __noinline__ void far_stretch(const BlockAttendArgs& a, int idx, int 
     const BlockView& c = a.c;
     const int lane = threadIdx.x & 31;
     const BlockItem it = block_item(c.layer_begin, c.B, c.Hkv, idx);
-    const int full = block_len(c, it.item) >> c.t_shift;
+    const int full = block_len(c, it.item) >> c.t_shift, blocks = a.selected ? min(a.n_select, full) : full;
     const size_t row0 = (((size_t)it.li * c.B + it.b) * c.Hkv + it.h) * c.G;
     float q[8][E], o[8][E], m[8], l[8], scale[8];
 #pragma unroll
@@ -218,10 +218,14 @@ __device__ __noinline__ void far_stretch(const BlockAttendArgs& a, int idx, int 
 #pragma unroll 1
     for (int j = g0 * kStep; j < g1 * kStep; j += group) {
         const int e0 = j >> c.t_shift;
-        int blk = e0;
-        if (a.selected) blk = e0 < min(a.n_select, full) ? a.selected[(size_t)idx * a.n_select + e0] : -1;
-        const long long page = blk >= 0 && blk < full ? block_page(c, it.item, blk) : -1;
-        if (page < 0) continue;
+        if (e0 >= blocks) break;
+        const int blk = a.selected ? a.selected[(size_t)idx * a.n_select + e0] : e0;
+        if (blk < 0) continue;
+        const long long page = blk < full ? block_page(c, it.item, blk) : -1;
+        if (page < 0) {  // the kernel's own way records only what it has come to
+            if (lane == 0) record_error(c.status, blk < full ? LETHE_ERR_PAGE : LETHE_ERR_INVALID_ARG, it.item);
+            continue;
+        }
         const float ks = c.k_scale[page], vs = c.v_scale[page];
         const size_t at = ((size_t)page * c.T + (j & (c.T - 1))) * D + E * lane;
 #pragma unroll 1

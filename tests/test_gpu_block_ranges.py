@@ -232,3 +232,42 @@ def test_blocks_of_zeros_among_small_ones(ctx, L, B, lens, T):
 @pytest.mark.parametrize("spread", [1.0, 40.0])
 def test_blocks_of_zeros_and_others_in_turn(ctx, L, B, lens, D, T, sizes, spread):
     blocks_in_turn(ctx, L, B, lens, D, T, sizes, spread)
+
+
+# ------------------------------------------------------------------- what the device refuses, among such values
+
+def test_bad_pages_and_entries_among_values_far_apart(ctx):
+    """A page outside the pool and an entry that is no full block are left out and recorded wherever in the list they stand.  As many
+    items of one length as the GPU has warps: each warp has one from end to end, and comes to the scales of a run of 32 blocks first."""
+    from paper_2511_06029_b200 import binding
+    T, B, bad = 16, torch.cuda.get_device_properties(0).multi_processor_count * 8, 39
+    st = BlockState(1, B, 1, 1, 64, T, 41, T * 41, True, seed=4)
+    st.v_scale *= torch.where(torch.arange(41) % 2 == 1, 1e-20, 1e20).float()
+    q = queries(st, 1)
+    cache = st.device_cache(with_range=False)
+    out = torch.empty_like(q, device="cuda")
+    full = torch.arange(41, dtype=torch.int32).expand(1, B, 1, 41).clone()
+    few = BlockState.__new__(BlockState)               # the statement for the items that are looked at
+    few.__dict__.update(st.__dict__)
+    few.B = 9
+
+    def check_first(lists):
+        want, _, bound, _ = few.attend(0, q[:, :9], [0.1], lists[:, :9])
+        few.v = st.v.abs()
+        bound = bound + APART * few.attend(0, q[:, :9], [0.1], lists[:, :9])[0] + unseen(few, q[:, :9], 0.1)
+        few.v = st.v
+        assert bool(((out[:, :9].cpu().double() - want).abs() <= bound).all())
+
+    page = cache.page_table[0, 7, 0, bad].clone()
+    cache.page_table[0, 7, 0, bad] = st.n_pages
+    ctx.block_attend(cache, 0, 1, q.cuda(), [0.1], out)
+    assert ctx.poll_status() == (binding.ERR_PAGE, 7)
+    cache.page_table[0, 7, 0, bad] = page
+    lists = full.clone()
+    lists[0, 7, 0, bad] = -1
+    check_first(lists)
+    given = lists.clone()
+    given[0, 7, 0, bad] = 41
+    ctx.block_attend(cache, 0, 1, q.cuda(), [0.1], out, selected=given.cuda())
+    assert ctx.poll_status() == (binding.ERR_INVALID_ARG, 7)
+    check_first(lists)
