@@ -112,7 +112,8 @@ typedef struct {
  * graphs go on using it, and it stays allocated until lethe_destroy (a buffer grows by a quarter at least, so all
  * that it has outgrown is less than four times what it has).  A call that would have to grow scratch
  * while its stream is being captured is refused with LETHE_ERR_UNSUPPORTED (size the scratch with
- * scratch_bytes_hint, or make the same call once before capturing).  A prune round also leaves the order of the
+ * scratch_bytes_hint, which also covers the block-cache calls' counters for up to 32768 items, or make the same call
+ * once before capturing).  A prune round also leaves the order of the
  * items' lengths for the decode calls on all layers of that cache: 4 bytes per item, one list for each number of
  * items, kept until lethe_destroy, so that captured decode calls stay valid whatever is pruned between their replays
  * (a captured round whose number of items no earlier round had leaves none).  Calls and graph replays of one context

@@ -274,9 +274,12 @@ lethe_status lethe_create(lethe_ctx** out, int device, size_t scratch_bytes_hint
     }
     ctx->sched = reinterpret_cast<unsigned int*>(ctx->status + 2);
     if (scratch_bytes_hint) {
-        if (ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, scratch_bytes_hint, "scratch") != LETHE_OK) {
-            cudaFree(ctx->status);
-            delete ctx;
+        // the block calls' counters lie apart from the scratch: 32 bytes per item for as many items as the hint covers, up to 32768
+        const size_t counters = scratch_bytes_hint < ((size_t)1 << 20) ? scratch_bytes_hint : (size_t)1 << 20;
+        if (ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, scratch_bytes_hint, "scratch") != LETHE_OK ||
+            ensure(ctx, &ctx->block_cnt, &ctx->block_cnt_bytes, counters, "block counters") != LETHE_OK ||
+            cudaMemset(ctx->block_cnt, 0, ctx->block_cnt_bytes) != cudaSuccess) {
+            lethe_destroy(ctx);
             return LETHE_ERR_CUDA;
         }
     }
