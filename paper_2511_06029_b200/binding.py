@@ -451,19 +451,19 @@ class Context:
                                                 None if rotary is None else ctypes.byref(rotary.c), _dp(out), _dp(lse),
                                                 _stream(self.device)))
 
-    @staticmethod
-    def _append_args(cache, nl, chunk_start, act, k_new, v_new, rotary, q, q_out):
+    # get_device() is -1 for a host tensor: one comparison says that a tensor is where the context's kernels run.
+    def _append_args(self, cache, nl, chunk_start, act, k_new, v_new, rotary, q, q_out):
         """Checks what append and block_append have in common; the number of tokens."""
-        n = k_new.shape[1]
-        assert chunk_start.is_cuda and chunk_start.is_contiguous() and chunk_start.dtype == torch.int32 and chunk_start.numel() == cache.batch + 1
+        n, dev = k_new.shape[1], self.device
+        assert cache.len.get_device() == dev and chunk_start.get_device() == dev and chunk_start.is_contiguous() and chunk_start.dtype == torch.int32 and chunk_start.numel() == cache.batch + 1
         want = (nl, n, cache.n_kv_heads, cache.head_dim)
         for t in (k_new, v_new):
-            assert t.is_cuda and t.dtype == act and t.shape == want and t.is_contiguous()
-        assert (q is None) == (q_out is None) and (rotary is None or rotary.n_tokens == n)
+            assert t.get_device() == dev and t.dtype == act and t.shape == want and t.is_contiguous()
+        assert (q is None) == (q_out is None) and (rotary is None or (rotary.n_tokens == n and rotary.axis_pos.get_device() == dev))
         if q is not None:
             want = (nl, n, cache.n_q_heads, cache.head_dim)
-            assert q.is_cuda and q.dtype == act and q.shape == want and q.is_contiguous()
-            assert q_out is q or (q_out.is_cuda and q_out.dtype == act and q_out.shape == want and q_out.is_contiguous())
+            assert q.get_device() == dev and q.dtype == act and q.shape == want and q.is_contiguous()
+            assert q_out is q or (q_out.get_device() == dev and q_out.dtype == act and q_out.shape == want and q_out.is_contiguous())
         return n
 
     def append(self, cache: Cache, layer_begin: int, layer_end: int, chunk_start: torch.Tensor, max_chunk: int, k_new, v_new, token_pos,
@@ -471,7 +471,7 @@ class Context:
         """k_new, v_new [nl][n_tokens][Hkv][D]; chunk_start [B + 1] and token_pos [n_tokens] int32; q, q_out [nl][n_tokens][Hq][D] (with
         rotary) or None.  All contiguous device tensors."""
         n = self._append_args(cache, layer_end - layer_begin, chunk_start, cache.act_dtype, k_new, v_new, rotary, q, q_out)
-        assert token_pos.is_cuda and token_pos.is_contiguous() and token_pos.dtype == torch.int32 and token_pos.numel() == n
+        assert token_pos.get_device() == self.device and token_pos.is_contiguous() and token_pos.dtype == torch.int32 and token_pos.numel() == n
         self._check(self.lib.lethe_append(self.h, ctypes.byref(cache.c), layer_begin, layer_end, chunk_start.data_ptr(), n, max_chunk,
                                           None if q is None else q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), token_pos.data_ptr(),
                                           None if rotary is None else rotary.ref, None if q is None else q_out.data_ptr(),
@@ -489,19 +489,20 @@ class Context:
     def block_read(self, cache: BlockCache, layer_begin: int, layer_end: int, slot_begin: Optional[torch.Tensor], k_out, v_out):
         """k_out, v_out bfloat16 [nl][B][Hkv][n_slots][D]; slot_begin [B] int32 on the device, or None for slot 0."""
         lead = (layer_end - layer_begin, cache.batch, cache.n_kv_heads, k_out.shape[3], cache.head_dim)
+        assert cache.len.get_device() == self.device
         for t in (k_out, v_out):
-            assert t.is_cuda and t.dtype == torch.bfloat16 and t.shape == lead and t.is_contiguous()
-        assert slot_begin is None or (slot_begin.is_cuda and slot_begin.is_contiguous() and slot_begin.dtype == torch.int32 and slot_begin.numel() == cache.batch)
+            assert t.get_device() == self.device and t.dtype == torch.bfloat16 and t.shape == lead and t.is_contiguous()
+        assert slot_begin is None or (slot_begin.get_device() == self.device and slot_begin.is_contiguous() and slot_begin.dtype == torch.int32 and slot_begin.numel() == cache.batch)
         self._check(self.lib.lethe_block_read(self.h, cache.ref, layer_begin, layer_end, None if slot_begin is None else slot_begin.data_ptr(),
                                               k_out.shape[3], k_out.data_ptr(), v_out.data_ptr(), _raw_stream(self.device)))
 
-    @staticmethod
-    def _block_query(cache, layer_begin, layer_end, selected, *tensors):
+    def _block_query(self, cache, layer_begin, layer_end, selected, *tensors):
         want = (layer_end - layer_begin, cache.batch, cache.n_q_heads, cache.head_dim)
+        assert cache.len.get_device() == self.device
         for t in tensors:
-            assert t.is_cuda and t.dtype == torch.bfloat16 and t.shape == want and t.is_contiguous()
+            assert t.get_device() == self.device and t.dtype == torch.bfloat16 and t.shape == want and t.is_contiguous()
         if selected is not None:
-            assert selected.is_cuda and selected.dtype == torch.int32 and selected.is_contiguous() and selected.dim() == 4
+            assert selected.get_device() == self.device and selected.dtype == torch.int32 and selected.is_contiguous() and selected.dim() == 4
             assert selected.shape[:3] == (want[0], cache.batch, cache.n_kv_heads) and selected.shape[3] > 0
 
     def block_select(self, cache: BlockCache, layer_begin: int, layer_end: int, q, sink: int, recent: int, selected: torch.Tensor):
@@ -515,7 +516,7 @@ class Context:
         """q, out [nl][B][Hq][D] bfloat16; scale one float per layer of the cache; lse [nl][B][Hq] float32 or None; selected as
         block_select leaves it, or None for all blocks."""
         self._block_query(cache, layer_begin, layer_end, selected, q, out)
-        assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.shape == q.shape[:3] and lse.is_contiguous())
+        assert lse is None or (lse.get_device() == self.device and lse.dtype == torch.float32 and lse.shape == q.shape[:3] and lse.is_contiguous())
         sc = scale_c if scale_c is not None else self._scale(scale)
         self._check(self.lib.lethe_block_attend(self.h, cache.ref, layer_begin, layer_end, q.data_ptr(), sc,
                                                 None if selected is None else selected.data_ptr(), 0 if selected is None else selected.shape[3],
