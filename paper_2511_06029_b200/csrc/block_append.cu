@@ -2,7 +2,7 @@
 // Measured (Llama-8B heads): a prompt of 8205 tokens, 184 MB, 43 us for the append = 4.3 TB/s; with the queries in a launch of their own 29 + 30
 // us, since filling blocks is a chain of short steps (rows, angles, magnitude, codes, range) that a few resident blocks of threads go
 // through at 1.7 TB/s: now the queries' stream runs beside it.  Two heads to a block of threads against one and four: 74, 77 and 77 us for a
-// prompt with its reading back, before that.  Single tokens of 8 sequences and 32 layers: 7 us with a warp to an item, 18 with a block.
+// prompt with its reading back, before that.  Single tokens of 8 sequences and 32 layers: 7 us, 23 where one of them fills blocks.
 #include "block.cuh"
 
 namespace lethe {
@@ -13,7 +13,11 @@ namespace {
 using bf16 = __nv_bfloat16;
 constexpr int kQueryRows = 16, kManyQueryRows = 32, kQueryTokens = 2;
 constexpr int kPlenty = 1184;  // blocks to fill: eight for each of 148 SMs
-constexpr int kFewTokens = 4;  // tokens to a sequence that a warp takes one after the other
+// Single tokens of this many items and more have a warp to an item, others a block of threads.  A warp's row is the cheaper one, a
+// sequence that fills blocks the dearer one, since its heads' warps lie together.  On average over the steps of sequences in blocks of 32:
+// 64 items 7 us with warps and 4.5 with blocks, 2048 items 10.4 and 10.2, 16384 items 42 and 54 (without a full block 6.7 and 9.4 of 2048
+// items, with one sequence's 23 and 13).  Two and more tokens: 2048 items 9.4 to 31 us with warps, 10.2 to 16 with blocks.
+constexpr int kManyItems = 2048;
 
 // Magnitudes of two bf16 are two 16-bit whole numbers in the same order; from kNotFinite on they are infinities and NaN.
 constexpr unsigned kNotFinite = 0x7f80;
@@ -68,8 +72,8 @@ __device__ __forceinline__ Filled filled(const BlockView& c, const NewRows& in, 
 }
 
 // Blocks of threads: first those of the items.
-// FEW (calls of a few tokens to a sequence): one to as many items as it has warps, since mostly a few rows go to open blocks, a warp's
-// work; items that fill a block then have all warps, one after the other.
+// FEW (calls of one token to a sequence, of many items): one to as many items as it has warps, since mostly a row goes to an open block, a
+// warp's work; items that fill a block then have all warps, one after the other.
 // Else: `units` to `heads` (1 .. 8) KV heads of a sequence, which share the cosines and sines of their tokens (where they have the same length, as
 // they mostly do).  Unit u quantises the u-th of the blocks that the call fills; unit 0 also moves what is left over to the open block (it
 // has read the rows that were there by then).
@@ -367,31 +371,25 @@ __global__ void __launch_bounds__(256, TPT == 1 ? 4 : TPT == 2 ? 3 : 2) block_ap
         const Filled f = some[w];
         const bool fills = f.n1 > 0 && f.n1 >> c.t_shift > f.n0 >> c.t_shift;
         if (f.n1 < 0 && lane == 0) record_error(c.status, LETHE_ERR_CAPACITY, f.item);
-        if (f.n1 > 0 && !fills)
-            for (int slot = f.n0; slot < f.n1; ++slot) {
-                if (rotated) {
-                    __syncwarp();
-                    for (int p = lane; p < half; p += 32) turn_by(turn_of(in, p), in.axis_pos[(size_t)axis_of(in, p) * in.n_tokens + f.s0 + slot - f.n0], cs[w][p], sn[w][p]);
-                    __syncwarp();
-                }
-                if (lane < kPerRow) {
-                    int at0, at1;
-                    uint4 kx, ky;
-                    load_row((const bf16*)in.k + row_of(f, slot), lane, rotated, cs[w], sn[w], at0, at1, kx, ky);
-                    const bf16* v = (const bf16*)in.v + row_of(f, slot);
-                    const uint4 vx = *reinterpret_cast<const uint4*>(v + at0), vy = *reinterpret_cast<const uint4*>(v + at1);
-                    if (VEC && rotated) turn_row(lane, cs[w], sn[w], kx, ky);
-                    put(f, slot, at0, at1, kx, ky, vx, vy);
-                }
+        if (f.n1 > 0 && !fills) {
+            if (rotated) {
+                for (int p = lane; p < half; p += 32) turn_by(turn_of(in, p), in.axis_pos[(size_t)axis_of(in, p) * in.n_tokens + f.s0], cs[w][p], sn[w][p]);
+                __syncwarp();
             }
+            if (lane < kPerRow) {
+                int at0, at1;
+                uint4 kx, ky;
+                load_row((const bf16*)in.k + row_of(f, f.n0), lane, rotated, cs[w], sn[w], at0, at1, kx, ky);
+                const bf16* v = (const bf16*)in.v + row_of(f, f.n0);
+                const uint4 vx = *reinterpret_cast<const uint4*>(v + at0), vy = *reinterpret_cast<const uint4*>(v + at1);
+                if (VEC && rotated) turn_row(lane, cs[w], sn[w], kx, ky);
+                put(f, f.n0, at0, at1, kx, ky, vx, vy);
+            }
+        }
         if (__syncthreads_or(fills))
             for (int i = 0; i < nt / 32; ++i) {
                 const Filled o = some[i];
-                const int b0 = o.n0 >> c.t_shift, b1 = o.n1 >> c.t_shift;
-                if (o.n1 <= 0 || b1 == b0) continue;
-                to_block(o, b0, false);
-                __syncthreads();  // the open rows have been read
-                to_open(o, b1 << c.t_shift);
+                if (o.n1 > 0 && o.n1 >> c.t_shift > o.n0 >> c.t_shift) to_block(o, o.n0 >> c.t_shift, false);  // its last token: nothing stays open
             }
         if (lane == 0 && f.n1 > 0) c.len[f.item] = f.n1;
     }
@@ -484,7 +482,7 @@ cudaError_t launch_block_append(const BlockView& c, const NewRows& in, cudaStrea
     const int tasks = c.T * c.D / 16, threads = min(256, tasks), per = tasks / threads, group = threads / 32;
     Shape sh;
     sh.threads = threads;
-    sh.few = in.max_chunk <= kFewTokens;
+    sh.few = in.max_chunk == 1 && c.n_items >= kManyItems;
     // blocks that a sequence's tokens can fill: all but a last one that the call leaves open
     sh.units = max(1, (int)(((long long)in.max_chunk + c.T - 1) / c.T));
     // Two heads share their angles where there are blocks enough to fill the GPU all the same.

@@ -149,3 +149,45 @@ def test_more_items_than_the_table_of_places(ctx, D, T, lists):
     none = torch.isinf(z)
     assert torch.equal(torch.isinf(lse.cpu()), none) and bool(((lse.cpu().double() - z)[~none].abs() <= b_lse[~none]).all())
     assert ctx.poll_status()[0] == 0
+
+
+@pytest.mark.parametrize("D,T,rot,pairs", [(64, 16, 64, False), (64, 16, 50, True), (128, 32, 128, False), (128, 32, 0, False), (64, 128, 32, True), (128, 16, 42, False), (64, 64, 64, True)])
+@pytest.mark.parametrize("with_q", [False, True])
+def test_single_tokens_of_many_items(ctx, D, T, rot, pairs, with_q):
+    """2048 items and more, one token each or none: a warp to an item.  Some items fill a block, some have no room, heads of a sequence
+    differ in length; and the same of fewer items, a block of threads each, leaves the same."""
+    from paper_2511_06029_b200 import binding
+    g = torch.Generator().manual_seed(D + T)
+    L, B, Hkv = 2, 147, 7
+    lens = torch.randint(0, 2 * T, (L, B, Hkv), generator=g)
+    lens[:, ::3] = lens[:, ::3, :1]
+    lens[:, 5:20] = T - 1
+    lens[1, 30, 2] = lens[0, 3, 0] = 2 * T
+    chunks = [0 if b % 11 == 4 else 1 for b in range(B)]
+    chunks[3] = chunks[30] = 1
+    n = sum(chunks)
+    st = BlockState(L, B, 2 * Hkv, Hkv, D, T, 2, lens, True, seed=T)
+    caches = [st.device_cache() for _ in range(2)]
+    q, k, v = block_rows(st, L, n, T)
+    r, kr, qr = None, k, None
+    if rot:
+        r, _ = rotary(rot, 2, n, pairs, T)
+        kr, qr = rotated(ctx, r, k.cuda()).cpu(), rotated(ctx, r, q.cuda())
+    with_q = with_q and rot > 0
+    start = starts(chunks).cuda()
+    outs = [torch.empty_like(q, device="cuda") if with_q else None for _ in range(2)]
+    ctx.block_append(caches[0], 0, L, start, 1, k.cuda(), v.cuda(), rotary=r, q=q.cuda() if with_q else None, q_out=outs[0])
+    for l in range(L):
+        ctx.block_append(caches[1], l, l + 1, start, 1, k[l:l + 1].cuda(), v[l:l + 1].cuda(), rotary=r, q=q[l:l + 1].cuda() if with_q else None,
+                         q_out=outs[1][l:l + 1] if with_q else None)
+    st.append(0, starts(chunks), kr, v)
+    for c, o in zip(caches, outs):
+        same_blocks(st, c)
+        assert o is None or torch.equal(o, qr)
+    assert ctx.poll_status()[0] == binding.ERR_CAPACITY
+    # the same without a page for the blocks that are filled next
+    caches[0].len[:] = T - 1
+    caches[0].page_table[0, :9, :, 0] = -1
+    ctx.block_append(caches[0], 0, L, start, 1, k.cuda(), v.cuda(), rotary=r)
+    assert ctx.poll_status()[0] == binding.ERR_PAGE
+    assert torch.equal(caches[0].len.cpu(), T - 1 + torch.tensor(chunks, dtype=torch.int32).view(1, B, 1).expand(L, B, Hkv))
