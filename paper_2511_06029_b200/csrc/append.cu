@@ -13,9 +13,13 @@ namespace lethe {
 namespace {
 
 constexpr int kAppendThreads = 192;
-constexpr int kFewRows = 16;   // rows per block where there are few tokens; even: K and V of an item stay together
-constexpr int kManyRows = 48;  // otherwise
+constexpr int kFewRows = 16;   // rows per block of one token; even: K and V of an item stay together
+constexpr int kManyRows = 48;  // rows per block of kManyTokens tokens
 constexpr int kManyTokens = 2;
+// Small blocks of one token, for the latency, up to this many of them; else what a block does once, the chain of loads above all, serves
+// two tokens.  Both sides (us, one token first): 768 blocks 5.8 and 6.4, 1536 blocks 8.5 and 7.1, 2304 blocks 10.6 and 8.0; single tokens of 8
+// sequences and 32 layers (768) 5.1 and 5.8, of 16 (1536) 8.0 and 6.1.
+constexpr int kManyBlocks = 1024;
 
 enum { kSame = 0, kE4m3 = 1, kE5m2 = 2 };
 
@@ -198,20 +202,21 @@ __global__ void __launch_bounds__(256) append_len_kernel(const int32_t* chunk_st
     if (n_new > 0 && n_old + (long long)n_new <= cap_tokens) len[it.item] = n_old + n_new;
 }
 
-// One token to a sequence at most, and blocks of one token: nobody else needs an item's old length.
-bool sets_len(const AppendArgs& a) { return a.in.max_chunk == 1 && a.in.n_tokens < 1024; }
+// One token to a sequence at most: nobody else needs an item's old length.  (A thread has at most one row to place.)
+static_assert(kManyRows * kManyTokens <= kAppendThreads && kFewRows <= kAppendThreads, "");
+bool sets_len(const AppendArgs& a) { return a.in.max_chunk == 1; }
 
 template <typename T, int KV>
 cudaError_t launch_t(const AppendArgs& a, cudaStream_t stream) {
     const int rows = a.nl * (2 * a.Hkv + (a.in.q ? a.Hq : 0));
     const bool vec = !a.in.axis_pos || rotation_in_pieces<T>(a.in);
-    // Few tokens: small blocks of one, for the latency.  Many: what a block does once, the chain of loads above all, serves two.
-    if (a.in.n_tokens >= 1024 && vec) {
+    const long long small = (long long)a.in.n_tokens * ((rows + kFewRows - 1) / kFewRows);
+    if (small >= kManyBlocks && vec) {
         const int blocks = (rows + kManyRows - 1) / kManyRows, per_block = ((rows + blocks - 1) / blocks + 1) & ~1;  // even
         const unsigned grid = (unsigned)((a.in.n_tokens + kManyTokens - 1) / kManyTokens) * (unsigned)((rows + per_block - 1) / per_block);
-        return launch_dependent(append_kernel<T, KV, true, kManyTokens>, dim3(grid), kAppendThreads, 0, stream, a, rows, per_block, false);
+        return launch_dependent(append_kernel<T, KV, true, kManyTokens>, dim3(grid), kAppendThreads, 0, stream, a, rows, per_block, sets_len(a));
     }
-    const unsigned grid = (unsigned)a.in.n_tokens * (unsigned)((rows + kFewRows - 1) / kFewRows);
+    const unsigned grid = (unsigned)small;
     return vec ? launch_dependent(append_kernel<T, KV, true, 1>, dim3(grid), kAppendThreads, 0, stream, a, rows, kFewRows, sets_len(a))
                : launch_dependent(append_kernel<T, KV, false, 1>, dim3(grid), kAppendThreads, 0, stream, a, rows, kFewRows, sets_len(a));
 }

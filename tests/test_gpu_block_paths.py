@@ -191,3 +191,31 @@ def test_single_tokens_of_many_items(ctx, D, T, rot, pairs, with_q):
     ctx.block_append(caches[0], 0, L, start, 1, k.cuda(), v.cuda(), rotary=r)
     assert ctx.poll_status()[0] == binding.ERR_PAGE
     assert torch.equal(caches[0].len.cpu(), T - 1 + torch.tensor(chunks, dtype=torch.int32).view(1, B, 1).expand(L, B, Hkv))
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3, torch.float32])
+@pytest.mark.parametrize("L,B,Hq,Hkv,rot", [(9, 40, 6, 3, 64), (20, 17, 1, 1, 0), (3, 600, 2, 1, 32), (16, 33, 5, 5, 42)])
+def test_append_single_tokens_of_many_rows(ctx, dtype, L, B, Hq, Hkv, rot):
+    """One token to a sequence (or none, or no room), more rows than small blocks are taken for: two tokens to a block, which sets the
+    lengths; an odd number of tokens."""
+    from paper_2511_06029_b200 import binding
+    st, cache = state_and_cache(L, B, Hq, Hkv, 64, 16, 6, dtype, 16, seed=B)
+    cache.len[L - 1, 1, 0] = 16
+    chunks = [0 if b % 5 == 2 else 1 for b in range(B)]
+    chunks[0] += (sum(chunks) + 1) % 2 and -1
+    n = sum(chunks)
+    assert n % 2
+    q, k, v = rows(L, n, Hq, Hkv, 64, dtype, seed=n)
+    pos = torch.arange(n, dtype=torch.int32)
+    r, kr = None, k
+    if rot:
+        r, _ = rotary(rot, 2, n, True)
+        kr = rotated(ctx, r, k.cuda()).cpu()
+    start = starts(chunks)
+    want = expected(st, cache, 0, start, kr, v, pos)
+    q_out = torch.empty_like(q, device="cuda") if rot else None
+    ctx.append(cache, 0, L, start.cuda(), 1, k.cuda(), v.cuda(), pos.cuda(), rotary=r, q=q.cuda() if rot else None, q_out=q_out)
+    same(cache, want)
+    if rot:
+        assert torch.equal(raw(q_out), raw(rotated(ctx, r, q.cuda())))
+    assert ctx.poll_status()[0] == binding.ERR_CAPACITY
