@@ -1427,6 +1427,7 @@ static lethe_status block_view(lethe_ctx* ctx, const lethe_block_cache* c, int l
     v->capacity = c->capacity; v->cap_tokens = c->capacity * c->block_tokens;
     v->layer_begin = layer_begin; v->nl = layer_end - layer_begin;
     v->n_items = (int)(v->nl * heads);
+    v->sm_count = ctx->sm_count;
     return LETHE_OK;
 }
 
@@ -1523,9 +1524,10 @@ lethe_status lethe_block_attend(lethe_ctx* ctx, const lethe_block_cache* c, int 
         if (!(fabsf(scale[l]) <= 1e30f)) return fail(ctx, LETHE_ERR_INVALID_ARG, "scale must be finite");
         a.c.scale_log2[l] = scale[l] * 1.4426950408889634f;
     }
-    // the line of 16-token groups is counted in 32 bits
-    const long long most = selected && n_select < c->capacity ? n_select : c->capacity;
-    if (a.c.n_items * (most * (a.c.T / 16) + 2 * (a.c.T / 16) + 4) > 0x3fffffffLL)
+    // an item's length on the line, which is counted in 32 bits: its beginning, its steps of full blocks and its open rows
+    const long long most = selected && n_select < c->capacity ? n_select : c->capacity, rows = a.c.T;
+    const long long line = kBlockPad + (most * rows + kBlockStep - 1) / kBlockStep + kBlockTail * ((rows + 31) / 32);
+    if (a.c.n_items * line > 0x3fffffffLL)
         return fail(ctx, LETHE_ERR_UNSUPPORTED, "block_attend: too many blocks for one call; cover fewer layers");
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return fail(ctx, LETHE_ERR_CUDA, "cannot select the context's device");

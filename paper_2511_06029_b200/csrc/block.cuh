@@ -51,7 +51,7 @@ struct BlockView {
     int32_t* status;
     long long n_pages;          // blocks that exist: pages, or items * capacity
     int B, Hq, Hkv, G, D, T, t_shift, capacity, cap_tokens;
-    int layer_begin, nl, n_items;
+    int layer_begin, nl, n_items, sm_count;
     float scale_log2[kMaxLayers];  // lethe_block_attend: softmax scale per absolute layer, in log2 units
 };
 

@@ -32,9 +32,7 @@ namespace lethe {
 namespace {
 
 constexpr int kThreads = kBlockWarps * 32;
-constexpr int kStep = 32;       // tokens of a step
-constexpr int kTailWeight = 3;  // length on the line of 32 open rows, which are fetched without a ring
-constexpr int kPad = 3;         // and of an item's beginning: its length, first pages, queries and first tile come one after the other
+constexpr int kStep = kBlockStep, kTailWeight = kBlockTail, kPad = kBlockPad;
 constexpr int kLine = 2048;     // items whose places on the line are kept in shared memory; of more, only every so many-th is
 constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
 constexpr float kLift = 9.f;    // p' is kept up by this (log2)
@@ -583,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 put = put + 1 == NS ? 0 : put + 1;
             };
 
-            // queries: whole numbers below 2^20, in three digits, in the order of the key codes
+            // queries: whole numbers of up to 2^20 either way (21 bits), in three digits, in the order of the key codes
             uint32_t qf[3][4 * C];
             float scale2[2], open2[2];
             int queued = min(g1, g0 + NS);

@@ -7,10 +7,13 @@
 namespace lethe {
 
 constexpr int kBlockWarps = 8;  // warps of a CTA, each with a ring of its own; one CTA per SM
-constexpr int kBlockStages = 2;  // steps of 32 tokens in a ring at D = 128
+constexpr int kBlockStep = 32;  // tokens of a step
+constexpr int kBlockTail = 3;   // length on the line of 32 open rows, which are fetched without a ring
+constexpr int kBlockPad = 3;    // and of an item's beginning: its length, first pages, queries and first tile come one after the other
+constexpr int kBlockStages = 2;  // steps in a ring at D = 128
 
 struct alignas(64) BlockMaps {
-    CUtensorMap k, v;  // [blocks * block_tokens][D] bytes, boxes of 16 rows
+    CUtensorMap k, v;  // [blocks * block_tokens][D] bytes, boxes of a step's rows, or of a block's where those are fewer
 };
 
 struct BlockAttendArgs {

@@ -219,3 +219,27 @@ def test_append_single_tokens_of_many_rows(ctx, dtype, L, B, Hq, Hkv, rot):
     if rot:
         assert torch.equal(raw(q_out), raw(rotated(ctx, r, q.cuda())))
     assert ctx.poll_status()[0] == binding.ERR_CAPACITY
+
+
+def test_attend_takes_what_its_line_holds(ctx):
+    """Long page tables of empty items: refused where the line of 32-token steps no longer fits 32 bits, not before.  (Nothing is read of
+    the tables: all lengths are zero.)"""
+    import ctypes
+    from paper_2511_06029_b200 import binding
+    st = BlockState(3, 2, 2, 2, 64, 128, 1, 0, True, seed=1)
+    cache = st.device_cache(with_range=False)
+    q = torch.ones((3, 6, 2, 64), dtype=torch.bfloat16, device="cuda")     # room for six sequences
+    out = torch.ones_like(q)
+    scale = (ctypes.c_float * 3)(0.1, 0.1, 0.1)
+    c = binding.lethe_block_cache.from_buffer_copy(cache.c)
+
+    def attend():
+        return ctx.lib.lethe_block_attend(ctx.h, ctypes.byref(c), 0, 3, q.data_ptr(), scale, None, 0, out.data_ptr(), None, None)
+
+    c.capacity = 2 ** 24 - 1                                   # 12 items: 12 x (2^24 x 4 + ..) < 2^30
+    assert attend() == 0
+    torch.cuda.synchronize()
+    assert not bool(out.view(-1)[:3 * 2 * 2 * 64].any()) and ctx.poll_status()[0] == 0
+    wide = torch.zeros((3, 6, 2), dtype=torch.int32, device="cuda")
+    c.batch, c.len = 6, wide.data_ptr()                        # 36 items
+    assert attend() == binding.ERR_UNSUPPORTED
