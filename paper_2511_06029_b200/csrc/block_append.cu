@@ -12,7 +12,9 @@ namespace {
 
 using bf16 = __nv_bfloat16;
 constexpr int kQueryRows = 16, kManyQueryRows = 32, kQueryTokens = 2;
-constexpr int kPlenty = 1184;  // blocks to fill: eight for each of 148 SMs
+// Blocks to fill for each SM from which two heads share their angles.  Both sides at D = 128 (us, a head each first): 5.1 for each (752 in all)
+// 21.5 and 23.7 with queries, 16.0 and 16.7 without; 8.2 35.2 and 34.3, 20.8 and 19.1; 13.9 54 and 51, 30 and 24; 27 98 and 90, 56 and 45.
+constexpr int kPlenty = 8;
 // Single tokens of this many items and more have a warp to an item, others a block of threads.  A warp's row is the cheaper one, a
 // sequence that fills blocks the dearer one, since its heads' warps lie together.  On average over the steps of sequences in blocks of 32:
 // 64 items 7 us with warps and 4.5 with blocks, 2048 items 10.4 and 10.2, 16384 items 42 and 54 (without a full block 6.7 and 9.4 of 2048
@@ -485,9 +487,8 @@ cudaError_t launch_block_append(const BlockView& c, const NewRows& in, cudaStrea
     sh.few = in.max_chunk == 1 && c.n_items >= kManyItems;
     // blocks that a sequence's tokens can fill: all but a last one that the call leaves open
     sh.units = max(1, (int)(((long long)in.max_chunk + c.T - 1) / c.T));
-    // Two heads share their angles where there are blocks enough to fill the GPU all the same.
     const long long to_fill = (long long)c.nl * c.Hkv * (in.n_tokens / c.T + c.B);
-    sh.heads = to_fill >= kPlenty ? 2 : 1;
+    sh.heads = to_fill >= (long long)kPlenty * c.sm_count ? 2 : 1;
     sh.kv_blocks = sh.few ? (unsigned)((c.n_items + group - 1) / group) : (unsigned)c.nl * c.B * ((c.Hkv + sh.heads - 1) / sh.heads) * sh.units;
     const int q_tok = sh.few ? 1 : kQueryTokens, q_rows = sh.few ? kQueryRows : kManyQueryRows;
     sh.grid = sh.kv_blocks + (in.q ? (unsigned)((in.n_tokens + q_tok - 1) / q_tok) * (unsigned)((c.nl * c.Hq + q_rows - 1) / q_rows) : 0);
