@@ -243,3 +243,20 @@ def test_attend_takes_what_its_line_holds(ctx):
     wide = torch.zeros((3, 6, 2), dtype=torch.int32, device="cuda")
     c.batch, c.len = 6, wide.data_ptr()                        # 36 items
     assert attend() == binding.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("B,chunk", [(3, 45), (300, 1), (40, 2)])
+def test_appends_without_ranges_and_in_place(ctx, B, chunk):
+    """A cache from which nothing is selected has no ranges; queries rotated where they lie.  As with ranges and apart."""
+    L, Hkv, D, T = 2, 4, 64, 16
+    st = BlockState(L, B, 2 * Hkv, Hkv, D, T, chunk // T + 3, torch.randint(0, 2 * T, (L, B, Hkv), generator=torch.Generator().manual_seed(B)), False, seed=B)
+    n = B * chunk
+    q, k, v = (x.cuda() for x in block_rows(st, L, n, B))
+    r, _ = rotary(64, 2, n, False, B)
+    kr, qr = rotated(ctx, r, k).cpu(), rotated(ctx, r, q)
+    cache = st.device_cache(with_range=False)
+    ctx.block_append(cache, 0, L, starts([chunk] * B).cuda(), chunk, k, v, rotary=r, q=q, q_out=q)
+    st.append(0, starts([chunk] * B), kr, v.cpu())
+    cache.k_range = st.k_range.cuda()     # not the call's business
+    same_blocks(st, cache)
+    assert torch.equal(q, qr) and ctx.poll_status()[0] == 0
