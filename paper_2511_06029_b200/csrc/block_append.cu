@@ -1,8 +1,8 @@
 // lethe_block_append and lethe_block_read: filling a cache in 8 bits with a scale for each block of tokens, and reading it back.
-// Measured (Llama-8B heads): a prompt of 8205 tokens, 184 MB, 43 us for the append = 4.3 TB/s; with the queries in a launch of their own 29 + 30
+// Measured (Llama-8B heads): a prompt of 8205 tokens, 184 MB, 45 us for the append = 4.1 TB/s; with the queries in a launch of their own 29 + 30
 // us, since filling blocks is a chain of short steps (rows, angles, magnitude, codes, range) that a few resident blocks of threads go
-// through at 1.7 TB/s: now the queries' stream runs beside it.  Two heads to a block of threads against one and four: 74, 77 and 77 us for a
-// prompt with its reading back, before that.  Single tokens of 8 sequences and 32 layers: 7 us, 23 where one of them fills blocks.
+// through at 1.7 TB/s: now the queries' stream runs beside it.  Single tokens of 8 sequences and 32 layers: 5 us, 22 where one of them fills
+// blocks.  Reading 34 MB of rows back 9 us, 13 where the codes come from memory.
 #include "block.cuh"
 
 namespace lethe {

@@ -17,10 +17,10 @@
 // probabilities in two terms.  Stretches whose value scales leave the range that one m can serve, or whose open rows overflow, are done once
 // more by far_stretch, plainly.
 //
-// Measured (us): a step of the Llama-8B shape, 571 MB, 101 = 5.7 TB/s, 0.86 of the copy rate; one sequence of 131072 tokens, 268 MB, 48 = 0.85;
-// a ragged batch in blocks of 16 61 = 0.80; one layer of the first 13 (3.5 until the first tiles are asked for, 2 to 5 for two or three steps
-// a warp, 4 for the merges).  8 warps with two tiles each: the more is in flight the further apart the warps of an SM end (16 warps of
-// three 16-token tiles: 78 to 105 us, 113 in all; 12 of two: 83 to 95, 105), and fewer warps leave no time for a conversion of the keys,
+// Measured (us, calls captured in a graph): a step of the Llama-8B shape, 571 MB, 102 = 5.6 TB/s, 0.86 of the copy rate; one sequence of 131072
+// tokens, 268 MB, 51 = 0.81; a ragged batch in blocks of 16 62 = 0.79; one layer of the first 13 (3.5 until the first tiles are asked for, 2 to 5
+// for two or three steps a warp, 4 for the merges).  8 warps with two tiles each: the more is in flight the further apart the warps of an SM end
+// (16 warps of three 16-token tiles: 78 to 105 us, 113 in all; 12 of two: 83 to 95, 105), and fewer warps leave no time for a conversion of the keys,
 // which is why the logits come from the codes (f16 keys on 8 warps: 124).  Letting warps that are ahead wait for the others: 155.
 #include <string.h>
 
@@ -37,7 +37,8 @@ constexpr int kLine = 2048;     // items whose places on the line are kept in sh
 constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
 constexpr float kLift = 9.f;    // p' is kept up by this (log2)
 // Value scales that a stretch takes with one m: up to 2^40 either side of the first of them, which lies between 2^-40 and 2^60.  The sum
-// of p' / vs lies between 2^-31 and 2^72 then, with 2^17 tokens, and O, up to 2^39, stays in fp32 with that and the scale as factors.
+// of p' / vs lies between 2^-31 and 2^72 then, with 2^17 tokens (2^82 with open rows, whose scale is 1), and O, up to 2^39 from full blocks, stays
+// in fp32 with that and the scale as factors.
 constexpr float kFar = 0x1p40f, kLeastRef = 0x1p-40f, kMostRef = 0x1p60f;
 constexpr float kZeroLog2 = -40.f;  // where a block of zeros, which only the sum of probabilities knows, counts for m
 
@@ -444,8 +445,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
         __syncthreads();
     }
     const long long total = sm.prefix[kThreads];
-    // Warps in use: at least two steps each (or an item's beginning), as far as there are.  Few short items behind a selection take 21.2 us with
-    // two, 21.5 with one, 22.8 with three and 23.8 with four.
+    // Warps in use: at least two steps each (or an item's beginning), as far as there are.  Over seven calls behind a selection, 10 to 23 us: with
+    // one 1.3 less to 0.5 more, with three 0.1 less to 1.5 more, with four 0.2 less to 2.5 more.
     const long long warps = min((long long)a.n_cta * kBlockWarps, (total + 1) / 2);
     if ((long long)blockIdx.x * kBlockWarps >= warps) return;
     auto cta_at = [&](int pos) { return (int)(((pos + 1LL) * warps - 1) / total) / kBlockWarps; };

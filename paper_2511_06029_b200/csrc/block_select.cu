@@ -5,9 +5,9 @@
 // block costs 2 D multiplications whatever G is.  Whole numbers: |up|, |down| <= 8 * 127 fit 16 bits, the sum stays below 2^24.
 // Bound by memory: 2 D bytes for each block.  The blocks of an item are split over several thread blocks; the last of them to finish
 // selects: the n-th greatest key by histograms over a narrowing range, then one ordered pass.
-// Measured: 64 items of 1024 blocks, 17 MB, about 10 us, of which 4 until the scores are there, 1 for the arrival and 4 for choosing 64 of them
-// (three ranges, five barriers each): a launch's chain of latencies, not the bytes (2.6 us).  Four blocks of a lane in flight
-// instead of two take 73 registers and with them a second wave: 2.5 us more.
+// Measured: 64 items of 1024 blocks, 17 MB, 11 us (13.5 with inputs that come from memory), of which 4 until the scores are there, 1 for the
+// arrival and 4 for choosing 64 of them (three ranges, five barriers each): a launch's chain of latencies, not the bytes (2.6 us).  Four
+// blocks of a lane in flight instead of two take 73 registers and with them a second wave: 2.5 us more.
 #include "block.cuh"
 
 namespace lethe {
