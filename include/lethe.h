@@ -515,8 +515,9 @@ lethe_status lethe_block_select(lethe_ctx *ctx, const lethe_block_cache *cache, 
  * (LETHE_ERR_PAGE).  Sums, softmax statistics and outputs are held in fp32.  Over full blocks a query row takes part as whole numbers of
  * 21 bits relative to its largest element (their products with the stored numbers are summed exactly) and the probabilities are rounded
  * to f16; over open rows the query takes part as it is and the probabilities in two bf16 terms.  A query row with a NaN or an infinity
- * gives NaN; an open row's value that is not finite makes its element of out not finite.  Values of any size are taken; where an
- * item's value scales are more than 2^40 apart or not between 2^-40 and 2^60, or open values overflow, at a thirtieth of
+ * gives NaN; an open row's value that is not finite makes its element of out not finite.  Values of any size are taken: an
+ * item's value scales up to 2^40 apart between 2^-50 and 2^60, and up to 2^10 beyond, as far as 2^-96 and 2^90, in one go, others (a block of
+ * zeros among scales below 2^-50 too) and open values whose sums overflow at a thirtieth of
  * the speed.  Scratch: 32 bytes per item and 1.3 MB of partial results.  The same inputs give the same bits.
  */
 lethe_status lethe_block_attend(lethe_ctx *ctx, const lethe_block_cache *cache, int layer_begin, int layer_end, const void *q,

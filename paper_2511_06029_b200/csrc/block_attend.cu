@@ -36,10 +36,11 @@ constexpr int kStep = kBlockStep, kTailWeight = kBlockTail, kPad = kBlockPad;
 constexpr int kLine = 2048;     // items whose places on the line are kept in shared memory; of more, only every so many-th is
 constexpr float kLazy = 6.f;    // how far (log2) a logit may lie above m
 constexpr float kLift = 9.f;    // p' is kept up by this (log2)
-// Value scales that a stretch takes with one m: up to 2^40 either side of the first of them, which lies between 2^-40 and 2^60.  The sum
-// of p' / vs lies between 2^-31 and 2^72 then, with 2^17 tokens (2^82 with open rows, whose scale is 1), and O, up to 2^39 from full blocks, stays
-// in fp32 with that and the scale as factors.
-constexpr float kFar = 0x1p40f, kLeastRef = 0x1p-40f, kMostRef = 0x1p60f;
+// Value scales that a stretch takes with one m: up to 2^40 either side of the first of them, r.  The sum of p' / vs lies between 2^-31 and 2^72
+// then, with 2^17 tokens, and with open rows, of scale 1, it may come down to 2^9 r or up to 2^22 r.  What has the largest scale sets m, so the
+// smallest one is 2^90 below it at most where r lies between 2^-50 and 2^60: shares of less than 2^-35 of the largest vanish.  Beyond, r may
+// be 2^-96 to 2^90, but scales only 2^10 further out (no block of zeros below 2^-50), 2^106 in all: shares of less than 2^-20 vanish.
+constexpr float kFar = 0x1p40f, kFarther = 0x1p10f, kLowRef = 0x1p-50f, kHighRef = 0x1p60f, kLeastRef = 0x1p-96f, kMostRef = 0x1p90f;
 constexpr float kZeroLog2 = -40.f;  // where a block of zeros, which only the sum of probabilities knows, counts for m
 
 template <int D>
@@ -168,6 +169,11 @@ struct Acc {
 
 // The root of exp2(a - b): a part that is 2^228 times as large as another may count for as much with a weight as small as that.
 __device__ __forceinline__ float root_diff(float a, float b) { return a == -INFINITY ? 0.f : fast_exp2(0.5f * (a - b)); }
+// A share of a sum, root x rest, as two factors: itself and 1, or the two where fp32 does not hold it.
+__device__ __forceinline__ float2 share_of(float root, float rest) {
+    const float share = root * rest;
+    return share < 0x1p-100f ? make_float2(root, rest) : make_float2(share, 1.f);
+}
 
 // Tokens of an item for values of any size: full blocks of the steps g0 .. g1 - 1 and open rows r0 .. r1 - 1, a warp, a token at a time with
 // D / 32 elements to a lane.  Leaves m, l (weight l 2^m) and O / l of each head in shared memory, or, with part = NULL, the item's output.
@@ -544,7 +550,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     }
                 }
                 const float rel = ask_vs * inv_ref;
-                far = far || __any_sync(0xffffffffu, ask_vs > 0.f && (rel > kFar || rel < 1.f / kFar));
+                const bool low = v_ref < kLowRef;
+                const float least = low ? 1.f / kFarther : 1.f / kFar, most = v_ref > kHighRef ? kFarther : kFar;
+                far = far || __any_sync(0xffffffffu, ask_page >= 0 && (rel > most || rel < (ask_vs > 0.f || low ? least : 0.f)));
                 lv = ask_page < 0 ? -INFINITY : ask_vs == 0.f ? kZeroLog2 : __log2f(rel);  // no block: no weight
                 iv = ask_vs == 0.f ? -kFar : __fdividef(1.f, rel);
             };
@@ -746,16 +754,17 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                 acc.l[1] += __shfl_xor_sync(0xffffffffu, acc.l[1], s);
             }
             // What leaves the stretch is divided by its sum: a mean of values is as large as they are, and a part's weight is its sum.
+            const float lift = v_ref < kLowRef ? 0x1p64f : 1.f, drop = v_ref < kLowRef ? 0x1p-64f : 1.f;  // the factor itself must not vanish
             float top[2], all = 0.f;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const float f = acc.l[k] == 0.f ? 0.f : __fdividef(v_ref, acc.l[k]);
+                const float f = acc.l[k] == 0.f ? 0.f : __fdividef(v_ref * lift, acc.l[k]);
                 top[k] = acc.l[k] == 0.f ? -INFINITY : acc.m[k] - kLift;
                 float sizes = 0.f;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    acc.o[i][k] *= f;
-                    acc.o[i][2 + k] *= f;
+                    acc.o[i][k] = acc.o[i][k] * f * drop;
+                    acc.o[i][2 + k] = acc.o[i][2 + k] * f * drop;
                     sizes += fabsf(acc.o[i][k]) + fabsf(acc.o[i][2 + k]);
                 }
                 if (acc.l[k] < INFINITY) all += sizes;  // a query that is not finite has a sum that is not, and gives NaN either way
@@ -839,7 +848,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             l = mine_l * half;
 #pragma unroll
             for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-            const float f = l == 0.f ? 0.f : __fdividef(mine_l, l);  // a part's share of the sum is half x f
+            const float2 share = share_of(half, l == 0.f ? 0.f : __fdividef(mine_l, l));  // a part's, of the sum
             float o[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -847,9 +856,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
             for (unsigned k = chain; k; k &= k - 1) {
                 const int r = __ffs(k) - 1;
                 const float* src = (r & 1 ? reinterpret_cast<const float*>(sm.ring[r >> 1]) : sm.first[r >> 1]) + head * D + E * lane;
-                const float hr = __shfl_sync(0xffffffffu, half, r), fr = __shfl_sync(0xffffffffu, f, r);
+                const float sx = __shfl_sync(0xffffffffu, share.x, r), sy = __shfl_sync(0xffffffffu, share.y, r);
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = fmaf(src[e] * hr, fr, o[e]);
+                for (int e = 0; e < E; ++e) o[e] = fmaf(src[e] * sx, sy, o[e]);
             }
             if (!whole) {
                 // the item goes on in other CTAs: the last of them to come here merges
@@ -903,18 +912,18 @@ __global__ void __launch_bounds__(kThreads, 1) block_attend_kernel(const __grid_
                     for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
                     l = fmaf(old, old_half, sum);
                     m = nm;
-                    const float inv = l == 0.f ? 0.f : __fdividef(1.f, l), f = old * inv, g = mine * inv;
+                    const float2 was = share_of(old_half, l == 0.f ? 0.f : __fdividef(old, l)), is = share_of(half, l == 0.f ? 0.f : __fdividef(mine, l));
 #pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] = o[e] * old_half * f;
+                    for (int e = 0; e < E; ++e) o[e] = o[e] * was.x * was.y;
 #pragma unroll 1
                     for (int k0 = 0; k0 < n; k0 += U) {
                         if (k0) ask(k0);
 #pragma unroll
                         for (int u = 0; u < U; ++u) {
-                            const float hk = __shfl_sync(0xffffffffu, half, (k0 + u) & 31), gk = __shfl_sync(0xffffffffu, g, (k0 + u) & 31);
+                            const float sx = __shfl_sync(0xffffffffu, is.x, (k0 + u) & 31), sy = __shfl_sync(0xffffffffu, is.y, (k0 + u) & 31);
                             if (k0 + u >= n) continue;
 #pragma unroll
-                            for (int e = 0; e < E; ++e) o[e] = fmaf(x[u][e] * hk, gk, o[e]);
+                            for (int e = 0; e < E; ++e) o[e] = fmaf(x[u][e] * sx, sy, o[e]);
                         }
                     }
                 }

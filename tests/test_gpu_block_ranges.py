@@ -114,7 +114,7 @@ def unseen(st, q, scale):
     scale, for each token and |x|, the largest open value.
 
     Values of zero have a share but no size, and nothing says against what they should be held.  Full blocks of zeros count among the
-    shares like blocks of 2^-40 of the reference r, the first scale (1 where there is none, 2^60 at most), open rows of zeros like others,
+    shares like blocks of 2^-40 of the reference r, the first scale (1 where there is none, 2^90 at most), open rows of zeros like others,
     that is like blocks of scale 1; a factor of 2^6 is how far m may lag.  What they outweigh so far that it leaves fp32 vanishes:
         full blocks before open zeros, rescaled:  p vs < p0 2^-126 2^6, times 127            -> p0 2^-113
         full blocks before full zeros, rescaled:  p vs < p0 2^-126 2^6 2^-40 r, times 127    -> p0 2^-153 r
@@ -129,7 +129,7 @@ def unseen(st, q, scale):
                 n, hs = int(st.len[li, b, h]) // st.T, slice(h * st.G, (h + 1) * st.G)
                 p = torch.softmax(q[li, b, hs].double() @ K.T * scale, 1)
                 scales, largest = st.v_scale[li, b, h, :n].double(), V[n * st.T:].abs().amax(1)
-                r = max([1.0] + [min(float(x), 2.0 ** 60) for x in scales])
+                r = max([1.0] + [min(float(x), 2.0 ** 90) for x in scales])
                 size = torch.cat([torch.where(scales == 0, r * 2.0 ** -40, scales).repeat_interleave(st.T), largest / 64])
                 room[li, b, hs, 0] = (p * size).amax(1) * 127 * n * st.T * 2.0 ** -34
                 if len(largest) and n:
